@@ -26,7 +26,7 @@ EPS = 1e-5                                   # layer norm
 LR, BETA1, BETA2, ADAM_EPS, DECAY = 1e-3, 0.9, 0.999, 1e-8, 0.01
 MAX_NORM = 1.0
 STATE_BLOCK = 128                            # elements that share a scale where states are held in 8 bits
-CHUNK = 128                                  # time steps between two states that a backward pass starts from
+CHUNK = 64                                   # time steps between two states that a backward pass starts from
 E4M3_MAX, TINY = 448.0, 2.0 ** -110          # a block whose largest value is below TINY is held as zeros
 
 
