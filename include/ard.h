@@ -677,6 +677,112 @@ ard_status ard_lstm_gates_bwd(ard_ctx* ctx, const ard_pattern* pat, ard_dtype dz
                               const float* dh, int lddh, int dh_scatter, float* dc_inout, void* dZ, int ldz_gate,
                               void* cuda_stream);
 
+/* ---- layer norm ------------------------------------------------------------------------------
+ * (Not in the paper: what stands between the layers of a deeper stack.)  For every row x of X [rows][N]:
+ *   mean = sum x / n,  rstd = 1 / sqrt(sum (x - mean)^2 / n + eps),  y = (x - mean) * rstd * weight + bias.
+ * pat NULL: n = N, all columns.  pat (a row pattern over N units): X, Y, dX, dY are COMPACT over its kept units, as
+ * ard_layer_fwd leaves activations (column j = kept unit j, leading dimensions >= N so that any pattern fits), the
+ * statistics are those of the n kept columns, weight and bias are full width and read at the kept units.  Columns >= n
+ * are neither read as values nor written.
+ * X, Y of element type `dtype`, any alignment (16-byte aligned pointers and rows are read and written in 16-byte
+ * pieces); weight, bias fp32 [N], NULL: 1 and 0; mean, rstd fp32 [rows], what the backward call needs, may be NULL when
+ * there is none.  Statistics and sums are fp32.  Y must not overlap X.
+ * Errors: ARD_ERR_INVALID_ARG (NULL, negative size, dtype, eps negative or not finite, tile pattern, another context's
+ * pattern), ARD_ERR_SHAPE (N differs from the pattern's, leading dimension below N), ARD_ERR_UNSUPPORTED (more than
+ * 2^30 rows; backward: N above 4 million).  Asynchronous. */
+ard_status ard_layer_norm_fwd(ard_ctx* ctx, const ard_pattern* pat, ard_dtype dtype, int rows, int N, float eps, const void* X,
+                              int ldx, const float* weight, const float* bias, void* Y, int ldy, float* mean, float* rstd,
+                              void* cuda_stream);
+/* Its adjoint.  With xh = (x - mean) * rstd and e = dy * weight:
+ *   dX = rstd * (e - sum e / n - xh * sum (e * xh) / n),  dweight = sum over rows of dy * xh,  dbias = sum over rows of dy.
+ * dX NULL: not wanted.  dweight and dbias fp32 [N], full width; either may be NULL; with a pattern their entries at
+ * dropped units are zeroed if zero_fill_dropped != 0, else left.  Rows are added in a fixed order: the same inputs give
+ * the same bits.  dX must not overlap X or dY.  Uses the context's scratch.  Asynchronous. */
+ard_status ard_layer_norm_bwd(ard_ctx* ctx, const ard_pattern* pat, ard_dtype dtype, int rows, int N, const void* dY, int lddy,
+                              const void* X, int ldx, const float* weight, const float* mean, const float* rstd, void* dX,
+                              int lddx, float* dweight, float* dbias, int zero_fill_dropped, void* cuda_stream);
+
+/* ---- gated linear recurrence -----------------------------------------------------------------
+ * (Not in the paper: a recurrent layer beside the LSTM whose gates see the input alone, so that all steps' gates come
+ * from products over T * B rows and what is left along the time axis is a scan.)  For t = 0 .. T-1, every sequence b
+ * and unit j, with s the logistic function:
+ *   f = s(Zf[t][b][j]),  c_t = f * c_{t-1} + (1 - f) * Zg[t][b][j],  Y[t][b][j] = alpha * s(Zo[t][b][j]) * c_t
+ * (Zo NULL: Y = alpha * c_t).  Zf, Zg, Zo are pre-activations in [T*B] rows with leading dimension ldz: three matrices,
+ * or the gate blocks of one.  pat NULL: j < H.  pat (a row pattern over H units, Sec. 7: one pattern for all steps):
+ * the matrices are COMPACT over the kept units (column j = kept unit j, leading dimensions >= H), columns >= n are
+ * neither read as values nor written; alpha is the rescale of the dropout.
+ *   lens  int32 [B] or NULL: sequence b has min(max(lens[b], 0), T) steps.  Rows behind its end are not read; in Y they
+ *         are written as zero, and the state stays what it was.
+ *   h0    fp32 [B][H] full width, the state before the first step; NULL: zero.
+ *   hT    fp32 [B][H] full width, the state after the last step, or NULL; entries of dropped units are left.  May be h0.
+ *   S     fp32 [ceil(T / ARD_GLR_CHUNK)][B][H], what the backward call starts from, or NULL when there is none.
+ * Decoding is T = 1 with hT = h0.  A gate of -infinity (f = 0) starts anew: a finite past does not enter, in either call.
+ * Z, Y of element type `dtype`, any alignment (columns on a grid of two elements are read in pairs); gates, states and
+ * sums are fp32.  Y must not overlap an input.
+ * Errors: as ard_layer_norm_fwd (H and T in the place of N and rows).  Asynchronous. */
+#define ARD_GLR_CHUNK 64
+ard_status ard_glr_forward(ard_ctx* ctx, const ard_pattern* pat, ard_dtype dtype, int T, int B, int H, float alpha,
+                           const void* Zf, const void* Zg, const void* Zo, int ldz, const int32_t* lens, const float* h0,
+                           void* Y, int ldy, float* hT, float* S, void* cuda_stream);
+/* Its adjoint: with q = dhT behind the last step, for t = T-1 .. 0
+ *   d = alpha * s(Zo) * dY + q,  dZo = alpha * dY * c_t * s(Zo) (1 - s(Zo)),  dZf = d * (c_{t-1} - Zg) * f * (1 - f),
+ *   dZg = d * (1 - f),  q = f * d,
+ * and dh0 = q in the end.  The states c are computed again from S, in fp32; Y is not needed.  dZf, dZg, dZo (rows of
+ * lddz) have the layout of Z; all three are written, rows behind a sequence's end as zero (a product that adds over all rows
+ * takes them as they are); dZo goes with Zo.  dhT, dh0 fp32 [B][H] full width, either may be NULL (zero; not wanted);
+ * entries of dropped units are left; dh0 may be dhT.  Gradients must not overlap an input.  Asynchronous. */
+ard_status ard_glr_backward(ard_ctx* ctx, const ard_pattern* pat, ard_dtype dtype, int T, int B, int H, float alpha,
+                            const void* Zf, const void* Zg, const void* Zo, int ldz, const int32_t* lens, const float* S,
+                            const void* dY, int lddy, const float* dhT, void* dZf, void* dZg, void* dZo, int lddz,
+                            float* dh0, void* cuda_stream);
+
+/* ---- optimiser -------------------------------------------------------------------------------
+ * (Not in the paper: what a training loop does with the gradients of ard_mlp_step and the other backward calls.) */
+typedef struct ard_adamw_tensor {
+  int64_t rows, cols;   /* the parameter is a matrix, or a vector with rows = 1                                       */
+  float* p;             /* [rows][cols] the parameter in fp32, leading dimension ldp                                  */
+  int64_t ldp;
+  const void* g;        /* [rows][cols] its gradient, element type g_dtype, leading dimension ldg                     */
+  int64_t ldg;
+  int g_dtype;          /* ARD_F32 or ARD_BF16                                                                        */
+  void* w;              /* [rows][cols] bf16 copy of the parameter for the products, leading dimension ldw, or NULL   */
+  int64_t ldw;
+  void* m;              /* the two states, rows * cols elements one after the other (element r * cols + c): fp32, or  */
+  void* v;              /*   8 bits (see below)                                                                       */
+  float* m_scale;       /* 8-bit states: one fp32 per ARD_ADAMW_BLOCK elements; not used otherwise                    */
+  float* v_scale;
+  double weight_decay;
+} ard_adamw_tensor;
+#define ARD_ADAMW_BLOCK 128
+/* One AdamW step over n tensors (HOST array, read before the call returns; its pointers are DEVICE pointers).  With
+ * g' = *grad_factor * g, lr' = lr * *lr_factor and t = step + *step_counter:
+ *   m = beta1 m + (1 - beta1) g',  v = beta2 v + (1 - beta2) g'^2,
+ *   p = p - lr' * (weight_decay * p + m / (1 - beta1^t) / (sqrt(v / (1 - beta2^t)) + eps)),  w = p rounded to bf16.
+ *   step_counter (DEVICE uint64), lr_factor, grad_factor (DEVICE float) are read when the kernel runs, so that a step
+ *   captured into a CUDA graph follows them; each may be NULL (0, 1, 1).  t counts from 1: with t = 0 nothing is done.
+ *   A grad_factor that is not finite (what ard_grad_norm writes for gradients that are not) leaves everything as it was.
+ * state_bits 32: m, v fp32.  state_bits 8: m and r = sqrt(v) as 8-bit floats (e4m3, one byte each), times the scale of
+ * their block of ARD_ADAMW_BLOCK elements, which is the block's largest value / 448.  They are rounded up or down at
+ * random with the mean kept: with beta2 = 0.999 the root moves by 0.05 % a step where neighbouring values are 6 to 12 % apart,
+ * and rounding to nearest would never let it move.  The random numbers are Philox4x32-10 with key `seed` and counter
+ * (t low, t high, element / 4, 1 + number of the tensor):
+ * word element % 4, its low half for m, its high half for r.  A root that is not zero is held as no less than the
+ * smallest 8-bit value; a block whose largest value is below 2^-110 as zeros.  All arithmetic is fp32 on the values
+ * before rounding.  States begin as zeros (bytes and scales).
+ * Tensors must not overlap one another.  Any alignment (16-byte aligned tensors without gaps between rows are read and
+ * written in 16-byte pieces).  Errors: ARD_ERR_INVALID_ARG (NULL, negative size, dtype, state_bits, beta outside [0, 1), lr, eps or
+ * weight_decay negative or not finite), ARD_ERR_SHAPE (leading dimension below cols, more than 2^34 elements).
+ * Nothing is launched unless all tensors are valid.  Asynchronous. */
+ard_status ard_adamw_step(ard_ctx* ctx, const ard_adamw_tensor* tensors, int n_tensors, double lr, double beta1, double beta2,
+                          double eps, int state_bits, uint64_t seed, uint64_t step, const uint64_t* step_counter,
+                          const float* lr_factor, const float* grad_factor, void* cuda_stream);
+/* The 2-norm over all gradients of the same table (only rows, cols, g, ldg, g_dtype are looked at), squares and sums in
+ * fp64 in a fixed order: out[0] = norm (DEVICE float[2]), out[1] = min(1, max_norm / (norm + 1e-6)), or NaN where the norm is not
+ * finite: the grad_factor of ard_adamw_step.  max_norm <= 0: out[1] = 1 unless the norm is not finite.  Uses the
+ * context's scratch.  Asynchronous. */
+ard_status ard_grad_norm(ard_ctx* ctx, const ard_adamw_tensor* tensors, int n_tensors, double max_norm, float* out,
+                         void* cuda_stream);
+
 /* ---- status ---------------------------------------------------------------------------------- */
 
 /* Synchronises `cuda_stream`, returns the sticky device status word (ARD_OK if no kernel reported

@@ -30,6 +30,11 @@ Pins (each lives in tests/test_oracle_*.py):
                            adjoint identities
   schedule.*               Eq. 12 == the library's skew-normal density, integrates to one; Eq. 13-14 by numerical
                            integration; shape 0 == normal; prescribed mean of the scaled curve; one maximum
+  layer_norm.*             torch's layer norm (fp64), forward and autograd gradients; central differences
+  glr.*                    torch autograd (fp64) on the recurrence written with library ops; central differences; a padded sequence ==
+                           the sequence alone; a sequence cut in two with its state handed on == the whole
+  adamw.*                  torch.optim.AdamW (fp64) over several steps; the generator's known answers (pattern.philox4x32_10); every
+                           8-bit float is its own rounding, the neighbours are those of torch.float8_e4m3fn, the mean is kept
   search.*                 gradient vs central differences; stationary points lie in the Gibbs family
                            ln k_i = beta (i-1)/i + c with beta = -2 (k.p_u - p)/lambda; small-lambda limit ==
                            the maximum-entropy distribution at rate p; Eq. 2-3 in exact rationals

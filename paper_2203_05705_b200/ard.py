@@ -29,6 +29,7 @@ ARD_PATH_AUTO, ARD_PATH_CUDA_CORE, ARD_PATH_TENSOR_CORE = 0, 1, 2
 (ARD_OPT_PDL, ARD_OPT_PDL_IN_CAPTURE, ARD_OPT_SIDE_STREAMS, ARD_OPT_CTA_PAIRS, ARD_OPT_BAND_ROWS,
  ARD_OPT_MLP_PERSISTENT, ARD_OPT_LSTM_COMPACT_H, ARD_OPT_LSTM_REFUSE) = range(8)
 ARD_STATIC_SCRATCH_BYTES = 8 << 20
+ARD_GLR_CHUNK, ARD_ADAMW_BLOCK = 64, 128
 
 EXPORTS = [
     "ard_create", "ard_destroy", "ard_set_path", "ard_set_option", "ard_set_tile_n", "ard_set_shared_tail", "ard_set_compact_reuse", "ard_set_distribution", "ard_quantise_distribution", "ard_search_distribution", "ard_get_distribution_cdf",
@@ -42,6 +43,7 @@ EXPORTS = [
     "ard_layer_products", "ard_rows_products", "ard_rows_gather", "ard_rows_fwd_compact", "ard_rows_bwd_data_compact", "ard_rows_bwd_weight_compact",
     "ard_blocks_create", "ard_blocks_destroy", "ard_blocks_predict", "ard_blocks_set_label", "ard_blocks_sample",
     "ard_blocks_fwd", "ard_blocks_bwd_weight", "ard_blocks_bwd_input", "ard_blocks_to_host", "ard_blocks_pattern", "ard_dropout_schedule", "ard_blocks_products",
+    "ard_layer_norm_fwd", "ard_layer_norm_bwd", "ard_glr_forward", "ard_glr_backward", "ard_adamw_step", "ard_grad_norm",
 ]
 
 _lib = None
@@ -53,6 +55,13 @@ class MlpLayer(C.Structure):
                 ("compact_out", C.c_int), ("dW_is_f32", C.c_int), ("alpha", C.c_float), ("ldw", C.c_int),
                 ("W", C.c_void_p), ("bias", C.c_void_p), ("Wk", C.c_void_p), ("A", C.c_void_p), ("dZ", C.c_void_p),
                 ("dWk", C.c_void_p), ("dW", C.c_void_p), ("db", C.c_void_p)]
+
+
+class AdamwTensor(C.Structure):
+    """struct ard_adamw_tensor of include/ard.h (device pointers as integers)."""
+    _fields_ = [("rows", C.c_int64), ("cols", C.c_int64), ("p", C.c_void_p), ("ldp", C.c_int64), ("g", C.c_void_p),
+                ("ldg", C.c_int64), ("g_dtype", C.c_int), ("w", C.c_void_p), ("ldw", C.c_int64), ("m", C.c_void_p),
+                ("v", C.c_void_p), ("m_scale", C.c_void_p), ("v_scale", C.c_void_p), ("weight_decay", C.c_double)]
 
 
 class ArdError(RuntimeError):
@@ -145,6 +154,12 @@ def lib():
         "ard_rows_fwd_compact": [vp, vp, i32, i32, i32, f32, vp, i32, vp, i32, vp, i32, vp],
         "ard_rows_bwd_data_compact": [vp, vp, i32, i32, i32, f32, vp, i32, vp, i32, vp, i32, vp],
         "ard_rows_bwd_weight_compact": [vp, vp, i32, i32, i32, i32, f32, vp, i32, vp, i32, vp, i32, vp],
+        "ard_layer_norm_fwd": [vp, vp, i32, i32, i32, f32, vp, i32, vp, vp, vp, i32, vp, vp, vp],
+        "ard_layer_norm_bwd": [vp, vp, i32, i32, i32, vp, i32, vp, i32, vp, vp, vp, vp, i32, vp, vp, i32, vp],
+        "ard_glr_forward": [vp, vp, i32, i32, i32, i32, f32, vp, vp, vp, i32, vp, vp, vp, i32, vp, vp, vp],
+        "ard_glr_backward": [vp, vp, i32, i32, i32, i32, f32, vp, vp, vp, i32, vp, vp, vp, i32, vp, vp, vp, vp, i32, vp, vp],
+        "ard_adamw_step": [vp, P(AdamwTensor), i32, C.c_double, C.c_double, C.c_double, C.c_double, i32, u64, u64, vp, vp, vp, vp],
+        "ard_grad_norm": [vp, P(AdamwTensor), i32, C.c_double, vp, vp],
     }
     for name, args in sig.items():
         fn = getattr(L, name)
@@ -427,6 +442,60 @@ def ard_mlp_step(ctx, layers, n_layers, B, X, ldx, dOut, lddout, dX, lddx, dist_
     """`layers`: the array made by mlp_layers()."""
     _check(lib().ard_mlp_step(ctx, layers, n_layers, B, _ptr(X), ldx, _ptr(dOut), lddout, _ptr(dX), lddx, dist_id,
                               seed, iteration_base, _ptr(iteration_counter), _stream(stream)), "ard_mlp_step")
+
+
+def ard_layer_norm_fwd(ctx, pat, dtype, rows, N, eps, X, ldx, weight, bias, Y, ldy, mean, rstd, stream=None):
+    _check(_calls().ard_layer_norm_fwd(ctx, pat, dtype, rows, N, eps, X, ldx, weight, bias, Y, ldy, mean, rstd,
+                                       _stream(stream)), "ard_layer_norm_fwd")
+
+
+def ard_layer_norm_bwd(ctx, pat, dtype, rows, N, dY, lddy, X, ldx, weight, mean, rstd, dX, lddx, dweight, dbias,
+                       zero_fill_dropped, stream=None):
+    _check(_calls().ard_layer_norm_bwd(ctx, pat, dtype, rows, N, dY, lddy, X, ldx, weight, mean, rstd, dX, lddx, dweight,
+                                       dbias, zero_fill_dropped, _stream(stream)), "ard_layer_norm_bwd")
+
+
+def ard_glr_forward(ctx, pat, dtype, T, B, H, alpha, Zf, Zg, Zo, ldz, lens, h0, Y, ldy, hT, S, stream=None):
+    _check(_calls().ard_glr_forward(ctx, pat, dtype, T, B, H, alpha, Zf, Zg, Zo, ldz, lens, h0, Y, ldy, hT, S,
+                                    _stream(stream)), "ard_glr_forward")
+
+
+def ard_glr_backward(ctx, pat, dtype, T, B, H, alpha, Zf, Zg, Zo, ldz, lens, S, dY, lddy, dhT, dZf, dZg, dZo, lddz, dh0,
+                     stream=None):
+    _check(_calls().ard_glr_backward(ctx, pat, dtype, T, B, H, alpha, Zf, Zg, Zo, ldz, lens, S, dY, lddy, dhT, dZf, dZg,
+                                     dZo, lddz, dh0, _stream(stream)), "ard_glr_backward")
+
+
+def adamw_tensors(tensors):
+    """Array of AdamwTensor for ard_adamw_step and ard_grad_norm from dicts of the fields of struct ard_adamw_tensor: tensors or
+    device pointers, or None.  Leading dimensions default to cols, g_dtype to that of a torch tensor g.  The array holds
+    pointers only: the tensors have to live as long as it does."""
+    arr = (AdamwTensor * max(len(tensors), 1))()
+    known = {f for f, _ in AdamwTensor._fields_}
+    for t, fields in zip(arr, tensors):
+        d = {"ldp": fields["cols"], "ldg": fields["cols"], "ldw": fields["cols"], **fields}
+        if set(d) - known:
+            raise ValueError("ard_adamw_tensor has no field %s" % ", ".join(sorted(set(d) - known)))
+        if "g_dtype" not in d:
+            kind = str(getattr(d["g"], "dtype", None))
+            if kind not in ("torch.float32", "torch.bfloat16"):
+                raise ValueError("g_dtype is to be given, or g as a tensor of float32 or bfloat16: got %s" % kind)
+            d["g_dtype"] = ARD_F32 if kind == "torch.float32" else ARD_BF16
+        for k, v in d.items():
+            setattr(t, k, _ptr(v) if k in ("p", "g", "w", "m", "v", "m_scale", "v_scale") else v)
+    return arr
+
+
+def ard_adamw_step(ctx, tensors, n_tensors, lr, beta1, beta2, eps, state_bits, seed, step, step_counter=None, lr_factor=None,
+                   grad_factor=None, stream=None):
+    """`tensors`: the array made by adamw_tensors()."""
+    _check(lib().ard_adamw_step(ctx, tensors, n_tensors, lr, beta1, beta2, eps, state_bits, seed, step, _ptr(step_counter),
+                                _ptr(lr_factor), _ptr(grad_factor), _stream(stream)), "ard_adamw_step")
+
+
+def ard_grad_norm(ctx, tensors, n_tensors, max_norm, out, stream=None):
+    """`tensors`: the array made by adamw_tensors()."""
+    _check(lib().ard_grad_norm(ctx, tensors, n_tensors, max_norm, _ptr(out), _stream(stream)), "ard_grad_norm")
 
 
 def ard_dropout_schedule(n_epochs, p_total, mean_epoch, var_epoch, lam, p_max=1.0):

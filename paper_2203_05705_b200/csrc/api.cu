@@ -1684,6 +1684,120 @@ ard_status ard_rows_products(ard_ctx* ctx, const ard_rows* rows, ard_dtype dW_dt
   return ARD_OK;
 }
 
+// A row pattern over N units of this context, or none.
+static ard_status check_units(ard_ctx* ctx, const ard_pattern* pat, int N) {
+  if (!pat) return ARD_OK;
+  if (pat->ctx != ctx || pat->kind != ARD_ROW) return ARD_ERR_INVALID_ARG;
+  return pat->N_dim == N ? ARD_OK : ARD_ERR_SHAPE;
+}
+
+static ard_status layer_norm_check(ard_ctx* ctx, const ard_pattern* pat, ard_dtype dtype, int rows, int N) {
+  if (!ctx || rows < 0 || N < 0) return ARD_ERR_INVALID_ARG;
+  if (dtype != ARD_F32 && dtype != ARD_BF16) return ARD_ERR_INVALID_ARG;
+  if (rows > (1 << 30)) return ARD_ERR_UNSUPPORTED;
+  return check_units(ctx, pat, N);
+}
+
+ard_status ard_layer_norm_fwd(ard_ctx* ctx, const ard_pattern* pat, ard_dtype dtype, int rows, int N, float eps, const void* X,
+                              int ldx, const float* weight, const float* bias, void* Y, int ldy, float* mean, float* rstd,
+                              void* cuda_stream) {
+  const ard_status st = layer_norm_check(ctx, pat, dtype, rows, N);
+  if (st != ARD_OK) return st;
+  if (!X || !Y || X == Y || !(eps >= 0.f) || !(eps < INFINITY)) return ARD_ERR_INVALID_ARG;
+  if (ldx < N || ldy < N) return ARD_ERR_SHAPE;
+  DeviceGuard guard(ctx->device);
+  return launch_layer_norm_fwd(ctx, pat ? pat->d_hdr : nullptr, dtype, rows, N, eps, X, ldx, weight, bias, Y, ldy, mean, rstd,
+                               (cudaStream_t)cuda_stream);
+}
+
+ard_status ard_layer_norm_bwd(ard_ctx* ctx, const ard_pattern* pat, ard_dtype dtype, int rows, int N, const void* dY, int lddy,
+                              const void* X, int ldx, const float* weight, const float* mean, const float* rstd, void* dX, int lddx,
+                              float* dweight, float* dbias, int zero_fill_dropped, void* cuda_stream) {
+  const ard_status st = layer_norm_check(ctx, pat, dtype, rows, N);
+  if (st != ARD_OK) return st;
+  if (!dY || !X || !mean || !rstd || dX == dY || dX == X) return ARD_ERR_INVALID_ARG;
+  if (ldx < N || lddy < N || (dX && lddx < N)) return ARD_ERR_SHAPE;
+  DeviceGuard guard(ctx->device);
+  return launch_layer_norm_bwd(ctx, pat ? pat->d_hdr : nullptr, dtype, rows, N, dY, lddy, X, ldx, weight, mean, rstd, dX, lddx, dweight,
+                               dbias, zero_fill_dropped ? 1 : 0, (cudaStream_t)cuda_stream);
+}
+
+static ard_status glr_check(ard_ctx* ctx, const ard_pattern* pat, ard_dtype dtype, int T, int B, int H, const void* Zf, const void* Zg,
+                            int ldz) {
+  if (!ctx || T < 0 || B < 0 || H < 0 || !Zf || !Zg) return ARD_ERR_INVALID_ARG;
+  if (dtype != ARD_F32 && dtype != ARD_BF16) return ARD_ERR_INVALID_ARG;
+  if (T > (1 << 30)) return ARD_ERR_UNSUPPORTED;
+  if (ldz < H) return ARD_ERR_SHAPE;
+  return check_units(ctx, pat, H);
+}
+
+ard_status ard_glr_forward(ard_ctx* ctx, const ard_pattern* pat, ard_dtype dtype, int T, int B, int H, float alpha, const void* Zf,
+                           const void* Zg, const void* Zo, int ldz, const int32_t* lens, const float* h0, void* Y, int ldy, float* hT,
+                           float* S, void* cuda_stream) {
+  const ard_status st = glr_check(ctx, pat, dtype, T, B, H, Zf, Zg, ldz);
+  if (st != ARD_OK) return st;
+  if (!Y || Y == Zf || Y == Zg || Y == Zo) return ARD_ERR_INVALID_ARG;
+  if (ldy < H) return ARD_ERR_SHAPE;
+  DeviceGuard guard(ctx->device);
+  return launch_glr_forward(ctx, pat ? pat->d_hdr : nullptr, dtype, T, B, H, alpha, Zf, Zg, Zo, ldz, lens, h0, Y, ldy, hT, S,
+                            (cudaStream_t)cuda_stream);
+}
+
+ard_status ard_glr_backward(ard_ctx* ctx, const ard_pattern* pat, ard_dtype dtype, int T, int B, int H, float alpha, const void* Zf,
+                            const void* Zg, const void* Zo, int ldz, const int32_t* lens, const float* S, const void* dY, int lddy,
+                            const float* dhT, void* dZf, void* dZg, void* dZo, int lddz, float* dh0, void* cuda_stream) {
+  const ard_status st = glr_check(ctx, pat, dtype, T, B, H, Zf, Zg, ldz);
+  if (st != ARD_OK) return st;
+  if (!S || !dY || !dZf || !dZg || (Zo != nullptr) != (dZo != nullptr)) return ARD_ERR_INVALID_ARG;
+  if (lddy < H || lddz < H) return ARD_ERR_SHAPE;
+  for (const void* out : {dZf, dZg, dZo})
+    for (const void* in : {Zf, Zg, Zo, dY})
+      if (out && out == in) return ARD_ERR_INVALID_ARG;
+  DeviceGuard guard(ctx->device);
+  return launch_glr_backward(ctx, pat ? pat->d_hdr : nullptr, dtype, T, B, H, alpha, Zf, Zg, Zo, ldz, lens, S, dY, lddy, dhT, dZf, dZg, dZo,
+                             lddz, dh0, (cudaStream_t)cuda_stream);
+}
+
+// What the step and the norm look at; state_bits is 0 for the norm.
+static ard_status adamw_check(const ard_adamw_tensor* tensors, int n_tensors, int state_bits) {
+  if (n_tensors < 0 || (n_tensors > 0 && !tensors)) return ARD_ERR_INVALID_ARG;
+  for (int i = 0; i < n_tensors; ++i) {
+    const ard_adamw_tensor& t = tensors[i];
+    if (t.rows < 0 || t.cols < 0) return ARD_ERR_INVALID_ARG;
+    if (t.rows == 0 || t.cols == 0) continue;
+    if (!t.g || (t.g_dtype != ARD_F32 && t.g_dtype != ARD_BF16)) return ARD_ERR_INVALID_ARG;
+    if (t.rows > (1ll << 34) || t.cols > (1ll << 34) || t.rows > (1ll << 34) / t.cols) return ARD_ERR_SHAPE;
+    if (t.rows > 1 && (t.ldg < t.cols || t.ldg > (1ll << 34))) return ARD_ERR_SHAPE;
+    if (state_bits == 0) continue;
+    if (!t.p || !t.m || !t.v || !(t.weight_decay >= 0.0) || !(t.weight_decay < INFINITY)) return ARD_ERR_INVALID_ARG;
+    if (state_bits == 8 && (!t.m_scale || !t.v_scale)) return ARD_ERR_INVALID_ARG;
+    if (t.rows > 1 && (t.ldp < t.cols || t.ldp > (1ll << 34))) return ARD_ERR_SHAPE;
+    if (t.rows > 1 && t.w && (t.ldw < t.cols || t.ldw > (1ll << 34))) return ARD_ERR_SHAPE;
+  }
+  return ARD_OK;
+}
+
+ard_status ard_adamw_step(ard_ctx* ctx, const ard_adamw_tensor* tensors, int n_tensors, double lr, double beta1, double beta2, double eps,
+                          int state_bits, uint64_t seed, uint64_t step, const uint64_t* step_counter, const float* lr_factor,
+                          const float* grad_factor, void* cuda_stream) {
+  if (!ctx || (state_bits != 8 && state_bits != 32)) return ARD_ERR_INVALID_ARG;
+  if (!(lr >= 0.0) || !(lr < INFINITY) || !(eps >= 0.0) || !(eps < INFINITY)) return ARD_ERR_INVALID_ARG;
+  if (!(beta1 >= 0.0) || !(beta1 < 1.0) || !(beta2 >= 0.0) || !(beta2 < 1.0)) return ARD_ERR_INVALID_ARG;
+  const ard_status st = adamw_check(tensors, n_tensors, state_bits);
+  if (st != ARD_OK) return st;
+  DeviceGuard guard(ctx->device);
+  return launch_adamw(ctx, tensors, n_tensors, lr, beta1, beta2, eps, state_bits, seed, step, step_counter, lr_factor, grad_factor,
+                      (cudaStream_t)cuda_stream);
+}
+
+ard_status ard_grad_norm(ard_ctx* ctx, const ard_adamw_tensor* tensors, int n_tensors, double max_norm, float* out, void* cuda_stream) {
+  if (!ctx || !out || max_norm != max_norm) return ARD_ERR_INVALID_ARG;
+  const ard_status st = adamw_check(tensors, n_tensors, 0);
+  if (st != ARD_OK) return st;
+  DeviceGuard guard(ctx->device);
+  return launch_grad_norm(ctx, tensors, n_tensors, max_norm, out, (cudaStream_t)cuda_stream);
+}
+
 ard_status ard_last_device_status(ard_ctx* ctx, void* cuda_stream) {
   if (!ctx) return ARD_ERR_INVALID_ARG;
   DeviceGuard guard(ctx->device);

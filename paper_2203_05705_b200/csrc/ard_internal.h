@@ -319,6 +319,23 @@ ard_status launch_lstm_gates_bwd(ard_ctx* ctx, const ard_pattern* pat, ard_dtype
                                  const float* dh, int lddh, int dh_scatter, float* dc_inout, void* dZ, int ldz_gate,
                                  cudaStream_t s);
 
+// Layer norm (layer_norm.cu), gated linear recurrence (glr.cu), optimiser (adamw.cu).  hdr: a row pattern's header, nullptr for all units.
+ard_status launch_layer_norm_fwd(ard_ctx* ctx, const int32_t* hdr, ard_dtype dtype, int rows, int N, float eps, const void* X, int ldx,
+                                 const float* weight, const float* bias, void* Y, int ldy, float* mean, float* rstd, cudaStream_t s);
+ard_status launch_layer_norm_bwd(ard_ctx* ctx, const int32_t* hdr, ard_dtype dtype, int rows, int N, const void* dY, int lddy,
+                                 const void* X, int ldx, const float* weight, const float* mean, const float* rstd, void* dX, int lddx,
+                                 float* dweight, float* dbias, int zero_fill, cudaStream_t s);
+ard_status launch_glr_forward(ard_ctx* ctx, const int32_t* hdr, ard_dtype dtype, int T, int B, int H, float alpha, const void* Zf,
+                              const void* Zg, const void* Zo, int ldz, const int32_t* lens, const float* h0, void* Y, int ldy, float* hT,
+                              float* S, cudaStream_t s);
+ard_status launch_glr_backward(ard_ctx* ctx, const int32_t* hdr, ard_dtype dtype, int T, int B, int H, float alpha, const void* Zf,
+                               const void* Zg, const void* Zo, int ldz, const int32_t* lens, const float* S, const void* dY, int lddy,
+                               const float* dhT, void* dZf, void* dZg, void* dZo, int lddz, float* dh0, cudaStream_t s);
+ard_status launch_adamw(ard_ctx* ctx, const ard_adamw_tensor* tensors, int n_tensors, double lr, double beta1, double beta2, double eps,
+                        int bits, uint64_t seed, uint64_t step, const uint64_t* counter, const float* lr_factor, const float* grad_factor,
+                        cudaStream_t s);
+ard_status launch_grad_norm(ard_ctx* ctx, const ard_adamw_tensor* tensors, int n_tensors, double max_norm, float* out, cudaStream_t s);
+
 // ---- programmatic dependent launch ----------------------------------------------------------------
 // Every kernel of the library is launched so that its blocks may become resident while the previous
 // kernel of the stream is still draining: the block set-up (barriers, tensor memory, index arithmetic)

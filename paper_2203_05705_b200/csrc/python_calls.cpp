@@ -160,7 +160,8 @@ PyMethodDef g_methods[] = {
     CALL(ard_rows_sample), CALL(ard_rows_products), CALL(ard_rows_gather), CALL(ard_rows_fwd), CALL(ard_rows_bwd_data),
     CALL(ard_rows_bwd_weight), CALL(ard_rows_fwd_compact), CALL(ard_rows_bwd_data_compact), CALL(ard_rows_bwd_weight_compact),
     CALL(ard_blocks_predict), CALL(ard_blocks_sample), CALL(ard_blocks_fwd), CALL(ard_blocks_bwd_weight),
-    CALL(ard_blocks_bwd_input), CALL(ard_blocks_products), {nullptr, nullptr, 0, nullptr}};
+    CALL(ard_blocks_bwd_input), CALL(ard_blocks_products),
+    CALL(ard_layer_norm_fwd), CALL(ard_layer_norm_bwd), CALL(ard_glr_forward), CALL(ard_glr_backward), {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 
