@@ -126,6 +126,21 @@ bool staged_by_threads(const ard_ctx* ctx, const ard_pattern* pat, GemmOp op, ar
 
 }  // namespace
 
+bool ard_encode_steps(ard_ctx* ctx, CUtensorMap* out, bool f32, const void* base, int cols, int rows, int steps, int ld, int box_cols,
+                      int box_steps) {
+  if (!ctx->encode_fn) return false;
+  const cuuint64_t row_bytes = (cuuint64_t)ld * (f32 ? 4 : 2), step_bytes = row_bytes * (cuuint64_t)rows;
+  if (step_bytes >= (1ull << 40)) return false;
+  cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)steps};
+  cuuint64_t strides[2] = {row_bytes, step_bytes};
+  cuuint32_t box[3] = {(cuuint32_t)box_cols, 1, (cuuint32_t)box_steps};
+  cuuint32_t estr[3] = {1, 1, 1};
+  return reinterpret_cast<EncodeTiledFn>(ctx->encode_fn)(
+             out, f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, estr,
+             CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 ard_status ard_encode_tcmap(ard_ctx* ctx, const void* base, int rows, int cols, int ld, int units, int variant,
                             int box_rows, int box_cols, TcMap* out) {
   return get_maps(ctx, base, rows, cols, ld, units, variant, 0, box_rows, box_cols, out);

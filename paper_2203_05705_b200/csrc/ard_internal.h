@@ -180,6 +180,10 @@ struct SharedTailOff {
 // One whole-matrix descriptor (see TcMap): [rows][cols] bf16 at `base`, pitch ld, boxes of box_rows x box_cols.
 ard_status ard_encode_tcmap(ard_ctx* ctx, const void* base, int rows, int cols, int ld, int units, int variant,
                             int box_rows, int box_cols, TcMap* out);
+// A descriptor of [steps][rows][cols] elements (bf16 or fp32) with a row pitch of ld elements, boxes of box_cols columns of one row in box_steps
+// steps, as they are (no swizzle), zeros outside.  False: the operand cannot be described.
+bool ard_encode_steps(ard_ctx* ctx, CUtensorMap* out, bool f32, const void* base, int cols, int rows, int steps, int ld, int box_cols,
+                      int box_steps);
 // The iteration of ard_mlp_step in one cooperative kernel; ARD_ERR_UNSUPPORTED (nothing enqueued) when the
 // stack does not fit it.
 ard_status launch_mlp_persistent(ard_ctx* ctx, const ard_mlp_layer* layers, int n_layers, int B, const void* X, int ldx,
