@@ -11,6 +11,7 @@
 #include <cooperative_groups.h>
 
 #include <initializer_list>
+#include <type_traits>
 #include <utility>
 
 #include "ard_internal.h"
@@ -40,11 +41,49 @@ struct GlrArgs {
   int* status;
 };
 
-// exp(x) and 1 / x to about two units in the last place, results below the normal range zero (x in range otherwise): the forms that keep
-// subnormals cost five instructions each, of which a gate has two.
-__device__ __forceinline__ float glr_exp(float x) {
+// A lane's channels.  Two of them go through one instruction (f32x2): these kernels run out of issue slots before anything else.
+template <int VEC>
+struct GlrV {
+  float v[VEC];
+  __device__ __forceinline__ static GlrV all(float x) {
+    GlrV r;
+#pragma unroll
+    for (int k = 0; k < VEC; ++k) r.v[k] = x;
+    return r;
+  }
+};
+template <int VEC>
+__device__ __forceinline__ GlrV<VEC> operator*(const GlrV<VEC>& a, const GlrV<VEC>& b) {
+  if constexpr (VEC == 2) {
+    const float2 r = __fmul2_rn(make_float2(a.v[0], a.v[1]), make_float2(b.v[0], b.v[1]));
+    return {{r.x, r.y}};
+  } else {
+    return {{a.v[0] * b.v[0]}};
+  }
+}
+template <int VEC>
+__device__ __forceinline__ GlrV<VEC> operator+(const GlrV<VEC>& a, const GlrV<VEC>& b) {
+  if constexpr (VEC == 2) {
+    const float2 r = __fadd2_rn(make_float2(a.v[0], a.v[1]), make_float2(b.v[0], b.v[1]));
+    return {{r.x, r.y}};
+  } else {
+    return {{a.v[0] + b.v[0]}};
+  }
+}
+template <int VEC>
+__device__ __forceinline__ GlrV<VEC> glr_fma(const GlrV<VEC>& a, const GlrV<VEC>& b, const GlrV<VEC>& c) {
+  if constexpr (VEC == 2) {
+    const float2 r = __ffma2_rn(make_float2(a.v[0], a.v[1]), make_float2(b.v[0], b.v[1]), make_float2(c.v[0], c.v[1]));
+    return {{r.x, r.y}};
+  } else {
+    return {{fmaf(a.v[0], b.v[0], c.v[0])}};
+  }
+}
+// 2^x and 1 / x to about two units in the last place, results below the normal range zero: the forms that keep subnormals cost five
+// instructions each, of which a gate has two.
+__device__ __forceinline__ float glr_exp2(float x) {
   float r;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x * 1.44269504f));
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
   return r;
 }
 __device__ __forceinline__ float glr_inverse(float x) {
@@ -54,11 +93,23 @@ __device__ __forceinline__ float glr_inverse(float x) {
 }
 // s(z), and 1 - s(z), each to the last bits of its own: where s(z) is above a half the other one is exp(-z) times it, not a difference.  exp(-z) of
 // infinity gives 0 and 1.
-__device__ __forceinline__ float glr_gate(float z) { return glr_inverse(1.f + glr_exp(-z)); }
-__device__ __forceinline__ float glr_gate(float z, float& rest) {
-  const float u = glr_exp(-z), f = glr_inverse(1.f + u);
-  rest = z >= 0.f ? u * f : 1.f - f;
+template <int VEC>
+__device__ __forceinline__ GlrV<VEC> glr_gate(const GlrV<VEC>& z, GlrV<VEC>& rest) {
+  GlrV<VEC> u = z * GlrV<VEC>::all(-1.44269504f);
+#pragma unroll
+  for (int k = 0; k < VEC; ++k) u.v[k] = glr_exp2(u.v[k]);
+  GlrV<VEC> f = u + GlrV<VEC>::all(1.f);
+#pragma unroll
+  for (int k = 0; k < VEC; ++k) f.v[k] = glr_inverse(f.v[k]);
+  const GlrV<VEC> small = u * f, large = glr_fma(f, GlrV<VEC>::all(-1.f), GlrV<VEC>::all(1.f));
+#pragma unroll
+  for (int k = 0; k < VEC; ++k) rest.v[k] = z.v[k] >= 0.f ? small.v[k] : large.v[k];
   return f;
+}
+template <int VEC>
+__device__ __forceinline__ GlrV<VEC> glr_gate(const GlrV<VEC>& z) {
+  GlrV<VEC> rest;
+  return glr_gate(z, rest);  // (what is not used is not computed)
 }
 
 // VEC channels of one step as they lie in memory, in one register.
@@ -75,17 +126,20 @@ __device__ __forceinline__ uint32_t glr_fetch(const T* p) {
   return q;
 }
 template <typename T, int VEC>
-__device__ __forceinline__ void glr_unpack(uint32_t q, float (&v)[VEC]) {
+__device__ __forceinline__ GlrV<VEC> glr_unpack(uint32_t q) {
+  GlrV<VEC> r;
   if constexpr (sizeof(T) == 4) {
-    v[0] = __uint_as_float(q);
+    r.v[0] = __uint_as_float(q);
   } else {
-    v[0] = __uint_as_float(q << 16);
-    if constexpr (VEC == 2) v[1] = __uint_as_float(q & 0xFFFF0000u);
+    r.v[0] = __uint_as_float(q << 16);
+    if constexpr (VEC == 2) r.v[1] = __uint_as_float(q & 0xFFFF0000u);
   }
+  return r;
 }
 // The first `valid` of the values.
 template <typename T, int VEC>
-__device__ __forceinline__ void glr_store(T* p, int valid, const float (&v)[VEC]) {
+__device__ __forceinline__ void glr_store(T* p, int valid, const GlrV<VEC>& x) {
+  const float* v = x.v;
   if constexpr (VEC == 2) {
     if (valid >= 2) {
       *reinterpret_cast<__nv_bfloat162*>(p) = __floats2bfloat162_rn(v[0], v[1]);
@@ -98,28 +152,16 @@ __device__ __forceinline__ void glr_store(T* p, int valid, const float (&v)[VEC]
   }
 }
 
-// Maps x -> A x + B of a lane's channels: [A, B][channel].
+// Maps x -> a x + b of a lane's channels.
 template <int VEC>
 struct GlrMap {
-  float a[VEC], b[VEC];
-  __device__ __forceinline__ static GlrMap none() {
-    GlrMap m;
-#pragma unroll
-    for (int v = 0; v < VEC; ++v) {
-      m.a[v] = 1.f;
-      m.b[v] = 0.f;
-    }
-    return m;
-  }
+  GlrV<VEC> a, b;
   // this one, then `next`
   __device__ __forceinline__ void then(const GlrMap& next) {
-#pragma unroll
-    for (int v = 0; v < VEC; ++v) {
-      a[v] *= next.a[v];
-      b[v] = fmaf(next.a[v], b[v], next.b[v]);
-    }
+    b = glr_fma(next.a, b, next.b);
+    a = a * next.a;
   }
-  __device__ __forceinline__ float of(float x, int v) const { return fmaf(a[v], x, b[v]); }
+  __device__ __forceinline__ GlrV<VEC> of(const GlrV<VEC>& x) const { return glr_fma(a, x, b); }
 };
 
 // What the kernels run over: units of CW * 32 * VEC channels of one sequence, `rounds` times CL slabs of WT * SPT steps each.
@@ -244,10 +286,10 @@ struct GlrFeed<T, VEC, M, WT, SPT, false> {
   __device__ __forceinline__ uint32_t raw(int, int m, int k) const { return q[m][k]; }
 };
 
-// The exchange of a slab: from this thread's map and the state x that enters the round, the state that enters this thread's steps and, in x, the
-// one behind the round.  The warps' maps are in s_warp, and a barrier has been passed.  The cluster's CTAs send each other their slabs' maps
-// by asynchronous stores that count on the receiver's barrier: a barrier of the cluster would wait for the outputs' stores, 2 us a round.
-// Every CTA hears from all of them in every round, so none is more than a round ahead and two sets of places are enough.
+// The maps of a slab's warps meet in `warp`; its last warp (in the order of the recurrence) leaves the state behind the round in `state`, where the
+// next round finds it.  The cluster's CTAs send each other their slabs' maps by asynchronous stores that count on the receiver's
+// barrier: a barrier of the cluster would wait for the outputs' stores, 2 us a round.  Every CTA hears from all of them in every round, so none is
+// more than a round ahead and two sets of places are enough.
 template <int VEC, int CW>
 struct GlrMail {
   GlrMap<VEC> box[2][GLR_CLUSTER][CW * 32];
@@ -259,65 +301,66 @@ __device__ __forceinline__ void glr_send(GlrMap<VEC>* box, uint64_t* bar, int r,
   asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(dst) : "r"(smem_u32(box)), "r"(r));
   asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(rbar) : "r"(smem_u32(bar)), "r"(r));
   if constexpr (VEC == 2)
-    asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v4.f32 [%0], {%1, %2, %3, %4}, [%5];" ::"r"(dst), "f"(m.a[0]),
-                 "f"(m.a[1]), "f"(m.b[0]), "f"(m.b[1]), "r"(rbar)
+    asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v4.f32 [%0], {%1, %2, %3, %4}, [%5];" ::"r"(dst), "f"(m.a.v[0]),
+                 "f"(m.a.v[1]), "f"(m.b.v[0]), "f"(m.b.v[1]), "r"(rbar)
                  : "memory");
   else
-    asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v2.f32 [%0], {%1, %2}, [%3];" ::"r"(dst), "f"(m.a[0]), "f"(m.b[0]),
+    asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v2.f32 [%0], {%1, %2}, [%3];" ::"r"(dst), "f"(m.a.v[0]), "f"(m.b.v[0]),
                  "r"(rbar)
                  : "memory");
 }
-// `mail`: rounds of the cluster so far.
 template <int VEC, int CW, int WT>
-__device__ __forceinline__ void glr_exchange(int wt, int ch, int mail, int set, int CL, int rank, bool forward, const GlrMap<VEC>& mine,
-                                             const GlrMap<VEC> (*s_warp)[WT][CW * 32], GlrMail<VEC, CW>* post, float (&x)[VEC], float (&enters)[VEC],
-                                             volatile int* s_gone, int* status) {
-  GlrMap<VEC> before = GlrMap<VEC>::none(), all = mine;
+struct GlrShared {
+  GlrMap<VEC> warp[2][WT][CW * 32];
+  GlrV<VEC> state[2][CW * 32];
+  GlrMail<VEC, CW> post;
+  uint64_t full[3];
+  int gone;
+};
+
+// Behind the barrier that follows the warps' maps: the state that enters this warp's steps.  x: what enters the unit's first round.  FORWARD: warps
+// count in the order of the steps, else against it.  `mail`: rounds of the cluster so far.
+template <bool FORWARD, int VEC, int CW, int WT>
+__device__ __forceinline__ GlrV<VEC> glr_enter(GlrShared<VEC, CW, WT>& sh, int wt, int ch, bool first, int mail, int CL, int rank,
+                                              const GlrV<VEC>& x, int* status) {
+  GlrV<VEC> c = x;
   if constexpr (WT > 1) {
-    all = before;
+    constexpr int LAST = FORWARD ? WT - 1 : 0;
+    const int set = mail & 1;
+    if (!first) c = sh.state[set][ch];
+    if (CL > 1) {
+      if (wt == LAST) {
+        GlrMap<VEC> all = sh.warp[set][WT - 1 - LAST][ch];
 #pragma unroll
-    for (int k = 0; k < WT; ++k) {
-      const int w = forward ? k : WT - 1 - k;
-      if (w == wt) before = all;
-      all.then(s_warp[set][w][ch]);
-    }
-  }
-  if (CL > 1) {
-    const int p = mail & 1;
-    if (wt == 0)
-      for (int r = 0; r < CL; ++r) glr_send<VEC>(&post->box[p][rank][ch], &post->bar[p], r, all);
-    if (threadIdx.x == 0) mbar_arrive_expect_tx(smem_u32(&post->bar[p]), (uint32_t)(CL * CW * 32 * sizeof(GlrMap<VEC>)));
-    mbar_wait(smem_u32(&post->bar[p]), (uint32_t)(mail >> 1) & 1u, s_gone, status);
-    for (int r = 0; r < CL; ++r) {
-      const GlrMap<VEC> m = post->box[p][r][ch];
-#pragma unroll
-      for (int v = 0; v < VEC; ++v) {
-        if (r == rank) enters[v] = x[v];
-        x[v] = m.of(x[v], v);
+        for (int k = 1; k < WT; ++k) all.then(sh.warp[set][FORWARD ? k : WT - 1 - k][ch]);
+        for (int r = 0; r < CL; ++r) glr_send<VEC>(&sh.post.box[set][rank][ch], &sh.post.bar[set], r, all);
+      }
+      if (threadIdx.x == 0) mbar_arrive_expect_tx(smem_u32(&sh.post.bar[set]), (uint32_t)(CL * CW * 32 * sizeof(GlrMap<VEC>)));
+      mbar_wait(smem_u32(&sh.post.bar[set]), (uint32_t)(mail >> 1) & 1u, &sh.gone, status);
+      for (int r = 0; r < rank; ++r) c = sh.post.box[set][r][ch].of(c);
+      if (wt == LAST) {
+        GlrV<VEC> behind = c;
+        for (int r = rank; r < CL; ++r) behind = sh.post.box[set][r][ch].of(behind);
+        sh.state[set ^ 1][ch] = behind;
       }
     }
-  } else {
-#pragma unroll
-    for (int v = 0; v < VEC; ++v) {
-      enters[v] = x[v];
-      x[v] = all.of(x[v], v);
+    if constexpr (FORWARD) {
+      for (int w = 0; w < wt; ++w) c = sh.warp[set][w][ch].of(c);
+    } else {
+      for (int w = WT - 1; w > wt; --w) c = sh.warp[set][w][ch].of(c);
     }
   }
-#pragma unroll
-  for (int v = 0; v < VEC; ++v) enters[v] = before.of(enters[v], v);
+  return c;
 }
 
 // Shared memory and barriers of either kernel, before it touches global memory.
-template <int VEC, int CW>
-__device__ __forceinline__ void glr_setup(int CL, GlrMail<VEC, CW>* post, uint64_t* full, int* s_gone, bool bulk) {
+template <typename Shared>
+__device__ __forceinline__ void glr_setup(int CL, Shared& sh) {
   if (threadIdx.x == 0) {
-    *s_gone = 0;
-    if (CL > 1) {
-      mbar_init(smem_u32(&post->bar[0]), 1);
-      mbar_init(smem_u32(&post->bar[1]), 1);
-    }
-    if (bulk)
-      for (int k = 0; k < 3; ++k) mbar_init(smem_u32(&full[k]), 1);
+    sh.gone = 0;
+    mbar_init(smem_u32(&sh.post.bar[0]), 1);
+    mbar_init(smem_u32(&sh.post.bar[1]), 1);
+    for (int k = 0; k < 3; ++k) mbar_init(smem_u32(&sh.full[k]), 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (CL > 1) cg::this_cluster().sync();  // the others' memory is written only once they run
@@ -329,19 +372,18 @@ __device__ __forceinline__ void glr_setup(int CL, GlrMail<VEC, CW>* post, uint64
 template <typename T, int VEC, bool GATE, int CW, int WT, int SPT, bool BULK>
 __global__ void __launch_bounds__(CW* WT * 32, CW* WT == 8 ? 2 : 1)
     glr_fwd_kernel(const GlrArgs a, int CL, const __grid_constant__ GlrTiles tiles) {
+  using V = GlrV<VEC>;
   constexpr int M = GATE ? 3 : 2, SLAB = WT * SPT;
   extern __shared__ __align__(128) uint8_t slots[];
-  __shared__ __align__(16) GlrMap<VEC> s_warp[2][WT][CW * 32];
-  __shared__ __align__(16) GlrMail<VEC, CW> post;
-  __shared__ uint64_t full[3];
-  __shared__ int s_gone;
-  glr_setup<VEC, CW>(CL, &post, full, &s_gone, BULK);
+  __shared__ __align__(16) GlrShared<VEC, CW, WT> sh;
+  glr_setup(CL, sh);
   const int cluster = blockIdx.x / CL, rank = blockIdx.x % CL, clusters = gridDim.x / CL;
   const GlrSpan sp(a, CW * 32 * VEC, SLAB * CL);
-  GlrFeed<T, VEC, M, WT, SPT, BULK> in(slots, full, &s_gone, cluster);
+  GlrFeed<T, VEC, M, WT, SPT, BULK> in(slots, sh.full, &sh.gone, cluster);
   if constexpr (BULK)
     if (threadIdx.x == 0)
       for (int k = 0; k < in.SLOTS; ++k) in.ask(a, sp, tiles, CL, rank, clusters, false);
+  const V alpha = V::all(a.alpha);
   int mail = 0;
   for (int unit = cluster; unit < sp.units; unit += clusters) {
     const GlrPlace<VEC, CW, WT> at(a, sp, unit);
@@ -356,67 +398,72 @@ __global__ void __launch_bounds__(CW* WT * 32, CW* WT == 8 ? 2 : 1)
       for (int m = 0; m < M; ++m) in.step[m] = (size_t)a.B * a.ldz;
       in.fetch(rank * SLAB + at.wt * SPT, at.len);
     }
-    float cs[VEC];  // the state that enters the round
+    V first;  // the state that enters the unit
 #pragma unroll
-    for (int v = 0; v < VEC; ++v) cs[v] = a.h0 && v < at.valid ? a.h0[at.of(a, sp, v)] : 0.f;
-    for (int it = 0; it < sp.rounds; ++it, ++mail) {
+    for (int v = 0; v < VEC; ++v) first.v[v] = a.h0 && v < at.valid ? a.h0[at.of(a, sp, v)] : 0.f;
+    const bool inside = (unit % sp.groups + 1) * (CW * 32 * VEC) <= sp.n;
+    V c = first;
+    // FULL: all steps of the slab are a sequence's, all channels of the unit exist; nothing is asked per step
+    auto slab = [&](auto full, int it) {
+      constexpr bool FULL = decltype(full)::value;
       const int t0 = (it * CL + rank) * SLAB + at.wt * SPT;
-      if constexpr (BULK) in.wait(a.status);
-      float f[SPT][VEC], x[SPT][VEC], o[GATE ? SPT : 1][VEC];
-      GlrMap<VEC> map = GlrMap<VEC>::none();
+      V f[SPT], x[SPT], o[GATE ? SPT : 1];
+      GlrMap<VEC> map;
 #pragma unroll
       for (int k = 0; k < SPT; ++k) {
-        glr_unpack<T, VEC>(in.raw(at.wt, 0, k), f[k]);
-        glr_unpack<T, VEC>(in.raw(at.wt, 1, k), x[k]);
-        if constexpr (GATE) glr_unpack<T, VEC>(in.raw(at.wt, 2, k), o[k]);
-        const bool live = t0 + k < at.len;
-#pragma unroll
-        for (int v = 0; v < VEC; ++v) {
-          float rest;
-          f[k][v] = glr_gate(f[k][v], rest);
-          x[k][v] *= rest;
-          if (!live) {
-            f[k][v] = 1.f;
-            x[k][v] = 0.f;
+        V rest;
+        f[k] = glr_gate(glr_unpack<T, VEC>(in.raw(at.wt, 0, k)), rest);
+        x[k] = rest * glr_unpack<T, VEC>(in.raw(at.wt, 1, k));
+        if constexpr (GATE) o[k] = alpha * glr_gate(glr_unpack<T, VEC>(in.raw(at.wt, 2, k)));
+        if constexpr (!FULL)
+          if (t0 + k >= at.len) {
+            f[k] = V::all(1.f);
+            x[k] = V::all(0.f);
           }
-          map.a[v] *= f[k][v];
-          map.b[v] = fmaf(f[k][v], map.b[v], x[k][v]);
-          if constexpr (GATE) o[k][v] = a.alpha * glr_gate(o[k][v]);
-        }
+        if (k == 0) map = {f[0], x[0]};
+        else map.then({f[k], x[k]});
       }
       if constexpr (!BULK)
         if (it + 1 < sp.rounds) in.fetch(t0 + SLAB * CL, at.len);
       if constexpr (WT > 1) {
-        s_warp[mail & 1][at.wt][at.ch] = map;
+        sh.warp[mail & 1][at.wt][at.ch] = map;
         __syncthreads();
       }
       if constexpr (BULK) {  // everybody has read the slot
         if (threadIdx.x == 0) in.ask(a, sp, tiles, CL, rank, clusters, false);
         in.next();
       }
-      float c[VEC];
-      glr_exchange<VEC, CW, WT>(at.wt, at.ch, mail, mail & 1, CL, rank, true, map, s_warp, &post, cs, c, &s_gone, a.status);
+      c = glr_enter<true>(sh, at.wt, at.ch, it == 0, mail, CL, rank, first, a.status);
       if (a.S && t0 % ARD_GLR_CHUNK == 0 && t0 < a.T)
 #pragma unroll
         for (int v = 0; v < VEC; ++v)
-          if (v < at.valid) a.S[((size_t)(t0 / ARD_GLR_CHUNK) * a.B + at.b) * a.H + at.j + v] = c[v];
+          if (v < at.valid) a.S[((size_t)(t0 / ARD_GLR_CHUNK) * a.B + at.b) * a.H + at.j + v] = c.v[v];
       T* out = y + (size_t)t0 * step_y;
 #pragma unroll
       for (int k = 0; k < SPT; ++k) {
-        float w[VEC];
-#pragma unroll
-        for (int v = 0; v < VEC; ++v) {
-          c[v] = fmaf(f[k][v], c[v], x[k][v]);
-          w[v] = t0 + k < at.len ? (GATE ? o[k][v] : a.alpha) * c[v] : 0.f;
+        c = glr_fma(f[k], c, x[k]);
+        V w = (GATE ? o[k] : alpha) * c;
+        if constexpr (FULL) {
+          glr_store<T, VEC>(out, VEC, w);
+        } else {
+          if (t0 + k >= at.len) w = V::all(0.f);
+          if (t0 + k < a.T) glr_store<T, VEC>(out, at.valid, w);
         }
-        if (t0 + k < a.T) glr_store<T, VEC>(out, at.valid, w);
         out += step_y;
       }
+      if (WT > 1 && CL == 1 && at.wt == WT - 1) sh.state[(mail & 1) ^ 1][at.ch] = c;
+    };
+    for (int it = 0; it < sp.rounds; ++it, ++mail) {
+      if constexpr (BULK) in.wait(a.status);
+      if (inside && ((it + 1) * CL) * SLAB <= at.len) slab(std::true_type{}, it);
+      else slab(std::false_type{}, it);
     }
-    if (a.hT && rank == 0 && at.wt == 0)
+    if (a.hT && rank == 0 && at.wt == WT - 1) {  // (the last warp's own words)
+      const V behind = WT > 1 && sp.rounds > 0 ? sh.state[mail & 1][at.ch] : c;
 #pragma unroll
       for (int v = 0; v < VEC; ++v)
-        if (v < at.valid) a.hT[at.of(a, sp, v)] = cs[v];
+        if (v < at.valid) a.hT[at.of(a, sp, v)] = behind.v[v];
+    }
   }
   if constexpr (BULK)
     if (threadIdx.x == 0) in.drain();
@@ -426,19 +473,19 @@ __global__ void __launch_bounds__(CW* WT * 32, CW* WT == 8 ? 2 : 1)
 template <typename T, int VEC, bool GATE, int CW, int WT, int SPT, bool BULK>
 __global__ void __launch_bounds__(CW* WT * 32, CW* WT == 8 ? 2 : 1)
     glr_bwd_kernel(const GlrArgs a, int CL, const __grid_constant__ GlrTiles tiles) {
+  using V = GlrV<VEC>;
   constexpr int M = GATE ? 4 : 3, SLAB = WT * SPT;
   extern __shared__ __align__(128) uint8_t slots[];
-  __shared__ __align__(16) GlrMap<VEC> s_warp[2][WT][CW * 32], s_back[2][WT][CW * 32];
-  __shared__ __align__(16) GlrMail<VEC, CW> post;
-  __shared__ uint64_t full[3];
-  __shared__ int s_gone;
-  glr_setup<VEC, CW>(CL, &post, full, &s_gone, BULK);
+  __shared__ __align__(16) GlrShared<VEC, CW, WT> sh;  // of the adjoint's maps
+  __shared__ __align__(16) GlrMap<VEC> s_states[2][WT][CW * 32];
+  glr_setup(CL, sh);
   const int cluster = blockIdx.x / CL, rank = blockIdx.x % CL, clusters = gridDim.x / CL;
   const GlrSpan sp(a, CW * 32 * VEC, SLAB * CL);
-  GlrFeed<T, VEC, M, WT, SPT, BULK> in(slots, full, &s_gone, cluster);
+  GlrFeed<T, VEC, M, WT, SPT, BULK> in(slots, sh.full, &sh.gone, cluster);
   if constexpr (BULK)
     if (threadIdx.x == 0)
       for (int k = 0; k < in.SLOTS; ++k) in.ask(a, sp, tiles, CL, rank, clusters, true);
+  const V alpha = V::all(a.alpha), minus = V::all(-1.f);
   int mail = 0;
   for (int unit = cluster; unit < sp.units; unit += clusters) {
     const GlrPlace<VEC, CW, WT> at(a, sp, unit);
@@ -458,96 +505,97 @@ __global__ void __launch_bounds__(CW* WT * 32, CW* WT == 8 ? 2 : 1)
       for (int m = 0; m < M; ++m) in.step[m] = (size_t)a.B * (m == 2 ? a.ldy : a.ldz);
       if (sp.rounds > 0) in.fetch(start(0) + at.wt * SPT, at.len);
     }
-    float qs[VEC];  // what arrives behind the round's last step
+    V first;  // what arrives behind the unit's last step
 #pragma unroll
-    for (int v = 0; v < VEC; ++v) qs[v] = a.h0 && v < at.valid ? a.h0[at.of(a, sp, v)] : 0.f;
-    for (int it = 0; it < sp.rounds; ++it, ++mail) {
+    for (int v = 0; v < VEC; ++v) first.v[v] = a.h0 && v < at.valid ? a.h0[at.of(a, sp, v)] : 0.f;
+    const bool inside = (unit % sp.groups + 1) * (CW * 32 * VEC) <= sp.n;
+    V q = first;
+    auto slab = [&](auto full, int it) {
+      constexpr bool FULL = decltype(full)::value;
       const int ts = start(it), t0 = ts + at.wt * SPT;
-      float c0[VEC];  // the state that enters the slab
+      V c0;  // the state that enters the slab
 #pragma unroll
       for (int v = 0; v < VEC; ++v)
-        c0[v] = ts < a.T && v < at.valid ? a.S[((size_t)(ts / ARD_GLR_CHUNK) * a.B + at.b) * a.H + at.j + v] : 0.f;
-      if constexpr (BULK) in.wait(a.status);
+        c0.v[v] = ts < a.T && v < at.valid ? a.S[((size_t)(ts / ARD_GLR_CHUNK) * a.B + at.b) * a.H + at.j + v] : 0.f;
       // e: alpha s(zo) dy, what arrives at c from y; no: 1 - s(zo)
-      float f[SPT][VEC], i[SPT][VEC], g[SPT][VEC], e[SPT][VEC], no[GATE ? SPT : 1][VEC];
-      GlrMap<VEC> map = GlrMap<VEC>::none(), back;
+      V f[SPT], i[SPT], g[SPT], e[SPT], no[GATE ? SPT : 1];
+      GlrMap<VEC> map, back;
 #pragma unroll
       for (int k = 0; k < SPT; ++k) {
-        glr_unpack<T, VEC>(in.raw(at.wt, 0, k), f[k]);
-        glr_unpack<T, VEC>(in.raw(at.wt, 1, k), g[k]);
-        glr_unpack<T, VEC>(in.raw(at.wt, 2, k), e[k]);
-        if constexpr (GATE) glr_unpack<T, VEC>(in.raw(at.wt, 3, k), no[k]);
-        const bool live = t0 + k < at.len;
-#pragma unroll
-        for (int v = 0; v < VEC; ++v) {
-          f[k][v] = glr_gate(f[k][v], i[k][v]);
-          e[k][v] *= a.alpha;
-          if constexpr (GATE) e[k][v] *= glr_gate(no[k][v], no[k][v]);
-          if (!live) {
-            f[k][v] = 1.f;
-            i[k][v] = g[k][v] = e[k][v] = 0.f;
-            if constexpr (GATE) no[k][v] = 0.f;
+        f[k] = glr_gate(glr_unpack<T, VEC>(in.raw(at.wt, 0, k)), i[k]);
+        g[k] = glr_unpack<T, VEC>(in.raw(at.wt, 1, k));
+        e[k] = alpha * glr_unpack<T, VEC>(in.raw(at.wt, 2, k));
+        if constexpr (GATE) e[k] = e[k] * glr_gate(glr_unpack<T, VEC>(in.raw(at.wt, 3, k)), no[k]);
+        if constexpr (!FULL)
+          if (t0 + k >= at.len) {
+            f[k] = V::all(1.f);
+            i[k] = g[k] = e[k] = V::all(0.f);
+            if constexpr (GATE) no[k] = V::all(0.f);
           }
-          map.a[v] *= f[k][v];
-          map.b[v] = fmaf(f[k][v], map.b[v], i[k][v] * g[k][v]);
-        }
+        const V b = i[k] * g[k];
+        if (k == 0) map = {f[0], b};
+        else map.then({f[k], b});
       }
       if constexpr (!BULK)
         if (it + 1 < sp.rounds) in.fetch(start(it + 1) + at.wt * SPT, at.len);
+      back.a = map.a;
+      back.b = f[SPT - 1] * e[SPT - 1];
 #pragma unroll
-      for (int v = 0; v < VEC; ++v) {
-        back.a[v] = map.a[v];
-        back.b[v] = 0.f;
-#pragma unroll
-        for (int k = SPT - 1; k >= 0; --k) back.b[v] = f[k][v] * (e[k][v] + back.b[v]);
-      }
-      GlrMap<VEC> before = GlrMap<VEC>::none();
+      for (int k = SPT - 2; k >= 0; --k) back.b = f[k] * (e[k] + back.b);
       if constexpr (WT > 1) {
-        s_warp[mail & 1][at.wt][at.ch] = map;
-        s_back[mail & 1][at.wt][at.ch] = back;
+        s_states[mail & 1][at.wt][at.ch] = map;
+        sh.warp[mail & 1][at.wt][at.ch] = back;
         __syncthreads();
-#pragma unroll
-        for (int w = 0; w < WT - 1; ++w)
-          if (w < at.wt) before.then(s_warp[mail & 1][w][at.ch]);
       }
       if constexpr (BULK) {
         if (threadIdx.x == 0) in.ask(a, sp, tiles, CL, rank, clusters, true);
         in.next();
       }
-      float q[VEC];
-      glr_exchange<VEC, CW, WT>(at.wt, at.ch, mail, mail & 1, CL, rank, false, back, s_back, &post, qs, q, &s_gone, a.status);
-      float c[SPT + 1][VEC];
+      q = glr_enter<false>(sh, at.wt, at.ch, it == 0, mail, CL, rank, first, a.status);
+      V c[SPT + 1];
+      c[0] = c0;
+      if constexpr (WT > 1)
+        for (int w = 0; w < at.wt; ++w) c[0] = s_states[mail & 1][w][at.ch].of(c[0]);
 #pragma unroll
-      for (int v = 0; v < VEC; ++v) {
-        c[0][v] = before.of(c0[v], v);
-#pragma unroll
-        for (int k = 0; k < SPT; ++k) c[k + 1][v] = fmaf(f[k][v], c[k][v], i[k][v] * g[k][v]);
-      }
+      for (int k = 0; k < SPT; ++k) c[k + 1] = glr_fma(f[k], c[k], i[k] * g[k]);
       size_t row = (size_t)(t0 + SPT - 1) * step_d;
 #pragma unroll
       for (int k = SPT - 1; k >= 0; --k) {
-        float of[VEC], og[VEC], oo[VEC];
-        const bool live = t0 + k < at.len;
-#pragma unroll
-        for (int v = 0; v < VEC; ++v) {
-          const float d = e[k][v] + q[v], di = d * i[k][v];
-          q[v] = f[k][v] * d;
-          of[v] = live ? di * f[k][v] * (c[k][v] - g[k][v]) : 0.f;
-          og[v] = live ? di : 0.f;
-          if constexpr (GATE) oo[v] = live ? e[k][v] * c[k + 1][v] * no[k][v] : 0.f;
-        }
-        if (t0 + k < a.T) {
-          glr_store<T, VEC>(dzf + row, at.valid, of);
-          glr_store<T, VEC>(dzg + row, at.valid, og);
-          if constexpr (GATE) glr_store<T, VEC>(dzo + row, at.valid, oo);
+        const V d = e[k] + q, di = d * i[k];
+        q = f[k] * d;
+        V of = (di * f[k]) * glr_fma(g[k], minus, c[k]), og = di, oo;
+        if constexpr (GATE) oo = (e[k] * no[k]) * c[k + 1];
+        if constexpr (FULL) {
+          glr_store<T, VEC>(dzf + row, VEC, of);
+          glr_store<T, VEC>(dzg + row, VEC, og);
+          if constexpr (GATE) glr_store<T, VEC>(dzo + row, VEC, oo);
+        } else {
+          if (t0 + k >= at.len) {
+            of = og = V::all(0.f);
+            if constexpr (GATE) oo = of;
+          }
+          if (t0 + k < a.T) {
+            glr_store<T, VEC>(dzf + row, at.valid, of);
+            glr_store<T, VEC>(dzg + row, at.valid, og);
+            if constexpr (GATE) glr_store<T, VEC>(dzo + row, at.valid, oo);
+          }
         }
         row -= step_d;
       }
+      if (WT > 1 && CL == 1 && at.wt == 0) sh.state[(mail & 1) ^ 1][at.ch] = q;
+    };
+    for (int it = 0; it < sp.rounds; ++it, ++mail) {
+      if constexpr (BULK) in.wait(a.status);
+      // (the round's last slab is rank 0's)
+      if (inside && (sp.rounds - it) * CL * SLAB <= at.len) slab(std::true_type{}, it);
+      else slab(std::false_type{}, it);
     }
-    if (a.hT && rank == 0 && at.wt == 0)
+    if (a.hT && rank == 0 && at.wt == 0) {
+      const V behind = WT > 1 && sp.rounds > 0 ? sh.state[mail & 1][at.ch] : q;
 #pragma unroll
       for (int v = 0; v < VEC; ++v)
-        if (v < at.valid) a.hT[at.of(a, sp, v)] = qs[v];
+        if (v < at.valid) a.hT[at.of(a, sp, v)] = behind.v[v];
+    }
   }
   if constexpr (BULK)
     if (threadIdx.x == 0) in.drain();
