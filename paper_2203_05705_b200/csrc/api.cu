@@ -237,6 +237,7 @@ ard_status ard_create(ard_ctx** out, int device, size_t workspace_bytes) {
   ctx->d_lstm_hc = nullptr;
   ctx->lstm_compact_h = 1;
   ctx->lstm_refuse = 0;
+  for (int& room : ctx->glr_room) room = 0;
   ctx->pdl_in_capture = 1;
   ctx->mlp_two_streams = 1;
   ctx->mlp_persistent = 1;

@@ -21,7 +21,7 @@ namespace {
 
 namespace cg = cooperative_groups;
 
-constexpr int GLR_CLUSTER = 8;  // most CTAs that share a sequence
+constexpr int GLR_CLUSTER = 16;  // most CTAs that share a sequence
 
 struct GlrArgs {
   const int32_t* hdr;  // nullptr: all H units
@@ -288,11 +288,11 @@ struct GlrFeed<T, VEC, M, WT, SPT, false> {
 
 // The maps of a slab's warps meet in `warp`; its last warp (in the order of the recurrence) leaves the state behind the round in `state`, where the
 // next round finds it.  The cluster's CTAs send each other their slabs' maps by asynchronous stores that count on the receiver's
-// barrier: a barrier of the cluster would wait for the outputs' stores, 2 us a round.  Every CTA hears from all of them in every round, so none is
-// more than a round ahead and two sets of places are enough.
-template <int VEC, int CW>
+// barrier: a barrier of the cluster would wait for the outputs' stores, 2 us a round (bulk copies between their memories: forward the same, backward
+// 30 % slower).  Every CTA hears from all of them in every round, so none is more than a round ahead and two sets of places are enough.
+template <int VEC, int CW, int FROM>
 struct GlrMail {
-  GlrMap<VEC> box[2][GLR_CLUSTER][CW * 32];
+  GlrMap<VEC> box[2][FROM][CW * 32];
   uint64_t bar[2];
 };
 template <int VEC>
@@ -313,7 +313,7 @@ template <int VEC, int CW, int WT>
 struct GlrShared {
   GlrMap<VEC> warp[2][WT][CW * 32];
   GlrV<VEC> state[2][CW * 32];
-  GlrMail<VEC, CW> post;
+  GlrMail<VEC, CW, (WT > 1 ? GLR_CLUSTER : 1)> post;
   uint64_t full[3];
   int gone;
 };
@@ -370,7 +370,7 @@ __device__ __forceinline__ void glr_setup(int CL, Shared& sh) {
 }
 
 template <typename T, int VEC, bool GATE, int CW, int WT, int SPT, bool BULK>
-__global__ void __launch_bounds__(CW* WT * 32, CW* WT == 8 ? 2 : 1)
+__global__ void __launch_bounds__(CW* WT * 32, CW* WT < 8 || SPT == 16 ? 1 : SPT < 8 ? 3 : 2)
     glr_fwd_kernel(const GlrArgs a, int CL, const __grid_constant__ GlrTiles tiles) {
   using V = GlrV<VEC>;
   constexpr int M = GATE ? 3 : 2, SLAB = WT * SPT;
@@ -471,7 +471,7 @@ __global__ void __launch_bounds__(CW* WT * 32, CW* WT == 8 ? 2 : 1)
 }
 
 template <typename T, int VEC, bool GATE, int CW, int WT, int SPT, bool BULK>
-__global__ void __launch_bounds__(CW* WT * 32, CW* WT == 8 ? 2 : 1)
+__global__ void __launch_bounds__(CW* WT * 32, CW* WT < 8 || SPT == 16 ? 1 : SPT < 8 ? 3 : 2)
     glr_bwd_kernel(const GlrArgs a, int CL, const __grid_constant__ GlrTiles tiles) {
   using V = GlrV<VEC>;
   constexpr int M = GATE ? 4 : 3, SLAB = WT * SPT;
@@ -518,7 +518,8 @@ __global__ void __launch_bounds__(CW* WT * 32, CW* WT == 8 ? 2 : 1)
       for (int v = 0; v < VEC; ++v)
         c0.v[v] = ts < a.T && v < at.valid ? a.S[((size_t)(ts / ARD_GLR_CHUNK) * a.B + at.b) * a.H + at.j + v] : 0.f;
       // e: alpha s(zo) dy, what arrives at c from y; no: 1 - s(zo)
-      V f[SPT], i[SPT], g[SPT], e[SPT], no[GATE ? SPT : 1];
+      V f[SPT], i[SPT], g[SPT], e[SPT];
+      [[maybe_unused]] V no[GATE ? SPT : 1];
       GlrMap<VEC> map, back;
 #pragma unroll
       for (int k = 0; k < SPT; ++k) {
@@ -563,7 +564,8 @@ __global__ void __launch_bounds__(CW* WT * 32, CW* WT == 8 ? 2 : 1)
       for (int k = SPT - 1; k >= 0; --k) {
         const V d = e[k] + q, di = d * i[k];
         q = f[k] * d;
-        V of = (di * f[k]) * glr_fma(g[k], minus, c[k]), og = di, oo;
+        V of = (di * f[k]) * glr_fma(g[k], minus, c[k]), og = di;
+        [[maybe_unused]] V oo;
         if constexpr (GATE) oo = (e[k] * no[k]) * c[k + 1];
         if constexpr (FULL) {
           glr_store<T, VEC>(dzf + row, VEC, of);
@@ -611,21 +613,25 @@ inline bool glr_pairs(std::initializer_list<const void*> ps, std::initializer_li
   return true;
 }
 
-// A cluster's CTAs take consecutive slabs of the time axis where the channels alone leave SMs idle.  With bulk copies the grid is what
-// the device holds at once (two CTAs an SM) and a CTA goes from unit to unit, its copies ahead of it; without, a CTA per unit.
+template <typename F>
+constexpr int glr_ring() { return F::SLOTS * F::SLOT; }
+
+inline long long glr_units(const GlrArgs& a, int channels) { return (long long)((a.H + channels - 1) / channels) * a.B; }
+
+// With bulk copies the grid is what the device holds at once (per_sm CTAs an SM) and a CTA goes from unit to unit, its copies ahead of it; without, a
+// CTA (a cluster) per unit.
 template <typename K>
-ard_status glr_launch(ard_ctx* ctx, K kern, const GlrArgs& a, const GlrTiles& tiles, int channels, int slab, int threads, int smem,
+ard_status glr_launch(ard_ctx* ctx, K kern, const GlrArgs& a, const GlrTiles& tiles, int channels, int CL, int threads, int smem, int per_sm,
                       cudaStream_t s) {
-  const long long slabs = ((long long)a.T + slab - 1) / slab, units = (long long)((a.H + channels - 1) / channels) * a.B;
-  const int resident = 2 * ctx->sm_count;
-  int CL = 1;
-  while (CL < GLR_CLUSTER && 2 * CL <= slabs && units * 2 * CL <= resident) CL *= 2;
+  const long long units = glr_units(a, channels);
   long long blocks = units * CL;
+  if (units > 0x7FFFFFFFll || blocks > 0x7FFFFFFFll) return ARD_ERR_UNSUPPORTED;
+  if (CL > 8) ARD_CUDA_OK(cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
   if (smem > 0) {
     ARD_CUDA_OK(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
-    if (blocks > resident) blocks = resident;
+    const int resident = per_sm * ctx->sm_count;
+    if (blocks > resident) blocks = resident / CL * CL;
   }
-  if (units > 0x7FFFFFFFll || blocks > 0x7FFFFFFFll) return ARD_ERR_UNSUPPORTED;
   if (CL > 1) ARD_CUDA_OK(ard_launch_cluster(ctx, kern, CL, dim3((unsigned)blocks), dim3(threads), smem, s, a, CL, tiles));
   else ARD_CUDA_OK(ard_launch(ctx, kern, dim3((unsigned)blocks), dim3(threads), smem, s, a, CL, tiles));
   ctx->launches++;
@@ -633,8 +639,23 @@ ard_status glr_launch(ard_ctx* ctx, K kern, const GlrArgs& a, const GlrTiles& ti
   return ARD_OK;
 }
 
-template <typename F>
-constexpr int glr_ring() { return F::SLOTS * F::SLOT; }
+// CTAs of a cluster that share a sequence's slabs (128 steps each, a CTA an SM), where the units alone leave more than half of the SMs idle: as many as
+// let all units run at once.  How many clusters of a size the device holds goes by how its SMs are grouped, and is asked once.
+inline int glr_cluster(ard_ctx* ctx, long long units, long long slabs) {
+  if (2 * units > ctx->sm_count || slabs < 2) return 1;
+  if (ctx->glr_room[2] == 0) {
+    auto kern = glr_fwd_kernel<__nv_bfloat16, 2, true, 1, 8, 16, true>;
+    constexpr int smem = glr_ring<GlrFeed<__nv_bfloat16, 2, 3, 8, 16, true>>();
+    cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    for (int cl = 2; cl <= GLR_CLUSTER; ++cl) ctx->glr_room[cl] = ard_cluster_room(ctx, kern, cl, 256, smem) / cl;
+    (void)cudaGetLastError();
+  }
+  int CL = GLR_CLUSTER;
+  while (CL > 1 && (CL > slabs || ctx->glr_room[CL] < units)) --CL;
+  const long long rounds = (slabs + CL - 1) / CL;
+  return (int)((slabs + rounds - 1) / rounds);
+}
 
 // Descriptors [T][B][H] of the M operands; false: not on a 16-byte grid.
 template <typename T, int VEC>
@@ -647,36 +668,53 @@ bool glr_tiles(ard_ctx* ctx, const GlrArgs& a, std::initializer_list<std::pair<c
   return true;
 }
 
+// Steps of a thread.  As few as a short sequence's slab of 8 warps needs (three CTAs an SM: 35 x 64 x 1024 11.3 -> 8.7 us); 16 (one CTA an SM) where
+// clusters share the sequences, since what a round costs besides its steps is then paid half as often; 8 otherwise.  run(SPT, CTAs an SM, cluster).
+template <typename Run>
+ard_status glr_steps(ard_ctx* ctx, const GlrArgs& a, int channels, Run run) {
+  if (a.T <= 16) return run(std::integral_constant<int, 2>{}, 3, 1);
+  if (a.T <= 40) return run(std::integral_constant<int, 5>{}, 3, 1);
+  const int CL = glr_cluster(ctx, glr_units(a, channels), ((long long)a.T + 127) / 128);
+  if (CL > 1) return run(std::integral_constant<int, 16>{}, 1, CL);
+  return run(std::integral_constant<int, 8>{}, 2, 1);
+}
+
 template <typename T, int VEC, bool GATE>
 struct GlrFwd {
   static ard_status run(ard_ctx* ctx, const GlrArgs& a, cudaStream_t s) {
     GlrTiles tiles;
-    if (a.T <= 1) return glr_launch(ctx, glr_fwd_kernel<T, VEC, GATE, 4, 1, 1, false>, a, tiles, 4 * 32 * VEC, 1, 128, 0, s);
-    if constexpr (VEC * sizeof(T) == 4) {
-      bool ok;
-      if constexpr (GATE) ok = glr_tiles<T, VEC>(ctx, a, {{a.Zf, a.ldz}, {a.Zg, a.ldz}, {a.Zo, a.ldz}}, 64, &tiles);
-      else ok = glr_tiles<T, VEC>(ctx, a, {{a.Zf, a.ldz}, {a.Zg, a.ldz}}, 64, &tiles);
-      if (ok)
-        return glr_launch(ctx, glr_fwd_kernel<T, VEC, GATE, 1, 8, 8, true>, a, tiles, 32 * VEC, 64, 256,
-                          glr_ring<GlrFeed<T, VEC, GATE ? 3 : 2, 8, 8, true>>(), s);
-    }
-    return glr_launch(ctx, glr_fwd_kernel<T, VEC, GATE, 1, 8, 8, false>, a, tiles, 32 * VEC, 64, 256, 0, s);
+    if (a.T <= 1) return glr_launch(ctx, glr_fwd_kernel<T, VEC, GATE, 4, 1, 1, false>, a, tiles, 4 * 32 * VEC, 1, 128, 0, 8, s);
+    return glr_steps(ctx, a, 32 * VEC, [&](auto steps, int per_sm, int CL) {
+      constexpr int SPT = decltype(steps)::value;
+      if constexpr (VEC * sizeof(T) == 4) {
+        bool ok;
+        if constexpr (GATE) ok = glr_tiles<T, VEC>(ctx, a, {{a.Zf, a.ldz}, {a.Zg, a.ldz}, {a.Zo, a.ldz}}, 8 * SPT, &tiles);
+        else ok = glr_tiles<T, VEC>(ctx, a, {{a.Zf, a.ldz}, {a.Zg, a.ldz}}, 8 * SPT, &tiles);
+        if (ok)
+          return glr_launch(ctx, glr_fwd_kernel<T, VEC, GATE, 1, 8, SPT, true>, a, tiles, 32 * VEC, CL, 256,
+                            glr_ring<GlrFeed<T, VEC, GATE ? 3 : 2, 8, SPT, true>>(), per_sm, s);
+      }
+      return glr_launch(ctx, glr_fwd_kernel<T, VEC, GATE, 1, 8, SPT, false>, a, tiles, 32 * VEC, CL, 256, 0, per_sm, s);
+    });
   }
 };
 template <typename T, int VEC, bool GATE>
 struct GlrBwd {
   static ard_status run(ard_ctx* ctx, const GlrArgs& a, cudaStream_t s) {
     GlrTiles tiles;
-    if (a.T <= 1) return glr_launch(ctx, glr_bwd_kernel<T, VEC, GATE, 4, 1, 1, false>, a, tiles, 4 * 32 * VEC, 1, 128, 0, s);
-    if constexpr (VEC * sizeof(T) == 4) {
-      bool ok;
-      if constexpr (GATE) ok = glr_tiles<T, VEC>(ctx, a, {{a.Zf, a.ldz}, {a.Zg, a.ldz}, {a.dY, a.ldy}, {a.Zo, a.ldz}}, 64, &tiles);
-      else ok = glr_tiles<T, VEC>(ctx, a, {{a.Zf, a.ldz}, {a.Zg, a.ldz}, {a.dY, a.ldy}}, 64, &tiles);
-      if (ok)
-        return glr_launch(ctx, glr_bwd_kernel<T, VEC, GATE, 1, 8, 8, true>, a, tiles, 32 * VEC, 64, 256,
-                          glr_ring<GlrFeed<T, VEC, GATE ? 4 : 3, 8, 8, true>>(), s);
-    }
-    return glr_launch(ctx, glr_bwd_kernel<T, VEC, GATE, 1, 8, 8, false>, a, tiles, 32 * VEC, 64, 256, 0, s);
+    if (a.T <= 1) return glr_launch(ctx, glr_bwd_kernel<T, VEC, GATE, 4, 1, 1, false>, a, tiles, 4 * 32 * VEC, 1, 128, 0, 8, s);
+    return glr_steps(ctx, a, 32 * VEC, [&](auto steps, int per_sm, int CL) {
+      constexpr int SPT = decltype(steps)::value;
+      if constexpr (VEC * sizeof(T) == 4) {
+        bool ok;
+        if constexpr (GATE) ok = glr_tiles<T, VEC>(ctx, a, {{a.Zf, a.ldz}, {a.Zg, a.ldz}, {a.dY, a.ldy}, {a.Zo, a.ldz}}, 8 * SPT, &tiles);
+        else ok = glr_tiles<T, VEC>(ctx, a, {{a.Zf, a.ldz}, {a.Zg, a.ldz}, {a.dY, a.ldy}}, 8 * SPT, &tiles);
+        if (ok)
+          return glr_launch(ctx, glr_bwd_kernel<T, VEC, GATE, 1, 8, SPT, true>, a, tiles, 32 * VEC, CL, 256,
+                            glr_ring<GlrFeed<T, VEC, GATE ? 4 : 3, 8, SPT, true>>(), per_sm, s);
+      }
+      return glr_launch(ctx, glr_bwd_kernel<T, VEC, GATE, 1, 8, SPT, false>, a, tiles, 32 * VEC, CL, 256, 0, per_sm, s);
+    });
   }
 };
 
