@@ -776,8 +776,8 @@ typedef struct ard_adamw_tensor {
 ard_status ard_adamw_step(ard_ctx* ctx, const ard_adamw_tensor* tensors, int n_tensors, double lr, double beta1, double beta2,
                           double eps, int state_bits, uint64_t seed, uint64_t step, const uint64_t* step_counter,
                           const float* lr_factor, const float* grad_factor, void* cuda_stream);
-/* The 2-norm over all gradients of the same table (only rows, cols, g, ldg, g_dtype are looked at), squares and sums in
- * fp64 in a fixed order: out[0] = norm (DEVICE float[2]), out[1] = min(1, max_norm / (norm + 1e-6)), or NaN where the norm is not
+/* The 2-norm over all gradients of the same table (only rows, cols, g, ldg, g_dtype are looked at), summed in fp64 in a
+ * fixed order (eight squares at a time in fp32 where their range allows it): out[0] = norm (DEVICE float[2]), out[1] = min(1, max_norm / (norm + 1e-6)), or NaN where the norm is not
  * finite: the grad_factor of ard_adamw_step.  max_norm <= 0: out[1] = 1 unless the norm is not finite.  Uses the
  * context's scratch.  Asynchronous. */
 ard_status ard_grad_norm(ard_ctx* ctx, const ard_adamw_tensor* tensors, int n_tensors, double max_norm, float* out,

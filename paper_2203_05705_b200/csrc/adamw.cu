@@ -135,6 +135,33 @@ __device__ __forceinline__ void aw_decode(uint32_t q, float scale, float (&v)[4]
   }
 }
 
+// 1 / x and sqrt(x) to the last bit or two in a few instructions: the instructions' approximations, improved once by Newton's step, in place of
+// division and square root rounded to the last bit (8 to 20 instructions each with their special cases).  What is rounded to 8 bits is worth the
+// step: an error of one unit more in the last place is a few values in a million more that fall on the other side of a border.
+__device__ __forceinline__ float aw_inverse(float x) {  // x normal
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return fmaf(r, fmaf(-x, r, 1.f), r);
+}
+__device__ __forceinline__ float aw_root(float x) {  // subnormal: 0
+  float r;
+  asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  const float s = x * r;
+  const float better = fmaf(0.5f * r, fmaf(-s, s, x), s);
+  return x < 1.17549435e-38f ? 0.f : better;
+}
+// The quotient of the step, and its root, which no rounding follows but the parameter's.
+__device__ __forceinline__ float aw_quick_root(float x) {
+  float r;
+  asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+__device__ __forceinline__ float aw_quick_inverse(float x) {
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+
 // a >= 0 rounded to the grid of the 8-bit floats (3 bits of mantissa; steps of 2^-9 below 2^-6), up with the probability of what is
 // cut off, which 16 random bits resolve to 2^-16 of a step.  Below 2^-6 the grid is that of [2^-6, 2^-5): adding 2^-6 puts the
 // value there.  The sum of the bits carries into the exponent where it should.
@@ -154,8 +181,8 @@ __device__ __forceinline__ uint32_t aw_encode(const float (&v)[4], const uint32_
   const uint32_t bits = __reduce_max_sync(0xFFFFFFFFu, nan ? 0x7FC00000u : __float_as_uint(mine));  // of values >= 0, in their order
   const float big = __uint_as_float(bits);
   const bool none = big < AW_TINY;
-  const float inv = none ? 0.f : E4M3_MAX / big;
-  scale = none ? 0.f : big / E4M3_MAX;
+  const float inv = none ? 0.f : E4M3_MAX * aw_inverse(big);
+  scale = none ? 0.f : big * (1.f / E4M3_MAX);
   float q[4];
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
@@ -172,81 +199,151 @@ __device__ __forceinline__ uint32_t aw_encode(const float (&v)[4], const uint32_
 constexpr int AW_QUADS = 2;
 constexpr int AW_TILE = AW_QUADS * AW_THREADS * 4;
 
+// What is the same for all elements of a launch, and of a tensor.
+struct AwStep {
+  float gf, beta1, beta2, omb1, omb2, eps, root_lift2, step1, lr_decay;
+  unsigned long long t, seed;
+};
+
+template <int BITS>
+struct AwState {
+  float m[4], v[4];
+  uint32_t mq, vq;
+  float ms, vs;
+};
+
+// Four elements from i on (n, flat: see aw_load4).  WHOLE: all of them are there, flat.
+template <int BITS, bool WHOLE>
+__device__ __forceinline__ void aw_fetch(const AwEntry& e, long long i, bool flat, float (&p)[4], float (&g)[4], AwState<BITS>& st) {
+  const long long n = WHOLE ? i + 4 : e.n;
+  const bool f = WHOLE || flat;
+  aw_load4(e.p, i, n, e.cols, e.ldp, f, p);
+  if (e.g_is_bf16) aw_load4((const __nv_bfloat16*)e.g, i, n, e.cols, e.ldg, f, g);
+  else aw_load4((const float*)e.g, i, n, e.cols, e.ldg, f, g);
+  if constexpr (BITS == 32) {
+    aw_load4((const float*)e.m, i, n, 1, 1, f, st.m);
+    aw_load4((const float*)e.v, i, n, 1, 1, f, st.v);
+  } else {
+    st.mq = aw_load_codes((const uint8_t*)e.m, i, n, f);
+    st.vq = aw_load_codes((const uint8_t*)e.v, i, n, f);
+    st.ms = e.m_scale[i >> 7];
+    st.vs = e.v_scale[i >> 7];
+  }
+}
+template <int BITS, bool WHOLE>
+__device__ __forceinline__ void aw_update(const AwEntry& e, const AwStep& a, long long i, bool flat, float (&p)[4], float (&g)[4],
+                                          AwState<BITS>& st) {
+  const long long n = WHOLE ? i + 4 : e.n;
+  const bool f = WHOLE || flat;
+  float (&m)[4] = st.m;
+  float (&v)[4] = st.v;
+  float r[4];
+  if constexpr (BITS == 8) {
+    aw_decode(st.mq, st.ms, m);
+    aw_decode(st.vq, st.vs, v);
+  }
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const float gk = g[k] * a.gf;
+    m[k] = fmaf(a.beta1, m[k], a.omb1 * gk);
+    v[k] = fmaf(a.beta2, BITS == 32 ? v[k] : v[k] * v[k], a.omb2 * gk * gk);
+    r[k] = BITS == 32 ? aw_quick_root(v[k]) : aw_root(v[k]);
+    const float move = a.step1 * m[k] * aw_quick_inverse(fmaf(r[k], a.root_lift2, a.eps));
+    p[k] = p[k] - fmaf(a.lr_decay, p[k], move);
+  }
+  aw_store4(e.p, i, n, e.cols, e.ldp, f, p);
+  if (e.w) aw_store4(e.w, i, n, e.cols, e.ldw, f, p);
+  if constexpr (BITS == 32) {
+    aw_store4((float*)e.m, i, n, 1, 1, f, m);
+    aw_store4((float*)e.v, i, n, 1, 1, f, v);
+  } else {
+    uint32_t c[4] = {(uint32_t)a.t, (uint32_t)(a.t >> 32), (uint32_t)(i >> 2), e.number};
+    philox4x32_10(c, (uint32_t)a.seed, (uint32_t)(a.seed >> 32));
+    uint32_t low[4], high[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      low[k] = c[k] & 0xFFFFu;
+      high[k] = c[k] >> 16;
+      if (!WHOLE && i + k >= n) m[k] = r[k] = 0.f;
+    }
+    float ms, vs;
+    const uint32_t mq = aw_encode<false>(m, low, ms), vq = aw_encode<true>(r, high, vs);
+    aw_store_codes((uint8_t*)e.m, i, n, f, mq);
+    aw_store_codes((uint8_t*)e.v, i, n, f, vq);
+    if ((threadIdx.x & 31) == 0) {
+      e.m_scale[i >> 7] = ms;
+      e.v_scale[i >> 7] = vs;
+    }
+  }
+}
+
 template <int BITS, int CAP>
-__global__ void __launch_bounds__(AW_THREADS) adamw_kernel(const __grid_constant__ AwTable<CAP> table, const AwArgs a) {
+__global__ void __launch_bounds__(AW_THREADS, 4) adamw_kernel(const __grid_constant__ AwTable<CAP> table, const AwArgs a) {
   __shared__ float s_lift[2];
   pdl_launch_dependents();
   pdl_wait_prior_grids();
-  const unsigned long long t = a.step + (a.counter ? *a.counter : 0ull);
-  if (t == 0) return;
-  const float gf = a.grad_factor ? *a.grad_factor : 1.f;
-  if (!(fabsf(gf) < INFINITY)) return;
+  AwStep st;
+  st.t = a.step + (a.counter ? *a.counter : 0ull);
+  if (st.t == 0) return;
+  st.gf = a.grad_factor ? *a.grad_factor : 1.f;
+  if (!(fabsf(st.gf) < INFINITY)) return;
   const float lr = a.lr_factor ? a.lr * *a.lr_factor : a.lr;
-  if (threadIdx.x < 2) s_lift[threadIdx.x] = (float)(-1.0 / expm1((double)t * (threadIdx.x ? a.ln_beta2 : a.ln_beta1)));
+  if (threadIdx.x < 2) {
+    const double lift = -1.0 / expm1((double)st.t * (threadIdx.x ? a.ln_beta2 : a.ln_beta1));
+    s_lift[threadIdx.x] = (float)(threadIdx.x ? sqrt(lift) : lift);
+  }
   __syncthreads();
-  const float lift2 = s_lift[1], step1 = lr * s_lift[0];
+  st.root_lift2 = s_lift[1];
+  st.step1 = lr * s_lift[0];
+  st.beta1 = a.beta1;
+  st.beta2 = a.beta2;
+  st.omb1 = a.one_minus_beta1;
+  st.omb2 = a.one_minus_beta2;
+  st.eps = a.eps;
+  st.seed = a.seed;
   for (unsigned long long tile = blockIdx.x; tile < table.tiles; tile += gridDim.x) {
     const AwEntry& e = table.e[aw_find(table, tile)];
-    const long long n = e.n, base = (long long)(tile - e.tile0) * AW_TILE;
-    const bool flat = e.flat;
+    const long long base = (long long)(tile - e.tile0) * AW_TILE;
+    st.lr_decay = lr * e.decay;
+    if (e.flat && base + AW_TILE <= e.n) {
+      // all loads of the tile before its first store
+      float p[AW_QUADS][4], g[AW_QUADS][4];
+      AwState<BITS> state[AW_QUADS];
 #pragma unroll
-    for (int u = 0; u < AW_QUADS; ++u) {
-      const long long i = base + (u * AW_THREADS + threadIdx.x) * 4;
-      if (BITS == 32 ? i >= n : (i & ~127ll) >= n) continue;  // (8 bits: a block's lanes stay together)
-      float p[4], g[4], m[4], v[4];
-      aw_load4(e.p, i, n, e.cols, e.ldp, flat, p);
-      if (e.g_is_bf16) aw_load4((const __nv_bfloat16*)e.g, i, n, e.cols, e.ldg, flat, g);
-      else aw_load4((const float*)e.g, i, n, e.cols, e.ldg, flat, g);
-      if (BITS == 32) {
-        aw_load4((const float*)e.m, i, n, 1, 1, flat, m);
-        aw_load4((const float*)e.v, i, n, 1, 1, flat, v);
-      } else {
-        const long long b = i >> 7;
-        aw_decode(aw_load_codes((const uint8_t*)e.m, i, n, flat), e.m_scale[b], m);
-        aw_decode(aw_load_codes((const uint8_t*)e.v, i, n, flat), e.v_scale[b], v);
-      }
-      float r[4];
+      for (int u = 0; u < AW_QUADS; ++u) aw_fetch<BITS, true>(e, base + (u * AW_THREADS + threadIdx.x) * 4, true, p[u], g[u], state[u]);
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const float gk = g[k] * gf;
-        m[k] = fmaf(a.beta1, m[k], a.one_minus_beta1 * gk);
-        const float old = BITS == 32 ? v[k] : v[k] * v[k];
-        v[k] = fmaf(a.beta2, old, a.one_minus_beta2 * gk * gk);
-        r[k] = BITS == 32 ? 0.f : sqrtf(v[k]);
-        const float move = step1 * m[k] / (sqrtf(v[k] * lift2) + a.eps);
-        p[k] = p[k] - fmaf(lr * e.decay, p[k], move);
-      }
-      aw_store4(e.p, i, n, e.cols, e.ldp, flat, p);
-      if (e.w) aw_store4(e.w, i, n, e.cols, e.ldw, flat, p);
-      if (BITS == 32) {
-        aw_store4((float*)e.m, i, n, 1, 1, flat, m);
-        aw_store4((float*)e.v, i, n, 1, 1, flat, v);
-      } else {
-        uint32_t c[4] = {(uint32_t)t, (uint32_t)(t >> 32), (uint32_t)(i >> 2), e.number};
-        philox4x32_10(c, (uint32_t)a.seed, (uint32_t)(a.seed >> 32));
-        uint32_t low[4], high[4];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          low[k] = c[k] & 0xFFFFu;
-          high[k] = c[k] >> 16;
-          if (i + k >= n) m[k] = r[k] = 0.f;
-        }
-        float ms, vs;
-        const uint32_t mq = aw_encode<false>(m, low, ms), vq = aw_encode<true>(r, high, vs);
-        aw_store_codes((uint8_t*)e.m, i, n, flat, mq);
-        aw_store_codes((uint8_t*)e.v, i, n, flat, vq);
-        if ((threadIdx.x & 31) == 0) {
-          e.m_scale[i >> 7] = ms;
-          e.v_scale[i >> 7] = vs;
-        }
+      for (int u = 0; u < AW_QUADS; ++u) aw_update<BITS, true>(e, st, base + (u * AW_THREADS + threadIdx.x) * 4, true, p[u], g[u], state[u]);
+    } else {
+#pragma unroll 1
+      for (int u = 0; u < AW_QUADS; ++u) {
+        const long long i = base + (u * AW_THREADS + threadIdx.x) * 4;
+        if (BITS == 32 ? i >= e.n : (i & ~127ll) >= e.n) continue;  // (8 bits: a block's lanes stay together)
+        float p[4], g[4];
+        AwState<BITS> state;
+        aw_fetch<BITS, false>(e, i, e.flat, p, g, state);
+        aw_update<BITS, false>(e, st, i, e.flat, p, g, state);
       }
     }
   }
 }
 
 // ---- norm of all gradients ------------------------------------------------------------------------
-constexpr int GN_QUADS = 4;
-constexpr int GN_TILE = GN_QUADS * AW_THREADS * 4;
+constexpr int GN_EIGHTS = 4;
+constexpr int GN_TILE = GN_EIGHTS * AW_THREADS * 8;
+
+// The squares of eight values.  Added in fp32 where that is as good: a sum that neither overflowed nor lies where squares lose their bits
+// (the additions' errors, of either sign, go under in millions of such sums).  Otherwise in fp64, which converts every value: 68 us in place of 24 for
+// 64 Mi bf16 values.
+__device__ __forceinline__ double gn_squares(const float (&g)[8]) {
+  float s = 0.f;
+#pragma unroll
+  for (int k = 0; k < 8; ++k) s = fmaf(g[k], g[k], s);
+  if (s > 8.3e-25f && s < INFINITY) return (double)s;
+  double x = 0.0;
+#pragma unroll
+  for (int k = 0; k < 8; ++k) x = fma((double)g[k], (double)g[k], x);
+  return x;
+}
 
 // Every CTA leaves the sum of its squares; the last one of the last launch adds them in the order of the CTAs.
 template <int CAP>
@@ -260,17 +357,47 @@ __global__ void __launch_bounds__(AW_THREADS) grad_norm_kernel(const __grid_cons
   for (unsigned long long tile = blockIdx.x; tile < table.tiles; tile += gridDim.x) {
     const AwEntry& e = table.e[aw_find(table, tile)];
     const long long base = (long long)(tile - e.tile0) * GN_TILE;
-    float g[GN_QUADS][4];
+    const int t = (int)threadIdx.x;
+    float g[GN_EIGHTS][8];
+    if (e.flat && base + GN_TILE <= e.n) {
+      if (e.g_is_bf16) {
+        uint4 q[GN_EIGHTS];
 #pragma unroll
-    for (int u = 0; u < GN_QUADS; ++u) {
-      const long long i = base + (u * AW_THREADS + threadIdx.x) * 4;
-      if (e.g_is_bf16) aw_load4((const __nv_bfloat16*)e.g, i, e.n, e.cols, e.ldg, e.flat, g[u]);
-      else aw_load4((const float*)e.g, i, e.n, e.cols, e.ldg, e.flat, g[u]);
+        for (int u = 0; u < GN_EIGHTS; ++u) q[u] = *reinterpret_cast<const uint4*>((const __nv_bfloat16*)e.g + base + (u * AW_THREADS + t) * 8);
+#pragma unroll
+        for (int u = 0; u < GN_EIGHTS; ++u) {
+          const uint32_t w[4] = {q[u].x, q[u].y, q[u].z, q[u].w};
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            g[u][2 * k] = __uint_as_float(w[k] << 16);
+            g[u][2 * k + 1] = __uint_as_float(w[k] & 0xFFFF0000u);
+          }
+        }
+      } else {
+#pragma unroll
+        for (int u = 0; u < GN_EIGHTS; ++u)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            // a warp's lanes read one after the other; which of a thread's eights a value belongs to does not matter
+            const float4 q = *reinterpret_cast<const float4*>((const float*)e.g + base + ((2 * u + h) * AW_THREADS + t) * 4);
+            g[u][4 * h] = q.x; g[u][4 * h + 1] = q.y; g[u][4 * h + 2] = q.z; g[u][4 * h + 3] = q.w;
+          }
+      }
+    } else {
+#pragma unroll
+      for (int u = 0; u < GN_EIGHTS; ++u)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          float q[4];
+          const long long i = base + (u * AW_THREADS + t) * 8 + 4 * h;
+          if (e.g_is_bf16) aw_load4((const __nv_bfloat16*)e.g, i, e.n, e.cols, e.ldg, e.flat, q);
+          else aw_load4((const float*)e.g, i, e.n, e.cols, e.ldg, e.flat, q);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) g[u][4 * h + k] = q[k];
+        }
     }
 #pragma unroll
-    for (int u = 0; u < GN_QUADS; ++u)
-#pragma unroll
-      for (int k = 0; k < 4; ++k) sum = fma((double)g[u][k], (double)g[u][k], sum);
+    for (int u = 0; u < GN_EIGHTS; ++u) sum += gn_squares(g[u]);
   }
   auto block_sum = [&](double x) {
 #pragma unroll
@@ -390,7 +517,7 @@ ard_status launch_adamw(ard_ctx* ctx, const ard_adamw_tensor* tensors, int n_ten
     if (table.n == 0) return ARD_OK;
     using T = std::remove_cv_t<std::remove_reference_t<decltype(table)>>;
     constexpr int CAP = sizeof(table.e) / sizeof(table.e[0]);
-    const unsigned long long room = 8ull * ctx->sm_count;
+    const unsigned long long room = 4ull * ctx->sm_count;
     const dim3 grid((unsigned)(table.tiles < room ? table.tiles : room));
     if (bits == 32) ARD_CUDA_OK(ard_launch(ctx, adamw_kernel<32, CAP>, grid, dim3(AW_THREADS), 0, s, (T)table, a));
     else ARD_CUDA_OK(ard_launch(ctx, adamw_kernel<8, CAP>, grid, dim3(AW_THREADS), 0, s, (T)table, a));

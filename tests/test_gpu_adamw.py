@@ -121,7 +121,7 @@ class Param:
         assert bool((self.ms[-(-n // 128):] == -5).all()) and bool((self.vs[-(-n // 128):] == -5).all())
 
 
-SIZES = [(1, 1), (1, 3), (1, 4), (1, 127), (1, 128), (1, 129), (1, 2048), (1, 2049), (3, 5), (10, 2048), (64, 33), (257, 129), (100, 1000), (1, 300001)]
+SIZES = [(1, 1), (1, 3), (1, 4), (1, 127), (1, 128), (1, 129), (1, 2048), (1, 2049), (3, 5), (10, 2048), (64, 33), (257, 129), (100, 1000), (1, 300001), (128, 4096)]
 
 
 @pytest.mark.parametrize("bits", [32, 8])
@@ -261,6 +261,27 @@ def test_norm(gd):
         assert not np.isfinite(float(out[0])) and np.isnan(float(out[1]))
     ard.ard_grad_norm(_h(), table, 0, 1.0, out)            # no gradients
     assert out.tolist() == [0.0, 1.0, 7.0]
+
+
+@pytest.mark.parametrize("gd", [torch.float32, BF])
+@pytest.mark.parametrize("n", [8191, 8192, 8193, 16384, 100000, 2 ** 20 + 8])
+def test_norm_of_whole_and_ragged_tiles(n, gd):
+    """Every element counts once: gradients of which one alone is not zero, at the tiles' borders, and all of them."""
+    g = torch.zeros(n, device="cuda", dtype=gd)
+    out = torch.zeros(2, device="cuda")
+    table = ard.adamw_tensors([{"rows": 1, "cols": n, "p": None, "g": g, "m": None, "v": None}])
+    for at in {0, 1, 3, 4, 7, 8, 1023, 1024, 2047, 2048, 4095, 4096, 8190, n // 2, n - 9, n - 2, n - 1} | set(range(8176, min(n, 8208))):
+        for value in (3.0, 2e-30):
+            g[at] = value
+            ard.ard_grad_norm(_h(), table, 1, 1.0, out)
+            g[at] = 0.0
+            want = float(torch.tensor(value).to(gd))
+            assert abs(float(out[0]) - want) <= 2 * U * want, at
+    g.copy_(torch.randn(n, device="cuda"))
+    ard.ard_grad_norm(_h(), table, 1, 1.0, out)
+    want, factor = OA.norm([host(g)], 1.0)
+    # sums of eight squares are off by at most eight units each, those over all of them by far less
+    assert abs(float(out[0]) - want) <= 2 * U * want and abs(float(out[1]) - factor) <= 4 * U * factor
 
 
 @pytest.mark.parametrize("bits", [32, 8])
