@@ -6,6 +6,7 @@
 
 #include "ard_internal.h"
 #include "philox.h"
+#include "sm100_ptx.h"
 
 namespace {
 
@@ -42,8 +43,10 @@ constexpr int AW_SMALL = 16, AW_LARGE = 216;
 
 struct AwArgs {
   float lr, beta1, beta2, one_minus_beta1, one_minus_beta2, eps;
+  float lift1, root_lift2;  // 1 / (1 - beta1^t) and the root of 1 / (1 - beta2^t), where the host knows t
   double ln_beta1, ln_beta2;
-  unsigned long long seed, step;
+  uint32_t keys[20];  // the generator's, of its ten rounds: read where they are used, not carried in registers
+  unsigned long long step;
   const unsigned long long* counter;
   const float* lr_factor;
   const float* grad_factor;
@@ -135,74 +138,68 @@ __device__ __forceinline__ void aw_decode(uint32_t q, float scale, float (&v)[4]
   }
 }
 
-// 1 / x and sqrt(x) to the last bit or two in a few instructions: the instructions' approximations, improved once by Newton's step, in place of
-// division and square root rounded to the last bit (8 to 20 instructions each with their special cases).  What is rounded to 8 bits is worth the
-// step: an error of one unit more in the last place is a few values in a million more that fall on the other side of a border.
-__device__ __forceinline__ float aw_inverse(float x) {  // x normal
+// sqrt(x) and 1 / x as the instructions approximate them, to a unit or two in the last place: rounded to the last bit they take 8 to 20 instructions
+// each, with their special cases, and the kernel with states in 8 bits runs out of issue slots.  States in 32 bits keep roots of subnormal numbers (eps
+// may be zero).
+template <int BITS>
+__device__ __forceinline__ float aw_root(float x) {
   float r;
-  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
-  return fmaf(r, fmaf(-x, r, 1.f), r);
-}
-__device__ __forceinline__ float aw_root(float x) {  // subnormal: 0
-  float r;
-  asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
-  const float s = x * r;
-  const float better = fmaf(0.5f * r, fmaf(-s, s, x), s);
-  return x < 1.17549435e-38f ? 0.f : better;
-}
-// The quotient of the step, and its root, which no rounding follows but the parameter's.
-__device__ __forceinline__ float aw_quick_root(float x) {
-  float r;
-  asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
+  if (BITS == 32) asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
+  else asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
   return r;
 }
-__device__ __forceinline__ float aw_quick_inverse(float x) {
+__device__ __forceinline__ float aw_inverse(float x) {
   float r;
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
   return r;
 }
+// Two elements in one instruction.
+__device__ __forceinline__ float2 operator*(float2 a, float2 b) { return __fmul2_rn(a, b); }
+__device__ __forceinline__ float2 operator+(float2 a, float2 b) { return __fadd2_rn(a, b); }
+__device__ __forceinline__ float2 aw_fma(float2 a, float2 b, float2 c) { return __ffma2_rn(a, b, c); }
+__device__ __forceinline__ float2 aw_both(float x) { return make_float2(x, x); }
 
-// a >= 0 rounded to the grid of the 8-bit floats (3 bits of mantissa; steps of 2^-9 below 2^-6), up with the probability of what is
-// cut off, which 16 random bits resolve to 2^-16 of a step.  Below 2^-6 the grid is that of [2^-6, 2^-5): adding 2^-6 puts the
-// value there.  The sum of the bits carries into the exponent where it should.
-__device__ __forceinline__ float aw_round(float a, uint32_t random16) {
-  const bool low = a < 0.015625f;
-  const float s = low ? a + 0.015625f : a;
-  const float q = __uint_as_float((__float_as_uint(s) + (random16 << 4) + 8u) & ~0xFFFFFu);
-  return fminf(low ? q - 0.015625f : q, E4M3_MAX);
-}
-
-// The 8-bit floats of a block of 128 values, four in each lane, and its scale (the same in all lanes).
-template <bool POSITIVE>
-__device__ __forceinline__ uint32_t aw_encode(const float (&v)[4], const uint32_t (&random16)[4], float& scale) {
-  const float mine = fmaxf(fmaxf(fabsf(v[0]), fabsf(v[1])), fmaxf(fabsf(v[2]), fabsf(v[3])));
-  // fmaxf drops NaN: a value that is not a number has to spoil its block, as it spoils states in 32 bits
-  const bool nan = v[0] != v[0] || v[1] != v[1] || v[2] != v[2] || v[3] != v[3];
-  const uint32_t bits = __reduce_max_sync(0xFFFFFFFFu, nan ? 0x7FC00000u : __float_as_uint(mine));  // of values >= 0, in their order
-  const float big = __uint_as_float(bits);
+// The 8-bit floats of a block of 128 values, four in each lane, and its scale (the same in all lanes).  ROOT: of values >= 0, from the words'
+// high halves; else from their low halves.
+// A value is rounded to the grid of the 8-bit floats (3 bits of mantissa; steps of 2^-9 below 2^-6), up with the probability of what is
+// cut off, which 16 random bits resolve to 2^-16 of a step: those bits are added below the mantissa's three, and all bits there cut off.  (Half a step
+// less and the conversion's rounding to nearest in place of the cut would be wrong where a sum passes 2^-5.)  Below 2^-6 the grid is that of
+// [2^-6, 2^-5): adding 2^-6 puts the value there.  Sums carry into the exponent where they should.  What passes 448 the conversion cuts off.
+template <bool ROOT>
+__device__ __forceinline__ uint32_t aw_encode(const float2 (&v)[2], const uint32_t (&words)[4], float& scale) {
+  float most = fmaxf(fmaxf(fabsf(v[0].x), fabsf(v[0].y)), fmaxf(fabsf(v[1].x), fabsf(v[1].y)));
+  // a value that is not a number, which the maximum drops, spoils its block, as it spoils states in 32 bits
+  const float2 sum = v[0] + v[1], any = sum * aw_both(0.f);
+  if (any.x + any.y != 0.f) most = __int_as_float(0x7FC00000);  // (or an infinity: its block is spoilt by what 0 times it gives)
+  const float big = __uint_as_float(__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(most)));  // of values >= 0, in their order
   const bool none = big < AW_TINY;
-  const float inv = none ? 0.f : E4M3_MAX * aw_inverse(big);
+  const float near = aw_inverse(big), inv = none ? 0.f : E4M3_MAX * fmaf(near, fmaf(-big, near, 1.f), near), least = none ? 0.f : 0.001953125f;
   scale = none ? 0.f : big * (1.f / E4M3_MAX);
-  float q[4];
+  uint32_t codes = 0;
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    q[k] = aw_round(fabsf(v[k]) * inv, random16[k]);
-    if (POSITIVE && v[k] > 0.f && !none) q[k] = fmaxf(q[k], 0.001953125f);
-    if (!POSITIVE) q[k] = copysignf(q[k], v[k]);
+  for (int h = 0; h < 2; ++h) {
+    const float2 a = make_float2(fabsf(v[h].x), fabsf(v[h].y)) * aw_both(inv);
+    const float2 shift = make_float2(a.x < 0.015625f ? 0.015625f : 0.f, a.y < 0.015625f ? 0.015625f : 0.f);
+    const float2 up = a + shift;
+    auto cut = [](float x, uint32_t word) {
+      return __uint_as_float((__float_as_uint(x) + ((ROOT ? word >> 12 : word << 4) & 0xFFFF0u) + 8u) & ~0xFFFFFu);
+    };
+    float2 q = aw_fma(shift, aw_both(-1.f), make_float2(cut(up.x, words[2 * h]), cut(up.y, words[2 * h + 1])));
+    if (ROOT) q = make_float2(fmaxf(q.x, v[h].x > 0.f ? least : 0.f), fmaxf(q.y, v[h].y > 0.f ? least : 0.f));
+    else q = make_float2(copysignf(q.x, v[h].x), copysignf(q.y, v[h].y));
+    codes |= (uint32_t)__nv_cvt_float2_to_fp8x2(q, __NV_SATFINITE, __NV_E4M3) << (16 * h);
   }
-  const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(q[0], q[1]), __NV_SATFINITE, __NV_E4M3);
-  const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(q[2], q[3]), __NV_SATFINITE, __NV_E4M3);
-  return lo | hi << 16;
+  return codes;
 }
 
 // The piece of a tensor that a CTA takes at a time.
-constexpr int AW_QUADS = 2;
+constexpr int AW_QUADS = 2;  // of each thread
 constexpr int AW_TILE = AW_QUADS * AW_THREADS * 4;
 
 // What is the same for all elements of a launch, and of a tensor.
 struct AwStep {
   float gf, beta1, beta2, omb1, omb2, eps, root_lift2, step1, lr_decay;
-  unsigned long long t, seed;
+  unsigned long long t;
 };
 
 template <int BITS>
@@ -231,25 +228,34 @@ __device__ __forceinline__ void aw_fetch(const AwEntry& e, long long i, bool fla
   }
 }
 template <int BITS, bool WHOLE>
-__device__ __forceinline__ void aw_update(const AwEntry& e, const AwStep& a, long long i, bool flat, float (&p)[4], float (&g)[4],
-                                          AwState<BITS>& st) {
+__device__ __forceinline__ void aw_update(const AwEntry& e, const AwStep& a, const uint32_t (&keys)[20], long long i, bool flat, float (&p)[4],
+                                          float (&g)[4], AwState<BITS>& st) {
   const long long n = WHOLE ? i + 4 : e.n;
   const bool f = WHOLE || flat;
   float (&m)[4] = st.m;
   float (&v)[4] = st.v;
-  float r[4];
+  float2 m2[2], r2[2];
   if constexpr (BITS == 8) {
     aw_decode(st.mq, st.ms, m);
     aw_decode(st.vq, st.vs, v);
   }
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    const float gk = g[k] * a.gf;
-    m[k] = fmaf(a.beta1, m[k], a.omb1 * gk);
-    v[k] = fmaf(a.beta2, BITS == 32 ? v[k] : v[k] * v[k], a.omb2 * gk * gk);
-    r[k] = BITS == 32 ? aw_quick_root(v[k]) : aw_root(v[k]);
-    const float move = a.step1 * m[k] * aw_quick_inverse(fmaf(r[k], a.root_lift2, a.eps));
-    p[k] = p[k] - fmaf(a.lr_decay, p[k], move);
+  for (int h = 0; h < 2; ++h) {
+    const float2 gk = make_float2(g[2 * h], g[2 * h + 1]) * aw_both(a.gf), p2 = make_float2(p[2 * h], p[2 * h + 1]);
+    float2 v2 = make_float2(v[2 * h], v[2 * h + 1]);
+    m2[h] = aw_fma(aw_both(a.beta1), make_float2(m[2 * h], m[2 * h + 1]), aw_both(a.omb1) * gk);
+    if (BITS == 8) v2 = v2 * v2;
+    v2 = aw_fma(aw_both(a.beta2), v2, (aw_both(a.omb2) * gk) * gk);
+    r2[h] = make_float2(aw_root<BITS>(v2.x), aw_root<BITS>(v2.y));
+    const float2 den = aw_fma(r2[h], aw_both(a.root_lift2), aw_both(a.eps));
+    const float2 move = (aw_both(a.step1) * m2[h]) * make_float2(aw_inverse(den.x), aw_inverse(den.y));
+    const float2 to = aw_fma(aw_both(-1.f), aw_fma(aw_both(a.lr_decay), p2, move), p2);
+    p[2 * h] = to.x;
+    p[2 * h + 1] = to.y;
+    m[2 * h] = m2[h].x;
+    m[2 * h + 1] = m2[h].y;
+    v[2 * h] = v2.x;
+    v[2 * h + 1] = v2.y;
   }
   aw_store4(e.p, i, n, e.cols, e.ldp, f, p);
   if (e.w) aw_store4(e.w, i, n, e.cols, e.ldw, f, p);
@@ -258,16 +264,16 @@ __device__ __forceinline__ void aw_update(const AwEntry& e, const AwStep& a, lon
     aw_store4((float*)e.v, i, n, 1, 1, f, v);
   } else {
     uint32_t c[4] = {(uint32_t)a.t, (uint32_t)(a.t >> 32), (uint32_t)(i >> 2), e.number};
-    philox4x32_10(c, (uint32_t)a.seed, (uint32_t)(a.seed >> 32));
-    uint32_t low[4], high[4];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      low[k] = c[k] & 0xFFFFu;
-      high[k] = c[k] >> 16;
-      if (!WHOLE && i + k >= n) m[k] = r[k] = 0.f;
-    }
+    for (int k = 0; k < 10; ++k) philox_round(c, keys[2 * k], keys[2 * k + 1]);
+    if (!WHOLE)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        if (i + 2 * h >= n) m2[h].x = r2[h].x = 0.f;
+        if (i + 2 * h + 1 >= n) m2[h].y = r2[h].y = 0.f;
+      }
     float ms, vs;
-    const uint32_t mq = aw_encode<false>(m, low, ms), vq = aw_encode<true>(r, high, vs);
+    const uint32_t mq = aw_encode<false>(m2, c, ms), vq = aw_encode<true>(r2, c, vs);
     aw_store_codes((uint8_t*)e.m, i, n, f, mq);
     aw_store_codes((uint8_t*)e.v, i, n, f, vq);
     if ((threadIdx.x & 31) == 0) {
@@ -277,54 +283,174 @@ __device__ __forceinline__ void aw_update(const AwEntry& e, const AwStep& a, lon
   }
 }
 
-template <int BITS, int CAP>
-__global__ void __launch_bounds__(AW_THREADS, 4) adamw_kernel(const __grid_constant__ AwTable<CAP> table, const AwArgs a) {
-  __shared__ float s_lift[2];
-  pdl_launch_dependents();
-  pdl_wait_prior_grids();
-  AwStep st;
+// 1 / (1 - beta^t), or its root.
+__host__ __device__ inline float aw_lift(unsigned long long t, double ln_beta, bool root) {
+  const double lift = -1.0 / expm1((double)t * ln_beta);
+  return (float)(root ? sqrt(lift) : lift);
+}
+
+// What the kernels do first; false: nothing is to be done.
+__device__ __forceinline__ bool aw_begin(const AwArgs& a, AwStep& st, float& lr, float (&s_lift)[2]) {
   st.t = a.step + (a.counter ? *a.counter : 0ull);
-  if (st.t == 0) return;
   st.gf = a.grad_factor ? *a.grad_factor : 1.f;
-  if (!(fabsf(st.gf) < INFINITY)) return;
-  const float lr = a.lr_factor ? a.lr * *a.lr_factor : a.lr;
-  if (threadIdx.x < 2) {
-    const double lift = -1.0 / expm1((double)st.t * (threadIdx.x ? a.ln_beta2 : a.ln_beta1));
-    s_lift[threadIdx.x] = (float)(threadIdx.x ? sqrt(lift) : lift);
+  if (st.t == 0 || !(fabsf(st.gf) < INFINITY)) return false;
+  lr = a.lr_factor ? a.lr * *a.lr_factor : a.lr;
+  float lift1 = a.lift1;
+  st.root_lift2 = a.root_lift2;
+  if (a.counter) {
+    if (threadIdx.x < 2) s_lift[threadIdx.x] = aw_lift(st.t, threadIdx.x ? a.ln_beta2 : a.ln_beta1, threadIdx.x);
+    __syncthreads();
+    lift1 = s_lift[0];
+    st.root_lift2 = s_lift[1];
   }
-  __syncthreads();
-  st.root_lift2 = s_lift[1];
-  st.step1 = lr * s_lift[0];
+  st.step1 = lr * lift1;
   st.beta1 = a.beta1;
   st.beta2 = a.beta2;
   st.omb1 = a.one_minus_beta1;
   st.omb2 = a.one_minus_beta2;
   st.eps = a.eps;
-  st.seed = a.seed;
+  return true;
+}
+// A tile that ends inside, or whose elements do not lie one after the other on 16 bytes.
+template <int BITS>
+__device__ __forceinline__ void aw_ragged(const AwEntry& e, const AwStep& st, const uint32_t (&keys)[20], long long base) {
+#pragma unroll 1
+  for (int u = 0; u < AW_QUADS; ++u) {
+    const long long i = base + (u * AW_THREADS + threadIdx.x) * 4;
+    if (BITS == 32 ? i >= e.n : (i & ~127ll) >= e.n) continue;  // (8 bits: a block's lanes stay together)
+    float p[4], g[4];
+    AwState<BITS> state;
+    aw_fetch<BITS, false>(e, i, e.flat, p, g, state);
+    aw_update<BITS, false>(e, st, keys, i, e.flat, p, g, state);
+  }
+}
+
+// States in 32 bits: a CTA a tile, all of a thread's loads ahead of its stores.  (On a grid of the resident CTAs, each with many tiles, the step of
+// 8192 x 8192 took 310 us, so 285: the loads of a CTA that begins run beside the stores of one that ends.)
+template <int CAP>
+__global__ void __launch_bounds__(AW_THREADS, 4) adamw_kernel(const __grid_constant__ AwTable<CAP> table, const __grid_constant__ AwArgs a) {
+  __shared__ float s_lift[2];
+  pdl_launch_dependents();
+  pdl_wait_prior_grids();
+  AwStep st;
+  float lr;
+  if (!aw_begin(a, st, lr, s_lift)) return;
   for (unsigned long long tile = blockIdx.x; tile < table.tiles; tile += gridDim.x) {
     const AwEntry& e = table.e[aw_find(table, tile)];
     const long long base = (long long)(tile - e.tile0) * AW_TILE;
     st.lr_decay = lr * e.decay;
     if (e.flat && base + AW_TILE <= e.n) {
-      // all loads of the tile before its first store
       float p[AW_QUADS][4], g[AW_QUADS][4];
-      AwState<BITS> state[AW_QUADS];
+      AwState<32> state[AW_QUADS];
 #pragma unroll
-      for (int u = 0; u < AW_QUADS; ++u) aw_fetch<BITS, true>(e, base + (u * AW_THREADS + threadIdx.x) * 4, true, p[u], g[u], state[u]);
+      for (int u = 0; u < AW_QUADS; ++u) aw_fetch<32, true>(e, base + (u * AW_THREADS + threadIdx.x) * 4, true, p[u], g[u], state[u]);
 #pragma unroll
-      for (int u = 0; u < AW_QUADS; ++u) aw_update<BITS, true>(e, st, base + (u * AW_THREADS + threadIdx.x) * 4, true, p[u], g[u], state[u]);
+      for (int u = 0; u < AW_QUADS; ++u)
+        aw_update<32, true>(e, st, a.keys, base + (u * AW_THREADS + threadIdx.x) * 4, true, p[u], g[u], state[u]);
     } else {
-#pragma unroll 1
-      for (int u = 0; u < AW_QUADS; ++u) {
-        const long long i = base + (u * AW_THREADS + threadIdx.x) * 4;
-        if (BITS == 32 ? i >= e.n : (i & ~127ll) >= e.n) continue;  // (8 bits: a block's lanes stay together)
-        float p[4], g[4];
-        AwState<BITS> state;
-        aw_fetch<BITS, false>(e, i, e.flat, p, g, state);
-        aw_update<BITS, false>(e, st, i, e.flat, p, g, state);
-      }
+      aw_ragged<32>(e, st, a.keys, base);
     }
   }
+}
+
+// States in 8 bits: 14 to 20 bytes are read for an element whose arithmetic takes some 90 instructions, so registers cannot hold what has to be in flight
+// (36 bytes for a thread's quad: 2.2 TB/s).  Tiles come through a ring in shared memory by bulk copies, four tiles ahead.  (Three CTAs an
+// SM leave 80 registers, too few: 170 us in place of 146 for 36 M elements.)
+constexpr int AW8_SLOTS = 5, AW8_PER_SM = 2;
+constexpr int AW8_P = 0, AW8_G = AW_TILE * 4, AW8_M = AW8_G + AW_TILE * 4, AW8_V = AW8_M + AW_TILE, AW8_MS = AW8_V + AW_TILE,
+              AW8_VS = AW8_MS + AW_TILE / 32, AW8_SLOT = AW8_VS + AW_TILE / 32;
+template <int CAP>
+__global__ void __launch_bounds__(AW_THREADS, AW8_PER_SM) adamw8_kernel(const __grid_constant__ AwTable<CAP> table, const __grid_constant__ AwArgs a,
+                                                                       int* status) {
+  extern __shared__ __align__(128) uint8_t slots[];
+  __shared__ __align__(8) uint64_t full[AW8_SLOTS];
+  __shared__ float s_lift[2];
+  __shared__ int s_gone;
+  if (threadIdx.x == 0) {
+    for (int k = 0; k < AW8_SLOTS; ++k) mbar_init(smem_u32(&full[k]), 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    s_gone = 0;
+  }
+  __syncthreads();
+  pdl_launch_dependents();
+  pdl_wait_prior_grids();
+  AwStep st;
+  float lr;
+  if (!aw_begin(a, st, lr, s_lift)) return;
+  auto whole = [&](const AwEntry& e, long long base) { return e.flat && base + AW_TILE <= e.n; };
+  unsigned long long ahead = blockIdx.x;  // the next tile to ask for (thread 0)
+  int asked = 0, slot = 0, phase = 0, taken = 0;
+  bool gone = false;  // a copy did not come within two seconds: the rest is left, the status says so
+  auto ask = [&] {
+    if (ahead >= table.tiles || gone) return;
+    const AwEntry& e = table.e[aw_find(table, ahead)];
+    const long long base = (long long)(ahead - e.tile0) * AW_TILE;
+    const int to = asked++ % AW8_SLOTS;
+    const uint32_t bar = smem_u32(&full[to]), dst = smem_u32(slots + to * AW8_SLOT);
+    ahead += gridDim.x;
+    if (!whole(e, base)) {
+      mbar_arrive(bar);
+      return;
+    }
+    const uint32_t gbytes = e.g_is_bf16 ? AW_TILE * 2 : AW_TILE * 4;
+    mbar_arrive_expect_tx(bar, AW_TILE * 6 + gbytes + AW_TILE / 16);
+    auto copy = [&](uint32_t at, const void* src, uint32_t bytes) {
+      asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst + at), "l"(src),
+                   "r"(bytes), "r"(bar)
+                   : "memory");
+    };
+    copy(AW8_P, e.p + base, AW_TILE * 4);
+    copy(AW8_G, (const uint8_t*)e.g + base * (e.g_is_bf16 ? 2 : 4), gbytes);
+    copy(AW8_M, (const uint8_t*)e.m + base, AW_TILE);
+    copy(AW8_V, (const uint8_t*)e.v + base, AW_TILE);
+    copy(AW8_MS, e.m_scale + base / 128, AW_TILE / 32);
+    copy(AW8_VS, e.v_scale + base / 128, AW_TILE / 32);
+  };
+  if (threadIdx.x == 0)
+    for (int k = 0; k < AW8_SLOTS; ++k) ask();
+  for (unsigned long long tile = blockIdx.x; tile < table.tiles; tile += gridDim.x) {
+    const AwEntry& e = table.e[aw_find(table, tile)];
+    const long long base = (long long)(tile - e.tile0) * AW_TILE;
+    st.lr_decay = lr * e.decay;
+    if (!gone && !mbar_wait(smem_u32(&full[slot]), (uint32_t)phase, &s_gone, status)) gone = true;
+    const bool w = whole(e, base);
+    float p[AW_QUADS][4], g[AW_QUADS][4];
+    AwState<8> state[AW_QUADS];
+    if (w) {
+      const uint8_t* from = slots + slot * AW8_SLOT;
+#pragma unroll
+      for (int u = 0; u < AW_QUADS; ++u) {
+        const int at = (u * AW_THREADS + threadIdx.x) * 4;
+        aw_load4((const float*)(from + AW8_P), at, AW_TILE, 0, 0, true, p[u]);
+        if (e.g_is_bf16) aw_load4((const __nv_bfloat16*)(from + AW8_G), at, AW_TILE, 0, 0, true, g[u]);
+        else aw_load4((const float*)(from + AW8_G), at, AW_TILE, 0, 0, true, g[u]);
+        state[u].mq = *reinterpret_cast<const uint32_t*>(from + AW8_M + at);
+        state[u].vq = *reinterpret_cast<const uint32_t*>(from + AW8_V + at);
+        state[u].ms = reinterpret_cast<const float*>(from + AW8_MS)[at / 128];
+        state[u].vs = reinterpret_cast<const float*>(from + AW8_VS)[at / 128];
+      }
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) ask();
+    if (!gone) ++taken;
+    if (++slot == AW8_SLOTS) {
+      slot = 0;
+      phase ^= 1;
+    }
+    if (gone) continue;
+    if (w) {
+#pragma unroll
+      for (int u = 0; u < AW_QUADS; ++u)
+        aw_update<8, true>(e, st, a.keys, base + (u * AW_THREADS + threadIdx.x) * 4, true, p[u], g[u], state[u]);
+    } else {
+      aw_ragged<8>(e, st, a.keys, base);
+    }
+  }
+  if (threadIdx.x == 0)  // copies that did not come get the same time again before the CTA ends: they write to its memory
+    for (int k = taken; gone && k < asked; ++k) {
+      bool ok = false;
+      for (int poll = 0; poll < 2000 && !ok; ++poll) ok = mbar_try_wait_hint(smem_u32(&full[k % AW8_SLOTS]), (uint32_t)(k / AW8_SLOTS) & 1u, 1000000u);
+    }
 }
 
 // ---- norm of all gradients ------------------------------------------------------------------------
@@ -458,7 +584,8 @@ AwEntry aw_entry(const ard_adamw_tensor& t, int number, bool grads_only, unsigne
   e.g_is_bf16 = t.g_dtype == ARD_BF16;
   e.flat = e.ldg == t.cols && on16(t.g);
   if (!grads_only)
-    e.flat = e.flat && e.ldp == t.cols && on16(t.p) && on16(t.m) && on16(t.v) && (!t.w || (e.ldw == t.cols && on16(t.w)));
+    e.flat = e.flat && e.ldp == t.cols && on16(t.p) && on16(t.m) && on16(t.v) && (!t.w || (e.ldw == t.cols && on16(t.w))) &&
+             on16(t.m_scale) && on16(t.v_scale);
   return e;
 }
 
@@ -508,8 +635,13 @@ ard_status launch_adamw(ard_ctx* ctx, const ard_adamw_tensor* tensors, int n_ten
   a.eps = (float)eps;
   a.ln_beta1 = beta1 > 0.0 ? log(beta1) : -1e300;
   a.ln_beta2 = beta2 > 0.0 ? log(beta2) : -1e300;
-  a.seed = seed;
+  for (int k = 0; k < 10; ++k) {
+    a.keys[2 * k] = (uint32_t)seed + (uint32_t)k * 0x9E3779B9u;
+    a.keys[2 * k + 1] = (uint32_t)(seed >> 32) + (uint32_t)k * 0xBB67AE85u;
+  }
   a.step = step;
+  a.lift1 = aw_lift(step, a.ln_beta1, false);
+  a.root_lift2 = aw_lift(step, a.ln_beta2, true);
   a.counter = reinterpret_cast<const unsigned long long*>(counter);
   a.lr_factor = lr_factor;
   a.grad_factor = grad_factor;
@@ -517,10 +649,17 @@ ard_status launch_adamw(ard_ctx* ctx, const ard_adamw_tensor* tensors, int n_ten
     if (table.n == 0) return ARD_OK;
     using T = std::remove_cv_t<std::remove_reference_t<decltype(table)>>;
     constexpr int CAP = sizeof(table.e) / sizeof(table.e[0]);
-    const unsigned long long room = 4ull * ctx->sm_count;
-    const dim3 grid((unsigned)(table.tiles < room ? table.tiles : room));
-    if (bits == 32) ARD_CUDA_OK(ard_launch(ctx, adamw_kernel<32, CAP>, grid, dim3(AW_THREADS), 0, s, (T)table, a));
-    else ARD_CUDA_OK(ard_launch(ctx, adamw_kernel<8, CAP>, grid, dim3(AW_THREADS), 0, s, (T)table, a));
+    if (bits == 32) {
+      const unsigned long long most = 1ull << 30;
+      const dim3 grid((unsigned)(table.tiles < most ? table.tiles : most));
+      ARD_CUDA_OK(ard_launch(ctx, adamw_kernel<CAP>, grid, dim3(AW_THREADS), 0, s, (T)table, a));
+    } else {
+      constexpr int smem = AW8_SLOTS * AW8_SLOT;
+      const unsigned long long room = (unsigned long long)AW8_PER_SM * ctx->sm_count;
+      const dim3 grid((unsigned)(table.tiles < room ? table.tiles : room));
+      ARD_CUDA_OK(cudaFuncSetAttribute(adamw8_kernel<CAP>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+      ARD_CUDA_OK(ard_launch(ctx, adamw8_kernel<CAP>, grid, dim3(AW_THREADS), smem, s, (T)table, a, ctx->d_status));
+    }
     ctx->launches++;
     ARD_CUDA_OK(cudaGetLastError());
     return ARD_OK;
