@@ -311,12 +311,12 @@ __device__ __forceinline__ bool aw_begin(const AwArgs& a, AwStep& st, float& lr,
   st.eps = a.eps;
   return true;
 }
-// A tile that ends inside, or whose elements do not lie one after the other on 16 bytes.
-template <int BITS>
-__device__ __forceinline__ void aw_ragged(const AwEntry& e, const AwStep& st, const uint32_t (&keys)[20], long long base) {
+// A tile of QUADS x THREADS quads that ends inside, or whose elements do not lie one after the other on 16 bytes.
+template <int BITS, int QUADS, int THREADS>
+__device__ __forceinline__ void aw_ragged(const AwEntry& e, const AwStep& st, const uint32_t (&keys)[20], long long base, int thread) {
 #pragma unroll 1
-  for (int u = 0; u < AW_QUADS; ++u) {
-    const long long i = base + (u * AW_THREADS + threadIdx.x) * 4;
+  for (int u = 0; u < QUADS; ++u) {
+    const long long i = base + (u * THREADS + thread) * 4;
     if (BITS == 32 ? i >= e.n : (i & ~127ll) >= e.n) continue;  // (8 bits: a block's lanes stay together)
     float p[4], g[4];
     AwState<BITS> state;
@@ -348,105 +348,108 @@ __global__ void __launch_bounds__(AW_THREADS, 4) adamw_kernel(const __grid_const
       for (int u = 0; u < AW_QUADS; ++u)
         aw_update<32, true>(e, st, a.keys, base + (u * AW_THREADS + threadIdx.x) * 4, true, p[u], g[u], state[u]);
     } else {
-      aw_ragged<32>(e, st, a.keys, base);
+      aw_ragged<32, AW_QUADS, AW_THREADS>(e, st, a.keys, base, (int)threadIdx.x);
     }
   }
 }
 
-// States in 8 bits: 14 to 20 bytes are read for an element whose arithmetic takes some 90 instructions, so registers cannot hold what has to be in flight
-// (36 bytes for a thread's quad: 2.2 TB/s).  Tiles come through a ring in shared memory by bulk copies, four tiles ahead.  (Three CTAs an
-// SM leave 80 registers, too few: 170 us in place of 146 for 36 M elements.)
-constexpr int AW8_SLOTS = 5, AW8_PER_SM = 2;
-constexpr int AW8_P = 0, AW8_G = AW_TILE * 4, AW8_M = AW8_G + AW_TILE * 4, AW8_V = AW8_M + AW_TILE, AW8_MS = AW8_V + AW_TILE,
-              AW8_VS = AW8_MS + AW_TILE / 32, AW8_SLOT = AW8_VS + AW_TILE / 32;
+// States in 8 bits: 14 to 20 bytes are read for an element whose arithmetic takes some 80 instructions, so registers cannot hold what has to be in flight
+// (36 bytes for a thread's quad: 2.2 TB/s).  Every warp has its own tiles, which come through a ring in shared memory by bulk copies ahead of it: no
+// barrier among warps, four quads of a lane to a search of the table.  (Tiles of a CTA, two quads and four: 148 and 124 us for 36 M elements.)
+constexpr int AW8_QUADS = 4, AW8_TILE = AW8_QUADS * 128, AW8_SLOTS = 2, AW8_PER_SM = 2, AW8_WARPS = AW_THREADS / 32;
+constexpr int AW8_UNROLL = 4;
+static_assert(AW8_QUADS % 4 == 0, "bulk copies of the scales: multiples of 16 bytes");
+constexpr int AW8_P = 0, AW8_G = AW8_TILE * 4, AW8_M = AW8_G + AW8_TILE * 4, AW8_V = AW8_M + AW8_TILE, AW8_MS = AW8_V + AW8_TILE,
+              AW8_VS = AW8_MS + AW8_QUADS * 4, AW8_SLOT = AW8_VS + AW8_QUADS * 4;
 template <int CAP>
 __global__ void __launch_bounds__(AW_THREADS, AW8_PER_SM) adamw8_kernel(const __grid_constant__ AwTable<CAP> table, const __grid_constant__ AwArgs a,
                                                                        int* status) {
-  extern __shared__ __align__(128) uint8_t slots[];
-  __shared__ __align__(8) uint64_t full[AW8_SLOTS];
+  extern __shared__ __align__(128) uint8_t slots[];  // [warps][AW8_SLOTS][AW8_SLOT]
+  __shared__ __align__(8) uint64_t bars[AW8_WARPS][AW8_SLOTS];
   __shared__ float s_lift[2];
   __shared__ int s_gone;
-  if (threadIdx.x == 0) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  uint64_t* full = bars[warp];
+  uint8_t* mine = slots + (size_t)warp * AW8_SLOTS * AW8_SLOT;
+  if (lane == 0) {
     for (int k = 0; k < AW8_SLOTS; ++k) mbar_init(smem_u32(&full[k]), 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    s_gone = 0;
   }
+  if (threadIdx.x == 0) s_gone = 0;
   __syncthreads();
   pdl_launch_dependents();
   pdl_wait_prior_grids();
   AwStep st;
   float lr;
   if (!aw_begin(a, st, lr, s_lift)) return;
-  auto whole = [&](const AwEntry& e, long long base) { return e.flat && base + AW_TILE <= e.n; };
-  unsigned long long ahead = blockIdx.x;  // the next tile to ask for (thread 0)
+  auto whole = [&](const AwEntry& e, long long base) { return e.flat && base + AW8_TILE <= e.n; };
+  const unsigned long long stride = (unsigned long long)gridDim.x * AW8_WARPS;
+  unsigned long long ahead = (unsigned long long)blockIdx.x * AW8_WARPS + warp;  // the next tile to ask for (lane 0)
   int asked = 0, slot = 0, phase = 0, taken = 0;
   bool gone = false;  // a copy did not come within two seconds: the rest is left, the status says so
   auto ask = [&] {
     if (ahead >= table.tiles || gone) return;
     const AwEntry& e = table.e[aw_find(table, ahead)];
-    const long long base = (long long)(ahead - e.tile0) * AW_TILE;
+    const long long base = (long long)(ahead - e.tile0) * AW8_TILE;
     const int to = asked++ % AW8_SLOTS;
-    const uint32_t bar = smem_u32(&full[to]), dst = smem_u32(slots + to * AW8_SLOT);
-    ahead += gridDim.x;
+    const uint32_t bar = smem_u32(&full[to]), dst = smem_u32(mine + to * AW8_SLOT);
+    ahead += stride;
     if (!whole(e, base)) {
       mbar_arrive(bar);
       return;
     }
-    const uint32_t gbytes = e.g_is_bf16 ? AW_TILE * 2 : AW_TILE * 4;
-    mbar_arrive_expect_tx(bar, AW_TILE * 6 + gbytes + AW_TILE / 16);
+    const uint32_t gbytes = e.g_is_bf16 ? AW8_TILE * 2 : AW8_TILE * 4;
+    mbar_arrive_expect_tx(bar, AW8_TILE * 6 + gbytes + AW8_QUADS * 8);
     auto copy = [&](uint32_t at, const void* src, uint32_t bytes) {
       asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst + at), "l"(src),
                    "r"(bytes), "r"(bar)
                    : "memory");
     };
-    copy(AW8_P, e.p + base, AW_TILE * 4);
+    copy(AW8_P, e.p + base, AW8_TILE * 4);
     copy(AW8_G, (const uint8_t*)e.g + base * (e.g_is_bf16 ? 2 : 4), gbytes);
-    copy(AW8_M, (const uint8_t*)e.m + base, AW_TILE);
-    copy(AW8_V, (const uint8_t*)e.v + base, AW_TILE);
-    copy(AW8_MS, e.m_scale + base / 128, AW_TILE / 32);
-    copy(AW8_VS, e.v_scale + base / 128, AW_TILE / 32);
+    copy(AW8_M, (const uint8_t*)e.m + base, AW8_TILE);
+    copy(AW8_V, (const uint8_t*)e.v + base, AW8_TILE);
+    copy(AW8_MS, e.m_scale + base / 128, AW8_QUADS * 4);
+    copy(AW8_VS, e.v_scale + base / 128, AW8_QUADS * 4);
   };
-  if (threadIdx.x == 0)
+  if (lane == 0)
     for (int k = 0; k < AW8_SLOTS; ++k) ask();
-  for (unsigned long long tile = blockIdx.x; tile < table.tiles; tile += gridDim.x) {
+  for (unsigned long long tile = (unsigned long long)blockIdx.x * AW8_WARPS + warp; tile < table.tiles; tile += stride) {
     const AwEntry& e = table.e[aw_find(table, tile)];
-    const long long base = (long long)(tile - e.tile0) * AW_TILE;
+    const long long base = (long long)(tile - e.tile0) * AW8_TILE;
     st.lr_decay = lr * e.decay;
     if (!gone && !mbar_wait(smem_u32(&full[slot]), (uint32_t)phase, &s_gone, status)) gone = true;
-    const bool w = whole(e, base);
-    float p[AW_QUADS][4], g[AW_QUADS][4];
-    AwState<8> state[AW_QUADS];
-    if (w) {
-      const uint8_t* from = slots + slot * AW8_SLOT;
-#pragma unroll
-      for (int u = 0; u < AW_QUADS; ++u) {
-        const int at = (u * AW_THREADS + threadIdx.x) * 4;
-        aw_load4((const float*)(from + AW8_P), at, AW_TILE, 0, 0, true, p[u]);
-        if (e.g_is_bf16) aw_load4((const __nv_bfloat16*)(from + AW8_G), at, AW_TILE, 0, 0, true, g[u]);
-        else aw_load4((const float*)(from + AW8_G), at, AW_TILE, 0, 0, true, g[u]);
-        state[u].mq = *reinterpret_cast<const uint32_t*>(from + AW8_M + at);
-        state[u].vq = *reinterpret_cast<const uint32_t*>(from + AW8_V + at);
-        state[u].ms = reinterpret_cast<const float*>(from + AW8_MS)[at / 128];
-        state[u].vs = reinterpret_cast<const float*>(from + AW8_VS)[at / 128];
+    gone = __any_sync(0xFFFFFFFFu, gone);
+    if (!gone) {
+      ++taken;
+      if (whole(e, base)) {
+        const uint8_t* from = mine + slot * AW8_SLOT;
+#pragma unroll AW8_UNROLL
+        for (int u = 0; u < AW8_QUADS; ++u) {
+          const int at = (u * 32 + lane) * 4;
+          float p[4], g[4];
+          AwState<8> state;
+          aw_load4((const float*)(from + AW8_P), at, AW8_TILE, 0, 0, true, p);
+          if (e.g_is_bf16) aw_load4((const __nv_bfloat16*)(from + AW8_G), at, AW8_TILE, 0, 0, true, g);
+          else aw_load4((const float*)(from + AW8_G), at, AW8_TILE, 0, 0, true, g);
+          state.mq = *reinterpret_cast<const uint32_t*>(from + AW8_M + at);
+          state.vq = *reinterpret_cast<const uint32_t*>(from + AW8_V + at);
+          state.ms = reinterpret_cast<const float*>(from + AW8_MS)[u];
+          state.vs = reinterpret_cast<const float*>(from + AW8_VS)[u];
+          aw_update<8, true>(e, st, a.keys, base + at, true, p, g, state);
+        }
+      } else {
+        aw_ragged<8, AW8_QUADS, 32>(e, st, a.keys, base, lane);
       }
     }
-    __syncthreads();
-    if (threadIdx.x == 0) ask();
-    if (!gone) ++taken;
+    __syncwarp();  // the slot has been read
+    if (lane == 0) ask();
     if (++slot == AW8_SLOTS) {
       slot = 0;
       phase ^= 1;
     }
-    if (gone) continue;
-    if (w) {
-#pragma unroll
-      for (int u = 0; u < AW_QUADS; ++u)
-        aw_update<8, true>(e, st, a.keys, base + (u * AW_THREADS + threadIdx.x) * 4, true, p[u], g[u], state[u]);
-    } else {
-      aw_ragged<8>(e, st, a.keys, base);
-    }
   }
-  if (threadIdx.x == 0)  // copies that did not come get the same time again before the CTA ends: they write to its memory
+  if (lane == 0)  // copies that did not come get the same time again before the CTA ends: they write to its memory
     for (int k = taken; gone && k < asked; ++k) {
       bool ok = false;
       for (int poll = 0; poll < 2000 && !ok; ++poll) ok = mbar_try_wait_hint(smem_u32(&full[k % AW8_SLOTS]), (uint32_t)(k / AW8_SLOTS) & 1u, 1000000u);
@@ -645,7 +648,7 @@ ard_status launch_adamw(ard_ctx* ctx, const ard_adamw_tensor* tensors, int n_ten
   a.counter = reinterpret_cast<const unsigned long long*>(counter);
   a.lr_factor = lr_factor;
   a.grad_factor = grad_factor;
-  return aw_launches(tensors, n_tensors, false, AW_TILE, [&](const auto& table, int) {
+  return aw_launches(tensors, n_tensors, false, bits == 32 ? AW_TILE : AW8_TILE, [&](const auto& table, int) {
     if (table.n == 0) return ARD_OK;
     using T = std::remove_cv_t<std::remove_reference_t<decltype(table)>>;
     constexpr int CAP = sizeof(table.e) / sizeof(table.e[0]);
@@ -654,9 +657,9 @@ ard_status launch_adamw(ard_ctx* ctx, const ard_adamw_tensor* tensors, int n_ten
       const dim3 grid((unsigned)(table.tiles < most ? table.tiles : most));
       ARD_CUDA_OK(ard_launch(ctx, adamw_kernel<CAP>, grid, dim3(AW_THREADS), 0, s, (T)table, a));
     } else {
-      constexpr int smem = AW8_SLOTS * AW8_SLOT;
-      const unsigned long long room = (unsigned long long)AW8_PER_SM * ctx->sm_count;
-      const dim3 grid((unsigned)(table.tiles < room ? table.tiles : room));
+      constexpr int smem = AW8_WARPS * AW8_SLOTS * AW8_SLOT;
+      const unsigned long long room = (unsigned long long)AW8_PER_SM * ctx->sm_count, want = (table.tiles + AW8_WARPS - 1) / AW8_WARPS;
+      const dim3 grid((unsigned)(want < room ? want : room));
       ARD_CUDA_OK(cudaFuncSetAttribute(adamw8_kernel<CAP>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
       ARD_CUDA_OK(ard_launch(ctx, adamw8_kernel<CAP>, grid, dim3(AW_THREADS), smem, s, (T)table, a, ctx->d_status));
     }
