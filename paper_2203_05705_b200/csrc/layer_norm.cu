@@ -2,6 +2,8 @@
 // over the compact columns that a row pattern keeps.
 //
 // One pass over memory bounds both: the forward call reads x and writes y, the backward call reads x and dy and writes dx.
+#include <type_traits>
+
 #include "ard_internal.h"
 #include "sm100_ptx.h"
 
@@ -166,61 +168,90 @@ __global__ void __launch_bounds__(LN_SUM_WARPS * 32) ln_dw_sum_kernel(LnShape sh
 template <typename T>
 constexpr int LN_PER = 16 / (int)sizeof(T);  // elements of a piece
 
+// Two elements in one instruction (f32x2): with one each these kernels run out of issue slots before the memory is busy.
+__device__ __forceinline__ float2 operator*(float2 a, float2 b) { return __fmul2_rn(a, b); }
+__device__ __forceinline__ float2 operator+(float2 a, float2 b) { return __fadd2_rn(a, b); }
+__device__ __forceinline__ float2 ln_fma(float2 a, float2 b, float2 c) { return __ffma2_rn(a, b, c); }
+__device__ __forceinline__ float2 ln_both(float x) { return make_float2(x, x); }
+
 template <typename T>
-__device__ __forceinline__ void ln_unpack(const uint4& q, float (&v)[LN_PER<T>]) {
+constexpr int LN_PAIRS = LN_PER<T> / 2;
+template <typename T>
+__device__ __forceinline__ void ln_unpack(const uint4& q, float2 (&v)[LN_PAIRS<T>]) {
   const uint32_t w[4] = {q.x, q.y, q.z, q.w};
   if constexpr (sizeof(T) == 2) {
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      v[2 * k] = __uint_as_float(w[k] << 16);
-      v[2 * k + 1] = __uint_as_float(w[k] & 0xFFFF0000u);
-    }
+    for (int k = 0; k < 4; ++k) v[k] = make_float2(__uint_as_float(w[k] << 16), __uint_as_float(w[k] & 0xFFFF0000u));
   } else {
 #pragma unroll
-    for (int k = 0; k < 4; ++k) v[k] = __uint_as_float(w[k]);
+    for (int k = 0; k < 2; ++k) v[k] = make_float2(__uint_as_float(w[2 * k]), __uint_as_float(w[2 * k + 1]));
   }
 }
-// The first `valid` values of a piece.
-template <typename T>
-__device__ __forceinline__ void ln_store(T* p, int valid, const float (&v)[LN_PER<T>]) {
-  if (valid >= LN_PER<T>) {
-    uint32_t w[4];
+// The piece of column j from shared memory, elements from column n on as zero.  RAGGED: n may end inside a piece (asked once for all rows: the
+// questions, predicated rather than branched around, were two thirds of the instructions).
+template <typename T, bool RAGGED>
+__device__ __forceinline__ void ln_piece(const uint8_t* row, int j, int n, float2 (&v)[LN_PAIRS<T>]) {
+  uint4 q = make_uint4(0u, 0u, 0u, 0u);
+  if (j < n) q = *reinterpret_cast<const uint4*>(row + (size_t)j * sizeof(T));
+  ln_unpack<T>(q, v);
+  if (RAGGED && j + LN_PER<T> > n)
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      if constexpr (sizeof(T) == 2) {
-        __nv_bfloat162 b = __floats2bfloat162_rn(v[2 * k], v[2 * k + 1]);
+    for (int k = 0; k < LN_PAIRS<T>; ++k) {
+      if (j + 2 * k >= n) v[k].x = 0.f;
+      if (j + 2 * k + 1 >= n) v[k].y = 0.f;
+    }
+}
+// The first `valid` values of a piece.
+template <typename T, bool RAGGED>
+__device__ __forceinline__ void ln_store(T* p, int valid, const float2 (&v)[LN_PAIRS<T>]) {
+  if (!RAGGED || valid >= LN_PER<T>) {
+    uint32_t w[4];
+    if constexpr (sizeof(T) == 2) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        __nv_bfloat162 b = __floats2bfloat162_rn(v[k].x, v[k].y);
         w[k] = *reinterpret_cast<uint32_t*>(&b);
-      } else {
-        w[k] = __float_as_uint(v[k]);
+      }
+    } else {
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        w[2 * k] = __float_as_uint(v[k].x);
+        w[2 * k + 1] = __float_as_uint(v[k].y);
       }
     }
     *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
     return;
   }
 #pragma unroll
-  for (int k = 0; k < LN_PER<T>; ++k)
-    if (k < valid) ln_put(p, k, v[k]);
+  for (int k = 0; k < LN_PAIRS<T>; ++k) {
+    if (2 * k < valid) ln_put(p, 2 * k, v[k].x);
+    if (2 * k + 1 < valid) ln_put(p, 2 * k + 1, v[k].y);
+  }
 }
 // weight or bias at the units of a piece's columns; `other` where there is none.
-template <int PER>
-__device__ __forceinline__ void ln_params(const float* w, float other, const LnCols& c, int j, float (&v)[PER]) {
+template <int PAIRS>
+__device__ __forceinline__ void ln_params(const float* w, float other, const LnCols& c, int j, float2 (&v)[PAIRS]) {
 #pragma unroll
-  for (int k = 0; k < PER; ++k) v[k] = w && j + k < c.n ? w[c.b0 + (size_t)(j + k) * c.dp] : other;
+  for (int k = 0; k < PAIRS; ++k) {
+    v[k].x = w && j + 2 * k < c.n ? w[c.b0 + (size_t)(j + 2 * k) * c.dp] : other;
+    v[k].y = w && j + 2 * k + 1 < c.n ? w[c.b0 + (size_t)(j + 2 * k + 1) * c.dp] : other;
+  }
 }
 // The same of whole pieces on 16 bytes, all columns kept; not to be kept in registers (CTAs of 1024 threads, 64 registers each): they come from
 // the L1 cache for every row.
-template <int PER>
-__device__ __forceinline__ void ln_params_now(const float* w, float other, int j, float (&v)[PER]) {
+template <int PAIRS>
+__device__ __forceinline__ void ln_params_now(const float* w, float other, int j, float2 (&v)[PAIRS]) {
 #pragma unroll
-  for (int k = 0; k < PER; k += 4) {
+  for (int k = 0; k < PAIRS; k += 2) {
     float4 q = make_float4(other, other, other, other);
-    if (w) asm volatile("ld.global.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(q.x), "=f"(q.y), "=f"(q.z), "=f"(q.w) : "l"(w + j + k));
-    v[k] = q.x; v[k + 1] = q.y; v[k + 2] = q.z; v[k + 3] = q.w;
+    if (w) asm volatile("ld.global.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(q.x), "=f"(q.y), "=f"(q.z), "=f"(q.w) : "l"(w + j + 2 * k));
+    v[k] = make_float2(q.x, q.y);
+    v[k + 1] = make_float2(q.z, q.w);
   }
 }
 
 // The sums of M values over the TPR threads of a row; with more than a warp through shared memory, of which a call and the next use
-// different halves (one barrier of the CTA per call, the same number of calls in all its threads).
+// different halves (one barrier of the group per call).
 template <int TPR, int M>
 __device__ __forceinline__ void ln_row_sums(float (&x)[M], float (*red)[M][32], int& half) {
 #pragma unroll
@@ -233,7 +264,7 @@ __device__ __forceinline__ void ln_row_sums(float (&x)[M], float (*red)[M][32], 
     if (lane == 0)
 #pragma unroll
       for (int m = 0; m < M; ++m) red[half][m][warp] = x[m];
-    __syncthreads();
+    asm volatile("bar.sync %0, %1;" ::"r"(1 + (int)threadIdx.x / TPR), "n"(TPR) : "memory");
 #pragma unroll
     for (int m = 0; m < M; ++m) {
       float t = 0.f;
@@ -247,271 +278,322 @@ __device__ __forceinline__ void ln_row_sums(float (&x)[M], float (*red)[M][32], 
 }
 
 // Rows reach the TPR threads that hold them through a ring of slots in shared memory, filled by bulk copies that the first of them asks for
-// several rows ahead: what is in flight costs no registers, and 100 to 200 KB an SM are in flight whatever the row's length.
+// several rounds ahead: what is in flight costs no registers, and 100 to 200 KB an SM are in flight whatever the row's length.  A round is R
+// consecutive rows: their sums share barriers and run beside one another.
 constexpr int LN_SLOTS = 8;
 struct LnRing {
-  int slots;       // per row of threads
-  int slot_bytes;  // M operands of a row, each rounded up to 16 bytes
+  int slots;      // per group of threads
+  int row_bytes;  // of an operand, rounded up to 16 bytes
 };
-template <typename T, int TPR, int G, int M>
+template <typename T, int TPR, int G, int R, int M>
 struct LnRows {
   const T* src[M];
   int ld[M];
   uint8_t* mine;
   uint64_t* full;
   LnRing ring;
-  int r0, stride, rounds, rows;
+  int g0, stride, rounds, rows;
   uint32_t bytes;
-  bool gone;  // a copy did not come within two seconds: the rest is left, the status says so
+  int slot, phase;  // of the round that is being worked on
+  bool gone;        // a copy did not come within two seconds: the rest is left, the status says so
   int gone_at;
 
   __device__ __forceinline__ LnRows(const LnShape& sh, const LnCols& c, LnRing rg, uint8_t* slots, uint64_t (*bars)[LN_SLOTS]) {
     const int g = threadIdx.x / TPR;
     ring = rg;
-    mine = slots + (size_t)g * ring.slots * ring.slot_bytes;
+    mine = slots + (size_t)g * ring.slots * (M * R * ring.row_bytes);
     full = bars[g];
     bytes = ((uint32_t)c.n * (uint32_t)sizeof(T) + 15u) & ~15u;
     rows = sh.rows;
     stride = gridDim.x * G;
-    rounds = (rows + stride - 1) / stride;
-    r0 = blockIdx.x * G + g;
+    rounds = ((rows + R - 1) / R + stride - 1) / stride;
+    g0 = blockIdx.x * G + g;
+    slot = phase = 0;
     gone = false;
     gone_at = 0;
   }
-  __device__ __forceinline__ long long row(int it) const { return r0 + (long long)it * stride; }
-  __device__ __forceinline__ const uint8_t* slot(int it, int m) const {
-    return mine + (size_t)(it % ring.slots) * ring.slot_bytes + m * (ring.slot_bytes / M);
-  }
-  // By the first thread of the row, for round `it`; whoever read the slot before has passed a barrier since.
+  __device__ __forceinline__ long long row(int it, int q) const { return (g0 + (long long)it * stride) * R + q; }
+  __device__ __forceinline__ bool live(int it, int q) const { return row(it, q) < rows && !gone; }
+  __device__ __forceinline__ const uint8_t* at(int q, int m) const { return mine + (size_t)((slot * R + q) * M + m) * ring.row_bytes; }
+  // By the first thread of the group, for round `it`; whoever read the slot before has passed a barrier since.
   __device__ __forceinline__ void ask(int it) const {
-    if (it >= rounds || row(it) >= rows) return;
-    const uint32_t bar = smem_u32(&full[it % ring.slots]);
-    mbar_arrive_expect_tx(bar, M * bytes);
+    if (it >= rounds || row(it, 0) >= rows || gone) return;
+    const int to = it % ring.slots, here = (int)min((long long)R, rows - row(it, 0));
+    const uint32_t bar = smem_u32(&full[to]), dst = smem_u32(mine + (size_t)to * (M * R * ring.row_bytes));
+    mbar_arrive_expect_tx(bar, (uint32_t)(M * here) * bytes);
+    for (int q = 0; q < here; ++q)
 #pragma unroll
-    for (int m = 0; m < M; ++m)
-      asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(smem_u32(slot(it, m))),
-                   "l"(src[m] + (size_t)row(it) * ld[m]), "r"(bytes), "r"(bar)
-                   : "memory");
+      for (int m = 0; m < M; ++m)
+        asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(
+                         dst + (uint32_t)((q * M + m) * ring.row_bytes)),
+                     "l"(src[m] + (size_t)row(it, q) * ld[m]), "r"(bytes), "r"(bar)
+                     : "memory");
   }
-  __device__ __forceinline__ bool wait(int it, volatile int* s_gone, int* status) {
-    if (!gone && !mbar_wait(smem_u32(&full[it % ring.slots]), (uint32_t)(it / ring.slots) & 1u, s_gone, status)) {
+  __device__ __forceinline__ void wait(int it, volatile int* s_gone, int* status) {
+    if (!gone && row(it, 0) < rows && !mbar_wait(smem_u32(&full[slot]), (uint32_t)phase, s_gone, status)) {
       gone = true;
       gone_at = it;
     }
-    return !gone;
+  }
+  __device__ __forceinline__ void next() {
+    if (++slot == ring.slots) {
+      slot = 0;
+      phase ^= 1;
+    }
   }
   // Before the CTA ends without some of its copies (asked up to round `asked`): they get the same time, for they write to its memory.
   __device__ __forceinline__ void drain(int asked) const {
-    for (int it = gone_at; it <= asked && it < rounds && row(it) < rows; ++it) {
+    for (int it = gone_at; it <= asked && it < rounds && row(it, 0) < rows; ++it) {
       bool ok = false;
       for (int poll = 0; poll < 2000 && !ok; ++poll) ok = mbar_try_wait_hint(smem_u32(&full[it % ring.slots]), (uint32_t)(it / ring.slots) & 1u, 1000000u);
     }
   }
 };
-
-// Forward: two sums over a row's registers, the second about the mean (a sum of squares alone loses the variance of a row with a large
-// mean).  The barrier of the first one says that the row's slot has been read.
-template <typename T, int TPR, int V, int NT>
-__global__ void __launch_bounds__(NT, 1) ln_fwd_kernel(LnShape sh, float eps, const T* X, int ldx, const float* weight, const float* bias,
-                                                    T* Y, int ldy, float* mean, float* rstd, LnRing ring, int* status) {
-  constexpr int PER = LN_PER<T>, G = NT / TPR;
-  constexpr bool KEEP = NT < 1024;
-  extern __shared__ __align__(128) uint8_t slots[];  // [G][slots][slot_bytes]
-  __shared__ float red[2][1][32];
-  __shared__ __align__(8) uint64_t full[G][LN_SLOTS];
-  __shared__ int s_gone;
-  const int t = threadIdx.x % TPR;
-  if (t == 0)
-    for (int k = 0; k < ring.slots; ++k) mbar_init(smem_u32(&full[threadIdx.x / TPR][k]), 1);
-  if (threadIdx.x == 0) s_gone = 0;
-  asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+template <int G>
+__device__ __forceinline__ void ln_setup(uint64_t (*full)[LN_SLOTS], int slots, int* s_gone) {
+  if (threadIdx.x == 0) {
+    *s_gone = 0;
+    for (int g = 0; g < G; ++g)
+      for (int k = 0; k < slots; ++k) mbar_init(smem_u32(&full[g][k]), 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
   __syncthreads();
   pdl_launch_dependents();
   pdl_wait_prior_grids();
+}
+
+// Forward: two sums over a row's registers, the second about the mean (a sum of squares alone loses the variance of a row with a large
+// mean).  The barrier of the first one says that the round's slot has been read.
+template <typename T, int TPR, int V, int NT, int R>
+__global__ void __launch_bounds__(NT, NT >= 512 ? 1 : 512 / NT) ln_fwd_kernel(LnShape sh, float eps, const T* X, int ldx, const float* weight, const float* bias,
+                                                       T* Y, int ldy, float* mean, float* rstd, LnRing ring, int* status) {
+  constexpr int PER = LN_PER<T>, PAIRS = LN_PAIRS<T>, G = NT / TPR;
+  constexpr bool KEEP = NT < 1024;
+  constexpr int one = KEEP ? 1 : 0;
+  extern __shared__ __align__(128) uint8_t slots[];
+  __shared__ float red[2][R][32];
+  __shared__ __align__(8) uint64_t full[G][LN_SLOTS];
+  __shared__ int s_gone;
+  ln_setup<G>(full, ring.slots, &s_gone);
+  const int t = threadIdx.x % TPR;
   const LnCols c = ln_cols(sh);
   const float inv_n = 1.f / (float)c.n;
-  LnRows<T, TPR, G, 1> in(sh, c, ring, slots, full);
+  LnRows<T, TPR, G, R, 1> in(sh, c, ring, slots, full);
   in.src[0] = X;
   in.ld[0] = ldx;
   if (t == 0)
     for (int k = 0; k < ring.slots; ++k) in.ask(k);
-  float w[KEEP ? V : 1][PER], b[KEEP ? V : 1][PER];
+  float2 w[KEEP ? V : 1][PAIRS], b[KEEP ? V : 1][PAIRS];
   if constexpr (KEEP)
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-      ln_params<PER>(weight, 1.f, c, (v * TPR + t) * PER, w[v]);
-      ln_params<PER>(bias, 0.f, c, (v * TPR + t) * PER, b[v]);
+      ln_params<PAIRS>(weight, 1.f, c, (v * TPR + t) * PER, w[v]);
+      ln_params<PAIRS>(bias, 0.f, c, (v * TPR + t) * PER, b[v]);
     }
   int half = 0;
-  for (int it = 0; it < in.rounds; ++it) {
-    const long long r = in.row(it);
-    const bool live = r < sh.rows && in.wait(it, &s_gone, status);
-    float x[V][PER];
-    float s[1] = {0.f};
+  auto loop = [&](auto ragged) {
+    constexpr bool RAGGED = decltype(ragged)::value;
+    for (int it = 0; it < in.rounds; ++it) {
+      in.wait(it, &s_gone, status);
+      float2 x[R][V][PAIRS];
+      float s[R], mu[R];
 #pragma unroll
-    for (int v = 0; v < V; ++v) {
-      const int j = (v * TPR + t) * PER;
-      uint4 q = make_uint4(0u, 0u, 0u, 0u);
-      if (live && j < c.n) q = *reinterpret_cast<const uint4*>(in.slot(it, 0) + (size_t)j * sizeof(T));
-      ln_unpack<T>(q, x[v]);
+      for (int q = 0; q < R; ++q) {
+        float2 sum = ln_both(0.f);
+        const int n = in.live(it, q) ? c.n : 0;
 #pragma unroll
-      for (int k = 0; k < PER; ++k) {
-        if (j + k >= c.n) x[v][k] = 0.f;
-        s[0] += x[v][k];
-      }
-    }
-    ln_row_sums<TPR, 1>(s, red, half);
-    if (TPR == 32) __syncwarp();
-    if (t == 0 && !in.gone) in.ask(it + ring.slots);
-    const float mu = s[0] * inv_n;
-    s[0] = 0.f;
+        for (int v = 0; v < V; ++v) {
+          ln_piece<T, RAGGED>(in.at(q, 0), (v * TPR + t) * PER, n, x[q][v]);
 #pragma unroll
-    for (int v = 0; v < V; ++v)
-#pragma unroll
-      for (int k = 0; k < PER; ++k) {
-        x[v][k] -= mu;
-        if ((v * TPR + t) * PER + k < c.n) s[0] = fmaf(x[v][k], x[v][k], s[0]);
-      }
-    ln_row_sums<TPR, 1>(s, red, half);
-    const float rs = 1.f / sqrtf(fmaf(s[0], inv_n, eps));
-    if (!live) continue;
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-      const int j = (v * TPR + t) * PER;
-      if (j < c.n) {
-        constexpr int one = KEEP ? 1 : 0;
-        if constexpr (!KEEP) {
-          ln_params_now<PER>(weight, 1.f, j, w[0]);
-          ln_params_now<PER>(bias, 0.f, j, b[0]);
+          for (int k = 0; k < PAIRS; ++k) sum = sum + x[q][v][k];
         }
+        s[q] = sum.x + sum.y;
+      }
+      ln_row_sums<TPR, R>(s, red, half);
+      if (TPR == 32) __syncwarp();
+      if (t == 0) in.ask(it + ring.slots);
+      in.next();
 #pragma unroll
-        for (int k = 0; k < PER; ++k) x[v][k] = fmaf(x[v][k] * rs, w[one * v][k], b[one * v][k]);
-        ln_store<T>(Y + (size_t)r * ldy + j, c.n - j, x[v]);
+      for (int q = 0; q < R; ++q) {
+        mu[q] = s[q] * inv_n;
+        float2 sum = ln_both(0.f);
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+          const int j = (v * TPR + t) * PER;
+#pragma unroll
+          for (int k = 0; k < PAIRS; ++k) x[q][v][k] = x[q][v][k] + ln_both(-mu[q]);
+          if (RAGGED ? j + PER > c.n : j >= c.n)
+#pragma unroll
+            for (int k = 0; k < PAIRS; ++k) {
+              if (!RAGGED || j + 2 * k >= c.n) x[q][v][k].x = 0.f;
+              if (!RAGGED || j + 2 * k + 1 >= c.n) x[q][v][k].y = 0.f;
+            }
+#pragma unroll
+          for (int k = 0; k < PAIRS; ++k) sum = ln_fma(x[q][v][k], x[q][v][k], sum);
+        }
+        s[q] = sum.x + sum.y;
+      }
+      ln_row_sums<TPR, R>(s, red, half);
+#pragma unroll
+      for (int q = 0; q < R; ++q) {
+        if (!in.live(it, q)) continue;
+        const float rs = 1.f / sqrtf(fmaf(s[q], inv_n, eps));
+        const long long r = in.row(it, q);
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+          const int j = (v * TPR + t) * PER;
+          if (j < c.n) {
+            if constexpr (!KEEP) {
+              ln_params_now<PAIRS>(weight, 1.f, j, w[0]);
+              ln_params_now<PAIRS>(bias, 0.f, j, b[0]);
+            }
+#pragma unroll
+            for (int k = 0; k < PAIRS; ++k) x[q][v][k] = ln_fma(x[q][v][k] * ln_both(rs), w[one * v][k], b[one * v][k]);
+            ln_store<T, RAGGED>(Y + (size_t)r * ldy + j, c.n - j, x[q][v]);
+          }
+        }
+        if (t == 0) {
+          if (mean) mean[r] = mu[q];
+          if (rstd) rstd[r] = rs;
+        }
       }
     }
-    if (t == 0) {
-      if (mean) mean[r] = mu;
-      if (rstd) rstd[r] = rs;
-    }
-  }
+  };
+  if (c.n % PER) loop(std::true_type{});
+  else loop(std::false_type{});
   if (in.gone && t == 0) in.drain(in.gone_at + ring.slots - 1);
 }
 
 // Backward: a thread keeps its columns' sums for the weight and the bias over all rows of the CTA and leaves them in `partial`
 // [CTA][2][N].  A row is read from its slot twice, for its sums and for dx, which costs less than the registers that would hold it; its slot is
-// asked for again one row later: the barrier of that row's sums says that nobody reads it any more.
-template <typename T, int TPR, int V, int NT>
-__global__ void __launch_bounds__(NT, 1) ln_bwd_kernel(LnShape sh, const T* dY, int lddy, const T* X, int ldx, const float* weight,
-                                                    const float* mean, const float* rstd, T* dX, int lddx, float* partial,
-                                                    LnRing ring, int* status) {
-  constexpr int PER = LN_PER<T>, G = NT / TPR;
+// asked for again one round later: the barrier of that round's sums says that nobody reads it any more.
+template <typename T, int TPR, int V, int NT, int R>
+__global__ void __launch_bounds__(NT, NT >= 512 ? 1 : 512 / NT) ln_bwd_kernel(LnShape sh, const T* dY, int lddy, const T* X, int ldx, const float* weight,
+                                                       const float* mean, const float* rstd, T* dX, int lddx, float* partial,
+                                                       LnRing ring, int* status) {
+  constexpr int PER = LN_PER<T>, PAIRS = LN_PAIRS<T>, G = NT / TPR;
   constexpr bool KEEP = NT < 1024;
-  extern __shared__ __align__(128) uint8_t slots[];  // [G][slots][slot_bytes]; at the end the sums of the G rows of threads
-  __shared__ float red[2][2][32];
+  constexpr int one = KEEP ? 1 : 0;
+  extern __shared__ __align__(128) uint8_t slots[];  // at the end the sums of the CTA's groups
+  __shared__ float red[2][2 * R][32];
   __shared__ __align__(8) uint64_t full[G][LN_SLOTS];
   __shared__ int s_gone;
+  ln_setup<G>(full, ring.slots, &s_gone);
   const int t = threadIdx.x % TPR, g = threadIdx.x / TPR;
-  if (t == 0)
-    for (int k = 0; k < ring.slots; ++k) mbar_init(smem_u32(&full[g][k]), 1);
-  if (threadIdx.x == 0) s_gone = 0;
-  asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-  __syncthreads();
-  pdl_launch_dependents();
-  pdl_wait_prior_grids();
   const LnCols c = ln_cols(sh);
   const float inv_n = 1.f / (float)c.n;
-  LnRows<T, TPR, G, 2> in(sh, c, ring, slots, full);
+  LnRows<T, TPR, G, R, 2> in(sh, c, ring, slots, full);
   in.src[0] = X;
   in.ld[0] = ldx;
   in.src[1] = dY;
   in.ld[1] = lddy;
   if (t == 0)
     for (int k = 0; k < ring.slots; ++k) in.ask(k);
-  constexpr int one = KEEP ? 1 : 0;
-  float dw[V][PER], db[V][PER], w[KEEP ? V : 1][PER];
+  float2 dw[V][PAIRS], db[V][PAIRS], w[KEEP ? V : 1][PAIRS];
 #pragma unroll
   for (int v = 0; v < V; ++v) {
-    if constexpr (KEEP) ln_params<PER>(weight, 1.f, c, (v * TPR + t) * PER, w[v]);
+    if constexpr (KEEP) ln_params<PAIRS>(weight, 1.f, c, (v * TPR + t) * PER, w[v]);
 #pragma unroll
-    for (int k = 0; k < PER; ++k) dw[v][k] = db[v][k] = 0.f;
+    for (int k = 0; k < PAIRS; ++k) dw[v][k] = db[v][k] = ln_both(0.f);
   }
   int half = 0;
-  float mu = 0.f, rs = 0.f;
-  if (in.r0 < sh.rows) {
-    mu = mean[in.r0];
-    rs = rstd[in.r0];
-  }
-  for (int it = 0; it < in.rounds; ++it) {
-    const long long row = in.row(it);
-    const bool live = row < sh.rows && in.wait(it, &s_gone, status);
-    float mu2 = 0.f, rs2 = 0.f;  // of the next row, fetched behind this one's arithmetic
-    if (row + in.stride < sh.rows) {
-      mu2 = mean[row + in.stride];
-      rs2 = rstd[row + in.stride];
+  float mu[R], rs[R];  // of the round's rows; the next ones' are fetched behind this one's arithmetic
+  auto stats = [&](int it, int q, float& m, float& r) {
+    m = r = 0.f;
+    if (it < in.rounds && in.row(it, q) < sh.rows) {
+      m = mean[in.row(it, q)];
+      r = rstd[in.row(it, q)];
     }
-    float s[2] = {0.f, 0.f};
-    if (live) {
+  };
 #pragma unroll
-      for (int v = 0; v < V; ++v) {
-        const int j = (v * TPR + t) * PER;
-        if (j < c.n) {
-          float x[PER], dy[PER];
-          ln_unpack<T>(*reinterpret_cast<const uint4*>(in.slot(it, 0) + (size_t)j * sizeof(T)), x);
-          ln_unpack<T>(*reinterpret_cast<const uint4*>(in.slot(it, 1) + (size_t)j * sizeof(T)), dy);
-          if constexpr (!KEEP) ln_params_now<PER>(weight, 1.f, j, w[0]);
+  for (int q = 0; q < R; ++q) stats(0, q, mu[q], rs[q]);
+  auto loop = [&](auto ragged) {
+    constexpr bool RAGGED = decltype(ragged)::value;
+    for (int it = 0; it < in.rounds; ++it) {
+      in.wait(it, &s_gone, status);
+      float mu2[R], rs2[R], s[2 * R];
 #pragma unroll
-          for (int k = 0; k < PER; ++k) {
-            const bool real = j + k < c.n;
-            const float xh = real ? (x[k] - mu) * rs : 0.f, d = real ? dy[k] : 0.f, e = d * w[one * v][k];
-            s[0] += e;
-            s[1] = fmaf(e, xh, s[1]);
-            dw[v][k] = fmaf(d, xh, dw[v][k]);
-            db[v][k] += d;
+      for (int q = 0; q < R; ++q) stats(it + 1, q, mu2[q], rs2[q]);
+#pragma unroll
+      for (int q = 0; q < R; ++q) {
+        const float2 scale = ln_both(rs[q]), offset = ln_both(-mu[q]);
+        float2 s1 = ln_both(0.f), s2 = ln_both(0.f);
+        if (in.live(it, q)) {
+#pragma unroll
+          for (int v = 0; v < V; ++v) {
+            const int j = (v * TPR + t) * PER;
+            if (j < c.n) {
+              float2 x[PAIRS], dy[PAIRS];
+              ln_piece<T, RAGGED>(in.at(q, 0), j, c.n, x);
+              ln_piece<T, RAGGED>(in.at(q, 1), j, c.n, dy);
+              if constexpr (!KEEP) ln_params_now<PAIRS>(weight, 1.f, j, w[0]);
+#pragma unroll
+              for (int k = 0; k < PAIRS; ++k) {
+                const float2 xh = (x[k] + offset) * scale, e = dy[k] * w[one * v][k];
+                s1 = s1 + e;
+                s2 = ln_fma(e, xh, s2);
+                dw[v][k] = ln_fma(dy[k], xh, dw[v][k]);
+                db[v][k] = db[v][k] + dy[k];
+              }
+            }
+          }
+        }
+        s[2 * q] = s1.x + s1.y;
+        s[2 * q + 1] = s2.x + s2.y;
+      }
+      ln_row_sums<TPR, 2 * R>(s, red, half);
+      if (TPR == 32) __syncwarp();
+      if (t == 0 && it > 0) in.ask(it - 1 + ring.slots);
+#pragma unroll
+      for (int q = 0; q < R; ++q) {
+        if (!dX || !in.live(it, q)) continue;
+        const float2 scale = ln_both(rs[q]), offset = ln_both(-mu[q]);
+        const float2 s1 = ln_both(-s[2 * q] * inv_n), s2 = ln_both(-s[2 * q + 1] * inv_n);
+        T* dx = dX + (size_t)in.row(it, q) * lddx;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+          const int j = (v * TPR + t) * PER;
+          if (j < c.n) {
+            float2 x[PAIRS], dy[PAIRS];
+            ln_piece<T, RAGGED>(in.at(q, 0), j, c.n, x);
+            ln_piece<T, RAGGED>(in.at(q, 1), j, c.n, dy);
+            if constexpr (!KEEP) ln_params_now<PAIRS>(weight, 1.f, j, w[0]);
+#pragma unroll
+            for (int k = 0; k < PAIRS; ++k)
+              x[k] = scale * ln_fma((x[k] + offset) * scale, s2, ln_fma(dy[k], w[one * v][k], s1));
+            ln_store<T, RAGGED>(dx + j, c.n - j, x);
           }
         }
       }
-    }
-    ln_row_sums<TPR, 2>(s, red, half);
-    if (TPR == 32) __syncwarp();
-    if (t == 0 && it > 0 && !in.gone) in.ask(it - 1 + ring.slots);
-    if (live && dX) {
-      const float s1 = s[0] * inv_n, s2 = s[1] * inv_n;
+      in.next();
 #pragma unroll
-      for (int v = 0; v < V; ++v) {
-        const int j = (v * TPR + t) * PER;
-        if (j < c.n) {
-          float x[PER], dy[PER];
-          ln_unpack<T>(*reinterpret_cast<const uint4*>(in.slot(it, 0) + (size_t)j * sizeof(T)), x);
-          ln_unpack<T>(*reinterpret_cast<const uint4*>(in.slot(it, 1) + (size_t)j * sizeof(T)), dy);
-          if constexpr (!KEEP) ln_params_now<PER>(weight, 1.f, j, w[0]);
-#pragma unroll
-          for (int k = 0; k < PER; ++k) x[k] = rs * (dy[k] * w[one * v][k] - s1 - (x[k] - mu) * rs * s2);
-          ln_store<T>(dX + (size_t)row * lddx + j, c.n - j, x);
-        }
+      for (int q = 0; q < R; ++q) {
+        mu[q] = mu2[q];
+        rs[q] = rs2[q];
       }
     }
-    mu = mu2;
-    rs = rs2;
-  }
+  };
+  if (c.n % PER) loop(std::true_type{});
+  else loop(std::false_type{});
   if (in.gone && t == 0) in.drain(in.gone_at + ring.slots - 1);
   if (!partial) return;
-  // the rows of threads added in their order
+  // the groups' sums added in their order
   if constexpr (G > 1) {
-    float* sums = reinterpret_cast<float*>(slots);  // [2][V * TPR * PER]
+    float2* sums = reinterpret_cast<float2*>(slots);  // [2][V * TPR * PAIRS]
     for (int k = 0; k < G; ++k) {
       __syncthreads();
       if (g == k)
 #pragma unroll
         for (int v = 0; v < V; ++v)
 #pragma unroll
-          for (int q = 0; q < PER; ++q) {
-            const int j = (v * TPR + t) * PER + q;
+          for (int q = 0; q < PAIRS; ++q) {
+            const int j = (v * PAIRS + q) * TPR + t;
             if (k > 0) {
-              dw[v][q] += sums[j];
-              db[v][q] += sums[V * TPR * PER + j];
+              dw[v][q] = dw[v][q] + sums[j];
+              db[v][q] = db[v][q] + sums[V * TPR * PAIRS + j];
             }
             sums[j] = dw[v][q];
-            sums[V * TPR * PER + j] = db[v][q];
+            sums[V * TPR * PAIRS + j] = db[v][q];
           }
     }
     if (g != G - 1) return;
@@ -519,11 +601,16 @@ __global__ void __launch_bounds__(NT, 1) ln_bwd_kernel(LnShape sh, const T* dY, 
 #pragma unroll
   for (int v = 0; v < V; ++v)
 #pragma unroll
-    for (int q = 0; q < PER; ++q) {
-      const int j = (v * TPR + t) * PER + q;
+    for (int q = 0; q < PAIRS; ++q) {
+      const int j = (v * TPR + t) * PER + 2 * q;
+      float* to = partial + (size_t)blockIdx.x * 2 * sh.N + j;
       if (j < c.n) {
-        partial[((size_t)blockIdx.x * 2 + 0) * sh.N + j] = dw[v][q];
-        partial[((size_t)blockIdx.x * 2 + 1) * sh.N + j] = db[v][q];
+        to[0] = dw[v][q].x;
+        to[sh.N] = db[v][q].x;
+      }
+      if (j + 1 < c.n) {
+        to[1] = dw[v][q].y;
+        to[sh.N + 1] = db[v][q].y;
       }
     }
 }
@@ -532,28 +619,47 @@ inline bool ln_on16(const void* p, long long ld_bytes) { return (reinterpret_cas
 
 // Calls run(TPR, V, NT) (as integral constants) for rows of N elements: 16 elements a thread, 8 in short rows.  False: the row is too long.
 template <typename T, typename Run>
-bool ln_rows_of_threads(int N, Run run) {
+bool ln_groups(int N, Run run) {
   constexpr int PER = LN_PER<T>, V = 16 / PER;
 #define LN_TRY(TPR, VV, NT)                                                                                        \
   if (N <= TPR * VV * PER) {                                                                                       \
     run(std::integral_constant<int, TPR>{}, std::integral_constant<int, VV>{}, std::integral_constant<int, NT>{}); \
     return true;                                                                                                   \
   }
-  LN_TRY(32, V / 2, 128)
-  LN_TRY(32, V, 128)
-  LN_TRY(64, V, 128)
-  LN_TRY(128, V, 128)
-  LN_TRY(256, V, 256)
+  // CTAs of 512 threads, one an SM: 148 rows of partial sums to add up, not 592 (those took 15 us)
+  LN_TRY(32, V / 2, 512)
+  LN_TRY(32, V, 512)
+  LN_TRY(64, V, 512)
+  LN_TRY(128, V, 512)
+  LN_TRY(256, V, 512)
   LN_TRY(512, V, 512)
   LN_TRY(1024, V, 1024)
 #undef LN_TRY
   return false;
 }
+// Two rows a round, or one where that leaves groups without rows, where the slots do not fit, and in CTAs of 1024 threads.  M operands.  run(R, CTAs an
+// SM, CTAs, slots); false: not even two rows fit.
 constexpr int LN_SMEM = 200 << 10;  // of an SM, for the slots of its CTAs
-// Slots of a row of threads where per_sm CTAs of G such rows share an SM; below two: none.
-inline int ln_slots(int per_sm, int G, int slot_bytes) {
-  const int most = LN_SMEM / per_sm / (G * slot_bytes);
-  return most < LN_SLOTS ? most : LN_SLOTS;
+template <int NT, int G, int M, typename Run>
+bool ln_rounds(const ard_ctx* ctx, int rows, int row_bytes, Run run) {
+  const int per_sm = NT >= 512 ? 1 : 512 / NT;
+  const long long room = (long long)ctx->sm_count * per_sm;
+  auto slots = [&](int R) {
+    const int most = LN_SMEM / per_sm / (G * M * R * row_bytes);
+    return most < LN_SLOTS ? most : LN_SLOTS;
+  };
+  auto blocks = [&](int R) {
+    const long long want = (((long long)rows + R - 1) / R + G - 1) / G;
+    return (int)(want < room ? want : room);
+  };
+  if constexpr (NT < 1024)
+    if (slots(2) >= 2 && rows >= 2 * room * G) {
+      run(std::integral_constant<int, 2>{}, blocks(2), slots(2));
+      return true;
+    }
+  if (slots(1) < 2) return false;
+  run(std::integral_constant<int, 1>{}, blocks(1), slots(1));
+  return true;
 }
 
 template <typename T>
@@ -565,19 +671,19 @@ ard_status ln_fwd(ard_ctx* ctx, const LnShape& sh, float eps, const T* X, int ld
   if (ln_on16(X, ldx * es) && ln_on16(Y, ldy * es)) {
     const bool whole = !sh.hdr && sh.N % LN_PER<T> == 0 && ln_on16(weight, 0) && ln_on16(bias, 0);
     LnRing ring;
-    ring.slot_bytes = (int)((sh.N * es + 15) / 16 * 16);
-    ln_rows_of_threads<T>(sh.N, [&](auto tpr, auto v, auto nt) {
+    ring.row_bytes = (int)((sh.N * es + 15) / 16 * 16);
+    ln_groups<T>(sh.N, [&](auto tpr, auto v, auto nt) {
       constexpr int TPR = decltype(tpr)::value, V = decltype(v)::value, NT = decltype(nt)::value, G = NT / TPR;
-      const int per_sm = NT >= 512 ? 1 : 512 / NT;
-      ring.slots = ln_slots(per_sm, G, ring.slot_bytes);
-      if (ring.slots < 2 || (NT == 1024 && !whole)) return;
-      const int want = (sh.rows + G - 1) / G, room = ctx->sm_count * per_sm;
-      auto kern = ln_fwd_kernel<T, TPR, V, NT>;
-      err = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, LN_SMEM);
-      if (err == cudaSuccess)
-        err = ard_launch(ctx, kern, dim3(want < room ? want : room), dim3(NT), (size_t)G * ring.slots * ring.slot_bytes, s, sh, eps, X, ldx,
-                         weight, bias, Y, ldy, mean, rstd, ring, ctx->d_status);
-      done = true;
+      if (NT == 1024 && !whole) return;
+      done = ln_rounds<NT, G, 1>(ctx, sh.rows, ring.row_bytes, [&](auto r, int blocks, int slots) {
+        constexpr int R = decltype(r)::value;
+        ring.slots = slots;
+        auto kern = ln_fwd_kernel<T, TPR, V, NT, R>;
+        err = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, LN_SMEM);
+        if (err == cudaSuccess)
+          err = ard_launch(ctx, kern, dim3(blocks), dim3(NT), (size_t)G * slots * R * ring.row_bytes, s, sh, eps, X, ldx, weight, bias, Y, ldy,
+                           mean, rstd, ring, ctx->d_status);
+      });
     });
   }
   if (!done) {
@@ -606,26 +712,26 @@ ard_status ln_bwd(ard_ctx* ctx, const LnShape& sh, const T* dY, int lddy, const 
   if (!done && ln_on16(X, ldx * es) && ln_on16(dY, lddy * es) && ln_on16(dX, dX ? lddx * es : 0)) {
     const bool whole = !sh.hdr && sh.N % LN_PER<T> == 0 && ln_on16(weight, 0);
     LnRing ring;
-    ring.slot_bytes = 2 * (int)((sh.N * es + 15) / 16 * 16);
-    ln_rows_of_threads<T>(sh.N, [&](auto tpr, auto v, auto nt) {
+    ring.row_bytes = (int)((sh.N * es + 15) / 16 * 16);
+    ln_groups<T>(sh.N, [&](auto tpr, auto v, auto nt) {
       constexpr int TPR = decltype(tpr)::value, V = decltype(v)::value, NT = decltype(nt)::value, G = NT / TPR;
-      const int per_sm = NT >= 512 ? 1 : 512 / NT;
-      ring.slots = ln_slots(per_sm, G, ring.slot_bytes);
-      if (ring.slots < 2 || (NT == 1024 && !whole)) return;
-      long long blocks = ((long long)sh.rows + G - 1) / G;
-      if (blocks > (long long)ctx->sm_count * per_sm) blocks = (long long)ctx->sm_count * per_sm;
-      if (sums && blocks > fit) return;
-      size_t smem = (size_t)G * ring.slots * ring.slot_bytes;
-      const size_t exchange = G > 1 ? 2 * sizeof(float) * V * TPR * LN_PER<T> : 0;
-      if (smem < exchange) smem = exchange;
-      auto kern = ln_bwd_kernel<T, TPR, V, NT>;
-      err = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, LN_SMEM);
-      if (err == cudaSuccess)
-        err = ard_launch(ctx, kern, dim3((unsigned)blocks), dim3(NT), smem, s, sh, dY, lddy, X, ldx, weight, mean, rstd, dX, lddx, partial,
-                         ring, ctx->d_status);
-      slices = blocks;
-      ctx->launches++;
-      done = true;
+      if (NT == 1024 && !whole) return;
+      ln_rounds<NT, G, 2>(ctx, sh.rows, ring.row_bytes, [&](auto r, int blocks, int slots) {
+        constexpr int R = decltype(r)::value;
+        if (sums && blocks > fit) return;
+        ring.slots = slots;
+        size_t smem = (size_t)G * slots * 2 * R * ring.row_bytes;
+        const size_t exchange = G > 1 ? 2 * sizeof(float) * V * TPR * LN_PER<T> : 0;
+        if (smem < exchange) smem = exchange;
+        auto kern = ln_bwd_kernel<T, TPR, V, NT, R>;
+        err = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, LN_SMEM);
+        if (err == cudaSuccess)
+          err = ard_launch(ctx, kern, dim3(blocks), dim3(NT), smem, s, sh, dY, lddy, X, ldx, weight, mean, rstd, dX, lddx, partial, ring,
+                           ctx->d_status);
+        slices = blocks;
+        ctx->launches++;
+        done = true;
+      });
     });
     ARD_CUDA_OK(err);
   }
