@@ -26,6 +26,12 @@ __device__ __forceinline__ float ln_get(const __nv_bfloat16* x, size_t i) { retu
 __device__ __forceinline__ void ln_put(float* x, size_t i, float v) { x[i] = v; }
 __device__ __forceinline__ void ln_put(__nv_bfloat16* x, size_t i, float v) { x[i] = __float2bfloat16(v); }
 
+// The device's estimate and a Newton step: within an ulp or two, at a quarter of a root and a quotient's instructions, which every thread of a row spends.
+__device__ __forceinline__ float ln_rsqrt(float x) {
+  const float y = rsqrtf(x), h = y * fmaf(-x * y, y, 1.f);  // an infinite y (x = 0) or a NaN stays what it is
+  return isfinite(h) ? fmaf(0.5f, h, y) : y;
+}
+
 constexpr int LN_ANY_THREADS = 256;
 
 __device__ __forceinline__ float ln_block_sum(float x, float* red) {
@@ -60,7 +66,7 @@ __global__ void __launch_bounds__(LN_ANY_THREADS) ln_fwd_any_kernel(LnShape sh, 
       const float d = ln_get(x, j) - mu;
       s = fmaf(d, d, s);
     }
-    const float rs = 1.f / sqrtf(fmaf(ln_block_sum(s, red), inv_n, eps));
+    const float rs = ln_rsqrt(fmaf(ln_block_sum(s, red), inv_n, eps));
     for (int j = threadIdx.x; j < c.n; j += LN_ANY_THREADS) {
       const int u = c.b0 + j * c.dp;
       ln_put(y, j, fmaf((ln_get(x, j) - mu) * rs, weight ? weight[u] : 1.f, bias ? bias[u] : 0.f));
@@ -73,15 +79,11 @@ __global__ void __launch_bounds__(LN_ANY_THREADS) ln_fwd_any_kernel(LnShape sh, 
 }
 
 template <typename T>
-__global__ void __launch_bounds__(LN_ANY_THREADS) ln_dx_any_kernel(LnShape sh, const T* dY, int lddy, const T* X, int ldx,
-                                                                  const float* weight, const float* mean, const float* rstd, T* dX,
-                                                                  int lddx) {
-  __shared__ float red[LN_ANY_THREADS / 32];
-  pdl_launch_dependents();
-  pdl_wait_prior_grids();
-  const LnCols c = ln_cols(sh);
+__device__ __forceinline__ void ln_dx_any(const LnShape& sh, const LnCols& c, const T* dY, int lddy, const T* X, int ldx, const float* weight,
+                                          const float* mean, const float* rstd, T* dX, int lddx, int first, int blocks) {
+  __shared__ float red[2][LN_ANY_THREADS / 32];
   const float inv_n = 1.f / (float)c.n;
-  for (int r = blockIdx.x; r < sh.rows; r += gridDim.x) {
+  for (int r = first; r < sh.rows; r += blocks) {
     const T* x = X + (size_t)r * ldx;
     const T* dy = dY + (size_t)r * lddy;
     T* dx = dX + (size_t)r * lddx;
@@ -92,32 +94,42 @@ __global__ void __launch_bounds__(LN_ANY_THREADS) ln_dx_any_kernel(LnShape sh, c
       s1 += e;
       s2 = fmaf(e, (ln_get(x, j) - mu) * rs, s2);
     }
-    s1 = ln_block_sum(s1, red) * inv_n;
-    s2 = ln_block_sum(s2, red) * inv_n;
+    s1 = ln_block_sum(s1, red[0]) * inv_n;
+    s2 = ln_block_sum(s2, red[1]) * inv_n;
     for (int j = threadIdx.x; j < c.n; j += LN_ANY_THREADS) {
       const float e = ln_get(dy, j) * (weight ? weight[c.b0 + j * c.dp] : 1.f);
       ln_put(dx, j, rs * (e - s1 - (ln_get(x, j) - mu) * rs * s2));
     }
   }
 }
-
 // Sums of dy * xh and dy over a slice of the rows: partial [slice][2][N], column j at place j.
 template <typename T>
-__global__ void __launch_bounds__(LN_ANY_THREADS) ln_dw_any_kernel(LnShape sh, const T* dY, int lddy, const T* X, int ldx,
-                                                                  const float* mean, const float* rstd, float* partial, int per_slice) {
-  __shared__ float red[2][LN_ANY_THREADS / 32][32];
-  pdl_launch_dependents();
-  pdl_wait_prior_grids();
-  const int n = ln_cols(sh).n, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int slice = blockIdx.y, r1 = min((long long)sh.rows, (long long)(slice + 1) * per_slice);
-  for (int c0 = blockIdx.x * 32; c0 < n; c0 += gridDim.x * 32) {
+__device__ __forceinline__ void ln_dw_any(const LnShape& sh, int n, const T* dY, int lddy, const T* X, int ldx, const float* mean,
+                                          const float* rstd, float* partial, int per_slice, int slice, int first, int blocks) {
+  constexpr int WARPS = LN_ANY_THREADS / 32;
+  __shared__ float red[2][WARPS][32];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int r1 = (int)min((long long)sh.rows, (long long)(slice + 1) * per_slice);
+  for (int c0 = first * 32; c0 < n; c0 += blocks * 32) {
     const int j = c0 + lane;
     float w = 0.f, b = 0.f;
     if (j < n)
-      for (int r = slice * per_slice + warp; r < r1; r += LN_ANY_THREADS / 32) {
-        const float dy = ln_get(dY, (size_t)r * lddy + j);
-        w = fmaf(dy, (ln_get(X, (size_t)r * ldx + j) - mean[r]) * rstd[r], w);
-        b += dy;
+      for (int r0 = slice * per_slice + warp; r0 < r1; r0 += 4 * WARPS) {  // four rows' loads at once
+        float x[4], dy[4], m[4], q[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          const int r = min(r0 + u * WARPS, r1 - 1);
+          dy[u] = ln_get(dY, (size_t)r * lddy + j);
+          x[u] = ln_get(X, (size_t)r * ldx + j);
+          m[u] = mean[r];
+          q[u] = rstd[r];
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+          if (r0 + u * WARPS < r1) {
+            w = fmaf(dy[u], (x[u] - m[u]) * q[u], w);
+            b += dy[u];
+          }
       }
     red[0][warp][lane] = w;
     red[1][warp][lane] = b;
@@ -125,11 +137,23 @@ __global__ void __launch_bounds__(LN_ANY_THREADS) ln_dw_any_kernel(LnShape sh, c
     if (warp < 2 && j < n) {
       float t = 0.f;
 #pragma unroll
-      for (int k = 0; k < LN_ANY_THREADS / 32; ++k) t += red[warp][k][lane];
+      for (int k = 0; k < WARPS; ++k) t += red[warp][k][lane];
       partial[((size_t)slice * 2 + warp) * sh.N + j] = t;
     }
     __syncthreads();
   }
+}
+// Both in one launch: the first dx_blocks CTAs take rows, the others columns, gx of them a slice.
+template <typename T>
+__global__ void __launch_bounds__(LN_ANY_THREADS) ln_bwd_any_kernel(LnShape sh, const T* dY, int lddy, const T* X, int ldx, const float* weight,
+                                                                   const float* mean, const float* rstd, T* dX, int lddx, int dx_blocks,
+                                                                   float* partial, int per_slice, int gx) {
+  pdl_launch_dependents();
+  pdl_wait_prior_grids();
+  const LnCols c = ln_cols(sh);
+  const int k = (int)blockIdx.x - dx_blocks;
+  if (k < 0) ln_dx_any(sh, c, dY, lddy, X, ldx, weight, mean, rstd, dX, lddx, (int)blockIdx.x, dx_blocks);
+  else ln_dw_any(sh, c.n, dY, lddy, X, ldx, mean, rstd, partial, per_slice, k / gx, k % gx, gx);
 }
 
 // The slices' sums added in a fixed order, into the units' places: a warp's lanes take 32 columns, its CTA's warps the slices.
@@ -259,11 +283,6 @@ __device__ __forceinline__ void ln_params_now(const float* w, float other, int j
   }
 }
 
-// The device's estimate and a Newton step: within an ulp or two, at a quarter of a root and a quotient's instructions, which every thread of a row spends.
-__device__ __forceinline__ float ln_rsqrt(float x) {
-  const float y = rsqrtf(x), h = y * fmaf(-x * y, y, 1.f);  // an infinite y (x = 0) or a NaN stays what it is
-  return isfinite(h) ? fmaf(0.5f, h, y) : y;
-}
 // The sums of M values over the TPR threads of a row; with more than a warp through shared memory, of which a call and the next use
 // different halves (one barrier of the group per call).
 template <int TPR, int M>
@@ -767,23 +786,19 @@ ard_status ln_bwd(ard_ctx* ctx, const LnShape& sh, const T* dY, int lddy, const 
     ARD_CUDA_OK(err);
   }
   if (!done) {
-    if (dX) {
-      const int room = 8 * ctx->sm_count;
-      ARD_CUDA_OK(ard_launch(ctx, ln_dx_any_kernel<T>, dim3(sh.rows < room ? sh.rows : room), dim3(LN_ANY_THREADS), 0, s, sh, dY, lddy, X,
-                             ldx, weight, mean, rstd, dX, lddx));
-      ctx->launches++;
-    }
+    const int room = 8 * ctx->sm_count, dx_blocks = !dX ? 0 : sh.rows < room ? sh.rows : room;
+    int gx = (sh.N + 31) / 32, per = 0;
+    if (gx > 4096) gx = 4096;
     if (sums) {
-      const int gx = (sh.N + 31) / 32;
       slices = (sh.rows + 63) / 64;
       if (slices > fit) slices = fit;
       if (slices > 1024) slices = 1024;
-      const int per = (int)((sh.rows + slices - 1) / slices);
+      per = (int)((sh.rows + slices - 1) / slices);
       slices = (sh.rows + per - 1) / per;
-      ARD_CUDA_OK(ard_launch(ctx, ln_dw_any_kernel<T>, dim3(gx < 4096 ? gx : 4096, (unsigned)slices), dim3(LN_ANY_THREADS), 0, s, sh, dY,
-                             lddy, X, ldx, mean, rstd, partial, per));
-      ctx->launches++;
     }
+    ARD_CUDA_OK(ard_launch(ctx, ln_bwd_any_kernel<T>, dim3((unsigned)(dx_blocks + slices * gx)), dim3(LN_ANY_THREADS), 0, s, sh, dY, lddy, X, ldx,
+                           weight, mean, rstd, dX, lddx, dx_blocks, partial, per, gx));
+    ctx->launches++;
   }
   if (sums) {
     ARD_CUDA_OK(ard_launch(ctx, ln_dw_sum_kernel, dim3((sh.N + 31) / 32, 2), dim3(LN_SUM_WARPS * 32), 0, s, sh, (const float*)partial,
