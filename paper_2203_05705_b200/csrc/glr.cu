@@ -370,7 +370,7 @@ __device__ __forceinline__ void glr_setup(int CL, Shared& sh) {
 }
 
 template <typename T, int VEC, bool GATE, int CW, int WT, int SPT, bool BULK>
-__global__ void __launch_bounds__(CW* WT * 32, CW* WT < 8 || SPT == 16 ? 1 : SPT < 8 ? 3 : 2)
+__global__ void __launch_bounds__(CW* WT * 32, CW* WT < 8 ? 1 : SPT < 8 ? 3 : 2)
     glr_fwd_kernel(const GlrArgs a, int CL, const __grid_constant__ GlrTiles tiles) {
   using V = GlrV<VEC>;
   constexpr int M = GATE ? 3 : 2, SLAB = WT * SPT;
@@ -471,7 +471,7 @@ __global__ void __launch_bounds__(CW* WT * 32, CW* WT < 8 || SPT == 16 ? 1 : SPT
 }
 
 template <typename T, int VEC, bool GATE, int CW, int WT, int SPT, bool BULK>
-__global__ void __launch_bounds__(CW* WT * 32, CW* WT < 8 || SPT == 16 ? 1 : SPT < 8 ? 3 : 2)
+__global__ void __launch_bounds__(CW* WT * 32, CW* WT < 8 ? 1 : SPT < 8 ? 3 : 2)
     glr_bwd_kernel(const GlrArgs a, int CL, const __grid_constant__ GlrTiles tiles) {
   using V = GlrV<VEC>;
   constexpr int M = GATE ? 4 : 3, SLAB = WT * SPT;
@@ -639,13 +639,13 @@ ard_status glr_launch(ard_ctx* ctx, K kern, const GlrArgs& a, const GlrTiles& ti
   return ARD_OK;
 }
 
-// CTAs of a cluster that share a sequence's slabs (128 steps each, a CTA an SM), where the units alone leave more than half of the SMs idle: as many as
-// let all units run at once.  How many clusters of a size the device holds goes by how its SMs are grouped, and is asked once.
+// CTAs of a cluster that share a sequence's slabs (64 steps each), where the units alone leave more than half of the SMs idle: as many as let all units
+// run at once.  How many clusters of a size the device holds goes by how its SMs are grouped, and is asked once.
 inline int glr_cluster(ard_ctx* ctx, long long units, long long slabs) {
   if (2 * units > ctx->sm_count || slabs < 2) return 1;
   if (ctx->glr_room[2] == 0) {
-    auto kern = glr_fwd_kernel<__nv_bfloat16, 2, true, 1, 8, 16, true>;
-    constexpr int smem = glr_ring<GlrFeed<__nv_bfloat16, 2, 3, 8, 16, true>>();
+    auto kern = glr_fwd_kernel<__nv_bfloat16, 2, true, 1, 8, 8, true>;
+    constexpr int smem = glr_ring<GlrFeed<__nv_bfloat16, 2, 3, 8, 8, true>>();
     cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
     cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
     for (int cl = 2; cl <= GLR_CLUSTER; ++cl) ctx->glr_room[cl] = ard_cluster_room(ctx, kern, cl, 256, smem) / cl;
@@ -668,15 +668,14 @@ bool glr_tiles(ard_ctx* ctx, const GlrArgs& a, std::initializer_list<std::pair<c
   return true;
 }
 
-// Steps of a thread.  As few as a short sequence's slab of 8 warps needs (three CTAs an SM: 35 x 64 x 1024 11.3 -> 8.7 us); 16 (one CTA an SM) where
-// clusters share the sequences, since what a round costs besides its steps is then paid half as often; 8 otherwise.  run(SPT, CTAs an SM, cluster).
+// Steps of a thread.  As few as a short sequence's slab of 8 warps needs (three CTAs an SM: 35 x 64 x 1024 11.3 -> 8.7 us); 8, two CTAs an SM, otherwise.
+// (16 in clusters, one CTA an SM: what a round costs besides its steps is paid half as often, but nothing runs beside it: 16384 x 1 x 1024 50.9 / 81.2
+// us forward / backward, here 49 / 76.7; 4096 steps 17.4 / 25.8, here 15.7 / 23.)  run(SPT, CTAs an SM, cluster).
 template <typename Run>
 ard_status glr_steps(ard_ctx* ctx, const GlrArgs& a, int channels, Run run) {
   if (a.T <= 16) return run(std::integral_constant<int, 2>{}, 3, 1);
   if (a.T <= 40) return run(std::integral_constant<int, 5>{}, 3, 1);
-  const int CL = glr_cluster(ctx, glr_units(a, channels), ((long long)a.T + 127) / 128);
-  if (CL > 1) return run(std::integral_constant<int, 16>{}, 1, CL);
-  return run(std::integral_constant<int, 8>{}, 2, 1);
+  return run(std::integral_constant<int, 8>{}, 2, glr_cluster(ctx, glr_units(a, channels), ((long long)a.T + 63) / 64));
 }
 
 template <typename T, int VEC, bool GATE>
