@@ -164,7 +164,7 @@ struct GlrMap {
   __device__ __forceinline__ GlrV<VEC> of(const GlrV<VEC>& x) const { return glr_fma(a, x, b); }
 };
 
-// What the kernels run over: units of CW * 32 * VEC channels of one sequence, `rounds` times CL slabs of WT * SPT steps each.
+// What the kernels run over: units of W * VEC channels of one sequence, `rounds` times CL slabs of WT * SPT steps each.
 struct GlrSpan {
   int n, dp, b0, groups, units, rounds;
   __device__ __forceinline__ GlrSpan(const GlrArgs& a, int channels, int steps) {
@@ -182,16 +182,16 @@ struct GlrSpan {
   }
   __device__ __forceinline__ int len(const GlrArgs& a, int b) const { return a.lens ? min(max(a.lens[b], 0), a.T) : a.T; }
 };
-// A thread's place in a unit: VEC channels of one sequence, SPT consecutive steps of every slab.
-template <int VEC, int CW, int WT>
+// A thread's place in a unit: VEC channels of one sequence, SPT consecutive steps of every slab.  W threads stand side by side over the unit's channels
+// (warps, or half a warp), WT groups of them over a slab's steps.
+template <int VEC, int W, int WT>
 struct GlrPlace {
   int wt, ch, b, j, valid, col, len;
   __device__ __forceinline__ GlrPlace(const GlrArgs& a, const GlrSpan& sp, int unit) {
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    wt = warp % WT;
-    ch = warp / WT * 32 + lane;
+    wt = threadIdx.x / W;
+    ch = threadIdx.x % W;
     b = unit / sp.groups;
-    j = ((unit - b * sp.groups) * CW * 32 + ch) * VEC;
+    j = ((unit - b * sp.groups) * W + ch) * VEC;
     valid = max(0, min(VEC, sp.n - j));
     col = min(j, (sp.n - 1) / VEC * VEC);  // where a lane without channels reads
     len = sp.len(a, b);
@@ -201,18 +201,18 @@ struct GlrPlace {
   }
 };
 
-// Where M operands of a slab come from.  BULK: tiles [WT * SPT steps][32 * VEC channels] that the copy engine brings into a ring of
+// Where M operands of a slab come from.  BULK: tiles [WT * SPT steps][W * VEC channels] that the copy engine brings into a ring of
 // slots, several slabs ahead and over the ends of units (rows of 16-byte aligned pieces).  Otherwise registers, into which a
 // thread fetches its own values of the unit's next slab as soon as this one's are used.
 struct GlrTiles {
   CUtensorMap map[4];
 };
-template <typename T, int VEC, int M, int WT, int SPT, bool BULK>
+template <typename T, int VEC, int M, int W, int WT, int SPT, bool BULK>
 struct GlrFeed;
 
-template <typename T, int VEC, int M, int WT, int SPT>
-struct GlrFeed<T, VEC, M, WT, SPT, true> {
-  static constexpr int ROW = 32 * VEC * (int)sizeof(T), TILE = WT * SPT * ROW, SLOT = M * TILE;
+template <typename T, int VEC, int M, int W, int WT, int SPT>
+struct GlrFeed<T, VEC, M, W, WT, SPT, true> {
+  static constexpr int ROW = W * VEC * (int)sizeof(T), TILE = WT * SPT * ROW, SLOT = M * TILE;
   static constexpr int SLOTS = M == 4 ? 2 : 3;  // two CTAs an SM with 64 to 72 KB each
   uint8_t* slots;
   uint64_t* full;
@@ -231,7 +231,7 @@ struct GlrFeed<T, VEC, M, WT, SPT, true> {
     const int to = asked++ % SLOTS;
     const uint32_t bar = smem_u32(&full[to]), dst = smem_u32(slots + to * SLOT);
     if (ts < len) {
-      const int b = unit / sp.groups, x = (unit - b * sp.groups) * 32 * VEC;
+      const int b = unit / sp.groups, x = (unit - b * sp.groups) * W * VEC;
       mbar_arrive_expect_tx(bar, SLOT);
 #pragma unroll
       for (int m = 0; m < M; ++m)
@@ -264,13 +264,13 @@ struct GlrFeed<T, VEC, M, WT, SPT, true> {
       for (int poll = 0; poll < 2000 && !ok; ++poll) ok = mbar_try_wait_hint(smem_u32(&full[k % SLOTS]), (uint32_t)(k / SLOTS) & 1u, 1000000u);
     }
   }
-  __device__ __forceinline__ uint32_t raw(int wt, int m, int k) const {  // CW = 1
-    const uint8_t* p = slots + slot * SLOT + m * TILE + (wt * SPT + k) * ROW + (threadIdx.x & 31) * (VEC * (int)sizeof(T));
+  __device__ __forceinline__ uint32_t raw(int wt, int m, int k) const {
+    const uint8_t* p = slots + slot * SLOT + m * TILE + (wt * SPT + k) * ROW + (threadIdx.x % W) * (VEC * (int)sizeof(T));
     return *reinterpret_cast<const uint32_t*>(p);
   }
 };
-template <typename T, int VEC, int M, int WT, int SPT>
-struct GlrFeed<T, VEC, M, WT, SPT, false> {
+template <typename T, int VEC, int M, int W, int WT, int SPT>
+struct GlrFeed<T, VEC, M, W, WT, SPT, false> {
   uint32_t q[M][SPT];
   const T* src[M];
   size_t step[M];
@@ -290,9 +290,9 @@ struct GlrFeed<T, VEC, M, WT, SPT, false> {
 // next round finds it.  The cluster's CTAs send each other their slabs' maps by asynchronous stores that count on the receiver's
 // barrier: a barrier of the cluster would wait for the outputs' stores, 2 us a round (bulk copies between their memories: forward the same, backward
 // 30 % slower).  Every CTA hears from all of them in every round, so none is more than a round ahead and two sets of places are enough.
-template <int VEC, int CW, int FROM>
+template <int VEC, int W, int FROM>
 struct GlrMail {
-  GlrMap<VEC> box[2][FROM][CW * 32];
+  GlrMap<VEC> box[2][FROM][W];
   uint64_t bar[2];
 };
 template <int VEC>
@@ -309,19 +309,19 @@ __device__ __forceinline__ void glr_send(GlrMap<VEC>* box, uint64_t* bar, int r,
                  "r"(rbar)
                  : "memory");
 }
-template <int VEC, int CW, int WT>
+template <int VEC, int W, int WT>
 struct GlrShared {
-  GlrMap<VEC> warp[2][WT][CW * 32];
-  GlrV<VEC> state[2][CW * 32];
-  GlrMail<VEC, CW, (WT > 1 ? GLR_CLUSTER : 1)> post;
+  GlrMap<VEC> warp[2][WT][W];
+  GlrV<VEC> state[2][W];
+  GlrMail<VEC, W, (WT > 1 ? GLR_CLUSTER : 1)> post;
   uint64_t full[3];
   int gone;
 };
 
 // Behind the barrier that follows the warps' maps: the state that enters this warp's steps.  x: what enters the unit's first round.  FORWARD: warps
 // count in the order of the steps, else against it.  `mail`: rounds of the cluster so far.
-template <bool FORWARD, int VEC, int CW, int WT>
-__device__ __forceinline__ GlrV<VEC> glr_enter(GlrShared<VEC, CW, WT>& sh, int wt, int ch, bool first, int mail, int CL, int rank,
+template <bool FORWARD, int VEC, int W, int WT>
+__device__ __forceinline__ GlrV<VEC> glr_enter(GlrShared<VEC, W, WT>& sh, int wt, int ch, bool first, int mail, int CL, int rank,
                                               const GlrV<VEC>& x, int* status) {
   GlrV<VEC> c = x;
   if constexpr (WT > 1) {
@@ -335,7 +335,7 @@ __device__ __forceinline__ GlrV<VEC> glr_enter(GlrShared<VEC, CW, WT>& sh, int w
         for (int k = 1; k < WT; ++k) all.then(sh.warp[set][FORWARD ? k : WT - 1 - k][ch]);
         for (int r = 0; r < CL; ++r) glr_send<VEC>(&sh.post.box[set][rank][ch], &sh.post.bar[set], r, all);
       }
-      if (threadIdx.x == 0) mbar_arrive_expect_tx(smem_u32(&sh.post.bar[set]), (uint32_t)(CL * CW * 32 * sizeof(GlrMap<VEC>)));
+      if (threadIdx.x == 0) mbar_arrive_expect_tx(smem_u32(&sh.post.bar[set]), (uint32_t)(CL * W * sizeof(GlrMap<VEC>)));
       mbar_wait(smem_u32(&sh.post.bar[set]), (uint32_t)(mail >> 1) & 1u, &sh.gone, status);
       for (int r = 0; r < rank; ++r) c = sh.post.box[set][r][ch].of(c);
       if (wt == LAST) {
@@ -369,24 +369,24 @@ __device__ __forceinline__ void glr_setup(int CL, Shared& sh) {
   pdl_wait_prior_grids();
 }
 
-template <typename T, int VEC, bool GATE, int CW, int WT, int SPT, bool BULK>
-__global__ void __launch_bounds__(CW* WT * 32, CW* WT < 8 ? 1 : SPT < 8 ? 3 : 2)
+template <typename T, int VEC, bool GATE, int W, int WT, int SPT, bool BULK>
+__global__ void __launch_bounds__(W* WT, W* WT < 256 ? 1 : SPT < 8 ? 3 : 2)
     glr_fwd_kernel(const GlrArgs a, int CL, const __grid_constant__ GlrTiles tiles) {
   using V = GlrV<VEC>;
   constexpr int M = GATE ? 3 : 2, SLAB = WT * SPT;
   extern __shared__ __align__(128) uint8_t slots[];
-  __shared__ __align__(16) GlrShared<VEC, CW, WT> sh;
+  __shared__ __align__(16) GlrShared<VEC, W, WT> sh;
   glr_setup(CL, sh);
   const int cluster = blockIdx.x / CL, rank = blockIdx.x % CL, clusters = gridDim.x / CL;
-  const GlrSpan sp(a, CW * 32 * VEC, SLAB * CL);
-  GlrFeed<T, VEC, M, WT, SPT, BULK> in(slots, sh.full, &sh.gone, cluster);
+  const GlrSpan sp(a, W * VEC, SLAB * CL);
+  GlrFeed<T, VEC, M, W, WT, SPT, BULK> in(slots, sh.full, &sh.gone, cluster);
   if constexpr (BULK)
     if (threadIdx.x == 0)
       for (int k = 0; k < in.SLOTS; ++k) in.ask(a, sp, tiles, CL, rank, clusters, false);
   const V alpha = V::all(a.alpha);
   int mail = 0;
   for (int unit = cluster; unit < sp.units; unit += clusters) {
-    const GlrPlace<VEC, CW, WT> at(a, sp, unit);
+    const GlrPlace<VEC, W, WT> at(a, sp, unit);
     const size_t step_y = (size_t)a.B * a.ldy;
     T* y = (T*)a.Y + (size_t)at.b * a.ldy + at.j;
     if constexpr (!BULK) {
@@ -401,7 +401,7 @@ __global__ void __launch_bounds__(CW* WT * 32, CW* WT < 8 ? 1 : SPT < 8 ? 3 : 2)
     V first;  // the state that enters the unit
 #pragma unroll
     for (int v = 0; v < VEC; ++v) first.v[v] = a.h0 && v < at.valid ? a.h0[at.of(a, sp, v)] : 0.f;
-    const bool inside = (unit % sp.groups + 1) * (CW * 32 * VEC) <= sp.n;
+    const bool inside = (unit % sp.groups + 1) * (W * VEC) <= sp.n;
     V c = first;
     // FULL: all steps of the slab are a sequence's, all channels of the unit exist; nothing is asked per step
     auto slab = [&](auto full, int it) {
@@ -470,25 +470,25 @@ __global__ void __launch_bounds__(CW* WT * 32, CW* WT < 8 ? 1 : SPT < 8 ? 3 : 2)
   if (CL > 1) cg::this_cluster().sync();  // nobody leaves while mail may still come
 }
 
-template <typename T, int VEC, bool GATE, int CW, int WT, int SPT, bool BULK>
-__global__ void __launch_bounds__(CW* WT * 32, CW* WT < 8 ? 1 : SPT < 8 ? 3 : 2)
+template <typename T, int VEC, bool GATE, int W, int WT, int SPT, bool BULK>
+__global__ void __launch_bounds__(W* WT, W* WT < 256 ? 1 : SPT < 8 ? 3 : 2)
     glr_bwd_kernel(const GlrArgs a, int CL, const __grid_constant__ GlrTiles tiles) {
   using V = GlrV<VEC>;
   constexpr int M = GATE ? 4 : 3, SLAB = WT * SPT;
   extern __shared__ __align__(128) uint8_t slots[];
-  __shared__ __align__(16) GlrShared<VEC, CW, WT> sh;  // of the adjoint's maps
-  __shared__ __align__(16) GlrMap<VEC> s_states[2][WT][CW * 32];
+  __shared__ __align__(16) GlrShared<VEC, W, WT> sh;  // of the adjoint's maps
+  __shared__ __align__(16) GlrMap<VEC> s_states[2][WT][W];
   glr_setup(CL, sh);
   const int cluster = blockIdx.x / CL, rank = blockIdx.x % CL, clusters = gridDim.x / CL;
-  const GlrSpan sp(a, CW * 32 * VEC, SLAB * CL);
-  GlrFeed<T, VEC, M, WT, SPT, BULK> in(slots, sh.full, &sh.gone, cluster);
+  const GlrSpan sp(a, W * VEC, SLAB * CL);
+  GlrFeed<T, VEC, M, W, WT, SPT, BULK> in(slots, sh.full, &sh.gone, cluster);
   if constexpr (BULK)
     if (threadIdx.x == 0)
       for (int k = 0; k < in.SLOTS; ++k) in.ask(a, sp, tiles, CL, rank, clusters, true);
   const V alpha = V::all(a.alpha), minus = V::all(-1.f);
   int mail = 0;
   for (int unit = cluster; unit < sp.units; unit += clusters) {
-    const GlrPlace<VEC, CW, WT> at(a, sp, unit);
+    const GlrPlace<VEC, W, WT> at(a, sp, unit);
     const size_t step_d = (size_t)a.B * a.lddz, off_d = (size_t)at.b * a.lddz + at.j;
     T* dzf = (T*)a.dZf + off_d;
     T* dzg = (T*)a.dZg + off_d;
@@ -508,7 +508,7 @@ __global__ void __launch_bounds__(CW* WT * 32, CW* WT < 8 ? 1 : SPT < 8 ? 3 : 2)
     V first;  // what arrives behind the unit's last step
 #pragma unroll
     for (int v = 0; v < VEC; ++v) first.v[v] = a.h0 && v < at.valid ? a.h0[at.of(a, sp, v)] : 0.f;
-    const bool inside = (unit % sp.groups + 1) * (CW * 32 * VEC) <= sp.n;
+    const bool inside = (unit % sp.groups + 1) * (W * VEC) <= sp.n;
     V q = first;
     auto slab = [&](auto full, int it) {
       constexpr bool FULL = decltype(full)::value;
@@ -639,13 +639,12 @@ ard_status glr_launch(ard_ctx* ctx, K kern, const GlrArgs& a, const GlrTiles& ti
   return ARD_OK;
 }
 
-// CTAs of a cluster that share a sequence's slabs (64 steps each), where the units alone leave more than half of the SMs idle: as many as let all units
-// run at once.  How many clusters of a size the device holds goes by how its SMs are grouped, and is asked once.
+// CTAs of a cluster that share a sequence's slabs, where the units alone leave more than half of the SMs idle: as many as let all units run at once.  How many clusters of a size the device holds goes by how its SMs are grouped, and is asked once.
 inline int glr_cluster(ard_ctx* ctx, long long units, long long slabs) {
-  if (2 * units > ctx->sm_count || slabs < 2) return 1;
+  if (slabs < 2) return 1;
   if (ctx->glr_room[2] == 0) {
-    auto kern = glr_fwd_kernel<__nv_bfloat16, 2, true, 1, 8, 8, true>;
-    constexpr int smem = glr_ring<GlrFeed<__nv_bfloat16, 2, 3, 8, 8, true>>();
+    auto kern = glr_fwd_kernel<__nv_bfloat16, 2, true, 16, 16, 8, true>;
+    constexpr int smem = glr_ring<GlrFeed<__nv_bfloat16, 2, 3, 16, 16, 8, true>>();
     cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
     cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
     for (int cl = 2; cl <= GLR_CLUSTER; ++cl) ctx->glr_room[cl] = ard_cluster_room(ctx, kern, cl, 256, smem) / cl;
@@ -659,41 +658,49 @@ inline int glr_cluster(ard_ctx* ctx, long long units, long long slabs) {
 
 // Descriptors [T][B][H] of the M operands; false: not on a 16-byte grid.
 template <typename T, int VEC>
-bool glr_tiles(ard_ctx* ctx, const GlrArgs& a, std::initializer_list<std::pair<const void*, int>> operands, int steps, GlrTiles* out) {
+bool glr_tiles(ard_ctx* ctx, const GlrArgs& a, std::initializer_list<std::pair<const void*, int>> operands, int channels, int steps, GlrTiles* out) {
   int m = 0;
   for (const auto& op : operands) {
     if ((reinterpret_cast<uintptr_t>(op.first) & 15u) || (op.second * sizeof(T)) % 16) return false;
-    if (!ard_encode_steps(ctx, &out->map[m++], sizeof(T) == 4, op.first, a.H, a.B, a.T, op.second, 32 * VEC, steps)) return false;
+    if (!ard_encode_steps(ctx, &out->map[m++], sizeof(T) == 4, op.first, a.H, a.B, a.T, op.second, channels, steps)) return false;
   }
   return true;
 }
 
 // Steps of a thread.  As few as a short sequence's slab of 8 warps needs (three CTAs an SM: 35 x 64 x 1024 11.3 -> 8.7 us); 8, two CTAs an SM, otherwise.
 // (16 in clusters, one CTA an SM: what a round costs besides its steps is paid half as often, but nothing runs beside it: 16384 x 1 x 1024 50.9 / 81.2
-// us forward / backward, here 49 / 76.7; 4096 steps 17.4 / 25.8, here 15.7 / 23.)  run(SPT, CTAs an SM, cluster).
+// us forward / backward.)  Units as wide as a warp, or as half of one, twice as many steps long, where clusters of all that may share a sequence would leave
+// SMs idle: the same size 49.5 / 76.5 us in whole warps, 40.3 / 69.2 in halves; 16384 x 1 x 2048, which fills them either way, 71 / 117 and 71 / 128.
+// run(SPT, W, CTAs an SM, cluster).
 template <typename Run>
-ard_status glr_steps(ard_ctx* ctx, const GlrArgs& a, int channels, Run run) {
-  if (a.T <= 16) return run(std::integral_constant<int, 2>{}, 3, 1);
-  if (a.T <= 40) return run(std::integral_constant<int, 5>{}, 3, 1);
-  return run(std::integral_constant<int, 8>{}, 2, glr_cluster(ctx, glr_units(a, channels), ((long long)a.T + 63) / 64));
+ard_status glr_steps(ard_ctx* ctx, const GlrArgs& a, int vec, Run run) {
+  constexpr std::integral_constant<int, 32> warp{};
+  constexpr std::integral_constant<int, 16> half{};
+  constexpr std::integral_constant<int, 8> eight{};
+  if (a.T <= 16) return run(std::integral_constant<int, 2>{}, warp, 3, 1);
+  if (a.T <= 40) return run(std::integral_constant<int, 5>{}, warp, 3, 1);
+  const long long units = glr_units(a, 32 * vec);
+  if (2 * units > ctx->sm_count) return run(eight, warp, 2, 1);
+  if (units * GLR_CLUSTER > 2 * ctx->sm_count) return run(eight, warp, 2, glr_cluster(ctx, units, ((long long)a.T + 63) / 64));
+  return run(eight, half, 2, glr_cluster(ctx, glr_units(a, 16 * vec), ((long long)a.T + 127) / 128));
 }
 
 template <typename T, int VEC, bool GATE>
 struct GlrFwd {
   static ard_status run(ard_ctx* ctx, const GlrArgs& a, cudaStream_t s) {
     GlrTiles tiles;
-    if (a.T <= 1) return glr_launch(ctx, glr_fwd_kernel<T, VEC, GATE, 4, 1, 1, false>, a, tiles, 4 * 32 * VEC, 1, 128, 0, 8, s);
-    return glr_steps(ctx, a, 32 * VEC, [&](auto steps, int per_sm, int CL) {
-      constexpr int SPT = decltype(steps)::value;
+    if (a.T <= 1) return glr_launch(ctx, glr_fwd_kernel<T, VEC, GATE, 128, 1, 1, false>, a, tiles, 128 * VEC, 1, 128, 0, 8, s);
+    return glr_steps(ctx, a, VEC, [&](auto steps, auto width, int per_sm, int CL) {
+      constexpr int SPT = decltype(steps)::value, W = decltype(width)::value, WT = 256 / W;
       if constexpr (VEC * sizeof(T) == 4) {
         bool ok;
-        if constexpr (GATE) ok = glr_tiles<T, VEC>(ctx, a, {{a.Zf, a.ldz}, {a.Zg, a.ldz}, {a.Zo, a.ldz}}, 8 * SPT, &tiles);
-        else ok = glr_tiles<T, VEC>(ctx, a, {{a.Zf, a.ldz}, {a.Zg, a.ldz}}, 8 * SPT, &tiles);
+        if constexpr (GATE) ok = glr_tiles<T, VEC>(ctx, a, {{a.Zf, a.ldz}, {a.Zg, a.ldz}, {a.Zo, a.ldz}}, W * VEC, WT * SPT, &tiles);
+        else ok = glr_tiles<T, VEC>(ctx, a, {{a.Zf, a.ldz}, {a.Zg, a.ldz}}, W * VEC, WT * SPT, &tiles);
         if (ok)
-          return glr_launch(ctx, glr_fwd_kernel<T, VEC, GATE, 1, 8, SPT, true>, a, tiles, 32 * VEC, CL, 256,
-                            glr_ring<GlrFeed<T, VEC, GATE ? 3 : 2, 8, SPT, true>>(), per_sm, s);
+          return glr_launch(ctx, glr_fwd_kernel<T, VEC, GATE, W, WT, SPT, true>, a, tiles, W * VEC, CL, 256,
+                            glr_ring<GlrFeed<T, VEC, GATE ? 3 : 2, W, WT, SPT, true>>(), per_sm, s);
       }
-      return glr_launch(ctx, glr_fwd_kernel<T, VEC, GATE, 1, 8, SPT, false>, a, tiles, 32 * VEC, CL, 256, 0, per_sm, s);
+      return glr_launch(ctx, glr_fwd_kernel<T, VEC, GATE, W, WT, SPT, false>, a, tiles, W * VEC, CL, 256, 0, per_sm, s);
     });
   }
 };
@@ -701,18 +708,18 @@ template <typename T, int VEC, bool GATE>
 struct GlrBwd {
   static ard_status run(ard_ctx* ctx, const GlrArgs& a, cudaStream_t s) {
     GlrTiles tiles;
-    if (a.T <= 1) return glr_launch(ctx, glr_bwd_kernel<T, VEC, GATE, 4, 1, 1, false>, a, tiles, 4 * 32 * VEC, 1, 128, 0, 8, s);
-    return glr_steps(ctx, a, 32 * VEC, [&](auto steps, int per_sm, int CL) {
-      constexpr int SPT = decltype(steps)::value;
+    if (a.T <= 1) return glr_launch(ctx, glr_bwd_kernel<T, VEC, GATE, 128, 1, 1, false>, a, tiles, 128 * VEC, 1, 128, 0, 8, s);
+    return glr_steps(ctx, a, VEC, [&](auto steps, auto width, int per_sm, int CL) {
+      constexpr int SPT = decltype(steps)::value, W = decltype(width)::value, WT = 256 / W;
       if constexpr (VEC * sizeof(T) == 4) {
         bool ok;
-        if constexpr (GATE) ok = glr_tiles<T, VEC>(ctx, a, {{a.Zf, a.ldz}, {a.Zg, a.ldz}, {a.dY, a.ldy}, {a.Zo, a.ldz}}, 8 * SPT, &tiles);
-        else ok = glr_tiles<T, VEC>(ctx, a, {{a.Zf, a.ldz}, {a.Zg, a.ldz}, {a.dY, a.ldy}}, 8 * SPT, &tiles);
+        if constexpr (GATE) ok = glr_tiles<T, VEC>(ctx, a, {{a.Zf, a.ldz}, {a.Zg, a.ldz}, {a.dY, a.ldy}, {a.Zo, a.ldz}}, W * VEC, WT * SPT, &tiles);
+        else ok = glr_tiles<T, VEC>(ctx, a, {{a.Zf, a.ldz}, {a.Zg, a.ldz}, {a.dY, a.ldy}}, W * VEC, WT * SPT, &tiles);
         if (ok)
-          return glr_launch(ctx, glr_bwd_kernel<T, VEC, GATE, 1, 8, SPT, true>, a, tiles, 32 * VEC, CL, 256,
-                            glr_ring<GlrFeed<T, VEC, GATE ? 4 : 3, 8, SPT, true>>(), per_sm, s);
+          return glr_launch(ctx, glr_bwd_kernel<T, VEC, GATE, W, WT, SPT, true>, a, tiles, W * VEC, CL, 256,
+                            glr_ring<GlrFeed<T, VEC, GATE ? 4 : 3, W, WT, SPT, true>>(), per_sm, s);
       }
-      return glr_launch(ctx, glr_bwd_kernel<T, VEC, GATE, 1, 8, SPT, false>, a, tiles, 32 * VEC, CL, 256, 0, per_sm, s);
+      return glr_launch(ctx, glr_bwd_kernel<T, VEC, GATE, W, WT, SPT, false>, a, tiles, W * VEC, CL, 256, 0, per_sm, s);
     });
   }
 };

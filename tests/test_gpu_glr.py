@@ -281,3 +281,20 @@ def test_offsets_beyond_32_bits():
     ard.ard_glr_forward(h, None, BF16, T, 1, H, 1.0, big, big[..., H:], None, ld, None, None, y, H, None, None)
     ard.ard_glr_forward(h, None, BF16, T, 1, H, 1.0, z, z[..., H:], None, 2 * H, None, None, want, H, None, None)
     assert torch.equal(y, want)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("gate", [True, False])
+@pytest.mark.parametrize("T,B,H,lens,ld,off", [(300, 6, 320, None, 0, 0), (700, 6, 320, [700, 0, 64, 65, 321, 1], 0, 0), (129, 3, 450, [129, 128, 127], 6, 0),
+                                               (200, 6, 321, None, 0, 1), (65, 20, 64, None, 0, 0), (1100, 2, 640, None, 0, 0)])
+def test_clusters_of_whole_warps(dtype, gate, T, B, H, lens, ld, off):
+    """Between 19 and 74 units of a warp's channels: clusters share the sequences, and would fill the device without half warps."""
+    _both(Case(dtype, T, B, H, gate, lens=lens, ldz=ld, ldy=ld, lddz=ld, off=off, seed=T + H))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("T,B,H,dp,b,lens", [(300, 6, 640, 2, 2, None), (400, 2, 200, 3, 1, [400, 333]), (1000, 1, 64, 16, 5, None), (257, 3, 33, 33, 33, [0, 257, 129])])
+def test_clusters_over_kept_units(dtype, T, B, H, dp, b, lens):
+    pat = _ctx().pattern(ard.ARD_ROW, 16, H)
+    ard.ard_pattern_set(_ctx().h, pat, dp, b)
+    _both(Case(dtype, T, B, H, True, lens=lens, dp=dp, b=b, seed=T + dp), pat)
