@@ -27,7 +27,8 @@ struct AwEntry {
   float decay;
   unsigned number;           // 1 + place in the caller's table
   int g_is_bf16;
-  int flat;                  // no gaps between rows, all pointers on 16 bytes: read and written in pieces of 4 elements
+  int flat;                  // no gaps between rows, all pointers (but the scales') on 16 bytes: read and written in pieces of 4 elements
+  int scales16;              // the scales too: they come with the bulk copies
 };
 
 template <int CAP>
@@ -43,6 +44,7 @@ constexpr int AW_SMALL = 16, AW_LARGE = 216;
 
 struct AwArgs {
   float lr, beta1, beta2, one_minus_beta1, one_minus_beta2, eps;
+  float one;                // 1, as something that the compiler does not know
   float lift1, root_lift2;  // 1 / (1 - beta1^t) and the root of 1 / (1 - beta2^t), where the host knows t
   double ln_beta1, ln_beta2;
   uint32_t keys[20];  // the generator's, of its ten rounds: read where they are used, not carried in registers
@@ -139,13 +141,10 @@ __device__ __forceinline__ void aw_decode(uint32_t q, float scale, float (&v)[4]
 }
 
 // sqrt(x) and 1 / x as the instructions approximate them, to a unit or two in the last place: rounded to the last bit they take 8 to 20 instructions
-// each, with their special cases, and the kernel with states in 8 bits runs out of issue slots.  States in 32 bits keep roots of subnormal numbers (eps
-// may be zero).
-template <int BITS>
+// each, with their special cases, and the kernel with states in 8 bits runs out of issue slots.
 __device__ __forceinline__ float aw_root(float x) {
   float r;
-  if (BITS == 32) asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
-  else asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
   return r;
 }
 __device__ __forceinline__ float aw_inverse(float x) {
@@ -158,6 +157,16 @@ __device__ __forceinline__ float2 operator*(float2 a, float2 b) { return __fmul2
 __device__ __forceinline__ float2 operator+(float2 a, float2 b) { return __fadd2_rn(a, b); }
 __device__ __forceinline__ float2 aw_fma(float2 a, float2 b, float2 c) { return __ffma2_rn(a, b, c); }
 __device__ __forceinline__ float2 aw_both(float x) { return make_float2(x, x); }
+// Roots to the last bit: one of Heron's steps with its residual in one rounding (Markstein, IBM J. Res. Dev. 34, 1990), from the instruction's estimate of
+// 1 / sqrt(x).  No branches (they keep a thread's quads from running beside one another: 145 us for 36 M elements in place of 133): of x below 2^-126 the
+// result, below 2^-63, is not accurate, but is 0 only of 0; infinity gives NaN.
+__device__ __forceinline__ float2 aw_roots(float2 x) {
+  float2 y;
+  asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y.x) : "f"(fmaxf(x.x, 1.1754943508222875e-38f)));
+  asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y.y) : "f"(fmaxf(x.y, 1.1754943508222875e-38f)));
+  const float2 q = x * y;
+  return aw_fma(aw_fma(q * aw_both(-1.f), q, x), y * aw_both(0.5f), q);
+}
 
 // The 8-bit floats of a block of 128 values, four in each lane, and its scale (the same in all lanes).  ROOT: of values >= 0, from the words'
 // high halves; else from their low halves.
@@ -198,7 +207,7 @@ constexpr int AW_TILE = AW_QUADS * AW_THREADS * 4;
 
 // What is the same for all elements of a launch, and of a tensor.
 struct AwStep {
-  float gf, beta1, beta2, omb1, omb2, eps, root_lift2, step1, lr_decay;
+  float gf, beta1, beta2, omb1, omb2, eps, root_lift2, step1, lr_decay, one;
   unsigned long long t;
 };
 
@@ -234,28 +243,41 @@ __device__ __forceinline__ void aw_update(const AwEntry& e, const AwStep& a, con
   const bool f = WHOLE || flat;
   float (&m)[4] = st.m;
   float (&v)[4] = st.v;
-  float2 m2[2], r2[2];
+  float2 gk[2], m2[2], v2[2], r2[2];
   if constexpr (BITS == 8) {
     aw_decode(st.mq, st.ms, m);
     aw_decode(st.vq, st.vs, v);
   }
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
-    const float2 gk = make_float2(g[2 * h], g[2 * h + 1]) * aw_both(a.gf), p2 = make_float2(p[2 * h], p[2 * h + 1]);
-    float2 v2 = make_float2(v[2 * h], v[2 * h + 1]);
-    m2[h] = aw_fma(aw_both(a.beta1), make_float2(m[2 * h], m[2 * h + 1]), aw_both(a.omb1) * gk);
-    if (BITS == 8) v2 = v2 * v2;
-    v2 = aw_fma(aw_both(a.beta2), v2, (aw_both(a.omb2) * gk) * gk);
-    r2[h] = make_float2(aw_root<BITS>(v2.x), aw_root<BITS>(v2.y));
-    const float2 den = aw_fma(r2[h], aw_both(a.root_lift2), aw_both(a.eps));
+    gk[h] = make_float2(g[2 * h], g[2 * h + 1]) * aw_both(a.gf);
+    m2[h] = make_float2(m[2 * h], m[2 * h + 1]);
+    v2[h] = make_float2(v[2 * h], v[2 * h + 1]);
+    if constexpr (BITS == 8) {
+      // What decides how a state is rounded is computed operation by operation as the formulas stand, to the last bit: one unit off moves a value in a
+      // million to its other neighbour.  (Sums as products with one and sums: of a sum of two elements in one instruction the assembler makes one with the
+      // product before it, though both ask to be rounded.)
+      const float2 one = aw_both(a.one);
+      m2[h] = aw_fma(aw_both(a.beta1) * m2[h], one, aw_both(a.omb1) * gk[h]);
+      v2[h] = aw_fma(aw_both(a.beta2) * (v2[h] * v2[h]), one, (aw_both(a.omb2) * gk[h]) * gk[h]);
+      r2[h] = aw_roots(v2[h]);
+    } else {
+      m2[h] = aw_fma(aw_both(a.beta1), m2[h], aw_both(a.omb1) * gk[h]);
+      v2[h] = aw_fma(aw_both(a.beta2), v2[h], (aw_both(a.omb2) * gk[h]) * gk[h]);
+      r2[h] = make_float2(aw_root(v2[h].x), aw_root(v2[h].y));
+    }
+  }
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const float2 p2 = make_float2(p[2 * h], p[2 * h + 1]), den = aw_fma(r2[h], aw_both(a.root_lift2), aw_both(a.eps));
     const float2 move = (aw_both(a.step1) * m2[h]) * make_float2(aw_inverse(den.x), aw_inverse(den.y));
     const float2 to = aw_fma(aw_both(-1.f), aw_fma(aw_both(a.lr_decay), p2, move), p2);
     p[2 * h] = to.x;
     p[2 * h + 1] = to.y;
     m[2 * h] = m2[h].x;
     m[2 * h + 1] = m2[h].y;
-    v[2 * h] = v2.x;
-    v[2 * h + 1] = v2.y;
+    v[2 * h] = v2[h].x;
+    v[2 * h + 1] = v2[h].y;
   }
   aw_store4(e.p, i, n, e.cols, e.ldp, f, p);
   if (e.w) aw_store4(e.w, i, n, e.cols, e.ldw, f, p);
@@ -309,6 +331,7 @@ __device__ __forceinline__ bool aw_begin(const AwArgs& a, AwStep& st, float& lr,
   st.omb1 = a.one_minus_beta1;
   st.omb2 = a.one_minus_beta2;
   st.eps = a.eps;
+  st.one = a.one;
   return true;
 }
 // A tile of QUADS x THREADS quads that ends inside, or whose elements do not lie one after the other on 16 bytes.
@@ -355,7 +378,8 @@ __global__ void __launch_bounds__(AW_THREADS, 4) adamw_kernel(const __grid_const
 
 // States in 8 bits: 14 to 20 bytes are read for an element whose arithmetic takes some 80 instructions, so registers cannot hold what has to be in flight
 // (36 bytes for a thread's quad: 2.2 TB/s).  Every warp has its own tiles, which come through a ring in shared memory by bulk copies ahead of it: no
-// barrier among warps, four quads of a lane to a search of the table.  (Tiles of a CTA, two quads and four: 148 and 124 us for 36 M elements.)
+// barrier among warps, four quads of a lane to a search of the table.  (Tiles of a CTA, two quads and four: 148 and 124 us for 36 M elements, with states rounded
+// from values a unit or so off; so, to the last bit, 133 us, 143 where the scales come by lanes.)
 constexpr int AW8_QUADS = 4, AW8_TILE = AW8_QUADS * 128, AW8_SLOTS = 2, AW8_PER_SM = 2, AW8_WARPS = AW_THREADS / 32;
 constexpr int AW8_UNROLL = 4;
 static_assert(AW8_QUADS % 4 == 0, "bulk copies of the scales: multiples of 16 bytes");
@@ -399,7 +423,7 @@ __global__ void __launch_bounds__(AW_THREADS, AW8_PER_SM) adamw8_kernel(const __
       return;
     }
     const uint32_t gbytes = e.g_is_bf16 ? AW8_TILE * 2 : AW8_TILE * 4;
-    mbar_arrive_expect_tx(bar, AW8_TILE * 6 + gbytes + AW8_QUADS * 8);
+    mbar_arrive_expect_tx(bar, AW8_TILE * 6 + gbytes + (e.scales16 ? AW8_QUADS * 8 : 0));
     auto copy = [&](uint32_t at, const void* src, uint32_t bytes) {
       asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst + at), "l"(src),
                    "r"(bytes), "r"(bar)
@@ -409,8 +433,10 @@ __global__ void __launch_bounds__(AW_THREADS, AW8_PER_SM) adamw8_kernel(const __
     copy(AW8_G, (const uint8_t*)e.g + base * (e.g_is_bf16 ? 2 : 4), gbytes);
     copy(AW8_M, (const uint8_t*)e.m + base, AW8_TILE);
     copy(AW8_V, (const uint8_t*)e.v + base, AW8_TILE);
-    copy(AW8_MS, e.m_scale + base / 128, AW8_QUADS * 4);
-    copy(AW8_VS, e.v_scale + base / 128, AW8_QUADS * 4);
+    if (e.scales16) {
+      copy(AW8_MS, e.m_scale + base / 128, AW8_QUADS * 4);
+      copy(AW8_VS, e.v_scale + base / 128, AW8_QUADS * 4);
+    }
   };
   if (lane == 0)
     for (int k = 0; k < AW8_SLOTS; ++k) ask();
@@ -418,12 +444,17 @@ __global__ void __launch_bounds__(AW_THREADS, AW8_PER_SM) adamw8_kernel(const __
     const AwEntry& e = table.e[aw_find(table, tile)];
     const long long base = (long long)(tile - e.tile0) * AW8_TILE;
     st.lr_decay = lr * e.decay;
+    // scales off the 16-byte grid (those of a tensor among others in one buffer): a lane each, behind the wait into the copies' place
+    const bool by_lanes = !e.scales16 && whole(e, base) && lane < 2 * AW8_QUADS;
+    const float sc = by_lanes ? (lane < AW8_QUADS ? e.m_scale : e.v_scale - AW8_QUADS)[base / 128 + lane] : 0.f;
     if (!gone && !mbar_wait(smem_u32(&full[slot]), (uint32_t)phase, &s_gone, status)) gone = true;
     gone = __any_sync(0xFFFFFFFFu, gone);
     if (!gone) {
       ++taken;
       if (whole(e, base)) {
-        const uint8_t* from = mine + slot * AW8_SLOT;
+        uint8_t* from = mine + slot * AW8_SLOT;
+        if (by_lanes) reinterpret_cast<float*>(from + AW8_MS)[lane] = sc;  // (v's lie behind m's)
+        __syncwarp();
 #pragma unroll AW8_UNROLL
         for (int u = 0; u < AW8_QUADS; ++u) {
           const int at = (u * 32 + lane) * 4;
@@ -587,8 +618,8 @@ AwEntry aw_entry(const ard_adamw_tensor& t, int number, bool grads_only, unsigne
   e.g_is_bf16 = t.g_dtype == ARD_BF16;
   e.flat = e.ldg == t.cols && on16(t.g);
   if (!grads_only)
-    e.flat = e.flat && e.ldp == t.cols && on16(t.p) && on16(t.m) && on16(t.v) && (!t.w || (e.ldw == t.cols && on16(t.w))) &&
-             on16(t.m_scale) && on16(t.v_scale);
+    e.flat = e.flat && e.ldp == t.cols && on16(t.p) && on16(t.m) && on16(t.v) && (!t.w || (e.ldw == t.cols && on16(t.w)));
+  e.scales16 = on16(t.m_scale) && on16(t.v_scale);
   return e;
 }
 
@@ -633,6 +664,7 @@ ard_status launch_adamw(ard_ctx* ctx, const ard_adamw_tensor* tensors, int n_ten
   a.lr = (float)lr;
   a.beta1 = (float)beta1;
   a.beta2 = (float)beta2;
+  a.one = 1.f;
   a.one_minus_beta1 = (float)(1.0 - beta1);
   a.one_minus_beta2 = (float)(1.0 - beta2);
   a.eps = (float)eps;

@@ -309,3 +309,56 @@ def test_a_captured_step_follows_counter_and_gradients(bits):
         made.append([x for r in q for x in (r.p, r.m, r.v, r.w)] + [out])
     for a, b in zip(*made):
         assert torch.equal(torch.nan_to_num(a.float()), torch.nan_to_num(b.float()))
+
+
+def _eight(n, off, seed, g):
+    """Tensors for one step with states in 8 bits from zeros, the scales `off` floats into their memory."""
+    blocks = -(-n // 128)
+    new = lambda k, dt=torch.float32: torch.zeros(k, dtype=dt, device="cuda")  # noqa: E731
+    return dict(rows=1, cols=n, p=new(n), g=g, w=None, m=new(n, torch.uint8), v=new(n, torch.uint8), m_scale=new(blocks + off)[off:],
+                v_scale=new(blocks + off)[off:], weight_decay=0.0)
+
+
+def _steps(t, k=2):
+    table = ard.adamw_tensors([t])
+    for step in range(1, k + 1):
+        ard.ard_adamw_step(_h(), table, 1, LR, B1, B2, EPS, 8, 9, step)
+    torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("off", [1, 2, 3])
+@pytest.mark.parametrize("n", [512 * 40, 512 * 7 + 130, 128 * 3, 77])
+def test_scales_on_any_four_bytes(n, off):
+    """A tensor's scales among others' in one buffer: the same bits as on a 16-byte grid."""
+    g = torch.from_numpy(np.random.default_rng(n).normal(size=n).astype(np.float32)).cuda()
+    a, b = _eight(n, 0, 1, g), _eight(n, off, 1, g)
+    _steps(a)
+    _steps(b)
+    for k in ("p", "m", "v", "m_scale", "v_scale"):
+        assert torch.equal(a[k], b[k]), k
+
+
+def test_states_in_eight_bits_are_rounded_from_what_the_formulas_give_in_fp32():
+    """The scale of a block with one value is that value times 1 / 448.  m: every operation rounded, bit for bit.  The root: to the last bit but for values
+    within 2^-46 of the middle between two numbers, of which there is one in millions."""
+    n, f = 128 * 20000, np.float32
+    rng = np.random.default_rng(4)
+    values = (np.exp(rng.uniform(-25, 10, size=20000)) * rng.choice([-1, 1], size=20000)).astype(f)
+    g = np.zeros((20000, 128), f)
+    g[:, 5] = values
+    t = _eight(n, 0, 1, torch.from_numpy(g.reshape(-1)).cuda())
+    _steps(t, 1)
+    inverse = f(1) / f(448)
+    m = (f(1.0 - B1) * values).astype(f)
+    assert np.array_equal(t["m_scale"].cpu().numpy(), (np.abs(m) * inverse).astype(f))
+    v = ((f(1.0 - B2) * values).astype(f) * values).astype(f)
+    want, got = (np.sqrt(v) * inverse).astype(f), t["v_scale"].cpu().numpy()
+    same = got == want
+    assert same.mean() > 0.999 and (np.abs(got - want) <= np.spacing(want)).all()
+    # a second step: beta1 m + (1 - beta1) g of three roundings, m being its code times its scale
+    code = t["m"].view(torch.float8_e4m3fn).float().cpu().numpy().reshape(-1, 128)[:, 5]
+    before = (code * t["m_scale"].cpu().numpy()).astype(f)
+    ard.ard_adamw_step(_h(), ard.adamw_tensors([t]), 1, LR, B1, B2, EPS, 8, 9, 2)
+    torch.cuda.synchronize()
+    m = ((f(B1) * before).astype(f) + (f(1.0 - B1) * values).astype(f)).astype(f)
+    assert np.array_equal(t["m_scale"].cpu().numpy(), (np.abs(m) * inverse).astype(f))
