@@ -730,7 +730,7 @@ ard_status ard_glr_forward(ard_ctx* ctx, const ard_pattern* pat, ard_dtype dtype
  * and dh0 = q in the end.  The states c are computed again from S, in fp32; Y is not needed.  dZf, dZg, dZo (rows of
  * lddz) have the layout of Z; all three are written, rows behind a sequence's end as zero (a product that adds over all rows
  * takes them as they are); dZo goes with Zo.  dhT, dh0 fp32 [B][H] full width, either may be NULL (zero; not wanted);
- * entries of dropped units are left; dh0 may be dhT.  Gradients must not overlap an input.  Asynchronous. */
+ * entries of dropped units are left; dh0 may be dhT.  Gradients must not overlap an input or one another.  Asynchronous. */
 ard_status ard_glr_backward(ard_ctx* ctx, const ard_pattern* pat, ard_dtype dtype, int T, int B, int H, float alpha,
                             const void* Zf, const void* Zg, const void* Zo, int ldz, const int32_t* lens, const float* S,
                             const void* dY, int lddy, const float* dhT, void* dZf, void* dZg, void* dZo, int lddz,
@@ -771,7 +771,7 @@ typedef struct ard_adamw_tensor {
  * before rounding.  States begin as zeros (bytes and scales).
  * Tensors must not overlap one another.  Any alignment (16-byte aligned tensors without gaps between rows are read and
  * written in 16-byte pieces).  Errors: ARD_ERR_INVALID_ARG (NULL, negative size, dtype, state_bits, beta outside [0, 1), lr, eps or
- * weight_decay negative or not finite), ARD_ERR_SHAPE (leading dimension below cols, more than 2^34 elements).
+ * weight_decay negative or not finite, eps above 0 and below 2^-126), ARD_ERR_SHAPE (leading dimension below cols, more than 2^34 elements).
  * Nothing is launched unless all tensors are valid.  Asynchronous. */
 ard_status ard_adamw_step(ard_ctx* ctx, const ard_adamw_tensor* tensors, int n_tensors, double lr, double beta1, double beta2,
                           double eps, int state_bits, uint64_t seed, uint64_t step, const uint64_t* step_counter,

@@ -1719,7 +1719,7 @@ ard_status ard_layer_norm_fwd(ard_ctx* ctx, const ard_pattern* pat, ard_dtype dt
                               void* cuda_stream) {
   const ard_status st = layer_norm_check(ctx, pat, dtype, rows, N);
   if (st != ARD_OK) return st;
-  if (!X || !Y || X == Y || !(eps >= 0.f) || !(eps < INFINITY)) return ARD_ERR_INVALID_ARG;
+  if (!X || !Y || X == Y || (mean && mean == rstd) || !(eps >= 0.f) || !(eps < INFINITY)) return ARD_ERR_INVALID_ARG;
   if (ldx < N || ldy < N) return ARD_ERR_SHAPE;
   DeviceGuard guard(ctx->device);
   return launch_layer_norm_fwd(ctx, pat ? pat->d_hdr : nullptr, dtype, rows, N, eps, X, ldx, weight, bias, Y, ldy, mean, rstd,
@@ -1731,7 +1731,7 @@ ard_status ard_layer_norm_bwd(ard_ctx* ctx, const ard_pattern* pat, ard_dtype dt
                               float* dweight, float* dbias, int zero_fill_dropped, void* cuda_stream) {
   const ard_status st = layer_norm_check(ctx, pat, dtype, rows, N);
   if (st != ARD_OK) return st;
-  if (!dY || !X || !mean || !rstd || dX == dY || dX == X) return ARD_ERR_INVALID_ARG;
+  if (!dY || !X || !mean || !rstd || dX == dY || dX == X || (dweight && dweight == dbias)) return ARD_ERR_INVALID_ARG;
   if (ldx < N || lddy < N || (dX && lddx < N)) return ARD_ERR_SHAPE;
   DeviceGuard guard(ctx->device);
   return launch_layer_norm_bwd(ctx, pat ? pat->d_hdr : nullptr, dtype, rows, N, dY, lddy, X, ldx, weight, mean, rstd, dX, lddx, dweight,
@@ -1766,6 +1766,7 @@ ard_status ard_glr_backward(ard_ctx* ctx, const ard_pattern* pat, ard_dtype dtyp
   if (st != ARD_OK) return st;
   if (!S || !dY || !dZf || !dZg || (Zo != nullptr) != (dZo != nullptr)) return ARD_ERR_INVALID_ARG;
   if (lddy < H || lddz < H) return ARD_ERR_SHAPE;
+  if (dZf == dZg || dZf == dZo || dZg == dZo) return ARD_ERR_INVALID_ARG;
   for (const void* out : {dZf, dZg, dZo})
     for (const void* in : {Zf, Zg, Zo, dY})
       if (out && out == in) return ARD_ERR_INVALID_ARG;
@@ -1798,6 +1799,7 @@ ard_status ard_adamw_step(ard_ctx* ctx, const ard_adamw_tensor* tensors, int n_t
                           const float* grad_factor, void* cuda_stream) {
   if (!ctx || (state_bits != 8 && state_bits != 32)) return ARD_ERR_INVALID_ARG;
   if (!(lr >= 0.0) || !(lr < INFINITY) || !(eps >= 0.0) || !(eps < INFINITY)) return ARD_ERR_INVALID_ARG;
+  if (eps > 0.0 && eps < 1.1754943508222875e-38) return ARD_ERR_INVALID_ARG;  // 2^-126: what the kernels' quotients take for zero
   if (!(beta1 >= 0.0) || !(beta1 < 1.0) || !(beta2 >= 0.0) || !(beta2 < 1.0)) return ARD_ERR_INVALID_ARG;
   const ard_status st = adamw_check(tensors, n_tensors, state_bits);
   if (st != ARD_OK) return st;

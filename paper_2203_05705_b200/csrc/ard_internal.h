@@ -117,7 +117,7 @@ struct ard_ctx {
   void* d_lstm_hc;           // compact copies of h_{t-1} and h_t of the whole-sequence forward kernel, lstm_hc_bytes()
   int lstm_compact_h;        // ... which contracts over the kept units of h alone under a pattern
   int lstm_refuse;           // launches answered as though the device could not hold them: 1 clusters, 2 cooperative
-  int glr_room[17];          // clusters of so many CTAs, one an SM, that the device holds at once (0: not asked yet)
+  int glr_room[17];          // clusters of so many CTAs that the device holds at once (0: not asked yet)
   int use_pdl;        // launch kernels with programmatic stream serialization (see ard_launch)
   int pdl_in_capture; // ... also while the stream is being captured into a CUDA graph
   int stream_k;       // tensor-core row kernels: share the last, partial wave of tiles along the contraction

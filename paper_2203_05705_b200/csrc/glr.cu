@@ -458,6 +458,7 @@ __global__ void __launch_bounds__(W* WT, W* WT < 256 ? 1 : SPT < 8 ? 3 : 2)
       if (inside && ((it + 1) * CL) * SLAB <= at.len) slab(std::true_type{}, it);
       else slab(std::false_type{}, it);
     }
+    if (CL > 1 && a.hT && a.hT == a.h0) cg::this_cluster().sync();  // the others have read what is about to be overwritten
     if (a.hT && rank == 0 && at.wt == WT - 1) {  // (the last warp's own words)
       const V behind = WT > 1 && sp.rounds > 0 ? sh.state[mail & 1][at.ch] : c;
 #pragma unroll
@@ -592,6 +593,7 @@ __global__ void __launch_bounds__(W* WT, W* WT < 256 ? 1 : SPT < 8 ? 3 : 2)
       if (inside && (sp.rounds - it) * CL * SLAB <= at.len) slab(std::true_type{}, it);
       else slab(std::false_type{}, it);
     }
+    if (CL > 1 && a.hT && a.hT == a.h0) cg::this_cluster().sync();
     if (a.hT && rank == 0 && at.wt == 0) {
       const V behind = WT > 1 && sp.rounds > 0 ? sh.state[mail & 1][at.ch] : q;
 #pragma unroll

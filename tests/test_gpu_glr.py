@@ -298,3 +298,49 @@ def test_clusters_over_kept_units(dtype, T, B, H, dp, b, lens):
     pat = _ctx().pattern(ard.ARD_ROW, 16, H)
     ard.ard_pattern_set(_ctx().h, pat, dp, b)
     _both(Case(dtype, T, B, H, True, lens=lens, dp=dp, b=b, seed=T + dp), pat)
+
+
+@pytest.mark.parametrize("dtype,T,B,H,lens", [(BF16, 500, 1, 256, None), (F32, 300, 2, 64, [300, 40]), (BF16, 300, 6, 320, None),
+                                              (BF16, 30, 3, 64, [30, 0, 7]), (F32, 1, 3, 64, None)])
+def test_states_in_place(dtype, T, B, H, lens):
+    """hT may be h0, dh0 may be dhT: the same bits as in places of their own."""
+    c = Case(dtype, T, B, H, True, lens=lens, seed=T)
+    _both(c)
+    want, grad, y = c.hT.clone(), c.dh0.clone(), c.y.clone()
+    c.hT, c.dh0 = c.h0, c.dhT
+    c.forward(_ctx().h)
+    c.backward(_ctx().h)
+    assert torch.equal(c.hT, want) and torch.equal(c.dh0, grad) and torch.equal(c.y, y)
+
+
+@pytest.mark.parametrize("T,B,H", [(300, 1, 128), (300, 6, 320), (20, 2, 64)])
+def test_the_first_call_of_a_context_may_be_captured(T, B, H):
+    c, fresh = Case(BF16, T, B, H, True, seed=1), Ctx(0)
+    try:
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            c.forward(fresh.h)
+            c.backward(fresh.h)
+        graph.replay()
+        torch.cuda.synchronize()
+        c.check()
+        del graph
+    finally:
+        fresh.close()
+
+
+def test_two_streams_at_once():
+    """Calls on two streams share nothing but the inputs."""
+    cases = [Case(BF16, 900, 1, 256, True, seed=k) for k in range(2)] + [Case(BF16, 40, 30, 256, True, seed=k) for k in range(2)]
+    streams = [torch.cuda.Stream() for _ in cases]
+    torch.cuda.synchronize()
+    for _ in range(3):
+        for c, s in zip(cases, streams):
+            with torch.cuda.stream(s):
+                c.forward(_ctx().h)
+                c.backward(_ctx().h)
+    torch.cuda.synchronize()
+    for c in cases:
+        c.check()

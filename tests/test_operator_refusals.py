@@ -106,3 +106,20 @@ def test_table_of_tensors():
     with pytest.raises(KeyError):
         ard.adamw_tensors([{"rows": 1, "p": 64}])
     assert len(ard.adamw_tensors([])) == 1   # a table that no call looks into
+
+
+@pytest.mark.parametrize("name,good,change", [
+    ("ard_layer_norm_fwd", LN_FWD, dict(mean=P[5], rstd=P[5])), ("ard_layer_norm_bwd", LN_BWD, dict(dweight=P[5], dbias=P[5])),
+    ("ard_glr_backward", GLR_BWD, dict(dZf=P[6])), ("ard_glr_backward", GLR_BWD, dict(dZo=P[5])), ("ard_glr_backward", GLR_BWD, dict(dZo=P[6])),
+    ("ard_glr_backward", GLR_BWD, dict(Zo=None, dZo=None, dZg=P[5]))])
+def test_outputs_in_the_same_place(name, good, change):
+    with pytest.raises(ard.ArdError) as e:
+        getattr(ard, name)(CTX, *{**good, **change}.values(), stream=0)
+    assert e.value.status == INVALID
+
+
+@pytest.mark.parametrize("eps", [1e-40, 1e-50, 5e-324])
+def test_an_eps_that_fp32_holds_only_as_a_subnormal(eps):
+    with pytest.raises(ard.ArdError) as e:
+        ard.ard_adamw_step(CTX, ard.adamw_tensors([TENSOR]), 1, *{**STEP, "eps": eps}.values(), stream=0)
+    assert e.value.status == INVALID
