@@ -67,16 +67,18 @@ class GlrLayer:
             ard.ard_layer_fwd(self.ctx, self.pat, self.in_pat, ard.ARD_BF16, rows, I, H, 1.0, self.Xn, I, self._rows(self.Wk, k), I,
                               self._columns(self.p_b, k), self._columns(self.Z, k), 3 * H, ard.ARD_OUT_COMPACT)
 
-    def _input(self, X, rows):
-        if tuple(X.shape) != (rows, self.I) or X.dtype != BF or X.device != self.Xn.device or not X.is_contiguous():
-            raise ValueError("the input has to be contiguous bf16 %s on %s, got %s %s on %s"
-                             % ((rows, self.I), self.Xn.device, X.dtype, tuple(X.shape), X.device))
+    def _check(self, name, t, shape, dtype):
+        if t is not None and (tuple(t.shape) != shape or t.dtype != dtype or t.device != self.Xn.device or not t.is_contiguous()):
+            raise ValueError("%s has to be contiguous %s %s on %s, got %s %s on %s"
+                             % (name, dtype, shape, self.Xn.device, t.dtype, tuple(t.shape), t.device))
 
     def forward(self, X, alpha, h0=None, lens=None):
         """X: bf16 [T*B][I] (with in_pat compact), kept until backward().  Returns Y [T*B][H], compact: the kept units' columns are valid.
         h0: fp32 [B][H] or None; lens: int32 [B] or None; the last states are in hT."""
         T, B, H = self.T, self.B, self.H
-        self._input(X, T * B)
+        self._check("X", X, (T * B, self.I), BF)
+        self._check("h0", h0, (B, H), F32)
+        self._check("lens", lens, (B,), torch.int32)
         self.X, self.lens = X, lens
         self.pack()
         self._gates(X, T * B)
@@ -90,8 +92,8 @@ class GlrLayer:
         ctx, pat, ip, T, B, I, H = self.ctx, self.pat, self.in_pat, self.T, self.B, self.I, self.H
         if self.X is None:
             raise RuntimeError("backward() before forward()")
-        if tuple(dY.shape) != (T * B, H) or dY.dtype != BF or dY.device != self.Xn.device or not dY.is_contiguous():
-            raise ValueError("dY has to be contiguous bf16 %s on %s, got %s %s on %s" % ((T * B, H), self.Xn.device, dY.dtype, tuple(dY.shape), dY.device))
+        self._check("dY", dY, (T * B, H), BF)
+        self._check("dhT", dhT, (B, H), F32)
         z, dz = ([self._columns(t, k) for k in range(3)] for t in (self.Z, self.dZ))
         ard.ard_glr_backward(ctx, pat, ard.ARD_BF16, T, B, H, alpha, z[0], z[1], z[2], 3 * H, self.lens, self.S, dY, H, dhT, dz[0], dz[1], dz[2],
                              3 * H, self.dh0)
@@ -111,7 +113,7 @@ class GlrLayer:
     def step(self, x, alpha=1.0):
         """One token of every sequence: x bf16 [B][I]; h is the state before and after.  Returns y [B][H], compact.  The weights are those that pack()
         or forward() packed last.  Uses the buffers of forward(): not between it and its backward()."""
-        self._input(x, self.B)
+        self._check("x", x, (self.B, self.I), BF)
         self.X = None
         self._gates(x, self.B)
         z = [self._columns(self.Z, k) for k in range(3)]

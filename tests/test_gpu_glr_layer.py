@@ -280,9 +280,15 @@ def test_refusals():
         for bad in (x[:3], x.float(), x.cpu(), z(16, 4, dtype=BF, device="cuda").t()):
             with pytest.raises(ValueError):
                 ly.forward(bad, 1.0)
+        for bad in (dict(h0=z(2, 24, dtype=BF, device="cuda")), dict(h0=z(2, 16, device="cuda")), dict(lens=z(2, dtype=torch.int64, device="cuda")),
+                    dict(lens=z(3, dtype=torch.int32, device="cuda")), dict(lens=z(2, dtype=torch.int32))):
+            with pytest.raises(ValueError):
+                ly.forward(x, 1.0, **bad)
         ly.forward(x, 1.0)
         with pytest.raises(ValueError):
             ly.backward(1.0, z(4, 24, device="cuda"))
+        with pytest.raises(ValueError):
+            ly.backward(1.0, z(4, 24, dtype=BF, device="cuda"), z(2, 24, dtype=BF, device="cuda"))
         ly.step(x[:2])
         with pytest.raises(RuntimeError):
             ly.backward(1.0, z(4, 24, dtype=BF, device="cuda"))
