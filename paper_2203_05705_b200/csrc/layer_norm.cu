@@ -12,6 +12,7 @@ namespace {
 struct LnShape {
   const int32_t* hdr;  // nullptr: all N columns
   int rows, N;
+  __host__ __device__ __forceinline__ int pitch() const { return (N + 3) & ~3; }  // of a row of partial sums: written in pieces of 16 bytes
 };
 struct LnCols {
   int n, dp, b0;  // compact columns, and the unit of column j: b0 + j * dp
@@ -46,7 +47,7 @@ __device__ __forceinline__ float ln_block_sum(float x, float* red) {
   return x;
 }
 
-// Rows of any alignment and any length: a CTA per row, element by element, the row read again for each sum.
+// Rows of any length, and few short ones: a CTA per row, element by element, the row read again for each sum.
 template <typename T>
 __global__ void __launch_bounds__(LN_ANY_THREADS) ln_fwd_any_kernel(LnShape sh, float eps, const T* X, int ldx, const float* weight,
                                                                    const float* bias, T* Y, int ldy, float* mean, float* rstd) {
@@ -138,7 +139,7 @@ __device__ __forceinline__ void ln_dw_any(const LnShape& sh, int n, const T* dY,
       float t = 0.f;
 #pragma unroll
       for (int k = 0; k < WARPS; ++k) t += red[warp][k][lane];
-      partial[((size_t)slice * 2 + warp) * sh.N + j] = t;
+      partial[((size_t)slice * 2 + warp) * sh.pitch() + j] = t;
     }
     __syncthreads();
   }
@@ -176,7 +177,7 @@ __global__ void __launch_bounds__(LN_SUM_WARPS * 32) ln_dw_sum_kernel(LnShape sh
 #pragma unroll
       for (int u = 0; u < 8; ++u) {
         const int k = k0 + u * LN_SUM_WARPS;
-        x[u] = k < slices ? partial[((size_t)k * 2 + which) * sh.N + j] : 0.f;
+        x[u] = k < slices ? partial[((size_t)k * 2 + which) * sh.pitch() + j] : 0.f;
       }
 #pragma unroll
       for (int u = 0; u < 8; ++u) t += x[u];
@@ -196,8 +197,11 @@ __global__ void __launch_bounds__(LN_SUM_WARPS * 32) ln_dw_sum_kernel(LnShape sh
   }
 }
 
-// ---- rows on a 16-byte grid -------------------------------------------------------------------------
-// TPR threads hold a row, V pieces of 16 bytes each: piece v of thread t is number v * TPR + t.
+// ---- rows through rings of bulk copies ---------------------------------------------------------------
+// TPR threads hold a row, V pieces of 16 bytes each: piece v of thread t is number v * TPR + t.  16384 x 2048 bf16, forward / backward: 27.6 / 46.7 us (a
+// copy of the same bytes 20.6 / 30.8); the loads keep up, half of the issue slots are taken, warps wait for one another at the sums' barriers.  ON16: rows on
+// a 16-byte grid; others are cut out of the copies in shared memory and stored in pieces as wide as their grid (on 8 bytes 39 / 72 us, on 2 bytes
+// 53 / 77; a CTA a row element by element 75 / 141).
 template <typename T>
 constexpr int LN_PER = 16 / (int)sizeof(T);  // elements of a piece
 
@@ -221,11 +225,25 @@ __device__ __forceinline__ void ln_unpack(const uint4& q, float2 (&v)[LN_PAIRS<T
   }
 }
 // The piece of column j from shared memory, elements from column n on as zero.  RAGGED: n may end inside a piece (asked once for all rows: the
-// questions, predicated rather than branched around, were two thirds of the instructions).
-template <typename T, bool RAGGED>
-__device__ __forceinline__ void ln_piece(const uint8_t* row, int j, int n, float2 (&v)[LN_PAIRS<T>]) {
+// questions, predicated rather than branched around, were two thirds of the instructions).  Without ON16 the row begins at byte `off` of its place: the
+// piece is cut out of the 32 bytes that it lies in.
+template <typename T, bool RAGGED, bool ON16>
+__device__ __forceinline__ void ln_piece(const uint8_t* row, int off, int j, int n, float2 (&v)[LN_PAIRS<T>]) {
   uint4 q = make_uint4(0u, 0u, 0u, 0u);
-  if (j < n) q = *reinterpret_cast<const uint4*>(row + (size_t)j * sizeof(T));
+  if (j < n) {
+    q = *reinterpret_cast<const uint4*>(row + (size_t)j * sizeof(T));
+    if constexpr (!ON16) {
+      const uint4 r = *reinterpret_cast<const uint4*>(row + (size_t)j * sizeof(T) + 16);
+      uint32_t w[8] = {q.x, q.y, q.z, q.w, r.x, r.y, r.z, r.w};
+#pragma unroll
+      for (int k = 0; k < 6; ++k) w[k] = off & 8 ? w[k + 2] : w[k];
+#pragma unroll
+      for (int k = 0; k < 5; ++k) w[k] = off & 4 ? w[k + 1] : w[k];
+      const int bits = sizeof(T) == 2 ? (off & 2) * 8 : 0;
+      q = make_uint4(__funnelshift_r(w[0], w[1], bits), __funnelshift_r(w[1], w[2], bits), __funnelshift_r(w[2], w[3], bits),
+                     __funnelshift_r(w[3], w[4], bits));
+    }
+  }
   ln_unpack<T>(q, v);
   if (RAGGED && j + LN_PER<T> > n)
 #pragma unroll
@@ -235,7 +253,7 @@ __device__ __forceinline__ void ln_piece(const uint8_t* row, int j, int n, float
     }
 }
 // The first `valid` values of a piece.
-template <typename T, bool RAGGED>
+template <typename T, bool RAGGED, bool ON16>
 __device__ __forceinline__ void ln_store(T* p, int valid, const float2 (&v)[LN_PAIRS<T>]) {
   if (!RAGGED || valid >= LN_PER<T>) {
     uint32_t w[4];
@@ -252,13 +270,28 @@ __device__ __forceinline__ void ln_store(T* p, int valid, const float2 (&v)[LN_P
         w[2 * k + 1] = __float_as_uint(v[k].y);
       }
     }
-    *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
-    return;
-  }
+    const uint32_t off = ON16 ? 0u : (uint32_t)reinterpret_cast<uintptr_t>(p);  // its low bits are those of all of a row's pieces
+    if ((off & 15u) == 0) {
+      *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+    } else if ((off & 7u) == 0) {
 #pragma unroll
-  for (int k = 0; k < LN_PAIRS<T>; ++k) {
-    if (2 * k < valid) ln_put(p, 2 * k, v[k].x);
-    if (2 * k + 1 < valid) ln_put(p, 2 * k + 1, v[k].y);
+      for (int k = 0; k < 2; ++k) reinterpret_cast<uint2*>(p)[k] = make_uint2(w[2 * k], w[2 * k + 1]);
+    } else if ((off & 3u) == 0) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) reinterpret_cast<uint32_t*>(p)[k] = w[k];
+    } else {  // 2-byte elements
+      uint16_t* h = reinterpret_cast<uint16_t*>(p);
+      h[0] = (uint16_t)w[0];
+#pragma unroll
+      for (int k = 0; k < 3; ++k) *reinterpret_cast<uint32_t*>(h + 1 + 2 * k) = __funnelshift_r(w[k], w[k + 1], 16);
+      h[7] = (uint16_t)(w[3] >> 16);
+    }
+  } else {
+#pragma unroll
+    for (int k = 0; k < LN_PAIRS<T>; ++k) {
+      if (2 * k < valid) ln_put(p, 2 * k, v[k].x);
+      if (2 * k + 1 < valid) ln_put(p, 2 * k + 1, v[k].y);
+    }
   }
 }
 // weight or bias at the units of a piece's columns; `other` where there is none.
@@ -316,16 +349,16 @@ __device__ __forceinline__ void ln_row_sums(float (&x)[M], float (*red)[M][32], 
 constexpr int LN_SLOTS = 8;
 struct LnRing {
   int slots;      // per group of threads
-  int row_bytes;  // of an operand, rounded up to 16 bytes
+  int row_bytes;  // of an operand, rounded up to 16 bytes; 16 more where rows begin anywhere
 };
-template <typename T, int TPR, int G, int R, int M>
+template <typename T, int TPR, int G, int R, int M, bool ON16>
 struct LnRows {
   const T* src[M];
   int ld[M];
   uint8_t* mine;
   uint64_t* full;
   LnRing ring;
-  int g0, stride, rounds, rows;
+  int g0, stride, rounds, rows, n;
   uint32_t bytes;
   int slot, phase;  // of the round that is being worked on
   bool gone;        // a copy did not come within two seconds: the rest is left, the status says so
@@ -337,6 +370,7 @@ struct LnRows {
     mine = slots + (size_t)g * ring.slots * (M * R * ring.row_bytes);
     full = bars[g];
     bytes = ((uint32_t)c.n * (uint32_t)sizeof(T) + 15u) & ~15u;
+    n = c.n;
     rows = sh.rows;
     stride = gridDim.x * G;
     rounds = ((rows + R - 1) / R + stride - 1) / stride;
@@ -347,19 +381,33 @@ struct LnRows {
   }
   __device__ __forceinline__ long long row(int it, int q) const { return (g0 + (long long)it * stride) * R + q; }
   __device__ __forceinline__ bool live(int it, int q) const { return row(it, q) < rows && !gone; }
+  // Where operand m of row q of round `it` begins within 16 bytes: copies start at the 16-byte boundary before it.
+  __device__ __forceinline__ int off(int it, int q, int m) const {
+    return ON16 ? 0 : (int)(((uint32_t)reinterpret_cast<uintptr_t>(src[m]) + (uint32_t)row(it, q) * (uint32_t)ld[m] * (uint32_t)sizeof(T)) & 15u);
+  }
+  __device__ __forceinline__ uint32_t size(int it, int q, int m) const {
+    return ON16 ? bytes : (uint32_t)(off(it, q, m) + n * (int)sizeof(T) + 15) & ~15u;
+  }
   __device__ __forceinline__ const uint8_t* at(int q, int m) const { return mine + (size_t)((slot * R + q) * M + m) * ring.row_bytes; }
   // By the first thread of the group, for round `it`; whoever read the slot before has passed a barrier since.
   __device__ __forceinline__ void ask(int it) const {
     if (it >= rounds || row(it, 0) >= rows || gone) return;
     const int to = it % ring.slots, here = (int)min((long long)R, rows - row(it, 0));
     const uint32_t bar = smem_u32(&full[to]), dst = smem_u32(mine + (size_t)to * (M * R * ring.row_bytes));
-    mbar_arrive_expect_tx(bar, (uint32_t)(M * here) * bytes);
+    uint32_t all = (uint32_t)(M * here) * bytes;
+    if constexpr (!ON16) {
+      all = 0;
+      for (int q = 0; q < here; ++q)
+#pragma unroll
+        for (int m = 0; m < M; ++m) all += size(it, q, m);
+    }
+    mbar_arrive_expect_tx(bar, all);
     for (int q = 0; q < here; ++q)
 #pragma unroll
       for (int m = 0; m < M; ++m)
         asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(
                          dst + (uint32_t)((q * M + m) * ring.row_bytes)),
-                     "l"(src[m] + (size_t)row(it, q) * ld[m]), "r"(bytes), "r"(bar)
+                     "l"(reinterpret_cast<const uint8_t*>(src[m] + (size_t)row(it, q) * ld[m]) - off(it, q, m)), "r"(size(it, q, m)), "r"(bar)
                      : "memory");
   }
   __device__ __forceinline__ void wait(int it, volatile int* s_gone, int* status) {
@@ -397,7 +445,7 @@ __device__ __forceinline__ void ln_setup(uint64_t (*full)[LN_SLOTS], int slots, 
 
 // Forward: two sums over a row's registers, the second about the mean (a sum of squares alone loses the variance of a row with a large
 // mean).  The barrier of the first one says that the round's slot has been read.
-template <typename T, int TPR, int V, int NT, int R>
+template <typename T, int TPR, int V, int NT, int R, bool ON16>
 __global__ void __launch_bounds__(NT, NT >= 512 ? 1 : 512 / NT) ln_fwd_kernel(LnShape sh, float eps, const T* X, int ldx, const float* weight, const float* bias,
                                                        T* Y, int ldy, float* mean, float* rstd, LnRing ring, int* status) {
   constexpr int PER = LN_PER<T>, PAIRS = LN_PAIRS<T>, G = NT / TPR;
@@ -411,7 +459,7 @@ __global__ void __launch_bounds__(NT, NT >= 512 ? 1 : 512 / NT) ln_fwd_kernel(Ln
   const int t = threadIdx.x % TPR;
   const LnCols c = ln_cols(sh);
   const float inv_n = 1.f / (float)c.n;
-  LnRows<T, TPR, G, R, 1> in(sh, c, ring, slots, full);
+  LnRows<T, TPR, G, R, 1, ON16> in(sh, c, ring, slots, full);
   in.src[0] = X;
   in.ld[0] = ldx;
   if (t == 0)
@@ -436,7 +484,7 @@ __global__ void __launch_bounds__(NT, NT >= 512 ? 1 : 512 / NT) ln_fwd_kernel(Ln
         const int n = in.live(it, q) ? c.n : 0;
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-          ln_piece<T, RAGGED>(in.at(q, 0), (v * TPR + t) * PER, n, x[q][v]);
+          ln_piece<T, RAGGED, ON16>(in.at(q, 0), in.off(it, q, 0), (v * TPR + t) * PER, n, x[q][v]);
 #pragma unroll
           for (int k = 0; k < PAIRS; ++k) sum = sum + x[q][v][k];
         }
@@ -482,7 +530,7 @@ __global__ void __launch_bounds__(NT, NT >= 512 ? 1 : 512 / NT) ln_fwd_kernel(Ln
             }
 #pragma unroll
             for (int k = 0; k < PAIRS; ++k) x[q][v][k] = ln_fma(x[q][v][k] * ln_both(rs), w[one * v][k], b[one * v][k]);
-            ln_store<T, RAGGED>(Y + (size_t)r * ldy + j, c.n - j, x[q][v]);
+            ln_store<T, RAGGED, ON16>(Y + (size_t)r * ldy + j, c.n - j, x[q][v]);
           }
         }
         if (t == 0) {
@@ -500,7 +548,7 @@ __global__ void __launch_bounds__(NT, NT >= 512 ? 1 : 512 / NT) ln_fwd_kernel(Ln
 // Backward: a thread keeps its columns' sums for the weight and the bias over all rows of the CTA and leaves them in `partial`
 // [CTA][2][N].  A row is read from its slot twice, for its sums and for dx, which costs less than the registers that would hold it; its slot is
 // asked for again one round later: the barrier of that round's sums says that nobody reads it any more.
-template <typename T, int TPR, int V, int NT, int R>
+template <typename T, int TPR, int V, int NT, int R, bool ON16>
 __global__ void __launch_bounds__(NT, NT >= 512 ? 1 : 512 / NT) ln_bwd_kernel(LnShape sh, const T* dY, int lddy, const T* X, int ldx, const float* weight,
                                                        const float* mean, const float* rstd, T* dX, int lddx, float* partial,
                                                        LnRing ring, int* status) {
@@ -515,7 +563,7 @@ __global__ void __launch_bounds__(NT, NT >= 512 ? 1 : 512 / NT) ln_bwd_kernel(Ln
   const int t = threadIdx.x % TPR, g = threadIdx.x / TPR;
   const LnCols c = ln_cols(sh);
   const float inv_n = 1.f / (float)c.n;
-  LnRows<T, TPR, G, R, 2> in(sh, c, ring, slots, full);
+  LnRows<T, TPR, G, R, 2, ON16> in(sh, c, ring, slots, full);
   in.src[0] = X;
   in.ld[0] = ldx;
   in.src[1] = dY;
@@ -557,8 +605,8 @@ __global__ void __launch_bounds__(NT, NT >= 512 ? 1 : 512 / NT) ln_bwd_kernel(Ln
             const int j = (v * TPR + t) * PER;
             if (j < c.n) {
               float2 x[PAIRS], dy[PAIRS];
-              ln_piece<T, RAGGED>(in.at(q, 0), j, c.n, x);
-              ln_piece<T, RAGGED>(in.at(q, 1), j, c.n, dy);
+              ln_piece<T, RAGGED, ON16>(in.at(q, 0), in.off(it, q, 0), j, c.n, x);
+              ln_piece<T, RAGGED, ON16>(in.at(q, 1), in.off(it, q, 1), j, c.n, dy);
               if constexpr (!KEEP) ln_params_now<PAIRS>(weight, 1.f, j, w[0]);
 #pragma unroll
               for (int k = 0; k < PAIRS; ++k) {
@@ -588,13 +636,13 @@ __global__ void __launch_bounds__(NT, NT >= 512 ? 1 : 512 / NT) ln_bwd_kernel(Ln
           const int j = (v * TPR + t) * PER;
           if (j < c.n) {
             float2 x[PAIRS], dy[PAIRS];
-            ln_piece<T, RAGGED>(in.at(q, 0), j, c.n, x);
-            ln_piece<T, RAGGED>(in.at(q, 1), j, c.n, dy);
+            ln_piece<T, RAGGED, ON16>(in.at(q, 0), in.off(it, q, 0), j, c.n, x);
+            ln_piece<T, RAGGED, ON16>(in.at(q, 1), in.off(it, q, 1), j, c.n, dy);
             if constexpr (!KEEP) ln_params_now<PAIRS>(weight, 1.f, j, w[0]);
 #pragma unroll
             for (int k = 0; k < PAIRS; ++k)
               x[k] = scale * ln_fma((x[k] + offset) * scale, s2, ln_fma(dy[k], w[one * v][k], s1));
-            ln_store<T, RAGGED>(dx + j, c.n - j, x);
+            ln_store<T, RAGGED, ON16>(dx + j, c.n - j, x);
           }
         }
       }
@@ -631,51 +679,42 @@ __global__ void __launch_bounds__(NT, NT >= 512 ? 1 : 512 / NT) ln_bwd_kernel(Ln
     }
     if (g != G - 1) return;
   }
-  float* to = partial + (size_t)blockIdx.x * 2 * sh.N;
+  float* to = partial + (size_t)blockIdx.x * 2 * sh.pitch();
 #pragma unroll
-  for (int v = 0; v < V; ++v) {
-    const int j = (v * TPR + t) * PER;
-    if (j + PER <= c.n && sh.N % 4 == 0) {
+  for (int v = 0; v < V; ++v)
 #pragma unroll
-      for (int q = 0; q < PAIRS; q += 2) {
-        *reinterpret_cast<float4*>(to + j + 2 * q) = make_float4(dw[v][q].x, dw[v][q].y, dw[v][q + 1].x, dw[v][q + 1].y);
-        *reinterpret_cast<float4*>(to + sh.N + j + 2 * q) = make_float4(db[v][q].x, db[v][q].y, db[v][q + 1].x, db[v][q + 1].y);
-      }
-      continue;
-    }
-#pragma unroll
-    for (int q = 0; q < PAIRS; ++q) {
-      if (j + 2 * q < c.n) {
-        to[j + 2 * q] = dw[v][q].x;
-        to[sh.N + j + 2 * q] = db[v][q].x;
-      }
-      if (j + 2 * q + 1 < c.n) {
-        to[j + 2 * q + 1] = dw[v][q].y;
-        to[sh.N + j + 2 * q + 1] = db[v][q].y;
+    for (int q = 0; q < PAIRS; q += 2) {
+      const int j = (v * TPR + t) * PER + 2 * q;
+      if (j < c.n) {  // (behind the last column zeros)
+        *reinterpret_cast<float4*>(to + j) = make_float4(dw[v][q].x, dw[v][q].y, dw[v][q + 1].x, dw[v][q + 1].y);
+        *reinterpret_cast<float4*>(to + sh.pitch() + j) = make_float4(db[v][q].x, db[v][q].y, db[v][q + 1].x, db[v][q + 1].y);
       }
     }
-  }
 }
 
 inline bool ln_on16(const void* p, long long ld_bytes) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0 && ld_bytes % 16 == 0; }
 
-// Calls run(TPR, V, NT) (as integral constants) for rows of N elements: 16 elements a thread, 8 in short rows.  False: the row is too long.
-template <typename T, typename Run>
-bool ln_groups(int N, int rows, int sms, Run run) {
+// A CTA for each of a few short rows, all of them at once, rather than rings, whose setup takes longer than their rows: backward up to this many rows
+// (700 x 1500 7.5 us, with rings 8.9 and, off the 16-byte grid, 11.2; 148 x 2048 5.5 and 7.6; 2000 x 1024 11.6 and 9.5).
+inline bool ln_few(int rows, int N, int sms) { return rows <= 8 * sms && N <= 2048; }
+
+// Calls run(TPR, V, NT) (as integral constants) for rows of N elements: 16 elements a thread, 8 in short rows.  SMALL: in CTAs of 128 threads, which spread
+// over the SMs (forward, 148 x 2048: 2.7 us, a CTA a row 3.6).  False: the row is too long.
+template <typename T, bool SMALL, typename Run>
+bool ln_groups(int N, Run run) {
   constexpr int PER = LN_PER<T>, V = 16 / PER;
 #define LN_TRY(TPR, VV, NT)                                                                                        \
   if (N <= TPR * VV * PER) {                                                                                       \
     run(std::integral_constant<int, TPR>{}, std::integral_constant<int, VV>{}, std::integral_constant<int, NT>{}); \
     return true;                                                                                                   \
   }
-  // Few rows: CTAs of 128 threads, so that they spread over the SMs (64 x 256: 2.4 / 4.4 us forward / backward, 3.2 / 5.9 in CTAs of 512)
-  auto few = [&](int tpr) { return (long long)rows * tpr <= (long long)sms * 128; };
-  if (few(32)) {
+  if constexpr (SMALL) {
     LN_TRY(32, V / 2, 128)
     LN_TRY(32, V, 128)
+    LN_TRY(64, V, 128)
+    LN_TRY(128, V, 128)
+    return false;
   }
-  if (few(64)) LN_TRY(64, V, 128)
-  if (few(128)) LN_TRY(128, V, 128)
   // CTAs of 512 threads, one an SM: 148 rows of partial sums to add up, not 592 (those took 15 us)
   LN_TRY(32, V / 2, 512)
   LN_TRY(32, V, 512)
@@ -718,24 +757,31 @@ ard_status ln_fwd(ard_ctx* ctx, const LnShape& sh, float eps, const T* X, int ld
   cudaError_t err = cudaSuccess;
   bool done = false;
   const long long es = sizeof(T);
-  if (ln_on16(X, ldx * es) && ln_on16(Y, ldy * es)) {
-    const bool whole = !sh.hdr && sh.N % LN_PER<T> == 0 && ln_on16(weight, 0) && ln_on16(bias, 0);
+  auto run = [&](auto on16, auto small) {
+    constexpr bool ON16 = decltype(on16)::value;
+    const bool whole = ON16 && !sh.hdr && sh.N % LN_PER<T> == 0 && ln_on16(weight, 0) && ln_on16(bias, 0);
     LnRing ring;
-    ring.row_bytes = (int)((sh.N * es + 15) / 16 * 16);
-    ln_groups<T>(sh.N, sh.rows, ctx->sm_count, [&](auto tpr, auto v, auto nt) {
+    ring.row_bytes = (int)((sh.N * es + 15) / 16 * 16) + (ON16 ? 0 : 16);
+    ln_groups<T, decltype(small)::value>(sh.N, [&](auto tpr, auto v, auto nt) {
       constexpr int TPR = decltype(tpr)::value, V = decltype(v)::value, NT = decltype(nt)::value, G = NT / TPR;
-      if (NT == 1024 && !whole) return;
-      done = ln_rounds<NT, G, 1>(ctx, sh.rows, ring.row_bytes, [&](auto r, int blocks, int slots) {
-        constexpr int R = decltype(r)::value;
-        ring.slots = slots;
-        auto kern = ln_fwd_kernel<T, TPR, V, NT, R>;
-        err = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, LN_SMEM);
-        if (err == cudaSuccess)
-          err = ard_launch(ctx, kern, dim3(blocks), dim3(NT), (size_t)G * slots * R * ring.row_bytes, s, sh, eps, X, ldx, weight, bias, Y, ldy,
-                           mean, rstd, ring, ctx->d_status);
-      });
+      if constexpr (ON16 || NT < 1024) {
+        if (NT == 1024 && !whole) return;
+        done = ln_rounds<NT, G, 1>(ctx, sh.rows, ring.row_bytes, [&](auto r, int blocks, int slots) {
+          constexpr int R = decltype(r)::value;
+          ring.slots = slots;
+          auto kern = ln_fwd_kernel<T, TPR, V, NT, R, ON16>;
+          err = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, LN_SMEM);
+          if (err == cudaSuccess)
+            err = ard_launch(ctx, kern, dim3(blocks), dim3(NT), (size_t)G * slots * R * ring.row_bytes, s, sh, eps, X, ldx, weight, bias, Y, ldy,
+                             mean, rstd, ring, ctx->d_status);
+        });
+      }
     });
-  }
+  };
+  const bool on16 = ln_on16(X, ldx * es) && ln_on16(Y, ldy * es), few = ln_few(sh.rows, sh.N, ctx->sm_count);
+  if (few && on16 && sh.rows <= ctx->sm_count) run(std::true_type{}, std::true_type{});
+  else if (!few && on16) run(std::true_type{}, std::false_type{});
+  else if (!few) run(std::false_type{}, std::false_type{});
   if (!done) {
     const int room = 8 * ctx->sm_count;
     err = ard_launch(ctx, ln_fwd_any_kernel<T>, dim3(sh.rows < room ? sh.rows : room), dim3(LN_ANY_THREADS), 0, s, sh, eps, X, ldx, weight,
@@ -752,37 +798,46 @@ ard_status ln_bwd(ard_ctx* ctx, const LnShape& sh, const T* dY, int lddy, const 
                   const float* rstd, T* dX, int lddx, float* dweight, float* dbias, int zero_fill, cudaStream_t s) {
   const bool sums = dweight || dbias;
   if (!dX && !sums) return ARD_OK;
-  const long long fit = (long long)(sk_ws_bytes(ctx->sm_count) / sizeof(float) / 2) / sh.N;  // slices that the scratch holds
+  const long long fit = (long long)(sk_ws_bytes(ctx->sm_count) / sizeof(float) / 2) / sh.pitch();  // slices that the scratch holds
   if (sums && (!ctx->d_sk_ws || fit < 1)) return ARD_ERR_UNSUPPORTED;
   float* partial = sums ? (float*)ctx->d_sk_ws : nullptr;
   long long slices = 0;
   cudaError_t err = cudaSuccess;
   bool done = sh.rows == 0;
   const long long es = sizeof(T);
-  if (!done && ln_on16(X, ldx * es) && ln_on16(dY, lddy * es) && ln_on16(dX, dX ? lddx * es : 0)) {
-    const bool whole = !sh.hdr && sh.N % LN_PER<T> == 0 && ln_on16(weight, 0);
+  auto run = [&](auto on16) {
+    constexpr bool ON16 = decltype(on16)::value;
+    const bool whole = ON16 && !sh.hdr && sh.N % LN_PER<T> == 0 && ln_on16(weight, 0);
     LnRing ring;
-    ring.row_bytes = (int)((sh.N * es + 15) / 16 * 16);
-    ln_groups<T>(sh.N, sh.rows, ctx->sm_count, [&](auto tpr, auto v, auto nt) {
+    ring.row_bytes = (int)((sh.N * es + 15) / 16 * 16) + (ON16 ? 0 : 16);
+    ln_groups<T, false>(sh.N, [&](auto tpr, auto v, auto nt) {
       constexpr int TPR = decltype(tpr)::value, V = decltype(v)::value, NT = decltype(nt)::value, G = NT / TPR;
-      if (NT == 1024 && !whole) return;
-      ln_rounds<NT, G, 2>(ctx, sh.rows, ring.row_bytes, [&](auto r, int blocks, int slots) {
-        constexpr int R = decltype(r)::value;
-        if (sums && blocks > fit) return;
-        ring.slots = slots;
-        size_t smem = (size_t)G * slots * 2 * R * ring.row_bytes;
-        const size_t exchange = G > 1 ? 2 * sizeof(float) * V * TPR * LN_PER<T> : 0;
-        if (smem < exchange) smem = exchange;
-        auto kern = ln_bwd_kernel<T, TPR, V, NT, R>;
-        err = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, LN_SMEM);
-        if (err == cudaSuccess)
-          err = ard_launch(ctx, kern, dim3(blocks), dim3(NT), smem, s, sh, dY, lddy, X, ldx, weight, mean, rstd, dX, lddx, partial, ring,
-                           ctx->d_status);
-        slices = blocks;
-        ctx->launches++;
-        done = true;
-      });
+      if constexpr (ON16 || NT < 1024) {
+        if (NT == 1024 && !whole) return;
+        ln_rounds<NT, G, 2>(ctx, sh.rows, ring.row_bytes, [&](auto r, int blocks, int slots) {
+          constexpr int R = decltype(r)::value;
+          if (sums && blocks > fit) return;
+          ring.slots = slots;
+          size_t smem = (size_t)G * slots * 2 * R * ring.row_bytes;
+          if constexpr (G > 1) {
+            constexpr size_t exchange = 2 * sizeof(float) * V * TPR * LN_PER<T>;
+            if (smem < exchange) smem = exchange;
+          }
+          auto kern = ln_bwd_kernel<T, TPR, V, NT, R, ON16>;
+          err = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, LN_SMEM);
+          if (err == cudaSuccess)
+            err = ard_launch(ctx, kern, dim3(blocks), dim3(NT), smem, s, sh, dY, lddy, X, ldx, weight, mean, rstd, dX, lddx, partial, ring,
+                             ctx->d_status);
+          slices = blocks;
+          ctx->launches++;
+          done = true;
+        });
+      }
     });
+  };
+  if (!done && !ln_few(sh.rows, sh.N, ctx->sm_count)) {
+    if (ln_on16(X, ldx * es) && ln_on16(dY, lddy * es) && ln_on16(dX, dX ? lddx * es : 0)) run(std::true_type{});
+    else run(std::false_type{});
     ARD_CUDA_OK(err);
   }
   if (!done) {

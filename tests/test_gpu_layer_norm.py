@@ -231,3 +231,34 @@ def test_graph_replays_and_repeats_give_the_same_bits(dtype, rows, N):
         assert all(torch.equal(a, b) for a, b in zip(second, outs)) and not torch.equal(first[3], second[3])
     finally:
         ctx.close()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rows,N,ld,off", [(1300, 255, (0, 0, 0, 0), 0), (1300, 64, (1, 2, 3, 5), 1), (1250, 1, (0, 1, 2, 3), 3), (1400, 31, (4, 2, 1, 0), 2),
+                                           (1300, 1000, (0, 0, 0, 0), 4), (1200, 8, (0, 0, 0, 0), 5), (200, 2999, (2, 0, 4, 6), 3), (40, 8191, (0, 0, 0, 0), 0),
+                                           (1190, 520, (8, 8, 4, 8), 0), (1300, 2048, (2, 2, 2, 2), 6), (3, 2056, (1, 3, 5, 7), 7), (5000, 130, (0, 0, 0, 0), 0),
+                                           (37, 4096, (4, 4, 4, 4), 0)])
+def test_rows_that_begin_anywhere(dtype, rows, N, ld, off):
+    """More or longer rows than a CTA each is made for, off the 16-byte grid: their copies start ahead of them and end behind them, in NaN."""
+    ctx = Ctx(0)
+    try:
+        _run(ctx.h, None, dtype, rows, N, ld=ld, off=off, seed=N + off)
+        _run(ctx.h, None, dtype, rows, N, ld=ld, off=off, seed=N, affine=False)
+        if N >= 16:
+            pat = ctx.pattern(ard.ARD_ROW, 16, N)
+            ard.ard_pattern_set(ctx.h, pat, 3, 2)
+            _run(ctx.h, pat, dtype, rows, N, 3, 2, ld=ld, off=off, seed=N + 1)
+        assert ard.ard_last_device_status(ctx.h) == 0
+    finally:
+        ctx.close()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rows", [147, 148, 149, 1183, 1184, 1185])
+@pytest.mark.parametrize("N", [2048, 2047, 2056])
+def test_where_the_kernels_change(dtype, rows, N):
+    ctx = Ctx(0)
+    try:
+        _run(ctx.h, None, dtype, rows, N, seed=rows)
+    finally:
+        ctx.close()
