@@ -684,8 +684,9 @@ ard_status ard_lstm_gates_bwd(ard_ctx* ctx, const ard_pattern* pat, ard_dtype dz
  * ard_layer_fwd leaves activations (column j = kept unit j, leading dimensions >= N so that any pattern fits), the
  * statistics are those of the n kept columns, weight and bias are full width and read at the kept units.  Columns >= n
  * are neither read as values nor written.
- * X, Y of element type `dtype`, any alignment (fastest with 16-byte aligned pointers and rows); weight, bias fp32 [N], NULL: 1 and 0; mean, rstd fp32 [rows], what the backward call needs, may be NULL when
- * there is none.  Statistics and sums are fp32.  Y must not overlap X.
+ * X, Y of element type `dtype`, any alignment (fastest with 16-byte aligned pointers and rows); weight, bias fp32 [N],
+ * NULL: 1 and 0; mean, rstd fp32 [rows], what the backward call needs, may be NULL when there is none.  Statistics and
+ * sums are fp32.  Y must not overlap X.
  * Errors: ARD_ERR_INVALID_ARG (NULL, negative size, dtype, eps negative or not finite, tile pattern, another context's
  * pattern), ARD_ERR_SHAPE (N differs from the pattern's, leading dimension below N), ARD_ERR_UNSUPPORTED (more than
  * 2^30 rows; backward: N above 4 million).  Asynchronous. */
