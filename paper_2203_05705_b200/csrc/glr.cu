@@ -370,7 +370,7 @@ __device__ __forceinline__ void glr_setup(int CL, Shared& sh) {
 }
 
 template <typename T, int VEC, bool GATE, int W, int WT, int SPT, bool BULK>
-__global__ void __launch_bounds__(W* WT, W* WT < 256 ? 1 : SPT < 8 ? 3 : 2)
+__global__ void __launch_bounds__(W* WT, W* WT < 256 ? 1 : SPT < 8 && SPT != 4 ? 3 : 2)
     glr_fwd_kernel(const GlrArgs a, int CL, const __grid_constant__ GlrTiles tiles) {
   using V = GlrV<VEC>;
   constexpr int M = GATE ? 3 : 2, SLAB = WT * SPT;
@@ -472,7 +472,7 @@ __global__ void __launch_bounds__(W* WT, W* WT < 256 ? 1 : SPT < 8 ? 3 : 2)
 }
 
 template <typename T, int VEC, bool GATE, int W, int WT, int SPT, bool BULK>
-__global__ void __launch_bounds__(W* WT, W* WT < 256 ? 1 : SPT < 8 ? 3 : 2)
+__global__ void __launch_bounds__(W* WT, W* WT < 256 ? 1 : SPT < 8 && SPT != 4 ? 3 : 2)
     glr_bwd_kernel(const GlrArgs a, int CL, const __grid_constant__ GlrTiles tiles) {
   using V = GlrV<VEC>;
   constexpr int M = GATE ? 4 : 3, SLAB = WT * SPT;
@@ -721,7 +721,11 @@ struct GlrBwd {
           return glr_launch(ctx, glr_bwd_kernel<T, VEC, GATE, W, WT, SPT, true>, a, tiles, W * VEC, CL, 256,
                             glr_ring<GlrFeed<T, VEC, GATE ? 4 : 3, W, WT, SPT, true>>(), per_sm, s);
       }
-      return glr_launch(ctx, glr_bwd_kernel<T, VEC, GATE, W, WT, SPT, false>, a, tiles, W * VEC, CL, 256, 0, per_sm, s);
+      // 2-byte values fetched into registers: half the steps a thread, in units of half a warp (a slab is 64 steps, as the states lie), rather than registers
+      // spilt: 2048 x 8 x 2044 192 -> 152 us (4-byte values 118 -> 128, forward 75 -> 82: those stay)
+      if constexpr (SPT == 8 && sizeof(T) == 2)
+        return glr_launch(ctx, glr_bwd_kernel<T, VEC, GATE, 16, 16, 4, false>, a, tiles, 16 * VEC, CL, 256, 0, per_sm, s);
+      else return glr_launch(ctx, glr_bwd_kernel<T, VEC, GATE, W, WT, SPT, false>, a, tiles, W * VEC, CL, 256, 0, per_sm, s);
     });
   }
 };
