@@ -692,15 +692,204 @@ __global__ void __launch_bounds__(NT, NT >= 512 ? 1 : 512 / NT) ln_bwd_kernel(Ln
     }
 }
 
+// ---- short rows ------------------------------------------------------------------------------------
+// TPR lanes hold a row of up to 8 TPR elements, eight each, from global memory as it is: many rows and many warps (32 an SM) at once, and the next row's
+// loads ahead of this one's arithmetic.  16384 x 64 bf16 3.5 / 6.2 us (rings, a warp a row: 8.4 / 12.5), 60000 x 65 8.5 / 17.2
+// (29.5 / 46.6), 131072 x 256 forward 36.3 (39).
+// WIDE: a lane's elements lie together on 16 bytes; otherwise lanes take neighbouring elements.
+constexpr int LN_SHORT = 512, LN_SHORT_N = 256;
+template <int TPR, bool WIDE>
+__device__ __forceinline__ int ln_short_col(int t, int e) { return WIDE ? t * 8 + e : e * TPR + t; }
+template <typename T, int TPR, bool WIDE>
+__device__ __forceinline__ void ln_short_load(const T* row, int t, int n, float2 (&v)[4]) {
+  if (WIDE && t * 8 + 8 <= n) {
+    constexpr int PIECES = sizeof(T) / 2, PAIRS = LN_PAIRS<T>;
+#pragma unroll
+    for (int k = 0; k < PIECES; ++k) {
+      const uint4 q = *reinterpret_cast<const uint4*>(row + t * 8 + k * LN_PER<T>);
+      float2 x[PAIRS];
+      ln_unpack<T>(q, x);
+#pragma unroll
+      for (int h = 0; h < PAIRS; ++h) v[k * PAIRS + h] = x[h];
+    }
+    return;
+  }
+#pragma unroll
+  for (int h = 0; h < 4; ++h) {
+    const int a = ln_short_col<TPR, WIDE>(t, 2 * h), b = ln_short_col<TPR, WIDE>(t, 2 * h + 1);
+    v[h].x = a < n ? ln_get(row, a) : 0.f;
+    v[h].y = b < n ? ln_get(row, b) : 0.f;
+  }
+}
+template <typename T, int TPR, bool WIDE>
+__device__ __forceinline__ void ln_short_store(T* row, int t, int n, const float2 (&v)[4]) {
+  if (WIDE && t * 8 + 8 <= n) {
+    constexpr int PIECES = sizeof(T) / 2, PAIRS = LN_PAIRS<T>;
+#pragma unroll
+    for (int k = 0; k < PIECES; ++k) {
+      float2 x[PAIRS];
+#pragma unroll
+      for (int h = 0; h < PAIRS; ++h) x[h] = v[k * PAIRS + h];
+      ln_store<T, false, true>(row + t * 8 + k * LN_PER<T>, LN_PER<T>, x);
+    }
+    return;
+  }
+#pragma unroll
+  for (int h = 0; h < 4; ++h) {
+    const int a = ln_short_col<TPR, WIDE>(t, 2 * h), b = ln_short_col<TPR, WIDE>(t, 2 * h + 1);
+    if (a < n) ln_put(row, a, v[h].x);
+    if (b < n) ln_put(row, b, v[h].y);
+  }
+}
+template <int TPR, bool WIDE>
+__device__ __forceinline__ void ln_short_params(const float* w, float other, const LnCols& c, int t, float2 (&v)[4]) {
+#pragma unroll
+  for (int h = 0; h < 4; ++h) {
+    const int a = ln_short_col<TPR, WIDE>(t, 2 * h), b = ln_short_col<TPR, WIDE>(t, 2 * h + 1);
+    v[h].x = w && a < c.n ? w[c.b0 + a * c.dp] : other;
+    v[h].y = w && b < c.n ? w[c.b0 + b * c.dp] : other;
+  }
+}
+template <int TPR, int M>
+__device__ __forceinline__ void ln_lane_sums(float (&x)[M]) {
+#pragma unroll
+  for (int o = TPR / 2; o > 0; o >>= 1)
+#pragma unroll
+    for (int m = 0; m < M; ++m) x[m] += __shfl_xor_sync(0xFFFFFFFFu, x[m], o);
+}
+
+template <typename T, int TPR, bool WIDE>
+__global__ void __launch_bounds__(LN_SHORT, 2) ln_fwd_short_kernel(LnShape sh, float eps, const T* X, int ldx, const float* weight, const float* bias,
+                                                                  T* Y, int ldy, float* mean, float* rstd) {
+  constexpr int G = LN_SHORT / TPR;
+  pdl_launch_dependents();
+  pdl_wait_prior_grids();
+  const LnCols c = ln_cols(sh);
+  const float inv_n = 1.f / (float)c.n;
+  const int t = threadIdx.x % TPR, g = threadIdx.x / TPR;
+  const long long stride = (long long)gridDim.x * G;
+  float2 w[4], b[4], next[4];
+  ln_short_params<TPR, WIDE>(weight, 1.f, c, t, w);
+  ln_short_params<TPR, WIDE>(bias, 0.f, c, t, b);
+  auto load = [&](long long r) { ln_short_load<T, TPR, WIDE>(X + (size_t)r * ldx, t, r < sh.rows ? c.n : 0, next); };
+  long long r0 = (long long)blockIdx.x * G;
+  load(r0 + g);
+  for (; r0 < sh.rows; r0 += stride) {
+    const long long r = r0 + g;
+    float2 x[4];
+#pragma unroll
+    for (int h = 0; h < 4; ++h) x[h] = next[h];
+    load(r + stride);
+    float2 sum = (x[0] + x[1]) + (x[2] + x[3]);
+    float s[1] = {sum.x + sum.y};
+    ln_lane_sums<TPR, 1>(s);
+    const float mu = s[0] * inv_n;
+    sum = ln_both(0.f);
+#pragma unroll
+    for (int h = 0; h < 4; ++h) {
+      x[h] = x[h] + ln_both(-mu);
+      if (ln_short_col<TPR, WIDE>(t, 2 * h) >= c.n) x[h].x = 0.f;
+      if (ln_short_col<TPR, WIDE>(t, 2 * h + 1) >= c.n) x[h].y = 0.f;
+      sum = ln_fma(x[h], x[h], sum);
+    }
+    s[0] = sum.x + sum.y;
+    ln_lane_sums<TPR, 1>(s);
+    const float rs = ln_rsqrt(fmaf(s[0], inv_n, eps));
+    if (r < sh.rows) {
+#pragma unroll
+      for (int h = 0; h < 4; ++h) x[h] = ln_fma(x[h] * ln_both(rs), w[h], b[h]);
+      ln_short_store<T, TPR, WIDE>(Y + (size_t)r * ldy, t, c.n, x);
+      if (t == 0) {
+        if (mean) mean[r] = mu;
+        if (rstd) rstd[r] = rs;
+      }
+    }
+  }
+}
+
+template <typename T, int TPR, bool WIDE>
+__global__ void __launch_bounds__(LN_SHORT, 2) ln_bwd_short_kernel(LnShape sh, const T* dY, int lddy, const T* X, int ldx, const float* weight,
+                                                                  const float* mean, const float* rstd, T* dX, int lddx, float* partial) {
+  constexpr int G = LN_SHORT / TPR, COLS = TPR * 8;
+  __shared__ float2 sums[G][2][COLS / 2];
+  pdl_launch_dependents();
+  pdl_wait_prior_grids();
+  const LnCols c = ln_cols(sh);
+  const float inv_n = 1.f / (float)c.n;
+  const int t = threadIdx.x % TPR, g = threadIdx.x / TPR;
+  const long long stride = (long long)gridDim.x * G;
+  float2 w[4], dw[4], db[4];
+  ln_short_params<TPR, WIDE>(weight, 1.f, c, t, w);
+#pragma unroll
+  for (int h = 0; h < 4; ++h) dw[h] = db[h] = ln_both(0.f);
+  for (long long r0 = (long long)blockIdx.x * G; r0 < sh.rows; r0 += stride) {
+    const long long r = r0 + g;
+    const bool live = r < sh.rows;
+    float2 x[4], dy[4];
+    ln_short_load<T, TPR, WIDE>(X + (size_t)r * ldx, t, live ? c.n : 0, x);
+    ln_short_load<T, TPR, WIDE>(dY + (size_t)r * lddy, t, live ? c.n : 0, dy);
+    const float mu = live ? mean[r] : 0.f, rs = live ? rstd[r] : 0.f;
+    float2 s1 = ln_both(0.f), s2 = ln_both(0.f);
+#pragma unroll
+    for (int h = 0; h < 4; ++h) {  // (behind the last column dy is zero)
+      x[h] = (x[h] + ln_both(-mu)) * ln_both(rs);
+      dw[h] = ln_fma(dy[h], x[h], dw[h]);
+      db[h] = db[h] + dy[h];
+      dy[h] = dy[h] * w[h];
+      s1 = s1 + dy[h];
+      s2 = ln_fma(dy[h], x[h], s2);
+    }
+    float s[2] = {s1.x + s1.y, s2.x + s2.y};
+    ln_lane_sums<TPR, 2>(s);
+    if (dX && live) {
+      const float2 a = ln_both(-s[0] * inv_n), b = ln_both(-s[1] * inv_n);
+#pragma unroll
+      for (int h = 0; h < 4; ++h) x[h] = ln_both(rs) * ln_fma(x[h], b, dy[h] + a);
+      ln_short_store<T, TPR, WIDE>(dX + (size_t)r * lddx, t, c.n, x);
+    }
+  }
+  if (!partial) return;
+  // [group][2][column, in the order of the lanes' elements], added in the groups' order
+#pragma unroll
+  for (int h = 0; h < 4; ++h) {
+    sums[g][0][h * TPR + t] = dw[h];
+    sums[g][1][h * TPR + t] = db[h];
+  }
+  __syncthreads();
+  for (int k = threadIdx.x; k < COLS; k += LN_SHORT) {  // pairs of columns of either sum
+    const int which = k / (COLS / 2), at = k % (COLS / 2), h = at / TPR, lane = at % TPR;
+    float2 sum = ln_both(0.f);
+#pragma unroll 8
+    for (int q = 0; q < G; ++q) sum = sum + sums[q][which][at];
+    float* to = partial + ((size_t)blockIdx.x * 2 + which) * sh.pitch();
+    const int ja = ln_short_col<TPR, WIDE>(lane, 2 * h), jb = ln_short_col<TPR, WIDE>(lane, 2 * h + 1);
+    if (ja < c.n) to[ja] = sum.x;
+    if (jb < c.n) to[jb] = sum.y;
+  }
+}
+
 inline bool ln_on16(const void* p, long long ld_bytes) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0 && ld_bytes % 16 == 0; }
 
 // A CTA for each of a few short rows, all of them at once, rather than rings, whose setup takes longer than their rows: backward up to this many rows
 // (700 x 1500 7.5 us, with rings 8.9 and, off the 16-byte grid, 11.2; 148 x 2048 5.5 and 7.6; 2000 x 1024 11.6 and 9.5).
 inline bool ln_few(int rows, int N, int sms) { return rows <= 8 * sms && N <= 2048; }
 
-// Calls run(TPR, V, NT) (as integral constants) for rows of N elements: 16 elements a thread, 8 in short rows.  SMALL: in CTAs of 128 threads, which spread
+// Calls run(TPR, WIDE) for short rows.
+template <typename T, typename Run>
+void ln_short(const LnShape& sh, bool wide, Run run) {
+  auto width = [&](auto w) {
+    if (sh.N <= 64) run(std::integral_constant<int, 8>{}, w);
+    else if (sh.N <= 128) run(std::integral_constant<int, 16>{}, w);
+    else run(std::integral_constant<int, 32>{}, w);
+  };
+  if (wide) width(std::true_type{});
+  else width(std::false_type{});
+}
+
+enum { LN_FORWARD, LN_BACKWARD, LN_FEW };
+// Calls run(TPR, V, NT) (as integral constants) for rows of N elements: 16 elements a thread, 8 in short rows.  LN_FEW: in CTAs of 128 threads, which spread
 // over the SMs (forward, 148 x 2048: 2.7 us, a CTA a row 3.6).  False: the row is too long.
-template <typename T, bool SMALL, typename Run>
+template <typename T, int KIND, typename Run>
 bool ln_groups(int N, Run run) {
   constexpr int PER = LN_PER<T>, V = 16 / PER;
 #define LN_TRY(TPR, VV, NT)                                                                                        \
@@ -708,7 +897,7 @@ bool ln_groups(int N, Run run) {
     run(std::integral_constant<int, TPR>{}, std::integral_constant<int, VV>{}, std::integral_constant<int, NT>{}); \
     return true;                                                                                                   \
   }
-  if constexpr (SMALL) {
+  if constexpr (KIND == LN_FEW) {
     LN_TRY(32, V / 2, 128)
     LN_TRY(32, V, 128)
     LN_TRY(64, V, 128)
@@ -716,7 +905,7 @@ bool ln_groups(int N, Run run) {
     return false;
   }
   // CTAs of 512 threads, one an SM: 148 rows of partial sums to add up, not 592 (those took 15 us)
-  LN_TRY(32, V / 2, 512)
+  if constexpr (KIND == LN_BACKWARD) LN_TRY(32, V / 2, 512)
   LN_TRY(32, V, 512)
   LN_TRY(64, V, 512)
   LN_TRY(128, V, 512)
@@ -762,7 +951,7 @@ ard_status ln_fwd(ard_ctx* ctx, const LnShape& sh, float eps, const T* X, int ld
     const bool whole = ON16 && !sh.hdr && sh.N % LN_PER<T> == 0 && ln_on16(weight, 0) && ln_on16(bias, 0);
     LnRing ring;
     ring.row_bytes = (int)((sh.N * es + 15) / 16 * 16) + (ON16 ? 0 : 16);
-    ln_groups<T, decltype(small)::value>(sh.N, [&](auto tpr, auto v, auto nt) {
+    ln_groups<T, decltype(small)::value ? LN_FEW : LN_FORWARD>(sh.N, [&](auto tpr, auto v, auto nt) {
       constexpr int TPR = decltype(tpr)::value, V = decltype(v)::value, NT = decltype(nt)::value, G = NT / TPR;
       if constexpr (ON16 || NT < 1024) {
         if (NT == 1024 && !whole) return;
@@ -780,6 +969,14 @@ ard_status ln_fwd(ard_ctx* ctx, const LnShape& sh, float eps, const T* X, int ld
   };
   const bool on16 = ln_on16(X, ldx * es) && ln_on16(Y, ldy * es), few = ln_few(sh.rows, sh.N, ctx->sm_count);
   if (few && on16 && sh.rows <= ctx->sm_count) run(std::true_type{}, std::true_type{});
+  else if (!few && sh.N <= LN_SHORT_N)
+    ln_short<T>(sh, on16, [&](auto tpr, auto wide) {
+      constexpr int TPR = decltype(tpr)::value, G = LN_SHORT / TPR;
+      const long long blocks = ((long long)sh.rows + G - 1) / G, room = 2 * ctx->sm_count;
+      err = ard_launch(ctx, ln_fwd_short_kernel<T, TPR, decltype(wide)::value>, dim3((unsigned)(blocks < room ? blocks : room)), dim3(LN_SHORT), 0, s, sh,
+                       eps, X, ldx, weight, bias, Y, ldy, mean, rstd);
+      done = true;
+    });
   else if (!few && on16) run(std::true_type{}, std::false_type{});
   else if (!few) run(std::false_type{}, std::false_type{});
   if (!done) {
@@ -810,9 +1007,9 @@ ard_status ln_bwd(ard_ctx* ctx, const LnShape& sh, const T* dY, int lddy, const 
     const bool whole = ON16 && !sh.hdr && sh.N % LN_PER<T> == 0 && ln_on16(weight, 0);
     LnRing ring;
     ring.row_bytes = (int)((sh.N * es + 15) / 16 * 16) + (ON16 ? 0 : 16);
-    ln_groups<T, false>(sh.N, [&](auto tpr, auto v, auto nt) {
+    ln_groups<T, LN_BACKWARD>(sh.N, [&](auto tpr, auto v, auto nt) {
       constexpr int TPR = decltype(tpr)::value, V = decltype(v)::value, NT = decltype(nt)::value, G = NT / TPR;
-      if constexpr (ON16 || NT < 1024) {
+      if constexpr (ON16 || (NT < 1024 && V * LN_PER<T> > 8)) {
         if (NT == 1024 && !whole) return;
         ln_rounds<NT, G, 2>(ctx, sh.rows, ring.row_bytes, [&](auto r, int blocks, int slots) {
           constexpr int R = decltype(r)::value;
@@ -836,8 +1033,28 @@ ard_status ln_bwd(ard_ctx* ctx, const LnShape& sh, const T* dY, int lddy, const 
     });
   };
   if (!done && !ln_few(sh.rows, sh.N, ctx->sm_count)) {
-    if (ln_on16(X, ldx * es) && ln_on16(dY, lddy * es) && ln_on16(dX, dX ? lddx * es : 0)) run(std::true_type{});
-    else run(std::false_type{});
+    const bool on16 = ln_on16(X, ldx * es) && ln_on16(dY, lddy * es) && ln_on16(dX, dX ? lddx * es : 0);
+    // (rows of 129 to 256 on the grid through rings: 131072 x 256 56 us, by lanes 73)
+    if (sh.N <= (on16 ? 128 : LN_SHORT_N)) {
+      ln_short<T>(sh, on16, [&](auto tpr, auto wide) {
+        constexpr int TPR = decltype(tpr)::value, G = LN_SHORT / TPR;
+        constexpr bool WIDE = decltype(wide)::value;
+        if constexpr (!WIDE || TPR < 32) {
+          const long long most = ((long long)sh.rows + G - 1) / G, room = 2 * ctx->sm_count;
+          const int blocks = (int)(most < room ? most : room);
+          if (sums && blocks > fit) return;
+          err = ard_launch(ctx, ln_bwd_short_kernel<T, TPR, WIDE>, dim3(blocks), dim3(LN_SHORT), 0, s, sh, dY, lddy, X, ldx, weight, mean, rstd, dX, lddx,
+                           partial);
+          slices = blocks;
+          ctx->launches++;
+          done = true;
+        }
+      });
+    } else if (on16) {
+      run(std::true_type{});
+    } else {
+      run(std::false_type{});
+    }
     ARD_CUDA_OK(err);
   }
   if (!done) {

@@ -262,3 +262,19 @@ def test_where_the_kernels_change(dtype, rows, N):
         _run(ctx.h, None, dtype, rows, N, seed=rows)
     finally:
         ctx.close()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rows,N,ld,off", [(1185, 64, (0, 0, 0, 0), 0), (20000, 33, (0, 1, 2, 3), 1), (5000, 128, (8, 0, 8, 16), 0), (3000, 129, (0, 0, 0, 0), 0),
+                                           (9000, 256, (0, 8, 0, 8), 0), (2500, 250, (6, 6, 6, 6), 0), (40000, 8, (0, 0, 0, 0), 0), (30000, 3, (0, 0, 0, 0), 0),
+                                           (1200, 100, (4, 4, 4, 4), 0), (4000, 257, (0, 0, 0, 0), 3), (19000, 256, (1, 1, 1, 1), 0)])
+def test_many_short_rows(dtype, rows, N, ld, off):
+    ctx = Ctx(0)
+    try:
+        _run(ctx.h, None, dtype, rows, N, ld=ld, off=off, seed=N + off)
+        if N >= 16:
+            pat = ctx.pattern(ard.ARD_ROW, 16, N)
+            ard.ard_pattern_set(ctx.h, pat, 2, 2)
+            _run(ctx.h, pat, dtype, rows, N, 2, 2, ld=ld, off=off, zero_fill=0, seed=N + 1)
+    finally:
+        ctx.close()
