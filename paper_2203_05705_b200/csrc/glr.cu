@@ -340,7 +340,8 @@ __device__ __forceinline__ GlrV<VEC> glr_enter(GlrShared<VEC, W, WT>& sh, int wt
         for (int r = 0; r < CL; ++r) glr_send<VEC>(&sh.post.box[set][rank][ch], &sh.post.bar[set], r, all);
       }
       if (threadIdx.x == 0) mbar_arrive_expect_tx(smem_u32(&sh.post.bar[set]), (uint32_t)(CL * W * sizeof(GlrMap<VEC>)));
-      mbar_wait(smem_u32(&sh.post.bar[set]), (uint32_t)(mail >> 1) & 1u, &sh.gone, status);
+      // an acquire of the cluster's scope: other CTAs wrote what is read behind it
+      mbar_wait_cluster(smem_u32(&sh.post.bar[set]), (uint32_t)(mail >> 1) & 1u, &sh.gone, status);
       for (int r = 0; r < rank; ++r) c = sh.post.box[set][r][ch].of(c);
       if (wt == LAST) {
         GlrV<VEC> behind = c;
