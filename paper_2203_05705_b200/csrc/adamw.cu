@@ -453,7 +453,10 @@ __global__ void __launch_bounds__(AW_THREADS, AW8_PER_SM) adamw8_kernel(const __
       ++taken;
       if (whole(e, base)) {
         uint8_t* from = mine + slot * AW8_SLOT;
-        if (by_lanes) reinterpret_cast<float*>(from + AW8_MS)[lane] = sc;  // (v's lie behind m's)
+        if (by_lanes) {
+          reinterpret_cast<float*>(from + AW8_MS)[lane] = sc;  // (v's lie behind m's)
+          fence_proxy_async_smem();                            // before a later tile's bulk copies into the same bytes
+        }
         __syncwarp();
 #pragma unroll AW8_UNROLL
         for (int u = 0; u < AW8_QUADS; ++u) {
