@@ -45,6 +45,8 @@ class GlrLayer:
         self.Wk = new(3 * H, I, dtype=BF) if in_pat is not None else self.W   # packed in both dimensions
         self.dWk = new(3 * H, I) if in_pat is not None else self.dW
         self.X = None
+        self.X_live = None       # of padded batches
+        self.signs = (1 - 2 * (torch.arange(I, device="cuda") % 2)).to(BF)
 
     def _columns(self, t, k):
         return t.data_ptr() + k * self.H * t.element_size()
@@ -72,16 +74,30 @@ class GlrLayer:
             raise ValueError("%s has to be contiguous %s %s on %s, got %s %s on %s"
                              % (name, dtype, shape, self.Xn.device, t.dtype, tuple(t.shape), t.device))
 
+    def _live(self, X, lens):
+        """X without what a padded batch may hold behind its sequences' ends and the norm cannot carry.  Norm and products run over all rows; the gates'
+        gradients are zero there, which a product takes away only if what it is multiplied with is finite.  So values that are not finite, or whose
+        squares may not be, become +1 and -1 in turn (rows of which have a variance, for eps = 0: then all padded ones do)."""
+        T, B, I = self.T, self.B, self.I
+        if self.X_live is None:
+            self.X_live = torch.empty_like(self.Xn)
+        x = X.view(T, B, I)
+        stays = (torch.arange(T, device=X.device)[:, None] < lens).view(T, B, 1)
+        if self.eps > 0:
+            stays = stays | (x.abs() <= 2.0 ** 50)
+        return torch.where(stays, x, self.signs, out=self.X_live.view(T, B, I)).view(T * B, I)
+
     def forward(self, X, alpha, h0=None, lens=None):
         """X: bf16 [T*B][I] (with in_pat compact), kept until backward().  Returns Y [T*B][H], compact: the kept units' columns are valid.
-        h0: fp32 [B][H] or None; lens: int32 [B] or None; the last states are in hT."""
+        h0: fp32 [B][H] or None; lens: int32 [B] or None, rows of X and of backward()'s dY behind a sequence's end may hold anything; the last
+        states are in hT."""
         T, B, H = self.T, self.B, self.H
         self._check("X", X, (T * B, self.I), BF)
         self._check("h0", h0, (B, H), F32)
         self._check("lens", lens, (B,), torch.int32)
-        self.X, self.lens = X, lens
+        self.X, self.lens = X if lens is None else self._live(X, lens), lens
         self.pack()
-        self._gates(X, T * B)
+        self._gates(self.X, T * B)
         z = [self._columns(self.Z, k) for k in range(3)]
         ard.ard_glr_forward(self.ctx, self.pat, ard.ARD_BF16, T, B, H, alpha, z[0], z[1], z[2], 3 * H, lens, h0, self.Y, H, self.hT, self.S)
         return self.Y
