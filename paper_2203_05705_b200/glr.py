@@ -36,6 +36,7 @@ class GlrLayer:
         self.W = self.p_W.to(BF)
         self.dW, self.db, self.dnw, self.dnb = new(3 * H, I), new(3 * H), new(I), new(I)
         self.Xn, self.dXn, self.dX = (new(T * B, I, dtype=BF) for _ in range(3))
+        self.dXs = new(T * B, I)
         self.mean, self.rstd = new(T * B), new(T * B)
         self.Z, self.dZ = new(T * B, 3 * H, dtype=BF), new(T * B, 3 * H, dtype=BF)
         self.Y = new(T * B, H, dtype=BF)
@@ -119,9 +120,10 @@ class GlrLayer:
             if ip is not None:
                 ard.ard_expand_weight_grad_cols(ctx, pat, ip, ard.ARD_F32, I, H, self._rows(self.dWk, k), I, self._rows(self.dW, k), I, 1)
             ard.ard_bias_grad(ctx, pat, ard.ARD_BF16, T * B, H, dz[k], 3 * H, 1, self._columns(self.db, k), 1)
-            # the gates' shares of the input's gradient are added up in bf16, as ARD_FLAG_ACCUMULATE does
-            ard.ard_layer_bwd_data(ctx, pat, ip, ard.ARD_BF16, T * B, I, H, 1.0, dz[k], 3 * H, 1 | (ard.ARD_FLAG_ACCUMULATE if k else 0),
-                                   self._rows(self.Wk, k), I, None, 0, self.dXn, I)
+            # the gates' shares of the input's gradient are added up in fp32 and rounded once: they cancel in part, and the norm's adjoint takes means off
+            ard.ard_layer_bwd_data(ctx, pat, ip, ard.ARD_BF16, T * B, I, H, 1.0, dz[k], 3 * H,
+                                   1 | ard.ARD_FLAG_OUT_F32 | (ard.ARD_FLAG_ACCUMULATE if k else 0), self._rows(self.Wk, k), I, None, 0, self.dXs, I)
+        self.dXn.copy_(self.dXs)
         ard.ard_layer_norm_bwd(ctx, ip, ard.ARD_BF16, T * B, I, self.dXn, I, self.X, I, self.p_nw, self.mean, self.rstd, self.dX, I, self.dnw,
                                self.dnb, 1)
         return self.dX
