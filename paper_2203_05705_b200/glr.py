@@ -47,6 +47,7 @@ class GlrLayer:
         self.dWk = new(3 * H, I) if in_pat is not None else self.dW
         self.X = None
         self.X_live = None       # of padded batches
+        self.times = torch.arange(T, device="cuda")[:, None]
         self.signs = (1 - 2 * (torch.arange(I, device="cuda") % 2)).to(BF)
 
     def _columns(self, t, k):
@@ -77,16 +78,17 @@ class GlrLayer:
 
     def _live(self, X, lens):
         """X without what a padded batch may hold behind its sequences' ends and the norm cannot carry.  Norm and products run over all rows; the gates'
-        gradients are zero there, which a product takes away only if what it is multiplied with is finite.  So values that are not finite, or whose
-        squares may not be, become +1 and -1 in turn (rows of which have a variance, for eps = 0: then all padded ones do)."""
+        gradients are zero there, which a product takes away only if what it is multiplied with is finite.  So there values are held within 2^50 and NaN
+        becomes zero; with eps = 0, where a row also has to have a variance, padded rows become +1, -1, +1, ..."""
         T, B, I = self.T, self.B, self.I
         if self.X_live is None:
             self.X_live = torch.empty_like(self.Xn)
-        x = X.view(T, B, I)
-        stays = (torch.arange(T, device=X.device)[:, None] < lens).view(T, B, 1)
+        x, out = X.view(T, B, I), self.X_live.view(T, B, I)
+        rest = self.signs
         if self.eps > 0:
-            stays = stays | (x.abs() <= 2.0 ** 50)
-        return torch.where(stays, x, self.signs, out=self.X_live.view(T, B, I)).view(T * B, I)
+            rest = torch.clamp(x, -2.0 ** 50, 2.0 ** 50, out=out).nan_to_num_(0.0)
+        torch.where((self.times < lens).view(T, B, 1), x, rest, out=out)
+        return self.X_live
 
     def forward(self, X, alpha, h0=None, lens=None):
         """X: bf16 [T*B][I] (with in_pat compact), kept until backward().  Returns Y [T*B][H], compact: the kept units' columns are valid.
