@@ -768,7 +768,9 @@ typedef struct ard_adamw_tensor {
  * (t low, t high, element / 4, 1 + number of the tensor):
  * word element % 4, its low half for m, its high half for r.  A root that is not zero is held as no less than the
  * smallest 8-bit value; a block whose largest value is below 2^-110 as zeros.  All arithmetic is fp32 on the values
- * before rounding.  States begin as zeros (bytes and scales).
+ * before rounding.  Where v passes fp32's range it is infinite and its parameter only decays from then on; in 8 bits its
+ * root is held as 2^126, and with it the block's other roots that are not zero pass the range as well.  A NaN, or an
+ * infinite m, in 8 bits makes its whole block NaN.  States begin as zeros (bytes and scales).
  * Tensors must not overlap one another.  Any alignment (16-byte aligned tensors without gaps between rows are read and
  * written in 16-byte pieces).  Errors: ARD_ERR_INVALID_ARG (NULL, negative size, dtype, state_bits, beta outside [0, 1), lr, eps or
  * weight_decay negative or not finite, eps above 0 and below 2^-126), ARD_ERR_SHAPE (leading dimension below cols, more than 2^34 elements).

@@ -159,13 +159,13 @@ __device__ __forceinline__ float2 aw_fma(float2 a, float2 b, float2 c) { return 
 __device__ __forceinline__ float2 aw_both(float x) { return make_float2(x, x); }
 // Roots to the last bit: one of Heron's steps with its residual in one rounding (Markstein, IBM J. Res. Dev. 34, 1990), from the instruction's estimate of
 // 1 / sqrt(x).  No branches (they keep a thread's quads from running beside one another: 145 us for 36 M elements in place of 133): of x below 2^-126 the
-// result, below 2^-63, is not accurate, but is 0 only of 0; infinity gives NaN.
+// result, below 2^-63, is not accurate, but is 0 only of 0.  (Of infinity the steps give NaN: it, and NaN, stay what they are.)
 __device__ __forceinline__ float2 aw_roots(float2 x) {
   float2 y;
   asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y.x) : "f"(fmaxf(x.x, 1.1754943508222875e-38f)));
   asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y.y) : "f"(fmaxf(x.y, 1.1754943508222875e-38f)));
-  const float2 q = x * y;
-  return aw_fma(aw_fma(q * aw_both(-1.f), q, x), y * aw_both(0.5f), q);
+  const float2 q = x * y, r = aw_fma(aw_fma(q * aw_both(-1.f), q, x), y * aw_both(0.5f), q);
+  return make_float2(x.x < INFINITY ? r.x : x.x, x.y < INFINITY ? r.y : x.y);
 }
 
 // The 8-bit floats of a block of 128 values, four in each lane, and its scale (the same in all lanes).  ROOT: of values >= 0, from the words'
@@ -177,10 +177,14 @@ __device__ __forceinline__ float2 aw_roots(float2 x) {
 template <bool ROOT>
 __device__ __forceinline__ uint32_t aw_encode(const float2 (&v)[2], const uint32_t (&words)[4], float& scale) {
   float most = fmaxf(fmaxf(fabsf(v[0].x), fabsf(v[0].y)), fmaxf(fabsf(v[1].x), fabsf(v[1].y)));
-  // a value that is not a number, which the maximum drops, spoils its block, as it spoils states in 32 bits
-  const float2 sum = v[0] + v[1], any = sum * aw_both(0.f);
-  if (any.x + any.y != 0.f) most = __int_as_float(0x7FC00000);  // (or an infinity: its block is spoilt by what 0 times it gives)
-  const float big = __uint_as_float(__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(most)));  // of values >= 0, in their order
+  // a value that is not a number, which the maximum drops, spoils its block, as it spoils states in 32 bits; so does an infinite m
+  const float2 sum = v[0] + v[1], any = ROOT ? sum : sum * aw_both(0.f);
+  if (!(any.x + any.y <= INFINITY)) most = __int_as_float(0x7FC00000);
+  uint32_t bits = __reduce_max_sync(0xFFFFFFFFu, __float_as_uint(most));  // of values >= 0, in their order
+  // An infinite root (v beyond fp32) counts as 2^126, which no finite root reaches and whose square is infinite again: with a scale of infinity the block's
+  // zeros would be lost.
+  if (ROOT && bits == 0x7F800000u) bits = 0x7E800000u;
+  const float big = __uint_as_float(bits);
   const bool none = big < AW_TINY;
   const float near = aw_inverse(big), inv = none ? 0.f : E4M3_MAX * fmaf(near, fmaf(-big, near, 1.f), near), least = none ? 0.f : 0.001953125f;
   scale = none ? 0.f : big * (1.f / E4M3_MAX);
