@@ -75,3 +75,23 @@ def test_a_second_moment_beyond_fp32_beside_roots_that_are_zero():
     m, v = 1 - B1, 1 - B2
     want = 1 - LR * (m / (1 - B1 ** 4)) / (np.sqrt(v / (1 - B2 ** 4)) + 1e-8)
     assert abs(float(t["p"][7]) - want) <= 2 * U + 40 * U * abs(1 - want)
+
+
+@pytest.mark.parametrize("eps", [0.0, 1e-30])
+def test_second_moments_below_the_normal_range(eps):
+    """Gradients of 1e-21 to 1e-17: v is subnormal in fp32, its root is not."""
+    blocks = 4000
+    rng = np.random.default_rng(2)
+    values = (np.exp(rng.uniform(np.log(2e-21), np.log(1e-17), size=blocks)) * rng.choice([-1, 1], size=blocks)).astype(F)
+    g = np.zeros((blocks, 128), F)
+    g[:, 9] = values
+    t = _tensor(torch.from_numpy(g.reshape(-1)))
+    _step(t, 1, eps=eps)
+    v = (F(1.0 - B2) * values).astype(F) * values
+    assert (v > 0).all() and (v < 2.0 ** -126).mean() > 0.5
+    want = np.sqrt(v.astype(np.float64))
+    got = t["v_scale"].cpu().numpy().astype(np.float64) / float(INVERSE)
+    assert (np.abs(got - want) <= 4 * U * want).all()
+    m, lift1, lift2 = (1 - B1) * values.astype(np.float64), 1 / (1 - B1), 1 / (1 - B2)
+    p = -LR * m * lift1 / (want * np.sqrt(lift2) + eps)
+    assert (np.abs(t["p"].cpu().numpy().reshape(-1, 128)[:, 9] - p) <= 40 * U * np.abs(p)).all()
