@@ -179,7 +179,7 @@ template <bool ROOT>
 __device__ __forceinline__ uint32_t aw_encode(const float2 (&v)[2], const uint32_t (&words)[4], float& scale) {
   float most = fmaxf(fmaxf(fabsf(v[0].x), fabsf(v[0].y)), fmaxf(fabsf(v[1].x), fabsf(v[1].y)));
   // a value that is not a number, which the maximum drops, spoils its block, as it spoils states in 32 bits; so does an infinite m
-  const float2 sum = v[0] + v[1], any = ROOT ? sum : sum * aw_both(0.f);
+  const float2 any = ROOT ? v[0] + v[1] : aw_fma(v[0], aw_both(0.f), v[1] * aw_both(0.f));
   if (!(any.x + any.y <= INFINITY)) most = __int_as_float(0x7FC00000);
   uint32_t bits = __reduce_max_sync(0xFFFFFFFFu, __float_as_uint(most));  // of values >= 0, in their order
   // An infinite root (v beyond fp32) counts as 2^126, which no finite root reaches and whose square is infinite again: with a scale of infinity the block's
@@ -187,7 +187,9 @@ __device__ __forceinline__ uint32_t aw_encode(const float2 (&v)[2], const uint32
   if (ROOT && bits == 0x7F800000u) bits = 0x7E800000u;
   const float big = __uint_as_float(bits);
   const bool none = big < AW_TINY;
-  const float near = aw_inverse(big), inv = none ? 0.f : E4M3_MAX * fmaf(near, fmaf(-big, near, 1.f), near), least = none ? 0.f : 0.001953125f;
+  // (of m's largest value / 256: above 2^126 its own reciprocal is below the normal range, which the instruction takes for zero)
+  const float part = ROOT ? big : big * 0.00390625f, near = aw_inverse(part);
+  const float inv = none ? 0.f : E4M3_MAX * (ROOT ? 1.f : 0.00390625f) * fmaf(near, fmaf(-part, near, 1.f), near), least = none ? 0.f : 0.001953125f;
   scale = none ? 0.f : big * (1.f / E4M3_MAX);
   uint32_t codes = 0;
 #pragma unroll

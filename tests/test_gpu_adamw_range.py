@@ -95,3 +95,19 @@ def test_second_moments_below_the_normal_range(eps):
     m, lift1, lift2 = (1 - B1) * values.astype(np.float64), 1 / (1 - B1), 1 / (1 - B2)
     p = -LR * m * lift1 / (want * np.sqrt(lift2) + eps)
     assert (np.abs(t["p"].cpu().numpy().reshape(-1, 128)[:, 9] - p) <= 40 * U * np.abs(p)).all()
+
+
+@pytest.mark.parametrize("big", [8.4e37, 8.6e37, 3.3e38])
+def test_first_moments_up_to_fp32s_end(big):
+    """m = g; without a rate the parameters stay."""
+    g = torch.zeros(1024)
+    g[::128] = torch.tensor([1, -1, 1, -1, 1, -1, 1, -1.0]) * big
+    g[1::128] = big / 7
+    t = _tensor(g, 0.0, 1.0)
+    _step(t, 1, lr=0.0, b1=0.0)
+    codes = t["m"].view(torch.float8_e4m3fn).float()
+    assert bool((codes[::128].abs() == 448).all()) and bool((codes[::128].sign() == t["g"][::128].sign()).all())
+    assert bool((codes[1::128] == 64).all())      # 448 / 7: on the grid, and the division by 7 is off by less than a random word's half step
+    want = np.full(8, F(big)) * INVERSE
+    assert (np.abs(t["m_scale"].cpu().numpy() - want) <= np.spacing(want)).all()
+    assert bool((t["p"] == 1).all())
