@@ -518,7 +518,7 @@ __device__ __forceinline__ double gn_squares(const float (&g)[8]) {
 // Every CTA leaves the sum of its squares; the last one of the last launch adds them in the order of the CTAs.
 template <int CAP>
 __global__ void __launch_bounds__(AW_THREADS) grad_norm_kernel(const __grid_constant__ AwTable<CAP> table, double* partial, int before,
-                                                               int last_launch, unsigned int* count, float max_norm, float* out) {
+                                                               int last_launch, unsigned int* count, double max_norm, float* out) {
   __shared__ double red[AW_THREADS / 32];
   __shared__ int s_last;
   pdl_launch_dependents();
@@ -600,7 +600,7 @@ __global__ void __launch_bounds__(AW_THREADS) grad_norm_kernel(const __grid_cons
     const double norm = sqrt(x);
     const bool fine = norm <= 3.4028234663852886e38;
     out[0] = (float)norm;
-    out[1] = !fine ? __int_as_float(0x7FC00000) : max_norm > 0.f ? (float)fmin(1.0, (double)max_norm / (norm + 1e-6)) : 1.f;
+    out[1] = !fine ? __int_as_float(0x7FC00000) : max_norm > 0.0 ? (float)fmin(1.0, max_norm / (norm + 1e-6)) : 1.f;
   }
 }
 
@@ -723,7 +723,7 @@ ard_status launch_grad_norm(ard_ctx* ctx, const ard_adamw_tensor* tensors, int n
     if (grid < 1) grid = 1;  // no gradients at all: the norm is zero
     if (before + grid > most) return ARD_ERR_NOMEM;
     ARD_CUDA_OK(ard_launch(ctx, grad_norm_kernel<CAP>, dim3(grid), dim3(AW_THREADS), 0, s, (T)table, (double*)ctx->d_sk_ws, before,
-                           left == 0 ? 1 : 0, (unsigned int*)ctx->d_sk_cnt, (float)max_norm, out));
+                           left == 0 ? 1 : 0, (unsigned int*)ctx->d_sk_cnt, max_norm, out));
     before += grid;
     ctx->launches++;
     ARD_CUDA_OK(cudaGetLastError());

@@ -111,3 +111,12 @@ def test_first_moments_up_to_fp32s_end(big):
     want = np.full(8, F(big)) * INVERSE
     assert (np.abs(t["m_scale"].cpu().numpy() - want) <= np.spacing(want)).all()
     assert bool((t["p"] == 1).all())
+
+
+@pytest.mark.parametrize("most", [1e-45, 7e-46, 1e-60, 5e-324])
+def test_bounds_that_fp32_does_not_hold(most):
+    g = torch.full((1000,), 1e-3, device="cuda")
+    out = torch.zeros(2, device="cuda")
+    ard.ard_grad_norm(_h(), ard.adamw_tensors([{"rows": 1, "cols": 1000, "p": None, "g": g, "m": None, "v": None}]), 1, most, out)
+    norm, factor = OA.norm([g.double().cpu().numpy()], most)
+    assert abs(float(out[0]) - norm) <= 2 * U * norm and abs(float(out[1]) - factor) <= 2.0 ** -149
