@@ -12,7 +12,7 @@ namespace {
 struct LnShape {
   const int32_t* hdr;  // nullptr: all N columns
   int rows, N;
-  __host__ __device__ __forceinline__ int pitch() const { return (N + 3) & ~3; }  // of a row of partial sums: written in pieces of 16 bytes
+  __host__ __device__ __forceinline__ long long pitch() const { return ((long long)N + 3) & ~3ll; }  // of a row of partial sums: written in pieces of 16 bytes
 };
 struct LnCols {
   int n, dp, b0;  // compact columns, and the unit of column j: b0 + j * dp
@@ -55,21 +55,22 @@ __global__ void __launch_bounds__(LN_ANY_THREADS) ln_fwd_any_kernel(LnShape sh, 
   pdl_launch_dependents();
   pdl_wait_prior_grids();
   const LnCols c = ln_cols(sh);
+  const uint32_t n = (uint32_t)c.n;  // columns are counted without a sign: the one behind the last trip's may lie past 2^31
   const float inv_n = 1.f / (float)c.n;
   for (int r = blockIdx.x; r < sh.rows; r += gridDim.x) {
     const T* x = X + (size_t)r * ldx;
     T* y = Y + (size_t)r * ldy;
     float s = 0.f;
-    for (int j = threadIdx.x; j < c.n; j += LN_ANY_THREADS) s += ln_get(x, j);
+    for (uint32_t j = threadIdx.x; j < n; j += LN_ANY_THREADS) s += ln_get(x, j);
     const float mu = ln_block_sum(s, red) * inv_n;
     s = 0.f;
-    for (int j = threadIdx.x; j < c.n; j += LN_ANY_THREADS) {
+    for (uint32_t j = threadIdx.x; j < n; j += LN_ANY_THREADS) {
       const float d = ln_get(x, j) - mu;
       s = fmaf(d, d, s);
     }
     const float rs = ln_rsqrt(fmaf(ln_block_sum(s, red), inv_n, eps));
-    for (int j = threadIdx.x; j < c.n; j += LN_ANY_THREADS) {
-      const int u = c.b0 + j * c.dp;
+    for (uint32_t j = threadIdx.x; j < n; j += LN_ANY_THREADS) {
+      const uint32_t u = c.b0 + j * c.dp;
       ln_put(y, j, fmaf((ln_get(x, j) - mu) * rs, weight ? weight[u] : 1.f, bias ? bias[u] : 0.f));
     }
     if (threadIdx.x == 0) {
@@ -83,6 +84,7 @@ template <typename T>
 __device__ __forceinline__ void ln_dx_any(const LnShape& sh, const LnCols& c, const T* dY, int lddy, const T* X, int ldx, const float* weight,
                                           const float* mean, const float* rstd, T* dX, int lddx, int first, int blocks) {
   __shared__ float red[2][LN_ANY_THREADS / 32];
+  const uint32_t n = (uint32_t)c.n;
   const float inv_n = 1.f / (float)c.n;
   for (int r = first; r < sh.rows; r += blocks) {
     const T* x = X + (size_t)r * ldx;
@@ -90,14 +92,14 @@ __device__ __forceinline__ void ln_dx_any(const LnShape& sh, const LnCols& c, co
     T* dx = dX + (size_t)r * lddx;
     const float mu = mean[r], rs = rstd[r];
     float s1 = 0.f, s2 = 0.f;
-    for (int j = threadIdx.x; j < c.n; j += LN_ANY_THREADS) {
+    for (uint32_t j = threadIdx.x; j < n; j += LN_ANY_THREADS) {
       const float e = ln_get(dy, j) * (weight ? weight[c.b0 + j * c.dp] : 1.f);
       s1 += e;
       s2 = fmaf(e, (ln_get(x, j) - mu) * rs, s2);
     }
     s1 = ln_block_sum(s1, red[0]) * inv_n;
     s2 = ln_block_sum(s2, red[1]) * inv_n;
-    for (int j = threadIdx.x; j < c.n; j += LN_ANY_THREADS) {
+    for (uint32_t j = threadIdx.x; j < n; j += LN_ANY_THREADS) {
       const float e = ln_get(dy, j) * (weight ? weight[c.b0 + j * c.dp] : 1.f);
       ln_put(dx, j, rs * (e - s1 - (ln_get(x, j) - mu) * rs * s2));
     }
@@ -1059,9 +1061,10 @@ ard_status ln_bwd(ard_ctx* ctx, const LnShape& sh, const T* dY, int lddy, const 
   }
   if (!done) {
     const int room = 8 * ctx->sm_count, dx_blocks = !dX ? 0 : sh.rows < room ? sh.rows : room;
-    int gx = (sh.N + 31) / 32, per = 0;
-    if (gx > 4096) gx = 4096;
+    int gx = 1, per = 0;
     if (sums) {
+      gx = (sh.N + 31) / 32;
+      if (gx > 4096) gx = 4096;
       slices = (sh.rows + 63) / 64;
       if (slices > fit) slices = fit;
       if (slices > 1024) slices = 1024;
