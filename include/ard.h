@@ -719,7 +719,8 @@ ard_status ard_layer_norm_bwd(ard_ctx* ctx, const ard_pattern* pat, ard_dtype dt
  * Decoding is T = 1 with hT = h0.  A gate of -infinity (f = 0) starts anew: a finite past does not enter, in either call.
  * Z, Y of element type `dtype`, any alignment (columns on a grid of two elements are read in pairs); gates, states and
  * sums are fp32.  Y must not overlap an input.
- * Errors: as ard_layer_norm_fwd (H and T in the place of N and rows).  Asynchronous. */
+ * Errors: as ard_layer_norm_fwd (H and T in the place of N and rows; ARD_ERR_UNSUPPORTED also where the
+ * sequences' blocks of at least 16 units are more than 2^31 - 1).  Asynchronous. */
 #define ARD_GLR_CHUNK 64
 ard_status ard_glr_forward(ard_ctx* ctx, const ard_pattern* pat, ard_dtype dtype, int T, int B, int H, float alpha,
                            const void* Zf, const void* Zg, const void* Zo, int ldz, const int32_t* lens, const float* h0,

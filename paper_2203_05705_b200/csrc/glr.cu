@@ -180,10 +180,13 @@ struct GlrSpan {
       dp = a.hdr[HDR_DP];
       b0 = a.hdr[HDR_B] - 1;
     }
-    groups = (n + channels - 1) / channels;
-    units = groups * a.B;
+    groups = (int)(((long long)n + channels - 1) / channels);
+    units = groups * a.B;  // (at most 2^31 - 1: the host asks)
     rounds = (a.T + steps - 1) / steps;
   }
+  // The unit of a CTA (a cluster) after this one: so many further, or behind the last, whose number the sum may not pass.
+  __device__ __forceinline__ int after(int unit, int clusters) const { return units - unit > clusters ? unit + clusters : units; }
+  __device__ __forceinline__ bool inside(int unit, int channels) const { return n - unit % groups * channels >= channels; }
   __device__ __forceinline__ int len(const GlrArgs& a, int b) const { return a.lens ? min(max(a.lens[b], 0), a.T) : a.T; }
 };
 // A thread's place in a unit: VEC channels of one sequence, SPT consecutive steps of every slab.  W threads stand side by side over the unit's channels
@@ -248,7 +251,7 @@ struct GlrFeed<T, VEC, M, W, WT, SPT, true> {
     }
     if (++round == sp.rounds) {
       round = 0;
-      unit += clusters;
+      unit = sp.after(unit, clusters);
     }
   }
   __device__ __forceinline__ void wait(int* status) {
@@ -390,7 +393,7 @@ __global__ void __launch_bounds__(W* WT, W* WT < 256 ? 1 : SPT < 8 && SPT != 4 ?
       for (int k = 0; k < in.SLOTS; ++k) in.ask(a, sp, tiles, CL, rank, clusters, false);
   const V alpha = V::all(a.alpha);
   int mail = 0;
-  for (int unit = cluster; unit < sp.units; unit += clusters) {
+  for (int unit = cluster; unit < sp.units; unit = sp.after(unit, clusters)) {
     const GlrPlace<VEC, W, WT> at(a, sp, unit);
     const size_t step_y = (size_t)a.B * a.ldy;
     T* y = (T*)a.Y + (size_t)at.b * a.ldy + at.j;
@@ -406,7 +409,7 @@ __global__ void __launch_bounds__(W* WT, W* WT < 256 ? 1 : SPT < 8 && SPT != 4 ?
     V first;  // the state that enters the unit
 #pragma unroll
     for (int v = 0; v < VEC; ++v) first.v[v] = a.h0 && v < at.valid ? a.h0[at.of(a, sp, v)] : 0.f;
-    const bool inside = (unit % sp.groups + 1) * (W * VEC) <= sp.n;
+    const bool inside = sp.inside(unit, W * VEC);
     V c = first;
     // FULL: all steps of the slab are a sequence's, all channels of the unit exist; nothing is asked per step
     auto slab = [&](auto full, int it) {
@@ -493,7 +496,7 @@ __global__ void __launch_bounds__(W* WT, W* WT < 256 ? 1 : SPT < 8 && SPT != 4 ?
       for (int k = 0; k < in.SLOTS; ++k) in.ask(a, sp, tiles, CL, rank, clusters, true);
   const V alpha = V::all(a.alpha), minus = V::all(-1.f);
   int mail = 0;
-  for (int unit = cluster; unit < sp.units; unit += clusters) {
+  for (int unit = cluster; unit < sp.units; unit = sp.after(unit, clusters)) {
     const GlrPlace<VEC, W, WT> at(a, sp, unit);
     const size_t step_d = (size_t)a.B * a.lddz, off_d = (size_t)at.b * a.lddz + at.j;
     T* dzf = (T*)a.dZf + off_d;
@@ -514,7 +517,7 @@ __global__ void __launch_bounds__(W* WT, W* WT < 256 ? 1 : SPT < 8 && SPT != 4 ?
     V first;  // what arrives behind the unit's last step
 #pragma unroll
     for (int v = 0; v < VEC; ++v) first.v[v] = a.h0 && v < at.valid ? a.h0[at.of(a, sp, v)] : 0.f;
-    const bool inside = (unit % sp.groups + 1) * (W * VEC) <= sp.n;
+    const bool inside = sp.inside(unit, W * VEC);
     V q = first;
     auto slab = [&](auto full, int it) {
       constexpr bool FULL = decltype(full)::value;
@@ -623,7 +626,7 @@ inline bool glr_pairs(std::initializer_list<const void*> ps, std::initializer_li
 template <typename F>
 constexpr int glr_ring() { return F::SLOTS * F::SLOT; }
 
-inline long long glr_units(const GlrArgs& a, int channels) { return (long long)((a.H + channels - 1) / channels) * a.B; }
+inline long long glr_units(const GlrArgs& a, int channels) { return ((long long)a.H + channels - 1) / channels * a.B; }
 
 // With bulk copies the grid is what the device holds at once (per_sm CTAs an SM) and a CTA goes from unit to unit, its copies ahead of it; without, a
 // CTA (a cluster) per unit.
