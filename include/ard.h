@@ -684,12 +684,12 @@ ard_status ard_lstm_gates_bwd(ard_ctx* ctx, const ard_pattern* pat, ard_dtype dz
  * ard_layer_fwd leaves activations (column j = kept unit j, leading dimensions >= N so that any pattern fits), the
  * statistics are those of the n kept columns, weight and bias are full width and read at the kept units.  Columns >= n
  * are neither read as values nor written.
- * X, Y of element type `dtype`, any alignment (fastest with 16-byte aligned pointers and rows); weight, bias fp32 [N],
+ * X, Y of element type `dtype`, from any whole element on (fastest with 16-byte aligned pointers and rows); weight, bias fp32 [N],
  * NULL: 1 and 0; mean, rstd fp32 [rows], what the backward call needs, may be NULL when there is none.  Statistics and
  * sums are fp32.  Y must not overlap X.
  * Errors: ARD_ERR_INVALID_ARG (NULL, negative size, dtype, eps negative or not finite, tile pattern, another context's
- * pattern), ARD_ERR_SHAPE (N differs from the pattern's, leading dimension below N), ARD_ERR_UNSUPPORTED (more than
- * 2^30 rows; backward: N above 4 million).  Asynchronous. */
+ * pattern), ARD_ERR_SHAPE (N differs from the pattern's, leading dimension below N), ARD_ERR_ALIGNMENT (a pointer inside
+ * an element), ARD_ERR_UNSUPPORTED (more than 2^30 rows; backward with dweight or dbias: N above 4 million).  Asynchronous. */
 ard_status ard_layer_norm_fwd(ard_ctx* ctx, const ard_pattern* pat, ard_dtype dtype, int rows, int N, float eps, const void* X,
                               int ldx, const float* weight, const float* bias, void* Y, int ldy, float* mean, float* rstd,
                               void* cuda_stream);
@@ -717,7 +717,7 @@ ard_status ard_layer_norm_bwd(ard_ctx* ctx, const ard_pattern* pat, ard_dtype dt
  *   hT    fp32 [B][H] full width, the state after the last step, or NULL; entries of dropped units are left.  May be h0.
  *   S     fp32 [ceil(T / ARD_GLR_CHUNK)][B][H], what the backward call starts from, or NULL when there is none.
  * Decoding is T = 1 with hT = h0.  A gate of -infinity (f = 0) starts anew: a finite past does not enter, in either call.
- * Z, Y of element type `dtype`, any alignment (columns on a grid of two elements are read in pairs); gates, states and
+ * Z, Y of element type `dtype`, from any whole element on (columns on a grid of two elements are read in pairs); gates, states and
  * sums are fp32.  Y must not overlap an input.
  * Errors: as ard_layer_norm_fwd (H and T in the place of N and rows; ARD_ERR_UNSUPPORTED also where the
  * sequences' blocks of at least 16 units are more than 2^31 - 1).  Asynchronous. */
@@ -772,9 +772,10 @@ typedef struct ard_adamw_tensor {
  * before rounding.  Where v passes fp32's range it is infinite and its parameter only decays from then on; in 8 bits its
  * root is held as 2^126, and with it the block's other roots that are not zero pass the range as well.  A NaN, or an
  * infinite m, in 8 bits makes its whole block NaN.  States begin as zeros (bytes and scales).
- * Tensors must not overlap one another.  Any alignment (16-byte aligned tensors without gaps between rows are read and
+ * Tensors must not overlap one another and begin at any whole element (16-byte aligned tensors without gaps between rows are read and
  * written in 16-byte pieces).  Errors: ARD_ERR_INVALID_ARG (NULL, negative size, dtype, state_bits, beta outside [0, 1), lr, eps or
- * weight_decay negative or not finite, eps above 0 and below 2^-126), ARD_ERR_SHAPE (leading dimension below cols, more than 2^34 elements).
+ * weight_decay negative or not finite, eps above 0 and below 2^-126), ARD_ERR_SHAPE (leading dimension below cols, more than 2^34 elements),
+ * ARD_ERR_ALIGNMENT (a pointer inside an element).
  * Nothing is launched unless all tensors are valid.  Asynchronous. */
 ard_status ard_adamw_step(ard_ctx* ctx, const ard_adamw_tensor* tensors, int n_tensors, double lr, double beta1, double beta2,
                           double eps, int state_bits, uint64_t seed, uint64_t step, const uint64_t* step_counter,

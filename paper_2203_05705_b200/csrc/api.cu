@@ -1700,6 +1700,14 @@ ard_status ard_rows_products(ard_ctx* ctx, const ard_rows* rows, ard_dtype dW_dt
   return ARD_OK;
 }
 
+// Whether one of the pointers (or NULL) is no multiple of `bytes`: an element of that size cannot lie there.
+static bool off_elements(size_t bytes, std::initializer_list<const void*> ps) {
+  for (const void* p : ps)
+    if (reinterpret_cast<uintptr_t>(p) % bytes) return true;
+  return false;
+}
+static size_t element_bytes(int dtype) { return dtype == ARD_F32 ? 4 : 2; }
+
 // A row pattern over N units of this context, or none.
 static ard_status check_units(ard_ctx* ctx, const ard_pattern* pat, int N) {
   if (!pat) return ARD_OK;
@@ -1721,6 +1729,7 @@ ard_status ard_layer_norm_fwd(ard_ctx* ctx, const ard_pattern* pat, ard_dtype dt
   if (st != ARD_OK) return st;
   if (!X || !Y || X == Y || (mean && mean == rstd) || !(eps >= 0.f) || !(eps < INFINITY)) return ARD_ERR_INVALID_ARG;
   if (ldx < N || ldy < N) return ARD_ERR_SHAPE;
+  if (off_elements(element_bytes(dtype), {X, Y}) || off_elements(4, {weight, bias, mean, rstd})) return ARD_ERR_ALIGNMENT;
   DeviceGuard guard(ctx->device);
   return launch_layer_norm_fwd(ctx, pat ? pat->d_hdr : nullptr, dtype, rows, N, eps, X, ldx, weight, bias, Y, ldy, mean, rstd,
                                (cudaStream_t)cuda_stream);
@@ -1733,6 +1742,7 @@ ard_status ard_layer_norm_bwd(ard_ctx* ctx, const ard_pattern* pat, ard_dtype dt
   if (st != ARD_OK) return st;
   if (!dY || !X || !mean || !rstd || dX == dY || dX == X || (dweight && dweight == dbias)) return ARD_ERR_INVALID_ARG;
   if (ldx < N || lddy < N || (dX && lddx < N)) return ARD_ERR_SHAPE;
+  if (off_elements(element_bytes(dtype), {dY, X, dX}) || off_elements(4, {weight, mean, rstd, dweight, dbias})) return ARD_ERR_ALIGNMENT;
   DeviceGuard guard(ctx->device);
   return launch_layer_norm_bwd(ctx, pat ? pat->d_hdr : nullptr, dtype, rows, N, dY, lddy, X, ldx, weight, mean, rstd, dX, lddx, dweight,
                                dbias, zero_fill_dropped ? 1 : 0, (cudaStream_t)cuda_stream);
@@ -1754,6 +1764,7 @@ ard_status ard_glr_forward(ard_ctx* ctx, const ard_pattern* pat, ard_dtype dtype
   if (st != ARD_OK) return st;
   if (!Y || Y == Zf || Y == Zg || Y == Zo) return ARD_ERR_INVALID_ARG;
   if (ldy < H) return ARD_ERR_SHAPE;
+  if (off_elements(element_bytes(dtype), {Zf, Zg, Zo, Y}) || off_elements(4, {lens, h0, hT, S})) return ARD_ERR_ALIGNMENT;
   DeviceGuard guard(ctx->device);
   return launch_glr_forward(ctx, pat ? pat->d_hdr : nullptr, dtype, T, B, H, alpha, Zf, Zg, Zo, ldz, lens, h0, Y, ldy, hT, S,
                             (cudaStream_t)cuda_stream);
@@ -1770,6 +1781,7 @@ ard_status ard_glr_backward(ard_ctx* ctx, const ard_pattern* pat, ard_dtype dtyp
   for (const void* out : {dZf, dZg, dZo})
     for (const void* in : {Zf, Zg, Zo, dY})
       if (out && out == in) return ARD_ERR_INVALID_ARG;
+  if (off_elements(element_bytes(dtype), {Zf, Zg, Zo, dY, dZf, dZg, dZo}) || off_elements(4, {lens, S, dhT, dh0})) return ARD_ERR_ALIGNMENT;
   DeviceGuard guard(ctx->device);
   return launch_glr_backward(ctx, pat ? pat->d_hdr : nullptr, dtype, T, B, H, alpha, Zf, Zg, Zo, ldz, lens, S, dY, lddy, dhT, dZf, dZg, dZo,
                              lddz, dh0, (cudaStream_t)cuda_stream);
@@ -1785,11 +1797,15 @@ static ard_status adamw_check(const ard_adamw_tensor* tensors, int n_tensors, in
     if (!t.g || (t.g_dtype != ARD_F32 && t.g_dtype != ARD_BF16)) return ARD_ERR_INVALID_ARG;
     if (t.rows > (1ll << 34) || t.cols > (1ll << 34) || t.rows > (1ll << 34) / t.cols) return ARD_ERR_SHAPE;
     if (t.rows > 1 && (t.ldg < t.cols || t.ldg > (1ll << 34))) return ARD_ERR_SHAPE;
+    if (off_elements(element_bytes(t.g_dtype), {t.g})) return ARD_ERR_ALIGNMENT;
     if (state_bits == 0) continue;
     if (!t.p || !t.m || !t.v || !(t.weight_decay >= 0.0) || !(t.weight_decay < INFINITY)) return ARD_ERR_INVALID_ARG;
     if (state_bits == 8 && (!t.m_scale || !t.v_scale)) return ARD_ERR_INVALID_ARG;
     if (t.rows > 1 && (t.ldp < t.cols || t.ldp > (1ll << 34))) return ARD_ERR_SHAPE;
     if (t.rows > 1 && t.w && (t.ldw < t.cols || t.ldw > (1ll << 34))) return ARD_ERR_SHAPE;
+    if (off_elements(4, {t.p}) || off_elements(2, {t.w}) || (state_bits == 32 && off_elements(4, {t.m, t.v})) ||
+        (state_bits == 8 && off_elements(4, {t.m_scale, t.v_scale})))
+      return ARD_ERR_ALIGNMENT;
   }
   return ARD_OK;
 }
@@ -1801,6 +1817,7 @@ ard_status ard_adamw_step(ard_ctx* ctx, const ard_adamw_tensor* tensors, int n_t
   if (!(lr >= 0.0) || !(lr < INFINITY) || !(eps >= 0.0) || !(eps < INFINITY)) return ARD_ERR_INVALID_ARG;
   if (eps > 0.0 && eps < 1.1754943508222875e-38) return ARD_ERR_INVALID_ARG;  // 2^-126: what the kernels' quotients take for zero
   if (!(beta1 >= 0.0) || !(beta1 < 1.0) || !(beta2 >= 0.0) || !(beta2 < 1.0)) return ARD_ERR_INVALID_ARG;
+  if (off_elements(8, {step_counter}) || off_elements(4, {lr_factor, grad_factor})) return ARD_ERR_ALIGNMENT;
   const ard_status st = adamw_check(tensors, n_tensors, state_bits);
   if (st != ARD_OK) return st;
   DeviceGuard guard(ctx->device);
@@ -1810,6 +1827,7 @@ ard_status ard_adamw_step(ard_ctx* ctx, const ard_adamw_tensor* tensors, int n_t
 
 ard_status ard_grad_norm(ard_ctx* ctx, const ard_adamw_tensor* tensors, int n_tensors, double max_norm, float* out, void* cuda_stream) {
   if (!ctx || !out || max_norm != max_norm) return ARD_ERR_INVALID_ARG;
+  if (off_elements(4, {out})) return ARD_ERR_ALIGNMENT;
   const ard_status st = adamw_check(tensors, n_tensors, 0);
   if (st != ARD_OK) return st;
   DeviceGuard guard(ctx->device);
