@@ -774,7 +774,7 @@ typedef struct ard_adamw_tensor {
  * infinite m, in 8 bits makes its whole block NaN.  States begin as zeros (bytes and scales).
  * Tensors must not overlap one another and begin at any whole element (16-byte aligned tensors without gaps between rows are read and
  * written in 16-byte pieces).  Errors: ARD_ERR_INVALID_ARG (NULL, negative size, dtype, state_bits, beta outside [0, 1), lr, eps or
- * weight_decay negative or not finite, eps above 0 and below 2^-126), ARD_ERR_SHAPE (leading dimension below cols, more than 2^34 elements),
+ * weight_decay negative or not finite in fp32, eps above 0 and below 2^-126), ARD_ERR_SHAPE (leading dimension below cols, more than 2^34 elements),
  * ARD_ERR_ALIGNMENT (a pointer inside an element).
  * Nothing is launched unless all tensors are valid.  Asynchronous. */
 ard_status ard_adamw_step(ard_ctx* ctx, const ard_adamw_tensor* tensors, int n_tensors, double lr, double beta1, double beta2,

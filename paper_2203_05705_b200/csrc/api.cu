@@ -1799,7 +1799,7 @@ static ard_status adamw_check(const ard_adamw_tensor* tensors, int n_tensors, in
     if (t.rows > 1 && (t.ldg < t.cols || t.ldg > (1ll << 34))) return ARD_ERR_SHAPE;
     if (off_elements(element_bytes(t.g_dtype), {t.g})) return ARD_ERR_ALIGNMENT;
     if (state_bits == 0) continue;
-    if (!t.p || !t.m || !t.v || !(t.weight_decay >= 0.0) || !(t.weight_decay < INFINITY)) return ARD_ERR_INVALID_ARG;
+    if (!t.p || !t.m || !t.v || !(t.weight_decay >= 0.0) || !((float)t.weight_decay < INFINITY)) return ARD_ERR_INVALID_ARG;
     if (state_bits == 8 && (!t.m_scale || !t.v_scale)) return ARD_ERR_INVALID_ARG;
     if (t.rows > 1 && (t.ldp < t.cols || t.ldp > (1ll << 34))) return ARD_ERR_SHAPE;
     if (t.rows > 1 && t.w && (t.ldw < t.cols || t.ldw > (1ll << 34))) return ARD_ERR_SHAPE;
@@ -1814,7 +1814,7 @@ ard_status ard_adamw_step(ard_ctx* ctx, const ard_adamw_tensor* tensors, int n_t
                           int state_bits, uint64_t seed, uint64_t step, const uint64_t* step_counter, const float* lr_factor,
                           const float* grad_factor, void* cuda_stream) {
   if (!ctx || (state_bits != 8 && state_bits != 32)) return ARD_ERR_INVALID_ARG;
-  if (!(lr >= 0.0) || !(lr < INFINITY) || !(eps >= 0.0) || !(eps < INFINITY)) return ARD_ERR_INVALID_ARG;
+  if (!(lr >= 0.0) || !((float)lr < INFINITY) || !(eps >= 0.0) || !((float)eps < INFINITY)) return ARD_ERR_INVALID_ARG;  // (as the kernels hold them)
   if (eps > 0.0 && eps < 1.1754943508222875e-38) return ARD_ERR_INVALID_ARG;  // 2^-126: what the kernels' quotients take for zero
   if (!(beta1 >= 0.0) || !(beta1 < 1.0) || !(beta2 >= 0.0) || !(beta2 < 1.0)) return ARD_ERR_INVALID_ARG;
   if (off_elements(8, {step_counter}) || off_elements(4, {lr_factor, grad_factor})) return ARD_ERR_ALIGNMENT;
