@@ -12,7 +12,7 @@ namespace {
 struct LnShape {
   const int32_t* hdr;  // nullptr: all N columns
   int rows, N;
-  __host__ __device__ __forceinline__ long long pitch() const { return ((long long)N + 3) & ~3ll; }  // of a row of partial sums: written in pieces of 16 bytes
+  __host__ __device__ __forceinline__ int pitch() const { return (N + 3) & ~3; }  // of a row of partial sums (N <= 4 million): written in pieces of 16 bytes
 };
 struct LnCols {
   int n, dp, b0;  // compact columns, and the unit of column j: b0 + j * dp
@@ -47,30 +47,31 @@ __device__ __forceinline__ float ln_block_sum(float x, float* red) {
   return x;
 }
 
-// Rows of any length, and few short ones: a CTA per row, element by element, the row read again for each sum.
-template <typename T>
+// Rows of any length, and few short ones: a CTA per row, element by element, the row read again for each sum.  J counts the columns: int, or long long
+// where the number behind the last trip's may pass 2^31 (for all rows: 700 x 1500 forward 6.3 us in place of 4.4).
+constexpr int LN_INT_N = 1 << 30;
+template <typename T, typename J>
 __global__ void __launch_bounds__(LN_ANY_THREADS) ln_fwd_any_kernel(LnShape sh, float eps, const T* X, int ldx, const float* weight,
                                                                    const float* bias, T* Y, int ldy, float* mean, float* rstd) {
   __shared__ float red[LN_ANY_THREADS / 32];
   pdl_launch_dependents();
   pdl_wait_prior_grids();
   const LnCols c = ln_cols(sh);
-  const uint32_t n = (uint32_t)c.n;  // columns are counted without a sign: the one behind the last trip's may lie past 2^31
   const float inv_n = 1.f / (float)c.n;
   for (int r = blockIdx.x; r < sh.rows; r += gridDim.x) {
     const T* x = X + (size_t)r * ldx;
     T* y = Y + (size_t)r * ldy;
     float s = 0.f;
-    for (uint32_t j = threadIdx.x; j < n; j += LN_ANY_THREADS) s += ln_get(x, j);
+    for (J j = threadIdx.x; j < c.n; j += LN_ANY_THREADS) s += ln_get(x, j);
     const float mu = ln_block_sum(s, red) * inv_n;
     s = 0.f;
-    for (uint32_t j = threadIdx.x; j < n; j += LN_ANY_THREADS) {
+    for (J j = threadIdx.x; j < c.n; j += LN_ANY_THREADS) {
       const float d = ln_get(x, j) - mu;
       s = fmaf(d, d, s);
     }
     const float rs = ln_rsqrt(fmaf(ln_block_sum(s, red), inv_n, eps));
-    for (uint32_t j = threadIdx.x; j < n; j += LN_ANY_THREADS) {
-      const uint32_t u = c.b0 + j * c.dp;
+    for (J j = threadIdx.x; j < c.n; j += LN_ANY_THREADS) {
+      const J u = c.b0 + j * c.dp;
       ln_put(y, j, fmaf((ln_get(x, j) - mu) * rs, weight ? weight[u] : 1.f, bias ? bias[u] : 0.f));
     }
     if (threadIdx.x == 0) {
@@ -80,11 +81,10 @@ __global__ void __launch_bounds__(LN_ANY_THREADS) ln_fwd_any_kernel(LnShape sh, 
   }
 }
 
-template <typename T>
+template <typename T, typename J>
 __device__ __forceinline__ void ln_dx_any(const LnShape& sh, const LnCols& c, const T* dY, int lddy, const T* X, int ldx, const float* weight,
                                           const float* mean, const float* rstd, T* dX, int lddx, int first, int blocks) {
   __shared__ float red[2][LN_ANY_THREADS / 32];
-  const uint32_t n = (uint32_t)c.n;
   const float inv_n = 1.f / (float)c.n;
   for (int r = first; r < sh.rows; r += blocks) {
     const T* x = X + (size_t)r * ldx;
@@ -92,14 +92,14 @@ __device__ __forceinline__ void ln_dx_any(const LnShape& sh, const LnCols& c, co
     T* dx = dX + (size_t)r * lddx;
     const float mu = mean[r], rs = rstd[r];
     float s1 = 0.f, s2 = 0.f;
-    for (uint32_t j = threadIdx.x; j < n; j += LN_ANY_THREADS) {
+    for (J j = threadIdx.x; j < c.n; j += LN_ANY_THREADS) {
       const float e = ln_get(dy, j) * (weight ? weight[c.b0 + j * c.dp] : 1.f);
       s1 += e;
       s2 = fmaf(e, (ln_get(x, j) - mu) * rs, s2);
     }
     s1 = ln_block_sum(s1, red[0]) * inv_n;
     s2 = ln_block_sum(s2, red[1]) * inv_n;
-    for (uint32_t j = threadIdx.x; j < n; j += LN_ANY_THREADS) {
+    for (J j = threadIdx.x; j < c.n; j += LN_ANY_THREADS) {
       const float e = ln_get(dy, j) * (weight ? weight[c.b0 + j * c.dp] : 1.f);
       ln_put(dx, j, rs * (e - s1 - (ln_get(x, j) - mu) * rs * s2));
     }
@@ -147,7 +147,7 @@ __device__ __forceinline__ void ln_dw_any(const LnShape& sh, int n, const T* dY,
   }
 }
 // Both in one launch: the first dx_blocks CTAs take rows, the others columns, gx of them a slice.
-template <typename T>
+template <typename T, typename J>
 __global__ void __launch_bounds__(LN_ANY_THREADS) ln_bwd_any_kernel(LnShape sh, const T* dY, int lddy, const T* X, int ldx, const float* weight,
                                                                    const float* mean, const float* rstd, T* dX, int lddx, int dx_blocks,
                                                                    float* partial, int per_slice, int gx) {
@@ -155,7 +155,7 @@ __global__ void __launch_bounds__(LN_ANY_THREADS) ln_bwd_any_kernel(LnShape sh, 
   pdl_wait_prior_grids();
   const LnCols c = ln_cols(sh);
   const int k = (int)blockIdx.x - dx_blocks;
-  if (k < 0) ln_dx_any(sh, c, dY, lddy, X, ldx, weight, mean, rstd, dX, lddx, (int)blockIdx.x, dx_blocks);
+  if (k < 0) ln_dx_any<T, J>(sh, c, dY, lddy, X, ldx, weight, mean, rstd, dX, lddx, (int)blockIdx.x, dx_blocks);
   else ln_dw_any(sh, c.n, dY, lddy, X, ldx, mean, rstd, partial, per_slice, k / gx, k % gx, gx);
 }
 
@@ -983,8 +983,8 @@ ard_status ln_fwd(ard_ctx* ctx, const LnShape& sh, float eps, const T* X, int ld
   else if (!few) run(std::false_type{}, std::false_type{});
   if (!done) {
     const int room = 8 * ctx->sm_count;
-    err = ard_launch(ctx, ln_fwd_any_kernel<T>, dim3(sh.rows < room ? sh.rows : room), dim3(LN_ANY_THREADS), 0, s, sh, eps, X, ldx, weight,
-                     bias, Y, ldy, mean, rstd);
+    auto kern = sh.N <= LN_INT_N ? ln_fwd_any_kernel<T, int> : ln_fwd_any_kernel<T, long long>;
+    err = ard_launch(ctx, kern, dim3(sh.rows < room ? sh.rows : room), dim3(LN_ANY_THREADS), 0, s, sh, eps, X, ldx, weight, bias, Y, ldy, mean, rstd);
   }
   ARD_CUDA_OK(err);
   ctx->launches++;
@@ -997,7 +997,7 @@ ard_status ln_bwd(ard_ctx* ctx, const LnShape& sh, const T* dY, int lddy, const 
                   const float* rstd, T* dX, int lddx, float* dweight, float* dbias, int zero_fill, cudaStream_t s) {
   const bool sums = dweight || dbias;
   if (!dX && !sums) return ARD_OK;
-  const long long fit = (long long)(sk_ws_bytes(ctx->sm_count) / sizeof(float) / 2) / sh.pitch();  // slices that the scratch holds
+  const long long fit = (long long)(sk_ws_bytes(ctx->sm_count) / sizeof(float) / 2) / (((long long)sh.N + 3) / 4 * 4);  // slices that the scratch holds
   if (sums && (!ctx->d_sk_ws || fit < 1)) return ARD_ERR_UNSUPPORTED;
   float* partial = sums ? (float*)ctx->d_sk_ws : nullptr;
   long long slices = 0;
@@ -1071,8 +1071,9 @@ ard_status ln_bwd(ard_ctx* ctx, const LnShape& sh, const T* dY, int lddy, const 
       per = (int)((sh.rows + slices - 1) / slices);
       slices = (sh.rows + per - 1) / per;
     }
-    ARD_CUDA_OK(ard_launch(ctx, ln_bwd_any_kernel<T>, dim3((unsigned)(dx_blocks + slices * gx)), dim3(LN_ANY_THREADS), 0, s, sh, dY, lddy, X, ldx,
-                           weight, mean, rstd, dX, lddx, dx_blocks, partial, per, gx));
+    auto kern = sh.N <= LN_INT_N ? ln_bwd_any_kernel<T, int> : ln_bwd_any_kernel<T, long long>;
+    ARD_CUDA_OK(ard_launch(ctx, kern, dim3((unsigned)(dx_blocks + slices * gx)), dim3(LN_ANY_THREADS), 0, s, sh, dY, lddy, X, ldx, weight, mean, rstd,
+                           dX, lddx, dx_blocks, partial, per, gx));
     ctx->launches++;
   }
   if (sums) {
