@@ -158,13 +158,12 @@ __device__ __forceinline__ float2 operator+(float2 a, float2 b) { return __fadd2
 __device__ __forceinline__ float2 aw_fma(float2 a, float2 b, float2 c) { return __ffma2_rn(a, b, c); }
 __device__ __forceinline__ float2 aw_both(float x) { return make_float2(x, x); }
 // Roots to the last bit: one of Heron's steps with its residual in one rounding (Markstein, IBM J. Res. Dev. 34, 1990), from the instruction's estimate of
-// 1 / sqrt(x), which takes subnormals (of those a unit or two in the last place).  No branches: they keep a thread's quads from running beside one another
-// (145 us for 36 M elements in place of 133, both without subnormals and infinity, which cost 6 us).  Of infinity the step gives NaN, which the maximum with
-// 2^-66 x, less than the root of any finite x, puts right; 0 and NaN stay what they are.
+// 1 / sqrt(x), which takes subnormals (of those a unit or two in the last place).  No branches: they keep a thread's quads from running beside one another.
+// Of 0 and infinity the step gives NaN, which the maximum with 2^-66 x, less than the root of any other finite x, puts right; NaN stays what it is.
 __device__ __forceinline__ float2 aw_roots(float2 x) {
   float2 y;
-  asm("rsqrt.approx.f32 %0, %1;" : "=f"(y.x) : "f"(fmaxf(x.x, 1.40129846e-45f)));
-  asm("rsqrt.approx.f32 %0, %1;" : "=f"(y.y) : "f"(fmaxf(x.y, 1.40129846e-45f)));
+  asm("rsqrt.approx.f32 %0, %1;" : "=f"(y.x) : "f"(x.x));
+  asm("rsqrt.approx.f32 %0, %1;" : "=f"(y.y) : "f"(x.y));
   const float2 q = x * y, r = aw_fma(aw_fma(q * aw_both(-1.f), q, x), y * aw_both(0.5f), q), less = x * aw_both(1.35525272e-20f);
   return make_float2(fmaxf(r.x, less.x), fmaxf(r.y, less.y));
 }
