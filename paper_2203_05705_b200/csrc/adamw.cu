@@ -382,10 +382,11 @@ __global__ void __launch_bounds__(AW_THREADS, 4) adamw_kernel(const __grid_const
   }
 }
 
-// States in 8 bits: 14 to 20 bytes are read for an element whose arithmetic takes some 80 instructions, so registers cannot hold what has to be in flight
-// (36 bytes for a thread's quad: 2.2 TB/s).  Every warp has its own tiles, which come through a ring in shared memory by bulk copies ahead of it: no
-// barrier among warps, four quads of a lane to a search of the table.  (Tiles of a CTA, two quads and four: 148 and 124 us for 36 M elements, with states rounded
-// from values a unit or so off; so, to the last bit, 133 us, 143 where the scales come by lanes.)
+// States in 8 bits: 8 to 10 bytes are read for an element whose arithmetic takes some 92 instructions, so registers cannot hold what has to be in
+// flight (36 bytes for a thread's quad: 2.2 TB/s).  Every warp has its own tiles, which come through a ring in shared memory by bulk copies ahead of it:
+// no barrier among warps, four quads of a lane to a search of the table.  36 M elements with a fp32 gradient 140 us, 150 where the scales come by lanes;
+// with a bf16 one 141.  (Tiles of a CTA, two quads and four: 148 and 124 us with states rounded from values a unit or so off; to the last bit 133 in
+// tiles of a warp; the rest is for moments at fp32's ends, infinity and subnormals.)
 constexpr int AW8_QUADS = 4, AW8_TILE = AW8_QUADS * 128, AW8_SLOTS = 2, AW8_PER_SM = 2, AW8_WARPS = AW_THREADS / 32;
 constexpr int AW8_UNROLL = 4;
 static_assert(AW8_QUADS % 4 == 0, "bulk copies of the scales: multiples of 16 bytes");
@@ -502,7 +503,7 @@ constexpr int GN_TILE = GN_EIGHTS * AW_THREADS * 8;
 
 // The squares of eight values.  Added in fp32 where that is as good: a sum that neither overflowed nor lies where squares lose their bits
 // (the additions' errors, of either sign, go under in millions of such sums).  Otherwise in fp64, which converts every value: 68 us in place of 24 for
-// 64 Mi bf16 values.
+// 64 Mi bf16 values.  (Zeros, as whole rows of dropped units, go that way too: every second row of 2048 zero 25.4 us, four of five 27.3.)
 __device__ __forceinline__ double gn_squares(const float (&g)[8]) {
   float s = 0.f;
 #pragma unroll

@@ -9,9 +9,11 @@
 // sequences), so gates are read once and outputs written once.  The adjoint starts its states from those that the forward call left
 // every ARD_GLR_CHUNK steps and computes the ones between again: 4 bytes in 64 steps in place of 4 in each.
 //
-// Memory would bound both (gates in, outputs out); what does is instruction issue and the way of the maps: 2048 x 8 x 2048 bf16 55.8 / 86.1 us forward /
-// backward (its bytes at a copy's rate 41.1 / 71.9; half to 60 % of the issue slots taken, 256 units on 296 places), 16384 x 1 x 1024 40.3 / 69 us
-// (20.6 / 36; sixteen rounds, each with the maps' way round a cluster), 35 x 64 x 1024 9 / 14.4 us (2.8 / 4.9), a single step of 64 x 1024 2.1 us.
+// Memory would bound both (gates in, outputs out); what does is instruction issue and the way of the maps: 2048 x 8 x 2048 bf16 56 / 87 us forward /
+// backward (its bytes at a copy's rate 41.1 / 71.9; half to 60 % of the issue slots taken, 256 units on 296 places), 16384 x 1 x 1024 40.5 / 69 us
+// (20.6 / 36; sixteen rounds, each with the maps' way round a cluster), 35 x 64 x 1024 8.8 / 14.4 us (2.8 / 4.9), a single step of 64 x 1024 2.2 us.
+// A slab behind a sequence's end costs as much as one inside it: gates of what the slot holds, maps, the barrier, and the zeros by stores that ask.
+// With three fifths of the cells of 2048 x 8 x 2048 inside 62 / 99 us.
 #include <cooperative_groups.h>
 
 #include <initializer_list>
@@ -95,8 +97,9 @@ __device__ __forceinline__ float glr_inverse(float x) {
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
   return r;
 }
-// s(z), and 1 - s(z), each to the last bits of its own: where s(z) is above a half the other one is exp(-z) times it, not a difference.  exp(-z) of
-// infinity gives 0 and 1.
+// s(z), and 1 - s(z), each relative to its own size: where s(z) is above a half the other one is exp(-z) times it, not a difference.  The exponential's
+// argument is a rounded product, so the smaller of the two is off by some |z| units in the last place beside the instructions' own two or three.  exp(-z)
+// of infinity gives 0 and 1.
 template <int VEC>
 __device__ __forceinline__ GlrV<VEC> glr_gate(const GlrV<VEC>& z, GlrV<VEC>& rest) {
   GlrV<VEC> u = z * GlrV<VEC>::all(-1.44269504f);
@@ -220,7 +223,7 @@ struct GlrFeed;
 template <typename T, int VEC, int M, int W, int WT, int SPT>
 struct GlrFeed<T, VEC, M, W, WT, SPT, true> {
   static constexpr int ROW = W * VEC * (int)sizeof(T), TILE = WT * SPT * ROW, SLOT = M * TILE;
-  static constexpr int SLOTS = M == 4 ? 2 : 3;  // two CTAs an SM with 64 to 72 KB each
+  static constexpr int SLOTS = M == 4 ? 2 : 3;  // two CTAs an SM with 48 to 72 KB each
   uint8_t* slots;
   uint64_t* full;
   int taken, slot, phase;       // slabs so far, and where the one that is being worked on lies
@@ -677,10 +680,18 @@ bool glr_tiles(ard_ctx* ctx, const GlrArgs& a, std::initializer_list<std::pair<c
   return true;
 }
 
-// Steps of a thread.  As few as a short sequence's slab of 8 warps needs (three CTAs an SM: 35 x 64 x 1024 11.3 -> 8.7 us); 8, two CTAs an SM, otherwise.
-// (16 in clusters, one CTA an SM: what a round costs besides its steps is paid half as often, but nothing runs beside it: 16384 x 1 x 1024 50.9 / 81.2
-// us forward / backward.)  Units as wide as a warp, or as half of one, twice as many steps long, where clusters of all that may share a sequence would leave
-// SMs idle: the same size 49.5 / 76.5 us in whole warps, 40.3 / 69.2 in halves; 16384 x 1 x 2048, which fills them either way, 71 / 117 and 71 / 128.
+// Steps of a thread.  A slab either holds the whole sequence or begins where the forward call left a state, every 64 steps: 2 or 5 steps a thread where
+// 8 warps of them reach the end, three CTAs an SM, otherwise 8, two CTAs an SM.  T x 64 x 1024 bf16, forward / backward:
+//   T = 16         2 steps 6.3 / 7.8 us    5 steps 8.5 / 11.8     8 steps 10.8 / 15.9
+//   T = 17, 24     5 steps 8.4 / 11.9, 8.5 / 12.6                 8 steps 10.8 / 16.0, 10.8 / 16.6
+//   T = 35, 40     5 steps 8.8 / 14.5, 8.3 / 13.6                 8 steps 11.2 / 17.6, 11.5 / 18.1
+//   T = 48, 64     8 steps 12.4 / 18.9, 12.6 / 17.9
+// (16 in clusters, one CTA an SM: what a round costs besides its steps is paid half as often, but nothing runs beside it: 16384 x 1 x 1024 50.9 / 81.2 us.)
+// Clusters where the units leave more than half of the SMs idle.  T = 4096, units a warp wide: 60 of them 36 / 58 us, 74 48 / 76, in clusters; 75, 100,
+// 147, 148 a CTA each 76 / 116, 88 / 137, 89 / 139, 72 / 112, where clusters of two or three (two CTAs fit an SM) would take 48 / 76, 65 / 105, 66 / 107,
+// 66 / 107: the edge stands too low.
+// Units as wide as a warp, or as half of one, twice as many steps long, where clusters of all that may share a sequence would leave SMs idle:
+// 16384 x 1 x 1024 49.5 / 76.5 us in whole warps, 40.3 / 69.2 in halves; 16384 x 1 x 2048, which fills them either way, 71 / 117 and 71 / 128.
 // run(SPT, W, CTAs an SM, cluster).
 template <typename Run>
 ard_status glr_steps(ard_ctx* ctx, const GlrArgs& a, int vec, Run run) {
