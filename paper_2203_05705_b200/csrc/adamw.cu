@@ -1,7 +1,8 @@
 // The optimiser's step over many tensors at once, and the norm of all gradients with the factor that clips them.
 //
-// Both are one pass over memory: per element the step reads p, g, m, v and writes p, m, v and the bf16 copy (28 to 30 bytes with
-// states in 32 bits, 16 to 18 in 8).  The table of tensors travels as a kernel parameter: nothing is copied or allocated per call.
+// Both are one pass over memory: per element the step reads p, g, m, v and writes p, m, v and the bf16 copy (28 to 30
+// bytes with states in 32 bits, 16 to 18 in 8).  The table of tensors travels as a kernel parameter: nothing is copied
+// or allocated per call.
 #include <cuda_fp8.h>
 
 #include "ard_internal.h"
@@ -38,8 +39,8 @@ struct AwTable {
   unsigned long long tiles;
 };
 
-// Tables travel in the launch: the small one keeps a launch over a handful of tensors as cheap as any other, the large one
-// (26 KB of the 32 KB that parameters may have) takes a network's.
+// Tables travel in the launch: the small one keeps a launch over a handful of tensors as cheap as any other, the large
+// one (26 KB of the 32 KB that parameters may have) takes a network's.
 constexpr int AW_SMALL = 16, AW_LARGE = 216;
 
 struct AwArgs {
@@ -140,8 +141,9 @@ __device__ __forceinline__ void aw_decode(uint32_t q, float scale, float (&v)[4]
   }
 }
 
-// sqrt(x) and 1 / x as the instructions approximate them, to a unit or two in the last place: rounded to the last bit they take 8 to 20 instructions
-// each, with their special cases, and the kernel with states in 8 bits runs out of issue slots.
+// sqrt(x) and 1 / x as the instructions approximate them, to a unit or two in the last place: rounded to the last bit
+// they take 8 to 20 instructions each, with their special cases, and the kernel with states in 8 bits runs out of issue
+// slots.
 __device__ __forceinline__ float aw_root(float x) {
   float r;
   asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
@@ -157,9 +159,10 @@ __device__ __forceinline__ float2 operator*(float2 a, float2 b) { return __fmul2
 __device__ __forceinline__ float2 operator+(float2 a, float2 b) { return __fadd2_rn(a, b); }
 __device__ __forceinline__ float2 aw_fma(float2 a, float2 b, float2 c) { return __ffma2_rn(a, b, c); }
 __device__ __forceinline__ float2 aw_both(float x) { return make_float2(x, x); }
-// Roots to the last bit: one of Heron's steps with its residual in one rounding (Markstein, IBM J. Res. Dev. 34, 1990), from the instruction's estimate of
-// 1 / sqrt(x), which takes subnormals (of those a unit or two in the last place).  No branches: they keep a thread's quads from running beside one another.
-// Of 0 and infinity the step gives NaN, which the maximum with 2^-66 x, less than the root of any other finite x, puts right; NaN stays what it is.
+// Roots to the last bit: one of Heron's steps with its residual in one rounding (Markstein, IBM J. Res. Dev. 34, 1990),
+// from the instruction's estimate of 1 / sqrt(x), which takes subnormals (of those a unit or two in the last place).
+// No branches: they keep a thread's quads from running beside one another. Of 0 and infinity the step gives NaN, which
+// the maximum with 2^-66 x, less than the root of any other finite x, puts right; NaN stays what it is.
 __device__ __forceinline__ float2 aw_roots(float2 x) {
   float2 y;
   asm("rsqrt.approx.f32 %0, %1;" : "=f"(y.x) : "f"(x.x));
@@ -168,25 +171,28 @@ __device__ __forceinline__ float2 aw_roots(float2 x) {
   return make_float2(fmaxf(r.x, less.x), fmaxf(r.y, less.y));
 }
 
-// The 8-bit floats of a block of 128 values, four in each lane, and its scale (the same in all lanes).  ROOT: of values >= 0, from the words'
-// high halves; else from their low halves.
-// A value is rounded to the grid of the 8-bit floats (3 bits of mantissa; steps of 2^-9 below 2^-6), up with the probability of what is
-// cut off, which 16 random bits resolve to 2^-16 of a step: those bits are added below the mantissa's three, and all bits there cut off.  (Half a step
-// less and the conversion's rounding to nearest in place of the cut would be wrong where a sum passes 2^-5.)  Below 2^-6 the grid is that of
-// [2^-6, 2^-5): adding 2^-6 puts the value there.  Sums carry into the exponent where they should.  What passes 448 the conversion cuts off.
+// The 8-bit floats of a block of 128 values, four in each lane, and its scale (the same in all lanes).  ROOT: of values
+// >= 0, from the words' high halves; else from their low halves. A value is rounded to the grid of the 8-bit floats (3
+// bits of mantissa; steps of 2^-9 below 2^-6), up with the probability of what is cut off, which 16 random bits resolve
+// to 2^-16 of a step: those bits are added below the mantissa's three, and all bits there cut off.  (Half a step less
+// and the conversion's rounding to nearest in place of the cut would be wrong where a sum passes 2^-5.)  Below 2^-6 the
+// grid is that of [2^-6, 2^-5): adding 2^-6 puts the value there.  Sums carry into the exponent where they should.
+// What passes 448 the conversion cuts off.
 template <bool ROOT>
 __device__ __forceinline__ uint32_t aw_encode(const float2 (&v)[2], const uint32_t (&words)[4], float& scale) {
   float most = fmaxf(fmaxf(fabsf(v[0].x), fabsf(v[0].y)), fmaxf(fabsf(v[1].x), fabsf(v[1].y)));
-  // a value that is not a number, which the maximum drops, spoils its block, as it spoils states in 32 bits; so does an infinite m
+  // a value that is not a number, which the maximum drops, spoils its block, as it spoils states in 32 bits; so does an
+  // infinite m
   const float2 any = ROOT ? v[0] + v[1] : aw_fma(v[0], aw_both(0.f), v[1] * aw_both(0.f));
   if (!(any.x + any.y <= INFINITY)) most = __int_as_float(0x7FC00000);
   uint32_t bits = __reduce_max_sync(0xFFFFFFFFu, __float_as_uint(most));  // of values >= 0, in their order
-  // An infinite root (v beyond fp32) counts as 2^126, which no finite root reaches and whose square is infinite again: with a scale of infinity the block's
-  // zeros would be lost.
+  // An infinite root (v beyond fp32) counts as 2^126, which no finite root reaches and whose square is infinite again:
+  // with a scale of infinity the block's zeros would be lost.
   if (ROOT && bits == 0x7F800000u) bits = 0x7E800000u;
   const float big = __uint_as_float(bits);
   const bool none = big < AW_TINY;
-  // (of m's largest value / 256: above 2^126 its own reciprocal is below the normal range, which the instruction takes for zero)
+  // (of m's largest value / 256: above 2^126 its own reciprocal is below the normal range, which the instruction takes
+  // for zero)
   const float part = ROOT ? big : big * 0.00390625f, near = aw_inverse(part);
   const float inv = none ? 0.f : E4M3_MAX * (ROOT ? 1.f : 0.00390625f) * fmaf(near, fmaf(-part, near, 1.f), near), least = none ? 0.f : 0.001953125f;
   scale = none ? 0.f : big * (1.f / E4M3_MAX);
@@ -260,9 +266,10 @@ __device__ __forceinline__ void aw_update(const AwEntry& e, const AwStep& a, con
     m2[h] = make_float2(m[2 * h], m[2 * h + 1]);
     v2[h] = make_float2(v[2 * h], v[2 * h + 1]);
     if constexpr (BITS == 8) {
-      // What decides how a state is rounded is computed operation by operation as the formulas stand, to the last bit: one unit off moves a value in a
-      // million to its other neighbour.  (Sums as products with one and sums: of a sum of two elements in one instruction the assembler makes one with the
-      // product before it, though both ask to be rounded.)
+      // What decides how a state is rounded is computed operation by operation as the formulas stand, to the last bit:
+      // one unit off moves a value in a million to its other neighbour.  (Sums as products with one and sums: of a sum
+      // of two elements in one instruction the assembler makes one with the product before it, though both ask to be
+      // rounded.)
       const float2 one = aw_both(a.one);
       m2[h] = aw_fma(aw_both(a.beta1) * m2[h], one, aw_both(a.omb1) * gk[h]);
       v2[h] = aw_fma(aw_both(a.beta2) * (v2[h] * v2[h]), one, (aw_both(a.omb2) * gk[h]) * gk[h]);
@@ -354,8 +361,9 @@ __device__ __forceinline__ void aw_ragged(const AwEntry& e, const AwStep& st, co
   }
 }
 
-// States in 32 bits: a CTA a tile, all of a thread's loads ahead of its stores.  (On a grid of the resident CTAs, each with many tiles, the step of
-// 8192 x 8192 with a bf16 gradient took 310 us, so 274, 6.85 TB/s: the loads of a CTA that begins run beside the stores of one that ends.)
+// States in 32 bits: a CTA a tile, all of a thread's loads ahead of its stores.  (On a grid of the resident CTAs, each
+// with many tiles, the step of 8192 x 8192 with a bf16 gradient took 310 us, so 274, 6.85 TB/s: the loads of a CTA that
+// begins run beside the stores of one that ends.)
 template <int CAP>
 __global__ void __launch_bounds__(AW_THREADS, 4) adamw_kernel(const __grid_constant__ AwTable<CAP> table, const __grid_constant__ AwArgs a) {
   __shared__ float s_lift[2];
@@ -382,11 +390,12 @@ __global__ void __launch_bounds__(AW_THREADS, 4) adamw_kernel(const __grid_const
   }
 }
 
-// States in 8 bits: 8 to 10 bytes are read for an element whose arithmetic takes some 92 instructions, so registers cannot hold what has to be in
-// flight (36 bytes for a thread's quad: 2.2 TB/s).  Every warp has its own tiles, which come through a ring in shared memory by bulk copies ahead of it:
-// no barrier among warps, four quads of a lane to a search of the table.  36 M elements with a fp32 gradient 140 us, 150 where the scales come by lanes;
-// with a bf16 one 141.  (Tiles of a CTA, two quads and four: 148 and 124 us with states rounded from values a unit or so off; to the last bit 133 in
-// tiles of a warp; the rest is for moments at fp32's ends, infinity and subnormals.)
+// States in 8 bits: 8 to 10 bytes are read for an element whose arithmetic takes some 92 instructions, so registers
+// cannot hold what has to be in flight (36 bytes for a thread's quad: 2.2 TB/s).  Every warp has its own tiles, which
+// come through a ring in shared memory by bulk copies ahead of it: no barrier among warps, four quads of a lane to a
+// search of the table.  36 M elements with a fp32 gradient 140 us, 150 where the scales come by lanes; with a bf16 one
+// 141.  (Tiles of a CTA, two quads and four: 148 and 124 us with states rounded from values a unit or so off; to the
+// last bit 133 in tiles of a warp; the rest is for moments at fp32's ends, infinity and subnormals.)
 constexpr int AW8_QUADS = 4, AW8_TILE = AW8_QUADS * 128, AW8_SLOTS = 2, AW8_PER_SM = 2, AW8_WARPS = AW_THREADS / 32;
 constexpr int AW8_UNROLL = 4;
 static_assert(AW8_QUADS % 4 == 0, "bulk copies of the scales: multiples of 16 bytes");
@@ -451,7 +460,8 @@ __global__ void __launch_bounds__(AW_THREADS, AW8_PER_SM) adamw8_kernel(const __
     const AwEntry& e = table.e[aw_find(table, tile)];
     const long long base = (long long)(tile - e.tile0) * AW8_TILE;
     st.lr_decay = lr * e.decay;
-    // scales off the 16-byte grid (those of a tensor among others in one buffer): a lane each, behind the wait into the copies' place
+    // scales off the 16-byte grid (those of a tensor among others in one buffer): a lane each, behind the wait into the
+    // copies' place
     const bool by_lanes = !e.scales16 && whole(e, base) && lane < 2 * AW8_QUADS;
     const float sc = by_lanes ? (lane < AW8_QUADS ? e.m_scale : e.v_scale - AW8_QUADS)[base / 128 + lane] : 0.f;
     if (!gone && !mbar_wait(smem_u32(&full[slot]), (uint32_t)phase, &s_gone, status)) gone = true;
@@ -501,9 +511,10 @@ __global__ void __launch_bounds__(AW_THREADS, AW8_PER_SM) adamw8_kernel(const __
 constexpr int GN_EIGHTS = 4;
 constexpr int GN_TILE = GN_EIGHTS * AW_THREADS * 8;
 
-// The squares of eight values.  Added in fp32 where that is as good: a sum that neither overflowed nor lies where squares lose their bits
-// (the additions' errors, of either sign, go under in millions of such sums).  Otherwise in fp64, which converts every value: 68 us in place of 24 for
-// 64 Mi bf16 values.  (Zeros, as whole rows of dropped units, go that way too: every second row of 2048 zero 25.4 us, four of five 27.3.)
+// The squares of eight values.  Added in fp32 where that is as good: a sum that neither overflowed nor lies where
+// squares lose their bits (the additions' errors, of either sign, go under in millions of such sums).  Otherwise in
+// fp64, which converts every value: 68 us in place of 24 for 64 Mi bf16 values.  (Zeros, as whole rows of dropped
+// units, go that way too: every second row of 2048 zero 25.4 us, four of five 27.3.)
 __device__ __forceinline__ double gn_squares(const float (&g)[8]) {
   float s = 0.f;
 #pragma unroll

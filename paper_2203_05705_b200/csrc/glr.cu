@@ -4,16 +4,18 @@
 //   dzo_t = alpha dy_t c_t s(zo_t) (1 - s(zo_t)),  dzf_t = d_t (c_{t-1} - g_t) f_t (1 - f_t),  dzg_t = d_t (1 - f_t).
 //
 // Both recurrences are compositions of maps x -> A x + B, so the time axis can be cut: a thread holds SPT steps of its
-// channels in registers, composes their map, and applies the steps once it knows the state that enters them.  The maps of a slab's
-// warps meet in shared memory, those of consecutive slabs in the shared memory of a cluster of CTAs (few channels, long
-// sequences), so gates are read once and outputs written once.  The adjoint starts its states from those that the forward call left
-// every ARD_GLR_CHUNK steps and computes the ones between again: 4 bytes in 64 steps in place of 4 in each.
+// channels in registers, composes their map, and applies the steps once it knows the state that enters them.  The maps
+// of a slab's warps meet in shared memory, those of consecutive slabs in the shared memory of a cluster of CTAs (few
+// channels, long sequences), so gates are read once and outputs written once.  The adjoint starts its states from those
+// that the forward call left every ARD_GLR_CHUNK steps and computes the ones between again: 4 bytes in 64 steps in
+// place of 4 in each.
 //
-// Memory would bound both (gates in, outputs out); what does is instruction issue and the way of the maps: 2048 x 8 x 2048 bf16 56 / 87 us forward /
-// backward (its bytes at a copy's rate 41.1 / 71.9; half to 60 % of the issue slots taken, 256 units on 296 places), 16384 x 1 x 1024 40.5 / 69 us
-// (20.6 / 36; sixteen rounds, each with the maps' way round a cluster), 35 x 64 x 1024 8.8 / 14.4 us (2.8 / 4.9), a single step of 64 x 1024 2.2 us.
-// A slab behind a sequence's end costs as much as one inside it: gates of what the slot holds, maps, the barrier, and the zeros by stores that ask.
-// With three fifths of the cells of 2048 x 8 x 2048 inside 62 / 99 us.
+// Memory would bound both (gates in, outputs out); what does is instruction issue and the way of the maps: 2048 x 8 x
+// 2048 bf16 56 / 87 us forward / backward (its bytes at a copy's rate 41.1 / 71.9; half to 60 % of the issue slots
+// taken, 256 units on 296 places), 16384 x 1 x 1024 40.5 / 69 us (20.6 / 36; sixteen rounds, each with the maps' way
+// round a cluster), 35 x 64 x 1024 8.8 / 14.4 us (2.8 / 4.9), a single step of 64 x 1024 2.2 us. A slab behind a
+// sequence's end costs as much as one inside it: gates of what the slot holds, maps, the barrier, and the zeros by
+// stores that ask. With three fifths of the cells of 2048 x 8 x 2048 inside 62 / 99 us.
 #include <cooperative_groups.h>
 
 #include <initializer_list>
@@ -47,7 +49,8 @@ struct GlrArgs {
   int* status;
 };
 
-// A lane's channels.  Two of them go through one instruction (f32x2): these kernels run out of issue slots before anything else.
+// A lane's channels.  Two of them go through one instruction (f32x2): these kernels run out of issue slots before
+// anything else.
 template <int VEC>
 struct GlrV {
   float v[VEC];
@@ -85,8 +88,8 @@ __device__ __forceinline__ GlrV<VEC> glr_fma(const GlrV<VEC>& a, const GlrV<VEC>
     return {{fmaf(a.v[0], b.v[0], c.v[0])}};
   }
 }
-// 2^x and 1 / x to about two units in the last place, results below the normal range zero: the forms that keep subnormals cost five
-// instructions each, of which a gate has two.
+// 2^x and 1 / x to about two units in the last place, results below the normal range zero: the forms that keep
+// subnormals cost five instructions each, of which a gate has two.
 __device__ __forceinline__ float glr_exp2(float x) {
   float r;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
@@ -97,9 +100,9 @@ __device__ __forceinline__ float glr_inverse(float x) {
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
   return r;
 }
-// s(z), and 1 - s(z), each relative to its own size: where s(z) is above a half the other one is exp(-z) times it, not a difference.  The exponential's
-// argument is a rounded product, so the smaller of the two is off by some |z| units in the last place beside the instructions' own two or three.  exp(-z)
-// of infinity gives 0 and 1.
+// s(z), and 1 - s(z), each relative to its own size: where s(z) is above a half the other one is exp(-z) times it, not
+// a difference.  The exponential's argument is a rounded product, so the smaller of the two is off by some |z| units in
+// the last place beside the instructions' own two or three.  exp(-z) of infinity gives 0 and 1.
 template <int VEC>
 __device__ __forceinline__ GlrV<VEC> glr_gate(const GlrV<VEC>& z, GlrV<VEC>& rest) {
   GlrV<VEC> u = z * GlrV<VEC>::all(-1.44269504f);
@@ -187,13 +190,14 @@ struct GlrSpan {
     units = groups * a.B;  // (at most 2^31 - 1: the host asks)
     rounds = (a.T + steps - 1) / steps;
   }
-  // The unit of a CTA (a cluster) after this one: so many further, or behind the last, whose number the sum may not pass.
+  // The unit of a CTA (a cluster) after this one: so many further, or behind the last, whose number the sum may not
+  // pass.
   __device__ __forceinline__ int after(int unit, int clusters) const { return units - unit > clusters ? unit + clusters : units; }
   __device__ __forceinline__ bool inside(int unit, int channels) const { return n - unit % groups * channels >= channels; }
   __device__ __forceinline__ int len(const GlrArgs& a, int b) const { return a.lens ? min(max(a.lens[b], 0), a.T) : a.T; }
 };
-// A thread's place in a unit: VEC channels of one sequence, SPT consecutive steps of every slab.  W threads stand side by side over the unit's channels
-// (warps, or half a warp), WT groups of them over a slab's steps.
+// A thread's place in a unit: VEC channels of one sequence, SPT consecutive steps of every slab.  W threads stand side
+// by side over the unit's channels (warps, or half a warp), WT groups of them over a slab's steps.
 template <int VEC, int W, int WT>
 struct GlrPlace {
   int wt, ch, b, j, valid, col, len;
@@ -211,9 +215,9 @@ struct GlrPlace {
   }
 };
 
-// Where M operands of a slab come from.  BULK: tiles [WT * SPT steps][W * VEC channels] that the copy engine brings into a ring of
-// slots, several slabs ahead and over the ends of units (rows of 16-byte aligned pieces).  Otherwise registers, into which a
-// thread fetches its own values of the unit's next slab as soon as this one's are used.
+// Where M operands of a slab come from.  BULK: tiles [WT * SPT steps][W * VEC channels] that the copy engine brings
+// into a ring of slots, several slabs ahead and over the ends of units (rows of 16-byte aligned pieces).  Otherwise
+// registers, into which a thread fetches its own values of the unit's next slab as soon as this one's are used.
 struct GlrTiles {
   CUtensorMap map[4];
 };
@@ -296,10 +300,11 @@ struct GlrFeed<T, VEC, M, W, WT, SPT, false> {
   __device__ __forceinline__ uint32_t raw(int, int m, int k) const { return q[m][k]; }
 };
 
-// The maps of a slab's warps meet in `warp`; its last warp (in the order of the recurrence) leaves the state behind the round in `state`, where the
-// next round finds it.  The cluster's CTAs send each other their slabs' maps by asynchronous stores that count on the receiver's
-// barrier: a barrier of the cluster would wait for the outputs' stores, 2 us a round (bulk copies between their memories: forward the same, backward
-// 30 % slower).  Every CTA hears from all of them in every round, so none is more than a round ahead and two sets of places are enough.
+// The maps of a slab's warps meet in `warp`; its last warp (in the order of the recurrence) leaves the state behind the
+// round in `state`, where the next round finds it.  The cluster's CTAs send each other their slabs' maps by
+// asynchronous stores that count on the receiver's barrier: a barrier of the cluster would wait for the outputs'
+// stores, 2 us a round (bulk copies between their memories: forward the same, backward 30 % slower).  Every CTA hears
+// from all of them in every round, so none is more than a round ahead and two sets of places are enough.
 template <int VEC, int W, int FROM>
 struct GlrMail {
   GlrMap<VEC> box[2][FROM][W];
@@ -328,8 +333,8 @@ struct GlrShared {
   int gone;
 };
 
-// Behind the barrier that follows the warps' maps: the state that enters this warp's steps.  x: what enters the unit's first round.  FORWARD: warps
-// count in the order of the steps, else against it.  `mail`: rounds of the cluster so far.
+// Behind the barrier that follows the warps' maps: the state that enters this warp's steps.  x: what enters the unit's
+// first round.  FORWARD: warps count in the order of the steps, else against it.  `mail`: rounds of the cluster so far.
 template <bool FORWARD, int VEC, int W, int WT>
 __device__ __forceinline__ GlrV<VEC> glr_enter(GlrShared<VEC, W, WT>& sh, int wt, int ch, bool first, int mail, int CL, int rank,
                                               const GlrV<VEC>& x, int* status) {
@@ -631,8 +636,8 @@ constexpr int glr_ring() { return F::SLOTS * F::SLOT; }
 
 inline long long glr_units(const GlrArgs& a, int channels) { return ((long long)a.H + channels - 1) / channels * a.B; }
 
-// With bulk copies the grid is what the device holds at once (per_sm CTAs an SM) and a CTA goes from unit to unit, its copies ahead of it; without, a
-// CTA (a cluster) per unit.
+// With bulk copies the grid is what the device holds at once (per_sm CTAs an SM) and a CTA goes from unit to unit, its
+// copies ahead of it; without, a CTA (a cluster) per unit.
 template <typename K>
 ard_status glr_launch(ard_ctx* ctx, K kern, const GlrArgs& a, const GlrTiles& tiles, int channels, int CL, int threads, int smem, int per_sm,
                       cudaStream_t s) {
@@ -652,7 +657,9 @@ ard_status glr_launch(ard_ctx* ctx, K kern, const GlrArgs& a, const GlrTiles& ti
   return ARD_OK;
 }
 
-// CTAs of a cluster that share a sequence's slabs, where the units alone leave more than half of the SMs idle: as many as let all units run at once.  How many clusters of a size the device holds goes by how its SMs are grouped, and is asked once.
+// CTAs of a cluster that share a sequence's slabs, where the units alone leave more than half of the SMs idle: as many
+// as let all units run at once.  How many clusters of a size the device holds goes by how its SMs are grouped, and is
+// asked once.
 inline int glr_cluster(ard_ctx* ctx, long long units, long long slabs) {
   if (slabs < 2) return 1;
   if (ctx->glr_room[2] == 0) {
@@ -680,19 +687,20 @@ bool glr_tiles(ard_ctx* ctx, const GlrArgs& a, std::initializer_list<std::pair<c
   return true;
 }
 
-// Steps of a thread.  A slab either holds the whole sequence or begins where the forward call left a state, every 64 steps: 2 or 5 steps a thread where
-// 8 warps of them reach the end, three CTAs an SM, otherwise 8, two CTAs an SM.  T x 64 x 1024 bf16, forward / backward:
+// Steps of a thread.  A slab either holds the whole sequence or begins where the forward call left a state, every 64
+// steps: 2 or 5 steps a thread where 8 warps of them reach the end, three CTAs an SM, otherwise 8, two CTAs an SM.  T x
+// 64 x 1024 bf16, forward / backward:
 //   T = 16         2 steps 6.3 / 7.8 us    5 steps 8.5 / 11.8     8 steps 10.8 / 15.9
 //   T = 17, 24     5 steps 8.4 / 11.9, 8.5 / 12.6                 8 steps 10.8 / 16.0, 10.8 / 16.6
 //   T = 35, 40     5 steps 8.8 / 14.5, 8.3 / 13.6                 8 steps 11.2 / 17.6, 11.5 / 18.1
 //   T = 48, 64     8 steps 12.4 / 18.9, 12.6 / 17.9
-// (16 in clusters, one CTA an SM: what a round costs besides its steps is paid half as often, but nothing runs beside it: 16384 x 1 x 1024 50.9 / 81.2 us.)
-// Clusters where the units leave more than half of the SMs idle.  T = 4096, units a warp wide: 60 of them 36 / 58 us, 74 48 / 76, in clusters; 75, 100,
-// 147, 148 a CTA each 76 / 116, 88 / 137, 89 / 139, 72 / 112, where clusters of two or three (two CTAs fit an SM) would take 48 / 76, 65 / 105, 66 / 107,
-// 66 / 107: the edge stands too low.
-// Units as wide as a warp, or as half of one, twice as many steps long, where clusters of all that may share a sequence would leave SMs idle:
-// 16384 x 1 x 1024 49.5 / 76.5 us in whole warps, 40.3 / 69.2 in halves; 16384 x 1 x 2048, which fills them either way, 71 / 117 and 71 / 128.
-// run(SPT, W, CTAs an SM, cluster).
+// (16 in clusters, one CTA an SM: what a round costs besides its steps is paid half as often, but nothing runs beside
+// it: 16384 x 1 x 1024 50.9 / 81.2 us.) Clusters where the units leave more than half of the SMs idle.  T = 4096, units
+// a warp wide: 60 of them 36 / 58 us, 74 48 / 76, in clusters; 75, 100, 147, 148 a CTA each 76 / 116, 88 / 137, 89 /
+// 139, 72 / 112, where clusters of two or three (two CTAs fit an SM) would take 48 / 76, 65 / 105, 66 / 107, 66 / 107:
+// the edge stands too low. Units as wide as a warp, or as half of one, twice as many steps long, where clusters of all
+// that may share a sequence would leave SMs idle: 16384 x 1 x 1024 49.5 / 76.5 us in whole warps, 40.3 / 69.2 in
+// halves; 16384 x 1 x 2048, which fills them either way, 71 / 117 and 71 / 128. run(SPT, W, CTAs an SM, cluster).
 template <typename Run>
 ard_status glr_steps(ard_ctx* ctx, const GlrArgs& a, int vec, Run run) {
   constexpr std::integral_constant<int, 32> warp{};
@@ -740,8 +748,9 @@ struct GlrBwd {
           return glr_launch(ctx, glr_bwd_kernel<T, VEC, GATE, W, WT, SPT, true>, a, tiles, W * VEC, CL, 256,
                             glr_ring<GlrFeed<T, VEC, GATE ? 4 : 3, W, WT, SPT, true>>(), per_sm, s);
       }
-      // 2-byte values fetched into registers: half the steps a thread, in units of half a warp (a slab is 64 steps, as the states lie), rather than registers
-      // spilt: 2048 x 8 x 2044 192 -> 152 us (4-byte values 118 -> 128, forward 75 -> 82: those stay)
+      // 2-byte values fetched into registers: half the steps a thread, in units of half a warp (a slab is 64 steps, as
+      // the states lie), rather than registers spilt: 2048 x 8 x 2044 192 -> 152 us (4-byte values 118 -> 128, forward
+      // 75 -> 82: those stay)
       if constexpr (SPT == 8 && sizeof(T) == 2)
         return glr_launch(ctx, glr_bwd_kernel<T, VEC, GATE, 16, 16, 4, false>, a, tiles, 16 * VEC, CL, 256, 0, per_sm, s);
       else return glr_launch(ctx, glr_bwd_kernel<T, VEC, GATE, W, WT, SPT, false>, a, tiles, W * VEC, CL, 256, 0, per_sm, s);

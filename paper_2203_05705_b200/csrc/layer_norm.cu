@@ -1,7 +1,8 @@
-// Layer norm over the rows of a matrix, and its adjoint with the reduction of the weight's and the bias's gradient; over all columns or
-// over the compact columns that a row pattern keeps.
+// Layer norm over the rows of a matrix, and its adjoint with the reduction of the weight's and the bias's gradient;
+// over all columns or over the compact columns that a row pattern keeps.
 //
-// One pass over memory bounds both: the forward call reads x and writes y, the backward call reads x and dy and writes dx.
+// One pass over memory bounds both: the forward call reads x and writes y, the backward call reads x and dy and writes
+// dx.
 #include <type_traits>
 
 #include "ard_internal.h"
@@ -27,7 +28,8 @@ __device__ __forceinline__ float ln_get(const __nv_bfloat16* x, size_t i) { retu
 __device__ __forceinline__ void ln_put(float* x, size_t i, float v) { x[i] = v; }
 __device__ __forceinline__ void ln_put(__nv_bfloat16* x, size_t i, float v) { x[i] = __float2bfloat16(v); }
 
-// The device's estimate and a Newton step: within an ulp or two, at a quarter of a root and a quotient's instructions, which every thread of a row spends.
+// The device's estimate and a Newton step: within an ulp or two, at a quarter of a root and a quotient's instructions,
+// which every thread of a row spends.
 __device__ __forceinline__ float ln_rsqrt(float x) {
   const float y = rsqrtf(x), h = y * fmaf(-x * y, y, 1.f);  // an infinite y (x = 0) or a NaN stays what it is
   return isfinite(h) ? fmaf(0.5f, h, y) : y;
@@ -47,8 +49,9 @@ __device__ __forceinline__ float ln_block_sum(float x, float* red) {
   return x;
 }
 
-// Rows of any length, and few short ones: a CTA per row, element by element, the row read again for each sum.  J counts the columns: int, or long long
-// where the number behind the last trip's may pass 2^31 (for all rows: 700 x 1500 forward 6.3 us in place of 4.4).
+// Rows of any length, and few short ones: a CTA per row, element by element, the row read again for each sum.  J counts
+// the columns: int, or long long where the number behind the last trip's may pass 2^31 (for all rows: 700 x 1500
+// forward 6.3 us in place of 4.4).
 constexpr int LN_INT_N = 1 << 30;
 template <typename T, typename J>
 __global__ void __launch_bounds__(LN_ANY_THREADS) ln_fwd_any_kernel(LnShape sh, float eps, const T* X, int ldx, const float* weight,
@@ -159,7 +162,8 @@ __global__ void __launch_bounds__(LN_ANY_THREADS) ln_bwd_any_kernel(LnShape sh, 
   else ln_dw_any(sh, c.n, dY, lddy, X, ldx, mean, rstd, partial, per_slice, k / gx, k % gx, gx);
 }
 
-// The slices' sums added in a fixed order, into the units' places: a warp's lanes take 32 columns, its CTA's warps the slices.
+// The slices' sums added in a fixed order, into the units' places: a warp's lanes take 32 columns, its CTA's warps the
+// slices.
 constexpr int LN_SUM_WARPS = 32;
 __global__ void __launch_bounds__(LN_SUM_WARPS * 32) ln_dw_sum_kernel(LnShape sh, const float* partial, int slices, float* dweight,
                                                                      float* dbias, int zero_fill) {
@@ -173,7 +177,8 @@ __global__ void __launch_bounds__(LN_SUM_WARPS * 32) ln_dw_sum_kernel(LnShape sh
   const int j = blockIdx.x * 32 + lane;
   float t = 0.f;
   if (j < c.n) {
-    // eight at once, asked one by one: left to itself the compiler takes the last seven of a loop after one another, each a trip to the L2
+    // eight at once, asked one by one: left to itself the compiler takes the last seven of a loop after one another,
+    // each a trip to the L2
     for (int k0 = warp; k0 < slices; k0 += 8 * LN_SUM_WARPS) {
       float x[8];
 #pragma unroll
@@ -207,7 +212,8 @@ __global__ void __launch_bounds__(LN_SUM_WARPS * 32) ln_dw_sum_kernel(LnShape sh
 template <typename T>
 constexpr int LN_PER = 16 / (int)sizeof(T);  // elements of a piece
 
-// Two elements in one instruction (f32x2): with one each these kernels run out of issue slots before the memory is busy.
+// Two elements in one instruction (f32x2): with one each these kernels run out of issue slots before the memory is
+// busy.
 __device__ __forceinline__ float2 operator*(float2 a, float2 b) { return __fmul2_rn(a, b); }
 __device__ __forceinline__ float2 operator+(float2 a, float2 b) { return __fadd2_rn(a, b); }
 __device__ __forceinline__ float2 ln_fma(float2 a, float2 b, float2 c) { return __ffma2_rn(a, b, c); }
@@ -226,9 +232,9 @@ __device__ __forceinline__ void ln_unpack(const uint4& q, float2 (&v)[LN_PAIRS<T
     for (int k = 0; k < 2; ++k) v[k] = make_float2(__uint_as_float(w[2 * k]), __uint_as_float(w[2 * k + 1]));
   }
 }
-// The piece of column j from shared memory, elements from column n on as zero.  RAGGED: n may end inside a piece (asked once for all rows: the
-// questions, predicated rather than branched around, were two thirds of the instructions).  Without ON16 the row begins at byte `off` of its place: the
-// piece is cut out of the 32 bytes that it lies in.
+// The piece of column j from shared memory, elements from column n on as zero.  RAGGED: n may end inside a piece (asked
+// once for all rows: the questions, predicated rather than branched around, were two thirds of the instructions).
+// Without ON16 the row begins at byte `off` of its place: the piece is cut out of the 32 bytes that it lies in.
 template <typename T, bool RAGGED, bool ON16>
 __device__ __forceinline__ void ln_piece(const uint8_t* row, int off, int j, int n, float2 (&v)[LN_PAIRS<T>]) {
   uint4 q = make_uint4(0u, 0u, 0u, 0u);
@@ -305,8 +311,8 @@ __device__ __forceinline__ void ln_params(const float* w, float other, const LnC
     v[k].y = w && j + 2 * k + 1 < c.n ? w[c.b0 + (size_t)(j + 2 * k + 1) * c.dp] : other;
   }
 }
-// The same of whole pieces on 16 bytes, all columns kept; not to be kept in registers (CTAs of 1024 threads, 64 registers each): they come from
-// the L1 cache for every row.
+// The same of whole pieces on 16 bytes, all columns kept; not to be kept in registers (CTAs of 1024 threads, 64
+// registers each): they come from the L1 cache for every row.
 template <int PAIRS>
 __device__ __forceinline__ void ln_params_now(const float* w, float other, int j, float2 (&v)[PAIRS]) {
 #pragma unroll
@@ -318,8 +324,8 @@ __device__ __forceinline__ void ln_params_now(const float* w, float other, int j
   }
 }
 
-// The sums of M values over the TPR threads of a row; with more than a warp through shared memory, of which a call and the next use
-// different halves (one barrier of the group per call).
+// The sums of M values over the TPR threads of a row; with more than a warp through shared memory, of which a call and
+// the next use different halves (one barrier of the group per call).
 template <int TPR, int M>
 __device__ __forceinline__ void ln_row_sums(float (&x)[M], float (*red)[M][32], int& half) {
 #pragma unroll
@@ -345,9 +351,10 @@ __device__ __forceinline__ void ln_row_sums(float (&x)[M], float (*red)[M][32], 
   }
 }
 
-// Rows reach the TPR threads that hold them through a ring of slots in shared memory, filled by bulk copies that the first of them asks for
-// several rounds ahead: what is in flight costs no registers, and 100 to 200 KB an SM are in flight whatever the row's length.  A round is R
-// consecutive rows: their sums share barriers and run beside one another.
+// Rows reach the TPR threads that hold them through a ring of slots in shared memory, filled by bulk copies that the
+// first of them asks for several rounds ahead: what is in flight costs no registers, and 100 to 200 KB an SM are in
+// flight whatever the row's length.  A round is R consecutive rows: their sums share barriers and run beside one
+// another.
 constexpr int LN_SLOTS = 8;
 struct LnRing {
   int slots;      // per group of threads
@@ -424,7 +431,8 @@ struct LnRows {
       phase ^= 1;
     }
   }
-  // Before the CTA ends without some of its copies (asked up to round `asked`): they get the same time, for they write to its memory.
+  // Before the CTA ends without some of its copies (asked up to round `asked`): they get the same time, for they write
+  // to its memory.
   __device__ __forceinline__ void drain(int asked) const {
     for (int it = gone_at; it <= asked && it < rounds && row(it, 0) < rows; ++it) {
       bool ok = false;
@@ -445,8 +453,8 @@ __device__ __forceinline__ void ln_setup(uint64_t (*full)[LN_SLOTS], int slots, 
   pdl_wait_prior_grids();
 }
 
-// Forward: two sums over a row's registers, the second about the mean (a sum of squares alone loses the variance of a row with a large
-// mean).  The barrier of the first one says that the round's slot has been read.
+// Forward: two sums over a row's registers, the second about the mean (a sum of squares alone loses the variance of a
+// row with a large mean).  The barrier of the first one says that the round's slot has been read.
 template <typename T, int TPR, int V, int NT, int R, bool ON16>
 __global__ void __launch_bounds__(NT, NT >= 512 ? 1 : 512 / NT) ln_fwd_kernel(LnShape sh, float eps, const T* X, int ldx, const float* weight, const float* bias,
                                                        T* Y, int ldy, float* mean, float* rstd, LnRing ring, int* status) {
@@ -547,9 +555,10 @@ __global__ void __launch_bounds__(NT, NT >= 512 ? 1 : 512 / NT) ln_fwd_kernel(Ln
   if (in.gone && t == 0) in.drain(in.gone_at + ring.slots - 1);
 }
 
-// Backward: a thread keeps its columns' sums for the weight and the bias over all rows of the CTA and leaves them in `partial`
-// [CTA][2][N].  A row is read from its slot twice, for its sums and for dx, which costs less than the registers that would hold it; its slot is
-// asked for again one round later: the barrier of that round's sums says that nobody reads it any more.
+// Backward: a thread keeps its columns' sums for the weight and the bias over all rows of the CTA and leaves them in
+// `partial` [CTA][2][N].  A row is read from its slot twice, for its sums and for dx, which costs less than the
+// registers that would hold it; its slot is asked for again one round later: the barrier of that round's sums says that
+// nobody reads it any more.
 template <typename T, int TPR, int V, int NT, int R, bool ON16>
 __global__ void __launch_bounds__(NT, NT >= 512 ? 1 : 512 / NT) ln_bwd_kernel(LnShape sh, const T* dY, int lddy, const T* X, int ldx, const float* weight,
                                                        const float* mean, const float* rstd, T* dX, int lddx, float* partial,
@@ -872,8 +881,9 @@ __global__ void __launch_bounds__(LN_SHORT, 2) ln_bwd_short_kernel(LnShape sh, c
 
 inline bool ln_on16(const void* p, long long ld_bytes) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0 && ld_bytes % 16 == 0; }
 
-// A CTA for each of a few short rows, all of them at once, rather than rings, whose setup takes longer than their rows: backward up to this many rows
-// (700 x 1500 7.5 us, with rings 8.9 and, off the 16-byte grid, 11.2; 148 x 2048 5.5 and 7.6; 2000 x 1024 11.6 and 9.5).
+// A CTA for each of a few short rows, all of them at once, rather than rings, whose setup takes longer than their rows:
+// backward up to this many rows (700 x 1500 7.5 us, with rings 8.9 and, off the 16-byte grid, 11.2; 148 x 2048 5.5 and
+// 7.6; 2000 x 1024 11.6 and 9.5).
 inline bool ln_few(int rows, int N, int sms) { return rows <= 8 * sms && N <= 2048; }
 
 // Calls run(TPR, WIDE) for short rows.
@@ -889,8 +899,9 @@ void ln_short(const LnShape& sh, bool wide, Run run) {
 }
 
 enum { LN_FORWARD, LN_BACKWARD, LN_FEW };
-// Calls run(TPR, V, NT) (as integral constants) for rows of N elements: 16 elements a thread, 8 in short rows.  LN_FEW: in CTAs of 128 threads, which spread
-// over the SMs (forward, 148 x 2048: 2.7 us, a CTA a row 3.6).  False: the row is too long.
+// Calls run(TPR, V, NT) (as integral constants) for rows of N elements: 16 elements a thread, 8 in short rows.  LN_FEW:
+// in CTAs of 128 threads, which spread over the SMs (forward, 148 x 2048: 2.7 us, a CTA a row 3.6).  False: the row is
+// too long.
 template <typename T, int KIND, typename Run>
 bool ln_groups(int N, Run run) {
   constexpr int PER = LN_PER<T>, V = 16 / PER;
@@ -917,8 +928,8 @@ bool ln_groups(int N, Run run) {
 #undef LN_TRY
   return false;
 }
-// Two rows a round, or one where that leaves groups without rows, where the slots do not fit, and in CTAs of 1024 threads.  M operands.  run(R, CTAs an
-// SM, CTAs, slots); false: not even two rows fit.
+// Two rows a round, or one where that leaves groups without rows, where the slots do not fit, and in CTAs of 1024
+// threads.  M operands.  run(R, CTAs an SM, CTAs, slots); false: not even two rows fit.
 constexpr int LN_SMEM = 200 << 10;  // of an SM, for the slots of its CTAs
 template <int NT, int G, int M, typename Run>
 bool ln_rounds(const ard_ctx* ctx, int rows, int row_bytes, Run run) {
