@@ -787,6 +787,48 @@ ard_status ard_adamw_step(ard_ctx* ctx, const ard_adamw_tensor* tensors, int n_t
 ard_status ard_grad_norm(ard_ctx* ctx, const ard_adamw_tensor* tensors, int n_tensors, double max_norm, float* out,
                          void* cuda_stream);
 
+/* ---- embedding -------------------------------------------------------------------------------
+ * (Not in the paper: what stands below the first layer of a language model.)  Row r of Y is the table's row of token ids[r], scaled:
+ *   Y[r][j] = alpha * table[ids[r]][j].
+ * pat NULL: j < N.  pat (a row pattern over N units): Y and dY are COMPACT over the kept units (column j = kept unit j, leading
+ * dimensions >= N), the table is full width; alpha may carry the rescale of the dropout.  Columns >= n are neither read nor
+ * written.  ids int32 [rows]: a negative one is padding, its row of Y is zero and adds nothing to the gradient; so is one of V
+ * or more, and the device status becomes ARD_ERR_INVALID_ARG.
+ * table [V][N] and Y of element type `dtype`, from any whole element on (fastest with 16-byte aligned pointers and rows); the product with alpha
+ * is fp32.  Y must not overlap the table.  Errors: as ard_layer_norm_fwd.  Asynchronous. */
+ard_status ard_embedding_fwd(ard_ctx* ctx, const ard_pattern* pat, ard_dtype dtype, int rows, int V, int N, float alpha,
+                             const int32_t* ids, const void* table, int ldt, void* Y, int ldy, void* cuda_stream);
+/* Its adjoint:  dtable[v][j] (+)= alpha * sum over r with ids[r] = v of dY[r][j],  dtable fp32 [V][N], full width.  accumulate
+ * = 0: all of it is written, tokens that no row holds and dropped units as zero; accumulate != 0: added to what stands there (the output
+ * layer's gradient where both share the table), the rest is left.  Sums are fp32 in an order that the sizes fix: the same inputs give the same
+ * bits.  Asynchronous. */
+ard_status ard_embedding_bwd(ard_ctx* ctx, const ard_pattern* pat, ard_dtype dtype, int rows, int V, int N, float alpha,
+                             const int32_t* ids, const void* dY, int lddy, float* dtable, int lddt, int accumulate,
+                             void* cuda_stream);
+
+/* ---- loss ------------------------------------------------------------------------------------
+ * (Not in the paper: what stands above the output layer.)  For every row z of the logits Z [rows][V], with its label and a
+ * teacher's k top logits t over the tokens id, p = softmax(t / tau) over those k:
+ *   loss[r] = hard * (log sum_j exp z_j - z_label) + soft * tau^2 * sum_i p_i (log p_i - log softmax(z / tau)_{id_i}),
+ *   dZ[r][j] = w_r * (hard * (softmax(z)_j - [j = label]) + soft * tau * (softmax(z / tau)_j - sum of p_i with id_i = j)),
+ *   total = sum over r of w_r * loss[r].
+ *   labels         int32 [rows] or NULL (no row has one); a negative label: the row has none.
+ *   teacher_ids    int32 [rows][k] with leading dimension ldk; entries that are negative, or whose logit is -infinity, do not
+ *                  count, and a row where none counts has no teacher; a token may come up twice.  NULL with k = 0.
+ *   teacher_logits fp32, laid out alike.
+ *   row_weight     fp32 [rows], w_r, or NULL (1).  A row whose weight is 0, or with neither label nor teacher (hard = 0 and soft = 0
+ *                  take them away), is not read: its loss is 0 and its gradient zeros.
+ *   loss           fp32 [rows]; total: fp32 on the device, summed in fp64 in a fixed order, or NULL.
+ *   dZ             like Z (lddz), or NULL: not wanted.  May be Z itself, else must not overlap it.
+ * Labels and teacher's tokens of V or more count as absent, and the device status becomes ARD_ERR_INVALID_ARG.  Logits of -infinity are classes
+ * without probability; a row of nothing else gives NaN.  Z, dZ of element type `dtype`, from any whole element on; sums are fp32.
+ * Uses the context's scratch.  Errors: ARD_ERR_INVALID_ARG (NULL, negative size, dtype, tau not positive or not finite, also its inverse, hard or soft not
+ * finite), ARD_ERR_SHAPE (leading dimension below V or k), ARD_ERR_ALIGNMENT (a pointer inside an element), ARD_ERR_UNSUPPORTED
+ * (k above 1024, rows above 2^30).  Asynchronous. */
+ard_status ard_distill_loss(ard_ctx* ctx, ard_dtype dtype, int rows, int V, const void* Z, int ldz, const int32_t* labels, int k,
+                            const int32_t* teacher_ids, const float* teacher_logits, int ldk, float tau, float hard, float soft,
+                            const float* row_weight, float* loss, float* total, void* dZ, int lddz, void* cuda_stream);
+
 /* ---- status ---------------------------------------------------------------------------------- */
 
 /* Synchronises `cuda_stream`, returns the sticky device status word (ARD_OK if no kernel reported

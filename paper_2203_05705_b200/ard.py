@@ -44,6 +44,7 @@ EXPORTS = [
     "ard_blocks_create", "ard_blocks_destroy", "ard_blocks_predict", "ard_blocks_set_label", "ard_blocks_sample",
     "ard_blocks_fwd", "ard_blocks_bwd_weight", "ard_blocks_bwd_input", "ard_blocks_to_host", "ard_blocks_pattern", "ard_dropout_schedule", "ard_blocks_products",
     "ard_layer_norm_fwd", "ard_layer_norm_bwd", "ard_glr_forward", "ard_glr_backward", "ard_adamw_step", "ard_grad_norm",
+    "ard_embedding_fwd", "ard_embedding_bwd", "ard_distill_loss",
 ]
 
 _lib = None
@@ -160,6 +161,9 @@ def lib():
         "ard_glr_backward": [vp, vp, i32, i32, i32, i32, f32, vp, vp, vp, i32, vp, vp, vp, i32, vp, vp, vp, vp, i32, vp, vp],
         "ard_adamw_step": [vp, P(AdamwTensor), i32, C.c_double, C.c_double, C.c_double, C.c_double, i32, u64, u64, vp, vp, vp, vp],
         "ard_grad_norm": [vp, P(AdamwTensor), i32, C.c_double, vp, vp],
+        "ard_embedding_fwd": [vp, vp, i32, i32, i32, i32, f32, vp, vp, i32, vp, i32, vp],
+        "ard_embedding_bwd": [vp, vp, i32, i32, i32, i32, f32, vp, vp, i32, vp, i32, i32, vp],
+        "ard_distill_loss": [vp, i32, i32, i32, vp, i32, vp, i32, vp, vp, i32, f32, f32, f32, vp, vp, vp, vp, i32, vp],
     }
     for name, args in sig.items():
         fn = getattr(L, name)
@@ -496,6 +500,21 @@ def ard_adamw_step(ctx, tensors, n_tensors, lr, beta1, beta2, eps, state_bits, s
 def ard_grad_norm(ctx, tensors, n_tensors, max_norm, out, stream=None):
     """`tensors`: the array made by adamw_tensors()."""
     _check(lib().ard_grad_norm(ctx, tensors, n_tensors, max_norm, _ptr(out), _stream(stream)), "ard_grad_norm")
+
+
+def ard_embedding_fwd(ctx, pat, dtype, rows, V, N, alpha, ids, table, ldt, Y, ldy, stream=None):
+    _check(_calls().ard_embedding_fwd(ctx, pat, dtype, rows, V, N, alpha, ids, table, ldt, Y, ldy, _stream(stream)), "ard_embedding_fwd")
+
+
+def ard_embedding_bwd(ctx, pat, dtype, rows, V, N, alpha, ids, dY, lddy, dtable, lddt, accumulate, stream=None):
+    _check(_calls().ard_embedding_bwd(ctx, pat, dtype, rows, V, N, alpha, ids, dY, lddy, dtable, lddt, 1 if accumulate else 0,
+                                      _stream(stream)), "ard_embedding_bwd")
+
+
+def ard_distill_loss(ctx, dtype, rows, V, Z, ldz, labels, k, teacher_ids, teacher_logits, ldk, tau, hard, soft, row_weight, loss, total, dZ,
+                     lddz, stream=None):
+    _check(_calls().ard_distill_loss(ctx, dtype, rows, V, Z, ldz, labels, k, teacher_ids, teacher_logits, ldk, tau, hard, soft, row_weight,
+                                     loss, total, dZ, lddz, _stream(stream)), "ard_distill_loss")
 
 
 def ard_dropout_schedule(n_epochs, p_total, mean_epoch, var_epoch, lam, p_max=1.0):

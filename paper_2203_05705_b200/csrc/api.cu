@@ -1834,6 +1834,47 @@ ard_status ard_grad_norm(ard_ctx* ctx, const ard_adamw_tensor* tensors, int n_te
   return launch_grad_norm(ctx, tensors, n_tensors, max_norm, out, (cudaStream_t)cuda_stream);
 }
 
+ard_status ard_embedding_fwd(ard_ctx* ctx, const ard_pattern* pat, ard_dtype dtype, int rows, int V, int N, float alpha, const int32_t* ids,
+                             const void* table, int ldt, void* Y, int ldy, void* cuda_stream) {
+  const ard_status st = layer_norm_check(ctx, pat, dtype, rows, N);
+  if (st != ARD_OK) return st;
+  if (V < 0 || (rows > 0 && (!ids || !table || !Y || Y == table))) return ARD_ERR_INVALID_ARG;
+  if (ldt < N || ldy < N) return ARD_ERR_SHAPE;
+  if (off_elements(element_bytes(dtype), {table, Y}) || off_elements(4, {ids})) return ARD_ERR_ALIGNMENT;
+  DeviceGuard guard(ctx->device);
+  return launch_embedding_fwd(ctx, pat ? pat->d_hdr : nullptr, dtype, rows, V, N, alpha, ids, table, ldt, Y, ldy, (cudaStream_t)cuda_stream);
+}
+
+ard_status ard_embedding_bwd(ard_ctx* ctx, const ard_pattern* pat, ard_dtype dtype, int rows, int V, int N, float alpha, const int32_t* ids,
+                             const void* dY, int lddy, float* dtable, int lddt, int accumulate, void* cuda_stream) {
+  const ard_status st = layer_norm_check(ctx, pat, dtype, rows, N);
+  if (st != ARD_OK) return st;
+  if (V < 0 || (rows > 0 && (!ids || !dY || dtable == dY)) || (V > 0 && !dtable)) return ARD_ERR_INVALID_ARG;
+  if (lddy < N || lddt < N) return ARD_ERR_SHAPE;
+  if (off_elements(element_bytes(dtype), {dY}) || off_elements(4, {ids, dtable})) return ARD_ERR_ALIGNMENT;
+  DeviceGuard guard(ctx->device);
+  return launch_embedding_bwd(ctx, pat ? pat->d_hdr : nullptr, dtype, rows, V, N, alpha, ids, dY, lddy, dtable, lddt, accumulate ? 1 : 0,
+                              (cudaStream_t)cuda_stream);
+}
+
+ard_status ard_distill_loss(ard_ctx* ctx, ard_dtype dtype, int rows, int V, const void* Z, int ldz, const int32_t* labels, int k,
+                            const int32_t* teacher_ids, const float* teacher_logits, int ldk, float tau, float hard, float soft,
+                            const float* row_weight, float* loss, float* total, void* dZ, int lddz, void* cuda_stream) {
+  const ard_status st = layer_norm_check(ctx, nullptr, dtype, rows, V);
+  if (st != ARD_OK) return st;
+  if (k < 0 || (rows > 0 && (!Z || !loss || loss == total || (k > 0 && (!teacher_ids || !teacher_logits))))) return ARD_ERR_INVALID_ARG;
+  if (!(tau > 0.f) || !(tau < INFINITY) || !(1.4426950408889634 / (double)tau < 3.4028234663852886e38)) return ARD_ERR_INVALID_ARG;
+  if (!(fabsf(hard) < INFINITY) || !(fabsf(soft) < INFINITY) || !(fabsf(soft * tau * tau) < INFINITY)) return ARD_ERR_INVALID_ARG;
+  if (ldz < V || (dZ && lddz < V) || ldk < k) return ARD_ERR_SHAPE;
+  if (dZ && dZ == Z && lddz != ldz) return ARD_ERR_SHAPE;
+  if (k > 1024) return ARD_ERR_UNSUPPORTED;
+  if (off_elements(element_bytes(dtype), {Z, dZ}) || off_elements(4, {labels, teacher_ids, teacher_logits, row_weight, loss, total}))
+    return ARD_ERR_ALIGNMENT;
+  DeviceGuard guard(ctx->device);
+  return launch_distill_loss(ctx, dtype, rows, V, Z, ldz, labels, k, teacher_ids, teacher_logits, ldk, tau, hard, soft, row_weight, loss, total, dZ,
+                             lddz, (cudaStream_t)cuda_stream);
+}
+
 ard_status ard_last_device_status(ard_ctx* ctx, void* cuda_stream) {
   if (!ctx) return ARD_ERR_INVALID_ARG;
   DeviceGuard guard(ctx->device);

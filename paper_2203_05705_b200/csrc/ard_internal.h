@@ -341,6 +341,15 @@ ard_status launch_adamw(ard_ctx* ctx, const ard_adamw_tensor* tensors, int n_ten
                         cudaStream_t s);
 ard_status launch_grad_norm(ard_ctx* ctx, const ard_adamw_tensor* tensors, int n_tensors, double max_norm, float* out, cudaStream_t s);
 
+// Embedding (embedding.cu), loss (distill.cu).
+ard_status launch_embedding_fwd(ard_ctx* ctx, const int32_t* hdr, ard_dtype dtype, int rows, int V, int N, float alpha, const int32_t* ids,
+                                const void* table, int ldt, void* Y, int ldy, cudaStream_t s);
+ard_status launch_embedding_bwd(ard_ctx* ctx, const int32_t* hdr, ard_dtype dtype, int rows, int V, int N, float alpha, const int32_t* ids,
+                                const void* dY, int lddy, float* dtable, int lddt, int accumulate, cudaStream_t s);
+ard_status launch_distill_loss(ard_ctx* ctx, ard_dtype dtype, int rows, int V, const void* Z, long long ldz, const int32_t* labels, int k,
+                               const int32_t* t_ids, const float* t, int ldk, float tau, float hard, float soft, const float* weight,
+                               float* loss, float* total, void* dZ, long long lddz, cudaStream_t s);
+
 // ---- programmatic dependent launch ----------------------------------------------------------------
 // Every kernel of the library is launched so that its blocks may become resident while the previous
 // kernel of the stream is still draining: the block set-up (barriers, tensor memory, index arithmetic)
