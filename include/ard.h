@@ -737,6 +737,44 @@ ard_status ard_glr_backward(ard_ctx* ctx, const ard_pattern* pat, ard_dtype dtyp
                             const void* dY, int lddy, const float* dhT, void* dZf, void* dZg, void* dZo, int lddz,
                             float* dh0, void* cuda_stream);
 
+/* ---- gated delta rule ------------------------------------------------------------------------
+ * (Not in the paper: the recurrence above with a matrix for a state, which a step writes to where its key points.)  For every sequence b
+ * and head, with a state S [Dk][Dv], s the logistic function, q and k divided by sqrt(sum of their squares + eps):
+ *   f = s(Zf[t][b][head]),  beta = s(Zb[t][b][head]),  u = beta * (v_t - f * S_{t-1}^T k_t),  S_t = f * S_{t-1} + k_t u^T,
+ *   Y[t][b] = scale * S_t^T q_t.
+ * Q, K [T*B] rows of heads * Dk columns (leading dimensions ldq, ldk), V and Y of heads * Dv, Zf and Zb of heads (ldz): matrices of their own,
+ * or column blocks of one.  eps < 0: q and k are taken as they are; a row of zeros with eps = 0 stays zeros.
+ *   lens  int32 [B] or NULL: sequence b has min(max(lens[b], 0), T) steps.  Rows behind its end are not read; in Y they
+ *         are written as zero, and the state stays what it was.
+ *   h0    fp32 [B][heads][Dk][Dv], the state before the first step; NULL: zero.
+ *   hT    the state after the last step, like h0, or NULL.  May be h0.
+ *   S     fp32 [ceil(T / ARD_DELTA_CHUNK)][B][heads][Dk][Dv], what the backward call starts from, or NULL when there is none.
+ *   work  device memory of ard_delta_work_bytes(T, B, heads, Dk, Dv, 0 or, for the backward call, 1) bytes, from any byte on; holds nothing between
+ *         calls, so one piece serves many layers whose calls are ordered.  NULL where that is 0 (decoding).
+ * Decoding is T = 1 with hT = h0.  A gate of -infinity (f = 0) starts anew.  Q, K, V, Z, Y are ARD_BF16, from any whole element on (fastest
+ * with 16-byte aligned pointers and rows, Dk and Dv multiples of 8); gates, states and their products are fp32.  Y must not overlap an input.
+ * Errors: ARD_ERR_INVALID_ARG (NULL, negative size, unknown dtype, scale or eps not finite), ARD_ERR_SHAPE (leading dimension too small),
+ * ARD_ERR_ALIGNMENT (a pointer inside an element), ARD_ERR_NOMEM (work_bytes too small), ARD_ERR_UNSUPPORTED (ARD_F32, Dk or Dv above 128, T
+ * above 2^30, more than 2^31 - 1 chunks or blocks of 32 columns over all sequences and heads).  Asynchronous. */
+#define ARD_DELTA_CHUNK 64
+size_t ard_delta_work_bytes(int T, int B, int heads, int Dk, int Dv, int backward);
+ard_status ard_delta_forward(ard_ctx* ctx, ard_dtype dtype, int T, int B, int heads, int Dk, int Dv, float scale, float eps, const void* Q,
+                             int ldq, const void* K, int ldk, const void* V, int ldv, const void* Zf, const void* Zb, int ldz,
+                             const int32_t* lens, const float* h0, void* Y, int ldy, float* hT, float* S, void* work,
+                             size_t work_bytes, void* cuda_stream);
+/* Its adjoint: with D = dhT behind the last step, for t = T-1 .. 0
+ *   D += scale * q_t dY_t^T,  du = D^T k_t,  dV = beta * du,  dZb = (1 - beta) * du . u,  dq_t = scale * S_t dY_t,
+ *   dk_t = D u - beta f * S_{t-1} du,  D = f * (D - beta k_t du^T),  dZf = (1 - f) * <D, S_{t-1}>,
+ * then dQ and dK through the division by the lengths, and dh0 = D in the end.  The steps inside a chunk are computed again from S;
+ * Y is not needed.  dQ, dK, dV, dZf, dZb have the layout of Q, K, V, Zf, Zb; all five are written, rows behind a sequence's end
+ * as zero.  dhT, dh0 like h0, either may be NULL (zero; not wanted); dh0 may be dhT.  Gradients must not overlap an input or one another.  The same
+ * inputs give the same bits.  Asynchronous. */
+ard_status ard_delta_backward(ard_ctx* ctx, ard_dtype dtype, int T, int B, int heads, int Dk, int Dv, float scale, float eps, const void* Q,
+                              int ldq, const void* K, int ldk, const void* V, int ldv, const void* Zf, const void* Zb, int ldz,
+                              const int32_t* lens, const float* S, const void* dY, int lddy, const float* dhT, void* dQ, int lddq,
+                              void* dK, int lddk, void* dV, int lddv, void* dZf, void* dZb, int lddz, float* dh0, void* work,
+                              size_t work_bytes, void* cuda_stream);
+
 /* ---- optimiser -------------------------------------------------------------------------------
  * (Not in the paper: what a training loop does with the gradients of ard_mlp_step and the other backward calls.) */
 typedef struct ard_adamw_tensor {

@@ -29,7 +29,7 @@ ARD_PATH_AUTO, ARD_PATH_CUDA_CORE, ARD_PATH_TENSOR_CORE = 0, 1, 2
 (ARD_OPT_PDL, ARD_OPT_PDL_IN_CAPTURE, ARD_OPT_SIDE_STREAMS, ARD_OPT_CTA_PAIRS, ARD_OPT_BAND_ROWS,
  ARD_OPT_MLP_PERSISTENT, ARD_OPT_LSTM_COMPACT_H, ARD_OPT_LSTM_REFUSE) = range(8)
 ARD_STATIC_SCRATCH_BYTES = 8 << 20
-ARD_GLR_CHUNK, ARD_ADAMW_BLOCK = 64, 128
+ARD_GLR_CHUNK, ARD_DELTA_CHUNK, ARD_ADAMW_BLOCK = 64, 64, 128
 
 EXPORTS = [
     "ard_create", "ard_destroy", "ard_set_path", "ard_set_option", "ard_set_tile_n", "ard_set_shared_tail", "ard_set_compact_reuse", "ard_set_distribution", "ard_quantise_distribution", "ard_search_distribution", "ard_get_distribution_cdf",
@@ -44,7 +44,7 @@ EXPORTS = [
     "ard_blocks_create", "ard_blocks_destroy", "ard_blocks_predict", "ard_blocks_set_label", "ard_blocks_sample",
     "ard_blocks_fwd", "ard_blocks_bwd_weight", "ard_blocks_bwd_input", "ard_blocks_to_host", "ard_blocks_pattern", "ard_dropout_schedule", "ard_blocks_products",
     "ard_layer_norm_fwd", "ard_layer_norm_bwd", "ard_glr_forward", "ard_glr_backward", "ard_adamw_step", "ard_grad_norm",
-    "ard_embedding_fwd", "ard_embedding_bwd", "ard_distill_loss",
+    "ard_delta_work_bytes", "ard_delta_forward", "ard_delta_backward", "ard_embedding_fwd", "ard_embedding_bwd", "ard_distill_loss",
 ]
 
 _lib = None
@@ -161,6 +161,9 @@ def lib():
         "ard_glr_backward": [vp, vp, i32, i32, i32, i32, f32, vp, vp, vp, i32, vp, vp, vp, i32, vp, vp, vp, vp, i32, vp, vp],
         "ard_adamw_step": [vp, P(AdamwTensor), i32, C.c_double, C.c_double, C.c_double, C.c_double, i32, u64, u64, vp, vp, vp, vp],
         "ard_grad_norm": [vp, P(AdamwTensor), i32, C.c_double, vp, vp],
+        "ard_delta_forward": [vp, i32, i32, i32, i32, i32, i32, f32, f32, vp, i32, vp, i32, vp, i32, vp, vp, i32, vp, vp, vp, i32, vp, vp, vp, sz, vp],
+        "ard_delta_backward": [vp, i32, i32, i32, i32, i32, i32, f32, f32, vp, i32, vp, i32, vp, i32, vp, vp, i32, vp, vp, vp, i32, vp, vp, i32, vp, i32,
+                               vp, i32, vp, vp, i32, vp, vp, sz, vp],
         "ard_embedding_fwd": [vp, vp, i32, i32, i32, i32, f32, vp, vp, i32, vp, i32, vp],
         "ard_embedding_bwd": [vp, vp, i32, i32, i32, i32, f32, vp, vp, i32, vp, i32, i32, vp],
         "ard_distill_loss": [vp, i32, i32, i32, vp, i32, vp, i32, vp, vp, i32, f32, f32, f32, vp, vp, vp, vp, i32, vp],
@@ -170,6 +173,8 @@ def lib():
         fn.argtypes = args
         fn.restype = i32
     L.ard_launch_count.restype = u64
+    L.ard_delta_work_bytes.argtypes = [i32] * 6
+    L.ard_delta_work_bytes.restype = sz
     L.ard_blocks_pattern.argtypes = [vp]
     L.ard_blocks_pattern.restype = vp
     L.ard_status_string.argtypes = [i32]
@@ -500,6 +505,23 @@ def ard_adamw_step(ctx, tensors, n_tensors, lr, beta1, beta2, eps, state_bits, s
 def ard_grad_norm(ctx, tensors, n_tensors, max_norm, out, stream=None):
     """`tensors`: the array made by adamw_tensors()."""
     _check(lib().ard_grad_norm(ctx, tensors, n_tensors, max_norm, _ptr(out), _stream(stream)), "ard_grad_norm")
+
+
+def ard_delta_work_bytes(T, B, heads, Dk, Dv, backward):
+    """Bytes of device memory that ard_delta_forward (backward = False) or ard_delta_backward wants for `work`."""
+    return int(lib().ard_delta_work_bytes(T, B, heads, Dk, Dv, 1 if backward else 0))
+
+
+def ard_delta_forward(ctx, dtype, T, B, heads, Dk, Dv, scale, eps, Q, ldq, K, ldk, V, ldv, Zf, Zb, ldz, lens, h0, Y, ldy, hT, S, work, work_bytes,
+                      stream=None):
+    _check(_calls().ard_delta_forward(ctx, dtype, T, B, heads, Dk, Dv, scale, eps, Q, ldq, K, ldk, V, ldv, Zf, Zb, ldz, lens, h0, Y, ldy, hT, S,
+                                      work, work_bytes, _stream(stream)), "ard_delta_forward")
+
+
+def ard_delta_backward(ctx, dtype, T, B, heads, Dk, Dv, scale, eps, Q, ldq, K, ldk, V, ldv, Zf, Zb, ldz, lens, S, dY, lddy, dhT, dQ, lddq, dK, lddk,
+                       dV, lddv, dZf, dZb, lddz, dh0, work, work_bytes, stream=None):
+    _check(_calls().ard_delta_backward(ctx, dtype, T, B, heads, Dk, Dv, scale, eps, Q, ldq, K, ldk, V, ldv, Zf, Zb, ldz, lens, S, dY, lddy, dhT, dQ,
+                                       lddq, dK, lddk, dV, lddv, dZf, dZb, lddz, dh0, work, work_bytes, _stream(stream)), "ard_delta_backward")
 
 
 def ard_embedding_fwd(ctx, pat, dtype, rows, V, N, alpha, ids, table, ldt, Y, ldy, stream=None):

@@ -1787,6 +1787,72 @@ ard_status ard_glr_backward(ard_ctx* ctx, const ard_pattern* pat, ard_dtype dtyp
                              lddz, dh0, (cudaStream_t)cuda_stream);
 }
 
+static ard_status delta_check(ard_ctx* ctx, ard_dtype dtype, int T, int B, int heads, int Dk, int Dv, float scale, float eps, const void* Q, int ldq,
+                              const void* K, int ldk, const void* V, int ldv, const void* Zf, const void* Zb, int ldz) {
+  if (!ctx || T < 0 || B < 0 || heads < 0 || Dk < 0 || Dv < 0) return ARD_ERR_INVALID_ARG;
+  if (dtype != ARD_F32 && dtype != ARD_BF16) return ARD_ERR_INVALID_ARG;
+  if (!(fabsf(scale) < INFINITY) || !(fabsf(eps) < INFINITY)) return ARD_ERR_INVALID_ARG;
+  if (T > 0 && (!Q || !K || !V || !Zf || !Zb)) return ARD_ERR_INVALID_ARG;
+  if (dtype == ARD_F32 || Dk > 128 || Dv > 128 || T > (1 << 30)) return ARD_ERR_UNSUPPORTED;
+  const long long most = 0x7FFFFFFFll, n = (long long)B * heads;
+  if (n * 4 > most || (T > 0 && n > most / ((T + ARD_DELTA_CHUNK - 1) / ARD_DELTA_CHUNK))) return ARD_ERR_UNSUPPORTED;
+  if (ldq < (long long)heads * Dk || ldk < (long long)heads * Dk || ldv < (long long)heads * Dv || ldz < heads) return ARD_ERR_SHAPE;
+  return ARD_OK;
+}
+
+size_t ard_delta_work_bytes(int T, int B, int heads, int Dk, int Dv, int backward) {
+  if (T < 0 || B < 0 || heads < 0 || Dk < 0 || Dv < 0 || Dk > 128 || Dv > 128) return 0;
+  return delta_work_bytes(T, B, heads, Dk, Dv, backward != 0);
+}
+
+ard_status ard_delta_forward(ard_ctx* ctx, ard_dtype dtype, int T, int B, int heads, int Dk, int Dv, float scale, float eps, const void* Q, int ldq,
+                             const void* K, int ldk, const void* V, int ldv, const void* Zf, const void* Zb, int ldz, const int32_t* lens,
+                             const float* h0, void* Y, int ldy, float* hT, float* S, void* work, size_t work_bytes, void* cuda_stream) {
+  const ard_status st = delta_check(ctx, dtype, T, B, heads, Dk, Dv, scale, eps, Q, ldq, K, ldk, V, ldv, Zf, Zb, ldz);
+  if (st != ARD_OK) return st;
+  if (T > 0) {
+    if (!Y || (S && (S == h0 || S == hT))) return ARD_ERR_INVALID_ARG;
+    for (const void* in : {Q, K, V, Zf, Zb})
+      if (Y == in) return ARD_ERR_INVALID_ARG;
+    if (ldy < (long long)heads * Dv) return ARD_ERR_SHAPE;
+  }
+  if (off_elements(2, {Q, K, V, Zf, Zb, Y}) || off_elements(4, {lens, h0, hT, S})) return ARD_ERR_ALIGNMENT;
+  const size_t need = delta_work_bytes(T, B, heads, Dk, Dv, false);
+  if (need > 0 && !work) return ARD_ERR_INVALID_ARG;
+  if (work_bytes < need) return ARD_ERR_NOMEM;
+  DeviceGuard guard(ctx->device);
+  return launch_delta_forward(ctx, T, B, heads, Dk, Dv, scale, eps, Q, ldq, K, ldk, V, ldv, Zf, Zb, ldz, lens, h0, Y, ldy, hT, S, work,
+                              (cudaStream_t)cuda_stream);
+}
+
+ard_status ard_delta_backward(ard_ctx* ctx, ard_dtype dtype, int T, int B, int heads, int Dk, int Dv, float scale, float eps, const void* Q, int ldq,
+                              const void* K, int ldk, const void* V, int ldv, const void* Zf, const void* Zb, int ldz, const int32_t* lens,
+                              const float* S, const void* dY, int lddy, const float* dhT, void* dQ, int lddq, void* dK, int lddk, void* dV,
+                              int lddv, void* dZf, void* dZb, int lddz, float* dh0, void* work, size_t work_bytes, void* cuda_stream) {
+  const ard_status st = delta_check(ctx, dtype, T, B, heads, Dk, Dv, scale, eps, Q, ldq, K, ldk, V, ldv, Zf, Zb, ldz);
+  if (st != ARD_OK) return st;
+  const void* const outs[] = {dQ, dK, dV, dZf, dZb};
+  if (T > 0) {
+    if (!S || !dY || S == dh0) return ARD_ERR_INVALID_ARG;
+    for (int i = 0; i < 5; ++i) {
+      if (!outs[i]) return ARD_ERR_INVALID_ARG;
+      for (int j = 0; j < i; ++j)
+        if (outs[i] == outs[j]) return ARD_ERR_INVALID_ARG;
+      for (const void* in : {Q, K, V, Zf, Zb, dY})
+        if (outs[i] == in) return ARD_ERR_INVALID_ARG;
+    }
+    if (lddy < (long long)heads * Dv || lddq < (long long)heads * Dk || lddk < (long long)heads * Dk || lddv < (long long)heads * Dv || lddz < heads)
+      return ARD_ERR_SHAPE;
+  }
+  if (off_elements(2, {Q, K, V, Zf, Zb, dY, dQ, dK, dV, dZf, dZb}) || off_elements(4, {lens, S, dhT, dh0})) return ARD_ERR_ALIGNMENT;
+  const size_t need = delta_work_bytes(T, B, heads, Dk, Dv, true);
+  if (need > 0 && !work) return ARD_ERR_INVALID_ARG;
+  if (work_bytes < need) return ARD_ERR_NOMEM;
+  DeviceGuard guard(ctx->device);
+  return launch_delta_backward(ctx, T, B, heads, Dk, Dv, scale, eps, Q, ldq, K, ldk, V, ldv, Zf, Zb, ldz, lens, S, dY, lddy, dhT, dQ, lddq, dK, lddk,
+                               dV, lddv, dZf, dZb, lddz, dh0, work, (cudaStream_t)cuda_stream);
+}
+
 // What the step and the norm look at; state_bits is 0 for the norm.
 static ard_status adamw_check(const ard_adamw_tensor* tensors, int n_tensors, int state_bits) {
   if (n_tensors < 0 || (n_tensors > 0 && !tensors)) return ARD_ERR_INVALID_ARG;

@@ -341,7 +341,15 @@ ard_status launch_adamw(ard_ctx* ctx, const ard_adamw_tensor* tensors, int n_ten
                         cudaStream_t s);
 ard_status launch_grad_norm(ard_ctx* ctx, const ard_adamw_tensor* tensors, int n_tensors, double max_norm, float* out, cudaStream_t s);
 
-// Embedding (embedding.cu), loss (distill.cu).
+// Gated delta rule (delta.cu), embedding (embedding.cu), loss (distill.cu).
+size_t delta_work_bytes(int T, int B, int heads, int Dk, int Dv, bool backward);
+ard_status launch_delta_forward(ard_ctx* ctx, int T, int B, int heads, int Dk, int Dv, float scale, float eps, const void* Q, int ldq, const void* K,
+                                int ldk, const void* V, int ldv, const void* Zf, const void* Zb, int ldz, const int32_t* lens, const float* h0,
+                                void* Y, int ldy, float* hT, float* S, void* work, cudaStream_t s);
+ard_status launch_delta_backward(ard_ctx* ctx, int T, int B, int heads, int Dk, int Dv, float scale, float eps, const void* Q, int ldq,
+                                 const void* K, int ldk, const void* V, int ldv, const void* Zf, const void* Zb, int ldz, const int32_t* lens,
+                                 const float* S, const void* dY, int lddy, const float* dhT, void* dQ, int lddq, void* dK, int lddk, void* dV,
+                                 int lddv, void* dZf, void* dZb, int lddz, float* dh0, void* work, cudaStream_t s);
 ard_status launch_embedding_fwd(ard_ctx* ctx, const int32_t* hdr, ard_dtype dtype, int rows, int V, int N, float alpha, const int32_t* ids,
                                 const void* table, int ldt, void* Y, int ldy, cudaStream_t s);
 ard_status launch_embedding_bwd(ard_ctx* ctx, const int32_t* hdr, ard_dtype dtype, int rows, int V, int N, float alpha, const int32_t* ids,

@@ -162,7 +162,8 @@ PyMethodDef g_methods[] = {
     CALL(ard_blocks_predict), CALL(ard_blocks_sample), CALL(ard_blocks_fwd), CALL(ard_blocks_bwd_weight),
     CALL(ard_blocks_bwd_input), CALL(ard_blocks_products),
     CALL(ard_layer_norm_fwd), CALL(ard_layer_norm_bwd), CALL(ard_glr_forward), CALL(ard_glr_backward),
-    CALL(ard_embedding_fwd), CALL(ard_embedding_bwd), CALL(ard_distill_loss), {nullptr, nullptr, 0, nullptr}};
+    CALL(ard_embedding_fwd), CALL(ard_embedding_bwd), CALL(ard_distill_loss), CALL(ard_delta_forward), CALL(ard_delta_backward),
+    {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 
