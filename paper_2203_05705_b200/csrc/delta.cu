@@ -26,9 +26,8 @@ namespace {
 
 constexpr int DL_CHUNK = 64;
 constexpr int DL_THREADS = 256;
+constexpr int DL_SQ = DL_CHUNK * DL_CHUNK;
 constexpr int DL_LD64 = DL_CHUNK + 8;  // pitch of [64][64] matrices in shared memory: rows on different banks
-constexpr int DL_CB = 32;              // columns of the state that a CTA of the scans holds
-constexpr int DL_LDC = DL_CB + 8;
 
 using bf = __nv_bfloat16;
 
@@ -53,15 +52,36 @@ struct DlArgs {
   bf *dZf, *dZb;
   long long lddz;
   float* dh0;
-  int vec_q, vec_k, vec_dy;  // whether rows lie on a grid of 16 bytes
+  int vec_q, vec_k, vec_dy, vec_s;  // whether rows lie on a grid of 16 bytes
   // work, by unit = chunk * B * heads + sequence * heads + head
-  bf* tri;       // [units][3][64][64] (I + A)^-1 in three parts
-  bf* p;         // [units][3][64][64] scale * (G o Q K^T) in three parts
-  float* row;    // [units][DL_ROWS][64] what each step has of its own
-  float* x;      // [units][64][Dv]
-  float* d;      // [units][Dk][Dv] the gradient of the state behind a chunk
+  bf* tri;     // [units][3][64][64] (I + A)^-1 in three parts
+  bf* p;       // [units][3][64][64] scale * (G o Q K^T) in three parts
+  float* row;  // [units][DL_ROW_FLOATS]
+  bf* x;       // [units][2][64][ldx] X in two parts
+  bf* d;       // [units][2][DK][ldx] the gradient of the state behind a chunk
+  int ldx;
 };
-enum { DL_RK, DL_RQ, DL_BETA, DL_F, DL_REST, DL_FIRST, DL_LAST, DL_ROWS };  // 1/|k|, 1/|q|, b, f, 1 - f, g_i, G_Ci
+
+// What a chunk's steps have of their own.  G_ij = f_{j+1} .. f_i is kept as products of gates: inside a block of 16 steps as it is, across blocks a_i, the whole
+// blocks between, and b_j.
+struct DlRow {
+  float rk[DL_CHUNK], rq[DL_CHUNK];        // 1 / |k|, 1 / |q|
+  float beta[DL_CHUNK], f[DL_CHUNK], rest[DL_CHUNK];  // b, f, 1 - f
+  float first[DL_CHUNK], last[DL_CHUNK];   // g_i = f_1 .. f_i and G_Ci
+  float from[DL_CHUNK], to[DL_CHUNK];      // a_i: from its block's first step to i; b_j: from behind j to its block's last step
+  float block[4];                          // a whole block
+  float diag[4][16][17];                   // [block][i][j], zero above the diagonal
+};
+constexpr int DL_ROW_FLOATS = (int)(sizeof(DlRow) / 4);
+static_assert(sizeof(DlRow) % 16 == 0, "copied in pieces of 16 bytes");
+
+__device__ __forceinline__ float dl_decay(const DlRow& r, int i, int j) {  // i >= j, or j in i's block
+  const int bi = i >> 4, bj = j >> 4;
+  if (bi == bj) return r.diag[bi][i & 15][j & 15];
+  float g = r.from[i] * r.to[j];
+  for (int b = bj + 1; b < bi; ++b) g *= r.block[b];
+  return g;
+}
 
 // ---- building blocks --------------------------------------------------------------------------------
 __device__ __forceinline__ void dl_ldsm(uint32_t (&r)[4], const bf* p) {
@@ -94,16 +114,19 @@ __device__ __forceinline__ void dl_mma(float (&c)[4], const uint32_t (&a)[4], ui
                : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-// c[NT][4] += A (16 rows m0) * B (8 NT columns n0) over the contraction [k0, k1), operands in PA and PB parts `sa`, `sb` elements apart.  Parts i
-// and j are multiplied where i + j <= MOST: smaller products are below what is kept.
-template <int NT, bool AT, bool BKN, int PA, int PB, int MOST>
-__device__ __forceinline__ void dl_product(float (&c)[NT][4], const bf* a, int lda, int sa, const bf* b, int ldb, int sb, int m0, int n0, int k0, int k1,
-                                           int lane) {
+// c[MT][NT][4] += A (16 MT rows from m0) * B (8 NT columns from n0) over the contraction [k0, k1), operands in PA and PB parts `sa`, `sb` elements
+// apart.  Parts i and j are multiplied where i + j <= MOST: smaller products are below what is kept.
+template <int MT, int NT, bool AT, bool BKN, int PA, int PB, int MOST>
+__device__ __forceinline__ void dl_product(float (&c)[MT][NT][4], const bf* a, int lda, int sa, const bf* b, int ldb, int sb, int m0, int n0, int k0,
+                                           int k1, int lane) {
   static_assert(NT % 2 == 0, "columns by sixteens");
+#pragma unroll 2
   for (int k = k0; k < k1; k += 16) {
-    uint32_t ra[PA][4];
+    uint32_t ra[MT][PA][4];
 #pragma unroll
-    for (int i = 0; i < PA; ++i) dl_a<AT>(ra[i], a + i * sa, lda, m0, k, lane);
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+      for (int i = 0; i < PA; ++i) dl_a<AT>(ra[m][i], a + i * sa, lda, m0 + 16 * m, k, lane);
 #pragma unroll
     for (int n = 0; n < NT; n += 2) {
 #pragma unroll
@@ -113,8 +136,11 @@ __device__ __forceinline__ void dl_product(float (&c)[NT][4], const bf* a, int l
 #pragma unroll
         for (int i = PA - 1; i >= 0; --i)
           if (i + j <= MOST) {
-            dl_mma(c[n], ra[i], rb[0], rb[1]);
-            dl_mma(c[n + 1], ra[i], rb[2], rb[3]);
+#pragma unroll
+            for (int m = 0; m < MT; ++m) {
+              dl_mma(c[m][n], ra[m][i], rb[0], rb[1]);
+              dl_mma(c[m][n + 1], ra[m][i], rb[2], rb[3]);
+            }
           }
       }
     }
@@ -149,26 +175,46 @@ __device__ __forceinline__ void dl_gate(float z, float& f, float& rest) {
   rest = z >= 0.f ? small : big;
 }
 
-// [64][cols] of a matrix whose rows are `step` elements apart, to shared memory with pitch ld; rows from `live` on and columns up to
-// `pad` are zeros.
-__device__ __forceinline__ void dl_load(bf* s, int ld, const bf* g, long long step, int live, int cols, int pad, int vec) {
-  const int pieces = pad / 8;
-  for (int i = threadIdx.x; i < DL_CHUNK * pieces; i += blockDim.x) {
-    const int r = i / pieces, c = (i - r * pieces) * 8;
-    uint4 q = make_uint4(0, 0, 0, 0);
-    if (r < live && c < cols) {
-      const bf* p = g + r * step + c;
-      if (vec) {
-        q = *reinterpret_cast<const uint4*>(p);
-      } else {
-        bf e[8];
+__device__ __forceinline__ void dl_copy16(void* s, const void* g, bool there) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(s)), "l"(g), "r"(there ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void dl_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int LEFT>
+__device__ __forceinline__ void dl_wait() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory");
+}
+
+// [64][cols] of a matrix whose rows are `step` elements apart, on its way to shared memory with pitch ld; rows from `live` on and columns up to PAD are
+// zeros.  Rows off the grid of 16 bytes go through registers, at once.
+template <int PAD>
+__device__ __forceinline__ void dl_load(bf* s, int ld, const bf* g, long long step, int live, int cols, int vec) {
+  constexpr int PIECES = PAD / 8;
+  for (int i = threadIdx.x; i < DL_CHUNK * PIECES; i += blockDim.x) {
+    const int r = i / PIECES, c = (i % PIECES) * 8;
+    const bool there = r < live && c < cols;
+    const bf* p = there ? g + r * step + c : g;
+    if (vec) {
+      dl_copy16(s + r * ld + c, p, there);
+    } else {
+      bf e[8];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) e[k] = c + k < cols ? p[k] : __float2bfloat16_rn(0.f);
-        memcpy(&q, e, 16);
-      }
+      for (int k = 0; k < 8; ++k) e[k] = there && c + k < cols ? p[k] : __float2bfloat16_rn(0.f);
+      uint4 q;
+      memcpy(&q, e, 16);
+      *reinterpret_cast<uint4*>(s + r * ld + c) = q;
     }
-    *reinterpret_cast<uint4*>(s + r * ld + c) = q;
   }
+}
+// PARTS matrices [64][64] from the work.
+template <int PARTS>
+__device__ __forceinline__ void dl_load64(bf* s, const bf* g) {
+  for (int i = threadIdx.x; i < PARTS * DL_CHUNK * 8; i += blockDim.x) {
+    const int r = i >> 3, c = (i & 7) * 8;  // rows of all parts, one after the other
+    dl_copy16(s + r * DL_LD64 + c, g + r * DL_CHUNK + c, true);
+  }
+}
+__device__ __forceinline__ void dl_load_row(DlRow& s, const float* g) {
+  for (int i = threadIdx.x; i < DL_ROW_FLOATS / 4; i += blockDim.x) dl_copy16(reinterpret_cast<float*>(&s) + 4 * i, g + 4 * i, true);
 }
 
 struct DlUnit {
@@ -189,15 +235,45 @@ __device__ __forceinline__ DlUnit dl_unit(const DlArgs& a, int chunk, long long 
 }
 
 // ---- a chunk's triangular system ----------------------------------------------------------------------
+constexpr int DL_LDA = DL_CHUNK + 1;
 template <int DK>
 struct DlPrepShared {
-  bf k[DL_CHUNK][DK + 8], q[DL_CHUNK][DK + 8];
-  float g[DL_CHUNK][DL_CHUNK + 1];  // G_ij
-  float a[DL_CHUNK][DL_CHUNK + 1];  // A, below the diagonal
-  float t[DL_CHUNK][DL_CHUNK + 1];  // its inverse with ones on the diagonal
-  float tmp[3][16][17];
-  float row[DL_ROWS][DL_CHUNK];
+  union {
+    struct {
+      bf k[DL_CHUNK][DK + 8], q[DL_CHUNK][DK + 8];
+    };
+    struct {
+      float t[DL_CHUNK][DL_LDA];  // the inverse, with ones on the diagonal
+      float tmp[3][16][17];
+    };
+  };
+  float a[DL_CHUNK][DL_LDA];  // A, below the diagonal
+  DlRow row;
 };
+
+// The blocks D below the diagonal of 16 x 16 blocks: T_ij = -T_ii sum_{j <= k < i} A_ik T_kj, all of them side by side.
+template <int D, typename Sh>
+__device__ __forceinline__ void dl_inverse_blocks(Sh& sh, int er, int ec) {
+  float s[4 - D];
+#pragma unroll
+  for (int j = 0; j < 4 - D; ++j) s[j] = 0.f;
+#pragma unroll 8
+  for (int k = 0; k < 16 * D; ++k)
+#pragma unroll
+    for (int j = 0; j < 4 - D; ++j) s[j] = fmaf(sh.a[16 * (j + D) + er][16 * j + k], sh.t[16 * j + k][16 * j + ec], s[j]);
+#pragma unroll
+  for (int j = 0; j < 4 - D; ++j) sh.tmp[j][er][ec] = s[j];
+  __syncthreads();
+#pragma unroll
+  for (int j = 0; j < 4 - D; ++j) s[j] = 0.f;
+#pragma unroll
+  for (int k = 0; k < 16; ++k)
+#pragma unroll
+    for (int j = 0; j < 4 - D; ++j) s[j] = fmaf(sh.t[16 * (j + D) + er][16 * (j + D) + k], sh.tmp[j][k][ec], s[j]);
+#pragma unroll
+  for (int j = 0; j < 4 - D; ++j) sh.t[16 * (j + D) + er][16 * j + ec] = -s[j];
+  __syncthreads();
+}
 
 template <int DK>
 __global__ void __launch_bounds__(DL_THREADS) delta_prep_kernel(const DlArgs a) {
@@ -209,8 +285,9 @@ __global__ void __launch_bounds__(DL_THREADS) delta_prep_kernel(const DlArgs a) 
   const long long units = (long long)a.B * a.heads;
   const DlUnit u = dl_unit(a, (int)(blockIdx.x / units), blockIdx.x % units);
   if (u.live == 0) return;  // nobody asks
-  dl_load(&sh.k[0][0], DK + 8, a.K + u.row0 * a.ldk + (long long)u.head * a.Dk, a.B * a.ldk, u.live, a.Dk, DK, a.vec_k);
-  dl_load(&sh.q[0][0], DK + 8, a.Q + u.row0 * a.ldq + (long long)u.head * a.Dk, a.B * a.ldq, u.live, a.Dk, DK, a.vec_q);
+  dl_load<DK>(&sh.k[0][0], DK + 8, a.K + u.row0 * a.ldk + (long long)u.head * a.Dk, a.B * a.ldk, u.live, a.Dk, a.vec_k);
+  dl_load<DK>(&sh.q[0][0], DK + 8, a.Q + u.row0 * a.ldq + (long long)u.head * a.Dk, a.B * a.ldq, u.live, a.Dk, a.vec_q);
+  dl_commit();
   if (t < DL_CHUNK) {
     float f = 1.f, rest = 0.f, beta = 0.f, no;
     if (t < u.live) {
@@ -218,14 +295,16 @@ __global__ void __launch_bounds__(DL_THREADS) delta_prep_kernel(const DlArgs a) 
       dl_gate(__bfloat162float(a.Zf[r]), f, rest);
       dl_gate(__bfloat162float(a.Zb[r]), beta, no);
     }
-    sh.row[DL_F][t] = f;
-    sh.row[DL_REST][t] = rest;
-    sh.row[DL_BETA][t] = beta;
+    sh.row.f[t] = f;
+    sh.row.rest[t] = rest;
+    sh.row.beta[t] = beta;
   }
+  dl_wait<0>();
   __syncthreads();
   {  // lengths: four threads a row
     const int r = t >> 2, part = t & 3;
     float kk = 0.f, qq = 0.f;
+#pragma unroll 8
     for (int c = part * 2; c < DK; c += 8) {
       const float2 x = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&sh.k[r][c]));
       const float2 y = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&sh.q[r][c]));
@@ -239,231 +318,276 @@ __global__ void __launch_bounds__(DL_THREADS) delta_prep_kernel(const DlArgs a) 
     }
     if (part == 0) {
       kk += a.eps, qq += a.eps;
-      sh.row[DL_RK][r] = a.eps < 0.f ? 1.f : kk > 0.f ? 1.f / sqrtf(kk) : 0.f;
-      sh.row[DL_RQ][r] = a.eps < 0.f ? 1.f : qq > 0.f ? 1.f / sqrtf(qq) : 0.f;
+      sh.row.rk[r] = a.eps < 0.f ? 1.f : kk > 0.f ? 1.f / sqrtf(kk) : 0.f;
+      sh.row.rq[r] = a.eps < 0.f ? 1.f : qq > 0.f ? 1.f / sqrtf(qq) : 0.f;
     }
   }
-  if (t < DL_CHUNK) {  // a column of the decays
-    float g = 1.f;
-    sh.g[t][t] = 1.f;
-    for (int i = t + 1; i < DL_CHUNK; ++i) sh.g[i][t] = g *= sh.row[DL_F][i];
-    sh.row[DL_LAST][t] = g;
-  } else if (t == DL_CHUNK) {
-    float g = 1.f;
-    for (int i = 0; i < DL_CHUNK; ++i) sh.row[DL_FIRST][i] = g *= sh.row[DL_F][i];
+  if (t < DL_CHUNK) {  // a column of the decays inside its block
+    const int b = t >> 4, j = t & 15;
+    float f[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) f[i] = sh.row.f[16 * b + i];
+    float g = 1.f, all = 1.f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      if (i > j) g *= f[i];
+      sh.row.diag[b][i][j] = i < j ? 0.f : g;
+      all *= f[i];
+      if (i == j) sh.row.from[t] = all;
+    }
+    sh.row.to[t] = g;
+    if (j == 15) sh.row.block[b] = all;
   }
   __syncthreads();
+  if (t < DL_CHUNK) {
+    const int b = t >> 4;
+    float first = sh.row.from[t], last = sh.row.to[t];
+    for (int i = 0; i < b; ++i) first *= sh.row.block[i];
+    for (int i = b + 1; i < 4; ++i) last *= sh.row.block[i];
+    sh.row.first[t] = first;
+    sh.row.last[t] = last;
+  }
   // K K^T (warps 0..3) and Q K^T (4..7), sixteen rows a warp
   {
-    float c[8][4] = {};
-    const int m0 = (warp & 3) * 16;
+    float c[1][8][4] = {};
+    const int m0 = (warp < 4 ? warp : 7 - warp) * 16;
     const bool keys = warp < 4;
-    dl_product<8, false, false, 1, 1, 0>(c, keys ? &sh.k[0][0] : &sh.q[0][0], DK + 8, 0, &sh.k[0][0], DK + 8, 0, m0, 0, 0, DK, lane);
-    bf* P = a.p + u.unit * 3 * DL_CHUNK * DL_CHUNK;
+    dl_product<1, 8, false, false, 1, 1, 0>(c, keys ? &sh.k[0][0] : &sh.q[0][0], DK + 8, 0, &sh.k[0][0], DK + 8, 0, m0, 0, 0, DK, lane);
+    bf* P = a.p + u.unit * 3 * DL_SQ;
 #pragma unroll
-    for (int n = 0; n < 8; ++n)
+    for (int h = 0; h < 2; ++h) {
+      const int i = m0 + (lane >> 2) + 8 * h;
+      const float by = keys ? sh.row.rk[i] * sh.row.beta[i] : sh.row.rq[i] * a.scale;
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int i = m0 + (lane >> 2) + 8 * h, j = 8 * n + 2 * (lane & 3);
+      for (int n = 0; n < 8; ++n) {
+        const int j = 8 * n + 2 * (lane & 3);
         float x[2];
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
           const int jj = j + e;
-          const bool on = keys ? jj < i : jj <= i;
-          x[e] = on ? c[n][2 * h + e] * sh.row[DL_RK][jj] * sh.g[i][jj] * (keys ? sh.row[DL_RK][i] * sh.row[DL_BETA][i] : sh.row[DL_RQ][i] * a.scale) : 0.f;
+          x[e] = (keys ? jj < i : jj <= i) ? c[0][n][2 * h + e] * sh.row.rk[jj] * dl_decay(sh.row, i, jj) * by : 0.f;
           if (keys) sh.a[i][jj] = x[e];
         }
-        if (!keys) dl_put<3>(P + i * DL_CHUNK + j, DL_CHUNK * DL_CHUNK, x[0], x[1]);
+        if (!keys) dl_put<3>(P + i * DL_CHUNK + j, DL_SQ, x[0], x[1]);
       }
+    }
   }
   __syncthreads();
-  // the inverse: blocks of 16 on the diagonal by substitution, then those below it from block to block
+  // the inverse: blocks of 16 on the diagonal by substitution, then those below it (q and k have been read: it lies where they were)
   if (t < DL_CHUNK) {
     const int b0 = t & ~15, j = t & 15;
     float x[16];
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-      float s = 0.f;
+      float s = 0.f, s1 = 0.f;
 #pragma unroll
-      for (int k = 0; k < i; ++k) s = fmaf(sh.a[b0 + i][b0 + k], x[k], s);
-      x[i] = i == j ? 1.f : i > j ? -s : 0.f;
+      for (int k = 0; k < i; ++k) (k & 1 ? s1 : s) = fmaf(sh.a[b0 + i][b0 + k], x[k], k & 1 ? s1 : s);
+      x[i] = i == j ? 1.f : i > j ? -(s + s1) : 0.f;
       sh.t[b0 + i][b0 + j] = x[i];
     }
   }
   __syncthreads();
-  const int er = t >> 4, ec = t & 15;
-  for (int d = 1; d < 4; ++d) {
-    for (int j = 0; j + d < 4; ++j) {
-      const int i = j + d;
-      float s = 0.f;
-      for (int k = 16 * j; k < 16 * i; ++k) s = fmaf(sh.a[16 * i + er][k], sh.t[k][16 * j + ec], s);
-      sh.tmp[j][er][ec] = s;
-    }
-    __syncthreads();
-    for (int j = 0; j + d < 4; ++j) {
-      const int i = j + d;
-      float s = 0.f;
+  dl_inverse_blocks<1>(sh, t >> 4, t & 15);
+  dl_inverse_blocks<2>(sh, t >> 4, t & 15);
+  dl_inverse_blocks<3>(sh, t >> 4, t & 15);
+  bf* tri = a.tri + u.unit * 3 * DL_SQ;
 #pragma unroll
-      for (int k = 0; k < 16; ++k) s = fmaf(sh.t[16 * i + er][16 * i + k], sh.tmp[j][k][ec], s);
-      sh.t[16 * i + er][16 * j + ec] = -s;
-    }
-    __syncthreads();
-  }
-  bf* tri = a.tri + u.unit * 3 * DL_CHUNK * DL_CHUNK;
-  for (int i = t; i < DL_CHUNK * DL_CHUNK / 2; i += DL_THREADS) {
+  for (int i = t; i < DL_SQ / 2; i += DL_THREADS) {
     const int r = i / (DL_CHUNK / 2), c = 2 * (i % (DL_CHUNK / 2));
     const bool on = c / 16 <= r / 16;
-    dl_put<3>(tri + r * DL_CHUNK + c, DL_CHUNK * DL_CHUNK, on ? sh.t[r][c] : 0.f, on ? sh.t[r][c + 1] : 0.f);
+    dl_put<3>(tri + r * DL_CHUNK + c, DL_SQ, on ? sh.t[r][c] : 0.f, on ? sh.t[r][c + 1] : 0.f);
   }
-  float* row = a.row + u.unit * DL_ROWS * DL_CHUNK;
-  for (int i = t; i < DL_ROWS * DL_CHUNK; i += DL_THREADS) row[i] = (&sh.row[0][0])[i];
+  float* row = a.row + u.unit * DL_ROW_FLOATS;
+  for (int i = t; i < DL_ROW_FLOATS; i += DL_THREADS) row[i] = reinterpret_cast<const float*>(&sh.row)[i];
 }
 
-// PARTS matrices [64][64] from the work to shared memory.
-__device__ __forceinline__ void dl_load64(bf* s, const bf* g, int parts) {
-  for (int i = threadIdx.x; i < parts * DL_CHUNK * 8; i += blockDim.x) {
-    const int r = i >> 3, c = (i & 7) * 8;  // rows of all parts, one after the other
-    *reinterpret_cast<uint4*>(s + r * DL_LD64 + c) = *reinterpret_cast<const uint4*>(g + r * DL_CHUNK + c);
-  }
-}
-
-// The warps' tiles of a state [DK][DL_CB]: 16 rows, NT times 8 columns.
-template <int DK>
-struct DlState {
-  static constexpr int MT = DK / 16, WN = 8 / MT, NT = DL_CB / 8 / WN;
-  __device__ __forceinline__ static int m0(int warp) { return (warp % MT) * 16; }
-  __device__ __forceinline__ static int n0(int warp) { return (warp / MT) * NT * 8; }
+// How the 8 warps of a scan share a state [DK][CB] and a chunk's matrices [64][CB].
+template <int DK, int CB>
+struct DlTiles {
+  // the state: 16 SM rows by 16 columns a warp
+  static constexpr int SM = DK * CB / (8 * 256);
+  static_assert(SM == 1 || SM == 2, "tiles of 16 or 32 rows");
+  __device__ __forceinline__ static int srow(int warp) { return warp % (DK / 16 / SM) * 16 * SM; }
+  __device__ __forceinline__ static int scol(int warp) { return warp / (DK / 16 / SM) * 16; }
+  // [64][CB] by half of the warps: 16 HM rows by 16 columns
+  static constexpr int HM = CB / 16;
+  __device__ __forceinline__ static int hrow(int w) { return w % (4 / HM) * 16 * HM; }
+  __device__ __forceinline__ static int hcol(int w) { return w / (4 / HM) * 16; }
+  // [64][CB] by 16 x 16, CB = 16: by the first four warps.  Where work grows or falls with the row, warps w and w + 4, which issue from one scheduler, have
+  // the same between them.
+  __device__ __forceinline__ static bool has(int warp) { return CB > 16 || warp < 4; }
+  __device__ __forceinline__ static int row(int warp) { return (warp < 4 ? warp : 7 - warp) * 16; }
+  __device__ __forceinline__ static int col(int warp) { return (warp >> 2) * 16; }
 };
+template <int MT, typename F>
+__device__ __forceinline__ void dl_each(int lane, int m0, int n0, F f) {  // f(tile row, tile column, half, row, column of a pair)
+#pragma unroll
+  for (int m = 0; m < MT; ++m)
+#pragma unroll
+    for (int n = 0; n < 2; ++n)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) f(m, n, h, m0 + 16 * m + (lane >> 2) + 8 * h, n0 + 8 * n + 2 * (lane & 3));
+}
 
-// A state's tile from or to [Dk][Dv] in memory, or zeros.
-template <int DK, typename F>
-__device__ __forceinline__ void dl_each(int warp, int lane, F f) {
-  using St = DlState<DK>;
+// A warp's tile of a state, from and to [Dk][Dv] in memory.
+template <int SM>
+__device__ __forceinline__ void dl_state_get(float (&s)[SM][2][4], const float* g, int Dk, int Dv, int c0, int lane, int m0, int n0) {
+  dl_each<SM>(lane, m0, n0, [&](int m, int n, int h, int d, int c) {
 #pragma unroll
-  for (int n = 0; n < St::NT; ++n)
-#pragma unroll
-    for (int h = 0; h < 2; ++h) f(n, h, St::m0(warp) + (lane >> 2) + 8 * h, St::n0(warp) + 8 * n + 2 * (lane & 3));
+    for (int e = 0; e < 2; ++e) s[m][n][2 * h + e] = g && d < Dk && c0 + c + e < Dv ? g[(long long)d * Dv + c0 + c + e] : 0.f;
+  });
+}
+template <int SM>
+__device__ __forceinline__ void dl_state_put(const float (&s)[SM][2][4], float* g, int Dk, int Dv, int c0, int lane, int m0, int n0) {
+  dl_each<SM>(lane, m0, n0, [&](int m, int n, int h, int d, int c) {
+    if (d >= Dk || c0 + c >= Dv) return;
+    float* p = g + (long long)d * Dv + c0 + c;
+    if ((reinterpret_cast<uintptr_t>(p) & 7u) == 0 && c0 + c + 1 < Dv) {
+      *reinterpret_cast<float2*>(p) = make_float2(s[m][n][2 * h], s[m][n][2 * h + 1]);
+    } else {
+      p[0] = s[m][n][2 * h];
+      if (c0 + c + 1 < Dv) p[1] = s[m][n][2 * h + 1];
+    }
+  });
+}
+__device__ __forceinline__ void dl_store2(bf* p, float x, float y, bool two) {
+  if (two && (reinterpret_cast<uintptr_t>(p) & 3u) == 0) {
+    *reinterpret_cast<__nv_bfloat162*>(p) = __floats2bfloat162_rn(x, y);
+  } else {
+    p[0] = __float2bfloat16_rn(x);
+    if (two) p[1] = __float2bfloat16_rn(y);
+  }
+}
+// Rows of a chunk behind the sequence's end, in CB columns.
+template <int CB>
+__device__ __forceinline__ void dl_zero_rows(bf* g, long long step, int from, int to, int cols) {
+  for (int i = from * CB + threadIdx.x; i < to * CB; i += blockDim.x)
+    if (i % CB < cols) g[(i / CB) * step + i % CB] = __float2bfloat16_rn(0.f);
 }
 
 // ---- forward from chunk to chunk --------------------------------------------------------------------
-template <int DK>
+// Three meetings of the warps a chunk: R = b (V - g K S) is there, U is there, the state is there.  What the next chunk reads is on its way meanwhile: each buffer is
+// asked for behind the meeting that ends its last use.
+template <int DK, int CB>
 struct DlScanShared {
-  bf k[DL_CHUNK][DK + 8], q[DL_CHUNK][DK + 8];
+  static constexpr int LDC = CB + 8;
+  bf k[2][DL_CHUNK][DK + 8], q[DL_CHUNK][DK + 8];
   bf tri[3][DL_CHUNK][DL_LD64];
   bf p[2][DL_CHUNK][DL_LD64];
-  bf s[3][DK][DL_LDC];
-  bf r[3][DL_CHUNK][DL_LDC];   // b (V - g K S)
-  bf u[2][DL_CHUNK][DL_LDC];
-  bf us[3][DL_CHUNK][DL_LDC];  // U times G_Ci / |k_i|
-  float row[DL_ROWS][DL_CHUNK];
+  bf s[3][DK][LDC];
+  bf r[3][DL_CHUNK][LDC];
+  bf u[2][DL_CHUNK][LDC];
+  bf us[3][DL_CHUNK][LDC];  // U times G_Ci / |k_i|
+  DlRow row[2];
 };
 
-template <int DK>
-__global__ void __launch_bounds__(DL_THREADS) delta_scan_kernel(const DlArgs a) {
-  using St = DlState<DK>;
+template <int DK, int CB>
+__global__ void __launch_bounds__(DL_THREADS, 1) delta_scan_kernel(const DlArgs a) {
+  using Tl = DlTiles<DK, CB>;
+  constexpr int LDK = DK + 8, LDC = CB + 8, PS = DK * LDC, PC = DL_CHUNK * LDC, PT = DL_CHUNK * DL_LD64;
   extern __shared__ __align__(16) uint8_t dl_smem[];
-  auto& sh = *reinterpret_cast<DlScanShared<DK>*>(dl_smem);
+  auto& sh = *reinterpret_cast<DlScanShared<DK, CB>*>(dl_smem);
   pdl_launch_dependents();
   pdl_wait_prior_grids();
-  const int t = threadIdx.x, warp = t >> 5, lane = t & 31;
-  const int blocks = (a.Dv + DL_CB - 1) / DL_CB;
-  const long long n = blockIdx.x / blocks;
-  const int c0 = (int)(blockIdx.x % blocks) * DL_CB, cols = min(DL_CB, a.Dv - c0);
-  const long long size = (long long)a.Dk * a.Dv;
-  float s[St::NT][4];
-  dl_each<DK>(warp, lane, [&](int i, int h, int d, int c) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int blocks = (a.Dv + CB - 1) / CB;
+  const long long n = blockIdx.x / blocks, size = (long long)a.Dk * a.Dv, heads = (long long)a.B * a.heads;
+  const int c0 = (int)(blockIdx.x % blocks) * CB, cols = min(CB, a.Dv - c0);
+  const int sr = Tl::srow(warp), sc = Tl::scol(warp), hr = Tl::hrow(warp & 3), hc = Tl::hcol(warp & 3);
+  const bool reads = warp >= 4;  // half of the warps follow the keys, half the queries
+  float s[Tl::SM][2][4];
+  dl_state_get<Tl::SM>(s, a.h0 ? a.h0 + n * size : nullptr, a.Dk, a.Dv, c0, lane, sr, sc);
+  const DlUnit u0 = dl_unit(a, 0, n);
+  const int len = a.lens ? min(max(a.lens[u0.b], 0), a.T) : a.T, chunks = (len + DL_CHUNK - 1) / DL_CHUNK;
+  const bf *Q = a.Q + (long long)u0.head * a.Dk, *K = a.K + (long long)u0.head * a.Dk, *V = a.V + (long long)u0.head * a.Dv + c0;
+  bf* Y = a.Y + (long long)u0.head * a.Dv + c0;
+  auto fetch_kq = [&](int chunk) {
+    if (chunk < chunks) {
+      const DlUnit u = dl_unit(a, chunk, n);
+      dl_load<DK>(&sh.k[chunk & 1][0][0], LDK, K + u.row0 * a.ldk, a.B * a.ldk, u.live, a.Dk, a.vec_k);
+      dl_load<DK>(&sh.q[0][0], LDK, Q + u.row0 * a.ldq, a.B * a.ldq, u.live, a.Dk, a.vec_q);
+      dl_load_row(sh.row[chunk & 1], a.row + u.unit * DL_ROW_FLOATS);
+    }
+    dl_commit();
+  };
+  auto fetch_tri = [&](int chunk) {
+    if (chunk < chunks) dl_load64<3>(&sh.tri[0][0][0], a.tri + (chunk * heads + n) * 3 * DL_SQ);
+    dl_commit();
+  };
+  float v[Tl::HM][2][4] = {};
+  auto fetch_v = [&](int chunk) {
+    if (chunk >= chunks || reads) return;
+    const DlUnit u = dl_unit(a, chunk, n);
+    dl_each<Tl::HM>(lane, hr, hc, [&](int m, int i, int h, int r, int c) {
 #pragma unroll
-    for (int e = 0; e < 2; ++e) s[i][2 * h + e] = a.h0 && d < a.Dk && c + e < cols ? a.h0[n * size + (long long)d * a.Dv + c0 + c + e] : 0.f;
-  });
-  auto store = [&](float* out) {
-    dl_each<DK>(warp, lane, [&](int i, int h, int d, int c) {
-#pragma unroll
-      for (int e = 0; e < 2; ++e)
-        if (d < a.Dk && c + e < cols) out[(long long)d * a.Dv + c0 + c + e] = s[i][2 * h + e];
+      for (int e = 0; e < 2; ++e) v[m][i][2 * h + e] = r < u.live && c + e < cols ? __bfloat162float(V[(u.row0 + (long long)r * a.B) * a.ldv + c + e]) : 0.f;
     });
   };
-  const int chunks = (a.T + DL_CHUNK - 1) / DL_CHUNK;
-  const int m0 = (warp & 3) * 16, n0 = (warp >> 2) * 16;  // this warp's tile of [64][DL_CB] matrices
+  fetch_kq(0);
+  fetch_tri(0);
+  fetch_v(0);
   for (int chunk = 0; chunk < chunks; ++chunk) {
     const DlUnit u = dl_unit(a, chunk, n);
-    if (a.S) store(a.S + ((long long)chunk * a.B * a.heads + n) * size);
-    if (u.live < DL_CHUNK) {  // rows behind the sequence's end
-      const int steps = min(DL_CHUNK, a.T - chunk * DL_CHUNK);
-      for (int i = u.live * DL_CB + t; i < steps * DL_CB; i += DL_THREADS)
-        if (i % DL_CB < cols) a.Y[(u.row0 + (long long)(i / DL_CB) * a.B) * a.ldy + (long long)u.head * a.Dv + c0 + i % DL_CB] = __float2bfloat16_rn(0.f);
-      if (u.live == 0) continue;
-    }
-    dl_load(&sh.k[0][0], DK + 8, a.K + u.row0 * a.ldk + (long long)u.head * a.Dk, a.B * a.ldk, u.live, a.Dk, DK, a.vec_k);
-    dl_load(&sh.q[0][0], DK + 8, a.Q + u.row0 * a.ldq + (long long)u.head * a.Dk, a.B * a.ldq, u.live, a.Dk, DK, a.vec_q);
-    dl_load64(&sh.tri[0][0][0], a.tri + u.unit * 3 * DL_CHUNK * DL_CHUNK, 3);
-    dl_load64(&sh.p[0][0][0], a.p + u.unit * 3 * DL_CHUNK * DL_CHUNK, 2);
-    const float* row = a.row + u.unit * DL_ROWS * DL_CHUNK;
-    for (int i = t; i < DL_ROWS * DL_CHUNK; i += DL_THREADS) (&sh.row[0][0])[i] = row[i];
-    dl_each<DK>(warp, lane, [&](int i, int h, int d, int c) { dl_put<3>(&sh.s[0][d][c], DK * DL_LDC, s[i][2 * h], s[i][2 * h + 1]); });
-    float v[2][4];
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const int r = m0 + (lane >> 2) + 8 * h, c = n0 + 8 * i + 2 * (lane & 3) + e;
-          v[i][2 * h + e] = r < u.live && c < cols ? __bfloat162float(a.V[(u.row0 + (long long)r * a.B) * a.ldv + (long long)u.head * a.Dv + c0 + c]) : 0.f;
-        }
+    const DlRow& row = sh.row[chunk & 1];
+    const bf* k = &sh.k[chunk & 1][0][0];
+    if (a.S) dl_state_put<Tl::SM>(s, a.S + u.unit * size, a.Dk, a.Dv, c0, lane, sr, sc);
+    dl_each<Tl::SM>(lane, sr, sc, [&](int m, int i, int h, int d, int c) { dl_put<3>(&sh.s[0][d][c], PS, s[m][i][2 * h], s[m][i][2 * h + 1]); });
+    dl_wait<1>();
     __syncthreads();
-    float o[2][4] = {};
-    {
-      float e[2][4] = {};
-      dl_product<2, false, true, 1, 3, 2>(e, &sh.k[0][0], DK + 8, 0, &sh.s[0][0][0], DL_LDC, DK * DL_LDC, m0, n0, 0, DK, lane);
-      dl_product<2, false, true, 1, 2, 1>(o, &sh.q[0][0], DK + 8, 0, &sh.s[0][0][0], DL_LDC, DK * DL_LDC, m0, n0, 0, DK, lane);
+    dl_load64<2>(&sh.p[0][0][0], a.p + u.unit * 3 * DL_SQ);
+    dl_commit();
+    float o[Tl::HM][2][4] = {};
+    if (reads) {
+      dl_product<Tl::HM, 2, false, true, 1, 2, 1>(o, &sh.q[0][0], LDK, 0, &sh.s[0][0][0], LDC, PS, hr, hc, 0, DK, lane);
+      dl_each<Tl::HM>(lane, hr, hc, [&](int m, int i, int h, int r, int) {
+        const float g = a.scale * row.first[r] * row.rq[r];
+        o[m][i][2 * h] *= g;
+        o[m][i][2 * h + 1] *= g;
+      });
+    } else {
+      dl_product<Tl::HM, 2, false, true, 1, 3, 2>(o, k, LDK, 0, &sh.s[0][0][0], LDC, PS, hr, hc, 0, DK, lane);
+      dl_each<Tl::HM>(lane, hr, hc, [&](int m, int i, int h, int r, int c) {
+        const float b = row.beta[r], g = -row.first[r] * row.rk[r];
+        dl_put<3>(&sh.r[0][r][c], PC, b * fmaf(g, o[m][i][2 * h], v[m][i][2 * h]), b * fmaf(g, o[m][i][2 * h + 1], v[m][i][2 * h + 1]));
+      });
+    }
+    dl_wait<1>();
+    __syncthreads();
+    fetch_kq(chunk + 1);
+    fetch_v(chunk + 1);
+    if (Tl::has(warp)) {
+      const int m0 = Tl::row(warp), n0 = Tl::col(warp);
+      float x[1][2][4] = {};
+      dl_product<1, 2, false, true, 3, 3, 2>(x, &sh.tri[0][0][0], DL_LD64, PT, &sh.r[0][0][0], LDC, PC, m0, n0, 0, m0 + 16, lane);
+      dl_each<1>(lane, m0, n0, [&](int, int i, int h, int r, int c) {
+        const float g = row.last[r] * row.rk[r], x0 = x[0][i][2 * h], x1 = x[0][i][2 * h + 1];
+        dl_put<2>(&sh.u[0][r][c], PC, x0, x1);
+        dl_put<3>(&sh.us[0][r][c], PC, g * x0, g * x1);
+      });
+    }
+    dl_wait<1>();
+    __syncthreads();
+    fetch_tri(chunk + 1);
+    const float whole = row.first[DL_CHUNK - 1];
+#pragma unroll
+    for (int m = 0; m < Tl::SM; ++m)
 #pragma unroll
       for (int i = 0; i < 2; ++i)
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const int r = m0 + (lane >> 2) + 8 * h, c = n0 + 8 * i + 2 * (lane & 3);
-          const float b = sh.row[DL_BETA][r], g = sh.row[DL_FIRST][r] * sh.row[DL_RK][r];
-          dl_put<3>(&sh.r[0][r][c], DL_CHUNK * DL_LDC, b * fmaf(-g, e[i][2 * h], v[i][2 * h]), b * fmaf(-g, e[i][2 * h + 1], v[i][2 * h + 1]));
-          const float go = a.scale * sh.row[DL_FIRST][r] * sh.row[DL_RQ][r];
-          o[i][2 * h] *= go;
-          o[i][2 * h + 1] *= go;
-        }
+        for (int e = 0; e < 4; ++e) s[m][i][e] *= whole;
+    dl_product<Tl::SM, 2, true, true, 1, 3, 2>(s, k, LDK, 0, &sh.us[0][0][0], LDC, PC, sr, sc, 0, DL_CHUNK, lane);
+    if (reads) {
+      dl_product<Tl::HM, 2, false, true, 2, 2, 1>(o, &sh.p[0][0][0], DL_LD64, PT, &sh.u[0][0][0], LDC, PC, hr, hc, 0, hr + 16 * Tl::HM, lane);
+      dl_each<Tl::HM>(lane, hr, hc, [&](int m, int i, int h, int r, int c) {
+        if (r < u.live && c < cols) dl_store2(Y + (u.row0 + (long long)r * a.B) * a.ldy + c, o[m][i][2 * h], o[m][i][2 * h + 1], c + 1 < cols);
+      });
     }
-    __syncthreads();
-    {
-      float x[2][4] = {};
-      dl_product<2, false, true, 3, 3, 2>(x, &sh.tri[0][0][0], DL_LD64, DL_CHUNK * DL_LD64, &sh.r[0][0][0], DL_LDC, DL_CHUNK * DL_LDC, m0, n0, 0, m0 + 16, lane);
-#pragma unroll
-      for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const int r = m0 + (lane >> 2) + 8 * h, c = n0 + 8 * i + 2 * (lane & 3);
-          const float g = sh.row[DL_LAST][r] * sh.row[DL_RK][r];
-          dl_put<2>(&sh.u[0][r][c], DL_CHUNK * DL_LDC, x[i][2 * h], x[i][2 * h + 1]);
-          dl_put<3>(&sh.us[0][r][c], DL_CHUNK * DL_LDC, g * x[i][2 * h], g * x[i][2 * h + 1]);
-        }
-    }
-    __syncthreads();
-    const float whole = sh.row[DL_FIRST][DL_CHUNK - 1];
-#pragma unroll
-    for (int i = 0; i < St::NT; ++i)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) s[i][e] *= whole;
-    dl_product<St::NT, true, true, 1, 3, 2>(s, &sh.k[0][0], DK + 8, 0, &sh.us[0][0][0], DL_LDC, DL_CHUNK * DL_LDC, St::m0(warp), St::n0(warp), 0, DL_CHUNK, lane);
-    dl_product<2, false, true, 2, 2, 1>(o, &sh.p[0][0][0], DL_LD64, DL_CHUNK * DL_LD64, &sh.u[0][0][0], DL_LDC, DL_CHUNK * DL_LDC, m0, n0, 0, m0 + 16, lane);
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int r = m0 + (lane >> 2) + 8 * h, c = n0 + 8 * i + 2 * (lane & 3);
-        if (r >= u.live) continue;
-        bf* y = a.Y + (u.row0 + (long long)r * a.B) * a.ldy + (long long)u.head * a.Dv + c0 + c;
-#pragma unroll
-        for (int e = 0; e < 2; ++e)
-          if (c + e < cols) y[e] = __float2bfloat16_rn(o[i][2 * h + e]);
-      }
-    __syncthreads();
   }
-  if (a.hT) store(a.hT + n * size);
+  if (a.hT) dl_state_put<Tl::SM>(s, a.hT + n * size, a.Dk, a.Dv, c0, lane, sr, sc);
+  for (int chunk = len / DL_CHUNK; chunk * DL_CHUNK < a.T; ++chunk) {
+    const DlUnit u = dl_unit(a, chunk, n);
+    dl_zero_rows<CB>(Y + u.row0 * a.ldy, a.B * a.ldy, u.live, min(DL_CHUNK, a.T - chunk * DL_CHUNK), cols);
+  }
 }
 
 // ---- step by step -----------------------------------------------------------------------------------
@@ -600,120 +724,130 @@ __global__ void __launch_bounds__(DL_THREADS) delta_steps_kernel(const DlArgs a)
 }
 
 // ---- adjoint from chunk to chunk --------------------------------------------------------------------
-template <int DK>
+// As the forward scan: dU is there, W = -g b X / |k| is there, the gradient of the state is there.
+template <int DK, int CB>
 struct DlBackShared {
-  bf k[DL_CHUNK][DK + 8], q[DL_CHUNK][DK + 8];
+  static constexpr int LDC = CB + 8;
+  bf k[2][DL_CHUNK][DK + 8], q[DL_CHUNK][DK + 8];
   bf tri[3][DL_CHUNK][DL_LD64];
   bf p[3][DL_CHUNK][DL_LD64];
-  bf d[3][DK][DL_LDC];
-  bf dy[DL_CHUNK][DL_LDC];
-  bf du[3][DL_CHUNK][DL_LDC];
-  bf w[3][DL_CHUNK][DL_LDC];   // -g / |k| b X
-  bf ys[3][DL_CHUNK][DL_LDC];  // scale g / |q| dY
-  float row[DL_ROWS][DL_CHUNK];
+  bf d[3][DK][LDC];
+  bf dy[DL_CHUNK][LDC];
+  bf du[3][DL_CHUNK][LDC];
+  bf w[3][DL_CHUNK][LDC];
+  bf ys[3][DL_CHUNK][LDC];  // scale g / |q| dY
+  DlRow row[2];
 };
 
-template <int DK>
-__global__ void __launch_bounds__(DL_THREADS) delta_back_kernel(const DlArgs a) {
-  using St = DlState<DK>;
+template <int DK, int CB>
+__global__ void __launch_bounds__(DL_THREADS, 1) delta_back_kernel(const DlArgs a) {
+  using Tl = DlTiles<DK, CB>;
+  constexpr int LDK = DK + 8, LDC = CB + 8, PS = DK * LDC, PC = DL_CHUNK * LDC, PT = DL_CHUNK * DL_LD64;
   extern __shared__ __align__(16) uint8_t dl_smem[];
-  auto& sh = *reinterpret_cast<DlBackShared<DK>*>(dl_smem);
+  auto& sh = *reinterpret_cast<DlBackShared<DK, CB>*>(dl_smem);
   pdl_launch_dependents();
   pdl_wait_prior_grids();
-  const int t = threadIdx.x, warp = t >> 5, lane = t & 31;
-  const int blocks = (a.Dv + DL_CB - 1) / DL_CB;
-  const long long n = blockIdx.x / blocks;
-  const int c0 = (int)(blockIdx.x % blocks) * DL_CB, cols = min(DL_CB, a.Dv - c0);
-  const long long size = (long long)a.Dk * a.Dv;
-  float s[St::NT][4];
-  dl_each<DK>(warp, lane, [&](int i, int h, int d, int c) {
-#pragma unroll
-    for (int e = 0; e < 2; ++e) s[i][2 * h + e] = a.dhT && d < a.Dk && c + e < cols ? a.dhT[n * size + (long long)d * a.Dv + c0 + c + e] : 0.f;
-  });
-  auto store = [&](float* out) {
-    dl_each<DK>(warp, lane, [&](int i, int h, int d, int c) {
-#pragma unroll
-      for (int e = 0; e < 2; ++e)
-        if (d < a.Dk && c + e < cols) out[(long long)d * a.Dv + c0 + c + e] = s[i][2 * h + e];
-    });
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int blocks = (a.Dv + CB - 1) / CB;
+  const long long n = blockIdx.x / blocks, size = (long long)a.Dk * a.Dv, heads = (long long)a.B * a.heads;
+  const int c0 = (int)(blockIdx.x % blocks) * CB, cols = min(CB, a.Dv - c0);
+  const int sr = Tl::srow(warp), sc = Tl::scol(warp);
+  float s[Tl::SM][2][4];
+  dl_state_get<Tl::SM>(s, a.dhT ? a.dhT + n * size : nullptr, a.Dk, a.Dv, c0, lane, sr, sc);
+  const DlUnit u0 = dl_unit(a, 0, n);
+  const int len = a.lens ? min(max(a.lens[u0.b], 0), a.T) : a.T, chunks = (len + DL_CHUNK - 1) / DL_CHUNK;
+  const bf *Q = a.Q + (long long)u0.head * a.Dk, *K = a.K + (long long)u0.head * a.Dk, *dY = a.dY + (long long)u0.head * a.Dv + c0;
+  bf* dV = a.dV + (long long)u0.head * a.Dv + c0;
+  auto fetch_k = [&](int chunk) {  // and what the first stage reads beside it
+    if (chunk >= 0) {
+      const DlUnit u = dl_unit(a, chunk, n);
+      dl_load<DK>(&sh.k[chunk & 1][0][0], LDK, K + u.row0 * a.ldk, a.B * a.ldk, u.live, a.Dk, a.vec_k);
+      dl_load<CB>(&sh.dy[0][0], LDC, dY + u.row0 * a.lddy, a.B * a.lddy, u.live, cols, a.vec_dy);
+      dl_load64<3>(&sh.p[0][0][0], a.p + u.unit * 3 * DL_SQ);
+      dl_load_row(sh.row[chunk & 1], a.row + u.unit * DL_ROW_FLOATS);
+    }
+    dl_commit();
   };
-  const int m0 = (warp & 3) * 16, n0 = (warp >> 2) * 16;
-  for (int chunk = (a.T + DL_CHUNK - 1) / DL_CHUNK - 1; chunk >= 0; --chunk) {
+  auto fetch_tri = [&](int chunk) {
+    if (chunk >= 0) dl_load64<3>(&sh.tri[0][0][0], a.tri + (chunk * heads + n) * 3 * DL_SQ);
+    dl_commit();
+  };
+  fetch_k(chunks - 1);
+  fetch_tri(chunks - 1);
+  for (int chunk = chunks - 1; chunk >= 0; --chunk) {
     const DlUnit u = dl_unit(a, chunk, n);
-    if (u.live < DL_CHUNK) {
-      const int steps = min(DL_CHUNK, a.T - chunk * DL_CHUNK);
-      for (int i = u.live * DL_CB + t; i < steps * DL_CB; i += DL_THREADS)
-        if (i % DL_CB < cols)
-          a.dV[(u.row0 + (long long)(i / DL_CB) * a.B) * a.lddv + (long long)u.head * a.Dv + c0 + i % DL_CB] = __float2bfloat16_rn(0.f);
-      if (u.live == 0) continue;
-    }
-    store(a.d + u.unit * size);
-    dl_load(&sh.k[0][0], DK + 8, a.K + u.row0 * a.ldk + (long long)u.head * a.Dk, a.B * a.ldk, u.live, a.Dk, DK, a.vec_k);
-    dl_load(&sh.q[0][0], DK + 8, a.Q + u.row0 * a.ldq + (long long)u.head * a.Dk, a.B * a.ldq, u.live, a.Dk, DK, a.vec_q);
-    dl_load(&sh.dy[0][0], DL_LDC, a.dY + u.row0 * a.lddy + (long long)u.head * a.Dv + c0, a.B * a.lddy, u.live, cols, DL_CB, a.vec_dy);
-    dl_load64(&sh.tri[0][0][0], a.tri + u.unit * 3 * DL_CHUNK * DL_CHUNK, 3);
-    dl_load64(&sh.p[0][0][0], a.p + u.unit * 3 * DL_CHUNK * DL_CHUNK, 3);
-    const float* row = a.row + u.unit * DL_ROWS * DL_CHUNK;
-    for (int i = t; i < DL_ROWS * DL_CHUNK; i += DL_THREADS) (&sh.row[0][0])[i] = row[i];
-    dl_each<DK>(warp, lane, [&](int i, int h, int d, int c) { dl_put<3>(&sh.d[0][d][c], DK * DL_LDC, s[i][2 * h], s[i][2 * h + 1]); });
+    const DlRow& row = sh.row[chunk & 1];
+    const bf* k = &sh.k[chunk & 1][0][0];
+    bf* D = a.d + u.unit * 2 * DK * a.ldx + c0;
+    dl_each<Tl::SM>(lane, sr, sc, [&](int m, int i, int h, int d, int c) {
+      uint32_t w[3];
+      dl_split<3>(s[m][i][2 * h], s[m][i][2 * h + 1], w);
+#pragma unroll
+      for (int e = 0; e < 3; ++e) {
+        *reinterpret_cast<uint32_t*>(&sh.d[e][d][c]) = w[e];
+        if (e < 2) *reinterpret_cast<uint32_t*>(D + ((long long)e * DK + d) * a.ldx + c) = w[e];
+      }
+    });
+    dl_wait<1>();
     __syncthreads();
-    {
-      float f[2][4] = {}, g[2][4] = {};
-      dl_product<2, false, true, 1, 3, 2>(f, &sh.k[0][0], DK + 8, 0, &sh.d[0][0][0], DL_LDC, DK * DL_LDC, m0, n0, 0, DK, lane);
-      dl_product<2, true, true, 3, 1, 2>(g, &sh.p[0][0][0], DL_LD64, DL_CHUNK * DL_LD64, &sh.dy[0][0], DL_LDC, 0, m0, n0, m0, DL_CHUNK, lane);
+    dl_load<DK>(&sh.q[0][0], LDK, Q + u.row0 * a.ldq, a.B * a.ldq, u.live, a.Dk, a.vec_q);
+    dl_commit();
+    if (Tl::has(warp)) {
+      const int m0 = Tl::row(warp), n0 = Tl::col(warp);
+      float f[1][2][4] = {}, g[1][2][4] = {};
+      dl_product<1, 2, false, true, 1, 3, 2>(f, k, LDK, 0, &sh.d[0][0][0], LDC, PS, m0, n0, 0, DK, lane);
+      dl_product<1, 2, true, true, 3, 1, 2>(g, &sh.p[0][0][0], DL_LD64, PT, &sh.dy[0][0], LDC, 0, m0, n0, m0, DL_CHUNK, lane);
+      dl_each<1>(lane, m0, n0, [&](int, int i, int h, int r, int c) {
+        const float l = row.last[r] * row.rk[r], gq = a.scale * row.first[r] * row.rq[r];
+        dl_put<3>(&sh.du[0][r][c], PC, fmaf(l, f[0][i][2 * h], g[0][i][2 * h]), fmaf(l, f[0][i][2 * h + 1], g[0][i][2 * h + 1]));
+        const float2 dy = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&sh.dy[r][c]));
+        dl_put<3>(&sh.ys[0][r][c], PC, gq * dy.x, gq * dy.y);
+      });
+    }
+    dl_wait<1>();
+    __syncthreads();
+    fetch_k(chunk - 1);
+    if (Tl::has(warp)) {
+      const int m0 = Tl::row(warp), n0 = Tl::col(warp);
+      float x[1][2][4] = {};
+      dl_product<1, 2, true, true, 3, 3, 2>(x, &sh.tri[0][0][0], DL_LD64, PT, &sh.du[0][0][0], LDC, PC, m0, n0, m0, DL_CHUNK, lane);
+      bf* X = a.x + u.unit * 2 * DL_CHUNK * a.ldx + c0;
+      dl_each<1>(lane, m0, n0, [&](int, int i, int h, int r, int c) {
+        const float beta = row.beta[r], g = -row.first[r] * row.rk[r] * beta, x0 = x[0][i][2 * h], x1 = x[0][i][2 * h + 1];
+        dl_put<3>(&sh.w[0][r][c], PC, g * x0, g * x1);
+        dl_put<2>(X + (long long)r * a.ldx + c, DL_CHUNK * a.ldx, x0, x1);
+        if (r < u.live && c < cols) dl_store2(dV + (u.row0 + (long long)r * a.B) * a.lddv + c, beta * x0, beta * x1, c + 1 < cols);
+      });
+    }
+    dl_wait<1>();
+    __syncthreads();
+    fetch_tri(chunk - 1);
+    const float whole = row.first[DL_CHUNK - 1];
+#pragma unroll
+    for (int m = 0; m < Tl::SM; ++m)
 #pragma unroll
       for (int i = 0; i < 2; ++i)
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const int r = m0 + (lane >> 2) + 8 * h, c = n0 + 8 * i + 2 * (lane & 3);
-          const float l = sh.row[DL_LAST][r] * sh.row[DL_RK][r];
-          dl_put<3>(&sh.du[0][r][c], DL_CHUNK * DL_LDC, fmaf(l, f[i][2 * h], g[i][2 * h]), fmaf(l, f[i][2 * h + 1], g[i][2 * h + 1]));
-          const float2 dy = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&sh.dy[r][c]));
-          const float gq = a.scale * sh.row[DL_FIRST][r] * sh.row[DL_RQ][r];
-          dl_put<3>(&sh.ys[0][r][c], DL_CHUNK * DL_LDC, gq * dy.x, gq * dy.y);
-        }
-    }
-    __syncthreads();
-    {
-      float x[2][4] = {};
-      dl_product<2, true, true, 3, 3, 2>(x, &sh.tri[0][0][0], DL_LD64, DL_CHUNK * DL_LD64, &sh.du[0][0][0], DL_LDC, DL_CHUNK * DL_LDC, m0, n0, m0, DL_CHUNK, lane);
-#pragma unroll
-      for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const int r = m0 + (lane >> 2) + 8 * h, c = n0 + 8 * i + 2 * (lane & 3);
-          const float beta = sh.row[DL_BETA][r], g = -sh.row[DL_FIRST][r] * sh.row[DL_RK][r] * beta;
-          dl_put<3>(&sh.w[0][r][c], DL_CHUNK * DL_LDC, g * x[i][2 * h], g * x[i][2 * h + 1]);
-#pragma unroll
-          for (int e = 0; e < 2; ++e)
-            if (c + e < cols) {
-              a.x[(u.unit * DL_CHUNK + r) * a.Dv + c0 + c + e] = x[i][2 * h + e];
-              if (r < u.live)
-                a.dV[(u.row0 + (long long)r * a.B) * a.lddv + (long long)u.head * a.Dv + c0 + c + e] = __float2bfloat16_rn(beta * x[i][2 * h + e]);
-            }
-        }
-    }
-    __syncthreads();
-    const float whole = sh.row[DL_FIRST][DL_CHUNK - 1];
-#pragma unroll
-    for (int i = 0; i < St::NT; ++i)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) s[i][e] *= whole;
-    dl_product<St::NT, true, true, 1, 3, 2>(s, &sh.q[0][0], DK + 8, 0, &sh.ys[0][0][0], DL_LDC, DL_CHUNK * DL_LDC, St::m0(warp), St::n0(warp), 0, DL_CHUNK, lane);
-    dl_product<St::NT, true, true, 1, 3, 2>(s, &sh.k[0][0], DK + 8, 0, &sh.w[0][0][0], DL_LDC, DL_CHUNK * DL_LDC, St::m0(warp), St::n0(warp), 0, DL_CHUNK, lane);
-    __syncthreads();
+        for (int e = 0; e < 4; ++e) s[m][i][e] *= whole;
+    dl_product<Tl::SM, 2, true, true, 1, 3, 2>(s, &sh.q[0][0], LDK, 0, &sh.ys[0][0][0], LDC, PC, sr, sc, 0, DL_CHUNK, lane);
+    dl_product<Tl::SM, 2, true, true, 1, 3, 2>(s, k, LDK, 0, &sh.w[0][0][0], LDC, PC, sr, sc, 0, DL_CHUNK, lane);
   }
-  if (a.dh0) store(a.dh0 + n * size);
+  if (a.dh0) dl_state_put<Tl::SM>(s, a.dh0 + n * size, a.Dk, a.Dv, c0, lane, sr, sc);
+  for (int chunk = len / DL_CHUNK; chunk * DL_CHUNK < a.T; ++chunk) {
+    const DlUnit u = dl_unit(a, chunk, n);
+    dl_zero_rows<CB>(dV + u.row0 * a.lddv, a.B * a.lddv, u.live, min(DL_CHUNK, a.T - chunk * DL_CHUNK), cols);
+  }
 }
 
 // ---- a chunk's own gradients ------------------------------------------------------------------------
-// With U again from the state that the forward call left, and o the products of entries,
+// With U again from the state S_0 that the forward call left, and o the products of entries,
 //   N = scale G o (dY U^T) (j <= i),  M = -b G o (X U^T) (j < i),
 //   dQ = scale g dY S_0^T + N K,  dK = N^T Q + (M + M^T) K - g b X S_0^T + G_C U D^T,  dZb = X.U (1 - b),
-//   d log f_t = sum over the chunk's steps from t on of (q.dq - v.dv) + <D, S_C>,  S_C = g_C S_0 + (G_C K)^T U,
-// for q and k divided by their lengths, then dq / |q| without its part along q.  (d log f: what scales the state by f scales what later queries read of it, less
-// what the later values would have replaced; starting from <D, S_C> in every chunk keeps the sums short.)
-constexpr int DL_GRAD_THREADS = 512;
+// for q and k divided by their lengths, then dq / |q| without its part along q.  What gate t sees is all that passes it:
+//   d log f_t = sum_{i >= t > j} W_ij + sum_{i >= t} a_i + sum_{j < t} c_j + g_C <D, S_0>,   W = N o Q K^T + M o K K^T,
+// a_i the parts of q_i.dq_i and k_i.dk_i that come from S_0, c_j that of k_j.dk_j that comes from D.  Each of them has f_t for a factor, so small
+// gates have small gradients to the last bit; (q.dq - v.dv) summed up backwards is the same in exact arithmetic and leaves a difference of large sums.
+constexpr int DL_GRAD_THREADS = 512, DL_GRAD_WARPS = DL_GRAD_THREADS / 32;
 
 template <int DK, int DV>
 struct DlGradShared {
@@ -722,45 +856,83 @@ struct DlGradShared {
   bf x[2][DL_CHUNK][DV + 8];
   bf u[2][DL_CHUNK][DV + 8];   // b (V - g K S), then U
   union {
-    bf s[2][DK][DV + 8];       // the state in front of the chunk, then the gradient D of that behind it
+    bf s[2][DK][DV + 8];       // S_0, then D
     bf m[3][2][DL_CHUNK][DL_LD64];  // N / |k_j|, N / |q_i|, (M + M^T) / |k_j|
   };
-  bf tri[2][DL_CHUNK][DL_LD64];
-  float g[DL_CHUNK][DL_CHUNK + 1];
-  float row[DL_ROWS][DL_CHUNK];
-  float red[3][4][DL_CHUNK];   // sums over a row, by groups of columns: q.dq, k.dk, k.(U D^T)
-  float xu[DL_CHUNK], xv[DL_CHUNK];
-  float ds[DL_GRAD_THREADS / 32];
+  union {
+    bf tri[2][DL_CHUNK][DL_LD64];
+    float w[DL_CHUNK][DL_CHUNK + 1];  // W, then its sums over i >= t inside blocks of 8
+  };
+  float over[8][DL_CHUNK];     // a block's whole sum
+  DlRow row;
+  float red[4][4][DL_CHUNK];   // sums over a row, by groups of columns: a_i, c_j, q.dq, k.dk
+  float xu[DL_CHUNK], seen[DL_CHUNK];
+  float ds[DL_GRAD_WARPS];
 };
 
-// [rows][cols] fp32 without gaps to two bf16 parts in shared memory; the rest of [pad_rows][pad_cols] becomes zeros.
-__device__ __forceinline__ void dl_load_f32(bf* s, int ld, int stride, const float* g, int rows, int cols, int pad_rows, int pad_cols, const float* with, float* dot) {
-  const int pairs = pad_cols / 2;
-  for (int i = threadIdx.x; i < pad_rows * pairs; i += blockDim.x) {
-    const int r = i / pairs, c = 2 * (i - r * pairs);
-    float x[2] = {0.f, 0.f};
+// A [Dk][Dv] state in fp32 to two bf16 parts in shared memory, zeros around it.  Its products with what `with` holds in two parts in memory, entry by entry,
+// are added to dot.
+template <int DK, int DV>
+__device__ __forceinline__ float dl_load_state(bf* s, const float* g, int Dk, int Dv, int vec, const bf* with, int ldx) {
+  constexpr int LD = DV + 8, QUADS = DV / 4, MINE = DK * QUADS / DL_GRAD_THREADS, AHEAD = MINE < 4 ? MINE : 4;
+  static_assert(MINE % AHEAD == 0, "whole rounds");
+  float dot = 0.f;
 #pragma unroll
-    for (int e = 0; e < 2; ++e)
-      if (r < rows && c + e < cols) {
-        x[e] = g[(long long)r * cols + c + e];
-        if (with) *dot = fmaf(x[e], with[(long long)r * cols + c + e], *dot);
+  for (int i0 = 0; i0 < MINE; i0 += AHEAD) {
+    float4 x[AHEAD];
+    uint2 hi[AHEAD], lo[AHEAD];
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) {
+      const int at = (i0 + i) * DL_GRAD_THREADS + threadIdx.x, d = at / QUADS, c = at % QUADS * 4;
+      x[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+      hi[i] = lo[i] = make_uint2(0u, 0u);
+      if (d < Dk && c < Dv) {
+        const float* p = g + (long long)d * Dv + c;
+        if (vec) {
+          x[i] = *reinterpret_cast<const float4*>(p);
+        } else {
+          x[i].x = p[0];
+          if (c + 1 < Dv) x[i].y = p[1];
+          if (c + 2 < Dv) x[i].z = p[2];
+          if (c + 3 < Dv) x[i].w = p[3];
+        }
+        hi[i] = *reinterpret_cast<const uint2*>(with + (long long)d * ldx + c);
+        lo[i] = *reinterpret_cast<const uint2*>(with + (long long)(DK + d) * ldx + c);
       }
-    dl_put<2>(s + r * ld + c, stride, x[0], x[1]);
+    }
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) {
+      const int at = (i0 + i) * DL_GRAD_THREADS + threadIdx.x, d = at / QUADS, c = at % QUADS * 4;
+      auto pair = [](uint32_t w) {
+        __nv_bfloat162 h;
+        memcpy(&h, &w, 4);
+        return __bfloat1622float2(h);
+      };
+      const float2 h0 = pair(hi[i].x), h1 = pair(hi[i].y), l0 = pair(lo[i].x), l1 = pair(lo[i].y);
+      dot = fmaf(x[i].x, h0.x + l0.x, fmaf(x[i].y, h0.y + l0.y, fmaf(x[i].z, h1.x + l1.x, fmaf(x[i].w, h1.y + l1.y, dot))));
+      uint32_t a[2], b[2];
+      dl_split<2>(x[i].x, x[i].y, a);
+      dl_split<2>(x[i].z, x[i].w, b);
+#pragma unroll
+      for (int e = 0; e < 2; ++e) *reinterpret_cast<uint2*>(s + (e * DK + d) * LD + c) = make_uint2(a[e], b[e]);
+    }
   }
+  return dot;
 }
-__device__ __forceinline__ void dl_store2(bf* p, float x, float y, bool two) {
-  if (two && (reinterpret_cast<uintptr_t>(p) & 3u) == 0) {
-    *reinterpret_cast<__nv_bfloat162*>(p) = __floats2bfloat162_rn(x, y);
-  } else {
-    p[0] = __float2bfloat16_rn(x);
-    if (two) p[1] = __float2bfloat16_rn(y);
+// PARTS matrices [ROWS][up to PAD] from the work, on their way to shared memory.
+template <int ROWS, int PAD, int PARTS>
+__device__ __forceinline__ void dl_load_parts(bf* s, const bf* g, int ldx, int cols) {
+  constexpr int PIECES = PAD / 8;
+  for (int i = threadIdx.x; i < PARTS * ROWS * PIECES; i += blockDim.x) {
+    const int r = i / PIECES, c = (i % PIECES) * 8;
+    dl_copy16(s + r * (PAD + 8) + c, g + (c < cols ? (long long)r * ldx + c : 0), c < cols);
   }
 }
 
 template <int DK, int DV>
 __global__ void __launch_bounds__(DL_GRAD_THREADS) delta_grad_kernel(const DlArgs a) {
   constexpr int NK = DK / 32, NV = DV / 32;  // tiles of 8 columns a warp of [64][DK] and [64][DV] matrices
-  constexpr int LDK = DK + 8, LDV = DV + 8, PV = DL_CHUNK * LDV, PM = DL_CHUNK * DL_LD64;
+  constexpr int LDK = DK + 8, LDV = DV + 8, PV = DL_CHUNK * LDV, PM = DL_CHUNK * DL_LD64, PS = DK * LDV;
   extern __shared__ __align__(16) uint8_t dl_smem[];
   auto& sh = *reinterpret_cast<DlGradShared<DK, DV>*>(dl_smem);
   pdl_launch_dependents();
@@ -771,127 +943,151 @@ __global__ void __launch_bounds__(DL_GRAD_THREADS) delta_grad_kernel(const DlArg
   const int steps = min(DL_CHUNK, a.T - u.chunk * DL_CHUNK);
   bf* dq = a.dQ + u.row0 * a.lddq + (long long)u.head * a.Dk;
   bf* dk = a.dK + u.row0 * a.lddk + (long long)u.head * a.Dk;
-  for (int i = u.live * DK + t; i < steps * DK; i += DL_GRAD_THREADS) {  // rows behind the sequence's end
-    const int r = i / DK, c = i % DK;
-    if (c >= a.Dk) continue;
-    dq[(long long)r * a.B * a.lddq + c] = __float2bfloat16_rn(0.f);
-    dk[(long long)r * a.B * a.lddk + c] = __float2bfloat16_rn(0.f);
-  }
+  dl_zero_rows<DK>(dq, a.B * a.lddq, u.live, steps, a.Dk);
+  dl_zero_rows<DK>(dk, a.B * a.lddk, u.live, steps, a.Dk);
   if (t >= u.live && t < steps) {
     const long long z = (u.row0 + (long long)t * a.B) * a.lddz + u.head;
     a.dZf[z] = a.dZb[z] = __float2bfloat16_rn(0.f);
   }
   if (u.live == 0) return;
-  const long long size = (long long)a.Dk * a.Dv;
-  const float* S0 = a.S + u.unit * size;
-  dl_load(&sh.k[0][0], LDK, a.K + u.row0 * a.ldk + (long long)u.head * a.Dk, a.B * a.ldk, u.live, a.Dk, DK, a.vec_k);
-  dl_load(&sh.q[0][0], LDK, a.Q + u.row0 * a.ldq + (long long)u.head * a.Dk, a.B * a.ldq, u.live, a.Dk, DK, a.vec_q);
-  dl_load(&sh.dy[0][0], LDV, a.dY + u.row0 * a.lddy + (long long)u.head * a.Dv, a.B * a.lddy, u.live, a.Dv, DV, a.vec_dy);
-  dl_load64(&sh.tri[0][0][0], a.tri + u.unit * 3 * DL_CHUNK * DL_CHUNK, 2);
-  for (int i = t; i < DL_ROWS * DL_CHUNK; i += DL_GRAD_THREADS) (&sh.row[0][0])[i] = a.row[u.unit * DL_ROWS * DL_CHUNK + i];
-  dl_load_f32(&sh.s[0][0][0], LDV, DK * LDV, S0, a.Dk, a.Dv, DK, DV, nullptr, nullptr);
-  dl_load_f32(&sh.x[0][0][0], LDV, PV, a.x + u.unit * DL_CHUNK * a.Dv, DL_CHUNK, a.Dv, DL_CHUNK, DV, nullptr, nullptr);
-  __syncthreads();
-  if (t < DL_CHUNK) {
-    float g = 1.f;
-    for (int i = 0; i < t; ++i) sh.g[i][t] = 0.f;
-    sh.g[t][t] = 1.f;
-    for (int i = t + 1; i < DL_CHUNK; ++i) sh.g[i][t] = g *= sh.row[DL_F][i];
-  }
-  const int m0 = (warp & 3) * 16, group = warp >> 2;
-  const int nk0 = group * NK * 8, nv0 = group * NV * 8, nm0 = group * 16;  // this warp's columns
+  dl_load<DK>(&sh.k[0][0], LDK, a.K + u.row0 * a.ldk + (long long)u.head * a.Dk, a.B * a.ldk, u.live, a.Dk, a.vec_k);
+  dl_load<DK>(&sh.q[0][0], LDK, a.Q + u.row0 * a.ldq + (long long)u.head * a.Dk, a.B * a.ldq, u.live, a.Dk, a.vec_q);
+  dl_load<DV>(&sh.dy[0][0], LDV, a.dY + u.row0 * a.lddy + (long long)u.head * a.Dv, a.B * a.lddy, u.live, a.Dv, a.vec_dy);
+  dl_load64<2>(&sh.tri[0][0][0], a.tri + u.unit * 3 * DL_SQ);
+  dl_load_row(sh.row, a.row + u.unit * DL_ROW_FLOATS);
+  dl_load_parts<DL_CHUNK, DV, 2>(&sh.x[0][0][0], a.x + u.unit * 2 * DL_CHUNK * a.ldx, a.ldx, a.Dv);
+  dl_commit();
+  // this warp's tile; where work grows or falls with the row, the warps of a scheduler have the same between them
+  const int group = warp >> 2, m0 = (group < 2 ? warp & 3 : 3 - (warp & 3)) * 16;
+  const int nk0 = group * NK * 8, nv0 = group * NV * 8, nm0 = group * 16;
   const int r0 = m0 + (lane >> 2), cl = 2 * (lane & 3);
-  auto v_at = [&](int r, int c) { return r < u.live && c < a.Dv ? __bfloat162float(a.V[(u.row0 + (long long)r * a.B) * a.ldv + (long long)u.head * a.Dv + c]) : 0.f; };
-  float aq[NK][4] = {}, ak[NK][4] = {};
-  {
-    float e[NV][4] = {};
-    dl_product<NV, false, true, 1, 2, 1>(e, &sh.k[0][0], LDK, 0, &sh.s[0][0][0], LDV, DK * LDV, m0, nv0, 0, DK, lane);
+  float v[NV][4];
 #pragma unroll
-    for (int i = 0; i < NV; ++i)
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int r = r0 + 8 * h, c = nv0 + 8 * i + cl;
-        const float b = sh.row[DL_BETA][r], g = sh.row[DL_FIRST][r] * sh.row[DL_RK][r];
-        dl_put<2>(&sh.u[0][r][c], PV, b * fmaf(-g, e[i][2 * h], v_at(r, c)), b * fmaf(-g, e[i][2 * h + 1], v_at(r, c + 1)));
-      }
-  }
-  dl_product<NK, false, false, 1, 2, 1>(aq, &sh.dy[0][0], LDV, 0, &sh.s[0][0][0], LDV, DK * LDV, m0, nk0, 0, DV, lane);
-  dl_product<NK, false, false, 2, 2, 1>(ak, &sh.x[0][0][0], LDV, PV, &sh.s[0][0][0], LDV, DK * LDV, m0, nk0, 0, DV, lane);
-#pragma unroll
-  for (int i = 0; i < NK; ++i)
+  for (int i = 0; i < NV; ++i)
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const float g = sh.row[DL_FIRST][r0 + 8 * (e >> 1)];
-      aq[i][e] *= a.scale * g;
-      ak[i][e] *= -g * sh.row[DL_BETA][r0 + 8 * (e >> 1)];
+      const int r = r0 + 8 * (e >> 1), c = nv0 + 8 * i + cl + (e & 1);
+      v[i][e] = r < u.live && c < a.Dv ? __bfloat162float(a.V[(u.row0 + (long long)r * a.B) * a.ldv + (long long)u.head * a.Dv + c]) : 0.f;
     }
-  __syncthreads();
-  {
-    float x[NV][4] = {};
-    dl_product<NV, false, true, 2, 2, 1>(x, &sh.tri[0][0][0], DL_LD64, PM, &sh.u[0][0][0], LDV, PV, m0, nv0, 0, m0 + 16, lane);
-    __syncthreads();
+  const bf* D = a.d + u.unit * 2 * DK * a.ldx;
+  float dot = dl_load_state<DK, DV>(&sh.s[0][0][0], a.S + u.unit * a.Dk * a.Dv, a.Dk, a.Dv, a.vec_s, D, a.ldx);
 #pragma unroll
-    for (int i = 0; i < NV; ++i)
-#pragma unroll
-      for (int h = 0; h < 2; ++h) dl_put<2>(&sh.u[0][r0 + 8 * h][nv0 + 8 * i + cl], PV, x[i][2 * h], x[i][2 * h + 1]);
-  }
-  // the gradient of the state behind the chunk, where the state in front of it was
-  float dot = 0.f;
-  dl_load_f32(&sh.s[0][0][0], LDV, DK * LDV, a.d + u.unit * size, a.Dk, a.Dv, DK, DV, S0, &dot);
-  dot = [&] {
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) dot += __shfl_xor_sync(0xFFFFFFFFu, dot, o);
-    return dot;
-  }();
+  for (int o = 16; o > 0; o >>= 1) dot += __shfl_xor_sync(0xFFFFFFFFu, dot, o);
   if (lane == 0) sh.ds[warp] = dot;
+  dl_wait<0>();
   __syncthreads();
-  {  // X.U and X.V: eight threads a row
-    const int r = t >> 3, part = t & 7;
-    float xu = 0.f, xv = 0.f;
-    for (int c = part * 2; c < DV; c += 16) {
-      float2 x = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&sh.x[0][r][c])), xl = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&sh.x[1][r][c]));
-      const float2 y = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&sh.u[0][r][c])), yl = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&sh.u[1][r][c]));
-      x.x += xl.x, x.y += xl.y;
-      xu = fmaf(x.x, y.x + yl.x, fmaf(x.y, y.y + yl.y, xu));
-      xv = fmaf(x.x, v_at(r, c), fmaf(x.y, v_at(r, c + 1), xv));
-    }
-#pragma unroll
-    for (int o = 1; o < 8; o *= 2) {
-      xu += __shfl_xor_sync(0xFFFFFFFFu, xu, o);
-      xv += __shfl_xor_sync(0xFFFFFFFFu, xv, o);
-    }
-    if (part == 0) sh.xu[r] = xu, sh.xv[r] = xv * sh.row[DL_BETA][r];
-  }
-  float nn[2][4] = {}, mm[2][4] = {};
-  if (nm0 <= m0) {
-    dl_product<2, false, false, 1, 2, 1>(nn, &sh.dy[0][0], LDV, 0, &sh.u[0][0][0], LDV, PV, m0, nm0, 0, DV, lane);
-    dl_product<2, false, false, 2, 2, 1>(mm, &sh.x[0][0][0], LDV, PV, &sh.u[0][0][0], LDV, PV, m0, nm0, 0, DV, lane);
-  }
-  auto row_sums = [&](int which, const float (&x)[NK][4], const bf* with, int scaled) {
+  auto row_sums = [&](int which, const float (&x)[1][NK][4], const bf* with, const float* by, bool more) {
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       float s = 0.f;
 #pragma unroll
       for (int i = 0; i < NK; ++i) {
         const float2 w = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(with + (r0 + 8 * h) * LDK + nk0 + 8 * i + cl));
-        s = fmaf(x[i][2 * h], w.x, fmaf(x[i][2 * h + 1], w.y, s));
+        s = fmaf(x[0][i][2 * h], w.x, fmaf(x[0][i][2 * h + 1], w.y, s));
       }
       s += __shfl_xor_sync(0xFFFFFFFFu, s, 1);
       s += __shfl_xor_sync(0xFFFFFFFFu, s, 2);
-      if ((lane & 3) == 0) sh.red[which][group][r0 + 8 * h] = s * sh.row[scaled][r0 + 8 * h];
+      s *= by[r0 + 8 * h];
+      if ((lane & 3) == 0) sh.red[which][group][r0 + 8 * h] = more ? sh.red[which][group][r0 + 8 * h] + s : s;
     }
   };
   {
-    float x[NK][4] = {};
-    dl_product<NK, false, false, 2, 2, 1>(x, &sh.u[0][0][0], LDV, PV, &sh.s[0][0][0], LDV, DK * LDV, m0, nk0, 0, DV, lane);
+    float e[1][NV][4] = {};
+    dl_product<1, NV, false, true, 1, 2, 1>(e, &sh.k[0][0], LDK, 0, &sh.s[0][0][0], LDV, PS, m0, nv0, 0, DK, lane);
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int r = r0 + 8 * h;
+        const float b = sh.row.beta[r], g = -sh.row.first[r] * sh.row.rk[r];
+        dl_put<2>(&sh.u[0][r][nv0 + 8 * i + cl], PV, b * fmaf(g, e[0][i][2 * h], v[i][2 * h]), b * fmaf(g, e[0][i][2 * h + 1], v[i][2 * h + 1]));
+      }
+  }
+  float aq[1][NK][4] = {}, ak[1][NK][4] = {};
+  dl_product<1, NK, false, false, 1, 2, 1>(aq, &sh.dy[0][0], LDV, 0, &sh.s[0][0][0], LDV, PS, m0, nk0, 0, DV, lane);
+  dl_product<1, NK, false, false, 2, 2, 1>(ak, &sh.x[0][0][0], LDV, PV, &sh.s[0][0][0], LDV, PS, m0, nk0, 0, DV, lane);
+#pragma unroll
+  for (int i = 0; i < NK; ++i)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float g = sh.row.first[r0 + 8 * (e >> 1)];
+      aq[0][i][e] *= a.scale * g;
+      ak[0][i][e] *= -g * sh.row.beta[r0 + 8 * (e >> 1)];
+    }
+  row_sums(0, aq, &sh.q[0][0], sh.row.rq, false);
+  row_sums(0, ak, &sh.k[0][0], sh.row.rk, true);
+  __syncthreads();
+  dl_load_parts<DK, DV, 2>(&sh.s[0][0][0], D, a.ldx, a.Dv);  // D, where S_0 was
+  dl_commit();
+  {
+    float x[1][NV][4] = {};
+    dl_product<1, NV, false, true, 2, 2, 1>(x, &sh.tri[0][0][0], DL_LD64, PM, &sh.u[0][0][0], LDV, PV, m0, nv0, 0, m0 + 16, lane);
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) dl_put<2>(&sh.u[0][r0 + 8 * h][nv0 + 8 * i + cl], PV, x[0][i][2 * h], x[0][i][2 * h + 1]);
+  }
+  __syncthreads();
+  {  // X.U: eight threads a row
+    const int r = t >> 3, part = t & 7;
+    float xu = 0.f;
+#pragma unroll
+    for (int c = part * 2; c < DV; c += 16) {
+      auto both = [&](bf (&m)[2][DL_CHUNK][DV + 8]) {
+        const float2 h = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&m[0][r][c])), l = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&m[1][r][c]));
+        return make_float2(h.x + l.x, h.y + l.y);
+      };
+      const float2 x = both(sh.x), y = both(sh.u);
+      xu = fmaf(x.x, y.x, fmaf(x.y, y.y, xu));
+    }
+#pragma unroll
+    for (int o = 1; o < 8; o *= 2) xu += __shfl_xor_sync(0xFFFFFFFFu, xu, o);
+    if (part == 0) sh.xu[r] = xu;
+  }
+  float nn[1][2][4] = {}, mm[1][2][4] = {};
+  if (nm0 <= m0) {
+    float qk[1][2][4] = {}, kk[1][2][4] = {};
+    dl_product<1, 2, false, false, 1, 2, 1>(nn, &sh.dy[0][0], LDV, 0, &sh.u[0][0][0], LDV, PV, m0, nm0, 0, DV, lane);
+    dl_product<1, 2, false, false, 2, 2, 1>(mm, &sh.x[0][0][0], LDV, PV, &sh.u[0][0][0], LDV, PV, m0, nm0, 0, DV, lane);
+    dl_product<1, 2, false, false, 1, 1, 0>(qk, &sh.q[0][0], LDK, 0, &sh.k[0][0], LDK, 0, m0, nm0, 0, DK, lane);
+    dl_product<1, 2, false, false, 1, 1, 0>(kk, &sh.k[0][0], LDK, 0, &sh.k[0][0], LDK, 0, m0, nm0, 0, DK, lane);
+#pragma unroll
+    for (int n = 0; n < 2; ++n)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int i = r0 + 8 * (e >> 1), j = nm0 + 8 * n + cl + (e & 1);
+        const float g = j <= i ? dl_decay(sh.row, i, j) : 0.f;
+        nn[0][n][e] *= a.scale * g;
+        mm[0][n][e] *= j < i ? -sh.row.beta[i] * g : 0.f;
+        sh.w[i][j] = j < i ? sh.row.rk[j] * fmaf(nn[0][n][e] * sh.row.rq[i], qk[0][n][e], mm[0][n][e] * sh.row.rk[i] * kk[0][n][e]) : 0.f;
+      }
+  } else {
+#pragma unroll
+    for (int n = 0; n < 2; ++n)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sh.w[r0 + 8 * (e >> 1)][nm0 + 8 * n + cl + (e & 1)] = 0.f;
+  }
+  dl_wait<0>();
+  __syncthreads();
+  {
+    float x[1][NK][4] = {};
+    dl_product<1, NK, false, false, 2, 2, 1>(x, &sh.u[0][0][0], LDV, PV, &sh.s[0][0][0], LDV, PS, m0, nk0, 0, DV, lane);
 #pragma unroll
     for (int i = 0; i < NK; ++i)
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        x[i][e] *= sh.row[DL_LAST][r0 + 8 * (e >> 1)];
-        ak[i][e] += x[i][e];
+        x[0][i][e] *= sh.row.last[r0 + 8 * (e >> 1)];
+        ak[0][i][e] += x[0][i][e];
       }
-    row_sums(2, x, &sh.k[0][0], DL_RK);
+    row_sums(1, x, &sh.k[0][0], sh.row.rk, false);
+  }
+  {  // W summed over later rows, in blocks of eight
+    const int j = t & 63, b = t >> 6;
+    float s = 0.f;
+#pragma unroll
+    for (int i = 7; i >= 0; --i) sh.w[8 * b + i][j] = s += sh.w[8 * b + i][j];
+    sh.over[b][j] = s;
   }
   __syncthreads();
   if (nm0 <= m0) {
@@ -900,16 +1096,14 @@ __global__ void __launch_bounds__(DL_GRAD_THREADS) delta_grad_kernel(const DlArg
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const int i = r0 + 8 * h, j = nm0 + 8 * n + cl;
-        const float g0 = sh.g[i][j], g1 = sh.g[i][j + 1];  // zero above the diagonal
-        const float x = a.scale * g0 * nn[n][2 * h], y = a.scale * g1 * nn[n][2 * h + 1];
-        dl_put<2>(&sh.m[0][0][i][j], PM, x * sh.row[DL_RK][j], y * sh.row[DL_RK][j + 1]);
-        dl_put<2>(&sh.m[1][0][i][j], PM, x * sh.row[DL_RQ][i], y * sh.row[DL_RQ][i]);
+        const float x = nn[0][n][2 * h], y = nn[0][n][2 * h + 1], rq = sh.row.rq[i];
+        dl_put<2>(&sh.m[0][0][i][j], PM, x * sh.row.rk[j], y * sh.row.rk[j + 1]);
+        dl_put<2>(&sh.m[1][0][i][j], PM, x * rq, y * rq);
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
           const int jj = j + e;
           if (jj > i) continue;
-          const float z = jj < i ? -sh.row[DL_BETA][i] * (e ? g1 : g0) * mm[n][2 * h + e] : 0.f;
-          float lo = z * sh.row[DL_RK][jj], up = z * sh.row[DL_RK][i];
+          float lo = mm[0][n][2 * h + e] * sh.row.rk[jj], up = mm[0][n][2 * h + e] * sh.row.rk[i];
 #pragma unroll
           for (int part = 0; part < 2; ++part) {
             const bf bl = __float2bfloat16_rn(lo), bu = __float2bfloat16_rn(up);
@@ -921,51 +1115,71 @@ __global__ void __launch_bounds__(DL_GRAD_THREADS) delta_grad_kernel(const DlArg
         }
       }
   }
+  {  // what passes gate r: eight threads
+    const int r = t >> 3, part = t & 7;
+    float s = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const int j = part + 8 * e;
+      if (j >= r) continue;
+      s += sh.w[r][j];
+      for (int b = (r >> 3) + 1; b < 8; ++b) s += sh.over[b][j];
+    }
+#pragma unroll
+    for (int o = 1; o < 8; o *= 2) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
+    if (part == 0) sh.seen[r] = s;
+  }
   __syncthreads();
-  dl_product<NK, false, true, 2, 1, 1>(aq, &sh.m[0][0][0][0], DL_LD64, PM, &sh.k[0][0], LDK, 0, m0, nk0, 0, m0 + 16, lane);
-  dl_product<NK, true, true, 2, 1, 1>(ak, &sh.m[1][0][0][0], DL_LD64, PM, &sh.q[0][0], LDK, 0, m0, nk0, m0, DL_CHUNK, lane);
-  dl_product<NK, false, true, 2, 1, 1>(ak, &sh.m[2][0][0][0], DL_LD64, PM, &sh.k[0][0], LDK, 0, m0, nk0, 0, DL_CHUNK, lane);
-  row_sums(0, aq, &sh.q[0][0], DL_RQ);
-  row_sums(1, ak, &sh.k[0][0], DL_RK);
+  dl_product<1, NK, false, true, 2, 1, 1>(aq, &sh.m[0][0][0][0], DL_LD64, PM, &sh.k[0][0], LDK, 0, m0, nk0, 0, m0 + 16, lane);
+  dl_product<1, NK, true, true, 2, 1, 1>(ak, &sh.m[1][0][0][0], DL_LD64, PM, &sh.q[0][0], LDK, 0, m0, nk0, m0, DL_CHUNK, lane);
+  dl_product<1, NK, false, true, 2, 1, 1>(ak, &sh.m[2][0][0][0], DL_LD64, PM, &sh.k[0][0], LDK, 0, m0, nk0, 0, DL_CHUNK, lane);
+  row_sums(2, aq, &sh.q[0][0], sh.row.rq, false);
+  row_sums(3, ak, &sh.k[0][0], sh.row.rk, false);
   __syncthreads();
   auto red = [&](int which, int r) { return (sh.red[which][0][r] + sh.red[which][1][r]) + (sh.red[which][2][r] + sh.red[which][3][r]); };
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     const int r = r0 + 8 * h;
     if (r >= u.live) continue;
-    const float rq = sh.row[DL_RQ][r], rk = sh.row[DL_RK][r];
+    const float rq = sh.row.rq[r], rk = sh.row.rk[r];
     // q of length one gives up what its gradient has along it
-    const float along_q = a.eps < 0.f ? 0.f : red(0, r) * rq, along_k = a.eps < 0.f ? 0.f : red(1, r) * rk;
+    const float along_q = a.eps < 0.f ? 0.f : red(2, r) * rq, along_k = a.eps < 0.f ? 0.f : red(3, r) * rk;
 #pragma unroll
     for (int i = 0; i < NK; ++i) {
       const int c = nk0 + 8 * i + cl;
       if (c >= a.Dk) continue;
       const float2 q = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&sh.q[r][c])), k = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&sh.k[r][c]));
-      dl_store2(dq + (long long)r * a.B * a.lddq + c, rq * fmaf(-along_q, q.x, aq[i][2 * h]), rq * fmaf(-along_q, q.y, aq[i][2 * h + 1]), c + 1 < a.Dk);
-      dl_store2(dk + (long long)r * a.B * a.lddk + c, rk * fmaf(-along_k, k.x, ak[i][2 * h]), rk * fmaf(-along_k, k.y, ak[i][2 * h + 1]), c + 1 < a.Dk);
+      dl_store2(dq + (long long)r * a.B * a.lddq + c, rq * fmaf(-along_q, q.x, aq[0][i][2 * h]), rq * fmaf(-along_q, q.y, aq[0][i][2 * h + 1]), c + 1 < a.Dk);
+      dl_store2(dk + (long long)r * a.B * a.lddk + c, rk * fmaf(-along_k, k.x, ak[0][i][2 * h]), rk * fmaf(-along_k, k.y, ak[0][i][2 * h + 1]), c + 1 < a.Dk);
     }
   }
   if (warp == 0) {  // lane: steps lane and 32 + lane
     float ds = 0.f;
 #pragma unroll
-    for (int w = 0; w < DL_GRAD_THREADS / 32; ++w) ds += sh.ds[w];
-    float x0 = red(0, lane) - sh.xv[lane], x1 = red(0, 32 + lane) - sh.xv[32 + lane], end = red(2, lane) + red(2, 32 + lane);
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) end += __shfl_xor_sync(0xFFFFFFFFu, end, o);
-    end = fmaf(sh.row[DL_FIRST][DL_CHUNK - 1], ds, end);
+    for (int w = 0; w < DL_GRAD_WARPS; ++w) ds += sh.ds[w];
+    ds *= sh.row.first[DL_CHUNK - 1];
+    float x0 = red(0, lane), x1 = red(0, 32 + lane);           // a: sums from here on
+    const float c0 = red(1, lane), c1 = red(1, 32 + lane);
+    float y0 = c0, y1 = c1;                                    // c: sums up to here
 #pragma unroll
     for (int o = 1; o < 32; o *= 2) {
-      const float y0 = __shfl_down_sync(0xFFFFFFFFu, x0, o), y1 = __shfl_down_sync(0xFFFFFFFFu, x1, o);
-      if (lane + o < 32) x0 += y0, x1 += y1;
+      const float dx0 = __shfl_down_sync(0xFFFFFFFFu, x0, o), dx1 = __shfl_down_sync(0xFFFFFFFFu, x1, o);
+      const float dy0 = __shfl_up_sync(0xFFFFFFFFu, y0, o), dy1 = __shfl_up_sync(0xFFFFFFFFu, y1, o);
+      if (lane + o < 32) x0 += dx0, x1 += dx1;
+      if (lane >= o) y0 += dy0, y1 += dy1;
     }
     x0 += __shfl_sync(0xFFFFFFFFu, x1, 0);
+    y1 += __shfl_sync(0xFFFFFFFFu, y0, 31);
+    // c of the step itself does not pass its own gate; taken off by the neighbour's sum, not by a difference
+    const float before0 = __shfl_up_sync(0xFFFFFFFFu, y0, 1), before1 = __shfl_up_sync(0xFFFFFFFFu, y1, 1), half = __shfl_sync(0xFFFFFFFFu, y0, 31);
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       const int r = lane + 32 * h;
+      const float c = lane > 0 ? (h ? before1 : before0) : h ? half : 0.f;
       if (r >= u.live) continue;
       const long long z = (u.row0 + (long long)r * a.B) * a.lddz + u.head;
-      a.dZf[z] = __float2bfloat16_rn(((h ? x1 : x0) + end) * sh.row[DL_REST][r]);
-      a.dZb[z] = __float2bfloat16_rn(sh.xu[r] * (1.f - sh.row[DL_BETA][r]));
+      a.dZf[z] = __float2bfloat16_rn((sh.seen[r] + (h ? x1 : x0) + c + ds) * sh.row.rest[r]);
+      a.dZb[z] = __float2bfloat16_rn(sh.xu[r] * (1.f - sh.row.beta[r]));
     }
   }
 }
@@ -979,8 +1193,9 @@ inline long long dl_units(int T, int B, int heads) { return (long long)((T + DL_
 struct DlPlan {
   size_t tri, p, row, x, d, bytes;
 };
+inline int dl_ldx(int Dv) { return Dv <= 64 ? 64 : 128; }
 DlPlan dl_plan(int T, int B, int heads, int Dk, int Dv, bool backward) {
-  const size_t units = (size_t)dl_units(T, B, heads);
+  const size_t units = (size_t)dl_units(T, B, heads), pitch = (size_t)dl_ldx(Dv) * 2;
   DlPlan w;
   size_t at = 0;
   auto take = [&](size_t bytes) {
@@ -988,11 +1203,11 @@ DlPlan dl_plan(int T, int B, int heads, int Dk, int Dv, bool backward) {
     at += (units * bytes + 255) / 256 * 256;
     return here;
   };
-  w.tri = take(3 * DL_CHUNK * DL_CHUNK * 2);
-  w.p = take(3 * DL_CHUNK * DL_CHUNK * 2);
-  w.row = take(DL_ROWS * DL_CHUNK * 4);
-  w.x = take(backward ? (size_t)DL_CHUNK * Dv * 4 : 0);
-  w.d = take(backward ? (size_t)Dk * Dv * 4 : 0);
+  w.tri = take(3 * DL_SQ * 2);
+  w.p = take(3 * DL_SQ * 2);
+  w.row = take(sizeof(DlRow));
+  w.x = take(backward ? 2 * DL_CHUNK * pitch : 0);
+  w.d = take(backward ? 2 * (Dk <= 64 ? 64 : 128) * pitch : 0);
   w.bytes = at + 256;  // the caller's memory may begin anywhere
   return w;
 }
@@ -1001,54 +1216,39 @@ void dl_set_work(DlArgs& a, void* work, const DlPlan& w) {
   a.tri = reinterpret_cast<bf*>(p + w.tri);
   a.p = reinterpret_cast<bf*>(p + w.p);
   a.row = reinterpret_cast<float*>(p + w.row);
-  a.x = reinterpret_cast<float*>(p + w.x);
-  a.d = reinterpret_cast<float*>(p + w.d);
+  a.x = reinterpret_cast<bf*>(p + w.x);
+  a.d = reinterpret_cast<bf*>(p + w.d);
+  a.ldx = dl_ldx(a.Dv);
 }
 
-template <int DK>
-ard_status dl_prep(ard_ctx* ctx, const DlArgs& a, cudaStream_t s) {
-  const int smem = (int)sizeof(DlPrepShared<DK>);
-  ARD_CUDA_OK(cudaFuncSetAttribute(delta_prep_kernel<DK>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
-  ARD_CUDA_OK(ard_launch(ctx, delta_prep_kernel<DK>, dim3((unsigned)dl_units(a.T, a.B, a.heads)), dim3(DL_THREADS), smem, s, a));
+template <typename K>
+ard_status dl_run(ard_ctx* ctx, K kern, long long grid, int threads, size_t smem, const DlArgs& a, cudaStream_t s) {
+  ARD_CUDA_OK(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+  ARD_CUDA_OK(ard_launch(ctx, kern, dim3((unsigned)grid), dim3(threads), smem, s, a));
   ctx->launches++;
   ARD_CUDA_OK(cudaGetLastError());
   return ARD_OK;
 }
-template <int DK>
-ard_status dl_forward(ard_ctx* ctx, const DlArgs& a, cudaStream_t s) {
-  const ard_status st = dl_prep<DK>(ctx, a, s);
+template <int DK, int CB>
+ard_status dl_chunks(ard_ctx* ctx, const DlArgs& a, bool backward, cudaStream_t s) {
+  const long long units = dl_units(a.T, a.B, a.heads), grid = (long long)a.B * a.heads * ((a.Dv + CB - 1) / CB);
+  ard_status st = dl_run(ctx, delta_prep_kernel<DK>, units, DL_THREADS, sizeof(DlPrepShared<DK>), a, s);
   if (st != ARD_OK) return st;
-  const int smem = (int)sizeof(DlScanShared<DK>);
-  const long long grid = (long long)a.B * a.heads * ((a.Dv + DL_CB - 1) / DL_CB);
-  ARD_CUDA_OK(cudaFuncSetAttribute(delta_scan_kernel<DK>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
-  ARD_CUDA_OK(ard_launch(ctx, delta_scan_kernel<DK>, dim3((unsigned)grid), dim3(DL_THREADS), smem, s, a));
-  ctx->launches++;
-  ARD_CUDA_OK(cudaGetLastError());
-  return ARD_OK;
+  if (!backward) return dl_run(ctx, delta_scan_kernel<DK, CB>, grid, DL_THREADS, sizeof(DlScanShared<DK, CB>), a, s);
+  st = dl_run(ctx, delta_back_kernel<DK, CB>, grid, DL_THREADS, sizeof(DlBackShared<DK, CB>), a, s);
+  if (st != ARD_OK) return st;
+  if (a.Dv <= 64) return dl_run(ctx, delta_grad_kernel<DK, 64>, units, DL_GRAD_THREADS, sizeof(DlGradShared<DK, 64>), a, s);
+  return dl_run(ctx, delta_grad_kernel<DK, 128>, units, DL_GRAD_THREADS, sizeof(DlGradShared<DK, 128>), a, s);
+}
+ard_status dl_chunks(ard_ctx* ctx, const DlArgs& a, bool backward, cudaStream_t s) {
+  if (a.Dk <= 64) return dl_chunks<64, 32>(ctx, a, backward, s);
+  // columns of a state: 32 a CTA, 16 where that still leaves an SM for each
+  const bool few = (long long)a.B * a.heads * ((a.Dv + 15) / 16) <= ctx->sm_count;
+  return few ? dl_chunks<128, 16>(ctx, a, backward, s) : dl_chunks<128, 32>(ctx, a, backward, s);
 }
 
-template <int DK>
-ard_status dl_backward(ard_ctx* ctx, const DlArgs& a, cudaStream_t s) {
-  const ard_status st = dl_prep<DK>(ctx, a, s);
-  if (st != ARD_OK) return st;
-  const int smem = (int)sizeof(DlBackShared<DK>);
-  const long long grid = (long long)a.B * a.heads * ((a.Dv + DL_CB - 1) / DL_CB);
-  ARD_CUDA_OK(cudaFuncSetAttribute(delta_back_kernel<DK>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
-  ARD_CUDA_OK(ard_launch(ctx, delta_back_kernel<DK>, dim3((unsigned)grid), dim3(DL_THREADS), smem, s, a));
-  ctx->launches++;
-  ARD_CUDA_OK(cudaGetLastError());
-  auto grad = [&](auto kern, int bytes) {
-    ARD_CUDA_OK(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes));
-    ARD_CUDA_OK(ard_launch(ctx, kern, dim3((unsigned)dl_units(a.T, a.B, a.heads)), dim3(DL_GRAD_THREADS), bytes, s, a));
-    ctx->launches++;
-    ARD_CUDA_OK(cudaGetLastError());
-    return ARD_OK;
-  };
-  if (a.Dv <= 64) return grad(delta_grad_kernel<DK, 64>, (int)sizeof(DlGradShared<DK, 64>));
-  return grad(delta_grad_kernel<DK, 128>, (int)sizeof(DlGradShared<DK, 128>));
-}
-
-static_assert(sizeof(DlGradShared<128, 128>) <= 227 * 1024 && sizeof(DlBackShared<128>) <= 227 * 1024 && sizeof(DlScanShared<128>) <= 227 * 1024, "shared memory of an SM");
+static_assert(sizeof(DlGradShared<128, 128>) <= 227 * 1024 && sizeof(DlBackShared<128, 32>) <= 227 * 1024 && sizeof(DlScanShared<128, 32>) <= 227 * 1024,
+              "shared memory of an SM");
 
 }  // namespace
 
@@ -1076,7 +1276,7 @@ ard_status launch_delta_forward(ard_ctx* ctx, int T, int B, int heads, int Dk, i
     return ARD_OK;
   }
   dl_set_work(a, work, dl_plan(T, B, heads, Dk, Dv, false));
-  return Dk <= 64 ? dl_forward<64>(ctx, a, s) : dl_forward<128>(ctx, a, s);
+  return dl_chunks(ctx, a, false, s);
 }
 
 ard_status launch_delta_backward(ard_ctx* ctx, int T, int B, int heads, int Dk, int Dv, float scale, float eps, const void* Q, int ldq, const void* K, int ldk,
@@ -1099,6 +1299,7 @@ ard_status launch_delta_backward(ard_ctx* ctx, int T, int B, int heads, int Dk, 
   a.dQ = (bf*)dQ, a.dK = (bf*)dK, a.dV = (bf*)dV, a.lddq = lddq, a.lddk = lddk, a.lddv = lddv;
   a.dZf = (bf*)dZf, a.dZb = (bf*)dZb, a.lddz = lddz, a.dh0 = dh0;
   a.vec_q = dl_on16(Q, ldq, Dk), a.vec_k = dl_on16(K, ldk, Dk), a.vec_dy = dl_on16(dY, lddy, Dv);
+  a.vec_s = Dv % 4 == 0 && (reinterpret_cast<uintptr_t>(S) & 15u) == 0;
   dl_set_work(a, work, dl_plan(T, B, heads, Dk, Dv, true));
-  return Dk <= 64 ? dl_backward<64>(ctx, a, s) : dl_backward<128>(ctx, a, s);
+  return dl_chunks(ctx, a, true, s);
 }
