@@ -52,7 +52,7 @@ struct DlArgs {
   bf *dZf, *dZb;
   long long lddz;
   float* dh0;
-  int vec_q, vec_k, vec_dy, vec_s;  // whether rows lie on a grid of 16 bytes
+  int vec_q, vec_k, vec_v, vec_dy, vec_s;  // whether rows lie on a grid of 16 bytes
   // work, by unit = chunk * B * heads + sequence * heads + head
   bf* tri;     // [units][3][64][64] (I + A)^-1 in three parts
   bf* p;       // [units][3][64][64] scale * (G o Q K^T) in three parts
@@ -64,16 +64,23 @@ struct DlArgs {
 
 // What a chunk's steps have of their own.  G_ij = f_{j+1} .. f_i is kept as products of gates: inside a block of 16 steps as it is, across blocks a_i, the whole
 // blocks between, and b_j.
-struct DlRow {
+struct DlSteps {                 // what the scans read
+  float beta[DL_CHUNK];          // b
+  float kin[DL_CHUNK];           // g_i / |k_i|,  g_i = f_1 .. f_i
+  float kout[DL_CHUNK];          // G_Ci / |k_i|
+  float qin[DL_CHUNK];           // scale g_i / |q_i|
+  float first[DL_CHUNK];         // g_i
+};
+struct DlRow : DlSteps {
   float rk[DL_CHUNK], rq[DL_CHUNK];        // 1 / |k|, 1 / |q|
-  float beta[DL_CHUNK], f[DL_CHUNK], rest[DL_CHUNK];  // b, f, 1 - f
-  float first[DL_CHUNK], last[DL_CHUNK];   // g_i = f_1 .. f_i and G_Ci
+  float f[DL_CHUNK], rest[DL_CHUNK];       // f, 1 - f
+  float last[DL_CHUNK];                    // G_Ci
   float from[DL_CHUNK], to[DL_CHUNK];      // a_i: from its block's first step to i; b_j: from behind j to its block's last step
   float block[4];                          // a whole block
   float diag[4][16][17];                   // [block][i][j], zero above the diagonal
 };
 constexpr int DL_ROW_FLOATS = (int)(sizeof(DlRow) / 4);
-static_assert(sizeof(DlRow) % 16 == 0, "copied in pieces of 16 bytes");
+static_assert(sizeof(DlRow) % 16 == 0 && sizeof(DlSteps) % 16 == 0, "copied in pieces of 16 bytes");
 
 __device__ __forceinline__ float dl_decay(const DlRow& r, int i, int j) {  // i >= j, or j in i's block
   const int bi = i >> 4, bj = j >> 4;
@@ -185,11 +192,12 @@ __device__ __forceinline__ void dl_wait() {
 }
 
 // [64][cols] of a matrix whose rows are `step` elements apart, on its way to shared memory with pitch ld; rows from `live` on and columns up to PAD are
-// zeros.  Rows off the grid of 16 bytes go through registers, at once.
+// zeros.  Rows off the grid of 16 bytes go through registers, at once.  By threads t of `of`.
 template <int PAD>
-__device__ __forceinline__ void dl_load(bf* s, int ld, const bf* g, long long step, int live, int cols, int vec) {
+__device__ __forceinline__ void dl_load(bf* s, int ld, const bf* g, long long step, int live, int cols, int vec, int t, int of) {
   constexpr int PIECES = PAD / 8;
-  for (int i = threadIdx.x; i < DL_CHUNK * PIECES; i += blockDim.x) {
+#pragma unroll 4
+  for (int i = t; i < DL_CHUNK * PIECES; i += of) {
     const int r = i / PIECES, c = (i % PIECES) * 8;
     const bool there = r < live && c < cols;
     const bf* p = there ? g + r * step + c : g;
@@ -207,14 +215,16 @@ __device__ __forceinline__ void dl_load(bf* s, int ld, const bf* g, long long st
 }
 // PARTS matrices [64][64] from the work.
 template <int PARTS>
-__device__ __forceinline__ void dl_load64(bf* s, const bf* g) {
-  for (int i = threadIdx.x; i < PARTS * DL_CHUNK * 8; i += blockDim.x) {
+__device__ __forceinline__ void dl_load64(bf* s, const bf* g, int t, int of) {
+#pragma unroll 4
+  for (int i = t; i < PARTS * DL_CHUNK * 8; i += of) {
     const int r = i >> 3, c = (i & 7) * 8;  // rows of all parts, one after the other
     dl_copy16(s + r * DL_LD64 + c, g + r * DL_CHUNK + c, true);
   }
 }
-__device__ __forceinline__ void dl_load_row(DlRow& s, const float* g) {
-  for (int i = threadIdx.x; i < DL_ROW_FLOATS / 4; i += blockDim.x) dl_copy16(reinterpret_cast<float*>(&s) + 4 * i, g + 4 * i, true);
+template <typename Row>  // all of a row's numbers, or those that come first
+__device__ __forceinline__ void dl_load_row(Row& s, const float* g, int t, int of) {
+  for (int i = t; i < (int)(sizeof(Row) / 16); i += of) dl_copy16(reinterpret_cast<float*>(&s) + 4 * i, g + 4 * i, true);
 }
 
 struct DlUnit {
@@ -285,8 +295,8 @@ __global__ void __launch_bounds__(DL_THREADS) delta_prep_kernel(const DlArgs a) 
   const long long units = (long long)a.B * a.heads;
   const DlUnit u = dl_unit(a, (int)(blockIdx.x / units), blockIdx.x % units);
   if (u.live == 0) return;  // nobody asks
-  dl_load<DK>(&sh.k[0][0], DK + 8, a.K + u.row0 * a.ldk + (long long)u.head * a.Dk, a.B * a.ldk, u.live, a.Dk, a.vec_k);
-  dl_load<DK>(&sh.q[0][0], DK + 8, a.Q + u.row0 * a.ldq + (long long)u.head * a.Dk, a.B * a.ldq, u.live, a.Dk, a.vec_q);
+  dl_load<DK>(&sh.k[0][0], DK + 8, a.K + u.row0 * a.ldk + (long long)u.head * a.Dk, a.B * a.ldk, u.live, a.Dk, a.vec_k, t, DL_THREADS);
+  dl_load<DK>(&sh.q[0][0], DK + 8, a.Q + u.row0 * a.ldq + (long long)u.head * a.Dk, a.B * a.ldq, u.live, a.Dk, a.vec_q, t, DL_THREADS);
   dl_commit();
   if (t < DL_CHUNK) {
     float f = 1.f, rest = 0.f, beta = 0.f, no;
@@ -346,6 +356,9 @@ __global__ void __launch_bounds__(DL_THREADS) delta_prep_kernel(const DlArgs a) 
     for (int i = b + 1; i < 4; ++i) last *= sh.row.block[i];
     sh.row.first[t] = first;
     sh.row.last[t] = last;
+    sh.row.kin[t] = first * sh.row.rk[t];
+    sh.row.kout[t] = last * sh.row.rk[t];
+    sh.row.qin[t] = a.scale * first * sh.row.rq[t];
   }
   // K K^T (warps 0..3) and Q K^T (4..7), sixteen rows a warp
   {
@@ -354,21 +367,29 @@ __global__ void __launch_bounds__(DL_THREADS) delta_prep_kernel(const DlArgs a) 
     const bool keys = warp < 4;
     dl_product<1, 8, false, false, 1, 1, 0>(c, keys ? &sh.k[0][0] : &sh.q[0][0], DK + 8, 0, &sh.k[0][0], DK + 8, 0, m0, 0, 0, DK, lane);
     bf* P = a.p + u.unit * 3 * DL_SQ;
+    const int bi = m0 >> 4;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const int i = m0 + (lane >> 2) + 8 * h;
+      const int r = (lane >> 2) + 8 * h, i = m0 + r;
       const float by = keys ? sh.row.rk[i] * sh.row.beta[i] : sh.row.rq[i] * a.scale;
 #pragma unroll
-      for (int n = 0; n < 8; ++n) {
-        const int j = 8 * n + 2 * (lane & 3);
-        float x[2];
+      for (int bj = 0; bj < 4; ++bj) {
+        float across = by * sh.row.from[i];  // of what lies in earlier blocks
+        for (int b = bj + 1; b < bi; ++b) across *= sh.row.block[b];
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const int jj = j + e;
-          x[e] = (keys ? jj < i : jj <= i) ? c[0][n][2 * h + e] * sh.row.rk[jj] * dl_decay(sh.row, i, jj) * by : 0.f;
-          if (keys) sh.a[i][jj] = x[e];
+        for (int n = 2 * bj; n < 2 * bj + 2; ++n) {
+          const int j = 8 * n + 2 * (lane & 3);
+          float x[2];
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const int jj = j + e;
+            const float g = bj < bi ? across * sh.row.to[jj] : bj == bi ? by * sh.row.diag[bj][r][jj & 15] : 0.f;
+            x[e] = keys && jj >= i ? 0.f : c[0][n][2 * h + e] * sh.row.rk[jj] * g;
+            if (bj > bi || jj > i) x[e] = 0.f;
+            if (keys) sh.a[i][jj] = x[e];
+          }
+          if (!keys) dl_put<3>(P + i * DL_CHUNK + j, DL_SQ, x[0], x[1]);
         }
-        if (!keys) dl_put<3>(P + i * DL_CHUNK + j, DL_SQ, x[0], x[1]);
       }
     }
   }
@@ -401,54 +422,62 @@ __global__ void __launch_bounds__(DL_THREADS) delta_prep_kernel(const DlArgs a) 
   for (int i = t; i < DL_ROW_FLOATS; i += DL_THREADS) row[i] = reinterpret_cast<const float*>(&sh.row)[i];
 }
 
-// How the 8 warps of a scan share a state [DK][CB] and a chunk's matrices [64][CB].
-template <int DK, int CB>
-struct DlTiles {
-  // the state: 16 SM rows by 16 columns a warp
-  static constexpr int SM = DK * CB / (8 * 256);
-  static_assert(SM == 1 || SM == 2, "tiles of 16 or 32 rows");
-  __device__ __forceinline__ static int srow(int warp) { return warp % (DK / 16 / SM) * 16 * SM; }
-  __device__ __forceinline__ static int scol(int warp) { return warp / (DK / 16 / SM) * 16; }
-  // [64][CB] by half of the warps: 16 HM rows by 16 columns
-  static constexpr int HM = CB / 16;
-  __device__ __forceinline__ static int hrow(int w) { return w % (4 / HM) * 16 * HM; }
-  __device__ __forceinline__ static int hcol(int w) { return w / (4 / HM) * 16; }
-  // [64][CB] by 16 x 16, CB = 16: by the first four warps.  Where work grows or falls with the row, warps w and w + 4, which issue from one scheduler, have
-  // the same between them.
-  __device__ __forceinline__ static bool has(int warp) { return CB > 16 || warp < 4; }
-  __device__ __forceinline__ static int row(int warp) { return (warp < 4 ? warp : 7 - warp) * 16; }
-  __device__ __forceinline__ static int col(int warp) { return (warp >> 2) * 16; }
-};
-template <int MT, typename F>
-__device__ __forceinline__ void dl_each(int lane, int m0, int n0, F f) {  // f(tile row, tile column, half, row, column of a pair)
-#pragma unroll
-  for (int m = 0; m < MT; ++m)
-#pragma unroll
-    for (int n = 0; n < 2; ++n)
-#pragma unroll
-      for (int h = 0; h < 2; ++h) f(m, n, h, m0 + 16 * m + (lane >> 2) + 8 * h, n0 + 8 * n + 2 * (lane & 3));
+// ---- from chunk to chunk ----------------------------------------------------------------------------
+// A warp holds 16 columns of the state, transposed, as accumulators [16 columns][DK].  As rows of a left operand they lie in registers the way a product wants them, and so do
+// the results that follow from them: E' = S' K', R' = b (V' - g E'), U' = R' T', S' += U' K.  Nothing of this goes through shared memory, which holds what all columns
+// share (K, Q, T, P), two chunks deep.  Beside each such warp stands one that does what nobody waits for: forward the outputs, which take the state's and U's parts over
+// shared memory, backward what comes from dY alone.
+// Some of a CTA's warps, in branches of their own (0: all of them).
+__device__ __forceinline__ void dl_meet(int id, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
+__device__ __forceinline__ uint32_t dl_transposed(uint32_t x) {  // of 8 x 8 bf16, a pair a lane
+  uint32_t r;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
+  return r;
 }
-
-// A warp's tile of a state, from and to [Dk][Dv] in memory.
-template <int SM>
-__device__ __forceinline__ void dl_state_get(float (&s)[SM][2][4], const float* g, int Dk, int Dv, int c0, int lane, int m0, int n0) {
-  dl_each<SM>(lane, m0, n0, [&](int m, int n, int h, int d, int c) {
-#pragma unroll
-    for (int e = 0; e < 2; ++e) s[m][n][2 * h + e] = g && d < Dk && c0 + c + e < Dv ? g[(long long)d * Dv + c0 + c + e] : 0.f;
-  });
+__device__ __forceinline__ uint32_t dl_pack(float x, float y) {
+  uint32_t w[1];
+  dl_split<1>(x, y, w);
+  return w[0];
 }
-template <int SM>
-__device__ __forceinline__ void dl_state_put(const float (&s)[SM][2][4], float* g, int Dk, int Dv, int c0, int lane, int m0, int n0) {
-  dl_each<SM>(lane, m0, n0, [&](int m, int n, int h, int d, int c) {
-    if (d >= Dk || c0 + c >= Dv) return;
-    float* p = g + (long long)d * Dv + c0 + c;
-    if ((reinterpret_cast<uintptr_t>(p) & 7u) == 0 && c0 + c + 1 < Dv) {
-      *reinterpret_cast<float2*>(p) = make_float2(s[m][n][2 * h], s[m][n][2 * h + 1]);
-    } else {
-      p[0] = s[m][n][2 * h];
-      if (c0 + c + 1 < Dv) p[1] = s[m][n][2 * h + 1];
-    }
-  });
+__device__ __forceinline__ float2 dl_unpack(uint32_t w) {
+  __nv_bfloat162 h;
+  memcpy(&h, &w, 4);
+  return __bfloat1622float2(h);
+}
+// Sixteen of an accumulator's columns (tiles c0, c1 of 8) as a left operand in PARTS parts.
+template <int PARTS>
+__device__ __forceinline__ void dl_left(const float (&c0)[4], const float (&c1)[4], uint32_t (&a)[PARTS][4]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    uint32_t w[PARTS];
+    const float(&c)[4] = i < 2 ? c0 : c1;
+    dl_split<PARTS>(c[2 * (i & 1)], c[2 * (i & 1) + 1], w);
+#pragma unroll
+    for (int p = 0; p < PARTS; ++p) a[p][i] = w[p];
+  }
+}
+// c0, c1 += A * B for 16 columns of the right operand in PB parts, products of parts i + j <= MOST.
+template <int PA, int PB, int MOST, bool KN>
+__device__ __forceinline__ void dl_step(float (&c0)[4], float (&c1)[4], const uint32_t (&a)[PA][4], const bf* b, int ld, int stride, int n0, int k0, int lane) {
+#pragma unroll
+  for (int j = PB - 1; j >= 0; --j) {  // small parts first
+    uint32_t rb[4];
+    dl_b<KN>(rb, b + j * stride, ld, n0, k0, lane);
+#pragma unroll
+    for (int i = PA - 1; i >= 0; --i)
+      if (i + j <= MOST) {
+        dl_mma(c0, a[i], rb[0], rb[1]);
+        dl_mma(c1, a[i], rb[2], rb[3]);
+      }
+  }
+}
+// A warp's state S' [16][DK], from and to [Dk][Dv] in memory: f(tile, element, row d, column c).
+template <int DK, typename F>
+__device__ __forceinline__ void dl_state(int lane, F f) {
+#pragma unroll
+  for (int n = 0; n < DK / 8; ++n)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) f(n, e, 8 * n + 2 * (lane & 3) + (e & 1), (lane >> 2) + 8 * (e >> 1));
 }
 __device__ __forceinline__ void dl_store2(bf* p, float x, float y, bool two) {
   if (two && (reinterpret_cast<uintptr_t>(p) & 3u) == 0) {
@@ -458,135 +487,366 @@ __device__ __forceinline__ void dl_store2(bf* p, float x, float y, bool two) {
     if (two) p[1] = __float2bfloat16_rn(y);
   }
 }
-// Rows of a chunk behind the sequence's end, in CB columns.
-template <int CB>
-__device__ __forceinline__ void dl_zero_rows(bf* g, long long step, int from, int to, int cols) {
-  for (int i = from * CB + threadIdx.x; i < to * CB; i += blockDim.x)
-    if (i % CB < cols) g[(i / CB) * step + i % CB] = __float2bfloat16_rn(0.f);
+// Sixteen columns of a chunk, [16][64] in accumulators, to rows of bf16; x times by[step] where by is given.
+__device__ __forceinline__ void dl_rows_out(const float (&x)[8][4], const float* by, bf* g, long long step, int live, int cols, int lane) {
+#pragma unroll
+  for (int n = 0; n < 8; ++n) {
+    float2 m = make_float2(1.f, 1.f);
+    if (by) m = *reinterpret_cast<const float2*>(by + 8 * n + 2 * (lane & 3));
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const uint32_t w = dl_transposed(dl_pack(x[n][2 * h] * m.x, x[n][2 * h + 1] * m.y));
+      const int r = 8 * n + (lane >> 2), c = 8 * h + 2 * (lane & 3);
+      if (r >= live || c >= cols) continue;
+      bf* p = g + r * step + c;
+      if (c + 1 < cols && (reinterpret_cast<uintptr_t>(p) & 3u) == 0) {
+        *reinterpret_cast<uint32_t*>(p) = w;
+      } else {
+        bf e[2];
+        memcpy(e, &w, 4);
+        p[0] = e[0];
+        if (c + 1 < cols) p[1] = e[1];
+      }
+    }
+  }
+}
+// Rows of a chunk behind the sequence's end.
+__device__ __forceinline__ void dl_zero_rows(bf* g, long long step, int from, int to, int cols, int t, int of) {
+  for (int i = from * cols + t; i < to * cols; i += of) g[(i / cols) * step + i % cols] = __float2bfloat16_rn(0.f);
 }
 
-// ---- forward from chunk to chunk --------------------------------------------------------------------
-// Three meetings of the warps a chunk: R = b (V - g K S) is there, U is there, the state is there.  What the next chunk reads is on its way meanwhile: each buffer is
-// asked for behind the meeting that ends its last use.
-template <int DK, int CB>
+template <int DK, int NP>
 struct DlScanShared {
-  static constexpr int LDC = CB + 8;
-  bf k[2][DL_CHUNK][DK + 8], q[DL_CHUNK][DK + 8];
-  bf tri[3][DL_CHUNK][DL_LD64];
-  bf p[2][DL_CHUNK][DL_LD64];
-  bf s[3][DK][LDC];
-  bf r[3][DL_CHUNK][LDC];
-  bf u[2][DL_CHUNK][LDC];
-  bf us[3][DL_CHUNK][LDC];  // U times G_Ci / |k_i|
-  DlRow row[2];
+  bf k[2][DL_CHUNK][DK + 8], q[2][DL_CHUNK][DK + 8];
+  bf tri[2][3][DL_CHUNK][DL_LD64];
+  bf p[2][2][DL_CHUNK][DL_LD64];
+  bf v[2][DL_CHUNK][NP * 16 + 8];
+  uint4 s[NP][DK / 16][2][32];  // the state's parts as left operands
+  uint4 u[NP][4][2][32];        // U's
+  DlSteps row[2];
 };
 
-template <int DK, int CB>
-__global__ void __launch_bounds__(DL_THREADS, 1) delta_scan_kernel(const DlArgs a) {
-  using Tl = DlTiles<DK, CB>;
-  constexpr int LDK = DK + 8, LDC = CB + 8, PS = DK * LDC, PC = DL_CHUNK * LDC, PT = DL_CHUNK * DL_LD64;
+template <int DK, int NP>
+__global__ void __launch_bounds__(64 * NP, 1) delta_scan_kernel(const DlArgs a) {
+  constexpr int LDK = DK + 8, LDV = NP * 16 + 8, PT = DL_CHUNK * DL_LD64, HELP = 32 * NP;
   extern __shared__ __align__(16) uint8_t dl_smem[];
-  auto& sh = *reinterpret_cast<DlScanShared<DK, CB>*>(dl_smem);
+  auto& sh = *reinterpret_cast<DlScanShared<DK, NP>*>(dl_smem);
   pdl_launch_dependents();
   pdl_wait_prior_grids();
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int blocks = (a.Dv + CB - 1) / CB;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, pair = warp % NP;
+  const bool helper = warp >= NP;
+  const int blocks = (a.Dv + NP * 16 - 1) / (NP * 16);
   const long long n = blockIdx.x / blocks, size = (long long)a.Dk * a.Dv, heads = (long long)a.B * a.heads;
-  const int c0 = (int)(blockIdx.x % blocks) * CB, cols = min(CB, a.Dv - c0);
-  const int sr = Tl::srow(warp), sc = Tl::scol(warp), hr = Tl::hrow(warp & 3), hc = Tl::hcol(warp & 3);
-  const bool reads = warp >= 4;  // half of the warps follow the keys, half the queries
-  float s[Tl::SM][2][4];
-  dl_state_get<Tl::SM>(s, a.h0 ? a.h0 + n * size : nullptr, a.Dk, a.Dv, c0, lane, sr, sc);
+  const int c0 = (int)(blockIdx.x % blocks) * NP * 16, cols = min(NP * 16, a.Dv - c0);  // the CTA's columns
+  const int mine = min(max(cols - 16 * pair, 0), 16);                                    // the pair's
   const DlUnit u0 = dl_unit(a, 0, n);
   const int len = a.lens ? min(max(a.lens[u0.b], 0), a.T) : a.T, chunks = (len + DL_CHUNK - 1) / DL_CHUNK;
   const bf *Q = a.Q + (long long)u0.head * a.Dk, *K = a.K + (long long)u0.head * a.Dk, *V = a.V + (long long)u0.head * a.Dv + c0;
   bf* Y = a.Y + (long long)u0.head * a.Dv + c0;
-  auto fetch_kq = [&](int chunk) {
+  auto fetch = [&](int chunk) {  // by the helpers
     if (chunk < chunks) {
       const DlUnit u = dl_unit(a, chunk, n);
-      dl_load<DK>(&sh.k[chunk & 1][0][0], LDK, K + u.row0 * a.ldk, a.B * a.ldk, u.live, a.Dk, a.vec_k);
-      dl_load<DK>(&sh.q[0][0], LDK, Q + u.row0 * a.ldq, a.B * a.ldq, u.live, a.Dk, a.vec_q);
-      dl_load_row(sh.row[chunk & 1], a.row + u.unit * DL_ROW_FLOATS);
+      const int at = chunk & 1, t = threadIdx.x - HELP;
+      dl_load<DK>(&sh.k[at][0][0], LDK, K + u.row0 * a.ldk, a.B * a.ldk, u.live, a.Dk, a.vec_k, t, HELP);
+      dl_load<DK>(&sh.q[at][0][0], LDK, Q + u.row0 * a.ldq, a.B * a.ldq, u.live, a.Dk, a.vec_q, t, HELP);
+      dl_load<NP * 16>(&sh.v[at][0][0], LDV, V + u.row0 * a.ldv, a.B * a.ldv, u.live, cols, a.vec_v, t, HELP);
+      dl_load64<3>(&sh.tri[at][0][0][0], a.tri + u.unit * 3 * DL_SQ, t, HELP);
+      dl_load64<2>(&sh.p[at][0][0][0], a.p + u.unit * 3 * DL_SQ, t, HELP);
+      dl_load_row(sh.row[at], a.row + u.unit * DL_ROW_FLOATS, t, HELP);
     }
     dl_commit();
   };
-  auto fetch_tri = [&](int chunk) {
-    if (chunk < chunks) dl_load64<3>(&sh.tri[0][0][0], a.tri + (chunk * heads + n) * 3 * DL_SQ);
-    dl_commit();
-  };
-  float v[Tl::HM][2][4] = {};
-  auto fetch_v = [&](int chunk) {
-    if (chunk >= chunks || reads) return;
-    const DlUnit u = dl_unit(a, chunk, n);
-    dl_each<Tl::HM>(lane, hr, hc, [&](int m, int i, int h, int r, int c) {
+  if (helper) {
+    fetch(0);
+    for (int chunk = 0; chunk < chunks; ++chunk) {
+      const int at = chunk & 1;
+      dl_wait<0>();
+      dl_meet(0, 64 * NP);
+      fetch(chunk + 1);
+      dl_meet(1 + pair, 64);  // the state's parts are there
+      float o[8][4] = {};
 #pragma unroll
-      for (int e = 0; e < 2; ++e) v[m][i][2 * h + e] = r < u.live && c + e < cols ? __bfloat162float(V[(u.row0 + (long long)r * a.B) * a.ldv + c + e]) : 0.f;
-    });
-  };
-  fetch_kq(0);
-  fetch_tri(0);
-  fetch_v(0);
-  for (int chunk = 0; chunk < chunks; ++chunk) {
-    const DlUnit u = dl_unit(a, chunk, n);
-    const DlRow& row = sh.row[chunk & 1];
-    const bf* k = &sh.k[chunk & 1][0][0];
-    if (a.S) dl_state_put<Tl::SM>(s, a.S + u.unit * size, a.Dk, a.Dv, c0, lane, sr, sc);
-    dl_each<Tl::SM>(lane, sr, sc, [&](int m, int i, int h, int d, int c) { dl_put<3>(&sh.s[0][d][c], PS, s[m][i][2 * h], s[m][i][2 * h + 1]); });
-    dl_wait<1>();
-    __syncthreads();
-    dl_load64<2>(&sh.p[0][0][0], a.p + u.unit * 3 * DL_SQ);
-    dl_commit();
-    float o[Tl::HM][2][4] = {};
-    if (reads) {
-      dl_product<Tl::HM, 2, false, true, 1, 2, 1>(o, &sh.q[0][0], LDK, 0, &sh.s[0][0][0], LDC, PS, hr, hc, 0, DK, lane);
-      dl_each<Tl::HM>(lane, hr, hc, [&](int m, int i, int h, int r, int) {
-        const float g = a.scale * row.first[r] * row.rq[r];
-        o[m][i][2 * h] *= g;
-        o[m][i][2 * h + 1] *= g;
-      });
-    } else {
-      dl_product<Tl::HM, 2, false, true, 1, 3, 2>(o, k, LDK, 0, &sh.s[0][0][0], LDC, PS, hr, hc, 0, DK, lane);
-      dl_each<Tl::HM>(lane, hr, hc, [&](int m, int i, int h, int r, int c) {
-        const float b = row.beta[r], g = -row.first[r] * row.rk[r];
-        dl_put<3>(&sh.r[0][r][c], PC, b * fmaf(g, o[m][i][2 * h], v[m][i][2 * h]), b * fmaf(g, o[m][i][2 * h + 1], v[m][i][2 * h + 1]));
-      });
+      for (int kd = 0; kd < DK / 16; ++kd) {
+        uint32_t s[2][4];
+#pragma unroll
+        for (int p = 0; p < 2; ++p) {
+          const uint4 x = sh.s[pair][kd][p][lane];
+          s[p][0] = x.x, s[p][1] = x.y, s[p][2] = x.z, s[p][3] = x.w;
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) dl_step<2, 1, 1, false>(o[2 * i], o[2 * i + 1], s, &sh.q[at][0][0], LDK, 0, 16 * i, 16 * kd, lane);
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float2 g = *reinterpret_cast<const float2*>(&sh.row[at].qin[8 * i + 2 * (lane & 3)]);
+        o[i][0] *= g.x, o[i][1] *= g.y, o[i][2] *= g.x, o[i][3] *= g.y;
+      }
+      dl_meet(1 + NP + pair, 64);  // U's are
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        uint32_t x[2][4];
+#pragma unroll
+        for (int p = 0; p < 2; ++p) {
+          const uint4 y = sh.u[pair][k][p][lane];
+          x[p][0] = y.x, x[p][1] = y.y, x[p][2] = y.z, x[p][3] = y.w;
+        }
+#pragma unroll
+        for (int i = k; i < 4; ++i) dl_step<2, 2, 1, false>(o[2 * i], o[2 * i + 1], x, &sh.p[at][0][0][0], DL_LD64, PT, 16 * i, 16 * k, lane);
+      }
+      const DlUnit u = dl_unit(a, chunk, n);
+      dl_rows_out(o, nullptr, Y + u.row0 * a.ldy + 16 * pair, a.B * a.ldy, u.live, mine, lane);
     }
-    dl_wait<1>();
-    __syncthreads();
-    fetch_kq(chunk + 1);
-    fetch_v(chunk + 1);
-    if (Tl::has(warp)) {
-      const int m0 = Tl::row(warp), n0 = Tl::col(warp);
-      float x[1][2][4] = {};
-      dl_product<1, 2, false, true, 3, 3, 2>(x, &sh.tri[0][0][0], DL_LD64, PT, &sh.r[0][0][0], LDC, PC, m0, n0, 0, m0 + 16, lane);
-      dl_each<1>(lane, m0, n0, [&](int, int i, int h, int r, int c) {
-        const float g = row.last[r] * row.rk[r], x0 = x[0][i][2 * h], x1 = x[0][i][2 * h + 1];
-        dl_put<2>(&sh.u[0][r][c], PC, x0, x1);
-        dl_put<3>(&sh.us[0][r][c], PC, g * x0, g * x1);
-      });
+  } else {
+    float s[DK / 8][4];
+    const float* h0 = a.h0 ? a.h0 + n * size + c0 + 16 * pair : nullptr;
+    dl_state<DK>(lane, [&](int i, int e, int d, int c) { s[i][e] = h0 && d < a.Dk && c < mine ? h0[(long long)d * a.Dv + c] : 0.f; });
+    auto put = [&](float* g) { dl_state<DK>(lane, [&](int i, int e, int d, int c) { if (d < a.Dk && c < mine) g[(long long)d * a.Dv + c] = s[i][e]; }); };
+    for (int chunk = 0; chunk < chunks; ++chunk) {
+      const int at = chunk & 1;
+      const DlSteps& row = sh.row[at];
+      if (a.S) put(a.S + (chunk * heads + n) * size + c0 + 16 * pair);
+      dl_meet(0, 64 * NP);
+      float e[8][4] = {};
+#pragma unroll
+      for (int kd = 0; kd < DK / 16; ++kd) {
+        uint32_t x[3][4];
+        dl_left<3>(s[2 * kd], s[2 * kd + 1], x);
+        sh.s[pair][kd][0][lane] = make_uint4(x[0][0], x[0][1], x[0][2], x[0][3]);
+        sh.s[pair][kd][1][lane] = make_uint4(x[1][0], x[1][1], x[1][2], x[1][3]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) dl_step<3, 1, 2, false>(e[2 * i], e[2 * i + 1], x, &sh.k[at][0][0], LDK, 0, 16 * i, 16 * kd, lane);
+      }
+      dl_meet(1 + pair, 64);
+#pragma unroll
+      for (int i = 0; i < 8; i += 2) {
+        uint32_t v[4];
+        dl_ldsm_t(v, &sh.v[at][8 * i + (lane & 7) + ((lane >> 4) << 3)][16 * pair + ((lane >> 3) & 1) * 8]);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const int r = 8 * (i + j) + 2 * (lane & 3);
+          const float2 b = *reinterpret_cast<const float2*>(&row.beta[r]), g = *reinterpret_cast<const float2*>(&row.kin[r]);
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const float2 x = dl_unpack(v[2 * j + h]);
+            e[i + j][2 * h] = b.x * fmaf(-g.x, e[i + j][2 * h], x.x);
+            e[i + j][2 * h + 1] = b.y * fmaf(-g.y, e[i + j][2 * h + 1], x.y);
+          }
+        }
+      }
+      float x[8][4] = {};
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        uint32_t r[3][4];
+        dl_left<3>(e[2 * k], e[2 * k + 1], r);
+#pragma unroll
+        for (int i = k; i < 4; ++i) dl_step<3, 3, 2, false>(x[2 * i], x[2 * i + 1], r, &sh.tri[at][0][0][0], DL_LD64, PT, 16 * i, 16 * k, lane);
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        uint32_t w[2][4];
+        dl_left<2>(x[2 * k], x[2 * k + 1], w);
+        sh.u[pair][k][0][lane] = make_uint4(w[0][0], w[0][1], w[0][2], w[0][3]);
+        sh.u[pair][k][1][lane] = make_uint4(w[1][0], w[1][1], w[1][2], w[1][3]);
+      }
+      dl_meet(1 + NP + pair, 64);
+      const float whole = row.first[DL_CHUNK - 1];
+#pragma unroll
+      for (int i = 0; i < DK / 8; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) s[i][j] *= whole;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+#pragma unroll
+        for (int i = 2 * k; i < 2 * k + 2; ++i) {
+          const float2 g = *reinterpret_cast<const float2*>(&row.kout[8 * i + 2 * (lane & 3)]);
+          x[i][0] *= g.x, x[i][1] *= g.y, x[i][2] *= g.x, x[i][3] *= g.y;
+        }
+        uint32_t w[3][4];
+        dl_left<3>(x[2 * k], x[2 * k + 1], w);
+#pragma unroll
+        for (int i = 0; i < DK / 16; ++i) dl_step<3, 1, 2, true>(s[2 * i], s[2 * i + 1], w, &sh.k[at][0][0], LDK, 0, 16 * i, 16 * k, lane);
+      }
     }
-    dl_wait<1>();
-    __syncthreads();
-    fetch_tri(chunk + 1);
-    const float whole = row.first[DL_CHUNK - 1];
-#pragma unroll
-    for (int m = 0; m < Tl::SM; ++m)
-#pragma unroll
-      for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) s[m][i][e] *= whole;
-    dl_product<Tl::SM, 2, true, true, 1, 3, 2>(s, k, LDK, 0, &sh.us[0][0][0], LDC, PC, sr, sc, 0, DL_CHUNK, lane);
-    if (reads) {
-      dl_product<Tl::HM, 2, false, true, 2, 2, 1>(o, &sh.p[0][0][0], DL_LD64, PT, &sh.u[0][0][0], LDC, PC, hr, hc, 0, hr + 16 * Tl::HM, lane);
-      dl_each<Tl::HM>(lane, hr, hc, [&](int m, int i, int h, int r, int c) {
-        if (r < u.live && c < cols) dl_store2(Y + (u.row0 + (long long)r * a.B) * a.ldy + c, o[m][i][2 * h], o[m][i][2 * h + 1], c + 1 < cols);
-      });
-    }
+    if (a.hT) put(a.hT + n * size + c0 + 16 * pair);
   }
-  if (a.hT) dl_state_put<Tl::SM>(s, a.hT + n * size, a.Dk, a.Dv, c0, lane, sr, sc);
   for (int chunk = len / DL_CHUNK; chunk * DL_CHUNK < a.T; ++chunk) {
     const DlUnit u = dl_unit(a, chunk, n);
-    dl_zero_rows<CB>(Y + u.row0 * a.ldy, a.B * a.ldy, u.live, min(DL_CHUNK, a.T - chunk * DL_CHUNK), cols);
+    dl_zero_rows(Y + u.row0 * a.ldy, a.B * a.ldy, u.live, min(DL_CHUNK, a.T - chunk * DL_CHUNK), cols, threadIdx.x, 64 * NP);
+  }
+}
+
+// The adjoint: F' = D' K', dU' = G' + G_C F', X' = dU' T, D' = g_C D' + Y' + W' K with W = -g b X; the helpers bring G = scale P^T dY and Y = Q^T (scale g dY), which come
+// from the chunk alone.  P, which only they read, and only at first, is fetched behind its last use.
+template <int DK, int NP>
+struct DlBackShared {
+  bf k[2][DL_CHUNK][DK + 8], q[2][DL_CHUNK][DK + 8];
+  bf tri[2][3][DL_CHUNK][DL_LD64];
+  bf p[3][DL_CHUNK][DL_LD64];
+  bf dy[2][DL_CHUNK][NP * 16 + 8];
+  float4 g[NP][8][32];
+  float4 y[NP][DK / 8][32];
+  DlSteps row[2];
+};
+
+template <int DK, int NP>
+__global__ void __launch_bounds__(64 * NP, 1) delta_back_kernel(const DlArgs a) {
+  constexpr int LDK = DK + 8, LDV = NP * 16 + 8, PT = DL_CHUNK * DL_LD64, HELP = 32 * NP;
+  extern __shared__ __align__(16) uint8_t dl_smem[];
+  auto& sh = *reinterpret_cast<DlBackShared<DK, NP>*>(dl_smem);
+  pdl_launch_dependents();
+  pdl_wait_prior_grids();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, pair = warp % NP;
+  const bool helper = warp >= NP;
+  const int blocks = (a.Dv + NP * 16 - 1) / (NP * 16);
+  const long long n = blockIdx.x / blocks, size = (long long)a.Dk * a.Dv;
+  const int c0 = (int)(blockIdx.x % blocks) * NP * 16, cols = min(NP * 16, a.Dv - c0);
+  const int mine = min(max(cols - 16 * pair, 0), 16);
+  const DlUnit u0 = dl_unit(a, 0, n);
+  const int len = a.lens ? min(max(a.lens[u0.b], 0), a.T) : a.T, chunks = (len + DL_CHUNK - 1) / DL_CHUNK;
+  const bf *Q = a.Q + (long long)u0.head * a.Dk, *K = a.K + (long long)u0.head * a.Dk, *dY = a.dY + (long long)u0.head * a.Dv + c0;
+  bf* dV = a.dV + (long long)u0.head * a.Dv + c0;
+  if (helper) {
+    const int t = threadIdx.x - HELP;
+    auto fetch = [&](int chunk) {
+      if (chunk >= 0) {
+        const DlUnit u = dl_unit(a, chunk, n);
+        const int at = chunk & 1;
+        dl_load<DK>(&sh.k[at][0][0], LDK, K + u.row0 * a.ldk, a.B * a.ldk, u.live, a.Dk, a.vec_k, t, HELP);
+        dl_load<DK>(&sh.q[at][0][0], LDK, Q + u.row0 * a.ldq, a.B * a.ldq, u.live, a.Dk, a.vec_q, t, HELP);
+        dl_load<NP * 16>(&sh.dy[at][0][0], LDV, dY + u.row0 * a.lddy, a.B * a.lddy, u.live, cols, a.vec_dy, t, HELP);
+        dl_load64<3>(&sh.tri[at][0][0][0], a.tri + u.unit * 3 * DL_SQ, t, HELP);
+        dl_load_row(sh.row[at], a.row + u.unit * DL_ROW_FLOATS, t, HELP);
+      }
+    };
+    auto fetch_p = [&](int chunk) {
+      if (chunk >= 0) dl_load64<3>(&sh.p[0][0][0], a.p + dl_unit(a, chunk, n).unit * 3 * DL_SQ, t, HELP);
+    };
+    fetch(chunks - 1);
+    fetch_p(chunks - 1);
+    dl_commit();
+    for (int chunk = chunks - 1; chunk >= 0; --chunk) {
+      const int at = chunk & 1;
+      dl_wait<0>();
+      dl_meet(0, 64 * NP);
+      fetch(chunk - 1);
+      uint32_t y[4][1][4];  // dY' as a left operand
+#pragma unroll
+      for (int k = 0; k < 4; ++k) dl_a<true>(y[k][0], &sh.dy[at][0][0], LDV, 16 * pair, 16 * k, lane);
+      {
+        float g[8][4] = {};
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+#pragma unroll
+          for (int j = 0; j <= k; ++j) dl_step<1, 3, 2, true>(g[2 * j], g[2 * j + 1], y[k], &sh.p[0][0][0], DL_LD64, PT, 16 * j, 16 * k, lane);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sh.g[pair][i][lane] = make_float4(g[i][0], g[i][1], g[i][2], g[i][3]);
+      }
+      dl_meet(1 + pair, 64);
+      dl_meet(1 + 2 * NP, HELP);  // all of them have read P
+      fetch_p(chunk - 1);
+      dl_commit();
+      float s[DK / 8][4] = {};
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const float2 m0 = *reinterpret_cast<const float2*>(&sh.row[at].qin[16 * k + 2 * (lane & 3)]), m1 = *reinterpret_cast<const float2*>(&sh.row[at].qin[16 * k + 8 + 2 * (lane & 3)]);
+        uint32_t x[3][4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float2 v = dl_unpack(y[k][0][i]);
+          const float2 m = i < 2 ? m0 : m1;
+          uint32_t w[3];
+          dl_split<3>(v.x * m.x, v.y * m.y, w);
+#pragma unroll
+          for (int p = 0; p < 3; ++p) x[p][i] = w[p];
+        }
+#pragma unroll
+        for (int i = 0; i < DK / 16; ++i) dl_step<3, 1, 2, true>(s[2 * i], s[2 * i + 1], x, &sh.q[at][0][0], LDK, 0, 16 * i, 16 * k, lane);
+      }
+#pragma unroll
+      for (int i = 0; i < DK / 8; ++i) sh.y[pair][i][lane] = make_float4(s[i][0], s[i][1], s[i][2], s[i][3]);
+      dl_meet(1 + NP + pair, 64);
+    }
+  } else {
+    float s[DK / 8][4];
+    const float* last = a.dhT ? a.dhT + n * size + c0 + 16 * pair : nullptr;
+    dl_state<DK>(lane, [&](int i, int e, int d, int c) { s[i][e] = last && d < a.Dk && c < mine ? last[(long long)d * a.Dv + c] : 0.f; });
+    const bool here = c0 + 16 * pair < a.ldx;  // the work's rows end with 64 or 128 columns
+    for (int chunk = chunks - 1; chunk >= 0; --chunk) {
+      const int at = chunk & 1;
+      const DlSteps& row = sh.row[at];
+      const DlUnit u = dl_unit(a, chunk, n);
+      dl_meet(0, 64 * NP);
+      float f[8][4] = {};
+      bf* D = a.d + u.unit * 2 * DK * a.ldx + c0 + 16 * pair;
+#pragma unroll
+      for (int kd = 0; kd < DK / 16; ++kd) {
+        uint32_t x[3][4];
+        dl_left<3>(s[2 * kd], s[2 * kd + 1], x);
+#pragma unroll
+        for (int p = 0; p < 2; ++p)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const uint32_t w = dl_transposed(x[p][i]);
+            if (here) *reinterpret_cast<uint32_t*>(D + ((long long)p * DK + 16 * kd + 8 * (i >> 1) + (lane >> 2)) * a.ldx + 8 * (i & 1) + 2 * (lane & 3)) = w;
+          }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) dl_step<3, 1, 2, false>(f[2 * i], f[2 * i + 1], x, &sh.k[at][0][0], LDK, 0, 16 * i, 16 * kd, lane);
+      }
+      dl_meet(1 + pair, 64);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float4 g = sh.g[pair][i][lane];
+        const float2 l = *reinterpret_cast<const float2*>(&row.kout[8 * i + 2 * (lane & 3)]);
+        f[i][0] = fmaf(l.x, f[i][0], g.x), f[i][1] = fmaf(l.y, f[i][1], g.y), f[i][2] = fmaf(l.x, f[i][2], g.z), f[i][3] = fmaf(l.y, f[i][3], g.w);
+      }
+      float x[8][4] = {};
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        uint32_t r[3][4];
+        dl_left<3>(f[2 * k], f[2 * k + 1], r);
+#pragma unroll
+        for (int j = 0; j <= k; ++j) dl_step<3, 3, 2, true>(x[2 * j], x[2 * j + 1], r, &sh.tri[at][0][0][0], DL_LD64, PT, 16 * j, 16 * k, lane);
+      }
+      dl_rows_out(x, row.beta, dV + u.row0 * a.lddv + 16 * pair, a.B * a.lddv, u.live, mine, lane);
+      bf* X = a.x + u.unit * 2 * DL_CHUNK * a.ldx + c0 + 16 * pair;
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          uint32_t w[2];
+          dl_split<2>(x[i][2 * h], x[i][2 * h + 1], w);
+#pragma unroll
+          for (int p = 0; p < 2; ++p) {
+            const uint32_t y = dl_transposed(w[p]);
+            if (here) *reinterpret_cast<uint32_t*>(X + ((long long)p * DL_CHUNK + 8 * i + (lane >> 2)) * a.ldx + 8 * h + 2 * (lane & 3)) = y;
+          }
+        }
+      dl_meet(1 + NP + pair, 64);
+      const float whole = row.first[DL_CHUNK - 1];
+#pragma unroll
+      for (int i = 0; i < DK / 8; ++i) {
+        const float4 y = sh.y[pair][i][lane];
+        s[i][0] = fmaf(whole, s[i][0], y.x), s[i][1] = fmaf(whole, s[i][1], y.y), s[i][2] = fmaf(whole, s[i][2], y.z), s[i][3] = fmaf(whole, s[i][3], y.w);
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+#pragma unroll
+        for (int i = 2 * k; i < 2 * k + 2; ++i) {
+          const int r = 8 * i + 2 * (lane & 3);
+          const float2 b = *reinterpret_cast<const float2*>(&row.beta[r]), g = *reinterpret_cast<const float2*>(&row.kin[r]);
+          x[i][0] *= -b.x * g.x, x[i][1] *= -b.y * g.y, x[i][2] *= -b.x * g.x, x[i][3] *= -b.y * g.y;
+        }
+        uint32_t w[3][4];
+        dl_left<3>(x[2 * k], x[2 * k + 1], w);
+#pragma unroll
+        for (int i = 0; i < DK / 16; ++i) dl_step<3, 1, 2, true>(s[2 * i], s[2 * i + 1], w, &sh.k[at][0][0], LDK, 0, 16 * i, 16 * k, lane);
+      }
+    }
+    if (a.dh0) dl_state<DK>(lane, [&](int i, int e, int d, int c) { if (d < a.Dk && c < mine) a.dh0[n * size + (long long)d * a.Dv + c0 + 16 * pair + c] = s[i][e]; });
+  }
+  for (int chunk = len / DL_CHUNK; chunk * DL_CHUNK < a.T; ++chunk) {
+    const DlUnit u = dl_unit(a, chunk, n);
+    dl_zero_rows(dV + u.row0 * a.lddv, a.B * a.lddv, u.live, min(DL_CHUNK, a.T - chunk * DL_CHUNK), cols, threadIdx.x, 64 * NP);
   }
 }
 
@@ -723,122 +983,6 @@ __global__ void __launch_bounds__(DL_THREADS) delta_steps_kernel(const DlArgs a)
   if (a.hT) store(a.hT + n * size);
 }
 
-// ---- adjoint from chunk to chunk --------------------------------------------------------------------
-// As the forward scan: dU is there, W = -g b X / |k| is there, the gradient of the state is there.
-template <int DK, int CB>
-struct DlBackShared {
-  static constexpr int LDC = CB + 8;
-  bf k[2][DL_CHUNK][DK + 8], q[DL_CHUNK][DK + 8];
-  bf tri[3][DL_CHUNK][DL_LD64];
-  bf p[3][DL_CHUNK][DL_LD64];
-  bf d[3][DK][LDC];
-  bf dy[DL_CHUNK][LDC];
-  bf du[3][DL_CHUNK][LDC];
-  bf w[3][DL_CHUNK][LDC];
-  bf ys[3][DL_CHUNK][LDC];  // scale g / |q| dY
-  DlRow row[2];
-};
-
-template <int DK, int CB>
-__global__ void __launch_bounds__(DL_THREADS, 1) delta_back_kernel(const DlArgs a) {
-  using Tl = DlTiles<DK, CB>;
-  constexpr int LDK = DK + 8, LDC = CB + 8, PS = DK * LDC, PC = DL_CHUNK * LDC, PT = DL_CHUNK * DL_LD64;
-  extern __shared__ __align__(16) uint8_t dl_smem[];
-  auto& sh = *reinterpret_cast<DlBackShared<DK, CB>*>(dl_smem);
-  pdl_launch_dependents();
-  pdl_wait_prior_grids();
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int blocks = (a.Dv + CB - 1) / CB;
-  const long long n = blockIdx.x / blocks, size = (long long)a.Dk * a.Dv, heads = (long long)a.B * a.heads;
-  const int c0 = (int)(blockIdx.x % blocks) * CB, cols = min(CB, a.Dv - c0);
-  const int sr = Tl::srow(warp), sc = Tl::scol(warp);
-  float s[Tl::SM][2][4];
-  dl_state_get<Tl::SM>(s, a.dhT ? a.dhT + n * size : nullptr, a.Dk, a.Dv, c0, lane, sr, sc);
-  const DlUnit u0 = dl_unit(a, 0, n);
-  const int len = a.lens ? min(max(a.lens[u0.b], 0), a.T) : a.T, chunks = (len + DL_CHUNK - 1) / DL_CHUNK;
-  const bf *Q = a.Q + (long long)u0.head * a.Dk, *K = a.K + (long long)u0.head * a.Dk, *dY = a.dY + (long long)u0.head * a.Dv + c0;
-  bf* dV = a.dV + (long long)u0.head * a.Dv + c0;
-  auto fetch_k = [&](int chunk) {  // and what the first stage reads beside it
-    if (chunk >= 0) {
-      const DlUnit u = dl_unit(a, chunk, n);
-      dl_load<DK>(&sh.k[chunk & 1][0][0], LDK, K + u.row0 * a.ldk, a.B * a.ldk, u.live, a.Dk, a.vec_k);
-      dl_load<CB>(&sh.dy[0][0], LDC, dY + u.row0 * a.lddy, a.B * a.lddy, u.live, cols, a.vec_dy);
-      dl_load64<3>(&sh.p[0][0][0], a.p + u.unit * 3 * DL_SQ);
-      dl_load_row(sh.row[chunk & 1], a.row + u.unit * DL_ROW_FLOATS);
-    }
-    dl_commit();
-  };
-  auto fetch_tri = [&](int chunk) {
-    if (chunk >= 0) dl_load64<3>(&sh.tri[0][0][0], a.tri + (chunk * heads + n) * 3 * DL_SQ);
-    dl_commit();
-  };
-  fetch_k(chunks - 1);
-  fetch_tri(chunks - 1);
-  for (int chunk = chunks - 1; chunk >= 0; --chunk) {
-    const DlUnit u = dl_unit(a, chunk, n);
-    const DlRow& row = sh.row[chunk & 1];
-    const bf* k = &sh.k[chunk & 1][0][0];
-    bf* D = a.d + u.unit * 2 * DK * a.ldx + c0;
-    dl_each<Tl::SM>(lane, sr, sc, [&](int m, int i, int h, int d, int c) {
-      uint32_t w[3];
-      dl_split<3>(s[m][i][2 * h], s[m][i][2 * h + 1], w);
-#pragma unroll
-      for (int e = 0; e < 3; ++e) {
-        *reinterpret_cast<uint32_t*>(&sh.d[e][d][c]) = w[e];
-        if (e < 2) *reinterpret_cast<uint32_t*>(D + ((long long)e * DK + d) * a.ldx + c) = w[e];
-      }
-    });
-    dl_wait<1>();
-    __syncthreads();
-    dl_load<DK>(&sh.q[0][0], LDK, Q + u.row0 * a.ldq, a.B * a.ldq, u.live, a.Dk, a.vec_q);
-    dl_commit();
-    if (Tl::has(warp)) {
-      const int m0 = Tl::row(warp), n0 = Tl::col(warp);
-      float f[1][2][4] = {}, g[1][2][4] = {};
-      dl_product<1, 2, false, true, 1, 3, 2>(f, k, LDK, 0, &sh.d[0][0][0], LDC, PS, m0, n0, 0, DK, lane);
-      dl_product<1, 2, true, true, 3, 1, 2>(g, &sh.p[0][0][0], DL_LD64, PT, &sh.dy[0][0], LDC, 0, m0, n0, m0, DL_CHUNK, lane);
-      dl_each<1>(lane, m0, n0, [&](int, int i, int h, int r, int c) {
-        const float l = row.last[r] * row.rk[r], gq = a.scale * row.first[r] * row.rq[r];
-        dl_put<3>(&sh.du[0][r][c], PC, fmaf(l, f[0][i][2 * h], g[0][i][2 * h]), fmaf(l, f[0][i][2 * h + 1], g[0][i][2 * h + 1]));
-        const float2 dy = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&sh.dy[r][c]));
-        dl_put<3>(&sh.ys[0][r][c], PC, gq * dy.x, gq * dy.y);
-      });
-    }
-    dl_wait<1>();
-    __syncthreads();
-    fetch_k(chunk - 1);
-    if (Tl::has(warp)) {
-      const int m0 = Tl::row(warp), n0 = Tl::col(warp);
-      float x[1][2][4] = {};
-      dl_product<1, 2, true, true, 3, 3, 2>(x, &sh.tri[0][0][0], DL_LD64, PT, &sh.du[0][0][0], LDC, PC, m0, n0, m0, DL_CHUNK, lane);
-      bf* X = a.x + u.unit * 2 * DL_CHUNK * a.ldx + c0;
-      dl_each<1>(lane, m0, n0, [&](int, int i, int h, int r, int c) {
-        const float beta = row.beta[r], g = -row.first[r] * row.rk[r] * beta, x0 = x[0][i][2 * h], x1 = x[0][i][2 * h + 1];
-        dl_put<3>(&sh.w[0][r][c], PC, g * x0, g * x1);
-        dl_put<2>(X + (long long)r * a.ldx + c, DL_CHUNK * a.ldx, x0, x1);
-        if (r < u.live && c < cols) dl_store2(dV + (u.row0 + (long long)r * a.B) * a.lddv + c, beta * x0, beta * x1, c + 1 < cols);
-      });
-    }
-    dl_wait<1>();
-    __syncthreads();
-    fetch_tri(chunk - 1);
-    const float whole = row.first[DL_CHUNK - 1];
-#pragma unroll
-    for (int m = 0; m < Tl::SM; ++m)
-#pragma unroll
-      for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) s[m][i][e] *= whole;
-    dl_product<Tl::SM, 2, true, true, 1, 3, 2>(s, &sh.q[0][0], LDK, 0, &sh.ys[0][0][0], LDC, PC, sr, sc, 0, DL_CHUNK, lane);
-    dl_product<Tl::SM, 2, true, true, 1, 3, 2>(s, k, LDK, 0, &sh.w[0][0][0], LDC, PC, sr, sc, 0, DL_CHUNK, lane);
-  }
-  if (a.dh0) dl_state_put<Tl::SM>(s, a.dh0 + n * size, a.Dk, a.Dv, c0, lane, sr, sc);
-  for (int chunk = len / DL_CHUNK; chunk * DL_CHUNK < a.T; ++chunk) {
-    const DlUnit u = dl_unit(a, chunk, n);
-    dl_zero_rows<CB>(dV + u.row0 * a.lddv, a.B * a.lddv, u.live, min(DL_CHUNK, a.T - chunk * DL_CHUNK), cols);
-  }
-}
-
 // ---- a chunk's own gradients ------------------------------------------------------------------------
 // With U again from the state S_0 that the forward call left, and o the products of entries,
 //   N = scale G o (dY U^T) (j <= i),  M = -b G o (X U^T) (j < i),
@@ -943,18 +1087,18 @@ __global__ void __launch_bounds__(DL_GRAD_THREADS) delta_grad_kernel(const DlArg
   const int steps = min(DL_CHUNK, a.T - u.chunk * DL_CHUNK);
   bf* dq = a.dQ + u.row0 * a.lddq + (long long)u.head * a.Dk;
   bf* dk = a.dK + u.row0 * a.lddk + (long long)u.head * a.Dk;
-  dl_zero_rows<DK>(dq, a.B * a.lddq, u.live, steps, a.Dk);
-  dl_zero_rows<DK>(dk, a.B * a.lddk, u.live, steps, a.Dk);
+  dl_zero_rows(dq, a.B * a.lddq, u.live, steps, a.Dk, t, DL_GRAD_THREADS);
+  dl_zero_rows(dk, a.B * a.lddk, u.live, steps, a.Dk, t, DL_GRAD_THREADS);
   if (t >= u.live && t < steps) {
     const long long z = (u.row0 + (long long)t * a.B) * a.lddz + u.head;
     a.dZf[z] = a.dZb[z] = __float2bfloat16_rn(0.f);
   }
   if (u.live == 0) return;
-  dl_load<DK>(&sh.k[0][0], LDK, a.K + u.row0 * a.ldk + (long long)u.head * a.Dk, a.B * a.ldk, u.live, a.Dk, a.vec_k);
-  dl_load<DK>(&sh.q[0][0], LDK, a.Q + u.row0 * a.ldq + (long long)u.head * a.Dk, a.B * a.ldq, u.live, a.Dk, a.vec_q);
-  dl_load<DV>(&sh.dy[0][0], LDV, a.dY + u.row0 * a.lddy + (long long)u.head * a.Dv, a.B * a.lddy, u.live, a.Dv, a.vec_dy);
-  dl_load64<2>(&sh.tri[0][0][0], a.tri + u.unit * 3 * DL_SQ);
-  dl_load_row(sh.row, a.row + u.unit * DL_ROW_FLOATS);
+  dl_load<DK>(&sh.k[0][0], LDK, a.K + u.row0 * a.ldk + (long long)u.head * a.Dk, a.B * a.ldk, u.live, a.Dk, a.vec_k, t, DL_GRAD_THREADS);
+  dl_load<DK>(&sh.q[0][0], LDK, a.Q + u.row0 * a.ldq + (long long)u.head * a.Dk, a.B * a.ldq, u.live, a.Dk, a.vec_q, t, DL_GRAD_THREADS);
+  dl_load<DV>(&sh.dy[0][0], LDV, a.dY + u.row0 * a.lddy + (long long)u.head * a.Dv, a.B * a.lddy, u.live, a.Dv, a.vec_dy, t, DL_GRAD_THREADS);
+  dl_load64<2>(&sh.tri[0][0][0], a.tri + u.unit * 3 * DL_SQ, t, DL_GRAD_THREADS);
+  dl_load_row(sh.row, a.row + u.unit * DL_ROW_FLOATS, t, DL_GRAD_THREADS);
   dl_load_parts<DL_CHUNK, DV, 2>(&sh.x[0][0][0], a.x + u.unit * 2 * DL_CHUNK * a.ldx, a.ldx, a.Dv);
   dl_commit();
   // this warp's tile; where work grows or falls with the row, the warps of a scheduler have the same between them
@@ -1229,25 +1373,30 @@ ard_status dl_run(ard_ctx* ctx, K kern, long long grid, int threads, size_t smem
   ARD_CUDA_OK(cudaGetLastError());
   return ARD_OK;
 }
-template <int DK, int CB>
+template <int DK, int NP>
+ard_status dl_scan(ard_ctx* ctx, const DlArgs& a, bool backward, cudaStream_t s) {
+  const long long grid = (long long)a.B * a.heads * ((a.Dv + NP * 16 - 1) / (NP * 16));
+  return backward ? dl_run(ctx, delta_back_kernel<DK, NP>, grid, 64 * NP, sizeof(DlBackShared<DK, NP>), a, s)
+                  : dl_run(ctx, delta_scan_kernel<DK, NP>, grid, 64 * NP, sizeof(DlScanShared<DK, NP>), a, s);
+}
+template <int DK>
 ard_status dl_chunks(ard_ctx* ctx, const DlArgs& a, bool backward, cudaStream_t s) {
-  const long long units = dl_units(a.T, a.B, a.heads), grid = (long long)a.B * a.heads * ((a.Dv + CB - 1) / CB);
+  const long long units = dl_units(a.T, a.B, a.heads), groups = (a.Dv + 15) / 16, pairs = (long long)a.B * a.heads * groups;
   ard_status st = dl_run(ctx, delta_prep_kernel<DK>, units, DL_THREADS, sizeof(DlPrepShared<DK>), a, s);
   if (st != ARD_OK) return st;
-  if (!backward) return dl_run(ctx, delta_scan_kernel<DK, CB>, grid, DL_THREADS, sizeof(DlScanShared<DK, CB>), a, s);
-  st = dl_run(ctx, delta_back_kernel<DK, CB>, grid, DL_THREADS, sizeof(DlBackShared<DK, CB>), a, s);
-  if (st != ARD_OK) return st;
+  // columns go to as many SMs as there are, at most 64 to one
+  if (groups == 1 || pairs <= ctx->sm_count) st = dl_scan<DK, 1>(ctx, a, backward, s);
+  else if (groups == 2 || pairs <= 2ll * ctx->sm_count) st = dl_scan<DK, 2>(ctx, a, backward, s);
+  else st = dl_scan<DK, 4>(ctx, a, backward, s);
+  if (st != ARD_OK || !backward) return st;
   if (a.Dv <= 64) return dl_run(ctx, delta_grad_kernel<DK, 64>, units, DL_GRAD_THREADS, sizeof(DlGradShared<DK, 64>), a, s);
   return dl_run(ctx, delta_grad_kernel<DK, 128>, units, DL_GRAD_THREADS, sizeof(DlGradShared<DK, 128>), a, s);
 }
 ard_status dl_chunks(ard_ctx* ctx, const DlArgs& a, bool backward, cudaStream_t s) {
-  if (a.Dk <= 64) return dl_chunks<64, 32>(ctx, a, backward, s);
-  // columns of a state: 32 a CTA, 16 where that still leaves an SM for each
-  const bool few = (long long)a.B * a.heads * ((a.Dv + 15) / 16) <= ctx->sm_count;
-  return few ? dl_chunks<128, 16>(ctx, a, backward, s) : dl_chunks<128, 32>(ctx, a, backward, s);
+  return a.Dk <= 64 ? dl_chunks<64>(ctx, a, backward, s) : dl_chunks<128>(ctx, a, backward, s);
 }
 
-static_assert(sizeof(DlGradShared<128, 128>) <= 227 * 1024 && sizeof(DlBackShared<128, 32>) <= 227 * 1024 && sizeof(DlScanShared<128, 32>) <= 227 * 1024,
+static_assert(sizeof(DlGradShared<128, 128>) <= 227 * 1024 && sizeof(DlBackShared<128, 4>) <= 227 * 1024 && sizeof(DlScanShared<128, 4>) <= 227 * 1024,
               "shared memory of an SM");
 
 }  // namespace
@@ -1266,7 +1415,7 @@ ard_status launch_delta_forward(ard_ctx* ctx, int T, int B, int heads, int Dk, i
   a.Q = (const bf*)Q, a.K = (const bf*)K, a.V = (const bf*)V, a.ldq = ldq, a.ldk = ldk, a.ldv = ldv;
   a.Zf = (const bf*)Zf, a.Zb = (const bf*)Zb, a.ldz = ldz;
   a.lens = lens, a.h0 = h0, a.Y = (bf*)Y, a.ldy = ldy, a.hT = hT, a.S = S;
-  a.vec_q = dl_on16(Q, ldq, Dk), a.vec_k = dl_on16(K, ldk, Dk);
+  a.vec_q = dl_on16(Q, ldq, Dk), a.vec_k = dl_on16(K, ldk, Dk), a.vec_v = dl_on16(V, ldv, Dv);
   if (T <= DL_STEPS) {
     auto on16 = [](const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; };
     const bool vec = Dv % 4 == 0 && on16(h0) && on16(hT) && on16(S);
