@@ -58,7 +58,7 @@ struct DlArgs {
   bf* p;       // [units][3][64][64] scale * (G o Q K^T) in three parts
   float* row;  // [units][DL_ROW_FLOATS]
   bf* x;       // [units][2][64][ldx] X in two parts
-  bf* d;       // [units][2][DK][ldx] the gradient of the state behind a chunk
+  bf* d;       // [units][2][ldx][DK] the gradient of the state behind a chunk, transposed
   int ldx;
 };
 
@@ -81,14 +81,6 @@ struct DlRow : DlSteps {
 };
 constexpr int DL_ROW_FLOATS = (int)(sizeof(DlRow) / 4);
 static_assert(sizeof(DlRow) % 16 == 0 && sizeof(DlSteps) % 16 == 0, "copied in pieces of 16 bytes");
-
-__device__ __forceinline__ float dl_decay(const DlRow& r, int i, int j) {  // i >= j, or j in i's block
-  const int bi = i >> 4, bj = j >> 4;
-  if (bi == bj) return r.diag[bi][i & 15][j & 15];
-  float g = r.from[i] * r.to[j];
-  for (int b = bj + 1; b < bi; ++b) g *= r.block[b];
-  return g;
-}
 
 // ---- building blocks --------------------------------------------------------------------------------
 __device__ __forceinline__ void dl_ldsm(uint32_t (&r)[4], const bf* p) {
@@ -127,7 +119,7 @@ template <int MT, int NT, bool AT, bool BKN, int PA, int PB, int MOST>
 __device__ __forceinline__ void dl_product(float (&c)[MT][NT][4], const bf* a, int lda, int sa, const bf* b, int ldb, int sb, int m0, int n0, int k0,
                                            int k1, int lane) {
   static_assert(NT % 2 == 0, "columns by sixteens");
-#pragma unroll 2
+#pragma unroll 4
   for (int k = k0; k < k1; k += 16) {
     uint32_t ra[MT][PA][4];
 #pragma unroll
@@ -162,8 +154,8 @@ __device__ __forceinline__ void dl_split(float x, float y, uint32_t (&w)[PARTS])
     const __nv_bfloat162 h = __floats2bfloat162_rn(x, y);
     memcpy(&w[i], &h, 4);
     if (i + 1 < PARTS) {
-      x -= __low2float(h);
-      y -= __high2float(h);
+      const float2 r = __ffma2_rn(__bfloat1622float2(h), make_float2(-1.f, -1.f), make_float2(x, y));
+      x = r.x, y = r.y;
     }
   }
 }
@@ -192,35 +184,40 @@ __device__ __forceinline__ void dl_wait() {
 }
 
 // [64][cols] of a matrix whose rows are `step` elements apart, on its way to shared memory with pitch ld; rows from `live` on and columns up to PAD are
-// zeros.  Rows off the grid of 16 bytes go through registers, at once.  By threads t of `of`.
-template <int PAD>
-__device__ __forceinline__ void dl_load(bf* s, int ld, const bf* g, long long step, int live, int cols, int vec, int t, int of) {
-  constexpr int PIECES = PAD / 8;
-#pragma unroll 4
-  for (int i = t; i < DL_CHUNK * PIECES; i += of) {
-    const int r = i / PIECES, c = (i % PIECES) * 8;
-    const bool there = r < live && c < cols;
-    const bf* p = there ? g + r * step + c : g;
-    if (vec) {
-      dl_copy16(s + r * ld + c, p, there);
-    } else {
-      bf e[8];
+// zeros.  Rows off the grid of 16 bytes go through registers, at once.  By threads t of OF.
+template <int PAD, int OF>
+__device__ __forceinline__ void dl_load(bf* s, int ld, const bf* g, long long step, int live, int cols, int vec, int t) {
+  constexpr int PIECES = PAD / 8, ROWS = OF / PIECES, ROUNDS = DL_CHUNK / ROWS;
+  static_assert(OF % PIECES == 0 && DL_CHUNK % ROWS == 0, "whole rows a round");
+  const int c = (t % PIECES) * 8, r0 = t / PIECES;
+  const bool inside = c < cols;
+  const bf* p = g + r0 * step + (inside ? c : 0);
+  bf* d = s + r0 * ld + c;
+  if (vec) {
+    if (live == DL_CHUNK) {
 #pragma unroll
-      for (int k = 0; k < 8; ++k) e[k] = there && c + k < cols ? p[k] : __float2bfloat16_rn(0.f);
-      uint4 q;
-      memcpy(&q, e, 16);
-      *reinterpret_cast<uint4*>(s + r * ld + c) = q;
+      for (int i = 0; i < ROUNDS; ++i, p += ROWS * step) dl_copy16(d + i * ROWS * ld, p, inside);
+    } else {
+      for (int i = 0; i < ROUNDS; ++i, p += ROWS * step) dl_copy16(d + i * ROWS * ld, r0 + i * ROWS < live ? p : g, inside && r0 + i * ROWS < live);
     }
+    return;
+  }
+  for (int i = 0; i < ROUNDS; ++i, p += ROWS * step) {
+    bf e[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) e[k] = r0 + i * ROWS < live && c + k < cols ? p[k] : __float2bfloat16_rn(0.f);
+    uint4 q;
+    memcpy(&q, e, 16);
+    *reinterpret_cast<uint4*>(d + i * ROWS * ld) = q;
   }
 }
 // PARTS matrices [64][64] from the work.
-template <int PARTS>
-__device__ __forceinline__ void dl_load64(bf* s, const bf* g, int t, int of) {
-#pragma unroll 4
-  for (int i = t; i < PARTS * DL_CHUNK * 8; i += of) {
-    const int r = i >> 3, c = (i & 7) * 8;  // rows of all parts, one after the other
-    dl_copy16(s + r * DL_LD64 + c, g + r * DL_CHUNK + c, true);
-  }
+template <int PARTS, int OF>
+__device__ __forceinline__ void dl_load64(bf* s, const bf* g, int t) {
+  bf* d = s + (t >> 3) * DL_LD64 + (t & 7) * 8;  // rows of all parts, one after the other
+  g += t * 8;
+#pragma unroll
+  for (int i = 0; i < PARTS * DL_CHUNK * 8 / OF; ++i) dl_copy16(d + i * (OF / 8) * DL_LD64, g + i * OF * 8, true);
 }
 template <typename Row>  // all of a row's numbers, or those that come first
 __device__ __forceinline__ void dl_load_row(Row& s, const float* g, int t, int of) {
@@ -295,8 +292,8 @@ __global__ void __launch_bounds__(DL_THREADS) delta_prep_kernel(const DlArgs a) 
   const long long units = (long long)a.B * a.heads;
   const DlUnit u = dl_unit(a, (int)(blockIdx.x / units), blockIdx.x % units);
   if (u.live == 0) return;  // nobody asks
-  dl_load<DK>(&sh.k[0][0], DK + 8, a.K + u.row0 * a.ldk + (long long)u.head * a.Dk, a.B * a.ldk, u.live, a.Dk, a.vec_k, t, DL_THREADS);
-  dl_load<DK>(&sh.q[0][0], DK + 8, a.Q + u.row0 * a.ldq + (long long)u.head * a.Dk, a.B * a.ldq, u.live, a.Dk, a.vec_q, t, DL_THREADS);
+  dl_load<DK, DL_THREADS>(&sh.k[0][0], DK + 8, a.K + u.row0 * a.ldk + (long long)u.head * a.Dk, a.B * a.ldk, u.live, a.Dk, a.vec_k, t);
+  dl_load<DK, DL_THREADS>(&sh.q[0][0], DK + 8, a.Q + u.row0 * a.ldq + (long long)u.head * a.Dk, a.B * a.ldq, u.live, a.Dk, a.vec_q, t);
   dl_commit();
   if (t < DL_CHUNK) {
     float f = 1.f, rest = 0.f, beta = 0.f, no;
@@ -456,20 +453,40 @@ __device__ __forceinline__ void dl_left(const float (&c0)[4], const float (&c1)[
     for (int p = 0; p < PARTS; ++p) a[p][i] = w[p];
   }
 }
-// c0, c1 += A * B for 16 columns of the right operand in PB parts, products of parts i + j <= MOST.
-template <int PA, int PB, int MOST, bool KN>
-__device__ __forceinline__ void dl_step(float (&c0)[4], float (&c1)[4], const uint32_t (&a)[PA][4], const bf* b, int ld, int stride, int n0, int k0, int lane) {
+// c += A * B for the blocks FROM .. TO - 1 of 16 columns of the right operand, whose contraction begins at k0, in PB parts, products of parts i + j <= MOST.  An accumulator is not asked for
+// again before all others have had their turn.
+template <int FROM, int TO, int PA, int PB, int MOST, bool KN, int TILES>
+__device__ __forceinline__ void dl_step(float (&c)[TILES][4], const uint32_t (&a)[PA][4], const bf* b, int ld, int stride, int k0, int lane) {
 #pragma unroll
   for (int j = PB - 1; j >= 0; --j) {  // small parts first
-    uint32_t rb[4];
-    dl_b<KN>(rb, b + j * stride, ld, n0, k0, lane);
+    uint32_t rb[TO - FROM][4];
+#pragma unroll
+    for (int n = FROM; n < TO; ++n) dl_b<KN>(rb[n - FROM], b + j * stride, ld, 16 * n, k0, lane);
 #pragma unroll
     for (int i = PA - 1; i >= 0; --i)
       if (i + j <= MOST) {
-        dl_mma(c0, a[i], rb[0], rb[1]);
-        dl_mma(c1, a[i], rb[2], rb[3]);
+#pragma unroll
+        for (int n = FROM; n < TO; ++n) {
+          dl_mma(c[2 * n], a[i], rb[n - FROM][0], rb[n - FROM][1]);
+          dl_mma(c[2 * n + 1], a[i], rb[n - FROM][2], rb[n - FROM][3]);
+        }
       }
   }
+}
+// The blocks k .. 3, and 0 .. k, of [64] columns: what a triangular matrix leaves of the contraction's block k.
+template <int PA, int PB, int MOST, bool KN>
+__device__ __forceinline__ void dl_later(int k, float (&c)[8][4], const uint32_t (&a)[PA][4], const bf* b, int ld, int stride, int lane) {
+  if (k == 0) dl_step<0, 4, PA, PB, MOST, KN>(c, a, b, ld, stride, 0, lane);
+  if (k == 1) dl_step<1, 4, PA, PB, MOST, KN>(c, a, b, ld, stride, 16, lane);
+  if (k == 2) dl_step<2, 4, PA, PB, MOST, KN>(c, a, b, ld, stride, 32, lane);
+  if (k == 3) dl_step<3, 4, PA, PB, MOST, KN>(c, a, b, ld, stride, 48, lane);
+}
+template <int PA, int PB, int MOST, bool KN>
+__device__ __forceinline__ void dl_earlier(int k, float (&c)[8][4], const uint32_t (&a)[PA][4], const bf* b, int ld, int stride, int lane) {
+  if (k == 0) dl_step<0, 1, PA, PB, MOST, KN>(c, a, b, ld, stride, 0, lane);
+  if (k == 1) dl_step<0, 2, PA, PB, MOST, KN>(c, a, b, ld, stride, 16, lane);
+  if (k == 2) dl_step<0, 3, PA, PB, MOST, KN>(c, a, b, ld, stride, 32, lane);
+  if (k == 3) dl_step<0, 4, PA, PB, MOST, KN>(c, a, b, ld, stride, 48, lane);
 }
 // A warp's state S' [16][DK], from and to [Dk][Dv] in memory: f(tile, element, row d, column c).
 template <int DK, typename F>
@@ -547,11 +564,11 @@ __global__ void __launch_bounds__(64 * NP, 1) delta_scan_kernel(const DlArgs a) 
     if (chunk < chunks) {
       const DlUnit u = dl_unit(a, chunk, n);
       const int at = chunk & 1, t = threadIdx.x - HELP;
-      dl_load<DK>(&sh.k[at][0][0], LDK, K + u.row0 * a.ldk, a.B * a.ldk, u.live, a.Dk, a.vec_k, t, HELP);
-      dl_load<DK>(&sh.q[at][0][0], LDK, Q + u.row0 * a.ldq, a.B * a.ldq, u.live, a.Dk, a.vec_q, t, HELP);
-      dl_load<NP * 16>(&sh.v[at][0][0], LDV, V + u.row0 * a.ldv, a.B * a.ldv, u.live, cols, a.vec_v, t, HELP);
-      dl_load64<3>(&sh.tri[at][0][0][0], a.tri + u.unit * 3 * DL_SQ, t, HELP);
-      dl_load64<2>(&sh.p[at][0][0][0], a.p + u.unit * 3 * DL_SQ, t, HELP);
+      dl_load<DK, HELP>(&sh.k[at][0][0], LDK, K + u.row0 * a.ldk, a.B * a.ldk, u.live, a.Dk, a.vec_k, t);
+      dl_load<DK, HELP>(&sh.q[at][0][0], LDK, Q + u.row0 * a.ldq, a.B * a.ldq, u.live, a.Dk, a.vec_q, t);
+      dl_load<NP * 16, HELP>(&sh.v[at][0][0], LDV, V + u.row0 * a.ldv, a.B * a.ldv, u.live, cols, a.vec_v, t);
+      dl_load64<3, HELP>(&sh.tri[at][0][0][0], a.tri + u.unit * 3 * DL_SQ, t);
+      dl_load64<2, HELP>(&sh.p[at][0][0][0], a.p + u.unit * 3 * DL_SQ, t);
       dl_load_row(sh.row[at], a.row + u.unit * DL_ROW_FLOATS, t, HELP);
     }
     dl_commit();
@@ -573,8 +590,7 @@ __global__ void __launch_bounds__(64 * NP, 1) delta_scan_kernel(const DlArgs a) 
           const uint4 x = sh.s[pair][kd][p][lane];
           s[p][0] = x.x, s[p][1] = x.y, s[p][2] = x.z, s[p][3] = x.w;
         }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) dl_step<2, 1, 1, false>(o[2 * i], o[2 * i + 1], s, &sh.q[at][0][0], LDK, 0, 16 * i, 16 * kd, lane);
+        dl_step<0, 4, 2, 1, 1, false>(o, s, &sh.q[at][0][0], LDK, 0, 16 * kd, lane);
       }
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
@@ -590,8 +606,7 @@ __global__ void __launch_bounds__(64 * NP, 1) delta_scan_kernel(const DlArgs a) 
           const uint4 y = sh.u[pair][k][p][lane];
           x[p][0] = y.x, x[p][1] = y.y, x[p][2] = y.z, x[p][3] = y.w;
         }
-#pragma unroll
-        for (int i = k; i < 4; ++i) dl_step<2, 2, 1, false>(o[2 * i], o[2 * i + 1], x, &sh.p[at][0][0][0], DL_LD64, PT, 16 * i, 16 * k, lane);
+        dl_later<2, 2, 1, false>(k, o, x, &sh.p[at][0][0][0], DL_LD64, PT, lane);
       }
       const DlUnit u = dl_unit(a, chunk, n);
       dl_rows_out(o, nullptr, Y + u.row0 * a.ldy + 16 * pair, a.B * a.ldy, u.live, mine, lane);
@@ -601,10 +616,27 @@ __global__ void __launch_bounds__(64 * NP, 1) delta_scan_kernel(const DlArgs a) 
     const float* h0 = a.h0 ? a.h0 + n * size + c0 + 16 * pair : nullptr;
     dl_state<DK>(lane, [&](int i, int e, int d, int c) { s[i][e] = h0 && d < a.Dk && c < mine ? h0[(long long)d * a.Dv + c] : 0.f; });
     auto put = [&](float* g) { dl_state<DK>(lane, [&](int i, int e, int d, int c) { if (d < a.Dk && c < mine) g[(long long)d * a.Dv + c] = s[i][e]; }); };
+    const bool even = a.Dk % 2 == 0 && (reinterpret_cast<uintptr_t>(a.S) & 7u) == 0;
+    auto keep = [&](float* g) {  // for the backward call: transposed, as it lies here
+#pragma unroll
+      for (int i = 0; i < DK / 8; ++i)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int d = 8 * i + 2 * (lane & 3), c = (lane >> 2) + 8 * h;
+          if (d >= a.Dk || c >= mine) continue;
+          float* p = g + c * a.Dk + d;
+          if (even) {
+            *reinterpret_cast<float2*>(p) = make_float2(s[i][2 * h], s[i][2 * h + 1]);
+          } else {
+            p[0] = s[i][2 * h];
+            if (d + 1 < a.Dk) p[1] = s[i][2 * h + 1];
+          }
+        }
+    };
     for (int chunk = 0; chunk < chunks; ++chunk) {
       const int at = chunk & 1;
       const DlSteps& row = sh.row[at];
-      if (a.S) put(a.S + (chunk * heads + n) * size + c0 + 16 * pair);
+      if (a.S) keep(a.S + (chunk * heads + n) * size + (long long)(c0 + 16 * pair) * a.Dk);
       dl_meet(0, 64 * NP);
       float e[8][4] = {};
 #pragma unroll
@@ -613,8 +645,7 @@ __global__ void __launch_bounds__(64 * NP, 1) delta_scan_kernel(const DlArgs a) 
         dl_left<3>(s[2 * kd], s[2 * kd + 1], x);
         sh.s[pair][kd][0][lane] = make_uint4(x[0][0], x[0][1], x[0][2], x[0][3]);
         sh.s[pair][kd][1][lane] = make_uint4(x[1][0], x[1][1], x[1][2], x[1][3]);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) dl_step<3, 1, 2, false>(e[2 * i], e[2 * i + 1], x, &sh.k[at][0][0], LDK, 0, 16 * i, 16 * kd, lane);
+        dl_step<0, 4, 3, 1, 2, false>(e, x, &sh.k[at][0][0], LDK, 0, 16 * kd, lane);
       }
       dl_meet(1 + pair, 64);
 #pragma unroll
@@ -638,8 +669,7 @@ __global__ void __launch_bounds__(64 * NP, 1) delta_scan_kernel(const DlArgs a) 
       for (int k = 0; k < 4; ++k) {
         uint32_t r[3][4];
         dl_left<3>(e[2 * k], e[2 * k + 1], r);
-#pragma unroll
-        for (int i = k; i < 4; ++i) dl_step<3, 3, 2, false>(x[2 * i], x[2 * i + 1], r, &sh.tri[at][0][0][0], DL_LD64, PT, 16 * i, 16 * k, lane);
+        dl_later<3, 3, 2, false>(k, x, r, &sh.tri[at][0][0][0], DL_LD64, PT, lane);
       }
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
@@ -663,8 +693,8 @@ __global__ void __launch_bounds__(64 * NP, 1) delta_scan_kernel(const DlArgs a) 
         }
         uint32_t w[3][4];
         dl_left<3>(x[2 * k], x[2 * k + 1], w);
-#pragma unroll
-        for (int i = 0; i < DK / 16; ++i) dl_step<3, 1, 2, true>(s[2 * i], s[2 * i + 1], w, &sh.k[at][0][0], LDK, 0, 16 * i, 16 * k, lane);
+        dl_step<0, 4, 3, 1, 2, true>(s, w, &sh.k[at][0][0], LDK, 0, 16 * k, lane);
+        if constexpr (DK > 64) dl_step<4, 8, 3, 1, 2, true>(s, w, &sh.k[at][0][0], LDK, 0, 16 * k, lane);
       }
     }
     if (a.hT) put(a.hT + n * size + c0 + 16 * pair);
@@ -711,15 +741,15 @@ __global__ void __launch_bounds__(64 * NP, 1) delta_back_kernel(const DlArgs a) 
       if (chunk >= 0) {
         const DlUnit u = dl_unit(a, chunk, n);
         const int at = chunk & 1;
-        dl_load<DK>(&sh.k[at][0][0], LDK, K + u.row0 * a.ldk, a.B * a.ldk, u.live, a.Dk, a.vec_k, t, HELP);
-        dl_load<DK>(&sh.q[at][0][0], LDK, Q + u.row0 * a.ldq, a.B * a.ldq, u.live, a.Dk, a.vec_q, t, HELP);
-        dl_load<NP * 16>(&sh.dy[at][0][0], LDV, dY + u.row0 * a.lddy, a.B * a.lddy, u.live, cols, a.vec_dy, t, HELP);
-        dl_load64<3>(&sh.tri[at][0][0][0], a.tri + u.unit * 3 * DL_SQ, t, HELP);
+        dl_load<DK, HELP>(&sh.k[at][0][0], LDK, K + u.row0 * a.ldk, a.B * a.ldk, u.live, a.Dk, a.vec_k, t);
+        dl_load<DK, HELP>(&sh.q[at][0][0], LDK, Q + u.row0 * a.ldq, a.B * a.ldq, u.live, a.Dk, a.vec_q, t);
+        dl_load<NP * 16, HELP>(&sh.dy[at][0][0], LDV, dY + u.row0 * a.lddy, a.B * a.lddy, u.live, cols, a.vec_dy, t);
+        dl_load64<3, HELP>(&sh.tri[at][0][0][0], a.tri + u.unit * 3 * DL_SQ, t);
         dl_load_row(sh.row[at], a.row + u.unit * DL_ROW_FLOATS, t, HELP);
       }
     };
     auto fetch_p = [&](int chunk) {
-      if (chunk >= 0) dl_load64<3>(&sh.p[0][0][0], a.p + dl_unit(a, chunk, n).unit * 3 * DL_SQ, t, HELP);
+      if (chunk >= 0) dl_load64<3, HELP>(&sh.p[0][0][0], a.p + dl_unit(a, chunk, n).unit * 3 * DL_SQ, t);
     };
     fetch(chunks - 1);
     fetch_p(chunks - 1);
@@ -736,8 +766,7 @@ __global__ void __launch_bounds__(64 * NP, 1) delta_back_kernel(const DlArgs a) 
         float g[8][4] = {};
 #pragma unroll
         for (int k = 0; k < 4; ++k)
-#pragma unroll
-          for (int j = 0; j <= k; ++j) dl_step<1, 3, 2, true>(g[2 * j], g[2 * j + 1], y[k], &sh.p[0][0][0], DL_LD64, PT, 16 * j, 16 * k, lane);
+          dl_earlier<1, 3, 2, true>(k, g, y[k], &sh.p[0][0][0], DL_LD64, PT, lane);
 #pragma unroll
         for (int i = 0; i < 8; ++i) sh.g[pair][i][lane] = make_float4(g[i][0], g[i][1], g[i][2], g[i][3]);
       }
@@ -759,8 +788,8 @@ __global__ void __launch_bounds__(64 * NP, 1) delta_back_kernel(const DlArgs a) 
 #pragma unroll
           for (int p = 0; p < 3; ++p) x[p][i] = w[p];
         }
-#pragma unroll
-        for (int i = 0; i < DK / 16; ++i) dl_step<3, 1, 2, true>(s[2 * i], s[2 * i + 1], x, &sh.q[at][0][0], LDK, 0, 16 * i, 16 * k, lane);
+        dl_step<0, 4, 3, 1, 2, true>(s, x, &sh.q[at][0][0], LDK, 0, 16 * k, lane);
+        if constexpr (DK > 64) dl_step<4, 8, 3, 1, 2, true>(s, x, &sh.q[at][0][0], LDK, 0, 16 * k, lane);
       }
 #pragma unroll
       for (int i = 0; i < DK / 8; ++i) sh.y[pair][i][lane] = make_float4(s[i][0], s[i][1], s[i][2], s[i][3]);
@@ -777,7 +806,7 @@ __global__ void __launch_bounds__(64 * NP, 1) delta_back_kernel(const DlArgs a) 
       const DlUnit u = dl_unit(a, chunk, n);
       dl_meet(0, 64 * NP);
       float f[8][4] = {};
-      bf* D = a.d + u.unit * 2 * DK * a.ldx + c0 + 16 * pair;
+      bf* D = a.d + u.unit * 2 * DK * a.ldx + (long long)(c0 + 16 * pair) * DK;
 #pragma unroll
       for (int kd = 0; kd < DK / 16; ++kd) {
         uint32_t x[3][4];
@@ -785,12 +814,9 @@ __global__ void __launch_bounds__(64 * NP, 1) delta_back_kernel(const DlArgs a) 
 #pragma unroll
         for (int p = 0; p < 2; ++p)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const uint32_t w = dl_transposed(x[p][i]);
-            if (here) *reinterpret_cast<uint32_t*>(D + ((long long)p * DK + 16 * kd + 8 * (i >> 1) + (lane >> 2)) * a.ldx + 8 * (i & 1) + 2 * (lane & 3)) = w;
-          }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) dl_step<3, 1, 2, false>(f[2 * i], f[2 * i + 1], x, &sh.k[at][0][0], LDK, 0, 16 * i, 16 * kd, lane);
+          for (int i = 0; i < 4; ++i)
+            if (here) *reinterpret_cast<uint32_t*>(D + (p * a.ldx + 8 * (i & 1) + (lane >> 2)) * DK + 16 * kd + 8 * (i >> 1) + 2 * (lane & 3)) = x[p][i];
+        dl_step<0, 4, 3, 1, 2, false>(f, x, &sh.k[at][0][0], LDK, 0, 16 * kd, lane);
       }
       dl_meet(1 + pair, 64);
 #pragma unroll
@@ -804,8 +830,7 @@ __global__ void __launch_bounds__(64 * NP, 1) delta_back_kernel(const DlArgs a) 
       for (int k = 0; k < 4; ++k) {
         uint32_t r[3][4];
         dl_left<3>(f[2 * k], f[2 * k + 1], r);
-#pragma unroll
-        for (int j = 0; j <= k; ++j) dl_step<3, 3, 2, true>(x[2 * j], x[2 * j + 1], r, &sh.tri[at][0][0][0], DL_LD64, PT, 16 * j, 16 * k, lane);
+        dl_earlier<3, 3, 2, true>(k, x, r, &sh.tri[at][0][0][0], DL_LD64, PT, lane);
       }
       dl_rows_out(x, row.beta, dV + u.row0 * a.lddv + 16 * pair, a.B * a.lddv, u.live, mine, lane);
       bf* X = a.x + u.unit * 2 * DL_CHUNK * a.ldx + c0 + 16 * pair;
@@ -838,8 +863,8 @@ __global__ void __launch_bounds__(64 * NP, 1) delta_back_kernel(const DlArgs a) 
         }
         uint32_t w[3][4];
         dl_left<3>(x[2 * k], x[2 * k + 1], w);
-#pragma unroll
-        for (int i = 0; i < DK / 16; ++i) dl_step<3, 1, 2, true>(s[2 * i], s[2 * i + 1], w, &sh.k[at][0][0], LDK, 0, 16 * i, 16 * k, lane);
+        dl_step<0, 4, 3, 1, 2, true>(s, w, &sh.k[at][0][0], LDK, 0, 16 * k, lane);
+        if constexpr (DK > 64) dl_step<4, 8, 3, 1, 2, true>(s, w, &sh.k[at][0][0], LDK, 0, 16 * k, lane);
       }
     }
     if (a.dh0) dl_state<DK>(lane, [&](int i, int e, int d, int c) { if (d < a.Dk && c < mine) a.dh0[n * size + (long long)d * a.Dv + c0 + 16 * pair + c] = s[i][e]; });
@@ -910,7 +935,13 @@ __global__ void __launch_bounds__(DL_THREADS) delta_steps_kernel(const DlArgs a)
   if (len > 0) fetch(0);
   for (int step = 0; step < len; ++step) {
     const int at = step & 1;
-    if (a.S && step % DL_CHUNK == 0) store(a.S + ((long long)(step / DL_CHUNK) * a.B * a.heads + n) * size);
+    if (a.S && step == 0) {  // (there is one chunk) transposed, as the backward call reads it
+#pragma unroll
+      for (int i = 0; i < ROWS; ++i)
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          if (warp + WARPS * i < a.Dk && col(k) < a.Dv) a.S[n * size + (long long)col(k) * a.Dk + warp + WARPS * i] = s[i][k];
+    }
     if (t < 128) {
       kq[at][0][t] = nk;
       kq[at][1][t] = nq;
@@ -1000,7 +1031,7 @@ struct DlGradShared {
   bf x[2][DL_CHUNK][DV + 8];
   bf u[2][DL_CHUNK][DV + 8];   // b (V - g K S), then U
   union {
-    bf s[2][DK][DV + 8];       // S_0, then D
+    bf s[2][DV][DK + 8];       // S_0 transposed, then D
     bf m[3][2][DL_CHUNK][DL_LD64];  // N / |k_j|, N / |q_i|, (M + M^T) / |k_j|
   };
   union {
@@ -1014,11 +1045,11 @@ struct DlGradShared {
   float ds[DL_GRAD_WARPS];
 };
 
-// A [Dk][Dv] state in fp32 to two bf16 parts in shared memory, zeros around it.  Its products with what `with` holds in two parts in memory, entry by entry,
-// are added to dot.
+// A state [Dv][Dk] in fp32 to two bf16 parts in shared memory, zeros around it.  Returns this thread's share of its product, entry by entry, with what `with` [2][rows][DK] holds in
+// two parts in memory.
 template <int DK, int DV>
-__device__ __forceinline__ float dl_load_state(bf* s, const float* g, int Dk, int Dv, int vec, const bf* with, int ldx) {
-  constexpr int LD = DV + 8, QUADS = DV / 4, MINE = DK * QUADS / DL_GRAD_THREADS, AHEAD = MINE < 4 ? MINE : 4;
+__device__ __forceinline__ float dl_load_state(bf* s, const float* g, int Dk, int Dv, int vec, const bf* with, int rows) {
+  constexpr int LD = DK + 8, QUADS = DK / 4, MINE = DV * QUADS / DL_GRAD_THREADS, AHEAD = MINE < 4 ? MINE : 4;
   static_assert(MINE % AHEAD == 0, "whole rounds");
   float dot = 0.f;
 #pragma unroll
@@ -1027,26 +1058,26 @@ __device__ __forceinline__ float dl_load_state(bf* s, const float* g, int Dk, in
     uint2 hi[AHEAD], lo[AHEAD];
 #pragma unroll
     for (int i = 0; i < AHEAD; ++i) {
-      const int at = (i0 + i) * DL_GRAD_THREADS + threadIdx.x, d = at / QUADS, c = at % QUADS * 4;
+      const int at = (i0 + i) * DL_GRAD_THREADS + threadIdx.x, c = at / QUADS, d = at % QUADS * 4;
       x[i] = make_float4(0.f, 0.f, 0.f, 0.f);
       hi[i] = lo[i] = make_uint2(0u, 0u);
       if (d < Dk && c < Dv) {
-        const float* p = g + (long long)d * Dv + c;
+        const float* p = g + c * Dk + d;
         if (vec) {
           x[i] = *reinterpret_cast<const float4*>(p);
         } else {
           x[i].x = p[0];
-          if (c + 1 < Dv) x[i].y = p[1];
-          if (c + 2 < Dv) x[i].z = p[2];
-          if (c + 3 < Dv) x[i].w = p[3];
+          if (d + 1 < Dk) x[i].y = p[1];
+          if (d + 2 < Dk) x[i].z = p[2];
+          if (d + 3 < Dk) x[i].w = p[3];
         }
-        hi[i] = *reinterpret_cast<const uint2*>(with + (long long)d * ldx + c);
-        lo[i] = *reinterpret_cast<const uint2*>(with + (long long)(DK + d) * ldx + c);
+        hi[i] = *reinterpret_cast<const uint2*>(with + c * DK + d);
+        lo[i] = *reinterpret_cast<const uint2*>(with + (rows + c) * DK + d);
       }
     }
 #pragma unroll
     for (int i = 0; i < AHEAD; ++i) {
-      const int at = (i0 + i) * DL_GRAD_THREADS + threadIdx.x, d = at / QUADS, c = at % QUADS * 4;
+      const int at = (i0 + i) * DL_GRAD_THREADS + threadIdx.x, c = at / QUADS, d = at % QUADS * 4;
       auto pair = [](uint32_t w) {
         __nv_bfloat162 h;
         memcpy(&h, &w, 4);
@@ -1058,25 +1089,28 @@ __device__ __forceinline__ float dl_load_state(bf* s, const float* g, int Dk, in
       dl_split<2>(x[i].x, x[i].y, a);
       dl_split<2>(x[i].z, x[i].w, b);
 #pragma unroll
-      for (int e = 0; e < 2; ++e) *reinterpret_cast<uint2*>(s + (e * DK + d) * LD + c) = make_uint2(a[e], b[e]);
+      for (int e = 0; e < 2; ++e) *reinterpret_cast<uint2*>(s + (e * DV + c) * LD + d) = make_uint2(a[e], b[e]);
     }
   }
   return dot;
 }
-// PARTS matrices [ROWS][up to PAD] from the work, on their way to shared memory.
+// PARTS matrices [from][pitch] from the work, their first ROWS rows of up to PAD columns, on their way to shared memory; what is not in `rows` and `cols` becomes zeros.
 template <int ROWS, int PAD, int PARTS>
-__device__ __forceinline__ void dl_load_parts(bf* s, const bf* g, int ldx, int cols) {
-  constexpr int PIECES = PAD / 8;
-  for (int i = threadIdx.x; i < PARTS * ROWS * PIECES; i += blockDim.x) {
-    const int r = i / PIECES, c = (i % PIECES) * 8;
-    dl_copy16(s + r * (PAD + 8) + c, g + (c < cols ? (long long)r * ldx + c : 0), c < cols);
+__device__ __forceinline__ void dl_load_parts(bf* s, const bf* g, int from, int pitch, int rows, int cols) {
+  constexpr int PIECES = PAD / 8, ROUNDS = PARTS * ROWS * PIECES / DL_GRAD_THREADS, STEP = DL_GRAD_THREADS / PIECES;
+  const int c = threadIdx.x % PIECES * 8, r0 = threadIdx.x / PIECES;
+#pragma unroll
+  for (int i = 0; i < ROUNDS; ++i) {
+    const int all = r0 + i * STEP, part = all / ROWS, r = all % ROWS;
+    const bool there = c < cols && r < rows;
+    dl_copy16(s + all * (PAD + 8) + c, g + (there ? (part * from + r) * pitch + c : 0), there);
   }
 }
 
 template <int DK, int DV>
 __global__ void __launch_bounds__(DL_GRAD_THREADS) delta_grad_kernel(const DlArgs a) {
   constexpr int NK = DK / 32, NV = DV / 32;  // tiles of 8 columns a warp of [64][DK] and [64][DV] matrices
-  constexpr int LDK = DK + 8, LDV = DV + 8, PV = DL_CHUNK * LDV, PM = DL_CHUNK * DL_LD64, PS = DK * LDV;
+  constexpr int LDK = DK + 8, LDV = DV + 8, PV = DL_CHUNK * LDV, PM = DL_CHUNK * DL_LD64, PS = DV * LDK;
   extern __shared__ __align__(16) uint8_t dl_smem[];
   auto& sh = *reinterpret_cast<DlGradShared<DK, DV>*>(dl_smem);
   pdl_launch_dependents();
@@ -1094,25 +1128,35 @@ __global__ void __launch_bounds__(DL_GRAD_THREADS) delta_grad_kernel(const DlArg
     a.dZf[z] = a.dZb[z] = __float2bfloat16_rn(0.f);
   }
   if (u.live == 0) return;
-  dl_load<DK>(&sh.k[0][0], LDK, a.K + u.row0 * a.ldk + (long long)u.head * a.Dk, a.B * a.ldk, u.live, a.Dk, a.vec_k, t, DL_GRAD_THREADS);
-  dl_load<DK>(&sh.q[0][0], LDK, a.Q + u.row0 * a.ldq + (long long)u.head * a.Dk, a.B * a.ldq, u.live, a.Dk, a.vec_q, t, DL_GRAD_THREADS);
-  dl_load<DV>(&sh.dy[0][0], LDV, a.dY + u.row0 * a.lddy + (long long)u.head * a.Dv, a.B * a.lddy, u.live, a.Dv, a.vec_dy, t, DL_GRAD_THREADS);
-  dl_load64<2>(&sh.tri[0][0][0], a.tri + u.unit * 3 * DL_SQ, t, DL_GRAD_THREADS);
+  dl_load<DK, DL_GRAD_THREADS>(&sh.k[0][0], LDK, a.K + u.row0 * a.ldk + (long long)u.head * a.Dk, a.B * a.ldk, u.live, a.Dk, a.vec_k, t);
+  dl_load<DK, DL_GRAD_THREADS>(&sh.q[0][0], LDK, a.Q + u.row0 * a.ldq + (long long)u.head * a.Dk, a.B * a.ldq, u.live, a.Dk, a.vec_q, t);
+  dl_load<DV, DL_GRAD_THREADS>(&sh.dy[0][0], LDV, a.dY + u.row0 * a.lddy + (long long)u.head * a.Dv, a.B * a.lddy, u.live, a.Dv, a.vec_dy, t);
+  dl_load64<2, DL_GRAD_THREADS>(&sh.tri[0][0][0], a.tri + u.unit * 3 * DL_SQ, t);
   dl_load_row(sh.row, a.row + u.unit * DL_ROW_FLOATS, t, DL_GRAD_THREADS);
-  dl_load_parts<DL_CHUNK, DV, 2>(&sh.x[0][0][0], a.x + u.unit * 2 * DL_CHUNK * a.ldx, a.ldx, a.Dv);
+  dl_load_parts<DL_CHUNK, DV, 2>(&sh.x[0][0][0], a.x + u.unit * 2 * DL_CHUNK * a.ldx, DL_CHUNK, a.ldx, DL_CHUNK, a.Dv);
   dl_commit();
   // this warp's tile; where work grows or falls with the row, the warps of a scheduler have the same between them
   const int group = warp >> 2, m0 = (group < 2 ? warp & 3 : 3 - (warp & 3)) * 16;
   const int nk0 = group * NK * 8, nv0 = group * NV * 8, nm0 = group * 16;
   const int r0 = m0 + (lane >> 2), cl = 2 * (lane & 3);
-  float v[NV][4];
+  uint32_t v[NV][2];  // pairs of V
 #pragma unroll
-  for (int i = 0; i < NV; ++i)
+  for (int h = 0; h < 2; ++h) {
+    const int r = r0 + 8 * h;
+    const bf* p = a.V + (u.row0 + (long long)r * a.B) * a.ldv + (long long)u.head * a.Dv + nv0 + cl;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int r = r0 + 8 * (e >> 1), c = nv0 + 8 * i + cl + (e & 1);
-      v[i][e] = r < u.live && c < a.Dv ? __bfloat162float(a.V[(u.row0 + (long long)r * a.B) * a.ldv + (long long)u.head * a.Dv + c]) : 0.f;
+    for (int i = 0; i < NV; ++i) {
+      const int c = nv0 + 8 * i + cl;
+      v[i][h] = 0u;
+      if (r >= u.live || c >= a.Dv) continue;
+      if (a.vec_v) {
+        v[i][h] = *reinterpret_cast<const uint32_t*>(p + 8 * i);
+      } else {
+        bf e[2] = {p[8 * i], c + 1 < a.Dv ? p[8 * i + 1] : __float2bfloat16_rn(0.f)};
+        memcpy(&v[i][h], e, 4);
+      }
     }
+  }
   const bf* D = a.d + u.unit * 2 * DK * a.ldx;
   float dot = dl_load_state<DK, DV>(&sh.s[0][0][0], a.S + u.unit * a.Dk * a.Dv, a.Dk, a.Dv, a.vec_s, D, a.ldx);
 #pragma unroll
@@ -1137,19 +1181,20 @@ __global__ void __launch_bounds__(DL_GRAD_THREADS) delta_grad_kernel(const DlArg
   };
   {
     float e[1][NV][4] = {};
-    dl_product<1, NV, false, true, 1, 2, 1>(e, &sh.k[0][0], LDK, 0, &sh.s[0][0][0], LDV, PS, m0, nv0, 0, DK, lane);
+    dl_product<1, NV, false, false, 1, 2, 1>(e, &sh.k[0][0], LDK, 0, &sh.s[0][0][0], LDK, PS, m0, nv0, 0, DK, lane);
 #pragma unroll
     for (int i = 0; i < NV; ++i)
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const int r = r0 + 8 * h;
-        const float b = sh.row.beta[r], g = -sh.row.first[r] * sh.row.rk[r];
-        dl_put<2>(&sh.u[0][r][nv0 + 8 * i + cl], PV, b * fmaf(g, e[0][i][2 * h], v[i][2 * h]), b * fmaf(g, e[0][i][2 * h + 1], v[i][2 * h + 1]));
+        const float b = sh.row.beta[r], g = -sh.row.kin[r];
+        const float2 x = dl_unpack(v[i][h]);
+        dl_put<2>(&sh.u[0][r][nv0 + 8 * i + cl], PV, b * fmaf(g, e[0][i][2 * h], x.x), b * fmaf(g, e[0][i][2 * h + 1], x.y));
       }
   }
   float aq[1][NK][4] = {}, ak[1][NK][4] = {};
-  dl_product<1, NK, false, false, 1, 2, 1>(aq, &sh.dy[0][0], LDV, 0, &sh.s[0][0][0], LDV, PS, m0, nk0, 0, DV, lane);
-  dl_product<1, NK, false, false, 2, 2, 1>(ak, &sh.x[0][0][0], LDV, PV, &sh.s[0][0][0], LDV, PS, m0, nk0, 0, DV, lane);
+  dl_product<1, NK, false, true, 1, 2, 1>(aq, &sh.dy[0][0], LDV, 0, &sh.s[0][0][0], LDK, PS, m0, nk0, 0, DV, lane);
+  dl_product<1, NK, false, true, 2, 2, 1>(ak, &sh.x[0][0][0], LDV, PV, &sh.s[0][0][0], LDK, PS, m0, nk0, 0, DV, lane);
 #pragma unroll
   for (int i = 0; i < NK; ++i)
 #pragma unroll
@@ -1161,7 +1206,7 @@ __global__ void __launch_bounds__(DL_GRAD_THREADS) delta_grad_kernel(const DlArg
   row_sums(0, aq, &sh.q[0][0], sh.row.rq, false);
   row_sums(0, ak, &sh.k[0][0], sh.row.rk, true);
   __syncthreads();
-  dl_load_parts<DK, DV, 2>(&sh.s[0][0][0], D, a.ldx, a.Dv);  // D, where S_0 was
+  dl_load_parts<DV, DK, 2>(&sh.s[0][0][0], D, a.ldx, DK, a.Dv, DK);  // D, where S_0 was
   dl_commit();
   {
     float x[1][NV][4] = {};
@@ -1197,15 +1242,23 @@ __global__ void __launch_bounds__(DL_GRAD_THREADS) delta_grad_kernel(const DlArg
     dl_product<1, 2, false, false, 1, 1, 0>(qk, &sh.q[0][0], LDK, 0, &sh.k[0][0], LDK, 0, m0, nm0, 0, DK, lane);
     dl_product<1, 2, false, false, 1, 1, 0>(kk, &sh.k[0][0], LDK, 0, &sh.k[0][0], LDK, 0, m0, nm0, 0, DK, lane);
 #pragma unroll
-    for (int n = 0; n < 2; ++n)
+    for (int h = 0; h < 2; ++h) {
+      const int i = r0 + 8 * h, bi = m0 >> 4;
+      const float rqi = sh.row.rq[i], rki = sh.row.rk[i], beta = sh.row.beta[i];
+      float across = sh.row.from[i];
+      for (int b = group + 1; b < bi; ++b) across *= sh.row.block[b];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int i = r0 + 8 * (e >> 1), j = nm0 + 8 * n + cl + (e & 1);
-        const float g = j <= i ? dl_decay(sh.row, i, j) : 0.f;
-        nn[0][n][e] *= a.scale * g;
-        mm[0][n][e] *= j < i ? -sh.row.beta[i] * g : 0.f;
-        sh.w[i][j] = j < i ? sh.row.rk[j] * fmaf(nn[0][n][e] * sh.row.rq[i], qk[0][n][e], mm[0][n][e] * sh.row.rk[i] * kk[0][n][e]) : 0.f;
-      }
+      for (int n = 0; n < 2; ++n)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const int j = nm0 + 8 * n + cl + e;
+          const float g = group < bi ? across * sh.row.to[j] : sh.row.diag[bi][i & 15][j & 15];
+          float &x = nn[0][n][2 * h + e], &y = mm[0][n][2 * h + e];
+          x = j <= i ? x * a.scale * g : 0.f;
+          y = j < i ? y * -beta * g : 0.f;
+          sh.w[i][j] = j < i ? sh.row.rk[j] * fmaf(x * rqi, qk[0][n][2 * h + e], y * rki * kk[0][n][2 * h + e]) : 0.f;
+        }
+    }
   } else {
 #pragma unroll
     for (int n = 0; n < 2; ++n)
@@ -1216,7 +1269,7 @@ __global__ void __launch_bounds__(DL_GRAD_THREADS) delta_grad_kernel(const DlArg
   __syncthreads();
   {
     float x[1][NK][4] = {};
-    dl_product<1, NK, false, false, 2, 2, 1>(x, &sh.u[0][0][0], LDV, PV, &sh.s[0][0][0], LDV, PS, m0, nk0, 0, DV, lane);
+    dl_product<1, NK, false, true, 2, 2, 1>(x, &sh.u[0][0][0], LDV, PV, &sh.s[0][0][0], LDK, PS, m0, nk0, 0, DV, lane);
 #pragma unroll
     for (int i = 0; i < NK; ++i)
 #pragma unroll
@@ -1236,28 +1289,32 @@ __global__ void __launch_bounds__(DL_GRAD_THREADS) delta_grad_kernel(const DlArg
   __syncthreads();
   if (nm0 <= m0) {
 #pragma unroll
-    for (int n = 0; n < 2; ++n)
+    for (int h = 0; h < 2; ++h) {
+      const int i = r0 + 8 * h;
+      const float rq = sh.row.rq[i], rk = sh.row.rk[i];
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int i = r0 + 8 * h, j = nm0 + 8 * n + cl;
-        const float x = nn[0][n][2 * h], y = nn[0][n][2 * h + 1], rq = sh.row.rq[i];
-        dl_put<2>(&sh.m[0][0][i][j], PM, x * sh.row.rk[j], y * sh.row.rk[j + 1]);
+      for (int n = 0; n < 2; ++n) {
+        const int j = nm0 + 8 * n + cl;
+        const float x = nn[0][n][2 * h], y = nn[0][n][2 * h + 1], z0 = mm[0][n][2 * h], z1 = mm[0][n][2 * h + 1], rk0 = sh.row.rk[j], rk1 = sh.row.rk[j + 1];
+        dl_put<2>(&sh.m[0][0][i][j], PM, x * rk0, y * rk1);
         dl_put<2>(&sh.m[1][0][i][j], PM, x * rq, y * rq);
+        uint32_t lo[2], up[2];
+        dl_split<2>(z0 * rk0, z1 * rk1, lo);
+        dl_split<2>(z0 * rk, z1 * rk, up);
+        const int r = nm0 + 8 * n + (lane >> 2), c = m0 + 8 * h + cl;
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const int jj = j + e;
-          if (jj > i) continue;
-          float lo = mm[0][n][2 * h + e] * sh.row.rk[jj], up = mm[0][n][2 * h + e] * sh.row.rk[i];
-#pragma unroll
-          for (int part = 0; part < 2; ++part) {
-            const bf bl = __float2bfloat16_rn(lo), bu = __float2bfloat16_rn(up);
-            sh.m[2][part][i][jj] = bl;
-            sh.m[2][part][jj][i] = bu;
-            lo -= __bfloat162float(bl);
-            up -= __bfloat162float(bu);
+        for (int part = 0; part < 2; ++part) {
+          const uint32_t w = dl_transposed(up[part]);
+          // on the diagonal of 8 x 8 blocks both halves meet in one word, each zero where the other is not
+          if (nm0 == m0 && h == n) {
+            *reinterpret_cast<uint32_t*>(&sh.m[2][part][i][j]) = lo[part] | w;
+          } else if (nm0 < m0 || h > n) {
+            *reinterpret_cast<uint32_t*>(&sh.m[2][part][i][j]) = lo[part];
+            *reinterpret_cast<uint32_t*>(&sh.m[2][part][r][c]) = w;
           }
         }
       }
+    }
   }
   {  // what passes gate r: eight threads
     const int r = t >> 3, part = t & 7;
@@ -1448,7 +1505,8 @@ ard_status launch_delta_backward(ard_ctx* ctx, int T, int B, int heads, int Dk, 
   a.dQ = (bf*)dQ, a.dK = (bf*)dK, a.dV = (bf*)dV, a.lddq = lddq, a.lddk = lddk, a.lddv = lddv;
   a.dZf = (bf*)dZf, a.dZb = (bf*)dZb, a.lddz = lddz, a.dh0 = dh0;
   a.vec_q = dl_on16(Q, ldq, Dk), a.vec_k = dl_on16(K, ldk, Dk), a.vec_dy = dl_on16(dY, lddy, Dv);
-  a.vec_s = Dv % 4 == 0 && (reinterpret_cast<uintptr_t>(S) & 15u) == 0;
+  a.vec_v = dl_on16(V, ldv, Dv);
+  a.vec_s = Dk % 4 == 0 && (reinterpret_cast<uintptr_t>(S) & 15u) == 0;
   dl_set_work(a, work, dl_plan(T, B, heads, Dk, Dv, true));
   return dl_chunks(ctx, a, true, s);
 }
