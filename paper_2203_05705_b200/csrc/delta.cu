@@ -425,7 +425,10 @@ __global__ void __launch_bounds__(DL_THREADS) delta_prep_kernel(const DlArgs a) 
 // share (K, Q, T, P), two chunks deep.  Beside each such warp stands one that does what nobody waits for: forward the outputs, which take the state's and U's parts over
 // shared memory, backward what comes from dY alone.
 // Some of a CTA's warps, in branches of their own (0: all of them).
-__device__ __forceinline__ void dl_meet(int id, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
+__device__ __forceinline__ void dl_meet(int id, int threads) {
+  __syncwarp();
+  asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory");
+}
 __device__ __forceinline__ uint32_t dl_transposed(uint32_t x) {  // of 8 x 8 bf16, a pair a lane
   uint32_t r;
   asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));

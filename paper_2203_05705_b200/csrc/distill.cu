@@ -2,18 +2,21 @@
 //   p = softmax(t / tau),  L = hard (lse(z) - z[label]) + soft tau^2 sum_i p_i (log p_i - log softmax(z / tau)[id_i])
 //   dL/dz = hard (softmax(z) - [label]) + soft tau (softmax(z / tau) - sum_i p_i [id_i])
 //
-// Memory bounds it: a row is read once and its gradient written once, 4 bytes an element in bf16.  So a row stays where
-// it was read: in the registers of a CTA's threads (up to 32768 logits in bf16), or, longer than that, in the L2, which
-// holds the rows of all SMs twice over; the second look does not reach memory.  Each thread keeps the maximum of what
-// it holds and sums of exponentials relative to it, and these pairs meet once a row.  The gradient's few entries at the label and the
-// teacher's tokens are written again behind the others, by the threads that know all that falls on the same token.
-// A row of up to 128 logits is held by 8 or 32 lanes.
+// Memory bounds it: a row is read once and its gradient written once, 4 bytes an element in bf16; its exponentials, two an element (four where both temperatures
+// are wanted), take seven tenths of that time on the special function units.  So rows stream through a ring in shared memory, filled by bulk copies that one warp
+// asks for, while the others work on what is there, and a row too long for a ring of two is cut over a cluster of CTAs, which exchange a maximum and
+// sums once a row.  A third kind of warp does what depends on a few scattered logits: the teacher's softmax for the next row, and for this one the loss and the
+// gradient's entries at the label and the teacher's tokens, which are written once more behind the others.  Each thread keeps the maximum of what it looks at and
+// sums of exponentials relative to it; these pairs meet once a row.  Rows of up to 2048 logits (fp32: 1024) are held by a warp or 8 lanes, in registers.
+#include <cooperative_groups.h>
+
 #include "ard_internal.h"
 #include "sm100_ptx.h"
 
 namespace {
 
-constexpr int DS_MOST_TEACHER = 1024;
+namespace cg = cooperative_groups;
+
 constexpr float DS_LOG2E = 1.4426950408889634f;
 
 struct DsArgs {
@@ -28,10 +31,11 @@ struct DsArgs {
   const float* weight;
   float* loss;
   float* total;
-  double* partial;      // one a CTA
+  double* partial;      // one a CTA or cluster
   unsigned int* count;  // zero between launches
   void* dZ;
   int* status;
+  int slots, slot_bytes, slice;  // the ring; a CTA's vectors of a row
 };
 
 __device__ __forceinline__ float ds_exp2(float x) {
@@ -52,332 +56,8 @@ __device__ __forceinline__ T ds_from(float x) {
 // A thread's maximum where it has seen nothing but -infinity (or nothing): differences from it stay numbers.
 __device__ __forceinline__ float ds_floor(float m) { return fmaxf(m, -3.402823466e38f); }
 
-// exp of all but a maximum's share: the sums of another maximum in this one's terms.
+// Sums relative to the maximum `from` in terms of a larger one.
 __device__ __forceinline__ float ds_shift(float from, float to, float c) { return ds_exp2((from - to) * c); }
-
-// The teacher's entries of a row as smem holds them, and the label as one more.
-struct DsEntries {
-  int id[DS_MOST_TEACHER + 1];
-  float p[DS_MOST_TEACHER + 1];     // share of the teacher's distribution (the label's: not used)
-  float lp[DS_MOST_TEACHER];        // its logarithm
-  float z[DS_MOST_TEACHER + 1];     // the student's logit
-};
-
-__device__ __forceinline__ int ds_teacher_id(const DsArgs& a, long long r, int i) {
-  const int id = a.t_ids[r * a.ldk + i];
-  if (id >= a.V) atomicMax(a.status, (int)ARD_ERR_INVALID_ARG);
-  return id < a.V ? id : -1;
-}
-
-__device__ __forceinline__ float warp_max(float x) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) x = fmaxf(x, __shfl_xor_sync(0xFFFFFFFFu, x, o));
-  return x;
-}
-__device__ __forceinline__ float warp_sum(float x) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xFFFFFFFFu, x, o);
-  return x;
-}
-
-// One warp: a row's entries to shared memory.  Returns how many of the teacher's count (the softmax over them is complete).
-template <typename T>
-__device__ int ds_entries(const DsArgs& a, long long r, const T* z, int label, DsEntries& e) {
-  const int lane = threadIdx.x & 31;
-  float m = -INFINITY;
-  int live = 0;
-  for (int i = lane; i < a.k; i += 32) {
-    const int id = ds_teacher_id(a, r, i);
-    const float t = a.t[r * a.ldk + i];
-    const bool on = id >= 0 && t != -INFINITY;
-    e.id[i] = on ? id : -1;
-    e.lp[i] = t;
-    e.z[i] = on ? ds_f32(z[id]) : 0.f;
-    if (on) m = fmaxf(m, t), ++live;
-    if (on && t != t) m = t;
-  }
-  if (lane == 0) {
-    e.id[a.k] = label;
-    e.z[a.k] = label >= 0 ? ds_f32(z[label]) : 0.f;
-  }
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) live += __shfl_xor_sync(0xFFFFFFFFu, live, o);
-  if (live == 0) return 0;
-  m = warp_max(m);
-  float s = 0.f;
-  for (int i = lane; i < a.k; i += 32)
-    if (e.id[i] >= 0) s += expf((e.lp[i] - m) * a.inv_tau);
-  s = warp_sum(s);
-  const float log_s = logf(s);
-  for (int i = lane; i < a.k; i += 32)
-    if (e.id[i] >= 0) {
-      const float d = (e.lp[i] - m) * a.inv_tau;
-      e.p[i] = expf(d) / s;
-      e.lp[i] = d - log_s;
-    }
-  return live;
-}
-
-// Sum of a CTA's rows' losses, weighted, to its place; the last CTA adds all of them in a fixed order.  All threads call it.
-template <int THREADS>
-__device__ void ds_total(const DsArgs& a, double mine, double* red, int* s_last) {
-  const int t = threadIdx.x;
-  auto block_sum = [&](double x) {
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xFFFFFFFFu, x, o);
-    __syncthreads();
-    if ((t & 31) == 0) red[t >> 5] = x;
-    __syncthreads();
-    x = 0.0;
-#pragma unroll
-    for (int k = 0; k < THREADS / 32; ++k) x += red[k];
-    return x;
-  };
-  mine = block_sum(mine);
-  if (t == 0) {
-    __stcg(a.partial + blockIdx.x, mine);
-    __threadfence();
-    *s_last = atomicAdd(a.count, 1u) == gridDim.x - 1;
-  }
-  __syncthreads();
-  if (!*s_last) return;
-  __threadfence();
-  double x = 0.0;
-  for (int k = t; k < (int)gridDim.x; k += THREADS) x += __ldcg(a.partial + k);
-  x = block_sum(x);
-  if (t == 0) {
-    *a.count = 0u;
-    *a.total = (float)x;
-  }
-}
-
-// ---- a CTA a row ------------------------------------------------------------------------------------
-// Elements of a row as its threads take them: `head` ones in front of the first 16-byte boundary, vectors, and the rest; head and rest are less than a
-// vector each and go to the first threads, one element each.
-template <typename T>
-struct DsRow {
-  static constexpr int VEC = 16 / (int)sizeof(T);
-  int head, vecs, loose;  // loose: head and rest
-  __device__ __forceinline__ DsRow(const T* z, int V) {
-    const int off = (int)((reinterpret_cast<uintptr_t>(z) & 15u) / sizeof(T));
-    head = min(V, (VEC - off) & (VEC - 1));
-    vecs = (V - head) / VEC;
-    loose = V - vecs * VEC;
-  }
-  __device__ __forceinline__ int loose_at(int i) const { return i < head ? i : i + vecs * VEC; }
-};
-
-// NV vectors a thread in registers; NV = 0: looked at twice in memory.  TWO: the softmax at temperature 1 and the one at tau.
-template <typename T, int THREADS, int NV, bool TWO>
-__global__ void __launch_bounds__(THREADS, 1024 / THREADS) distill_row_kernel(const DsArgs a) {
-  constexpr int VEC = 16 / (int)sizeof(T), WARPS = THREADS / 32;
-  __shared__ DsEntries ent;
-  __shared__ float red_m[WARPS], red_s[WARPS], red_u[WARPS];
-  __shared__ double red_d[WARPS];
-  __shared__ int s_live, s_last;
-  pdl_launch_dependents();
-  pdl_wait_prior_grids();
-  const int t = threadIdx.x, warp = t >> 5, lane = t & 31;
-  const float c1 = TWO || a.soft == 0.f ? a.c : a.c_tau;  // of the only softmax, or of temperature 1's
-  double sum_loss = 0.0;
-  for (long long r = blockIdx.x; r < a.rows; r += gridDim.x) {
-    const T* z = (const T*)a.Z + r * a.ldz;
-    T* dz = a.dZ ? (T*)a.dZ + r * a.lddz : nullptr;
-    const DsRow<T> row(z, a.V);
-    const float w = a.weight ? a.weight[r] : 1.f;
-    int label = a.labels ? a.labels[r] : -1;
-    if (label >= a.V && t == 0) atomicMax(a.status, (int)ARD_ERR_INVALID_ARG);
-    if (label >= a.V || a.hard == 0.f) label = -1;
-    auto nothing = [&]() {  // there is nothing to learn from
-      if (dz) {
-        const DsRow<T> out(dz, a.V);
-        for (int i = t; i < out.vecs; i += THREADS) reinterpret_cast<uint4*>(dz + out.head)[i] = make_uint4(0, 0, 0, 0);
-        if (t < out.loose) dz[out.loose_at(t)] = ds_from<T>(0.f);
-      }
-      if (t == 0) a.loss[r] = 0.f;
-    };
-    if (w == 0.f || (label < 0 && a.k == 0)) {
-      nothing();
-      continue;
-    }
-    // what this thread holds: its maximum, then the exponentials' sums relative to it
-    uint4 q[NV > 0 ? NV : 1];
-    const uint4* zv = reinterpret_cast<const uint4*>(z + row.head);
-    const float edge = t < row.loose ? ds_f32(z[row.loose_at(t)]) : -INFINITY;
-    float m = edge, s = 0.f, u = 0.f;
-    auto unpack = [&](const uint4& v, float (&x)[VEC]) {
-      T e[VEC];
-      memcpy(e, &v, 16);
-#pragma unroll
-      for (int k = 0; k < VEC; ++k) x[k] = ds_f32(e[k]);
-    };
-    auto vector_max = [&](const float (&x)[VEC]) {
-      float y = x[0];
-#pragma unroll
-      for (int k = 1; k < VEC; ++k) y = fmaxf(y, x[k]);
-      return y;
-    };
-    auto add = [&](const float (&x)[VEC], float top) {
-#pragma unroll
-      for (int k = 0; k < VEC; ++k) {
-        const float d = x[k] - top;
-        s += ds_exp2(d * c1);
-        if (TWO) u += ds_exp2(d * a.c_tau);
-      }
-    };
-    if constexpr (NV > 0) {
-#pragma unroll
-      for (int i = 0; i < NV; ++i)
-        if (t + i * THREADS < row.vecs) q[i] = zv[t + i * THREADS];
-    }
-    if (warp == 0) {
-      const int live = ds_entries<T>(a, r, z, label, ent);
-      if (lane == 0) s_live = live;
-    }
-    if constexpr (NV > 0) {
-#pragma unroll
-      for (int i = 0; i < NV; ++i)
-        if (t + i * THREADS < row.vecs) {
-          float x[VEC];
-          unpack(q[i], x);
-          m = fmaxf(m, vector_max(x));
-        }
-      m = ds_floor(m);
-#pragma unroll
-      for (int i = 0; i < NV; ++i)
-        if (t + i * THREADS < row.vecs) {
-          float x[VEC];
-          unpack(q[i], x);
-          add(x, m);
-        }
-    } else {
-      m = ds_floor(m);
-      constexpr int AHEAD = 4;
-      for (int i0 = t; i0 < row.vecs; i0 += AHEAD * THREADS) {
-        uint4 v[AHEAD];
-#pragma unroll
-        for (int j = 0; j < AHEAD; ++j)
-          if (i0 + j * THREADS < row.vecs) v[j] = zv[i0 + j * THREADS];
-#pragma unroll
-        for (int j = 0; j < AHEAD; ++j) {
-          if (i0 + j * THREADS >= row.vecs) break;
-          float x[VEC];
-          unpack(v[j], x);
-          const float top = vector_max(x);
-          if (top > m) {
-            s *= ds_shift(m, top, c1);
-            if (TWO) u *= ds_shift(m, top, a.c_tau);
-            m = top;
-          }
-          add(x, m);
-        }
-      }
-    }
-    if (t < row.loose) {
-      s += ds_exp2((edge - m) * c1);  // fmaxf passes NaN over; the sums do not
-      if (TWO) u += ds_exp2((edge - m) * a.c_tau);
-    }
-    // the pairs of all threads
-    {
-      const float top = warp_max(m), by = ds_shift(m, top, c1);
-      s = warp_sum(s * by);
-      if (TWO) u = warp_sum(u * ds_shift(m, top, a.c_tau));
-      if (lane == 0) {
-        red_m[warp] = top;
-        red_s[warp] = s;
-        if (TWO) red_u[warp] = u;
-      }
-      __syncthreads();
-      m = red_m[0];
-#pragma unroll
-      for (int i = 1; i < WARPS; ++i) m = fmaxf(m, red_m[i]);
-      s = 0.f, u = 0.f;
-#pragma unroll
-      for (int i = 0; i < WARPS; ++i) {
-        s += red_s[i] * ds_shift(red_m[i], m, c1);
-        if (TWO) u += red_u[i] * ds_shift(red_m[i], m, a.c_tau);
-      }
-    }
-    const float hard = label >= 0 ? a.hard : 0.f, soft = s_live > 0 ? a.soft : 0.f;
-    if (hard == 0.f && soft == 0.f) {  // none of the teacher's entries counts
-      nothing();
-      __syncthreads();
-      continue;
-    }
-    const float by1 = w * (TWO ? hard : hard + soft * a.tau) / s, by_tau = TWO ? w * soft * a.tau / u : 0.f;
-    auto slope = [&](float x) {
-      const float d = x - m;
-      float g = by1 * ds_exp2(d * c1);
-      if (TWO) g = fmaf(by_tau, ds_exp2(d * a.c_tau), g);
-      return g;
-    };
-    if (dz) {
-      const bool same = ((reinterpret_cast<uintptr_t>(z) ^ reinterpret_cast<uintptr_t>(dz)) & 15u) == 0;
-      auto put = [&](int i, const uint4& v) {
-        float x[VEC];
-        unpack(v, x);
-        T e[VEC];
-#pragma unroll
-        for (int k = 0; k < VEC; ++k) e[k] = ds_from<T>(slope(x[k]));
-        if (same) {
-          uint4 o;
-          memcpy(&o, e, 16);
-          reinterpret_cast<uint4*>(dz + row.head)[i] = o;
-        } else {
-#pragma unroll
-          for (int k = 0; k < VEC; ++k) dz[row.head + i * VEC + k] = e[k];
-        }
-      };
-      if constexpr (NV > 0) {
-#pragma unroll
-        for (int i = 0; i < NV; ++i)
-          if (t + i * THREADS < row.vecs) put(t + i * THREADS, q[i]);
-      } else {
-        constexpr int AHEAD = 4;
-        for (int i0 = t; i0 < row.vecs; i0 += AHEAD * THREADS) {
-          uint4 v[AHEAD];
-#pragma unroll
-          for (int j = 0; j < AHEAD; ++j)
-            if (i0 + j * THREADS < row.vecs) v[j] = zv[i0 + j * THREADS];
-#pragma unroll
-          for (int j = 0; j < AHEAD; ++j)
-            if (i0 + j * THREADS < row.vecs) put(i0 + j * THREADS, v[j]);
-        }
-      }
-      if (t < row.loose) dz[row.loose_at(t)] = ds_from<T>(slope(edge));
-      __syncthreads();
-      for (int i = t; i <= a.k; i += THREADS) {
-        const int id = ent.id[i];
-        if (id < 0) continue;
-        float p = 0.f;  // all that falls on this token, in the entries' order
-        if (soft != 0.f)
-          for (int j = 0; j < a.k; ++j)
-            if (ent.id[j] == id) p += ent.p[j];
-        const float less = (id == label ? hard : 0.f) + soft * a.tau * p;
-        dz[id] = ds_from<T>(fmaf(-w, less, slope(ent.z[i])));
-      }
-    }
-    if (warp == 0) {
-      float kl = 0.f;
-      const float log_u = logf(TWO ? u : s);
-      if (soft != 0.f)
-        for (int i = lane; i < a.k; i += 32)
-          if (ent.id[i] >= 0 && ent.p[i] > 0.f) kl += ent.p[i] * (ent.lp[i] - ((ent.z[i] - m) * a.inv_tau - log_u));
-      kl = warp_sum(kl);
-      if (lane == 0) {
-        float L = soft * a.tau * a.tau * kl;
-        if (label >= 0) L = fmaf(hard, logf(s) - (ent.z[a.k] - m), L);
-        a.loss[r] = L;
-        sum_loss += (double)w * L;
-      }
-    }
-    __syncthreads();
-  }
-  if (a.total) ds_total<THREADS>(a, sum_loss, red_d, &s_last);
-}
-
-// ---- short rows -------------------------------------------------------------------------------------
-constexpr int DS_SHORT_THREADS = 256;
 
 template <int LANES>
 __device__ __forceinline__ float lanes_max(float x) {
@@ -392,112 +72,587 @@ __device__ __forceinline__ float lanes_sum(float x) {
   return x;
 }
 
-// LANES lanes a row of up to 4 * LANES logits.  The teacher's entries are looked at one after the other, and the lane that holds an entry's logit
-// takes it.
-template <typename T, int LANES>
-__global__ void __launch_bounds__(DS_SHORT_THREADS) distill_short_kernel(const DsArgs a) {
-  constexpr int EPT = 4, PER = DS_SHORT_THREADS / LANES;
-  __shared__ double red_d[DS_SHORT_THREADS / 32];
-  __shared__ int s_last;
+// Sixteen bytes of logits as pairs.
+template <typename T>
+struct DsVec {
+  static constexpr int N = 16 / (int)sizeof(T);
+  float2 v[N / 2];
+  __device__ __forceinline__ explicit DsVec(const uint4& q) {
+    if constexpr (sizeof(T) == 2) {
+      const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = make_float2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xFFFF0000u));
+    } else {
+      v[0] = make_float2(__uint_as_float(q.x), __uint_as_float(q.y));
+      v[1] = make_float2(__uint_as_float(q.z), __uint_as_float(q.w));
+    }
+  }
+  __device__ __forceinline__ float max() const {
+    float m = fmaxf(v[0].x, v[0].y);
+#pragma unroll
+    for (int i = 1; i < N / 2; ++i) m = fmaxf(m, fmaxf(v[i].x, v[i].y));
+    return m;
+  }
+  // Exponentials of (x - m) c, added up in pairs.
+  __device__ __forceinline__ void add(float2& s, float m, float c) const {
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i) {
+      const float2 d = __fmul2_rn(__fadd2_rn(v[i], make_float2(-m, -m)), make_float2(c, c));
+      s = __fadd2_rn(s, make_float2(ds_exp2(d.x), ds_exp2(d.y)));
+    }
+  }
+};
+
+// Elements of a row as vectors of 16 bytes: `head` ones in front of the first boundary, vectors, and the rest; head and rest are less than a vector each.
+template <typename T>
+struct DsRow {
+  static constexpr int VEC = 16 / (int)sizeof(T);
+  int head, vecs, loose;  // loose: head and rest
+  __device__ __forceinline__ DsRow(const T* z, int V) {
+    const int off = (int)((reinterpret_cast<uintptr_t>(z) & 15u) / sizeof(T));
+    head = min(V, (VEC - off) & (VEC - 1));
+    vecs = (V - head) / VEC;
+    loose = V - vecs * VEC;
+  }
+  __device__ __forceinline__ int loose_at(int i) const { return i < head ? i : i + vecs * VEC; }
+  // which vector an element is in, -1: loose
+  __device__ __forceinline__ int vec_of(int j) const { return j < head || j >= head + vecs * VEC ? -1 : (j - head) / VEC; }
+};
+
+// The gradient's factors of a row: g = by1 exp((x - m) c1) + by_tau exp((x - m) c_tau).
+struct DsSlope {
+  float m, by1, by_tau, c1, c_tau;
+  template <bool TWO>
+  __device__ __forceinline__ float at(float x) const {
+    const float d = x - m;
+    float g = by1 * ds_exp2(d * c1);
+    if (TWO) g = fmaf(by_tau, ds_exp2(d * c_tau), g);
+    return g;
+  }
+  template <bool TWO>
+  __device__ __forceinline__ float2 at(float2 x) const {
+    const float2 d = __fadd2_rn(x, make_float2(-m, -m)), a = __fmul2_rn(d, make_float2(c1, c1));
+    float2 g = __fmul2_rn(make_float2(by1, by1), make_float2(ds_exp2(a.x), ds_exp2(a.y)));
+    if (TWO) {
+      const float2 b = __fmul2_rn(d, make_float2(c_tau, c_tau));
+      g = __ffma2_rn(make_float2(by_tau, by_tau), make_float2(ds_exp2(b.x), ds_exp2(b.y)), g);
+    }
+    return g;
+  }
+};
+// A vector's gradient to memory; same: dz lies on the 16-byte grid where z does.
+template <typename T, bool TWO>
+__device__ __forceinline__ void ds_put(const DsSlope& f, const uint4& q, T* dz, bool same) {
+  constexpr int VEC = 16 / (int)sizeof(T);
+  const DsVec<T> x(q);
+  T e[VEC];
+#pragma unroll
+  for (int k = 0; k < VEC; k += 2) {
+    const float2 g = f.at<TWO>(x.v[k / 2]);
+    if constexpr (sizeof(T) == 2) {
+      const __nv_bfloat162 h = __floats2bfloat162_rn(g.x, g.y);
+      memcpy(e + k, &h, 4);
+    } else {
+      e[k] = g.x, e[k + 1] = g.y;
+    }
+  }
+  if (same) {
+    uint4 o;
+    memcpy(&o, e, 16);
+    *reinterpret_cast<uint4*>(dz) = o;
+  } else {
+#pragma unroll
+    for (int k = 0; k < VEC; ++k) dz[k] = e[k];
+  }
+}
+// A row's zeros, by `shares` groups of `of` threads each.
+template <typename T>
+__device__ __forceinline__ void ds_zero(T* dz, int V, int share, int shares, int t, int of) {
+  if (!dz) return;
+  const DsRow<T> out(dz, V);
+  for (int i = share * of + t; i < out.vecs; i += shares * of) reinterpret_cast<uint4*>(dz + out.head)[i] = make_uint4(0, 0, 0, 0);
+  if (share == 0)
+    for (int i = t; i < out.loose; i += of) dz[out.loose_at(i)] = ds_from<T>(0.f);
+}
+
+// The sum of a warp's rows' losses to its place; the last warp of the grid to come adds all of them in a fixed order.
+__device__ void ds_total(const DsArgs& a, double mine, int place, int places, int lane) {
+  unsigned last = 0;
+  if (lane == 0) {
+    __stcg(a.partial + place, mine);
+    __threadfence();
+    last = atomicAdd(a.count, 1u) == (unsigned)places - 1u;
+  }
+  if (!__shfl_sync(0xFFFFFFFFu, last, 0)) return;
+  __threadfence();
+  double x = 0.0;
+  for (int k = lane; k < places; k += 32) x += __ldcg(a.partial + k);
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xFFFFFFFFu, x, o);
+  if (lane == 0) {
+    *a.count = 0u;
+    *a.total = (float)x;
+  }
+}
+
+__device__ __forceinline__ int ds_label(const DsArgs& a, long long r) {
+  const int label = a.labels ? a.labels[r] : -1;
+  if (label >= a.V) atomicMax(a.status, (int)ARD_ERR_INVALID_ARG);
+  return label >= a.V || a.hard == 0.f ? -1 : label;
+}
+// An entry of the teacher's that counts, or -1.
+__device__ __forceinline__ int ds_entry(const DsArgs& a, long long r, int i, float& t) {
+  const int id = a.t_ids[r * a.ldk + i];
+  t = a.t[r * a.ldk + i];
+  if (id >= a.V) atomicMax(a.status, (int)ARD_ERR_INVALID_ARG);
+  return id >= 0 && id < a.V && t != -INFINITY ? id : -1;
+}
+
+// ---- short rows -------------------------------------------------------------------------------------
+constexpr int DS_SHORT_THREADS = 256, DS_SHORT_ENTRIES = 2;  // teacher's entries a lane
+
+// LANES lanes a row, NV vectors of 16 bytes a lane (WIDE) or NV single logits.
+template <typename T, int LANES, bool WIDE, int NV, bool TWO>
+__global__ void __launch_bounds__(DS_SHORT_THREADS) distill_lanes_kernel(const DsArgs a) {
+  constexpr int VEC = WIDE ? 16 / (int)sizeof(T) : 1, PER = DS_SHORT_THREADS / LANES, E = DS_SHORT_ENTRIES;
+  __shared__ double s_sum[DS_SHORT_THREADS / 32];
   pdl_launch_dependents();
   pdl_wait_prior_grids();
   const int t = threadIdx.x, lane = t & (LANES - 1);
+  const float c1 = TWO || a.soft == 0.f ? a.c : a.c_tau;  // of the only softmax, or of temperature 1's
   double sum_loss = 0.0;
   for (long long r0 = (long long)blockIdx.x * PER; r0 < a.rows; r0 += (long long)gridDim.x * PER) {
-    const long long r = r0 + t / LANES;
-    const bool in = r < a.rows;
-    const T* z = (const T*)a.Z + (in ? r : 0) * a.ldz;
+    const bool in = r0 + t / LANES < a.rows;
+    const long long r = in ? r0 + t / LANES : 0;
+    const T* z = (const T*)a.Z + r * a.ldz;
+    T* dz = a.dZ && in ? (T*)a.dZ + r * a.lddz : nullptr;
+    const DsRow<T> row(z, a.V);
+    // everything that has to come from memory is asked for at once; what a row without use holds is not looked at
     const float w = !in ? 0.f : a.weight ? a.weight[r] : 1.f;
-    int label = in && a.labels ? a.labels[r] : -1;
-    if (label >= a.V) atomicMax(a.status, (int)ARD_ERR_INVALID_ARG);
-    if (label >= a.V || a.hard == 0.f) label = -1;
-    const int k = in ? a.k : 0;
-    const bool look = w != 0.f && (label >= 0 || k > 0);
-    float x[EPT], less[EPT];
-    float m = -INFINITY;
+    const int label = in ? ds_label(a, r) : -1;
+    int id[E];
+    float p[E], lp[E], ze[E];
 #pragma unroll
-    for (int e = 0; e < EPT; ++e) {
-      x[e] = look && lane + e * LANES < a.V ? ds_f32(z[lane + e * LANES]) : -INFINITY;
-      m = fmaxf(m, x[e]);
-      less[e] = 0.f;
+    for (int e = 0; e < E; ++e) {
+      lp[e] = 0.f;
+      id[e] = in && lane + e * LANES < a.k ? ds_entry(a, r, lane + e * LANES, lp[e]) : -1;
+    }
+    const bool look = w != 0.f && (label >= 0 || a.k > 0);
+    uint4 q[WIDE ? NV : 1];
+    float x[WIDE ? 1 : NV];
+    float edge = -INFINITY, m;
+    if constexpr (WIDE) {
+      const uint4* zv = reinterpret_cast<const uint4*>(z + row.head);
+#pragma unroll
+      for (int i = 0; i < NV; ++i)
+        if (look && lane + i * LANES < row.vecs) q[i] = zv[lane + i * LANES];
+      if (look && lane < row.loose) edge = ds_f32(z[row.loose_at(lane)]);
+      m = edge;
+#pragma unroll
+      for (int i = 0; i < NV; ++i)
+        if (look && lane + i * LANES < row.vecs) m = fmaxf(m, DsVec<T>(q[i]).max());
+    } else {
+      m = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        x[i] = look && lane + i * LANES < a.V ? ds_f32(z[lane + i * LANES]) : -INFINITY;
+        m = fmaxf(m, x[i]);
+      }
     }
     m = ds_floor(lanes_max<LANES>(m));
-    float s = 0.f, u = 0.f;
+    float2 s2 = make_float2(0.f, 0.f), u2 = make_float2(0.f, 0.f);
+    if constexpr (WIDE) {
 #pragma unroll
-    for (int e = 0; e < EPT; ++e)
-      if (lane + e * LANES < a.V) {
-        s += ds_exp2((x[e] - m) * a.c);
-        u += ds_exp2((x[e] - m) * a.c_tau);
+      for (int i = 0; i < NV; ++i)
+        if (look && lane + i * LANES < row.vecs) {
+          const DsVec<T> y(q[i]);
+          y.add(s2, m, c1);
+          if (TWO) y.add(u2, m, a.c_tau);
+        }
+      s2.x += ds_exp2((edge - m) * c1);
+      if (TWO) u2.x += ds_exp2((edge - m) * a.c_tau);
+    } else {
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        s2.x += ds_exp2((x[i] - m) * c1);
+        if (TWO) u2.x += ds_exp2((x[i] - m) * a.c_tau);
       }
-    s = lanes_sum<LANES>(s);
-    u = lanes_sum<LANES>(u);
+    }
+    const float s = lanes_sum<LANES>(s2.x + s2.y), u = TWO ? lanes_sum<LANES>(u2.x + u2.y) : s;
     // the teacher's softmax
-    float tm = -INFINITY, ts = 0.f;
-    int live = 0;
-    if (look)
-      for (int i = lane; i < k; i += LANES) {
-        const int id = ds_teacher_id(a, r, i);
-        const float tv = a.t[r * a.ldk + i];
-        if (id >= 0 && tv != -INFINITY) tm = tv != tv ? tv : fmaxf(tm, tv), live = 1;
+    float tm = -INFINITY, ts = 0.f, live = 0.f;
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+      if (id[e] >= 0) {
+        live = 1.f;
+        tm = lp[e] != lp[e] ? lp[e] : fmaxf(tm, lp[e]);
       }
+    live = lanes_sum<LANES>(live);
     tm = lanes_max<LANES>(tm);
-    if (look && tm != -INFINITY)
-      for (int i = lane; i < k; i += LANES) {
-        const int id = a.t_ids[r * a.ldk + i];
-        const float tv = a.t[r * a.ldk + i];
-        if (id >= 0 && id < a.V && tv != -INFINITY) ts += expf((tv - tm) * a.inv_tau);
-      }
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      ze[e] = look && id[e] >= 0 ? ds_f32(z[id[e]]) : 0.f;
+      lp[e] = (lp[e] - tm) * a.inv_tau;
+      p[e] = id[e] >= 0 ? expf(lp[e]) : 0.f;
+      ts += p[e];
+    }
     ts = lanes_sum<LANES>(ts);
-    live = lanes_sum<LANES>((float)live) > 0.f;
-    const float hard = label >= 0 ? a.hard : 0.f, soft = live ? a.soft : 0.f;
-    float L = 0.f;
-    if (look && live) {
-      const float log_ts = logf(ts), log_u = logf(u);
-      for (int i = 0; i < k; ++i) {
-        const int id = a.t_ids[r * a.ldk + i];
-        const float tv = a.t[r * a.ldk + i];
-        if (id < 0 || id >= a.V || tv == -INFINITY || (id & (LANES - 1)) != lane) continue;
-        const float d = (tv - tm) * a.inv_tau, p = expf(d) / ts;
+    const float zl = look && label >= 0 ? ds_f32(z[label]) : 0.f;
+    const float hard = label >= 0 ? a.hard : 0.f, soft = live > 0.f ? a.soft : 0.f;
+    const bool some = look && (hard != 0.f || soft != 0.f);
+    const float log_s = logf(s), log_u = TWO ? logf(u) : log_s, log_ts = logf(ts);
+    float kl = 0.f;
 #pragma unroll
-        for (int e = 0; e < EPT; ++e)
-          if (id == lane + e * LANES) {
-            less[e] += soft * a.tau * p;
-            if (p > 0.f) L += p * (d - log_ts - ((x[e] - m) * a.inv_tau - log_u));
-          }
-      }
-      L *= soft * a.tau * a.tau;
+    for (int e = 0; e < E; ++e) {
+      p[e] = id[e] >= 0 ? p[e] / ts : 0.f;
+      if (id[e] >= 0 && p[e] != 0.f) kl += p[e] * (lp[e] - log_ts - ((ze[e] - m) * a.inv_tau - log_u));
     }
-    const float by1 = hard / s, by_tau = soft * a.tau / u;
-#pragma unroll
-    for (int e = 0; e < EPT; ++e) {
-      const int j = lane + e * LANES;
-      if (j >= a.V) continue;
-      if (j == label) {
-        less[e] += hard;
-        L = fmaf(hard, logf(s) - (x[e] - m), L);
-      }
-      if (in && a.dZ) {
-        const float d = x[e] - m;
-        float g = 0.f;
-        if (hard != 0.f) g = by1 * ds_exp2(d * a.c);
-        if (soft != 0.f) g = fmaf(by_tau, ds_exp2(d * a.c_tau), g);
-        ((T*)a.dZ)[r * a.lddz + j] = ds_from<T>(look ? w * (g - less[e]) : 0.f);
-      }
-    }
-    L = lanes_sum<LANES>(L);
+    kl = lanes_sum<LANES>(kl);
     if (in && lane == 0) {
-      a.loss[r] = look ? L : 0.f;
-      if (look) sum_loss += (double)w * L;
+      float L = 0.f;
+      if (some && soft != 0.f) L = soft * a.tau * a.tau * kl;
+      if (some && hard != 0.f) L = fmaf(hard, log_s - (zl - m), L);
+      a.loss[r] = L;
+      if (some) sum_loss += (double)w * L;
+    }
+    if (a.dZ) {
+      const DsSlope f = {m, w * (TWO ? hard : hard + soft * a.tau) / s, TWO ? w * soft * a.tau / u : 0.f, c1, a.c_tau};
+      if (dz && !some) ds_zero(dz, a.V, 0, 1, lane, LANES);
+      if (dz && some) {
+        if constexpr (WIDE) {
+          const bool same = ((reinterpret_cast<uintptr_t>(z) ^ reinterpret_cast<uintptr_t>(dz)) & 15u) == 0;
+#pragma unroll
+          for (int i = 0; i < NV; ++i)
+            if (lane + i * LANES < row.vecs) ds_put<T, TWO>(f, q[i], dz + row.head + (lane + i * LANES) * VEC, same);
+          if (lane < row.loose) dz[row.loose_at(lane)] = ds_from<T>(f.at<TWO>(edge));
+        } else {
+#pragma unroll
+          for (int i = 0; i < NV; ++i)
+            if (lane + i * LANES < a.V) dz[lane + i * LANES] = ds_from<T>(f.at<TWO>(x[i]));
+        }
+      }
+      __syncwarp();
+      // the label's entry and the teacher's once more, with all that falls on the same token, in the entries' order
+      float on[E], on_label = 0.f;
+#pragma unroll
+      for (int e = 0; e < E; ++e) on[e] = 0.f;
+#pragma unroll
+      for (int e = 0; e < E; ++e)
+        for (int j = 0; j < LANES && j + e * LANES < a.k; ++j) {
+          const int other = __shfl_sync(0xFFFFFFFFu, id[e], j, LANES);
+          const float share = __shfl_sync(0xFFFFFFFFu, p[e], j, LANES);
+          if (other == label && label >= 0) on_label += share;
+#pragma unroll
+          for (int d = 0; d < E; ++d)
+            if (id[d] == other) on[d] += share;
+        }
+      if (dz && some) {
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+          if (id[e] >= 0) dz[id[e]] = ds_from<T>(fmaf(-w, (id[e] == label ? hard : 0.f) + soft * a.tau * on[e], f.at<TWO>(ze[e])));
+        if (lane == 0 && label >= 0) dz[label] = ds_from<T>(fmaf(-w, hard + soft * a.tau * on_label, f.at<TWO>(zl)));
+      }
+      __syncwarp();
     }
   }
-  if (a.total) ds_total<DS_SHORT_THREADS>(a, sum_loss, red_d, &s_last);
+  if (!a.total) return;
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) sum_loss += __shfl_xor_sync(0xFFFFFFFFu, sum_loss, o);
+  if ((t & 31) == 0) s_sum[t >> 5] = sum_loss;
+  __syncthreads();
+  if (t >= 32) return;
+  double x = 0.0;
+  for (int k = 0; k < DS_SHORT_THREADS / 32; ++k) x += s_sum[k];
+  ds_total(a, x, blockIdx.x, gridDim.x, t);
 }
 
-template <typename T, int THREADS, int NV>
-ard_status ds_rows(ard_ctx* ctx, const DsArgs& a, bool two, cudaStream_t s) {
-  const long long room = (long long)(1024 / THREADS) * ctx->sm_count;
-  const dim3 grid((unsigned)(a.rows < room ? a.rows : room));
-  ARD_CUDA_OK(ard_launch(ctx, two ? distill_row_kernel<T, THREADS, NV, true> : distill_row_kernel<T, THREADS, NV, false>, grid, dim3(THREADS), 0, s, a));
+// ---- rows through a ring ------------------------------------------------------------------------------
+// WORKERS threads work on rows; behind them come a warp that fills the ring and one that has the entries.  `parts` CTAs, a cluster, share a row.
+constexpr int DS_SLOTS = 4;
+
+struct DsInfo {
+  float w;
+  int label;  // -1: none
+  int skip;
+};
+struct DsShared {
+  unsigned long long full[DS_SLOTS];
+  DsInfo info[DS_SLOTS];
+  float edge[DS_SLOTS][32];  // a row's loose logits
+  float red_m[2][16], red_s[2][16], red_u[2][16];  // of warps
+  float3 mail[2][8];         // of a cluster's CTAs
+  float soft[2];             // whether a row has a teacher
+  float3 sums[2];            // a row's maximum and sums, for the entries
+  int abort;
+};
+// Some of a CTA's warps, in branches of their own: those that wait, and those that only have to have come so far.
+__device__ __forceinline__ void ds_meet(int id, int threads) {
+  __syncwarp();
+  asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory");
+}
+__device__ __forceinline__ void ds_tell(int id, int threads) {
+  __syncwarp();
+  asm volatile("bar.arrive %0, %1;" ::"r"(id), "r"(threads) : "memory");
+}
+
+template <typename T, int WORKERS, bool TWO>
+__global__ void __launch_bounds__(WORKERS + 64, WORKERS > 256 ? 1 : 4) distill_ring_kernel(const DsArgs a, int parts) {
+  constexpr int VEC = 16 / (int)sizeof(T), WARPS = WORKERS / 32;
+  extern __shared__ __align__(128) uint8_t ds_smem[];
+  __shared__ DsShared sh;
+  // entries of two rows: token, share, its logarithm, logit; the label comes last
+  const int entries = a.k + 1;
+  int* e_id = reinterpret_cast<int*>(ds_smem + (size_t)a.slots * a.slot_bytes);
+  float *e_p = reinterpret_cast<float*>(e_id + 2 * entries), *e_lp = e_p + 2 * entries, *e_z = e_lp + 2 * entries;
+  pdl_launch_dependents();
+  const int t = threadIdx.x, warp = t >> 5, lane = t & 31;
+  const int rank = (int)(blockIdx.x % parts), first = (int)(blockIdx.x / parts), stride = (int)(gridDim.x / parts);
+  if (t == 0) {
+    for (int i = 0; i < DS_SLOTS; ++i) mbar_init(smem_u32(&sh.full[i]), 1);
+    sh.abort = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  __syncthreads();
+  if (parts > 1) cg::this_cluster().sync();  // every CTA of it is there
+  pdl_wait_prior_grids();
+  const float c1 = TWO || a.soft == 0.f ? a.c : a.c_tau;
+  const int v0 = rank * a.slice;  // this CTA's vectors of a row: v0 .. v0 + slice - 1
+  auto cluster_meet = [&]() {
+    asm volatile("barrier.cluster.arrive.release;" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
+  };
+  if (warp == WARPS) {  // fills the ring
+    auto fill = [&](long long r, int slot) {
+      const T* z = (const T*)a.Z + r * a.ldz;
+      const DsRow<T> row(z, a.V);
+      const float w = a.weight ? a.weight[r] : 1.f;
+      const int label = ds_label(a, r);
+      const bool skip = w == 0.f || (label < 0 && a.k == 0);
+      if (!skip && rank == 0 && lane < row.loose) sh.edge[slot][lane] = ds_f32(z[row.loose_at(lane)]);
+      __syncwarp();
+      if (lane == 0) {
+        sh.info[slot] = {w, label, skip ? 1 : 0};
+        const int mine = max(0, min(row.vecs - v0, a.slice));
+        const uint32_t bar = smem_u32(&sh.full[slot]);
+        if (skip || mine == 0) {
+          mbar_arrive(bar);
+        } else {
+          mbar_arrive_expect_tx(bar, (uint32_t)mine * 16u);
+          asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(smem_u32(ds_smem + (size_t)slot * a.slot_bytes)),
+                       "l"(z + row.head + (long long)v0 * VEC), "r"((uint32_t)mine * 16u), "r"(bar)
+                       : "memory");
+        }
+      }
+    };
+    int n = 0;
+    for (long long r = first; r < a.rows && n < a.slots; r += stride, ++n) fill(r, n);
+    n = 0;
+    for (long long r = first; r < a.rows; r += stride, ++n) {
+      if (parts > 1) cluster_meet();
+      ds_meet(2, WORKERS + 64);  // the row's slot has been read
+      const long long next = r + (long long)a.slots * stride;
+      if (next < a.rows) fill(next, n % a.slots);
+    }
+    return;
+  }
+  if (warp == WARPS + 1) {  // entries
+    auto prepare = [&](long long r, int at) {
+      int* id = e_id + at * entries;
+      float *p = e_p + at * entries, *lp = e_lp + at * entries, *ze = e_z + at * entries;
+      const T* z = (const T*)a.Z + r * a.ldz;
+      const int label = ds_label(a, r);
+      const bool use = (a.weight ? a.weight[r] : 1.f) != 0.f;
+      float m = -INFINITY;
+      int live = 0;
+      for (int i = lane; i < a.k; i += 32) {
+        float tv;
+        const int j = ds_entry(a, r, i, tv);
+        id[i] = j;
+        lp[i] = tv;
+        ze[i] = use && j >= 0 ? ds_f32(z[j]) : 0.f;
+        if (j >= 0) live = 1, m = tv != tv ? tv : fmaxf(m, tv);
+      }
+      if (lane == 0) {
+        id[a.k] = label;
+        ze[a.k] = use && label >= 0 ? ds_f32(z[label]) : 0.f;
+      }
+      live = __any_sync(0xFFFFFFFFu, live);
+      m = lanes_max<32>(m);
+      float s = 0.f;
+      for (int i = lane; i < a.k; i += 32)
+        if (id[i] >= 0) s += p[i] = expf(lp[i] = (lp[i] - m) * a.inv_tau);
+      s = lanes_sum<32>(s);
+      const float log_s = logf(s);
+      for (int i = lane; i < a.k; i += 32)
+        if (id[i] >= 0) p[i] /= s, lp[i] -= log_s;
+      if (lane == 0) sh.soft[at] = live ? a.soft : 0.f;
+      __syncwarp();
+    };
+    double sum_loss = 0.0;
+    int n = 0;
+    if (first < a.rows) prepare(first, 0);
+    for (long long r = first; r < a.rows; r += stride, ++n) {
+      const int at = n & 1;
+      const int* id = e_id + at * entries;
+      const float *p = e_p + at * entries, *lp = e_lp + at * entries, *ze = e_z + at * entries;
+      ds_meet(1, WORKERS + 32);  // the warps' maxima and sums are there, and this row's entries
+      if (parts > 1) cluster_meet();
+      const float w = a.weight ? a.weight[r] : 1.f;
+      if (r + stride < a.rows) prepare(r + stride, at ^ 1);
+      ds_meet(2, WORKERS + 64);  // the row's gradient has been written
+      const int label = id[a.k];
+      const float hard = label >= 0 ? a.hard : 0.f, soft = sh.soft[at];
+      if (w == 0.f || (hard == 0.f && soft == 0.f)) {
+        if (rank == 0 && lane == 0) a.loss[r] = 0.f;
+        continue;
+      }
+      const float3 q = sh.sums[at];
+      const DsSlope f = {q.x, w * (TWO ? hard : hard + soft * a.tau) / q.y, TWO ? w * soft * a.tau / q.z : 0.f, c1, a.c_tau};
+      if (a.dZ) {
+        const DsRow<T> row((const T*)a.Z + r * a.ldz, a.V);
+        T* dz = (T*)a.dZ + r * a.lddz;
+        for (int i = lane; i < entries; i += 32) {
+          const int j = id[i];
+          if (j < 0) continue;
+          const int v = row.vec_of(j);
+          if (v < 0 ? rank != 0 : v < v0 || v >= v0 + a.slice) continue;  // another CTA's
+          float share = 0.f;  // all that falls on this token, in the entries' order
+          if (soft != 0.f)
+            for (int o = 0; o < a.k; ++o)
+              if (id[o] == j) share += p[o];
+          dz[j] = ds_from<T>(fmaf(-w, (j == label ? hard : 0.f) + soft * a.tau * share, f.at<TWO>(ze[i])));
+        }
+      }
+      if (rank == 0) {
+        float kl = 0.f;
+        const float log_u = logf(TWO ? q.z : q.y);
+        if (soft != 0.f)
+          for (int i = lane; i < a.k; i += 32)
+            if (id[i] >= 0 && p[i] != 0.f) kl += p[i] * (lp[i] - ((ze[i] - q.x) * a.inv_tau - log_u));
+        kl = lanes_sum<32>(kl);
+        float L = soft != 0.f ? soft * a.tau * a.tau * kl : 0.f;
+        if (label >= 0) L = fmaf(hard, logf(q.y) - (ze[a.k] - q.x), L);
+        if (lane == 0) {
+          a.loss[r] = L;
+          sum_loss += (double)w * L;
+        }
+      }
+      __syncwarp();
+    }
+    if (a.total && rank == 0) ds_total(a, sum_loss, first, stride, lane);
+    return;
+  }
+  int n = 0;
+  for (long long r = first; r < a.rows; r += stride, ++n) {
+    const int slot = n % a.slots, at = n & 1;
+    const T* z = (const T*)a.Z + r * a.ldz;
+    T* dz = a.dZ ? (T*)a.dZ + r * a.lddz : nullptr;
+    const DsRow<T> row(z, a.V);
+    const int mine = max(0, min(row.vecs - v0, a.slice));
+    mbar_wait(smem_u32(&sh.full[slot]), (uint32_t)(n / a.slots) & 1u, &sh.abort, a.status);
+    const DsInfo info = sh.info[slot];
+    const uint4* zs = reinterpret_cast<const uint4*>(ds_smem + (size_t)slot * a.slot_bytes);
+    const bool edged = rank == 0 && t < row.loose && !info.skip;
+    const float edge = edged ? sh.edge[slot][t] : -INFINITY;
+    float m = edge;
+    float2 s2 = make_float2(0.f, 0.f), u2 = make_float2(0.f, 0.f);
+    if (!info.skip) {
+#pragma unroll 4
+      for (int i = t; i < mine; i += WORKERS) m = fmaxf(m, DsVec<T>(zs[i]).max());
+    }
+    m = ds_floor(m);
+    if (!info.skip) {
+#pragma unroll 4
+      for (int i = t; i < mine; i += WORKERS) {
+        const DsVec<T> x(zs[i]);
+        x.add(s2, m, c1);
+        if (TWO) x.add(u2, m, a.c_tau);
+      }
+      s2.x += ds_exp2((edge - m) * c1);  // fmaxf passes NaN over; the sums do not
+      if (TWO) u2.x += ds_exp2((edge - m) * a.c_tau);
+    }
+    float s = s2.x + s2.y, u = u2.x + u2.y;
+    {
+      const float top = lanes_max<32>(m);
+      s = lanes_sum<32>(s * ds_shift(m, top, c1));
+      if (TWO) u = lanes_sum<32>(u * ds_shift(m, top, a.c_tau));
+      if (lane == 0) {
+        sh.red_m[at][warp] = top;
+        sh.red_s[at][warp] = s;
+        if (TWO) sh.red_u[at][warp] = u;
+      }
+    }
+    ds_meet(1, WORKERS + 32);
+    m = sh.red_m[at][0];
+#pragma unroll
+    for (int i = 1; i < WARPS; ++i) m = fmaxf(m, sh.red_m[at][i]);
+    s = 0.f, u = 0.f;
+#pragma unroll
+    for (int i = 0; i < WARPS; ++i) {
+      s += sh.red_s[at][i] * ds_shift(sh.red_m[at][i], m, c1);
+      if (TWO) u += sh.red_u[at][i] * ds_shift(sh.red_m[at][i], m, a.c_tau);
+    }
+    if (parts > 1) {
+      if (t < parts) *cg::this_cluster().map_shared_rank(&sh.mail[at][rank], t) = make_float3(m, s, u);
+      cluster_meet();
+      m = sh.mail[at][0].x;
+      for (int i = 1; i < parts; ++i) m = fmaxf(m, sh.mail[at][i].x);
+      s = 0.f, u = 0.f;
+      for (int i = 0; i < parts; ++i) {
+        s += sh.mail[at][i].y * ds_shift(sh.mail[at][i].x, m, c1);
+        if (TWO) u += sh.mail[at][i].z * ds_shift(sh.mail[at][i].x, m, a.c_tau);
+      }
+    }
+    if (t == 0) sh.sums[at] = make_float3(m, s, u);
+    const float hard = info.label >= 0 ? a.hard : 0.f, soft = sh.soft[at];
+    if (info.skip || (hard == 0.f && soft == 0.f)) {
+      ds_zero(dz, a.V, rank, parts, t, WORKERS);
+    } else if (dz) {
+      const DsSlope f = {m, info.w * (TWO ? hard : hard + soft * a.tau) / s, TWO ? info.w * soft * a.tau / u : 0.f, c1, a.c_tau};
+      const bool same = ((reinterpret_cast<uintptr_t>(z) ^ reinterpret_cast<uintptr_t>(dz)) & 15u) == 0;
+      T* out = dz + row.head + (long long)v0 * VEC;
+#pragma unroll 4
+      for (int i = t; i < mine; i += WORKERS) ds_put<T, TWO>(f, zs[i], out + i * VEC, same);
+      if (edged) dz[row.loose_at(t)] = ds_from<T>(f.at<TWO>(edge));
+    }
+    fence_proxy_async_smem();  // what was read from the slot, before the next copy into it
+    ds_tell(2, WORKERS + 64);
+  }
+}
+
+template <typename T, int LANES, bool WIDE, int NV>
+ard_status ds_lanes(ard_ctx* ctx, const DsArgs& a, bool two, cudaStream_t s) {
+  const int per = DS_SHORT_THREADS / LANES;
+  const long long want = ((long long)a.rows + per - 1) / per, room = 8ll * ctx->sm_count;
+  const dim3 grid((unsigned)(want < room ? want : room));
+  ARD_CUDA_OK(ard_launch(ctx, two ? distill_lanes_kernel<T, LANES, WIDE, NV, true> : distill_lanes_kernel<T, LANES, WIDE, NV, false>, grid,
+                         dim3(DS_SHORT_THREADS), 0, s, a));
+  ctx->launches++;
+  ARD_CUDA_OK(cudaGetLastError());
+  return ARD_OK;
+}
+
+template <typename T, int WORKERS>
+ard_status ds_ring(ard_ctx* ctx, DsArgs a, bool two, int per_sm, cudaStream_t s) {
+  constexpr int VEC = 16 / (int)sizeof(T);
+  auto kern = two ? distill_ring_kernel<T, WORKERS, true> : distill_ring_kernel<T, WORKERS, false>;
+  const int entry_bytes = 2 * (a.k + 1) * 16, fixed = 2560;                 // (fixed: the kernel's own variables)
+  const int room = (227 * 1024 / per_sm - 1024 - fixed - entry_bytes) / 128 * 128;  // the ring's (1 KB a CTA is the system's)
+  const long long vecs = (long long)a.V / VEC;
+  // a row in two slots of one CTA, or cut over as few as will hold it; in one slot where 8 are not enough
+  int parts = 1;
+  while (parts < 8 && 2 * 16 * ((vecs + parts - 1) / parts) > room) parts *= 2;
+  a.slice = (int)((vecs + parts - 1) / parts);
+  const long long slot = ((long long)a.slice * 16 + 127) / 128 * 128;
+  if (slot > room) return ARD_ERR_UNSUPPORTED;
+  a.slot_bytes = slot > 0 ? (int)slot : 128;
+  a.slots = room / a.slot_bytes < DS_SLOTS ? room / a.slot_bytes : DS_SLOTS;
+  const size_t smem = (size_t)a.slots * a.slot_bytes + entry_bytes;
+  ARD_CUDA_OK(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+  long long clusters = (long long)per_sm * ctx->sm_count / parts;
+  if (parts > 1) clusters = ard_cluster_room(ctx, kern, parts, WORKERS + 64, (int)smem) / parts;
+  if (clusters > a.rows) clusters = a.rows;
+  ARD_CUDA_OK(ard_launch_cluster(ctx, kern, parts, dim3((unsigned)(clusters * parts)), dim3(WORKERS + 64), smem, s, a, parts));
   ctx->launches++;
   ARD_CUDA_OK(cudaGetLastError());
   return ARD_OK;
@@ -506,19 +661,15 @@ ard_status ds_rows(ard_ctx* ctx, const DsArgs& a, bool two, cudaStream_t s) {
 template <typename T>
 ard_status ds_launch(ard_ctx* ctx, const DsArgs& a, bool two, cudaStream_t s) {
   constexpr int VEC = 16 / (int)sizeof(T);
-  if (a.V <= 128) {
-    const int lanes = a.V <= 32 ? 8 : 32, per = DS_SHORT_THREADS / lanes;
-    const long long want = ((long long)a.rows + per - 1) / per, room = 8ll * ctx->sm_count;
-    const dim3 grid((unsigned)(want < room ? want : room));
-    ARD_CUDA_OK(ard_launch(ctx, lanes == 8 ? distill_short_kernel<T, 8> : distill_short_kernel<T, 32>, grid, dim3(DS_SHORT_THREADS), 0, s, a));
-    ctx->launches++;
-    ARD_CUDA_OK(cudaGetLastError());
-    return ARD_OK;
+  if (a.V <= 32 && a.k <= 8 * DS_SHORT_ENTRIES) return ds_lanes<T, 8, false, 4>(ctx, a, two, s);
+  if (a.k <= 32 * DS_SHORT_ENTRIES) {
+    if (a.V <= 128) return ds_lanes<T, 32, false, 4>(ctx, a, two, s);
+    if (a.V <= 32 * 2 * VEC) return ds_lanes<T, 32, true, 2>(ctx, a, two, s);
+    if (a.V <= 32 * 4 * VEC) return ds_lanes<T, 32, true, 4>(ctx, a, two, s);
+    if (a.V <= 32 * 8 * VEC) return ds_lanes<T, 32, true, 8>(ctx, a, two, s);
   }
-  if (a.V <= 128 * 4 * VEC) return ds_rows<T, 128, 4>(ctx, a, two, s);
-  if (a.V <= 256 * 8 * VEC) return ds_rows<T, 256, 8>(ctx, a, two, s);
-  if (a.V <= 512 * 8 * VEC) return ds_rows<T, 512, 8>(ctx, a, two, s);
-  return ds_rows<T, 512, 0>(ctx, a, two, s);
+  // four CTAs an SM while their rings hold two rows each
+  return (long long)a.V * (int)sizeof(T) <= 24 * 1024 ? ds_ring<T, 192>(ctx, a, two, 4, s) : ds_ring<T, 512>(ctx, a, two, 1, s);
 }
 
 }  // namespace
