@@ -367,22 +367,29 @@ __global__ void __launch_bounds__(DS_SHORT_THREADS) distill_lanes_kernel(const D
 }
 
 // ---- rows through a ring ------------------------------------------------------------------------------
-// WORKERS threads work on rows; behind them come a warp that fills the ring and one that has the entries.  `parts` CTAs, a cluster, share a row.
-constexpr int DS_SLOTS = 4;
+// A CTA's rows go to its TEAMS in turn, so that one team's barriers and sums pass while another's exponentials are at work.  A team is WORKERS threads and a warp that has the
+// entries; one more warp fills the ring for all of them.  `parts` CTAs, a cluster, share a row.
+constexpr int DS_SLOTS = 8, DS_PARTS = 8;
 
 struct DsInfo {
   float w;
   int label;  // -1: none
   int skip;
 };
+struct DsTeam {
+  float red_m[2][8], red_s[2][8], red_u[2][8];  // of its warps
+  float4 mail[2][DS_PARTS];                      // of the cluster's CTAs
+  unsigned long long post[2];                    // complete when all of them have come
+  float4 sums[2];                                // a row's maximum and sums, for the entries
+  float soft[2];                                 // whether a row has a teacher
+  float label_z[2];
+};
+template <int TEAMS>
 struct DsShared {
-  unsigned long long full[DS_SLOTS];
+  unsigned long long full[DS_SLOTS], empty[DS_SLOTS];
   DsInfo info[DS_SLOTS];
   float edge[DS_SLOTS][32];  // a row's loose logits
-  float red_m[2][16], red_s[2][16], red_u[2][16];  // of warps
-  float3 mail[2][8];         // of a cluster's CTAs
-  float soft[2];             // whether a row has a teacher
-  float3 sums[2];            // a row's maximum and sums, for the entries
+  DsTeam team[TEAMS];
   int abort;
 };
 // Some of a CTA's warps, in branches of their own: those that wait, and those that only have to have come so far.
@@ -395,20 +402,24 @@ __device__ __forceinline__ void ds_tell(int id, int threads) {
   asm volatile("bar.arrive %0, %1;" ::"r"(id), "r"(threads) : "memory");
 }
 
-template <typename T, int WORKERS, bool TWO>
-__global__ void __launch_bounds__(WORKERS + 64, WORKERS > 256 ? 1 : 4) distill_ring_kernel(const DsArgs a, int parts) {
+// Bytes of the teacher's entries of one row: token, share, its logarithm, logit; in fours, so that they are looked through four at a time.
+__host__ __device__ inline int ds_padded(int k) { return (k + 3) & ~3; }
+
+template <typename T, int WORKERS, int TEAMS, bool TWO>
+__global__ void __launch_bounds__(TEAMS * (WORKERS + 32) + 32, 1) distill_ring_kernel(const DsArgs a, int parts) {
   constexpr int VEC = 16 / (int)sizeof(T), WARPS = WORKERS / 32;
   extern __shared__ __align__(128) uint8_t ds_smem[];
-  __shared__ DsShared sh;
-  // entries of two rows: token, share, its logarithm, logit; the label comes last
-  const int entries = a.k + 1;
-  int* e_id = reinterpret_cast<int*>(ds_smem + (size_t)a.slots * a.slot_bytes);
-  float *e_p = reinterpret_cast<float*>(e_id + 2 * entries), *e_lp = e_p + 2 * entries, *e_z = e_lp + 2 * entries;
+  __shared__ DsShared<TEAMS> sh;
   pdl_launch_dependents();
-  const int t = threadIdx.x, warp = t >> 5, lane = t & 31;
+  const int t = threadIdx.x, lane = t & 31;
   const int rank = (int)(blockIdx.x % parts), first = (int)(blockIdx.x / parts), stride = (int)(gridDim.x / parts);
   if (t == 0) {
-    for (int i = 0; i < DS_SLOTS; ++i) mbar_init(smem_u32(&sh.full[i]), 1);
+    for (int i = 0; i < DS_SLOTS; ++i) {
+      mbar_init(smem_u32(&sh.full[i]), 1);
+      mbar_init(smem_u32(&sh.empty[i]), WARPS);
+    }
+    for (int i = 0; i < TEAMS; ++i)
+      for (int p = 0; p < 2; ++p) mbar_init(smem_u32(&sh.team[i].post[p]), 1);
     sh.abort = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -417,206 +428,233 @@ __global__ void __launch_bounds__(WORKERS + 64, WORKERS > 256 ? 1 : 4) distill_r
   pdl_wait_prior_grids();
   const float c1 = TWO || a.soft == 0.f ? a.c : a.c_tau;
   const int v0 = rank * a.slice;  // this CTA's vectors of a row: v0 .. v0 + slice - 1
-  auto cluster_meet = [&]() {
-    asm volatile("barrier.cluster.arrive.release;" ::: "memory");
-    asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
-  };
-  if (warp == WARPS) {  // fills the ring
-    auto fill = [&](long long r, int slot) {
+  if (t >= TEAMS * (WORKERS + 32)) {
+    // fills the ring; a row's weight, label and loose logits are asked for a row ahead
+    float w, edge;
+    int label;
+    auto ask = [&](long long r) {
       const T* z = (const T*)a.Z + r * a.ldz;
       const DsRow<T> row(z, a.V);
-      const float w = a.weight ? a.weight[r] : 1.f;
-      const int label = ds_label(a, r);
+      w = a.weight ? a.weight[r] : 1.f;
+      label = ds_label(a, r);
+      edge = rank == 0 && lane < row.loose ? ds_f32(z[row.loose_at(lane)]) : 0.f;
+    };
+    int n = 0;
+    ask(first);
+    for (long long r = first; r < a.rows; r += stride, ++n) {
+      const int slot = n % a.slots;
+      const T* z = (const T*)a.Z + r * a.ldz;
+      const DsRow<T> row(z, a.V);
+      if (n >= a.slots) mbar_wait(smem_u32(&sh.empty[slot]), (uint32_t)(n / a.slots - 1) & 1u, &sh.abort, a.status);
       const bool skip = w == 0.f || (label < 0 && a.k == 0);
-      if (!skip && rank == 0 && lane < row.loose) sh.edge[slot][lane] = ds_f32(z[row.loose_at(lane)]);
+      sh.edge[slot][lane] = edge;
       __syncwarp();
       if (lane == 0) {
         sh.info[slot] = {w, label, skip ? 1 : 0};
-        const int mine = max(0, min(row.vecs - v0, a.slice));
-        const uint32_t bar = smem_u32(&sh.full[slot]);
-        if (skip || mine == 0) {
+        const uint32_t bytes = skip ? 0u : (uint32_t)max(0, min(row.vecs - v0, a.slice)) * 16u, bar = smem_u32(&sh.full[slot]);
+        if (bytes == 0u) {
           mbar_arrive(bar);
         } else {
-          mbar_arrive_expect_tx(bar, (uint32_t)mine * 16u);
+          mbar_arrive_expect_tx(bar, bytes);
           asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(smem_u32(ds_smem + (size_t)slot * a.slot_bytes)),
-                       "l"(z + row.head + (long long)v0 * VEC), "r"((uint32_t)mine * 16u), "r"(bar)
+                       "l"(z + row.head + (long long)v0 * VEC), "r"(bytes), "r"(bar)
                        : "memory");
         }
       }
-    };
-    int n = 0;
-    for (long long r = first; r < a.rows && n < a.slots; r += stride, ++n) fill(r, n);
-    n = 0;
-    for (long long r = first; r < a.rows; r += stride, ++n) {
-      if (parts > 1) cluster_meet();
-      ds_meet(2, WORKERS + 64);  // the row's slot has been read
-      const long long next = r + (long long)a.slots * stride;
-      if (next < a.rows) fill(next, n % a.slots);
+      if (r + stride < a.rows) ask(r + stride);
     }
-    return;
-  }
-  if (warp == WARPS + 1) {  // entries
-    auto prepare = [&](long long r, int at) {
-      int* id = e_id + at * entries;
-      float *p = e_p + at * entries, *lp = e_lp + at * entries, *ze = e_z + at * entries;
-      const T* z = (const T*)a.Z + r * a.ldz;
-      const int label = ds_label(a, r);
-      const bool use = (a.weight ? a.weight[r] : 1.f) != 0.f;
-      float m = -INFINITY;
-      int live = 0;
-      for (int i = lane; i < a.k; i += 32) {
-        float tv;
-        const int j = ds_entry(a, r, i, tv);
-        id[i] = j;
-        lp[i] = tv;
-        ze[i] = use && j >= 0 ? ds_f32(z[j]) : 0.f;
-        if (j >= 0) live = 1, m = tv != tv ? tv : fmaxf(m, tv);
-      }
-      if (lane == 0) {
-        id[a.k] = label;
-        ze[a.k] = use && label >= 0 ? ds_f32(z[label]) : 0.f;
-      }
-      live = __any_sync(0xFFFFFFFFu, live);
-      m = lanes_max<32>(m);
-      float s = 0.f;
-      for (int i = lane; i < a.k; i += 32)
-        if (id[i] >= 0) s += p[i] = expf(lp[i] = (lp[i] - m) * a.inv_tau);
-      s = lanes_sum<32>(s);
-      const float log_s = logf(s);
-      for (int i = lane; i < a.k; i += 32)
-        if (id[i] >= 0) p[i] /= s, lp[i] -= log_s;
-      if (lane == 0) sh.soft[at] = live ? a.soft : 0.f;
-      __syncwarp();
-    };
-    double sum_loss = 0.0;
-    int n = 0;
-    if (first < a.rows) prepare(first, 0);
-    for (long long r = first; r < a.rows; r += stride, ++n) {
-      const int at = n & 1;
-      const int* id = e_id + at * entries;
-      const float *p = e_p + at * entries, *lp = e_lp + at * entries, *ze = e_z + at * entries;
-      ds_meet(1, WORKERS + 32);  // the warps' maxima and sums are there, and this row's entries
-      if (parts > 1) cluster_meet();
-      const float w = a.weight ? a.weight[r] : 1.f;
-      if (r + stride < a.rows) prepare(r + stride, at ^ 1);
-      ds_meet(2, WORKERS + 64);  // the row's gradient has been written
-      const int label = id[a.k];
-      const float hard = label >= 0 ? a.hard : 0.f, soft = sh.soft[at];
-      if (w == 0.f || (hard == 0.f && soft == 0.f)) {
-        if (rank == 0 && lane == 0) a.loss[r] = 0.f;
-        continue;
-      }
-      const float3 q = sh.sums[at];
-      const DsSlope f = {q.x, w * (TWO ? hard : hard + soft * a.tau) / q.y, TWO ? w * soft * a.tau / q.z : 0.f, c1, a.c_tau};
-      if (a.dZ) {
-        const DsRow<T> row((const T*)a.Z + r * a.ldz, a.V);
-        T* dz = (T*)a.dZ + r * a.lddz;
-        for (int i = lane; i < entries; i += 32) {
-          const int j = id[i];
-          if (j < 0) continue;
-          const int v = row.vec_of(j);
-          if (v < 0 ? rank != 0 : v < v0 || v >= v0 + a.slice) continue;  // another CTA's
-          float share = 0.f;  // all that falls on this token, in the entries' order
-          if (soft != 0.f)
-            for (int o = 0; o < a.k; ++o)
-              if (id[o] == j) share += p[o];
-          dz[j] = ds_from<T>(fmaf(-w, (j == label ? hard : 0.f) + soft * a.tau * share, f.at<TWO>(ze[i])));
+  } else {
+    const int team = t / (WORKERS + 32), tw = t % (WORKERS + 32), warp = tw >> 5;
+    DsTeam& tm = sh.team[team];
+    const int come = 1 + 2 * team, gone = 2 + 2 * team;  // barriers: a row's sums are there; its gradient has been written
+    const long long r1 = first + (long long)team * stride, step = (long long)TEAMS * stride;
+    if (warp == WARPS) {  // entries
+      const int kp = ds_padded(a.k);
+      int* e_id = reinterpret_cast<int*>(ds_smem + (size_t)a.slots * a.slot_bytes) + team * 8 * kp;
+      float *e_p = reinterpret_cast<float*>(e_id + 2 * kp), *e_lp = e_p + 2 * kp, *e_z = e_lp + 2 * kp;
+      auto prepare = [&](long long r, int at) {
+        int* id = e_id + at * kp;
+        float *p = e_p + at * kp, *lp = e_lp + at * kp, *ze = e_z + at * kp;
+        const T* z = (const T*)a.Z + r * a.ldz;
+        const int label = ds_label(a, r);
+        const bool use = (a.weight ? a.weight[r] : 1.f) != 0.f;
+        float m = -INFINITY;
+        int live = 0;
+        for (int i = lane; i < kp; i += 32) {
+          float tv = 0.f;
+          const int j = i < a.k ? ds_entry(a, r, i, tv) : -1;
+          id[i] = j;
+          lp[i] = tv;
+          p[i] = 0.f;
+          ze[i] = use && j >= 0 ? ds_f32(z[j]) : 0.f;
+          if (j >= 0) live = 1, m = tv != tv ? tv : fmaxf(m, tv);
         }
-      }
-      if (rank == 0) {
-        float kl = 0.f;
-        const float log_u = logf(TWO ? q.z : q.y);
-        if (soft != 0.f)
-          for (int i = lane; i < a.k; i += 32)
-            if (id[i] >= 0 && p[i] != 0.f) kl += p[i] * (lp[i] - ((ze[i] - q.x) * a.inv_tau - log_u));
-        kl = lanes_sum<32>(kl);
-        float L = soft != 0.f ? soft * a.tau * a.tau * kl : 0.f;
-        if (label >= 0) L = fmaf(hard, logf(q.y) - (ze[a.k] - q.x), L);
+        live = __any_sync(0xFFFFFFFFu, live);
+        m = lanes_max<32>(m);
+        float s = 0.f;
+        for (int i = lane; i < a.k; i += 32)
+          if (id[i] >= 0) s += p[i] = expf(lp[i] = (lp[i] - m) * a.inv_tau);
+        s = lanes_sum<32>(s);
+        const float log_s = logf(s);
+        for (int i = lane; i < a.k; i += 32)
+          if (id[i] >= 0) p[i] /= s, lp[i] -= log_s;
         if (lane == 0) {
-          a.loss[r] = L;
-          sum_loss += (double)w * L;
+          tm.soft[at] = live ? a.soft : 0.f;
+          tm.label_z[at] = use && label >= 0 ? ds_f32(z[label]) : 0.f;
         }
+        __syncwarp();
+      };
+      double sum_loss = 0.0;
+      int n = 0;
+      if (r1 < a.rows) prepare(r1, 0);
+      for (long long r = r1; r < a.rows; r += step, ++n) {
+        const int at = n & 1;
+        const int* id = e_id + at * kp;
+        const float *p = e_p + at * kp, *lp = e_lp + at * kp, *ze = e_z + at * kp;
+        ds_meet(come, WORKERS + 32);
+        const float w = a.weight ? a.weight[r] : 1.f;
+        const int label = ds_label(a, r);
+        if (r + step < a.rows) prepare(r + step, at ^ 1);
+        ds_meet(gone, WORKERS + 32);
+        const float hard = label >= 0 ? a.hard : 0.f, soft = tm.soft[at];
+        if (w == 0.f || (hard == 0.f && soft == 0.f)) {
+          if (rank == 0 && lane == 0) a.loss[r] = 0.f;
+          continue;
+        }
+        const float4 q = tm.sums[at];
+        const float zl = tm.label_z[at];
+        const DsSlope f = {q.x, w * (TWO ? hard : hard + soft * a.tau) / q.y, TWO ? w * soft * a.tau / q.z : 0.f, c1, a.c_tau};
+        if (a.dZ) {
+          const DsRow<T> row((const T*)a.Z + r * a.ldz, a.V);
+          T* dz = (T*)a.dZ + r * a.lddz;
+          for (int i = lane; i <= a.k; i += 32) {  // the label is the last one
+            const int j = i < a.k ? id[i] : label;
+            if (j < 0) continue;
+            const int v = row.vec_of(j);
+            if (v < 0 ? rank != 0 : v < v0 || v >= v0 + a.slice) continue;  // another CTA's
+            float share = 0.f;  // all that falls on this token, in the entries' order
+            if (soft != 0.f)
+              for (int o = 0; o < kp; o += 4) {
+                const int4 oi = *reinterpret_cast<const int4*>(id + o);
+                const float4 op = *reinterpret_cast<const float4*>(p + o);
+                share += oi.x == j ? op.x : 0.f;
+                share += oi.y == j ? op.y : 0.f;
+                share += oi.z == j ? op.z : 0.f;
+                share += oi.w == j ? op.w : 0.f;
+              }
+            dz[j] = ds_from<T>(fmaf(-w, (j == label ? hard : 0.f) + soft * a.tau * share, f.at<TWO>(i < a.k ? ze[i] : zl)));
+          }
+        }
+        if (rank == 0) {
+          float kl = 0.f;
+          const float log_u = logf(TWO ? q.z : q.y);
+          if (soft != 0.f)
+            for (int i = lane; i < a.k; i += 32)
+              if (id[i] >= 0 && p[i] != 0.f) kl += p[i] * (lp[i] - ((ze[i] - q.x) * a.inv_tau - log_u));
+          kl = lanes_sum<32>(kl);
+          float L = soft != 0.f ? soft * a.tau * a.tau * kl : 0.f;
+          if (label >= 0) L = fmaf(hard, logf(q.y) - (zl - q.x), L);
+          if (lane == 0) {
+            a.loss[r] = L;
+            sum_loss += (double)w * L;
+          }
+        }
+        __syncwarp();
       }
-      __syncwarp();
+      if (a.total && rank == 0) ds_total(a, sum_loss, first * TEAMS + team, stride * TEAMS, lane);
+    } else {
+      int n = 0;
+      for (long long r = r1; r < a.rows; r += step, ++n) {
+        const int all = n * TEAMS + team, slot = all % a.slots, at = n & 1;  // (rows of all teams lie in the ring in turn)
+        const T* z = (const T*)a.Z + r * a.ldz;
+        T* dz = a.dZ ? (T*)a.dZ + r * a.lddz : nullptr;
+        const DsRow<T> row(z, a.V);
+        const int mine = max(0, min(row.vecs - v0, a.slice));
+        mbar_wait(smem_u32(&sh.full[slot]), (uint32_t)(all / a.slots) & 1u, &sh.abort, a.status);
+        const DsInfo info = sh.info[slot];
+        const uint4* zs = reinterpret_cast<const uint4*>(ds_smem + (size_t)slot * a.slot_bytes);
+        const bool edged = rank == 0 && tw < row.loose && !info.skip;
+        const float edge = edged ? sh.edge[slot][tw] : -INFINITY;
+        float m = edge;
+        float2 s2 = make_float2(0.f, 0.f), u2 = make_float2(0.f, 0.f);
+        if (!info.skip) {
+#pragma unroll 4
+          for (int i = tw; i < mine; i += WORKERS) m = fmaxf(m, DsVec<T>(zs[i]).max());
+        }
+        m = ds_floor(m);
+        if (!info.skip) {
+#pragma unroll 4
+          for (int i = tw; i < mine; i += WORKERS) {
+            const DsVec<T> x(zs[i]);
+            x.add(s2, m, c1);
+            if (TWO) x.add(u2, m, a.c_tau);
+          }
+          s2.x += ds_exp2((edge - m) * c1);  // fmaxf passes NaN over; the sums do not
+          if (TWO) u2.x += ds_exp2((edge - m) * a.c_tau);
+        }
+        float s = s2.x + s2.y, u = u2.x + u2.y;
+        {
+          const float top = lanes_max<32>(m);
+          s = lanes_sum<32>(s * ds_shift(m, top, c1));
+          if (TWO) u = lanes_sum<32>(u * ds_shift(m, top, a.c_tau));
+          if (lane == 0) {
+            tm.red_m[at][warp] = top;
+            tm.red_s[at][warp] = s;
+            if (TWO) tm.red_u[at][warp] = u;
+          }
+        }
+        ds_meet(come, WORKERS + 32);
+        m = tm.red_m[at][0];
+#pragma unroll
+        for (int i = 1; i < WARPS; ++i) m = fmaxf(m, tm.red_m[at][i]);
+        s = 0.f, u = 0.f;
+#pragma unroll
+        for (int i = 0; i < WARPS; ++i) {
+          s += tm.red_s[at][i] * ds_shift(tm.red_m[at][i], m, c1);
+          if (TWO) u += tm.red_u[at][i] * ds_shift(tm.red_m[at][i], m, a.c_tau);
+        }
+        if (parts > 1) {
+          // to every CTA's mail; a place is written again two rows on, when its reader has sent the row between
+          const uint32_t post = smem_u32(&tm.post[at]);
+          if (tw == 0) mbar_arrive_expect_tx(post, (uint32_t)parts * 16u);
+          if (tw < parts) {
+            uint32_t place, bar;
+            asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(place) : "r"(smem_u32(&tm.mail[at][rank])), "r"(tw));
+            asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(bar) : "r"(post), "r"(tw));
+            st_async_f4(place, bar, m, s, u, 0.f);
+          }
+          mbar_wait_cluster(post, (uint32_t)(n >> 1) & 1u, &sh.abort, a.status);
+          m = tm.mail[at][0].x;
+          for (int i = 1; i < parts; ++i) m = fmaxf(m, tm.mail[at][i].x);
+          s = 0.f, u = 0.f;
+          for (int i = 0; i < parts; ++i) {
+            const float4 q = tm.mail[at][i];
+            s += q.y * ds_shift(q.x, m, c1);
+            if (TWO) u += q.z * ds_shift(q.x, m, a.c_tau);
+          }
+        }
+        if (tw == 0) tm.sums[at] = make_float4(m, s, u, 0.f);
+        const float hard = info.label >= 0 ? a.hard : 0.f, soft = tm.soft[at];
+        if (info.skip || (hard == 0.f && soft == 0.f)) {
+          ds_zero(dz, a.V, rank, parts, tw, WORKERS);
+        } else if (dz) {
+          const DsSlope f = {m, info.w * (TWO ? hard : hard + soft * a.tau) / s, TWO ? info.w * soft * a.tau / u : 0.f, c1, a.c_tau};
+          const bool same = ((reinterpret_cast<uintptr_t>(z) ^ reinterpret_cast<uintptr_t>(dz)) & 15u) == 0;
+          T* out = dz + row.head + (long long)v0 * VEC;
+#pragma unroll 4
+          for (int i = tw; i < mine; i += WORKERS) ds_put<T, TWO>(f, zs[i], out + i * VEC, same);
+          if (edged) dz[row.loose_at(tw)] = ds_from<T>(f.at<TWO>(edge));
+        }
+        fence_proxy_async_smem();  // what was read from the slot, before the next copy into it
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&sh.empty[slot]));
+        ds_tell(gone, WORKERS + 32);
+      }
     }
-    if (a.total && rank == 0) ds_total(a, sum_loss, first, stride, lane);
-    return;
   }
-  int n = 0;
-  for (long long r = first; r < a.rows; r += stride, ++n) {
-    const int slot = n % a.slots, at = n & 1;
-    const T* z = (const T*)a.Z + r * a.ldz;
-    T* dz = a.dZ ? (T*)a.dZ + r * a.lddz : nullptr;
-    const DsRow<T> row(z, a.V);
-    const int mine = max(0, min(row.vecs - v0, a.slice));
-    mbar_wait(smem_u32(&sh.full[slot]), (uint32_t)(n / a.slots) & 1u, &sh.abort, a.status);
-    const DsInfo info = sh.info[slot];
-    const uint4* zs = reinterpret_cast<const uint4*>(ds_smem + (size_t)slot * a.slot_bytes);
-    const bool edged = rank == 0 && t < row.loose && !info.skip;
-    const float edge = edged ? sh.edge[slot][t] : -INFINITY;
-    float m = edge;
-    float2 s2 = make_float2(0.f, 0.f), u2 = make_float2(0.f, 0.f);
-    if (!info.skip) {
-#pragma unroll 4
-      for (int i = t; i < mine; i += WORKERS) m = fmaxf(m, DsVec<T>(zs[i]).max());
-    }
-    m = ds_floor(m);
-    if (!info.skip) {
-#pragma unroll 4
-      for (int i = t; i < mine; i += WORKERS) {
-        const DsVec<T> x(zs[i]);
-        x.add(s2, m, c1);
-        if (TWO) x.add(u2, m, a.c_tau);
-      }
-      s2.x += ds_exp2((edge - m) * c1);  // fmaxf passes NaN over; the sums do not
-      if (TWO) u2.x += ds_exp2((edge - m) * a.c_tau);
-    }
-    float s = s2.x + s2.y, u = u2.x + u2.y;
-    {
-      const float top = lanes_max<32>(m);
-      s = lanes_sum<32>(s * ds_shift(m, top, c1));
-      if (TWO) u = lanes_sum<32>(u * ds_shift(m, top, a.c_tau));
-      if (lane == 0) {
-        sh.red_m[at][warp] = top;
-        sh.red_s[at][warp] = s;
-        if (TWO) sh.red_u[at][warp] = u;
-      }
-    }
-    ds_meet(1, WORKERS + 32);
-    m = sh.red_m[at][0];
-#pragma unroll
-    for (int i = 1; i < WARPS; ++i) m = fmaxf(m, sh.red_m[at][i]);
-    s = 0.f, u = 0.f;
-#pragma unroll
-    for (int i = 0; i < WARPS; ++i) {
-      s += sh.red_s[at][i] * ds_shift(sh.red_m[at][i], m, c1);
-      if (TWO) u += sh.red_u[at][i] * ds_shift(sh.red_m[at][i], m, a.c_tau);
-    }
-    if (parts > 1) {
-      if (t < parts) *cg::this_cluster().map_shared_rank(&sh.mail[at][rank], t) = make_float3(m, s, u);
-      cluster_meet();
-      m = sh.mail[at][0].x;
-      for (int i = 1; i < parts; ++i) m = fmaxf(m, sh.mail[at][i].x);
-      s = 0.f, u = 0.f;
-      for (int i = 0; i < parts; ++i) {
-        s += sh.mail[at][i].y * ds_shift(sh.mail[at][i].x, m, c1);
-        if (TWO) u += sh.mail[at][i].z * ds_shift(sh.mail[at][i].x, m, a.c_tau);
-      }
-    }
-    if (t == 0) sh.sums[at] = make_float3(m, s, u);
-    const float hard = info.label >= 0 ? a.hard : 0.f, soft = sh.soft[at];
-    if (info.skip || (hard == 0.f && soft == 0.f)) {
-      ds_zero(dz, a.V, rank, parts, t, WORKERS);
-    } else if (dz) {
-      const DsSlope f = {m, info.w * (TWO ? hard : hard + soft * a.tau) / s, TWO ? info.w * soft * a.tau / u : 0.f, c1, a.c_tau};
-      const bool same = ((reinterpret_cast<uintptr_t>(z) ^ reinterpret_cast<uintptr_t>(dz)) & 15u) == 0;
-      T* out = dz + row.head + (long long)v0 * VEC;
-#pragma unroll 4
-      for (int i = t; i < mine; i += WORKERS) ds_put<T, TWO>(f, zs[i], out + i * VEC, same);
-      if (edged) dz[row.loose_at(t)] = ds_from<T>(f.at<TWO>(edge));
-    }
-    fence_proxy_async_smem();  // what was read from the slot, before the next copy into it
-    ds_tell(2, WORKERS + 64);
+  if (parts > 1) {
+    __syncwarp();
+    cg::this_cluster().sync();  // nobody leaves while mail may still come
   }
 }
 
@@ -632,27 +670,30 @@ ard_status ds_lanes(ard_ctx* ctx, const DsArgs& a, bool two, cudaStream_t s) {
   return ARD_OK;
 }
 
-template <typename T, int WORKERS>
-ard_status ds_ring(ard_ctx* ctx, DsArgs a, bool two, int per_sm, cudaStream_t s) {
-  constexpr int VEC = 16 / (int)sizeof(T);
-  auto kern = two ? distill_ring_kernel<T, WORKERS, true> : distill_ring_kernel<T, WORKERS, false>;
-  const int entry_bytes = 2 * (a.k + 1) * 16, fixed = 2560;                 // (fixed: the kernel's own variables)
-  const int room = (227 * 1024 / per_sm - 1024 - fixed - entry_bytes) / 128 * 128;  // the ring's (1 KB a CTA is the system's)
-  const long long vecs = (long long)a.V / VEC;
-  // a row in two slots of one CTA, or cut over as few as will hold it; in one slot where 8 are not enough
-  int parts = 1;
-  while (parts < 8 && 2 * 16 * ((vecs + parts - 1) / parts) > room) parts *= 2;
+constexpr int DS_ROOM = 227 * 1024 - 4096;  // a CTA's ring and entries (beside the kernel's own variables)
+
+// Slots of a ring for rows of `vecs` vectors cut into `parts`.
+template <int TEAMS>
+int ds_slots(long long vecs, int k, int parts) {
+  const long long slot = ((vecs + parts - 1) / parts * 16 + 127) / 128 * 128;
+  return slot > 0 ? (int)((DS_ROOM - TEAMS * 32ll * ds_padded(k)) / slot) : DS_SLOTS;
+}
+template <typename T, int WORKERS, int TEAMS>
+ard_status ds_ring(ard_ctx* ctx, DsArgs a, bool two, int parts, cudaStream_t s) {
+  constexpr int THREADS = TEAMS * (WORKERS + 32) + 32;
+  auto kern = two ? distill_ring_kernel<T, WORKERS, TEAMS, true> : distill_ring_kernel<T, WORKERS, TEAMS, false>;
+  const long long vecs = (long long)a.V * (int)sizeof(T) / 16;
   a.slice = (int)((vecs + parts - 1) / parts);
-  const long long slot = ((long long)a.slice * 16 + 127) / 128 * 128;
-  if (slot > room) return ARD_ERR_UNSUPPORTED;
-  a.slot_bytes = slot > 0 ? (int)slot : 128;
-  a.slots = room / a.slot_bytes < DS_SLOTS ? room / a.slot_bytes : DS_SLOTS;
-  const size_t smem = (size_t)a.slots * a.slot_bytes + entry_bytes;
+  a.slot_bytes = a.slice > 0 ? (a.slice * 16 + 127) / 128 * 128 : 128;
+  const int slots = ds_slots<TEAMS>(vecs, a.k, parts);
+  if (slots < 1) return ARD_ERR_UNSUPPORTED;
+  a.slots = slots < DS_SLOTS ? slots : DS_SLOTS;
+  const size_t smem = (size_t)a.slots * a.slot_bytes + TEAMS * 32ull * ds_padded(a.k);
   ARD_CUDA_OK(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
-  long long clusters = (long long)per_sm * ctx->sm_count / parts;
-  if (parts > 1) clusters = ard_cluster_room(ctx, kern, parts, WORKERS + 64, (int)smem) / parts;
+  long long clusters = ctx->sm_count;
+  if (parts > 1) clusters = ard_cluster_room(ctx, kern, parts, THREADS, (int)smem) / parts;
   if (clusters > a.rows) clusters = a.rows;
-  ARD_CUDA_OK(ard_launch_cluster(ctx, kern, parts, dim3((unsigned)(clusters * parts)), dim3(WORKERS + 64), smem, s, a, parts));
+  ARD_CUDA_OK(ard_launch_cluster(ctx, kern, parts, dim3((unsigned)(clusters * parts)), dim3(THREADS), smem, s, a, parts));
   ctx->launches++;
   ARD_CUDA_OK(cudaGetLastError());
   return ARD_OK;
@@ -668,8 +709,12 @@ ard_status ds_launch(ard_ctx* ctx, const DsArgs& a, bool two, cudaStream_t s) {
     if (a.V <= 32 * 4 * VEC) return ds_lanes<T, 32, true, 4>(ctx, a, two, s);
     if (a.V <= 32 * 8 * VEC) return ds_lanes<T, 32, true, 8>(ctx, a, two, s);
   }
-  // four CTAs an SM while their rings hold two rows each
-  return (long long)a.V * (int)sizeof(T) <= 24 * 1024 ? ds_ring<T, 192>(ctx, a, two, 4, s) : ds_ring<T, 512>(ctx, a, two, 1, s);
+  // four teams where the ring holds a row for each and one on its way, else two, with rows cut over as few CTAs as that takes
+  const long long vecs = (long long)a.V / VEC;
+  if (ds_slots<4>(vecs, a.k, 1) >= 5) return ds_ring<T, 192, 4>(ctx, a, two, 1, s);
+  int parts = 1;
+  while (parts < DS_PARTS && ds_slots<2>(vecs, a.k, parts) < 3) parts *= 2;
+  return ds_ring<T, 256, 2>(ctx, a, two, parts, s);
 }
 
 }  // namespace
