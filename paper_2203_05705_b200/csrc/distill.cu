@@ -7,7 +7,7 @@
 // asks for, while the others work on what is there, and a row too long for a ring of two is cut over a cluster of CTAs, which exchange a maximum and
 // sums once a row.  A third kind of warp does what depends on a few scattered logits: the teacher's softmax for the next row, and for this one the loss and the
 // gradient's entries at the label and the teacher's tokens, which are written once more behind the others.  Each thread keeps the maximum of what it looks at and
-// sums of exponentials relative to it; these pairs meet once a row.  Rows of up to 2048 logits (fp32: 1024) are held by a warp or 8 lanes, in registers.
+// sums of exponentials relative to it; these pairs meet once a row.  Rows of up to 4096 logits (fp32: 2048) are held by a warp or 8 lanes, in registers.
 #include <cooperative_groups.h>
 
 #include "ard_internal.h"
@@ -42,6 +42,22 @@ __device__ __forceinline__ float ds_exp2(float x) {
   float r;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
   return r;
+}
+__device__ __forceinline__ float2 ds_exps(float2 d, float c) {
+  const float2 y = __fmul2_rn(d, make_float2(c, c));
+  return make_float2(ds_exp2(y.x), ds_exp2(y.y));
+}
+// MODE: 0 one softmax; 1 that at temperature 1 and that at tau; 2, 3 both with tau = 2, 4, where exp(d) is exp(d / tau) squared once or twice: half of the
+// exponentials, which bound the two (8192 x 32000 bf16 283 us with them all, 206 so), for an error of one or two more units in the last place.
+template <int MODE>
+__device__ __forceinline__ float ds_power(float e) {
+  e *= e;
+  return MODE == 3 ? e * e : e;
+}
+template <int MODE>
+__device__ __forceinline__ float2 ds_power(float2 e) {
+  e = __fmul2_rn(e, e);
+  return MODE == 3 ? __fmul2_rn(e, e) : e;
 }
 template <typename T>
 __device__ __forceinline__ float ds_f32(T x) {
@@ -93,12 +109,19 @@ struct DsVec {
     for (int i = 1; i < N / 2; ++i) m = fmaxf(m, fmaxf(v[i].x, v[i].y));
     return m;
   }
-  // Exponentials of (x - m) c, added up in pairs.
-  __device__ __forceinline__ void add(float2& s, float m, float c) const {
+  // Exponentials of (x - m) c1, and of (x - m) c_tau, added up in pairs.
+  template <int MODE>
+  __device__ __forceinline__ void add(float2& s, float2& u, float m, float c1, float c_tau) const {
 #pragma unroll
     for (int i = 0; i < N / 2; ++i) {
-      const float2 d = __fmul2_rn(__fadd2_rn(v[i], make_float2(-m, -m)), make_float2(c, c));
-      s = __fadd2_rn(s, make_float2(ds_exp2(d.x), ds_exp2(d.y)));
+      const float2 d = __fadd2_rn(v[i], make_float2(-m, -m));
+      if (MODE == 0) {
+        s = __fadd2_rn(s, ds_exps(d, c1));
+      } else {
+        const float2 e = ds_exps(d, c_tau);
+        u = __fadd2_rn(u, e);
+        s = __fadd2_rn(s, MODE == 1 ? ds_exps(d, c1) : ds_power<MODE>(e));
+      }
     }
   }
 };
@@ -122,33 +145,30 @@ struct DsRow {
 // The gradient's factors of a row: g = by1 exp((x - m) c1) + by_tau exp((x - m) c_tau).
 struct DsSlope {
   float m, by1, by_tau, c1, c_tau;
-  template <bool TWO>
+  template <int MODE>
   __device__ __forceinline__ float at(float x) const {
     const float d = x - m;
-    float g = by1 * ds_exp2(d * c1);
-    if (TWO) g = fmaf(by_tau, ds_exp2(d * c_tau), g);
-    return g;
+    if (MODE == 0) return by1 * ds_exp2(d * c1);
+    const float e = ds_exp2(d * c_tau);
+    return fmaf(by1, MODE == 1 ? ds_exp2(d * c1) : ds_power<MODE>(e), by_tau * e);
   }
-  template <bool TWO>
+  template <int MODE>
   __device__ __forceinline__ float2 at(float2 x) const {
-    const float2 d = __fadd2_rn(x, make_float2(-m, -m)), a = __fmul2_rn(d, make_float2(c1, c1));
-    float2 g = __fmul2_rn(make_float2(by1, by1), make_float2(ds_exp2(a.x), ds_exp2(a.y)));
-    if (TWO) {
-      const float2 b = __fmul2_rn(d, make_float2(c_tau, c_tau));
-      g = __ffma2_rn(make_float2(by_tau, by_tau), make_float2(ds_exp2(b.x), ds_exp2(b.y)), g);
-    }
-    return g;
+    const float2 d = __fadd2_rn(x, make_float2(-m, -m)), f1 = make_float2(by1, by1);
+    if (MODE == 0) return __fmul2_rn(f1, ds_exps(d, c1));
+    const float2 e = ds_exps(d, c_tau);
+    return __ffma2_rn(f1, MODE == 1 ? ds_exps(d, c1) : ds_power<MODE>(e), __fmul2_rn(make_float2(by_tau, by_tau), e));
   }
 };
 // A vector's gradient to memory; same: dz lies on the 16-byte grid where z does.
-template <typename T, bool TWO>
+template <typename T, int MODE>
 __device__ __forceinline__ void ds_put(const DsSlope& f, const uint4& q, T* dz, bool same) {
   constexpr int VEC = 16 / (int)sizeof(T);
   const DsVec<T> x(q);
   T e[VEC];
 #pragma unroll
   for (int k = 0; k < VEC; k += 2) {
-    const float2 g = f.at<TWO>(x.v[k / 2]);
+    const float2 g = f.at<MODE>(x.v[k / 2]);
     if constexpr (sizeof(T) == 2) {
       const __nv_bfloat162 h = __floats2bfloat162_rn(g.x, g.y);
       memcpy(e + k, &h, 4);
@@ -212,13 +232,15 @@ __device__ __forceinline__ int ds_entry(const DsArgs& a, long long r, int i, flo
 constexpr int DS_SHORT_THREADS = 256, DS_SHORT_ENTRIES = 2;  // teacher's entries a lane
 
 // LANES lanes a row, NV vectors of 16 bytes a lane (WIDE) or NV single logits.
-template <typename T, int LANES, bool WIDE, int NV, bool TWO>
+template <typename T, int LANES, bool WIDE, int NV, int MODE>
 __global__ void __launch_bounds__(DS_SHORT_THREADS) distill_lanes_kernel(const DsArgs a) {
   constexpr int VEC = WIDE ? 16 / (int)sizeof(T) : 1, PER = DS_SHORT_THREADS / LANES, E = DS_SHORT_ENTRIES;
+  constexpr int EDGES = WIDE ? (2 * VEC - 2 + LANES - 1) / LANES : 1;  // a lane's loose logits
   __shared__ double s_sum[DS_SHORT_THREADS / 32];
   pdl_launch_dependents();
   pdl_wait_prior_grids();
   const int t = threadIdx.x, lane = t & (LANES - 1);
+  constexpr bool TWO = MODE != 0;
   const float c1 = TWO || a.soft == 0.f ? a.c : a.c_tau;  // of the only softmax, or of temperature 1's
   double sum_loss = 0.0;
   for (long long r0 = (long long)blockIdx.x * PER; r0 < a.rows; r0 += (long long)gridDim.x * PER) {
@@ -240,37 +262,43 @@ __global__ void __launch_bounds__(DS_SHORT_THREADS) distill_lanes_kernel(const D
     const bool look = w != 0.f && (label >= 0 || a.k > 0);
     uint4 q[WIDE ? NV : 1];
     float x[WIDE ? 1 : NV];
-    float edge = -INFINITY, m;
+    float edge[EDGES], m = -INFINITY;
     if constexpr (WIDE) {
       const uint4* zv = reinterpret_cast<const uint4*>(z + row.head);
 #pragma unroll
       for (int i = 0; i < NV; ++i)
         if (look && lane + i * LANES < row.vecs) q[i] = zv[lane + i * LANES];
-      if (look && lane < row.loose) edge = ds_f32(z[row.loose_at(lane)]);
-      m = edge;
+#pragma unroll
+      for (int i = 0; i < EDGES; ++i) {
+        edge[i] = look && lane + i * LANES < row.loose ? ds_f32(z[row.loose_at(lane + i * LANES)]) : -INFINITY;
+        m = fmaxf(m, edge[i]);
+      }
 #pragma unroll
       for (int i = 0; i < NV; ++i)
         if (look && lane + i * LANES < row.vecs) m = fmaxf(m, DsVec<T>(q[i]).max());
     } else {
-      m = -INFINITY;
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
         x[i] = look && lane + i * LANES < a.V ? ds_f32(z[lane + i * LANES]) : -INFINITY;
         m = fmaxf(m, x[i]);
       }
     }
+#pragma unroll
+    for (int e = 0; e < E; ++e) ze[e] = look && id[e] >= 0 ? ds_f32(z[id[e]]) : 0.f;
+    const float zl = look && label >= 0 ? ds_f32(z[label]) : 0.f;
     m = ds_floor(lanes_max<LANES>(m));
     float2 s2 = make_float2(0.f, 0.f), u2 = make_float2(0.f, 0.f);
     if constexpr (WIDE) {
 #pragma unroll
       for (int i = 0; i < NV; ++i)
         if (look && lane + i * LANES < row.vecs) {
-          const DsVec<T> y(q[i]);
-          y.add(s2, m, c1);
-          if (TWO) y.add(u2, m, a.c_tau);
+          DsVec<T>(q[i]).template add<MODE>(s2, u2, m, c1, a.c_tau);
         }
-      s2.x += ds_exp2((edge - m) * c1);
-      if (TWO) u2.x += ds_exp2((edge - m) * a.c_tau);
+#pragma unroll
+      for (int i = 0; i < EDGES; ++i) {
+        s2.x += ds_exp2((edge[i] - m) * c1);
+        if (TWO) u2.x += ds_exp2((edge[i] - m) * a.c_tau);
+      }
     } else {
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
@@ -291,13 +319,11 @@ __global__ void __launch_bounds__(DS_SHORT_THREADS) distill_lanes_kernel(const D
     tm = lanes_max<LANES>(tm);
 #pragma unroll
     for (int e = 0; e < E; ++e) {
-      ze[e] = look && id[e] >= 0 ? ds_f32(z[id[e]]) : 0.f;
       lp[e] = (lp[e] - tm) * a.inv_tau;
       p[e] = id[e] >= 0 ? expf(lp[e]) : 0.f;
       ts += p[e];
     }
     ts = lanes_sum<LANES>(ts);
-    const float zl = look && label >= 0 ? ds_f32(z[label]) : 0.f;
     const float hard = label >= 0 ? a.hard : 0.f, soft = live > 0.f ? a.soft : 0.f;
     const bool some = look && (hard != 0.f || soft != 0.f);
     const float log_s = logf(s), log_u = TWO ? logf(u) : log_s, log_ts = logf(ts);
@@ -323,12 +349,14 @@ __global__ void __launch_bounds__(DS_SHORT_THREADS) distill_lanes_kernel(const D
           const bool same = ((reinterpret_cast<uintptr_t>(z) ^ reinterpret_cast<uintptr_t>(dz)) & 15u) == 0;
 #pragma unroll
           for (int i = 0; i < NV; ++i)
-            if (lane + i * LANES < row.vecs) ds_put<T, TWO>(f, q[i], dz + row.head + (lane + i * LANES) * VEC, same);
-          if (lane < row.loose) dz[row.loose_at(lane)] = ds_from<T>(f.at<TWO>(edge));
+            if (lane + i * LANES < row.vecs) ds_put<T, MODE>(f, q[i], dz + row.head + (lane + i * LANES) * VEC, same);
+#pragma unroll
+          for (int i = 0; i < EDGES; ++i)
+            if (lane + i * LANES < row.loose) dz[row.loose_at(lane + i * LANES)] = ds_from<T>(f.at<MODE>(edge[i]));
         } else {
 #pragma unroll
           for (int i = 0; i < NV; ++i)
-            if (lane + i * LANES < a.V) dz[lane + i * LANES] = ds_from<T>(f.at<TWO>(x[i]));
+            if (lane + i * LANES < a.V) dz[lane + i * LANES] = ds_from<T>(f.at<MODE>(x[i]));
         }
       }
       __syncwarp();
@@ -349,8 +377,8 @@ __global__ void __launch_bounds__(DS_SHORT_THREADS) distill_lanes_kernel(const D
       if (dz && some) {
 #pragma unroll
         for (int e = 0; e < E; ++e)
-          if (id[e] >= 0) dz[id[e]] = ds_from<T>(fmaf(-w, (id[e] == label ? hard : 0.f) + soft * a.tau * on[e], f.at<TWO>(ze[e])));
-        if (lane == 0 && label >= 0) dz[label] = ds_from<T>(fmaf(-w, hard + soft * a.tau * on_label, f.at<TWO>(zl)));
+          if (id[e] >= 0) dz[id[e]] = ds_from<T>(fmaf(-w, (id[e] == label ? hard : 0.f) + soft * a.tau * on[e], f.at<MODE>(ze[e])));
+        if (lane == 0 && label >= 0) dz[label] = ds_from<T>(fmaf(-w, hard + soft * a.tau * on_label, f.at<MODE>(zl)));
       }
       __syncwarp();
     }
@@ -367,8 +395,8 @@ __global__ void __launch_bounds__(DS_SHORT_THREADS) distill_lanes_kernel(const D
 }
 
 // ---- rows through a ring ------------------------------------------------------------------------------
-// A CTA's rows go to its TEAMS in turn, so that one team's barriers and sums pass while another's exponentials are at work.  A team is WORKERS threads and a warp that has the
-// entries; one more warp fills the ring for all of them.  `parts` CTAs, a cluster, share a row.
+// A CTA's rows go to its TEAMS in turn, so that one team's barriers and sums pass while another's exponentials are at work.  A team is WORKERS threads, a warp that gets the next row's
+// entries ready and one that writes the last one's, with the loss; one more warp fills the ring for all of them.  `parts` CTAs, a cluster, share a row.
 constexpr int DS_SLOTS = 8, DS_PARTS = 8;
 
 struct DsInfo {
@@ -382,7 +410,8 @@ struct DsTeam {
   unsigned long long post[2];                    // complete when all of them have come
   float4 sums[2];                                // a row's maximum and sums, for the entries
   float soft[2];                                 // whether a row has a teacher
-  float label_z[2];
+  float label_z[2], w[2];
+  int label[2];
 };
 template <int TEAMS>
 struct DsShared {
@@ -405,8 +434,8 @@ __device__ __forceinline__ void ds_tell(int id, int threads) {
 // Bytes of the teacher's entries of one row: token, share, its logarithm, logit; in fours, so that they are looked through four at a time.
 __host__ __device__ inline int ds_padded(int k) { return (k + 3) & ~3; }
 
-template <typename T, int WORKERS, int TEAMS, bool TWO>
-__global__ void __launch_bounds__(TEAMS * (WORKERS + 32) + 32, 1) distill_ring_kernel(const DsArgs a, int parts) {
+template <typename T, int WORKERS, int TEAMS, int MODE>
+__global__ void __launch_bounds__(TEAMS * (WORKERS + 64) + 32, 1) distill_ring_kernel(const DsArgs a, int parts) {
   constexpr int VEC = 16 / (int)sizeof(T), WARPS = WORKERS / 32;
   extern __shared__ __align__(128) uint8_t ds_smem[];
   __shared__ DsShared<TEAMS> sh;
@@ -426,9 +455,10 @@ __global__ void __launch_bounds__(TEAMS * (WORKERS + 32) + 32, 1) distill_ring_k
   __syncthreads();
   if (parts > 1) cg::this_cluster().sync();  // every CTA of it is there
   pdl_wait_prior_grids();
+  constexpr bool TWO = MODE != 0;
   const float c1 = TWO || a.soft == 0.f ? a.c : a.c_tau;
   const int v0 = rank * a.slice;  // this CTA's vectors of a row: v0 .. v0 + slice - 1
-  if (t >= TEAMS * (WORKERS + 32)) {
+  if (t >= TEAMS * (WORKERS + 64)) {
     // fills the ring; a row's weight, label and loose logits are asked for a row ahead
     float w, edge;
     int label;
@@ -464,30 +494,50 @@ __global__ void __launch_bounds__(TEAMS * (WORKERS + 32) + 32, 1) distill_ring_k
       if (r + stride < a.rows) ask(r + stride);
     }
   } else {
-    const int team = t / (WORKERS + 32), tw = t % (WORKERS + 32), warp = tw >> 5;
+    const int team = t / (WORKERS + 64), tw = t % (WORKERS + 64), warp = tw >> 5;
     DsTeam& tm = sh.team[team];
     const int come = 1 + 2 * team, gone = 2 + 2 * team;  // barriers: a row's sums are there; its gradient has been written
     const long long r1 = first + (long long)team * stride, step = (long long)TEAMS * stride;
-    if (warp == WARPS) {  // entries
-      const int kp = ds_padded(a.k);
-      int* e_id = reinterpret_cast<int*>(ds_smem + (size_t)a.slots * a.slot_bytes) + team * 8 * kp;
-      float *e_p = reinterpret_cast<float*>(e_id + 2 * kp), *e_lp = e_p + 2 * kp, *e_z = e_lp + 2 * kp;
+    const int kp = ds_padded(a.k);
+    int* e_id = reinterpret_cast<int*>(ds_smem + (size_t)a.slots * a.slot_bytes) + team * 8 * kp;
+    float *e_p = reinterpret_cast<float*>(e_id + 2 * kp), *e_lp = e_p + 2 * kp, *e_z = e_lp + 2 * kp;
+    if (warp == WARPS) {  // gets entries ready
+      // A row's entries come in two steps of memory, tokens and then their logits; the first is taken a row ahead of the second.
+      constexpr int AHEAD = 2;  // entries a lane that are held meanwhile
+      int next_id[AHEAD], next_label = -1;
+      float next_t[AHEAD], next_w = 0.f;
+      auto ask = [&](long long r) {
+        if (r >= a.rows) return;
+        next_label = ds_label(a, r);
+        next_w = a.weight ? a.weight[r] : 1.f;
+#pragma unroll
+        for (int e = 0; e < AHEAD; ++e) next_id[e] = lane + 32 * e < a.k ? ds_entry(a, r, lane + 32 * e, next_t[e]) : -1;
+      };
       auto prepare = [&](long long r, int at) {
         int* id = e_id + at * kp;
         float *p = e_p + at * kp, *lp = e_lp + at * kp, *ze = e_z + at * kp;
         const T* z = (const T*)a.Z + r * a.ldz;
-        const int label = ds_label(a, r);
-        const bool use = (a.weight ? a.weight[r] : 1.f) != 0.f;
+        const bool use = next_w != 0.f;
+        const float zl = use && next_label >= 0 ? ds_f32(z[next_label]) : 0.f;
         float m = -INFINITY;
         int live = 0;
-        for (int i = lane; i < kp; i += 32) {
-          float tv = 0.f;
-          const int j = i < a.k ? ds_entry(a, r, i, tv) : -1;
+        auto entry = [&](int i, int j, float tv, float zj) {
           id[i] = j;
           lp[i] = tv;
           p[i] = 0.f;
-          ze[i] = use && j >= 0 ? ds_f32(z[j]) : 0.f;
+          ze[i] = zj;
           if (j >= 0) live = 1, m = tv != tv ? tv : fmaxf(m, tv);
+        };
+        float zj[AHEAD];
+#pragma unroll
+        for (int e = 0; e < AHEAD; ++e) zj[e] = use && next_id[e] >= 0 ? ds_f32(z[next_id[e]]) : 0.f;
+#pragma unroll
+        for (int e = 0; e < AHEAD; ++e)
+          if (lane + 32 * e < kp) entry(lane + 32 * e, next_id[e], next_t[e], zj[e]);
+        for (int i = lane + 32 * AHEAD; i < kp; i += 32) {
+          float tv = 0.f;
+          const int j = i < a.k ? ds_entry(a, r, i, tv) : -1;
+          entry(i, j, tv, use && j >= 0 ? ds_f32(z[j]) : 0.f);
         }
         live = __any_sync(0xFFFFFFFFu, live);
         m = lanes_max<32>(m);
@@ -500,22 +550,31 @@ __global__ void __launch_bounds__(TEAMS * (WORKERS + 32) + 32, 1) distill_ring_k
           if (id[i] >= 0) p[i] /= s, lp[i] -= log_s;
         if (lane == 0) {
           tm.soft[at] = live ? a.soft : 0.f;
-          tm.label_z[at] = use && label >= 0 ? ds_f32(z[label]) : 0.f;
+          tm.label_z[at] = zl;
+          tm.w[at] = next_w;
+          tm.label[at] = next_label;
         }
         __syncwarp();
       };
+      int n = 0;
+      ask(r1);
+      if (r1 < a.rows) prepare(r1, 0);
+      for (long long r = r1; r < a.rows; r += step, ++n) {
+        ask(r + step);
+        ds_meet(come, WORKERS + 64);
+        if (r + step < a.rows) prepare(r + step, ~n & 1);
+      }
+    } else if (warp == WARPS + 1) {  // writes them
       double sum_loss = 0.0;
       int n = 0;
-      if (r1 < a.rows) prepare(r1, 0);
       for (long long r = r1; r < a.rows; r += step, ++n) {
         const int at = n & 1;
         const int* id = e_id + at * kp;
         const float *p = e_p + at * kp, *lp = e_lp + at * kp, *ze = e_z + at * kp;
-        ds_meet(come, WORKERS + 32);
-        const float w = a.weight ? a.weight[r] : 1.f;
-        const int label = ds_label(a, r);
-        if (r + step < a.rows) prepare(r + step, at ^ 1);
+        ds_tell(come, WORKERS + 64);  // the row before is done with: its entries' place may be taken
         ds_meet(gone, WORKERS + 32);
+        const float w = tm.w[at];
+        const int label = tm.label[at];
         const float hard = label >= 0 ? a.hard : 0.f, soft = tm.soft[at];
         if (w == 0.f || (hard == 0.f && soft == 0.f)) {
           if (rank == 0 && lane == 0) a.loss[r] = 0.f;
@@ -542,7 +601,7 @@ __global__ void __launch_bounds__(TEAMS * (WORKERS + 32) + 32, 1) distill_ring_k
                 share += oi.z == j ? op.z : 0.f;
                 share += oi.w == j ? op.w : 0.f;
               }
-            dz[j] = ds_from<T>(fmaf(-w, (j == label ? hard : 0.f) + soft * a.tau * share, f.at<TWO>(i < a.k ? ze[i] : zl)));
+            dz[j] = ds_from<T>(fmaf(-w, (j == label ? hard : 0.f) + soft * a.tau * share, f.at<MODE>(i < a.k ? ze[i] : zl)));
           }
         }
         if (rank == 0) {
@@ -585,9 +644,7 @@ __global__ void __launch_bounds__(TEAMS * (WORKERS + 32) + 32, 1) distill_ring_k
         if (!info.skip) {
 #pragma unroll 4
           for (int i = tw; i < mine; i += WORKERS) {
-            const DsVec<T> x(zs[i]);
-            x.add(s2, m, c1);
-            if (TWO) x.add(u2, m, a.c_tau);
+            DsVec<T>(zs[i]).template add<MODE>(s2, u2, m, c1, a.c_tau);
           }
           s2.x += ds_exp2((edge - m) * c1);  // fmaxf passes NaN over; the sums do not
           if (TWO) u2.x += ds_exp2((edge - m) * a.c_tau);
@@ -603,7 +660,7 @@ __global__ void __launch_bounds__(TEAMS * (WORKERS + 32) + 32, 1) distill_ring_k
             if (TWO) tm.red_u[at][warp] = u;
           }
         }
-        ds_meet(come, WORKERS + 32);
+        ds_meet(come, WORKERS + 64);
         m = tm.red_m[at][0];
 #pragma unroll
         for (int i = 1; i < WARPS; ++i) m = fmaxf(m, tm.red_m[at][i]);
@@ -642,8 +699,8 @@ __global__ void __launch_bounds__(TEAMS * (WORKERS + 32) + 32, 1) distill_ring_k
           const bool same = ((reinterpret_cast<uintptr_t>(z) ^ reinterpret_cast<uintptr_t>(dz)) & 15u) == 0;
           T* out = dz + row.head + (long long)v0 * VEC;
 #pragma unroll 4
-          for (int i = tw; i < mine; i += WORKERS) ds_put<T, TWO>(f, zs[i], out + i * VEC, same);
-          if (edged) dz[row.loose_at(tw)] = ds_from<T>(f.at<TWO>(edge));
+          for (int i = tw; i < mine; i += WORKERS) ds_put<T, MODE>(f, zs[i], out + i * VEC, same);
+          if (edged) dz[row.loose_at(tw)] = ds_from<T>(f.at<MODE>(edge));
         }
         fence_proxy_async_smem();  // what was read from the slot, before the next copy into it
         __syncwarp();
@@ -659,11 +716,11 @@ __global__ void __launch_bounds__(TEAMS * (WORKERS + 32) + 32, 1) distill_ring_k
 }
 
 template <typename T, int LANES, bool WIDE, int NV>
-ard_status ds_lanes(ard_ctx* ctx, const DsArgs& a, bool two, cudaStream_t s) {
+ard_status ds_lanes(ard_ctx* ctx, const DsArgs& a, int mode, cudaStream_t s) {
   const int per = DS_SHORT_THREADS / LANES;
   const long long want = ((long long)a.rows + per - 1) / per, room = 8ll * ctx->sm_count;
   const dim3 grid((unsigned)(want < room ? want : room));
-  ARD_CUDA_OK(ard_launch(ctx, two ? distill_lanes_kernel<T, LANES, WIDE, NV, true> : distill_lanes_kernel<T, LANES, WIDE, NV, false>, grid,
+  ARD_CUDA_OK(ard_launch(ctx, mode ? distill_lanes_kernel<T, LANES, WIDE, NV, 1> : distill_lanes_kernel<T, LANES, WIDE, NV, 0>, grid,
                          dim3(DS_SHORT_THREADS), 0, s, a));
   ctx->launches++;
   ARD_CUDA_OK(cudaGetLastError());
@@ -679,9 +736,12 @@ int ds_slots(long long vecs, int k, int parts) {
   return slot > 0 ? (int)((DS_ROOM - TEAMS * 32ll * ds_padded(k)) / slot) : DS_SLOTS;
 }
 template <typename T, int WORKERS, int TEAMS>
-ard_status ds_ring(ard_ctx* ctx, DsArgs a, bool two, int parts, cudaStream_t s) {
-  constexpr int THREADS = TEAMS * (WORKERS + 32) + 32;
-  auto kern = two ? distill_ring_kernel<T, WORKERS, TEAMS, true> : distill_ring_kernel<T, WORKERS, TEAMS, false>;
+ard_status ds_ring(ard_ctx* ctx, DsArgs a, int mode, int parts, cudaStream_t s) {
+  constexpr int THREADS = TEAMS * (WORKERS + 64) + 32;
+  auto kern = mode == 0   ? distill_ring_kernel<T, WORKERS, TEAMS, 0>
+              : mode == 1 ? distill_ring_kernel<T, WORKERS, TEAMS, 1>
+              : mode == 2 ? distill_ring_kernel<T, WORKERS, TEAMS, 2>
+                          : distill_ring_kernel<T, WORKERS, TEAMS, 3>;
   const long long vecs = (long long)a.V * (int)sizeof(T) / 16;
   a.slice = (int)((vecs + parts - 1) / parts);
   a.slot_bytes = a.slice > 0 ? (a.slice * 16 + 127) / 128 * 128 : 128;
@@ -700,21 +760,26 @@ ard_status ds_ring(ard_ctx* ctx, DsArgs a, bool two, int parts, cudaStream_t s) 
 }
 
 template <typename T>
-ard_status ds_launch(ard_ctx* ctx, const DsArgs& a, bool two, cudaStream_t s) {
+ard_status ds_launch(ard_ctx* ctx, const DsArgs& a, int mode, cudaStream_t s) {
   constexpr int VEC = 16 / (int)sizeof(T);
-  if (a.V <= 32 && a.k <= 8 * DS_SHORT_ENTRIES) return ds_lanes<T, 8, false, 4>(ctx, a, two, s);
+  // as few lanes a row as hold it and the teacher's entries: what a row needs once costs a warp the same for one row as for four
+  if (a.k <= 8 * DS_SHORT_ENTRIES) {
+    if (a.V <= 32) return ds_lanes<T, 8, false, 4>(ctx, a, mode, s);
+    if (a.V <= 128) return ds_lanes<T, 8, false, 16>(ctx, a, mode, s);
+    if (a.V <= 8 * 8 * VEC) return ds_lanes<T, 8, true, 8>(ctx, a, mode, s);
+  }
   if (a.k <= 32 * DS_SHORT_ENTRIES) {
-    if (a.V <= 128) return ds_lanes<T, 32, false, 4>(ctx, a, two, s);
-    if (a.V <= 32 * 2 * VEC) return ds_lanes<T, 32, true, 2>(ctx, a, two, s);
-    if (a.V <= 32 * 4 * VEC) return ds_lanes<T, 32, true, 4>(ctx, a, two, s);
-    if (a.V <= 32 * 8 * VEC) return ds_lanes<T, 32, true, 8>(ctx, a, two, s);
+    if (a.V <= 128) return ds_lanes<T, 32, false, 4>(ctx, a, mode, s);
+    if (a.V <= 32 * 4 * VEC) return ds_lanes<T, 32, true, 4>(ctx, a, mode, s);
+    if (a.V <= 32 * 8 * VEC) return ds_lanes<T, 32, true, 8>(ctx, a, mode, s);
+    if (a.V <= 32 * 16 * VEC) return ds_lanes<T, 32, true, 16>(ctx, a, mode, s);
   }
   // four teams where the ring holds a row for each and one on its way, else two, with rows cut over as few CTAs as that takes
   const long long vecs = (long long)a.V / VEC;
-  if (ds_slots<4>(vecs, a.k, 1) >= 5) return ds_ring<T, 192, 4>(ctx, a, two, 1, s);
+  if (ds_slots<4>(vecs, a.k, 1) >= 5) return ds_ring<T, 160, 4>(ctx, a, mode, 1, s);
   int parts = 1;
   while (parts < DS_PARTS && ds_slots<2>(vecs, a.k, parts) < 3) parts *= 2;
-  return ds_ring<T, 256, 2>(ctx, a, two, parts, s);
+  return ds_ring<T, 256, 2>(ctx, a, mode, parts, s);
 }
 
 }  // namespace
@@ -739,6 +804,6 @@ ard_status launch_distill_loss(ard_ctx* ctx, ard_dtype dtype, int rows, int V, c
   a.weight = weight, a.loss = loss, a.total = total, a.dZ = dZ, a.status = ctx->d_status;
   a.partial = (double*)ctx->d_sk_ws;
   a.count = (unsigned int*)ctx->d_sk_cnt;
-  const bool two = a.hard != 0.f && a.soft != 0.f && tau != 1.f;
-  return dtype == ARD_F32 ? ds_launch<float>(ctx, a, two, s) : ds_launch<__nv_bfloat16>(ctx, a, two, s);
+  const int mode = a.hard == 0.f || a.soft == 0.f || tau == 1.f ? 0 : tau == 2.f ? 2 : tau == 4.f ? 3 : 1;
+  return dtype == ARD_F32 ? ds_launch<float>(ctx, a, mode, s) : ds_launch<__nv_bfloat16>(ctx, a, mode, s);
 }

@@ -78,11 +78,12 @@ SIZES = [(BF16, 3, 1), (F32, 64, 10), (BF16, 33, 32), (BF16, 40, 33), (F32, 9, 1
 
 
 @pytest.mark.parametrize("dtype,rows,V", SIZES)
-@pytest.mark.parametrize("kind", ["labels", "teacher", "both", "both_tau"])
+@pytest.mark.parametrize("kind", ["labels", "teacher", "both", "both_tau", "both_2", "both_4"])
 def test_sizes(dtype, rows, V, kind):
     ctx = Ctx()
     how = {"labels": dict(k=0), "teacher": dict(k=min(5, 2 * V), tau=3.0, hard=0.0, soft=1.0), "both": dict(k=16, tau=1.0, hard=0.5, soft=0.25),
-           "both_tau": dict(k=70, tau=0.7, hard=0.3, soft=0.6)}[kind]
+           "both_tau": dict(k=70, tau=0.7, hard=0.3, soft=0.6), "both_2": dict(k=3, tau=2.0, hard=0.4, soft=0.6),
+           "both_4": dict(k=130, tau=4.0, hard=0.4, soft=0.6)}[kind]
     case = Case(dtype, rows, V, pad=V % 3, off=V % 5, **how)
     z = host(case.z)[:, :V]
     case.call(ctx)
