@@ -129,6 +129,8 @@ __global__ void __launch_bounds__(EB_THREADS, 1) embedding_bwd_kernel(const int3
   const int group = blockIdx.x % groups, c0 = (blockIdx.x / groups) * EB_COLS;
   const int tokens = (V - group - 1) / groups + 1;
   for (int i = t; i < (tokens + 31) / 32; i += EB_THREADS) sh.seen[i] = 0u;
+  using Raw = typename EmRaw<4 * sizeof(T)>::type;
+  const bool full = VEC && c0 + EB_COLS <= n;
   const bool tail = n - c0 <= EB_COLS;  // the columns behind the last kept unit's period are its own too
 
   // One token's sum to the gradient.
@@ -191,23 +193,30 @@ __global__ void __launch_bounds__(EB_THREADS, 1) embedding_bwd_kernel(const int3
       bool front = open_front;
       for (int i0 = from; i0 < to; i0 += EB_AHEAD) {
         float x[EB_AHEAD][4];
+        if (full) {  // all loads before the first use
+          Raw q[EB_AHEAD];
 #pragma unroll
-        for (int u = 0; u < EB_AHEAD; ++u) {
-          const int i = min(i0 + u, to - 1);
-          const T* src = dY + (size_t)sh.row[sh.key[i] & (EB_LIST - 1)] * lddy + c0;
-          if (VEC && c0 + 4 * lane + 3 < n) {
-            typename EmRaw<4 * sizeof(T)>::type q = *reinterpret_cast<const typename EmRaw<4 * sizeof(T)>::type*>(src + 4 * lane);
+          for (int u = 0; u < EB_AHEAD; ++u)
+            q[u] = *reinterpret_cast<const Raw*>(dY + (size_t)sh.row[sh.key[min(i0 + u, to - 1)] & (EB_LIST - 1)] * lddy + c0 + 4 * lane);
+#pragma unroll
+          for (int u = 0; u < EB_AHEAD; ++u) {
             T e[4];
-            memcpy(e, &q, sizeof(q));
+            memcpy(e, &q[u], sizeof(Raw));
 #pragma unroll
             for (int k = 0; k < 4; ++k) x[u][k] = em_f32(e[k]);
-          } else {
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              const int c = EbCols<T, VEC>::col(lane, k);
-              x[u][k] = c0 + c < n ? em_f32(src[c]) : 0.f;
-            }
           }
+        } else {
+          T e[EB_AHEAD][4];
+#pragma unroll
+          for (int u = 0; u < EB_AHEAD; ++u) {
+            const T* src = dY + (size_t)sh.row[sh.key[min(i0 + u, to - 1)] & (EB_LIST - 1)] * lddy + c0;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) e[u][k] = src[min(EbCols<T, VEC>::col(lane, k), n - 1 - c0)];  // (beyond them: nobody asks)
+          }
+#pragma unroll
+          for (int u = 0; u < EB_AHEAD; ++u)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) x[u][k] = em_f32(e[u][k]);
         }
 #pragma unroll
         for (int u = 0; u < EB_AHEAD; ++u) {
