@@ -52,6 +52,16 @@ CASES = [
     (BF16, 16385, 1, 64, (1, 1), 0, 0, "any", True),
     (BF16, 200, 300000, 16, (1, 1), 0, 0, "any", False),
     (BF16, 0, 40, 24, (1, 1), 0, 0, "any", False),
+    # few tokens: some clusters of CTAs, one token each
+    (BF16, 50000, 3, 24, (1, 1), 0, 0, "padded", False),
+    (F32, 5000, 2, 300, (1, 1), 1, 1, "any", True),
+    (BF16, 9000, 5, 1000, (3, 2), 8, 0, "zipf", False),
+    (F32, 3000, 7, 4, (1, 1), 0, 0, "any", False),
+    (BF16, 3, 2, 8, (1, 1), 0, 0, "any", False),
+    (BF16, 0, 2, 130, (2, 1), 0, 0, "any", False),
+    # tokens of more than one digit of the sort, lists that fill up several times
+    (BF16, 30000, 9000, 1500, (1, 1), 0, 0, "any", False),
+    (F32, 30000, 200000, 136, (1, 1), 0, 0, "zipf", True),
 ]
 
 
