@@ -21,6 +21,22 @@ from . import ard
 BF, F32 = torch.bfloat16, torch.float32
 
 
+def adamw_entries(parameters, state_bits):
+    """Entries for `ard.adamw_tensors` from (parameter, gradient, bf16 copy or None, decay), with states that begin as zeros."""
+    rows = []
+    for p, g, w, decay in parameters:
+        r, c = p.shape if p.dim() == 2 else (1, p.numel())
+        row = dict(rows=r, cols=c, p=p, g=g, w=w, weight_decay=decay)
+        if state_bits == 8:
+            blocks = -(-r * c // ard.ARD_ADAMW_BLOCK)
+            row.update(m=torch.zeros(r * c, dtype=torch.uint8, device="cuda"), v=torch.zeros(r * c, dtype=torch.uint8, device="cuda"),
+                       m_scale=torch.zeros(blocks, dtype=F32, device="cuda"), v_scale=torch.zeros(blocks, dtype=F32, device="cuda"))
+        else:
+            row.update(m=torch.zeros(r * c, dtype=F32, device="cuda"), v=torch.zeros(r * c, dtype=F32, device="cuda"))
+        rows.append(row)
+    return rows
+
+
 class GlrLayer:
     def __init__(self, ctx, pat, in_pat, T, B, I, H, W, bias, norm_weight, norm_bias, eps=1e-5):
         """pat: row pattern over the H units (K_dim I); in_pat: that of the layer below over its I units, or None.  W: [3H][I], blocks f | g | o along the
@@ -143,16 +159,5 @@ class GlrLayer:
 
     def adamw_rows(self, weight_decay=0.0, state_bits=32):
         """The layer's entries for `ard.adamw_tensors`, with states that begin as zeros; the decay is the weight's alone.  The caller keeps the list."""
-        rows = []
-        for p, g, w, decay in ((self.p_W, self.dW, self.W, weight_decay), (self.p_b, self.db, None, 0.0), (self.p_nw, self.dnw, None, 0.0),
-                               (self.p_nb, self.dnb, None, 0.0)):
-            r, c = p.shape if p.dim() == 2 else (1, p.numel())
-            row = dict(rows=r, cols=c, p=p, g=g, w=w, weight_decay=decay)
-            if state_bits == 8:
-                blocks = -(-r * c // ard.ARD_ADAMW_BLOCK)
-                row.update(m=torch.zeros(r * c, dtype=torch.uint8, device="cuda"), v=torch.zeros(r * c, dtype=torch.uint8, device="cuda"),
-                           m_scale=torch.zeros(blocks, dtype=F32, device="cuda"), v_scale=torch.zeros(blocks, dtype=F32, device="cuda"))
-            else:
-                row.update(m=torch.zeros(r * c, dtype=F32, device="cuda"), v=torch.zeros(r * c, dtype=F32, device="cuda"))
-            rows.append(row)
-        return rows
+        return adamw_entries(((self.p_W, self.dW, self.W, weight_decay), (self.p_b, self.db, None, 0.0), (self.p_nw, self.dnw, None, 0.0),
+                              (self.p_nb, self.dnb, None, 0.0)), state_bits)

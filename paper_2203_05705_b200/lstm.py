@@ -35,6 +35,14 @@ class LstmLayer:
         """X: bf16 [T][B][I]."""
         self.XH[:self.T, :, :self.I] = X
 
+    def load_tokens(self, ids, table, alpha=1.0):
+        """ids: int32 [T][B] (negative: padding, a row of zeros), table: bf16 [V][I]: x_t = alpha * table[ids[t]], written where the kernels read it."""
+        T, B, I = self.T, self.B, self.I
+        for name, v, shape, dtype in (("ids", ids, (T, B), torch.int32), ("table", table, (table.shape[0], I), self.XH.dtype)):
+            if tuple(v.shape) != shape or v.dtype != dtype or v.device != self.XH.device or not v.is_contiguous():
+                raise ValueError("%s has to be contiguous %s %s on %s, got %s %s on %s" % (name, dtype, shape, self.XH.device, v.dtype, tuple(v.shape), v.device))
+        ard.ard_embedding_fwd(self.ctx, None, ard.ARD_BF16, T * B, table.shape[0], I, alpha, ids, table, I, self.XH, self.KH)
+
     def forward(self, alpha):
         ard.ard_lstm_forward(self.ctx, self.pat, self.T, self.B, self.I, self.H, alpha, self.XH, self.W, self.KH,
                              None, self.C, self.G, self.Z)
@@ -86,12 +94,13 @@ class LstmStack:
             ard.ard_pattern_destroy(p)
 
     def forward(self, X, alphas):
-        """X: bf16 [T][B][I0].  Returns Yc of the top layer ([T*B][H], first n_keep columns valid, unscaled)."""
+        """X: bf16 [T][B][I0], or None: what layers[0].load_tokens left there.  Returns Yc of the top layer ([T*B][H], first n_keep columns valid, unscaled)."""
         ctx, T, B = self.ctx, self.T, self.B
         for l, ly in enumerate(self.layers):
             I, H, KH = ly.I, ly.H, ly.KH
             if l == 0:
-                ly.load_inputs(X)
+                if X is not None:
+                    ly.load_inputs(X)
                 ard.ard_lstm_forward(ctx, ly.pat, T, B, I, H, 1.0, ly.XH, ly.W, KH, None, ly.C, ly.G, ly.Z)
             else:
                 # input half over the kept outputs of the layer below: both operands compact
