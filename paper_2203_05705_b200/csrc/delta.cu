@@ -250,11 +250,16 @@ struct DlPrepShared {
       bf k[DL_CHUNK][DK + 8], q[DL_CHUNK][DK + 8];
     };
     struct {
-      float t[DL_CHUNK][DL_LDA];  // the inverse, with ones on the diagonal
-      float tmp[3][16][17];
+      float a[DL_CHUNK][DL_LDA];  // A, below the diagonal
+      union {
+        bf p[3][DL_CHUNK][DL_LD64];
+        struct {
+          float t[DL_CHUNK][DL_LDA];  // the inverse, with ones on the diagonal
+          float tmp[3][16][17];
+        };
+      };
     };
   };
-  float a[DL_CHUNK][DL_LDA];  // A, below the diagonal
   DlRow row;
 };
 
@@ -283,7 +288,7 @@ __device__ __forceinline__ void dl_inverse_blocks(Sh& sh, int er, int ec) {
 }
 
 template <int DK>
-__global__ void __launch_bounds__(DL_THREADS) delta_prep_kernel(const DlArgs a) {
+__global__ void __launch_bounds__(DL_THREADS, 4) delta_prep_kernel(const DlArgs a) {
   extern __shared__ __align__(16) uint8_t dl_smem[];
   auto& sh = *reinterpret_cast<DlPrepShared<DK>*>(dl_smem);
   pdl_launch_dependents();
@@ -363,7 +368,7 @@ __global__ void __launch_bounds__(DL_THREADS) delta_prep_kernel(const DlArgs a) 
     const int m0 = (warp < 4 ? warp : 7 - warp) * 16;
     const bool keys = warp < 4;
     dl_product<1, 8, false, false, 1, 1, 0>(c, keys ? &sh.k[0][0] : &sh.q[0][0], DK + 8, 0, &sh.k[0][0], DK + 8, 0, m0, 0, 0, DK, lane);
-    bf* P = a.p + u.unit * 3 * DL_SQ;
+    __syncthreads();  // q and k have been read: A and P lie where they were
     const int bi = m0 >> 4;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
@@ -385,13 +390,20 @@ __global__ void __launch_bounds__(DL_THREADS) delta_prep_kernel(const DlArgs a) 
             if (bj > bi || jj > i) x[e] = 0.f;
             if (keys) sh.a[i][jj] = x[e];
           }
-          if (!keys) dl_put<3>(P + i * DL_CHUNK + j, DL_SQ, x[0], x[1]);
+          if (!keys) dl_put<3>(&sh.p[0][i][j], DL_CHUNK * DL_LD64, x[0], x[1]);
         }
       }
     }
   }
   __syncthreads();
-  // the inverse: blocks of 16 on the diagonal by substitution, then those below it (q and k have been read: it lies where they were)
+  {
+    bf* P = a.p + u.unit * 3 * DL_SQ;
+#pragma unroll
+    for (int i = t; i < 3 * DL_CHUNK * 8; i += DL_THREADS)
+      *reinterpret_cast<uint4*>(P + i * 8) = *reinterpret_cast<const uint4*>(&sh.p[0][0][0] + (i >> 3) * DL_LD64 + (i & 7) * 8);
+  }
+  __syncthreads();
+  // the inverse, where P was: blocks of 16 on the diagonal by substitution, then those below it
   if (t < DL_CHUNK) {
     const int b0 = t & ~15, j = t & 15;
     float x[16];
@@ -1052,10 +1064,9 @@ struct DlGradShared {
 // two parts in memory.
 template <int DK, int DV>
 __device__ __forceinline__ float dl_load_state(bf* s, const float* g, int Dk, int Dv, int vec, const bf* with, int rows) {
-  constexpr int LD = DK + 8, QUADS = DK / 4, MINE = DV * QUADS / DL_GRAD_THREADS, AHEAD = MINE < 4 ? MINE : 4;
+  constexpr int LD = DK + 8, QUADS = DK / 4, MINE = DV * QUADS / DL_GRAD_THREADS, AHEAD = MINE;  // all of them at once: nothing else is held yet
   static_assert(MINE % AHEAD == 0, "whole rounds");
   float dot = 0.f;
-#pragma unroll
   for (int i0 = 0; i0 < MINE; i0 += AHEAD) {
     float4 x[AHEAD];
     uint2 hi[AHEAD], lo[AHEAD];
