@@ -432,15 +432,22 @@ __global__ void __launch_bounds__(DL_THREADS, 4) delta_prep_kernel(const DlArgs 
 }
 
 // ---- from chunk to chunk ----------------------------------------------------------------------------
-// A warp holds 16 columns of the state, transposed, as accumulators [16 columns][DK].  As rows of a left operand they lie in registers the way a product wants them, and so do
-// the results that follow from them: E' = S' K', R' = b (V' - g E'), U' = R' T', S' += U' K.  Nothing of this goes through shared memory, which holds what all columns
-// share (K, Q, T, P), two chunks deep.  Beside each such warp stands one that does what nobody waits for: forward the outputs, which take the state's and U's parts over
-// shared memory, backward what comes from dY alone.
+// Two warps hold 16 columns of the state, transposed, as accumulators [16 columns][DK / 2]: one the first half of its rows, one the second.  As rows of a left operand they lie
+// in registers the way a product wants them, and so do the results that follow from them: E' = S' K', R' = b (V' - g E'), U' = R' T', S' += U' K.  Of a chunk's 64 steps each of the two
+// finishes 32; they meet three times a chunk, for the sums E, for what the earlier steps' R says to the later ones, and for U.  What all columns share (K, Q, T, P) lies in shared memory.
+// Beside each two stands a warp that fetches the next chunk and does what nobody waits for: forward the outputs, which take the state's and U's parts over shared
+// memory, backward what comes from dY alone.  (A warp to 16 columns, with all of the state: 217 / 260 us for 2048 x 8 x 8 in place of 150 / 190: the chain of a chunk's products is twice as
+// long, and a scheduler has one of them.)
 // Some of a CTA's warps, in branches of their own (0: all of them).
 __device__ __forceinline__ void dl_meet(int id, int threads) {
   __syncwarp();
   asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory");
 }
+__device__ __forceinline__ void dl_tell(int id, int threads) {  // who need not wait
+  __syncwarp();
+  asm volatile("bar.arrive %0, %1;" ::"r"(id), "r"(threads) : "memory");
+}
+__device__ __forceinline__ void dl_take(const uint4& q, uint32_t (&a)[4]) { a[0] = q.x, a[1] = q.y, a[2] = q.z, a[3] = q.w; }
 __device__ __forceinline__ uint32_t dl_transposed(uint32_t x) {  // of 8 x 8 bf16, a pair a lane
   uint32_t r;
   asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
@@ -519,16 +526,17 @@ __device__ __forceinline__ void dl_store2(bf* p, float x, float y, bool two) {
     if (two) p[1] = __float2bfloat16_rn(y);
   }
 }
-// Sixteen columns of a chunk, [16][64] in accumulators, to rows of bf16; x times by[step] where by is given.
-__device__ __forceinline__ void dl_rows_out(const float (&x)[8][4], const float* by, bf* g, long long step, int live, int cols, int lane) {
+// Sixteen columns of a chunk's steps r0 .. r0 + 8 N - 1, in accumulators [16][8 N], to rows of bf16; x times by[step] where by is given.
+template <int N>
+__device__ __forceinline__ void dl_rows_out(const float (&x)[N][4], const float* by, bf* g, long long step, int r0, int live, int cols, int lane) {
 #pragma unroll
-  for (int n = 0; n < 8; ++n) {
+  for (int n = 0; n < N; ++n) {
     float2 m = make_float2(1.f, 1.f);
-    if (by) m = *reinterpret_cast<const float2*>(by + 8 * n + 2 * (lane & 3));
+    if (by) m = *reinterpret_cast<const float2*>(by + r0 + 8 * n + 2 * (lane & 3));
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       const uint32_t w = dl_transposed(dl_pack(x[n][2 * h] * m.x, x[n][2 * h + 1] * m.y));
-      const int r = 8 * n + (lane >> 2), c = 8 * h + 2 * (lane & 3);
+      const int r = r0 + 8 * n + (lane >> 2), c = 8 * h + 2 * (lane & 3);
       if (r >= live || c >= cols) continue;
       bf* p = g + r * step + c;
       if (c + 1 < cols && (reinterpret_cast<uintptr_t>(p) & 3u) == 0) {
@@ -549,95 +557,101 @@ __device__ __forceinline__ void dl_zero_rows(bf* g, long long step, int from, in
 
 template <int DK, int NP>
 struct DlScanShared {
-  bf k[2][DL_CHUNK][DK + 8], q[2][DL_CHUNK][DK + 8];
-  bf tri[2][3][DL_CHUNK][DL_LD64];
-  bf p[2][2][DL_CHUNK][DL_LD64];
-  bf v[2][DL_CHUNK][NP * 16 + 8];
+  bf k[2][DL_CHUNK][DK + 8], q[DL_CHUNK][DK + 8];
+  bf tri[3][DL_CHUNK][DL_LD64];
+  bf p[2][DL_CHUNK][DL_LD64];
+  bf v[DL_CHUNK][NP * 16 + 8];
   uint4 s[NP][DK / 16][2][32];  // the state's parts as left operands
   uint4 u[NP][4][2][32];        // U's
+  uint4 us[NP][4][3][32];       // those of U G_C / |k|
+  uint4 r[NP][2][3][32];        // the earlier steps' R
+  float4 e[NP][2][4][32];       // what a half of the state gives to the other half's steps
   DlSteps row[2];
 };
 
 template <int DK, int NP>
-__global__ void __launch_bounds__(64 * NP, 1) delta_scan_kernel(const DlArgs a) {
-  constexpr int LDK = DK + 8, LDV = NP * 16 + 8, PT = DL_CHUNK * DL_LD64, HELP = 32 * NP;
+__global__ void __launch_bounds__(96 * NP, 1) delta_scan_kernel(const DlArgs a) {
+  constexpr int LDK = DK + 8, LDV = NP * 16 + 8, PT = DL_CHUNK * DL_LD64, HELP = 32 * NP, ALL = 96 * NP, HALF = DK / 2;
   extern __shared__ __align__(16) uint8_t dl_smem[];
   auto& sh = *reinterpret_cast<DlScanShared<DK, NP>*>(dl_smem);
   pdl_launch_dependents();
   pdl_wait_prior_grids();
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, pair = warp % NP;
-  const bool helper = warp >= NP;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, pair = warp % NP, half = warp / NP;  // half 2: the helper
+  const int states = 1 + pair, updates = 1 + NP + pair, early = 1 + 2 * NP + pair, helpers = 1 + 3 * NP;  // barriers
   const int blocks = (a.Dv + NP * 16 - 1) / (NP * 16);
   const long long n = blockIdx.x / blocks, size = (long long)a.Dk * a.Dv, heads = (long long)a.B * a.heads;
   const int c0 = (int)(blockIdx.x % blocks) * NP * 16, cols = min(NP * 16, a.Dv - c0);  // the CTA's columns
-  const int mine = min(max(cols - 16 * pair, 0), 16);                                    // the pair's
+  const int mine = min(max(cols - 16 * pair, 0), 16);                                    // the three warps'
   const DlUnit u0 = dl_unit(a, 0, n);
   const int len = a.lens ? min(max(a.lens[u0.b], 0), a.T) : a.T, chunks = (len + DL_CHUNK - 1) / DL_CHUNK;
   const bf *Q = a.Q + (long long)u0.head * a.Dk, *K = a.K + (long long)u0.head * a.Dk, *V = a.V + (long long)u0.head * a.Dv + c0;
   bf* Y = a.Y + (long long)u0.head * a.Dv + c0;
-  auto fetch = [&](int chunk) {  // by the helpers
-    if (chunk < chunks) {
+  if (half == 2) {
+    const int t = threadIdx.x - 2 * HELP;
+    auto fetch_k = [&](int chunk) {
+      if (chunk >= chunks) return;
       const DlUnit u = dl_unit(a, chunk, n);
-      const int at = chunk & 1, t = threadIdx.x - HELP;
-      dl_load<DK, HELP>(&sh.k[at][0][0], LDK, K + u.row0 * a.ldk, a.B * a.ldk, u.live, a.Dk, a.vec_k, t);
-      dl_load<DK, HELP>(&sh.q[at][0][0], LDK, Q + u.row0 * a.ldq, a.B * a.ldq, u.live, a.Dk, a.vec_q, t);
-      dl_load<NP * 16, HELP>(&sh.v[at][0][0], LDV, V + u.row0 * a.ldv, a.B * a.ldv, u.live, cols, a.vec_v, t);
-      dl_load64<3, HELP>(&sh.tri[at][0][0][0], a.tri + u.unit * 3 * DL_SQ, t);
-      dl_load64<2, HELP>(&sh.p[at][0][0][0], a.p + u.unit * 3 * DL_SQ, t);
-      dl_load_row(sh.row[at], a.row + u.unit * DL_ROW_FLOATS, t, HELP);
-    }
+      dl_load<DK, HELP>(&sh.k[chunk & 1][0][0], LDK, K + u.row0 * a.ldk, a.B * a.ldk, u.live, a.Dk, a.vec_k, t);
+      dl_load_row(sh.row[chunk & 1], a.row + u.unit * DL_ROW_FLOATS, t, HELP);
+    };
+    auto fetch_others = [&](int chunk) {
+      if (chunk >= chunks) return;
+      const DlUnit u = dl_unit(a, chunk, n);
+      dl_load<DK, HELP>(&sh.q[0][0], LDK, Q + u.row0 * a.ldq, a.B * a.ldq, u.live, a.Dk, a.vec_q, t);
+      dl_load<NP * 16, HELP>(&sh.v[0][0], LDV, V + u.row0 * a.ldv, a.B * a.ldv, u.live, cols, a.vec_v, t);
+      dl_load64<3, HELP>(&sh.tri[0][0][0], a.tri + u.unit * 3 * DL_SQ, t);
+    };
+    fetch_k(0);
+    fetch_others(0);
     dl_commit();
-  };
-  if (helper) {
-    fetch(0);
     for (int chunk = 0; chunk < chunks; ++chunk) {
       const int at = chunk & 1;
       dl_wait<0>();
-      dl_meet(0, 64 * NP);
-      fetch(chunk + 1);
-      dl_meet(1 + pair, 64);  // the state's parts are there
+      dl_meet(0, ALL);
+      fetch_k(chunk + 1);
+      dl_load64<2, HELP>(&sh.p[0][0][0], a.p + (chunk * heads + n) * 3 * DL_SQ, t);
+      dl_commit();
+      dl_meet(states, 96);
       float o[8][4] = {};
 #pragma unroll
       for (int kd = 0; kd < DK / 16; ++kd) {
         uint32_t s[2][4];
 #pragma unroll
-        for (int p = 0; p < 2; ++p) {
-          const uint4 x = sh.s[pair][kd][p][lane];
-          s[p][0] = x.x, s[p][1] = x.y, s[p][2] = x.z, s[p][3] = x.w;
-        }
-        dl_step<0, 4, 2, 1, 1, false>(o, s, &sh.q[at][0][0], LDK, 0, 16 * kd, lane);
+        for (int p = 0; p < 2; ++p) dl_take(sh.s[pair][kd][p][lane], s[p]);
+        dl_step<0, 4, 2, 1, 1, false>(o, s, &sh.q[0][0], LDK, 0, 16 * kd, lane);
       }
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const float2 g = *reinterpret_cast<const float2*>(&sh.row[at].qin[8 * i + 2 * (lane & 3)]);
         o[i][0] *= g.x, o[i][1] *= g.y, o[i][2] *= g.x, o[i][3] *= g.y;
       }
-      dl_meet(1 + NP + pair, 64);  // U's are
+      dl_meet(updates, 96);
+      dl_wait<0>();
+      dl_meet(helpers, HELP);  // P is there, and nobody reads Q, V and T any more
+      fetch_others(chunk + 1);
+      dl_commit();
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
         uint32_t x[2][4];
 #pragma unroll
-        for (int p = 0; p < 2; ++p) {
-          const uint4 y = sh.u[pair][k][p][lane];
-          x[p][0] = y.x, x[p][1] = y.y, x[p][2] = y.z, x[p][3] = y.w;
-        }
-        dl_later<2, 2, 1, false>(k, o, x, &sh.p[at][0][0][0], DL_LD64, PT, lane);
+        for (int p = 0; p < 2; ++p) dl_take(sh.u[pair][k][p][lane], x[p]);
+        dl_later<2, 2, 1, false>(k, o, x, &sh.p[0][0][0], DL_LD64, PT, lane);
       }
       const DlUnit u = dl_unit(a, chunk, n);
-      dl_rows_out(o, nullptr, Y + u.row0 * a.ldy + 16 * pair, a.B * a.ldy, u.live, mine, lane);
+      dl_rows_out<8>(o, nullptr, Y + u.row0 * a.ldy + 16 * pair, a.B * a.ldy, 0, u.live, mine, lane);
     }
   } else {
-    float s[DK / 8][4];
+    float s[DK / 16][4];
+    const int d0 = half * HALF;  // this warp's rows of the state, and steps 32 half .. 32 half + 31 of a chunk
     const float* h0 = a.h0 ? a.h0 + n * size + c0 + 16 * pair : nullptr;
-    dl_state<DK>(lane, [&](int i, int e, int d, int c) { s[i][e] = h0 && d < a.Dk && c < mine ? h0[(long long)d * a.Dv + c] : 0.f; });
-    auto put = [&](float* g) { dl_state<DK>(lane, [&](int i, int e, int d, int c) { if (d < a.Dk && c < mine) g[(long long)d * a.Dv + c] = s[i][e]; }); };
+    dl_state<HALF>(lane, [&](int i, int e, int d, int c) { s[i][e] = h0 && d0 + d < a.Dk && c < mine ? h0[(long long)(d0 + d) * a.Dv + c] : 0.f; });
     const bool even = a.Dk % 2 == 0 && (reinterpret_cast<uintptr_t>(a.S) & 7u) == 0;
     auto keep = [&](float* g) {  // for the backward call: transposed, as it lies here
 #pragma unroll
-      for (int i = 0; i < DK / 8; ++i)
+      for (int i = 0; i < DK / 16; ++i)
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          const int d = 8 * i + 2 * (lane & 3), c = (lane >> 2) + 8 * h;
+          const int d = d0 + 8 * i + 2 * (lane & 3), c = (lane >> 2) + 8 * h;
           if (d >= a.Dk || c >= mine) continue;
           float* p = g + c * a.Dk + d;
           if (even) {
@@ -649,144 +663,184 @@ __global__ void __launch_bounds__(64 * NP, 1) delta_scan_kernel(const DlArgs a) 
         }
     };
     for (int chunk = 0; chunk < chunks; ++chunk) {
-      const int at = chunk & 1;
-      const DlSteps& row = sh.row[at];
+      const DlSteps& row = sh.row[chunk & 1];
+      const bf* k0 = &sh.k[chunk & 1][0][0];
+      const bf* tri = &sh.tri[0][0][0] + half * 32 * DL_LD64;  // this warp's steps
       if (a.S) keep(a.S + (chunk * heads + n) * size + (long long)(c0 + 16 * pair) * a.Dk);
-      dl_meet(0, 64 * NP);
-      float e[8][4] = {};
+      dl_meet(0, ALL);
+      float r[4][4];
+      {
+        float e[8][4] = {};
 #pragma unroll
-      for (int kd = 0; kd < DK / 16; ++kd) {
-        uint32_t x[3][4];
-        dl_left<3>(s[2 * kd], s[2 * kd + 1], x);
-        sh.s[pair][kd][0][lane] = make_uint4(x[0][0], x[0][1], x[0][2], x[0][3]);
-        sh.s[pair][kd][1][lane] = make_uint4(x[1][0], x[1][1], x[1][2], x[1][3]);
-        dl_step<0, 4, 3, 1, 2, false>(e, x, &sh.k[at][0][0], LDK, 0, 16 * kd, lane);
-      }
-      dl_meet(1 + pair, 64);
+        for (int kd = 0; kd < DK / 32; ++kd) {
+          uint32_t x[3][4];
+          dl_left<3>(s[2 * kd], s[2 * kd + 1], x);
+          sh.s[pair][half * (DK / 32) + kd][0][lane] = make_uint4(x[0][0], x[0][1], x[0][2], x[0][3]);
+          sh.s[pair][half * (DK / 32) + kd][1][lane] = make_uint4(x[1][0], x[1][1], x[1][2], x[1][3]);
+          dl_step<0, 4, 3, 1, 2, false>(e, x, k0, LDK, 0, d0 + 16 * kd, lane);
+        }
+        // each half of the state adds to all steps; a warp has the sums of its own
 #pragma unroll
-      for (int i = 0; i < 8; i += 2) {
-        uint32_t v[4];
-        dl_ldsm_t(v, &sh.v[at][8 * i + (lane & 7) + ((lane >> 4) << 3)][16 * pair + ((lane >> 3) & 1) * 8]);
+        for (int i = 0; i < 4; ++i) {
+          const float(&give)[4] = e[i + 4], (&give0)[4] = e[i];
+          sh.e[pair][half][i][lane] = half ? make_float4(give0[0], give0[1], give0[2], give0[3]) : make_float4(give[0], give[1], give[2], give[3]);
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          const int r = 8 * (i + j) + 2 * (lane & 3);
-          const float2 b = *reinterpret_cast<const float2*>(&row.beta[r]), g = *reinterpret_cast<const float2*>(&row.kin[r]);
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const float2 x = dl_unpack(v[2 * j + h]);
-            e[i + j][2 * h] = b.x * fmaf(-g.x, e[i + j][2 * h], x.x);
-            e[i + j][2 * h + 1] = b.y * fmaf(-g.y, e[i + j][2 * h + 1], x.y);
-          }
+          for (int j = 0; j < 4; ++j) r[i][j] = half ? e[i + 4][j] : e[i][j];
         }
       }
-      float x[8][4] = {};
+      dl_meet(states, 96);
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        uint32_t r[3][4];
-        dl_left<3>(e[2 * k], e[2 * k + 1], r);
-        dl_later<3, 3, 2, false>(k, x, r, &sh.tri[at][0][0][0], DL_LD64, PT, lane);
+      for (int i = 0; i < 4; i += 2) {
+        uint32_t v[4];
+        dl_ldsm_t(v, &sh.v[32 * half + 8 * i + (lane & 7) + ((lane >> 4) << 3)][16 * pair + ((lane >> 3) & 1) * 8]);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const float4 o = sh.e[pair][half ^ 1][i + j][lane];
+          const int at = 32 * half + 8 * (i + j) + 2 * (lane & 3);
+          const float2 b = *reinterpret_cast<const float2*>(&row.beta[at]), g = *reinterpret_cast<const float2*>(&row.kin[at]), x0 = dl_unpack(v[2 * j]), x1 = dl_unpack(v[2 * j + 1]);
+          r[i + j][0] = b.x * fmaf(-g.x, r[i + j][0] + o.x, x0.x);
+          r[i + j][1] = b.y * fmaf(-g.y, r[i + j][1] + o.y, x0.y);
+          r[i + j][2] = b.x * fmaf(-g.x, r[i + j][2] + o.z, x1.x);
+          r[i + j][3] = b.y * fmaf(-g.y, r[i + j][3] + o.w, x1.y);
+        }
       }
+      float x[4][4] = {};
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
+      for (int k = 0; k < 2; ++k) {
+        uint32_t w[3][4];
+        dl_left<3>(r[2 * k], r[2 * k + 1], w);
+        if (half == 0)
+#pragma unroll
+          for (int p = 0; p < 3; ++p) sh.r[pair][k][p][lane] = make_uint4(w[p][0], w[p][1], w[p][2], w[p][3]);
+        if (k == 0) dl_step<0, 2, 3, 3, 2, false>(x, w, tri, DL_LD64, PT, 32 * half, lane);
+        else dl_step<1, 2, 3, 3, 2, false>(x, w, tri, DL_LD64, PT, 32 * half + 16, lane);
+      }
+      if (half == 0) {
+        dl_tell(early, 64);
+      } else {
+        dl_meet(early, 64);
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          uint32_t w[3][4];
+#pragma unroll
+          for (int p = 0; p < 3; ++p) dl_take(sh.r[pair][k][p][lane], w[p]);
+          dl_step<0, 2, 3, 3, 2, false>(x, w, tri, DL_LD64, PT, 16 * k, lane);
+        }
+      }
+      uint32_t own[2][3][4];
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
         uint32_t w[2][4];
         dl_left<2>(x[2 * k], x[2 * k + 1], w);
-        sh.u[pair][k][0][lane] = make_uint4(w[0][0], w[0][1], w[0][2], w[0][3]);
-        sh.u[pair][k][1][lane] = make_uint4(w[1][0], w[1][1], w[1][2], w[1][3]);
+#pragma unroll
+        for (int p = 0; p < 2; ++p) sh.u[pair][2 * half + k][p][lane] = make_uint4(w[p][0], w[p][1], w[p][2], w[p][3]);
+#pragma unroll
+        for (int i = 2 * k; i < 2 * k + 2; ++i) {
+          const float2 g = *reinterpret_cast<const float2*>(&row.kout[32 * half + 8 * i + 2 * (lane & 3)]);
+          x[i][0] *= g.x, x[i][1] *= g.y, x[i][2] *= g.x, x[i][3] *= g.y;
+        }
+        dl_left<3>(x[2 * k], x[2 * k + 1], own[k]);
+#pragma unroll
+        for (int p = 0; p < 3; ++p) sh.us[pair][2 * half + k][p][lane] = make_uint4(own[k][p][0], own[k][p][1], own[k][p][2], own[k][p][3]);
       }
-      dl_meet(1 + NP + pair, 64);
       const float whole = row.first[DL_CHUNK - 1];
 #pragma unroll
-      for (int i = 0; i < DK / 8; ++i)
+      for (int i = 0; i < DK / 16; ++i)
 #pragma unroll
         for (int j = 0; j < 4; ++j) s[i][j] *= whole;
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
+      for (int k = 0; k < 2; ++k) dl_step<0, DK / 32, 3, 1, 2, true>(s, own[k], k0 + d0, LDK, 0, 32 * half + 16 * k, lane);
+      dl_meet(updates, 96);
 #pragma unroll
-        for (int i = 2 * k; i < 2 * k + 2; ++i) {
-          const float2 g = *reinterpret_cast<const float2*>(&row.kout[8 * i + 2 * (lane & 3)]);
-          x[i][0] *= g.x, x[i][1] *= g.y, x[i][2] *= g.x, x[i][3] *= g.y;
-        }
+      for (int k = 0; k < 2; ++k) {
         uint32_t w[3][4];
-        dl_left<3>(x[2 * k], x[2 * k + 1], w);
-        dl_step<0, 4, 3, 1, 2, true>(s, w, &sh.k[at][0][0], LDK, 0, 16 * k, lane);
-        if constexpr (DK > 64) dl_step<4, 8, 3, 1, 2, true>(s, w, &sh.k[at][0][0], LDK, 0, 16 * k, lane);
+#pragma unroll
+        for (int p = 0; p < 3; ++p) dl_take(sh.us[pair][2 * (half ^ 1) + k][p][lane], w[p]);
+        dl_step<0, DK / 32, 3, 1, 2, true>(s, w, k0 + d0, LDK, 0, 32 * (half ^ 1) + 16 * k, lane);
       }
     }
-    if (a.hT) put(a.hT + n * size + c0 + 16 * pair);
+    if (a.hT) dl_state<HALF>(lane, [&](int i, int e, int d, int c) { if (d0 + d < a.Dk && c < mine) a.hT[n * size + (long long)(d0 + d) * a.Dv + c0 + 16 * pair + c] = s[i][e]; });
   }
   for (int chunk = len / DL_CHUNK; chunk * DL_CHUNK < a.T; ++chunk) {
     const DlUnit u = dl_unit(a, chunk, n);
-    dl_zero_rows(Y + u.row0 * a.ldy, a.B * a.ldy, u.live, min(DL_CHUNK, a.T - chunk * DL_CHUNK), cols, threadIdx.x, 64 * NP);
+    dl_zero_rows(Y + u.row0 * a.ldy, a.B * a.ldy, u.live, min(DL_CHUNK, a.T - chunk * DL_CHUNK), cols, threadIdx.x, ALL);
   }
 }
 
 // The adjoint: F' = D' K', dU' = G' + G_C F', X' = dU' T, D' = g_C D' + Y' + W' K with W = -g b X; the helpers bring G = scale P^T dY and Y = Q^T (scale g dY), which come
-// from the chunk alone.  P, which only they read, and only at first, is fetched behind its last use.
+// from the chunk alone.
 template <int DK, int NP>
 struct DlBackShared {
-  bf k[2][DL_CHUNK][DK + 8], q[2][DL_CHUNK][DK + 8];
-  bf tri[2][3][DL_CHUNK][DL_LD64];
+  bf k[2][DL_CHUNK][DK + 8], q[DL_CHUNK][DK + 8];
+  bf tri[3][DL_CHUNK][DL_LD64];
   bf p[3][DL_CHUNK][DL_LD64];
-  bf dy[2][DL_CHUNK][NP * 16 + 8];
+  bf dy[DL_CHUNK][NP * 16 + 8];
   float4 g[NP][8][32];
   float4 y[NP][DK / 8][32];
+  uint4 w[NP][4][3][32];   // W's parts as left operands
+  uint4 r[NP][2][3][32];   // the later steps' dU
+  float4 e[NP][2][4][32];
   DlSteps row[2];
 };
 
 template <int DK, int NP>
-__global__ void __launch_bounds__(64 * NP, 1) delta_back_kernel(const DlArgs a) {
-  constexpr int LDK = DK + 8, LDV = NP * 16 + 8, PT = DL_CHUNK * DL_LD64, HELP = 32 * NP;
+__global__ void __launch_bounds__(96 * NP, 1) delta_back_kernel(const DlArgs a) {
+  constexpr int LDK = DK + 8, LDV = NP * 16 + 8, PT = DL_CHUNK * DL_LD64, HELP = 32 * NP, ALL = 96 * NP, HALF = DK / 2;
   extern __shared__ __align__(16) uint8_t dl_smem[];
   auto& sh = *reinterpret_cast<DlBackShared<DK, NP>*>(dl_smem);
   pdl_launch_dependents();
   pdl_wait_prior_grids();
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, pair = warp % NP;
-  const bool helper = warp >= NP;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, pair = warp % NP, half = warp / NP;
+  const int states = 1 + pair, updates = 1 + NP + pair, late = 1 + 2 * NP + pair, helpers = 1 + 3 * NP;
   const int blocks = (a.Dv + NP * 16 - 1) / (NP * 16);
-  const long long n = blockIdx.x / blocks, size = (long long)a.Dk * a.Dv;
+  const long long n = blockIdx.x / blocks, size = (long long)a.Dk * a.Dv, heads = (long long)a.B * a.heads;
   const int c0 = (int)(blockIdx.x % blocks) * NP * 16, cols = min(NP * 16, a.Dv - c0);
   const int mine = min(max(cols - 16 * pair, 0), 16);
   const DlUnit u0 = dl_unit(a, 0, n);
   const int len = a.lens ? min(max(a.lens[u0.b], 0), a.T) : a.T, chunks = (len + DL_CHUNK - 1) / DL_CHUNK;
   const bf *Q = a.Q + (long long)u0.head * a.Dk, *K = a.K + (long long)u0.head * a.Dk, *dY = a.dY + (long long)u0.head * a.Dv + c0;
   bf* dV = a.dV + (long long)u0.head * a.Dv + c0;
-  if (helper) {
-    const int t = threadIdx.x - HELP;
-    auto fetch = [&](int chunk) {
-      if (chunk >= 0) {
-        const DlUnit u = dl_unit(a, chunk, n);
-        const int at = chunk & 1;
-        dl_load<DK, HELP>(&sh.k[at][0][0], LDK, K + u.row0 * a.ldk, a.B * a.ldk, u.live, a.Dk, a.vec_k, t);
-        dl_load<DK, HELP>(&sh.q[at][0][0], LDK, Q + u.row0 * a.ldq, a.B * a.ldq, u.live, a.Dk, a.vec_q, t);
-        dl_load<NP * 16, HELP>(&sh.dy[at][0][0], LDV, dY + u.row0 * a.lddy, a.B * a.lddy, u.live, cols, a.vec_dy, t);
-        dl_load64<3, HELP>(&sh.tri[at][0][0][0], a.tri + u.unit * 3 * DL_SQ, t);
-        dl_load_row(sh.row[at], a.row + u.unit * DL_ROW_FLOATS, t, HELP);
-      }
+  if (half == 2) {
+    const int t = threadIdx.x - 2 * HELP;
+    auto fetch_k = [&](int chunk) {
+      if (chunk < 0) return;
+      const DlUnit u = dl_unit(a, chunk, n);
+      dl_load<DK, HELP>(&sh.k[chunk & 1][0][0], LDK, K + u.row0 * a.ldk, a.B * a.ldk, u.live, a.Dk, a.vec_k, t);
+      dl_load_row(sh.row[chunk & 1], a.row + u.unit * DL_ROW_FLOATS, t, HELP);
     };
-    auto fetch_p = [&](int chunk) {
-      if (chunk >= 0) dl_load64<3, HELP>(&sh.p[0][0][0], a.p + dl_unit(a, chunk, n).unit * 3 * DL_SQ, t);
+    auto fetch_p = [&](int chunk) {  // what the first stage reads
+      if (chunk < 0) return;
+      const DlUnit u = dl_unit(a, chunk, n);
+      dl_load<NP * 16, HELP>(&sh.dy[0][0], LDV, dY + u.row0 * a.lddy, a.B * a.lddy, u.live, cols, a.vec_dy, t);
+      dl_load64<3, HELP>(&sh.p[0][0][0], a.p + u.unit * 3 * DL_SQ, t);
     };
-    fetch(chunks - 1);
+    auto fetch_others = [&](int chunk) {
+      if (chunk < 0) return;
+      const DlUnit u = dl_unit(a, chunk, n);
+      dl_load<DK, HELP>(&sh.q[0][0], LDK, Q + u.row0 * a.ldq, a.B * a.ldq, u.live, a.Dk, a.vec_q, t);
+      dl_load64<3, HELP>(&sh.tri[0][0][0], a.tri + u.unit * 3 * DL_SQ, t);
+    };
+    fetch_k(chunks - 1);
     fetch_p(chunks - 1);
+    fetch_others(chunks - 1);
     dl_commit();
     for (int chunk = chunks - 1; chunk >= 0; --chunk) {
       const int at = chunk & 1;
       dl_wait<0>();
-      dl_meet(0, 64 * NP);
-      fetch(chunk - 1);
+      dl_meet(0, ALL);
+      fetch_k(chunk - 1);
       uint32_t y[4][1][4];  // dY' as a left operand
 #pragma unroll
-      for (int k = 0; k < 4; ++k) dl_a<true>(y[k][0], &sh.dy[at][0][0], LDV, 16 * pair, 16 * k, lane);
+      for (int k = 0; k < 4; ++k) dl_a<true>(y[k][0], &sh.dy[0][0], LDV, 16 * pair, 16 * k, lane);
       {
         float g[8][4] = {};
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
-          dl_earlier<1, 3, 2, true>(k, g, y[k], &sh.p[0][0][0], DL_LD64, PT, lane);
+        for (int k = 0; k < 4; ++k) dl_earlier<1, 3, 2, true>(k, g, y[k], &sh.p[0][0][0], DL_LD64, PT, lane);
 #pragma unroll
         for (int i = 0; i < 8; ++i) sh.g[pair][i][lane] = make_float4(g[i][0], g[i][1], g[i][2], g[i][3]);
       }
-      dl_meet(1 + pair, 64);
-      dl_meet(1 + 2 * NP, HELP);  // all of them have read P
+      dl_meet(states, 96);
+      dl_meet(helpers, HELP);  // all of them have read P and dY
       fetch_p(chunk - 1);
       dl_commit();
       float s[DK / 8][4] = {};
@@ -803,54 +857,121 @@ __global__ void __launch_bounds__(64 * NP, 1) delta_back_kernel(const DlArgs a) 
 #pragma unroll
           for (int p = 0; p < 3; ++p) x[p][i] = w[p];
         }
-        dl_step<0, 4, 3, 1, 2, true>(s, x, &sh.q[at][0][0], LDK, 0, 16 * k, lane);
-        if constexpr (DK > 64) dl_step<4, 8, 3, 1, 2, true>(s, x, &sh.q[at][0][0], LDK, 0, 16 * k, lane);
+        dl_step<0, 4, 3, 1, 2, true>(s, x, &sh.q[0][0], LDK, 0, 16 * k, lane);
+        if constexpr (DK > 64) dl_step<4, 8, 3, 1, 2, true>(s, x, &sh.q[0][0], LDK, 0, 16 * k, lane);
       }
 #pragma unroll
       for (int i = 0; i < DK / 8; ++i) sh.y[pair][i][lane] = make_float4(s[i][0], s[i][1], s[i][2], s[i][3]);
-      dl_meet(1 + NP + pair, 64);
+      dl_meet(updates, 96);
+      dl_meet(helpers, HELP);  // nobody reads Q and T any more
+      fetch_others(chunk - 1);
+      dl_commit();
     }
   } else {
-    float s[DK / 8][4];
+    float s[DK / 16][4];
+    const int d0 = half * HALF;
     const float* last = a.dhT ? a.dhT + n * size + c0 + 16 * pair : nullptr;
-    dl_state<DK>(lane, [&](int i, int e, int d, int c) { s[i][e] = last && d < a.Dk && c < mine ? last[(long long)d * a.Dv + c] : 0.f; });
+    dl_state<HALF>(lane, [&](int i, int e, int d, int c) { s[i][e] = last && d0 + d < a.Dk && c < mine ? last[(long long)(d0 + d) * a.Dv + c] : 0.f; });
     const bool here = c0 + 16 * pair < a.ldx;  // the work's rows end with 64 or 128 columns
     for (int chunk = chunks - 1; chunk >= 0; --chunk) {
-      const int at = chunk & 1;
-      const DlSteps& row = sh.row[at];
+      const DlSteps& row = sh.row[chunk & 1];
+      const bf* k0 = &sh.k[chunk & 1][0][0];
+      const bf* tri = &sh.tri[0][0][0] + half * 32;  // this warp's steps
       const DlUnit u = dl_unit(a, chunk, n);
-      dl_meet(0, 64 * NP);
-      float f[8][4] = {};
-      bf* D = a.d + u.unit * 2 * DK * a.ldx + (long long)(c0 + 16 * pair) * DK;
+      dl_meet(0, ALL);
+      float r[4][4];
+      {
+        float f[8][4] = {};
+        bf* D = a.d + u.unit * 2 * DK * a.ldx + (long long)(c0 + 16 * pair) * DK + d0;
 #pragma unroll
-      for (int kd = 0; kd < DK / 16; ++kd) {
-        uint32_t x[3][4];
-        dl_left<3>(s[2 * kd], s[2 * kd + 1], x);
+        for (int kd = 0; kd < DK / 32; ++kd) {
+          uint32_t x[3][4];
+          dl_left<3>(s[2 * kd], s[2 * kd + 1], x);
+          if (here)
 #pragma unroll
-        for (int p = 0; p < 2; ++p)
+            for (int p = 0; p < 2; ++p)
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
-            if (here) *reinterpret_cast<uint32_t*>(D + (p * a.ldx + 8 * (i & 1) + (lane >> 2)) * DK + 16 * kd + 8 * (i >> 1) + 2 * (lane & 3)) = x[p][i];
-        dl_step<0, 4, 3, 1, 2, false>(f, x, &sh.k[at][0][0], LDK, 0, 16 * kd, lane);
+              for (int i = 0; i < 4; ++i) *reinterpret_cast<uint32_t*>(D + (p * a.ldx + 8 * (i & 1) + (lane >> 2)) * DK + 16 * kd + 8 * (i >> 1) + 2 * (lane & 3)) = x[p][i];
+          dl_step<0, 4, 3, 1, 2, false>(f, x, k0, LDK, 0, d0 + 16 * kd, lane);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float(&give)[4] = f[i + 4], (&give0)[4] = f[i];
+          sh.e[pair][half][i][lane] = half ? make_float4(give0[0], give0[1], give0[2], give0[3]) : make_float4(give[0], give[1], give[2], give[3]);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) r[i][j] = half ? f[i + 4][j] : f[i][j];
+        }
       }
-      dl_meet(1 + pair, 64);
+      dl_meet(states, 96);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float4 g = sh.g[pair][i][lane];
-        const float2 l = *reinterpret_cast<const float2*>(&row.kout[8 * i + 2 * (lane & 3)]);
-        f[i][0] = fmaf(l.x, f[i][0], g.x), f[i][1] = fmaf(l.y, f[i][1], g.y), f[i][2] = fmaf(l.x, f[i][2], g.z), f[i][3] = fmaf(l.y, f[i][3], g.w);
+      for (int i = 0; i < 4; ++i) {
+        const float4 o = sh.e[pair][half ^ 1][i][lane], g = sh.g[pair][4 * half + i][lane];
+        const float2 l = *reinterpret_cast<const float2*>(&row.kout[32 * half + 8 * i + 2 * (lane & 3)]);
+        r[i][0] = fmaf(l.x, r[i][0] + o.x, g.x), r[i][1] = fmaf(l.y, r[i][1] + o.y, g.y), r[i][2] = fmaf(l.x, r[i][2] + o.z, g.z), r[i][3] = fmaf(l.y, r[i][3] + o.w, g.w);
       }
-      float x[8][4] = {};
+      float x[4][4] = {};
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        uint32_t r[3][4];
-        dl_left<3>(f[2 * k], f[2 * k + 1], r);
-        dl_earlier<3, 3, 2, true>(k, x, r, &sh.tri[at][0][0][0], DL_LD64, PT, lane);
+      for (int k = 0; k < 2; ++k) {
+        uint32_t w[3][4];
+        dl_left<3>(r[2 * k], r[2 * k + 1], w);
+        if (half == 1)
+#pragma unroll
+          for (int p = 0; p < 3; ++p) sh.r[pair][k][p][lane] = make_uint4(w[p][0], w[p][1], w[p][2], w[p][3]);
+        if (k == 0) dl_step<0, 1, 3, 3, 2, true>(x, w, tri, DL_LD64, PT, 32 * half, lane);
+        else dl_step<0, 2, 3, 3, 2, true>(x, w, tri, DL_LD64, PT, 32 * half + 16, lane);
       }
-      dl_rows_out(x, row.beta, dV + u.row0 * a.lddv + 16 * pair, a.B * a.lddv, u.live, mine, lane);
+      if (half == 1) {
+        dl_tell(late, 64);
+      } else {
+        dl_meet(late, 64);
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          uint32_t w[3][4];
+#pragma unroll
+          for (int p = 0; p < 3; ++p) dl_take(sh.r[pair][k][p][lane], w[p]);
+          dl_step<0, 2, 3, 3, 2, true>(x, w, tri, DL_LD64, PT, 32 + 16 * k, lane);
+        }
+      }
+      uint32_t own[2][3][4];
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        float m[2][4];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const int at = 32 * half + 8 * (2 * k + i) + 2 * (lane & 3);
+          const float2 b = *reinterpret_cast<const float2*>(&row.beta[at]), g = *reinterpret_cast<const float2*>(&row.kin[at]);
+          const float(&v)[4] = x[2 * k + i];
+          m[i][0] = v[0] * -b.x * g.x, m[i][1] = v[1] * -b.y * g.y, m[i][2] = v[2] * -b.x * g.x, m[i][3] = v[3] * -b.y * g.y;
+        }
+        dl_left<3>(m[0], m[1], own[k]);
+#pragma unroll
+        for (int p = 0; p < 3; ++p) sh.w[pair][2 * half + k][p][lane] = make_uint4(own[k][p][0], own[k][p][1], own[k][p][2], own[k][p][3]);
+      }
+      const float whole = row.first[DL_CHUNK - 1];
+#pragma unroll
+      for (int i = 0; i < DK / 16; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) s[i][j] *= whole;
+#pragma unroll
+      for (int k = 0; k < 2; ++k) dl_step<0, DK / 32, 3, 1, 2, true>(s, own[k], k0 + d0, LDK, 0, 32 * half + 16 * k, lane);
+      dl_meet(updates, 96);
+#pragma unroll
+      for (int i = 0; i < DK / 16; ++i) {
+        const float4 y = sh.y[pair][half * (DK / 16) + i][lane];
+        s[i][0] += y.x, s[i][1] += y.y, s[i][2] += y.z, s[i][3] += y.w;
+      }
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        uint32_t w[3][4];
+#pragma unroll
+        for (int p = 0; p < 3; ++p) dl_take(sh.w[pair][2 * (half ^ 1) + k][p][lane], w[p]);
+        dl_step<0, DK / 32, 3, 1, 2, true>(s, w, k0 + d0, LDK, 0, 32 * (half ^ 1) + 16 * k, lane);
+      }
+      // nobody waits for these
+      dl_rows_out<4>(x, row.beta, dV + u.row0 * a.lddv + 16 * pair, a.B * a.lddv, 32 * half, u.live, mine, lane);
       bf* X = a.x + u.unit * 2 * DL_CHUNK * a.ldx + c0 + 16 * pair;
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
+      for (int i = 0; i < 4; ++i)
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           uint32_t w[2];
@@ -858,35 +979,15 @@ __global__ void __launch_bounds__(64 * NP, 1) delta_back_kernel(const DlArgs a) 
 #pragma unroll
           for (int p = 0; p < 2; ++p) {
             const uint32_t y = dl_transposed(w[p]);
-            if (here) *reinterpret_cast<uint32_t*>(X + ((long long)p * DL_CHUNK + 8 * i + (lane >> 2)) * a.ldx + 8 * h + 2 * (lane & 3)) = y;
+            if (here) *reinterpret_cast<uint32_t*>(X + (p * DL_CHUNK + 32 * half + 8 * i + (lane >> 2)) * a.ldx + 8 * h + 2 * (lane & 3)) = y;
           }
         }
-      dl_meet(1 + NP + pair, 64);
-      const float whole = row.first[DL_CHUNK - 1];
-#pragma unroll
-      for (int i = 0; i < DK / 8; ++i) {
-        const float4 y = sh.y[pair][i][lane];
-        s[i][0] = fmaf(whole, s[i][0], y.x), s[i][1] = fmaf(whole, s[i][1], y.y), s[i][2] = fmaf(whole, s[i][2], y.z), s[i][3] = fmaf(whole, s[i][3], y.w);
-      }
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-#pragma unroll
-        for (int i = 2 * k; i < 2 * k + 2; ++i) {
-          const int r = 8 * i + 2 * (lane & 3);
-          const float2 b = *reinterpret_cast<const float2*>(&row.beta[r]), g = *reinterpret_cast<const float2*>(&row.kin[r]);
-          x[i][0] *= -b.x * g.x, x[i][1] *= -b.y * g.y, x[i][2] *= -b.x * g.x, x[i][3] *= -b.y * g.y;
-        }
-        uint32_t w[3][4];
-        dl_left<3>(x[2 * k], x[2 * k + 1], w);
-        dl_step<0, 4, 3, 1, 2, true>(s, w, &sh.k[at][0][0], LDK, 0, 16 * k, lane);
-        if constexpr (DK > 64) dl_step<4, 8, 3, 1, 2, true>(s, w, &sh.k[at][0][0], LDK, 0, 16 * k, lane);
-      }
     }
-    if (a.dh0) dl_state<DK>(lane, [&](int i, int e, int d, int c) { if (d < a.Dk && c < mine) a.dh0[n * size + (long long)d * a.Dv + c0 + 16 * pair + c] = s[i][e]; });
+    if (a.dh0) dl_state<HALF>(lane, [&](int i, int e, int d, int c) { if (d0 + d < a.Dk && c < mine) a.dh0[n * size + (long long)(d0 + d) * a.Dv + c0 + 16 * pair + c] = s[i][e]; });
   }
   for (int chunk = len / DL_CHUNK; chunk * DL_CHUNK < a.T; ++chunk) {
     const DlUnit u = dl_unit(a, chunk, n);
-    dl_zero_rows(dV + u.row0 * a.lddv, a.B * a.lddv, u.live, min(DL_CHUNK, a.T - chunk * DL_CHUNK), cols, threadIdx.x, 64 * NP);
+    dl_zero_rows(dV + u.row0 * a.lddv, a.B * a.lddv, u.live, min(DL_CHUNK, a.T - chunk * DL_CHUNK), cols, threadIdx.x, ALL);
   }
 }
 
@@ -1447,8 +1548,8 @@ ard_status dl_run(ard_ctx* ctx, K kern, long long grid, int threads, size_t smem
 template <int DK, int NP>
 ard_status dl_scan(ard_ctx* ctx, const DlArgs& a, bool backward, cudaStream_t s) {
   const long long grid = (long long)a.B * a.heads * ((a.Dv + NP * 16 - 1) / (NP * 16));
-  return backward ? dl_run(ctx, delta_back_kernel<DK, NP>, grid, 64 * NP, sizeof(DlBackShared<DK, NP>), a, s)
-                  : dl_run(ctx, delta_scan_kernel<DK, NP>, grid, 64 * NP, sizeof(DlScanShared<DK, NP>), a, s);
+  return backward ? dl_run(ctx, delta_back_kernel<DK, NP>, grid, 96 * NP, sizeof(DlBackShared<DK, NP>), a, s)
+                  : dl_run(ctx, delta_scan_kernel<DK, NP>, grid, 96 * NP, sizeof(DlScanShared<DK, NP>), a, s);
 }
 template <int DK>
 ard_status dl_chunks(ard_ctx* ctx, const DlArgs& a, bool backward, cudaStream_t s) {
