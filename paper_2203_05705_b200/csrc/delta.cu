@@ -602,15 +602,18 @@ __global__ void __launch_bounds__(96 * NP, 1) delta_scan_kernel(const DlArgs a) 
       dl_load64<3, HELP>(&sh.tri[0][0][0], a.tri + u.unit * 3 * DL_SQ, t);
     };
     fetch_k(0);
+    dl_commit();
     fetch_others(0);
     dl_commit();
     for (int chunk = 0; chunk < chunks; ++chunk) {
       const int at = chunk & 1;
-      dl_wait<0>();
-      dl_meet(0, ALL);
+      dl_wait<1>();
+      dl_meet(0, ALL);  // K is there
       fetch_k(chunk + 1);
       dl_load64<2, HELP>(&sh.p[0][0][0], a.p + (chunk * heads + n) * 3 * DL_SQ, t);
       dl_commit();
+      dl_wait<1>();
+      dl_meet(helpers, HELP);  // Q, V and T are
       dl_meet(states, 96);
       float o[8][4] = {};
 #pragma unroll
@@ -743,6 +746,7 @@ __global__ void __launch_bounds__(96 * NP, 1) delta_scan_kernel(const DlArgs a) 
 #pragma unroll
         for (int p = 0; p < 3; ++p) sh.us[pair][2 * half + k][p][lane] = make_uint4(own[k][p][0], own[k][p][1], own[k][p][2], own[k][p][3]);
       }
+      dl_meet(updates, 96);
       const float whole = row.first[DL_CHUNK - 1];
 #pragma unroll
       for (int i = 0; i < DK / 16; ++i)
@@ -750,7 +754,6 @@ __global__ void __launch_bounds__(96 * NP, 1) delta_scan_kernel(const DlArgs a) 
         for (int j = 0; j < 4; ++j) s[i][j] *= whole;
 #pragma unroll
       for (int k = 0; k < 2; ++k) dl_step<0, DK / 32, 3, 1, 2, true>(s, own[k], k0 + d0, LDK, 0, 32 * half + 16 * k, lane);
-      dl_meet(updates, 96);
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
         uint32_t w[3][4];
@@ -822,13 +825,15 @@ __global__ void __launch_bounds__(96 * NP, 1) delta_back_kernel(const DlArgs a) 
     };
     fetch_k(chunks - 1);
     fetch_p(chunks - 1);
+    dl_commit();
     fetch_others(chunks - 1);
     dl_commit();
     for (int chunk = chunks - 1; chunk >= 0; --chunk) {
       const int at = chunk & 1;
-      dl_wait<0>();
-      dl_meet(0, ALL);
+      dl_wait<1>();
+      dl_meet(0, ALL);  // K, P and dY are there
       fetch_k(chunk - 1);
+      dl_commit();
       uint32_t y[4][1][4];  // dY' as a left operand
 #pragma unroll
       for (int k = 0; k < 4; ++k) dl_a<true>(y[k][0], &sh.dy[0][0], LDV, 16 * pair, 16 * k, lane);
@@ -839,8 +844,9 @@ __global__ void __launch_bounds__(96 * NP, 1) delta_back_kernel(const DlArgs a) 
 #pragma unroll
         for (int i = 0; i < 8; ++i) sh.g[pair][i][lane] = make_float4(g[i][0], g[i][1], g[i][2], g[i][3]);
       }
+      dl_wait<1>();
+      dl_meet(helpers, HELP);  // Q and T are there, and nobody reads P and dY any more
       dl_meet(states, 96);
-      dl_meet(helpers, HELP);  // all of them have read P and dY
       fetch_p(chunk - 1);
       dl_commit();
       float s[DK / 8][4] = {};
