@@ -605,16 +605,16 @@ __global__ void __launch_bounds__(96 * NP, 1) delta_scan_kernel(const DlArgs a) 
     dl_commit();
     fetch_others(0);
     dl_commit();
+    dl_wait<1>();
+    if (chunks > 0) dl_tell(0, ALL);  // K is there: nobody else waits for this warp, whose outputs may lag behind
     for (int chunk = 0; chunk < chunks; ++chunk) {
       const int at = chunk & 1;
-      dl_wait<1>();
-      dl_meet(0, ALL);  // K is there
+      dl_wait<0>();
+      dl_meet(helpers, HELP);  // Q, V and T are there, and nobody reads P any more
+      dl_meet(states, 96);     // nor, since all have gone on to this chunk, the keys before it
       fetch_k(chunk + 1);
       dl_load64<2, HELP>(&sh.p[0][0][0], a.p + (chunk * heads + n) * 3 * DL_SQ, t);
       dl_commit();
-      dl_wait<1>();
-      dl_meet(helpers, HELP);  // Q, V and T are
-      dl_meet(states, 96);
       float o[8][4] = {};
 #pragma unroll
       for (int kd = 0; kd < DK / 16; ++kd) {
@@ -630,7 +630,8 @@ __global__ void __launch_bounds__(96 * NP, 1) delta_scan_kernel(const DlArgs a) 
       }
       dl_meet(updates, 96);
       dl_wait<0>();
-      dl_meet(helpers, HELP);  // P is there, and nobody reads Q, V and T any more
+      dl_meet(helpers, HELP);  // P and the next keys are there, and nobody reads Q, V and T any more
+      if (chunk + 1 < chunks) dl_tell(0, ALL);
       fetch_others(chunk + 1);
       dl_commit();
 #pragma unroll
@@ -796,7 +797,7 @@ __global__ void __launch_bounds__(96 * NP, 1) delta_back_kernel(const DlArgs a) 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, pair = warp % NP, half = warp / NP;
   const int states = 1 + pair, updates = 1 + NP + pair, late = 1 + 2 * NP + pair, helpers = 1 + 3 * NP;
   const int blocks = (a.Dv + NP * 16 - 1) / (NP * 16);
-  const long long n = blockIdx.x / blocks, size = (long long)a.Dk * a.Dv, heads = (long long)a.B * a.heads;
+  const long long n = blockIdx.x / blocks, size = (long long)a.Dk * a.Dv;
   const int c0 = (int)(blockIdx.x % blocks) * NP * 16, cols = min(NP * 16, a.Dv - c0);
   const int mine = min(max(cols - 16 * pair, 0), 16);
   const DlUnit u0 = dl_unit(a, 0, n);
@@ -811,67 +812,78 @@ __global__ void __launch_bounds__(96 * NP, 1) delta_back_kernel(const DlArgs a) 
       dl_load<DK, HELP>(&sh.k[chunk & 1][0][0], LDK, K + u.row0 * a.ldk, a.B * a.ldk, u.live, a.Dk, a.vec_k, t);
       dl_load_row(sh.row[chunk & 1], a.row + u.unit * DL_ROW_FLOATS, t, HELP);
     };
-    auto fetch_p = [&](int chunk) {  // what the first stage reads
+    auto fetch_mine = [&](int chunk) {  // what the helpers read
       if (chunk < 0) return;
       const DlUnit u = dl_unit(a, chunk, n);
       dl_load<NP * 16, HELP>(&sh.dy[0][0], LDV, dY + u.row0 * a.lddy, a.B * a.lddy, u.live, cols, a.vec_dy, t);
       dl_load64<3, HELP>(&sh.p[0][0][0], a.p + u.unit * 3 * DL_SQ, t);
-    };
-    auto fetch_others = [&](int chunk) {
-      if (chunk < 0) return;
-      const DlUnit u = dl_unit(a, chunk, n);
       dl_load<DK, HELP>(&sh.q[0][0], LDK, Q + u.row0 * a.ldq, a.B * a.ldq, u.live, a.Dk, a.vec_q, t);
-      dl_load64<3, HELP>(&sh.tri[0][0][0], a.tri + u.unit * 3 * DL_SQ, t);
     };
-    fetch_k(chunks - 1);
-    fetch_p(chunks - 1);
-    dl_commit();
-    fetch_others(chunks - 1);
-    dl_commit();
-    for (int chunk = chunks - 1; chunk >= 0; --chunk) {
-      const int at = chunk & 1;
-      dl_wait<1>();
-      dl_meet(0, ALL);  // K, P and dY are there
-      fetch_k(chunk - 1);
-      dl_commit();
-      uint32_t y[4][1][4];  // dY' as a left operand
+    auto fetch_tri = [&](int chunk) {
+      if (chunk >= 0) dl_load64<3, HELP>(&sh.tri[0][0][0], a.tri + dl_unit(a, chunk, n).unit * 3 * DL_SQ, t);
+    };
+    // G to shared memory and Y to registers: a chunk ahead of the state
+    float y[DK / 8][4];
+    auto ahead = [&](int chunk) {
+      uint32_t dy[4][1][4];  // dY' as a left operand
 #pragma unroll
-      for (int k = 0; k < 4; ++k) dl_a<true>(y[k][0], &sh.dy[0][0], LDV, 16 * pair, 16 * k, lane);
+      for (int k = 0; k < 4; ++k) dl_a<true>(dy[k][0], &sh.dy[0][0], LDV, 16 * pair, 16 * k, lane);
       {
         float g[8][4] = {};
 #pragma unroll
-        for (int k = 0; k < 4; ++k) dl_earlier<1, 3, 2, true>(k, g, y[k], &sh.p[0][0][0], DL_LD64, PT, lane);
+        for (int k = 0; k < 4; ++k) dl_earlier<1, 3, 2, true>(k, g, dy[k], &sh.p[0][0][0], DL_LD64, PT, lane);
 #pragma unroll
         for (int i = 0; i < 8; ++i) sh.g[pair][i][lane] = make_float4(g[i][0], g[i][1], g[i][2], g[i][3]);
       }
-      dl_wait<1>();
-      dl_meet(helpers, HELP);  // Q and T are there, and nobody reads P and dY any more
-      dl_meet(states, 96);
-      fetch_p(chunk - 1);
-      dl_commit();
-      float s[DK / 8][4] = {};
+#pragma unroll
+      for (int i = 0; i < DK / 8; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) y[i][j] = 0.f;
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        const float2 m0 = *reinterpret_cast<const float2*>(&sh.row[at].qin[16 * k + 2 * (lane & 3)]), m1 = *reinterpret_cast<const float2*>(&sh.row[at].qin[16 * k + 8 + 2 * (lane & 3)]);
+        const float* by = &sh.row[chunk & 1].qin[16 * k + 2 * (lane & 3)];
+        const float2 m0 = *reinterpret_cast<const float2*>(by), m1 = *reinterpret_cast<const float2*>(by + 8);
         uint32_t x[3][4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const float2 v = dl_unpack(y[k][0][i]);
+          const float2 v = dl_unpack(dy[k][0][i]);
           const float2 m = i < 2 ? m0 : m1;
           uint32_t w[3];
           dl_split<3>(v.x * m.x, v.y * m.y, w);
 #pragma unroll
           for (int p = 0; p < 3; ++p) x[p][i] = w[p];
         }
-        dl_step<0, 4, 3, 1, 2, true>(s, x, &sh.q[0][0], LDK, 0, 16 * k, lane);
-        if constexpr (DK > 64) dl_step<4, 8, 3, 1, 2, true>(s, x, &sh.q[0][0], LDK, 0, 16 * k, lane);
+        dl_step<0, 4, 3, 1, 2, true>(y, x, &sh.q[0][0], LDK, 0, 16 * k, lane);
+        if constexpr (DK > 64) dl_step<4, 8, 3, 1, 2, true>(y, x, &sh.q[0][0], LDK, 0, 16 * k, lane);
       }
-#pragma unroll
-      for (int i = 0; i < DK / 8; ++i) sh.y[pair][i][lane] = make_float4(s[i][0], s[i][1], s[i][2], s[i][3]);
-      dl_meet(updates, 96);
-      dl_meet(helpers, HELP);  // nobody reads Q and T any more
-      fetch_others(chunk - 1);
+    };
+    if (chunks > 0) {
+      fetch_k(chunks - 1);
+      fetch_mine(chunks - 1);
+      fetch_tri(chunks - 1);
       dl_commit();
+      dl_wait<0>();
+      dl_meet(helpers, HELP);
+      dl_tell(0, ALL);  // K is there
+      ahead(chunks - 1);
+    }
+    for (int chunk = chunks - 1; chunk >= 0; --chunk) {
+      dl_wait<0>();
+      dl_meet(helpers, HELP);  // T is there, and nobody reads P, Q and dY any more
+      dl_meet(states, 96);     // nor, since all have gone on to this chunk, the keys behind it and the last Y
+#pragma unroll
+      for (int i = 0; i < DK / 8; ++i) sh.y[pair][i][lane] = make_float4(y[i][0], y[i][1], y[i][2], y[i][3]);
+      fetch_k(chunk - 1);
+      fetch_mine(chunk - 1);
+      dl_commit();
+      dl_meet(updates, 96);
+      dl_wait<0>();
+      dl_meet(helpers, HELP);  // the next keys, P, Q and dY are there, and nobody reads T any more
+      if (chunk == 0) break;
+      dl_tell(0, ALL);
+      fetch_tri(chunk - 1);
+      dl_commit();
+      ahead(chunk - 1);
     }
   } else {
     float s[DK / 16][4];
