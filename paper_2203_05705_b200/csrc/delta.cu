@@ -225,19 +225,24 @@ __device__ __forceinline__ void dl_load_row(Row& s, const float* g, int t, int o
 }
 
 struct DlUnit {
-  int chunk, b, head, live;  // live: steps of the chunk that are inside the sequence
-  long long n, unit, row0;   // sequence and head; its place in the work; row of the chunk's first step
+  int chunk, b, head, len, live;  // len: the sequence's steps; live: those of the chunk that are inside it
+  uint32_t n;                     // sequence and head
+  long long unit, row0;           // its place in the work; row of the chunk's first step
 };
-__device__ __forceinline__ DlUnit dl_unit(const DlArgs& a, int chunk, long long n) {
-  DlUnit u;
+// (Sequences times heads, and chunks times those, are below 2^31.)
+__device__ __forceinline__ void dl_move(const DlArgs& a, DlUnit& u, int chunk) {
   u.chunk = chunk;
-  u.n = n;
-  u.b = (int)(n / a.heads);
-  u.head = (int)(n - (long long)u.b * a.heads);
-  const int len = a.lens ? min(max(a.lens[u.b], 0), a.T) : a.T;
-  u.live = min(max(len - chunk * DL_CHUNK, 0), DL_CHUNK);
-  u.unit = (long long)chunk * a.B * a.heads + n;
+  u.live = min(max(u.len - chunk * DL_CHUNK, 0), DL_CHUNK);
+  u.unit = (long long)chunk * (a.B * a.heads) + u.n;
   u.row0 = (long long)chunk * DL_CHUNK * a.B + u.b;
+}
+__device__ __forceinline__ DlUnit dl_unit(const DlArgs& a, int chunk, uint32_t n) {
+  DlUnit u;
+  u.n = n;
+  u.b = (int)(n / (uint32_t)a.heads);
+  u.head = (int)(n - (uint32_t)u.b * (uint32_t)a.heads);
+  u.len = a.lens ? min(max(a.lens[u.b], 0), a.T) : a.T;
+  dl_move(a, u, chunk);
   return u;
 }
 
@@ -294,7 +299,7 @@ __global__ void __launch_bounds__(DL_THREADS, 4) delta_prep_kernel(const DlArgs 
   pdl_launch_dependents();
   pdl_wait_prior_grids();
   const int t = threadIdx.x, warp = t >> 5, lane = t & 31;
-  const long long units = (long long)a.B * a.heads;
+  const uint32_t units = (uint32_t)a.B * (uint32_t)a.heads;
   const DlUnit u = dl_unit(a, (int)(blockIdx.x / units), blockIdx.x % units);
   if (u.live == 0) return;  // nobody asks
   dl_load<DK, DL_THREADS>(&sh.k[0][0], DK + 8, a.K + u.row0 * a.ldk + (long long)u.head * a.Dk, a.B * a.ldk, u.live, a.Dk, a.vec_k, t);
@@ -529,23 +534,27 @@ __device__ __forceinline__ void dl_store2(bf* p, float x, float y, bool two) {
 // Sixteen columns of a chunk's steps r0 .. r0 + 8 N - 1, in accumulators [16][8 N], to rows of bf16; x times by[step] where by is given.
 template <int N>
 __device__ __forceinline__ void dl_rows_out(const float (&x)[N][4], const float* by, bf* g, long long step, int r0, int live, int cols, int lane) {
+  const int r = r0 + (lane >> 2), c = 2 * (lane & 3);
+  bf* p = g + r * step + c;
+  const bool pairs = ((reinterpret_cast<uintptr_t>(g) | (uintptr_t)(step * 2)) & 3u) == 0 && (cols & 1) == 0;  // both of two columns are there, on a grid of 4 bytes
 #pragma unroll
-  for (int n = 0; n < N; ++n) {
+  for (int n = 0; n < N; ++n, p += 8 * step) {
     float2 m = make_float2(1.f, 1.f);
     if (by) m = *reinterpret_cast<const float2*>(by + r0 + 8 * n + 2 * (lane & 3));
+    uint32_t w[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) w[h] = dl_transposed(dl_pack(x[n][2 * h] * m.x, x[n][2 * h + 1] * m.y));
+    if (r + 8 * n >= live) continue;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const uint32_t w = dl_transposed(dl_pack(x[n][2 * h] * m.x, x[n][2 * h + 1] * m.y));
-      const int r = r0 + 8 * n + (lane >> 2), c = 8 * h + 2 * (lane & 3);
-      if (r >= live || c >= cols) continue;
-      bf* p = g + r * step + c;
-      if (c + 1 < cols && (reinterpret_cast<uintptr_t>(p) & 3u) == 0) {
-        *reinterpret_cast<uint32_t*>(p) = w;
+      if (c + 8 * h >= cols) continue;
+      if (pairs) {
+        *reinterpret_cast<uint32_t*>(p + 8 * h) = w[h];
       } else {
         bf e[2];
-        memcpy(e, &w, 4);
-        p[0] = e[0];
-        if (c + 1 < cols) p[1] = e[1];
+        memcpy(e, &w[h], 4);
+        p[8 * h] = e[0];
+        if (c + 8 * h + 1 < cols) p[8 * h + 1] = e[1];
       }
     }
   }
@@ -579,24 +588,25 @@ __global__ void __launch_bounds__(96 * NP, 1) delta_scan_kernel(const DlArgs a) 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, pair = warp % NP, half = warp / NP;  // half 2: the helper
   const int states = 1 + pair, updates = 1 + NP + pair, early = 1 + 2 * NP + pair, helpers = 1 + 3 * NP;  // barriers
   const int blocks = (a.Dv + NP * 16 - 1) / (NP * 16);
-  const long long n = blockIdx.x / blocks, size = (long long)a.Dk * a.Dv, heads = (long long)a.B * a.heads;
-  const int c0 = (int)(blockIdx.x % blocks) * NP * 16, cols = min(NP * 16, a.Dv - c0);  // the CTA's columns
+  const uint32_t n = blockIdx.x / (uint32_t)blocks;
+  const long long size = (long long)a.Dk * a.Dv;
+  const int c0 = (int)(blockIdx.x - n * (uint32_t)blocks) * NP * 16, cols = min(NP * 16, a.Dv - c0);  // the CTA's columns
   const int mine = min(max(cols - 16 * pair, 0), 16);                                    // the three warps'
-  const DlUnit u0 = dl_unit(a, 0, n);
-  const int len = a.lens ? min(max(a.lens[u0.b], 0), a.T) : a.T, chunks = (len + DL_CHUNK - 1) / DL_CHUNK;
-  const bf *Q = a.Q + (long long)u0.head * a.Dk, *K = a.K + (long long)u0.head * a.Dk, *V = a.V + (long long)u0.head * a.Dv + c0;
-  bf* Y = a.Y + (long long)u0.head * a.Dv + c0;
+  DlUnit u = dl_unit(a, 0, n);
+  const int chunks = (u.len + DL_CHUNK - 1) / DL_CHUNK;
+  const bf *Q = a.Q + (long long)u.head * a.Dk, *K = a.K + (long long)u.head * a.Dk, *V = a.V + (long long)u.head * a.Dv + c0;
+  bf* Y = a.Y + (long long)u.head * a.Dv + c0;
   if (half == 2) {
     const int t = threadIdx.x - 2 * HELP;
     auto fetch_k = [&](int chunk) {
       if (chunk >= chunks) return;
-      const DlUnit u = dl_unit(a, chunk, n);
+      dl_move(a, u, chunk);
       dl_load<DK, HELP>(&sh.k[chunk & 1][0][0], LDK, K + u.row0 * a.ldk, a.B * a.ldk, u.live, a.Dk, a.vec_k, t);
       dl_load_row(sh.row[chunk & 1], a.row + u.unit * DL_ROW_FLOATS, t, HELP);
     };
     auto fetch_others = [&](int chunk) {
       if (chunk >= chunks) return;
-      const DlUnit u = dl_unit(a, chunk, n);
+      dl_move(a, u, chunk);
       dl_load<DK, HELP>(&sh.q[0][0], LDK, Q + u.row0 * a.ldq, a.B * a.ldq, u.live, a.Dk, a.vec_q, t);
       dl_load<NP * 16, HELP>(&sh.v[0][0], LDV, V + u.row0 * a.ldv, a.B * a.ldv, u.live, cols, a.vec_v, t);
       dl_load64<3, HELP>(&sh.tri[0][0][0], a.tri + u.unit * 3 * DL_SQ, t);
@@ -613,7 +623,7 @@ __global__ void __launch_bounds__(96 * NP, 1) delta_scan_kernel(const DlArgs a) 
       dl_meet(helpers, HELP);  // Q, V and T are there, and nobody reads P any more
       dl_meet(states, 96);     // nor, since all have gone on to this chunk, the keys before it
       fetch_k(chunk + 1);
-      dl_load64<2, HELP>(&sh.p[0][0][0], a.p + (chunk * heads + n) * 3 * DL_SQ, t);
+      dl_load64<2, HELP>(&sh.p[0][0][0], a.p + ((long long)chunk * (a.B * a.heads) + n) * 3 * DL_SQ, t);
       dl_commit();
       float o[8][4] = {};
 #pragma unroll
@@ -641,7 +651,7 @@ __global__ void __launch_bounds__(96 * NP, 1) delta_scan_kernel(const DlArgs a) 
         for (int p = 0; p < 2; ++p) dl_take(sh.u[pair][k][p][lane], x[p]);
         dl_later<2, 2, 1, false>(k, o, x, &sh.p[0][0][0], DL_LD64, PT, lane);
       }
-      const DlUnit u = dl_unit(a, chunk, n);
+      dl_move(a, u, chunk);
       dl_rows_out<8>(o, nullptr, Y + u.row0 * a.ldy + 16 * pair, a.B * a.ldy, 0, u.live, mine, lane);
     }
   } else {
@@ -670,7 +680,7 @@ __global__ void __launch_bounds__(96 * NP, 1) delta_scan_kernel(const DlArgs a) 
       const DlSteps& row = sh.row[chunk & 1];
       const bf* k0 = &sh.k[chunk & 1][0][0];
       const bf* tri = &sh.tri[0][0][0] + half * 32 * DL_LD64;  // this warp's steps
-      if (a.S) keep(a.S + (chunk * heads + n) * size + (long long)(c0 + 16 * pair) * a.Dk);
+      if (a.S) keep(a.S + ((long long)chunk * (a.B * a.heads) + n) * size + (long long)(c0 + 16 * pair) * a.Dk);
       dl_meet(0, ALL);
       float r[4][4];
       {
@@ -765,8 +775,8 @@ __global__ void __launch_bounds__(96 * NP, 1) delta_scan_kernel(const DlArgs a) 
     }
     if (a.hT) dl_state<HALF>(lane, [&](int i, int e, int d, int c) { if (d0 + d < a.Dk && c < mine) a.hT[n * size + (long long)(d0 + d) * a.Dv + c0 + 16 * pair + c] = s[i][e]; });
   }
-  for (int chunk = len / DL_CHUNK; chunk * DL_CHUNK < a.T; ++chunk) {
-    const DlUnit u = dl_unit(a, chunk, n);
+  for (int chunk = u.len / DL_CHUNK; chunk * DL_CHUNK < a.T; ++chunk) {
+    dl_move(a, u, chunk);
     dl_zero_rows(Y + u.row0 * a.ldy, a.B * a.ldy, u.live, min(DL_CHUNK, a.T - chunk * DL_CHUNK), cols, threadIdx.x, ALL);
   }
 }
@@ -797,30 +807,31 @@ __global__ void __launch_bounds__(96 * NP, 1) delta_back_kernel(const DlArgs a) 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, pair = warp % NP, half = warp / NP;
   const int states = 1 + pair, updates = 1 + NP + pair, late = 1 + 2 * NP + pair, helpers = 1 + 3 * NP;
   const int blocks = (a.Dv + NP * 16 - 1) / (NP * 16);
-  const long long n = blockIdx.x / blocks, size = (long long)a.Dk * a.Dv;
-  const int c0 = (int)(blockIdx.x % blocks) * NP * 16, cols = min(NP * 16, a.Dv - c0);
+  const uint32_t n = blockIdx.x / (uint32_t)blocks;
+  const long long size = (long long)a.Dk * a.Dv;
+  const int c0 = (int)(blockIdx.x - n * (uint32_t)blocks) * NP * 16, cols = min(NP * 16, a.Dv - c0);
   const int mine = min(max(cols - 16 * pair, 0), 16);
-  const DlUnit u0 = dl_unit(a, 0, n);
-  const int len = a.lens ? min(max(a.lens[u0.b], 0), a.T) : a.T, chunks = (len + DL_CHUNK - 1) / DL_CHUNK;
-  const bf *Q = a.Q + (long long)u0.head * a.Dk, *K = a.K + (long long)u0.head * a.Dk, *dY = a.dY + (long long)u0.head * a.Dv + c0;
-  bf* dV = a.dV + (long long)u0.head * a.Dv + c0;
+  DlUnit u = dl_unit(a, 0, n);
+  const int chunks = (u.len + DL_CHUNK - 1) / DL_CHUNK;
+  const bf *Q = a.Q + (long long)u.head * a.Dk, *K = a.K + (long long)u.head * a.Dk, *dY = a.dY + (long long)u.head * a.Dv + c0;
+  bf* dV = a.dV + (long long)u.head * a.Dv + c0;
   if (half == 2) {
     const int t = threadIdx.x - 2 * HELP;
     auto fetch_k = [&](int chunk) {
       if (chunk < 0) return;
-      const DlUnit u = dl_unit(a, chunk, n);
+      dl_move(a, u, chunk);
       dl_load<DK, HELP>(&sh.k[chunk & 1][0][0], LDK, K + u.row0 * a.ldk, a.B * a.ldk, u.live, a.Dk, a.vec_k, t);
       dl_load_row(sh.row[chunk & 1], a.row + u.unit * DL_ROW_FLOATS, t, HELP);
     };
     auto fetch_mine = [&](int chunk) {  // what the helpers read
       if (chunk < 0) return;
-      const DlUnit u = dl_unit(a, chunk, n);
+      dl_move(a, u, chunk);
       dl_load<NP * 16, HELP>(&sh.dy[0][0], LDV, dY + u.row0 * a.lddy, a.B * a.lddy, u.live, cols, a.vec_dy, t);
       dl_load64<3, HELP>(&sh.p[0][0][0], a.p + u.unit * 3 * DL_SQ, t);
       dl_load<DK, HELP>(&sh.q[0][0], LDK, Q + u.row0 * a.ldq, a.B * a.ldq, u.live, a.Dk, a.vec_q, t);
     };
     auto fetch_tri = [&](int chunk) {
-      if (chunk >= 0) dl_load64<3, HELP>(&sh.tri[0][0][0], a.tri + dl_unit(a, chunk, n).unit * 3 * DL_SQ, t);
+      if (chunk >= 0) dl_load64<3, HELP>(&sh.tri[0][0][0], a.tri + ((long long)chunk * (a.B * a.heads) + n) * 3 * DL_SQ, t);
     };
     // G to shared memory and Y to registers: a chunk ahead of the state
     float y[DK / 8][4];
@@ -895,7 +906,7 @@ __global__ void __launch_bounds__(96 * NP, 1) delta_back_kernel(const DlArgs a) 
       const DlSteps& row = sh.row[chunk & 1];
       const bf* k0 = &sh.k[chunk & 1][0][0];
       const bf* tri = &sh.tri[0][0][0] + half * 32;  // this warp's steps
-      const DlUnit u = dl_unit(a, chunk, n);
+      dl_move(a, u, chunk);
       dl_meet(0, ALL);
       float r[4][4];
       {
@@ -1003,8 +1014,8 @@ __global__ void __launch_bounds__(96 * NP, 1) delta_back_kernel(const DlArgs a) 
     }
     if (a.dh0) dl_state<HALF>(lane, [&](int i, int e, int d, int c) { if (d0 + d < a.Dk && c < mine) a.dh0[n * size + (long long)(d0 + d) * a.Dv + c0 + 16 * pair + c] = s[i][e]; });
   }
-  for (int chunk = len / DL_CHUNK; chunk * DL_CHUNK < a.T; ++chunk) {
-    const DlUnit u = dl_unit(a, chunk, n);
+  for (int chunk = u.len / DL_CHUNK; chunk * DL_CHUNK < a.T; ++chunk) {
+    dl_move(a, u, chunk);
     dl_zero_rows(dV + u.row0 * a.lddv, a.B * a.lddv, u.live, min(DL_CHUNK, a.T - chunk * DL_CHUNK), cols, threadIdx.x, ALL);
   }
 }
@@ -1249,7 +1260,7 @@ __global__ void __launch_bounds__(DL_GRAD_THREADS) delta_grad_kernel(const DlArg
   pdl_launch_dependents();
   pdl_wait_prior_grids();
   const int t = threadIdx.x, warp = t >> 5, lane = t & 31;
-  const long long units = (long long)a.B * a.heads;
+  const uint32_t units = (uint32_t)a.B * (uint32_t)a.heads;
   const DlUnit u = dl_unit(a, (int)(blockIdx.x / units), blockIdx.x % units);
   const int steps = min(DL_CHUNK, a.T - u.chunk * DL_CHUNK);
   bf* dq = a.dQ + u.row0 * a.lddq + (long long)u.head * a.Dk;
