@@ -60,6 +60,7 @@ struct DlArgs {
   bf* x;       // [units][2][64][ldx] X in two parts
   bf* d;       // [units][2][ldx][DK] the gradient of the state behind a chunk, transposed
   int ldx;
+  int ahead;   // SMs
 };
 
 // What a chunk's steps have of their own.  G_ij = f_{j+1} .. f_i is kept as products of gates: inside a block of 16 steps as it is, across blocks a_i, the whole
@@ -1194,34 +1195,46 @@ struct DlGradShared {
 // two parts in memory.
 template <int DK, int DV>
 __device__ __forceinline__ float dl_load_state(bf* s, const float* g, int Dk, int Dv, int vec, const bf* with, int rows) {
-  constexpr int LD = DK + 8, QUADS = DK / 4, MINE = DV * QUADS / DL_GRAD_THREADS, AHEAD = MINE;  // all of them at once: nothing else is held yet
-  static_assert(MINE % AHEAD == 0, "whole rounds");
+  constexpr int LD = DK + 8, QUADS = DK / 4, AHEAD = DV * QUADS / DL_GRAD_THREADS;  // all of them at once: nothing else is held yet
   float dot = 0.f;
-  for (int i0 = 0; i0 < MINE; i0 += AHEAD) {
+  {
     float4 x[AHEAD];
     uint2 hi[AHEAD], lo[AHEAD];
+    const int d = threadIdx.x % QUADS * 4, c0 = threadIdx.x / QUADS;
+    constexpr int STEP = DL_GRAD_THREADS / QUADS;
 #pragma unroll
     for (int i = 0; i < AHEAD; ++i) {
-      const int at = (i0 + i) * DL_GRAD_THREADS + threadIdx.x, c = at / QUADS, d = at % QUADS * 4;
       x[i] = make_float4(0.f, 0.f, 0.f, 0.f);
       hi[i] = lo[i] = make_uint2(0u, 0u);
-      if (d < Dk && c < Dv) {
-        const float* p = g + c * Dk + d;
-        if (vec) {
-          x[i] = *reinterpret_cast<const float4*>(p);
-        } else {
-          x[i].x = p[0];
-          if (d + 1 < Dk) x[i].y = p[1];
-          if (d + 2 < Dk) x[i].z = p[2];
-          if (d + 3 < Dk) x[i].w = p[3];
-        }
-        hi[i] = *reinterpret_cast<const uint2*>(with + c * DK + d);
-        lo[i] = *reinterpret_cast<const uint2*>(with + (rows + c) * DK + d);
+    }
+    if (vec) {
+      if (d < Dk) {
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i)
+          if (c0 + i * STEP < Dv) x[i] = *reinterpret_cast<const float4*>(g + (c0 + i * STEP) * Dk + d);
       }
+    } else {
+#pragma unroll
+      for (int i = 0; i < AHEAD; ++i) {
+        const float* p = g + (c0 + i * STEP) * Dk + d;
+        const int n = c0 + i * STEP < Dv ? Dk - d : 0;
+        if (n > 0) x[i].x = p[0];
+        if (n > 1) x[i].y = p[1];
+        if (n > 2) x[i].z = p[2];
+        if (n > 3) x[i].w = p[3];
+      }
+    }
+    if (d < Dk) {
+#pragma unroll
+      for (int i = 0; i < AHEAD; ++i)
+        if (c0 + i * STEP < Dv) {
+          hi[i] = *reinterpret_cast<const uint2*>(with + (c0 + i * STEP) * DK + d);
+          lo[i] = *reinterpret_cast<const uint2*>(with + (rows + c0 + i * STEP) * DK + d);
+        }
     }
 #pragma unroll
     for (int i = 0; i < AHEAD; ++i) {
-      const int at = (i0 + i) * DL_GRAD_THREADS + threadIdx.x, c = at / QUADS, d = at % QUADS * 4;
+      const int c = c0 + i * STEP;
       auto pair = [](uint32_t w) {
         __nv_bfloat162 h;
         memcpy(&h, &w, 4);
@@ -1249,6 +1262,32 @@ __device__ __forceinline__ void dl_load_parts(bf* s, const bf* g, int from, int 
     const bool there = c < cols && r < rows;
     dl_copy16(s + all * (PAD + 8) + c, g + (there ? (part * from + r) * pitch + c : 0), there);
   }
+}
+
+// Lines of 128 bytes on their way to L2: `bytes` from p on, or rows of a chunk.
+__device__ __forceinline__ void dl_ahead(const void* p, long long bytes) {
+  for (long long i = threadIdx.x * 128ll; i < bytes; i += DL_GRAD_THREADS * 128)
+    asm volatile("prefetch.global.L2 [%0];" ::"l"(reinterpret_cast<const uint8_t*>(p) + i));
+}
+__device__ __forceinline__ void dl_ahead_rows(const bf* p, long long step, int live, int cols) {
+  const int r = threadIdx.x >> 3, c = (threadIdx.x & 7) * 64;
+  if (r < live && c < cols) asm volatile("prefetch.global.L2 [%0];" ::"l"(p + r * step + c));
+}
+// All that the unit of the CTA after this one on the SM reads, while this one computes: the loads of all SMs together are as fast as memory is, and nothing overlaps
+// them where one CTA fills an SM.
+__device__ __forceinline__ void dl_ahead(const DlArgs& a, long long at) {
+  const uint32_t units = (uint32_t)a.B * (uint32_t)a.heads;
+  const DlUnit u = dl_unit(a, (int)(at / units), (uint32_t)(at % units));
+  if (u.live == 0) return;
+  dl_ahead(a.S + u.unit * a.Dk * a.Dv, 4ll * a.Dk * a.Dv);
+  dl_ahead_rows(a.K + u.row0 * a.ldk + (long long)u.head * a.Dk, a.B * a.ldk, u.live, a.Dk);
+  dl_ahead_rows(a.Q + u.row0 * a.ldq + (long long)u.head * a.Dk, a.B * a.ldq, u.live, a.Dk);
+  dl_ahead_rows(a.V + u.row0 * a.ldv + (long long)u.head * a.Dv, a.B * a.ldv, u.live, a.Dv);
+  dl_ahead_rows(a.dY + u.row0 * a.lddy + (long long)u.head * a.Dv, a.B * a.lddy, u.live, a.Dv);
+  dl_ahead(a.x + u.unit * 2 * DL_CHUNK * a.ldx, 4ll * DL_CHUNK * a.ldx);
+  dl_ahead(a.d + u.unit * 2 * (a.Dk <= 64 ? 64 : 128) * a.ldx, 4ll * a.Dv * (a.Dk <= 64 ? 64 : 128));
+  dl_ahead(a.tri + u.unit * 3 * DL_SQ, 4ll * DL_SQ);
+  dl_ahead(a.row + u.unit * DL_ROW_FLOATS, 4ll * DL_ROW_FLOATS);
 }
 
 template <int DK, int DV>
@@ -1307,6 +1346,7 @@ __global__ void __launch_bounds__(DL_GRAD_THREADS) delta_grad_kernel(const DlArg
   for (int o = 16; o > 0; o >>= 1) dot += __shfl_xor_sync(0xFFFFFFFFu, dot, o);
   if (lane == 0) sh.ds[warp] = dot;
   dl_wait<0>();
+  if (blockIdx.x + (long long)a.ahead < gridDim.x) dl_ahead(a, blockIdx.x + (long long)a.ahead);
   __syncthreads();
   auto row_sums = [&](int which, const float (&x)[1][NK][4], const bf* with, const float* by, bool more) {
 #pragma unroll
@@ -1652,5 +1692,6 @@ ard_status launch_delta_backward(ard_ctx* ctx, int T, int B, int heads, int Dk, 
   a.vec_v = dl_on16(V, ldv, Dv);
   a.vec_s = Dk % 4 == 0 && (reinterpret_cast<uintptr_t>(S) & 15u) == 0;
   dl_set_work(a, work, dl_plan(T, B, heads, Dk, Dv, true));
+  a.ahead = ctx->sm_count;
   return dl_chunks(ctx, a, true, s);
 }
