@@ -248,7 +248,7 @@ __device__ __forceinline__ DlUnit dl_unit(const DlArgs& a, int chunk, uint32_t n
 }
 
 // ---- a chunk's triangular system ----------------------------------------------------------------------
-constexpr int DL_LDA = DL_CHUNK + 1;
+constexpr int DL_LDA = DL_CHUNK + 4;  // four neighbours at once, eight rows on different banks
 template <int DK>
 struct DlPrepShared {
   union {
@@ -261,7 +261,7 @@ struct DlPrepShared {
         bf p[3][DL_CHUNK][DL_LD64];
         struct {
           float t[DL_CHUNK][DL_LDA];  // the inverse, with ones on the diagonal
-          float tmp[3][16][17];
+          float tmp[6][16][8];
         };
       };
     };
@@ -269,28 +269,36 @@ struct DlPrepShared {
   DlRow row;
 };
 
-// The blocks D below the diagonal of 16 x 16 blocks: T_ij = -T_ii sum_{j <= k < i} A_ik T_kj, all of them side by side.
-template <int D, typename Sh>
-__device__ __forceinline__ void dl_inverse_blocks(Sh& sh, int er, int ec) {
-  float s[4 - D];
+// s += A T, two rows of A (from a) by two columns of T (from b), over `count` entries.
+__device__ __forceinline__ void dl_two_by_two(float (&s)[2][2], const float* a, const float* b, int ldb, int count) {
+#pragma unroll 4
+  for (int k = 0; k < count; k += 4, a += 4, b += 4 * ldb) {
+    const float4 a0 = *reinterpret_cast<const float4*>(a), a1 = *reinterpret_cast<const float4*>(a + DL_LDA);
+    const float2 b0 = *reinterpret_cast<const float2*>(b), b1 = *reinterpret_cast<const float2*>(b + ldb),
+                 b2 = *reinterpret_cast<const float2*>(b + 2 * ldb), b3 = *reinterpret_cast<const float2*>(b + 3 * ldb);
+    s[0][0] = fmaf(a0.w, b3.x, fmaf(a0.z, b2.x, fmaf(a0.y, b1.x, fmaf(a0.x, b0.x, s[0][0]))));
+    s[0][1] = fmaf(a0.w, b3.y, fmaf(a0.z, b2.y, fmaf(a0.y, b1.y, fmaf(a0.x, b0.y, s[0][1]))));
+    s[1][0] = fmaf(a1.w, b3.x, fmaf(a1.z, b2.x, fmaf(a1.y, b1.x, fmaf(a1.x, b0.x, s[1][0]))));
+    s[1][1] = fmaf(a1.w, b3.y, fmaf(a1.z, b2.y, fmaf(a1.y, b1.y, fmaf(a1.x, b0.y, s[1][1]))));
+  }
+}
+// The blocks below the diagonal of 16 x 16 blocks, T_ij = -T_ii sum_{j <= k < i} A_ik T_kj.  Columns do not see one another: a warp takes eight of them from top to
+// bottom, two rows by two columns a lane, which reads shared memory a third as often as an entry a thread does (the kernel spends most of its time there).
+template <typename Sh>
+__device__ __forceinline__ void dl_inverse_columns(Sh& sh, int warp, int lane) {
+  const int j = warp >> 1, r = 2 * (lane >> 2), c = 2 * (lane & 3), at = 8 * warp + c;
+  for (int i = j + 1; i < 4; ++i) {
+    float s[2][2] = {};
+    dl_two_by_two(s, &sh.a[16 * i + r][16 * j], &sh.t[16 * j][at], DL_LDA, 16 * (i - j));
 #pragma unroll
-  for (int j = 0; j < 4 - D; ++j) s[j] = 0.f;
-#pragma unroll 8
-  for (int k = 0; k < 16 * D; ++k)
+    for (int e = 0; e < 2; ++e) *reinterpret_cast<float2*>(&sh.tmp[warp][r + e][c]) = make_float2(s[e][0], s[e][1]);
+    __syncwarp();
+    s[0][0] = s[0][1] = s[1][0] = s[1][1] = 0.f;
+    dl_two_by_two(s, &sh.t[16 * i + r][16 * i], &sh.tmp[warp][0][c], 8, 16);
 #pragma unroll
-    for (int j = 0; j < 4 - D; ++j) s[j] = fmaf(sh.a[16 * (j + D) + er][16 * j + k], sh.t[16 * j + k][16 * j + ec], s[j]);
-#pragma unroll
-  for (int j = 0; j < 4 - D; ++j) sh.tmp[j][er][ec] = s[j];
-  __syncthreads();
-#pragma unroll
-  for (int j = 0; j < 4 - D; ++j) s[j] = 0.f;
-#pragma unroll
-  for (int k = 0; k < 16; ++k)
-#pragma unroll
-    for (int j = 0; j < 4 - D; ++j) s[j] = fmaf(sh.t[16 * (j + D) + er][16 * (j + D) + k], sh.tmp[j][k][ec], s[j]);
-#pragma unroll
-  for (int j = 0; j < 4 - D; ++j) sh.t[16 * (j + D) + er][16 * j + ec] = -s[j];
-  __syncthreads();
+    for (int e = 0; e < 2; ++e) *reinterpret_cast<float2*>(&sh.t[16 * i + r + e][at]) = make_float2(-s[e][0], -s[e][1]);
+    __syncwarp();
+  }
 }
 
 template <int DK>
@@ -423,15 +431,15 @@ __global__ void __launch_bounds__(DL_THREADS, 4) delta_prep_kernel(const DlArgs 
     }
   }
   __syncthreads();
-  dl_inverse_blocks<1>(sh, t >> 4, t & 15);
-  dl_inverse_blocks<2>(sh, t >> 4, t & 15);
-  dl_inverse_blocks<3>(sh, t >> 4, t & 15);
+  if (warp < 6) dl_inverse_columns(sh, warp, lane);
+  __syncthreads();
   bf* tri = a.tri + u.unit * 3 * DL_SQ;
 #pragma unroll
   for (int i = t; i < DL_SQ / 2; i += DL_THREADS) {
     const int r = i / (DL_CHUNK / 2), c = 2 * (i % (DL_CHUNK / 2));
     const bool on = c / 16 <= r / 16;
-    dl_put<3>(tri + r * DL_CHUNK + c, DL_SQ, on ? sh.t[r][c] : 0.f, on ? sh.t[r][c + 1] : 0.f);
+    const float2 x = on ? *reinterpret_cast<const float2*>(&sh.t[r][c]) : make_float2(0.f, 0.f);
+    dl_put<3>(tri + r * DL_CHUNK + c, DL_SQ, x.x, x.y);
   }
   float* row = a.row + u.unit * DL_ROW_FLOATS;
   for (int i = t; i < DL_ROW_FLOATS; i += DL_THREADS) row[i] = reinterpret_cast<const float*>(&sh.row)[i];
