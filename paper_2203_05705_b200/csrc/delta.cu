@@ -1385,8 +1385,27 @@ __global__ void __launch_bounds__(DL_GRAD_THREADS) delta_grad_kernel(const DlArg
       }
   }
   float aq[1][NK][4] = {}, ak[1][NK][4] = {};
-  dl_product<1, NK, false, true, 1, 2, 1>(aq, &sh.dy[0][0], LDV, 0, &sh.s[0][0][0], LDK, PS, m0, nk0, 0, DV, lane);
-  dl_product<1, NK, false, true, 2, 2, 1>(ak, &sh.x[0][0][0], LDV, PV, &sh.s[0][0][0], LDK, PS, m0, nk0, 0, DV, lane);
+#pragma unroll 2
+  for (int k = 0; k < DV; k += 16) {
+    uint32_t dy[4], x[2][4];
+    dl_a<false>(dy, &sh.dy[0][0], LDV, m0, k, lane);
+#pragma unroll
+    for (int p = 0; p < 2; ++p) dl_a<false>(x[p], &sh.x[p][0][0], LDV, m0, k, lane);
+#pragma unroll
+    for (int n = 0; n < NK; n += 2) {
+      uint32_t w[2][4];
+#pragma unroll
+      for (int p = 0; p < 2; ++p) dl_b<true>(w[p], &sh.s[p][0][0], LDK, nk0 + 8 * n, k, lane);
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        dl_mma(aq[0][n + e], dy, w[1][2 * e], w[1][2 * e + 1]);
+        dl_mma(ak[0][n + e], x[0], w[1][2 * e], w[1][2 * e + 1]);
+        dl_mma(aq[0][n + e], dy, w[0][2 * e], w[0][2 * e + 1]);
+        dl_mma(ak[0][n + e], x[1], w[0][2 * e], w[0][2 * e + 1]);
+        dl_mma(ak[0][n + e], x[0], w[0][2 * e], w[0][2 * e + 1]);
+      }
+    }
+  }
 #pragma unroll
   for (int i = 0; i < NK; ++i)
 #pragma unroll
@@ -1429,10 +1448,34 @@ __global__ void __launch_bounds__(DL_GRAD_THREADS) delta_grad_kernel(const DlArg
   float nn[1][2][4] = {}, mm[1][2][4] = {};
   if (nm0 <= m0) {
     float qk[1][2][4] = {}, kk[1][2][4] = {};
-    dl_product<1, 2, false, false, 1, 2, 1>(nn, &sh.dy[0][0], LDV, 0, &sh.u[0][0][0], LDV, PV, m0, nm0, 0, DV, lane);
-    dl_product<1, 2, false, false, 2, 2, 1>(mm, &sh.x[0][0][0], LDV, PV, &sh.u[0][0][0], LDV, PV, m0, nm0, 0, DV, lane);
-    dl_product<1, 2, false, false, 1, 1, 0>(qk, &sh.q[0][0], LDK, 0, &sh.k[0][0], LDK, 0, m0, nm0, 0, DK, lane);
-    dl_product<1, 2, false, false, 1, 1, 0>(kk, &sh.k[0][0], LDK, 0, &sh.k[0][0], LDK, 0, m0, nm0, 0, DK, lane);
+    // two products at a time share their right operand, and are more sums for the tensor pipe to go on with
+#pragma unroll 4
+    for (int k = 0; k < DV; k += 16) {
+      uint32_t dy[4], x[2][4], w[2][4];
+      dl_a<false>(dy, &sh.dy[0][0], LDV, m0, k, lane);
+#pragma unroll
+      for (int p = 0; p < 2; ++p) dl_a<false>(x[p], &sh.x[p][0][0], LDV, m0, k, lane), dl_b<false>(w[p], &sh.u[p][0][0], LDV, nm0, k, lane);
+#pragma unroll
+      for (int n = 0; n < 2; ++n) {
+        dl_mma(nn[0][n], dy, w[1][2 * n], w[1][2 * n + 1]);
+        dl_mma(mm[0][n], x[0], w[1][2 * n], w[1][2 * n + 1]);
+        dl_mma(nn[0][n], dy, w[0][2 * n], w[0][2 * n + 1]);
+        dl_mma(mm[0][n], x[1], w[0][2 * n], w[0][2 * n + 1]);
+        dl_mma(mm[0][n], x[0], w[0][2 * n], w[0][2 * n + 1]);
+      }
+    }
+#pragma unroll 4
+    for (int k = 0; k < DK; k += 16) {
+      uint32_t q[4], key[4], w[4];
+      dl_a<false>(q, &sh.q[0][0], LDK, m0, k, lane);
+      dl_a<false>(key, &sh.k[0][0], LDK, m0, k, lane);
+      dl_b<false>(w, &sh.k[0][0], LDK, nm0, k, lane);
+#pragma unroll
+      for (int n = 0; n < 2; ++n) {
+        dl_mma(qk[0][n], q, w[2 * n], w[2 * n + 1]);
+        dl_mma(kk[0][n], key, w[2 * n], w[2 * n + 1]);
+      }
+    }
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       const int i = r0 + 8 * h, bi = m0 >> 4;
