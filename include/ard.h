@@ -748,10 +748,12 @@ ard_status ard_glr_backward(ard_ctx* ctx, const ard_pattern* pat, ard_dtype dtyp
  *         are written as zero, and the state stays what it was.
  *   h0    fp32 [B][heads][Dk][Dv], the state before the first step; NULL: zero.
  *   hT    the state after the last step, like h0, or NULL.  May be h0.
- *   S     fp32 [ceil(T / ARD_DELTA_CHUNK)][B][heads][Dk][Dv], what the backward call starts from, or NULL when there is none.
+ *   S     fp32, ceil(T / ARD_DELTA_CHUNK) * B * heads * Dk * Dv of them, in an order of the library's own: what the backward call
+ *         starts from, or NULL when there is none.
  *   work  device memory of ard_delta_work_bytes(T, B, heads, Dk, Dv, 0 or, for the backward call, 1) bytes, from any byte on; holds nothing between
  *         calls, so one piece serves many layers whose calls are ordered.  NULL where that is 0 (decoding).
- * Decoding is T = 1 with hT = h0.  A gate of -infinity (f = 0) starts anew.  Q, K, V, Z, Y are ARD_BF16, from any whole element on (fastest
+ * Decoding is T = 1 with hT = h0.  A gate of -infinity (f = 0) starts anew.  Steps are computed ARD_DELTA_CHUNK at a time, so what a NaN or an
+ * infinity in a sequence's inputs makes of its own step and later ones it may make of the same chunk's earlier ones too.  Q, K, V, Z, Y are ARD_BF16, from any whole element on (fastest
  * with 16-byte aligned pointers and rows, Dk and Dv multiples of 8); gates, states and their products are fp32.  Y must not overlap an input.
  * Errors: ARD_ERR_INVALID_ARG (NULL, negative size, unknown dtype, scale or eps not finite), ARD_ERR_SHAPE (leading dimension too small),
  * ARD_ERR_ALIGNMENT (a pointer inside an element), ARD_ERR_NOMEM (work_bytes too small), ARD_ERR_UNSUPPORTED (ARD_F32, Dk or Dv above 128, T
@@ -833,7 +835,7 @@ ard_status ard_grad_norm(ard_ctx* ctx, const ard_adamw_tensor* tensors, int n_te
  * written.  ids int32 [rows]: a negative one is padding, its row of Y is zero and adds nothing to the gradient; so is one of V
  * or more, and the device status becomes ARD_ERR_INVALID_ARG.
  * table [V][N] and Y of element type `dtype`, from any whole element on (fastest with 16-byte aligned pointers and rows); the product with alpha
- * is fp32.  Y must not overlap the table.  Errors: as ard_layer_norm_fwd.  Asynchronous. */
+ * is fp32.  Y must not overlap the table.  Errors: as ard_layer_norm_fwd, and ARD_ERR_UNSUPPORTED for N above 2^30.  Asynchronous. */
 ard_status ard_embedding_fwd(ard_ctx* ctx, const ard_pattern* pat, ard_dtype dtype, int rows, int V, int N, float alpha,
                              const int32_t* ids, const void* table, int ldt, void* Y, int ldy, void* cuda_stream);
 /* Its adjoint:  dtable[v][j] (+)= alpha * sum over r with ids[r] = v of dY[r][j],  dtable fp32 [V][N], full width.  accumulate

@@ -1906,6 +1906,7 @@ ard_status ard_embedding_fwd(ard_ctx* ctx, const ard_pattern* pat, ard_dtype dty
   if (st != ARD_OK) return st;
   if (V < 0 || (rows > 0 && (!ids || !table || !Y || Y == table))) return ARD_ERR_INVALID_ARG;
   if (ldt < N || ldy < N) return ARD_ERR_SHAPE;
+  if (N > (1 << 30)) return ARD_ERR_UNSUPPORTED;
   if (off_elements(element_bytes(dtype), {table, Y}) || off_elements(4, {ids})) return ARD_ERR_ALIGNMENT;
   DeviceGuard guard(ctx->device);
   return launch_embedding_fwd(ctx, pat ? pat->d_hdr : nullptr, dtype, rows, V, N, alpha, ids, table, ldt, Y, ldy, (cudaStream_t)cuda_stream);
@@ -1917,6 +1918,7 @@ ard_status ard_embedding_bwd(ard_ctx* ctx, const ard_pattern* pat, ard_dtype dty
   if (st != ARD_OK) return st;
   if (V < 0 || (rows > 0 && (!ids || !dY || dtable == dY)) || (V > 0 && !dtable)) return ARD_ERR_INVALID_ARG;
   if (lddy < N || lddt < N) return ARD_ERR_SHAPE;
+  if (N > (1 << 30)) return ARD_ERR_UNSUPPORTED;
   if (off_elements(element_bytes(dtype), {dY}) || off_elements(4, {ids, dtable})) return ARD_ERR_ALIGNMENT;
   DeviceGuard guard(ctx->device);
   return launch_embedding_bwd(ctx, pat ? pat->d_hdr : nullptr, dtype, rows, V, N, alpha, ids, dY, lddy, dtable, lddt, accumulate ? 1 : 0,

@@ -535,7 +535,7 @@ inline bool on(const void* p, long long ld, int bytes, int es) { return reinterp
 template <typename T, int BYTES>
 ard_status em_fwd(ard_ctx* ctx, const int32_t* hdr, int rows, int V, int N, float alpha, const int32_t* ids, const void* table, int ldt, void* Y,
                   int ldy, cudaStream_t s) {
-  const int vecs = (N * (int)sizeof(T) + BYTES - 1) / BYTES;
+  const int vecs = (int)(((long long)N * (int)sizeof(T) + BYTES - 1) / BYTES);
   // four accesses a thread where that still leaves every SM its threads, else one
   const bool many = (double)rows * vecs >= 4.0 * 2048 * ctx->sm_count;
   int lanes = 1;

@@ -56,18 +56,18 @@ class TokenEnds:
         return self.x[:rows]
 
     def logits(self, y):
-        """y: bf16 [rows][N], kept until backward(), or fewer rows.  Returns z, whose first V columns are the logits."""
+        """y: bf16 [rows][N], or fewer rows.  Returns z, whose first V columns are the logits.  Not between loss() and its backward()."""
         rows = y.shape[0]
         if rows > self.rows:
             raise ValueError("y has %d rows, the model %d" % (rows, self.rows))
         self._check("y", y, (rows, self.N), BF)
-        self.y = y
+        self.y = None
         ard.ard_layer_fwd(self.ctx, self.pat, None, ard.ARD_BF16, rows, self.N, self.V, 1.0, y, self.N, self.table, self.N, None, self.z, self.ldz,
                           ard.ARD_OUT_COMPACT)
         return self.z[:rows]
 
     def loss(self, y, labels=None, teacher_ids=None, teacher_logits=None, tau=1.0, hard=1.0, soft=0.0, row_weight=None):
-        """The loss of y against labels (int32 [rows]) and a teacher's top logits (int32 and fp32 [rows][k]).  Returns total, fp32 [1] on the device; each row's is in
+        """The loss of y (kept until backward()) against labels (int32 [rows]) and a teacher's top logits (int32 and fp32 [rows][k]).  Returns total, fp32 [1] on the device; each row's is in
         losses, and the gradient of the logits takes the logits' place until backward()."""
         rows, k = y.shape[0], 0 if teacher_ids is None else teacher_ids.shape[1]
         self._check("labels", labels, (rows,), torch.int32)
@@ -79,10 +79,13 @@ class TokenEnds:
         self.logits(y)
         ard.ard_distill_loss(self.ctx, ard.ARD_BF16, rows, self.V, self.z, self.ldz, labels, k, teacher_ids, teacher_logits, k, tau, hard, soft, row_weight,
                              self.losses, self.total, self.z, self.ldz)
+        self.y = y
         return self.total
 
     def backward(self):
         """Behind loss(): returns dy bf16 [rows][N], what the layers' backward calls start from; the output's share of the table's gradient is in dtable."""
+        if self.y is None:
+            raise RuntimeError("backward() before loss()")
         rows = self.y.shape[0]
         ard.ard_layer_bwd_weight(self.ctx, self.pat, None, ard.ARD_BF16, ard.ARD_F32, rows, self.N, self.V, 1.0, self.y, self.N, self.z, self.ldz, 1,
                                  self.dtable, self.N, 1)
@@ -92,6 +95,8 @@ class TokenEnds:
 
     def embed_backward(self, dx):
         """Behind backward(): dx bf16 [rows][N], the gradient of embed()'s x (with in_pat compact), whose share is added to dtable."""
+        if self.ids is None:
+            raise RuntimeError("embed_backward() before embed()")
         self._check("dx", dx, (self.ids.shape[0], self.N), BF)
         ard.ard_embedding_bwd(self.ctx, self.in_pat, ard.ARD_BF16, self.ids.shape[0], self.V, self.N, self.alpha, self.ids, dx, self.N, self.dtable, self.N, True)
 

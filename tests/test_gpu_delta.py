@@ -280,3 +280,58 @@ def test_no_steps():
     ard.ard_delta_backward(ctx.h, BF16, 0, 2, 3, 16, 8, 1.0, 0.0, e, 48, e, 48, e, 24, e, e, 3, None, None, e, 24, None, e, 48, e, 48, e, 24, e, e, 3, out, None, 0)
     assert bool((out == 0).all())
     ctx.close()
+
+
+@pytest.mark.parametrize("T", [9, 100])
+def test_two_graphs_over_one_workspace(T):
+    """Two captured forward and backward passes of different sizes that share their work, replayed in turn on other inputs, on a stream of their own."""
+    ctx = Ctx()
+    cases = [Case(T, 3, 2, 64, 72, lens=[T, T // 2, 0]), Case(2 * T, 1, 5, 128, 128, seed=1)]
+    need = max(ard.ard_delta_work_bytes(c.T, c.B, c.h, c.Dk, c.Dv, True) for c in cases)
+    shared = torch.full((need,), 0xFF, dtype=torch.uint8, device="cuda")
+    side, graphs = torch.cuda.Stream(), []
+    for c in cases:
+        c.work = lambda backward, c=c: (shared, ard.ard_delta_work_bytes(c.T, c.B, c.h, c.Dk, c.Dv, backward))
+        side.wait_stream(torch.cuda.current_stream())
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1], stream=side):
+            c.forward(ctx, stream=side.cuda_stream)
+            c.backward(ctx, stream=side.cuda_stream)
+    for seed in (8, 9):
+        rng = np.random.default_rng(seed)
+        for c in cases:
+            c.fill(c.v, c.h * c.Dv, rng.normal(size=(c.T, c.B, c.h * c.Dv)))
+            c.fill(c.zf, c.h, rng.normal(size=(c.T, c.B, c.h)) * 1.5 + 3)
+            c.fill(c.dy, c.h * c.Dv, rng.normal(size=(c.T, c.B, c.h * c.Dv)))
+        for g in graphs:
+            g.replay()
+        for c in cases:
+            c.check()
+    ctx.close()
+
+
+def test_rows_that_lie_2_to_the_32_elements_apart():
+    """Column blocks of one matrix whose offsets pass 32 bits, in elements."""
+    T, B, h, Dk, Dv = 70, 1, 2, 16, 24
+    ld = 1 << 26
+    if torch.cuda.mem_get_info()[0] < 24 << 30:
+        pytest.skip("two matrices of 9.4 GB")
+    ctx = Ctx()
+    case = Case(T, B, h, Dk, Dv)
+    n = h * Dk
+    big, grad = (torch.empty((T, ld), dtype=BF, device="cuda") for _ in range(2))
+    at = (0, n, 2 * n, ld - 2 * h, ld - h)
+    widths = (n, n, h * Dv, h, h)
+    parts = [big[:, a:a + w] for a, w in zip(at, widths)]
+    for part, x in zip(parts, (case.q, case.k, case.v, case.zf, case.zb)):
+        part.copy_(x)
+    q, k, v, zf, zb = parts
+    outs = [grad[:, a:a + w] for a, w in zip(at, widths)]
+    w, size = case.work(True)
+    args = (ctx.h, BF16, T, B, h, Dk, Dv, case.scale, case.eps, q, ld, k, ld, v, ld, zf, zb, ld, None)
+    ard.ard_delta_forward(*args, case.h0, case.y, h * Dv, case.hT, case.S, w, size)
+    ard.ard_delta_backward(*args, case.S, case.dy, h * Dv, case.dhT, outs[0], ld, outs[1], ld, outs[2], ld, outs[3], outs[4], ld, case.dh0, w, size)
+    for mine, there in zip((case.dq, case.dk, case.dv, case.dzf, case.dzb), outs):
+        mine.copy_(there)
+    case.check()
+    ctx.close()

@@ -230,3 +230,25 @@ def test_no_rows():
     ard.ard_distill_loss(ctx.h, F32, 0, 10, e, 10, None, 0, None, None, 0, 1.0, 1.0, 0.0, None, e, total, None, 0)
     assert float(total) == 0.0
     ctx.close()
+
+
+@pytest.mark.parametrize("V", [40, 9000, 60000])
+def test_on_a_stream_and_from_a_graph(V):
+    """Captured on another stream than the current one and replayed on other logits: scratch and counters are as the call before left them."""
+    ctx = Ctx()
+    case = Case(BF16, 300, V, 5, tau=2.0, hard=0.6, soft=0.4, weights=False)
+    case.call(ctx)
+    labels, ids, t, w = case.keep
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.graph(graph, stream=side):
+        for _ in range(2):           # the second one begins where the first one ended
+            ard.ard_distill_loss(ctx.h, BF16, case.rows, V, case.z, V, labels, 5, ids, t, 5, 2.0, 0.6, 0.4, w, case.loss, case.total, case.dz, V,
+                                 stream=side.cuda_stream)
+    for seed in (1, 2):
+        g = torch.Generator(device="cuda").manual_seed(seed)
+        case.z.copy_(torch.randn(case.z.shape, generator=g, device="cuda") * 2)
+        case.total.fill_(float("nan"))
+        graph.replay()
+        case.check(host(case.z))
+    ctx.close()

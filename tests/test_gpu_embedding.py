@@ -65,6 +65,38 @@ CASES = [
 ]
 
 
+def test_on_a_stream_and_from_a_graph():
+    """On another stream than the current one, captured, and replayed on other tokens and gradients."""
+    ctx = Ctx()
+    rows, V, N = 3000, 500, 260
+    rng = np.random.default_rng(4)
+    ids = torch.from_numpy(tokens(rng, rows, V, "zipf")).cuda()
+    table, y, dy, dtable = matrix(rng, V, N, N, 0, BF16), matrix(None, rows, N, N, 0, BF16), matrix(rng, rows, N, N, 0, BF16), matrix(None, V, N, N, 0, F32)
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+
+    def both():
+        s = torch.cuda.current_stream().cuda_stream
+        ard.ard_embedding_fwd(ctx.h, None, BF16, rows, V, N, 1.0, ids, table, N, y, N, stream=s)
+        ard.ard_embedding_bwd(ctx.h, None, BF16, rows, V, N, 1.0, ids, dy, N, dtable, N, 0, stream=s)
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.graph(graph, stream=side):
+        both()
+    for seed in (5, 6):
+        rng = np.random.default_rng(seed)
+        ids.copy_(torch.from_numpy(tokens(rng, rows, V, "padded")))
+        dy.copy_(matrix(rng, rows, N, N, 0, BF16))
+        graph.replay()
+        got = y.clone(), dtable.clone()
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            both()
+        side.synchronize()
+        assert torch.equal(got[0], y) and torch.equal(got[1], dtable)
+        want, size, count = OE.bwd(ids.cpu().numpy(), host(dy), V, N, 1.0, np.arange(N))
+        assert (np.abs(host(dtable) - want) <= (count[:, None] + 3) * 2.0 ** -24 * size).all()
+    ctx.close()
+
+
 @pytest.mark.parametrize("case", CASES, ids=lambda c: "%s_%dx%dx%d_dp%d_%s%s" % ("f32" if c[0] == F32 else "bf16", c[1], c[2], c[3], c[4][0], c[7],
                                                                                "_add" if c[8] else ""))
 def test_both_ways(case):

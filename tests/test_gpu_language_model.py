@@ -211,6 +211,16 @@ def test_refusals():
         e.embed_backward(y[:, :-1])
     with pytest.raises(ValueError):
         TokenEnds(m.ctx.h, None, 4, 10, 8, torch.zeros(10, 9))
+    e.loss(y, m.labels)
+    e.logits(y)                      # takes the place of the gradient
+    with pytest.raises(RuntimeError):
+        e.backward()
+    fresh = TokenEnds(m.ctx.h, None, 4, 10, 8, torch.zeros(10, 8))
+    with pytest.raises(RuntimeError):
+        fresh.backward()
+    with pytest.raises(RuntimeError):
+        fresh.embed_backward(fresh.x)
+    fresh.close()
     m.close()
 
 

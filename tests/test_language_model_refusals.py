@@ -74,6 +74,14 @@ def test_pointers_inside_an_element(name, key):
         assert e.value.status == ALIGN
 
 
+def test_columns_of_a_table_are_bounded():
+    n = (1 << 30) + 1
+    for name, good, lds in (("ard_embedding_fwd", EMB_FWD, ("ldt", "ldy")), ("ard_embedding_bwd", EMB_BWD, ("lddy", "lddt"))):
+        with pytest.raises(ard.ArdError) as e:
+            getattr(ard, name)(CTX, *{**good, "N": n, lds[0]: n, lds[1]: n}.values(), stream=0)
+        assert e.value.status == UNSUPPORTED
+
+
 def test_work_of_the_delta_rule():
     size = ard.ard_delta_work_bytes
     assert size(1, 64, 8, 128, 128, False) == 0            # decoding takes none
