@@ -103,6 +103,7 @@ constexpr int EB_LIST = 1 << EB_PLACE_BITS;
 constexpr int EB_STEP = 4 * EB_THREADS;  // ids looked at at a time
 constexpr int EB_TOKENS = 1 << 18;       // most tokens of a CTA
 constexpr int EB_DIGIT = 6;              // bits of a token that a pass of the sort takes
+constexpr int EB_FEW = 256;              // lists up to here are sorted by counting
 
 struct EbShared {
   uint32_t key[2][EB_LIST];                    // token / groups, then the place in the list
@@ -131,7 +132,8 @@ struct EbDivisor {
   __device__ __forceinline__ explicit EbDivisor(uint32_t by) : d(by) {
     const int bits = 32 - __clz((int)(by - 1));
     shift = 31 + (by > 1 ? bits : 0);
-    magic = (uint32_t)(((1ull << shift) + by - 1) / by);
+    magic = (uint32_t)((double)(1ull << shift) / (double)by);  // (an integer division of 64 bits takes longer)
+    while ((unsigned long long)magic * by < (1ull << shift)) ++magic;
   }
   __device__ __forceinline__ uint32_t operator()(uint32_t x) const { return (uint32_t)(((unsigned long long)x * magic) >> shift); }
 };
@@ -157,10 +159,24 @@ __device__ __noinline__ void eb_write(const EbTable& g, long long token, float s
     else *reinterpret_cast<float4*>(out + j0) = make_float4(x[0], x[1], x[2], x[3]);
     return;
   }
+  const bool whole = VEC && g.wide && !add && j0 + 3 < g.c1 && (j0 + 4ll) * g.dp <= g.N;
+  if (whole) {  // four periods, which begin and end on 16 bytes
+    float x0 = x[0], x1 = x[1], x2 = x[2], x3 = x[3];
+    int d = 0;
+    for (int q = 0; q < g.dp; ++q) {
+      float v[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        v[i] = d == g.first ? x0 : 0.f;
+        if (++d == g.dp) d = 0, x0 = x1, x1 = x2, x2 = x3;
+      }
+      *reinterpret_cast<float4*>(out + (size_t)j0 * g.dp + 4 * q) = make_float4(v[0], v[1], v[2], v[3]);
+    }
+  }
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
     const int j = g.c0 + EbCols<VEC>::col(lane, k);
-    if (j >= g.c1) continue;
+    if (whole || j >= g.c1) continue;
     float* to = out + (size_t)j * g.dp;
     if (add) {
       atomicAdd(to + g.first, x[k]);
@@ -204,7 +220,7 @@ __global__ void __launch_bounds__(EB_THREADS, 1) embedding_bwd_kernel(const int3
   for (int i = t; i < (tokens + 31) / 32; i += EB_THREADS) sh.here[i] = sh.written[i] = 0u;
   using Raw = typename EmRaw<4 * sizeof(T)>::type;
   constexpr int EB_AHEAD = 32 / (int)sizeof(T);  // rows of dY in flight a warp: what 64 registers a thread hold
-  const bool full = VEC && (n & 3) == 0;  // a lane's columns are all there, or none is
+  const bool full = VEC && ((c1 - c0) & 3) == 0;  // a lane's columns are all there, or none is
   const bool on = c0 + 4 * lane < c1, fast = full && wide && dp == 1;
   const int mine = on ? 4 * lane : 0;
   const EbTable g = {dtable, lddt, dp, first, n, N, c0, c1, alpha, wide};
@@ -237,8 +253,23 @@ __global__ void __launch_bounds__(EB_THREADS, 1) embedding_bwd_kernel(const int3
   while ((1 << bits) < tokens) ++bits;
   auto work_off = [&](int m) {
     const int share = (m + EB_WARPS - 1) / EB_WARPS, from = min(m, warp * share), to = min(m, from + share);
+    const bool few = m <= EB_FEW;
     int src = 0;
-    for (int at = EB_PLACE_BITS; at < EB_PLACE_BITS + bits; at += EB_DIGIT) {
+    if (few) {  // a key's place is the number of smaller ones: no two are alike
+      if (t < m) {
+        const uint32_t k = sh.key[0][t];
+        int place = 0;
+#pragma unroll 4
+        for (int i = 0; i < m; i += 4) {
+          const uint4 q = *reinterpret_cast<const uint4*>(&sh.key[0][i]);
+          place += (q.x < k) + (i + 1 < m && q.y < k) + (i + 2 < m && q.z < k) + (i + 3 < m && q.w < k);
+        }
+        sh.key[1][place] = k;
+      }
+      eb_meet();
+      src = 1;
+    }
+    for (int at = EB_PLACE_BITS; !few && at < EB_PLACE_BITS + bits; at += EB_DIGIT) {
       // how often each digit comes up in a warp's share; the places follow from the counts of earlier digits and, for the same digit, earlier warps
       uint32_t* mine = sh.digits[warp];
       mine[lane] = mine[lane + 32] = 0u;
