@@ -105,6 +105,15 @@ constexpr int EB_TOKENS = 1 << 18;       // most tokens of a CTA
 constexpr int EB_DIGIT = 6;              // bits of a token that a pass of the sort takes
 constexpr int EB_FEW = 256;              // lists up to here are sorted by counting
 
+// What of a token's row of the gradient a warp writes: some kept columns, at most 128, and the dropped ones of their periods; the last CTA of columns has the row's end too.
+struct EbTable {
+  float* p;
+  int ld, dp, first, n, N, c0, c1;  // columns c0 .. c1 - 1 of the kept ones
+  float alpha;
+  int wide;  // rows on the grid of 16 bytes
+  __device__ __forceinline__ long long end() const { return c1 == n ? N : (long long)c1 * dp; }
+};
+
 struct EbShared {
   uint32_t key[2][EB_LIST];                    // token / groups, then the place in the list
   int32_t row[EB_LIST];
@@ -114,7 +123,8 @@ struct EbShared {
   uint32_t digits[EB_WARPS][1 << EB_DIGIT];    // how often each comes up in a warp's share, then where the share's begin
   uint32_t total[2];
   int count[EB_THREADS / 32];
-  int next;                                    // 32 tokens that nobody has written zeros for yet
+  int next;                                    // four tokens that nobody has written zeros for yet
+  EbTable table;
 };
 static_assert(sizeof(EbShared) <= 227 * 1024, "shared memory of an SM");
 
@@ -138,15 +148,8 @@ struct EbDivisor {
   __device__ __forceinline__ uint32_t operator()(uint32_t x) const { return (uint32_t)(((unsigned long long)x * magic) >> shift); }
 };
 
-// What of a token's row of the gradient a warp writes: some kept columns, at most 128, and the dropped ones of their periods; the last CTA of columns has the row's end too.
-struct EbTable {
-  float* p;
-  int ld, dp, first, n, N, c0, c1;  // columns c0 .. c1 - 1 of the kept ones
-  float alpha;
-  int wide;  // rows on the grid of 16 bytes
-  __device__ __forceinline__ long long end() const { return c1 == n ? N : (long long)c1 * dp; }
-};
-// (Out of line: it stands behind each of a round's rows, and sixteen copies of it do not fit the instruction cache.)
+// (Out of line: it stands behind each of a round's rows, and sixteen copies of it do not fit the instruction cache.  `g` lies in shared memory: local memory
+// would stand in line behind the stores of zeros.)
 template <bool VEC>
 __device__ __noinline__ void eb_write(const EbTable& g, long long token, float s0, float s1, float s2, float s3, bool add, int lane) {
   float* out = g.p + (size_t)token * g.ld;
@@ -223,7 +226,8 @@ __global__ void __launch_bounds__(EB_THREADS, 1) embedding_bwd_kernel(const int3
   const bool full = VEC && ((c1 - c0) & 3) == 0;  // a lane's columns are all there, or none is
   const bool on = c0 + 4 * lane < c1, fast = full && wide && dp == 1;
   const int mine = on ? 4 * lane : 0;
-  const EbTable g = {dtable, lddt, dp, first, n, N, c0, c1, alpha, wide};
+  const EbTable& g = sh.table;
+  if (t == 0) sh.table = {dtable, lddt, dp, first, n, N, c0, c1, alpha, wide};
   const EbDivisor by(groups);
   float* const fast_p = dtable + (size_t)group * lddt + c0 + mine;  // the group's first token
   const size_t fast_step = (size_t)groups * lddt;
@@ -545,7 +549,9 @@ __global__ void __launch_bounds__(EF_THREADS, 1) embedding_bwd_few_kernel(const 
   if (parts > 1) cg::this_cluster().sync();
   else __syncthreads();
   if (rank == 0 && warp == 0 && any) {
-    const EbTable g = {dtable, lddt, dp, first, n, N, c0, c0 + max(cols, 0), alpha, wide};
+    __shared__ EbTable table;
+    if (lane == 0) table = {dtable, lddt, dp, first, n, N, c0, c0 + max(cols, 0), alpha, wide};
+    __syncwarp();
     float x[4];
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
@@ -553,7 +559,7 @@ __global__ void __launch_bounds__(EF_THREADS, 1) embedding_bwd_few_kernel(const 
       x[k] = all[c];
       for (int p = 1; p < parts; ++p) x[k] += *cg::this_cluster().map_shared_rank(&all[c], p);
     }
-    eb_write<VEC>(g, token, x[0], x[1], x[2], x[3], accumulate, lane);
+    eb_write<VEC>(table, token, x[0], x[1], x[2], x[3], accumulate, lane);
   }
   if (parts > 1) {
     __syncwarp();
