@@ -203,13 +203,33 @@ __device__ __forceinline__ void dl_load(bf* s, int ld, const bf* g, long long st
     }
     return;
   }
-  for (int i = 0; i < ROUNDS; ++i, p += ROWS * step) {
-    bf e[8];
+  // Words of 4 bytes, shifted by an element where the piece begins inside one; a word is asked for if one of its elements is, else one that is there.
+  constexpr int MOST = OF <= 128 ? 8 : 2, AHEAD = ROUNDS < MOST ? ROUNDS : MOST;
+  auto word_of = [](const bf* x) { return reinterpret_cast<const uint32_t*>(reinterpret_cast<uintptr_t>(x) & ~(uintptr_t)3); };
+#pragma unroll 1
+  for (int i0 = 0; i0 < ROUNDS; i0 += AHEAD) {
+    uint32_t w[AHEAD][5];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) e[k] = r0 + i * ROWS < live && c + k < cols ? p[k] : __float2bfloat16_rn(0.f);
-    uint4 q;
-    memcpy(&q, e, 16);
-    *reinterpret_cast<uint4*>(d + i * ROWS * ld) = q;
+    for (int i = 0; i < AHEAD; ++i) {
+      const bf* x = p + i * (ROWS * step);
+      const int n = r0 + (i0 + i) * ROWS < live ? min(cols - c, 8) : 0, words = n > 0 ? (n + 1 + (int)((reinterpret_cast<uintptr_t>(x) >> 1) & 1u)) >> 1 : 0;
+      const uint32_t *from = word_of(x), *other = word_of(g);
+#pragma unroll
+      for (int k = 0; k < 5; ++k) w[i][k] = *(k < words ? from + k : other);
+    }
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) {
+      const int n = r0 + (i0 + i) * ROWS < live ? min(cols - c, 8) : 0, shift = (int)((reinterpret_cast<uintptr_t>(p + i * (ROWS * step)) >> 1) & 1u) * 16;
+      uint32_t q[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) q[k] = __funnelshift_r(w[i][k], w[i][k + 1], shift);
+      if (n < 8) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) q[k] = 2 * k + 1 < n ? q[k] : 2 * k < n ? q[k] & 0xFFFFu : 0u;
+      }
+      *reinterpret_cast<uint4*>(d + (i0 + i) * ROWS * ld) = make_uint4(q[0], q[1], q[2], q[3]);
+    }
+    p += AHEAD * (ROWS * step);
   }
 }
 // PARTS matrices [64][64] from the work.
