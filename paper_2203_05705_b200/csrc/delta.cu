@@ -16,9 +16,15 @@
 //
 // The state is fp32, and so are products that it goes through: an operand that is not bf16 to begin with is the sum of three bf16 matrices (24 bits), and
 // the products of their parts that fp32 can hold are added up.  Where a product ends in a bf16 output two parts are enough (17 bits, an
-// error of 2^-18 of a term where the output's rounding is 2^-9).  The products are small (64 x 32 x 128 a warp group, four in a row that wait for one another), which mma.sync takes from
-// registers and leaves in registers; a tcgen05 product would bring each result from tensor memory to registers, split it, and put it back, and
-// its 128 rows of an accumulator would leave half of the SMs without work at 64 heads.
+// error of 2^-18 of a term where the output's rounding is 2^-9).
+//
+// What goes from chunk to chunk is a chain: four products of 64 x 64 or 64 x 128 matrices with 16 columns of a state, each result split into parts
+// and the next one's operand.  mma.sync takes them from registers and leaves them in registers (measured here: 1000 multiply-adds a clock and SM).  A
+// tcgen05 product would bring each result from tensor memory to registers and its parts back, and its 128 rows of an accumulator would leave half of
+// the SMs without work at 64 sequences and heads.
+//
+// Time of 2048 steps, 8 sequences of 8 heads, 128 x 128: forward 250 us (systems 69, scan 190), backward 655 (systems 69, scan 216, gradients 378); of 16384 steps of
+// one sequence 850, a chunk in 3.0 us; of one step of 64 x 8 heads 14.7, for 67 MB.
 #include "ard_internal.h"
 #include "sm100_ptx.h"
 
@@ -321,6 +327,8 @@ __device__ __forceinline__ void dl_inverse_columns(Sh& sh, int warp, int lane) {
   }
 }
 
+// A CTA to a chunk of a head, four of them an SM, so that one's loads and barriers pass while others compute; K and Q come once, and what is made of them takes their
+// place in shared memory, which is busy for 60 % of the time: 2048 chunks of 128 columns 69 us.
 template <int DK>
 __global__ void __launch_bounds__(DL_THREADS, 4) delta_prep_kernel(const DlArgs a) {
   extern __shared__ __align__(16) uint8_t dl_smem[];
@@ -470,8 +478,10 @@ __global__ void __launch_bounds__(DL_THREADS, 4) delta_prep_kernel(const DlArgs 
 // in registers the way a product wants them, and so do the results that follow from them: E' = S' K', R' = b (V' - g E'), U' = R' T', S' += U' K.  Of a chunk's 64 steps each of the two
 // finishes 32; they meet three times a chunk, for the sums E, for what the earlier steps' R says to the later ones, and for U.  What all columns share (K, Q, T, P) lies in shared memory.
 // Beside each two stands a warp that fetches the next chunk and does what nobody waits for: forward the outputs, which take the state's and U's parts over shared
-// memory, backward what comes from dY alone.  (A warp to 16 columns, with all of the state: 217 / 260 us for 2048 x 8 x 8 in place of 150 / 190: the chain of a chunk's products is twice as
-// long, and a scheduler has one of them.)
+// memory, backward what comes from dY alone.  With 64 columns a CTA (2048 x 8 x 8: 128 CTAs) main warps and helpers have alike to do, 11 thousand cycles a chunk, of
+// which the tensor pipe is busy for 45 %; with 16 the helper's copies and products are the longer chain, 5.8 thousand.  (A warp to 16 columns, with all of the state:
+// 217 / 260 us for the two scans in place of 190 / 216, since its chain is twice as long and a scheduler has one of them; the state's parts in shared memory, eight
+// warps to a product: the forward call 599 us.)
 // Some of a CTA's warps, in branches of their own (0: all of them).
 __device__ __forceinline__ void dl_meet(int id, int threads) {
   __syncwarp();
@@ -709,7 +719,6 @@ __global__ void __launch_bounds__(96 * NP, 1) delta_scan_kernel(const DlArgs a) 
       const DlSteps& row = sh.row[chunk & 1];
       const bf* k0 = &sh.k[chunk & 1][0][0];
       const bf* tri = &sh.tri[0][0][0] + half * 32 * DL_LD64;  // this warp's steps
-      if (a.S) keep(a.S + ((long long)chunk * (a.B * a.heads) + n) * size + (long long)(c0 + 16 * pair) * a.Dk);
       dl_meet(0, ALL);
       float r[4][4];
       {
@@ -731,6 +740,7 @@ __global__ void __launch_bounds__(96 * NP, 1) delta_scan_kernel(const DlArgs a) 
           for (int j = 0; j < 4; ++j) r[i][j] = half ? e[i + 4][j] : e[i][j];
         }
       }
+      if (a.S) keep(a.S + ((long long)chunk * (a.B * a.heads) + n) * size + (long long)(c0 + 16 * pair) * a.Dk);
       dl_meet(states, 96);
 #pragma unroll
       for (int i = 0; i < 4; i += 2) {
@@ -1051,7 +1061,7 @@ __global__ void __launch_bounds__(96 * NP, 1) delta_back_kernel(const DlArgs a) 
 
 // ---- step by step -----------------------------------------------------------------------------------
 // The 8 warps of a CTA hold 128 rows of a state, 16 each, a lane the columns 4 lane + k (or lane + 32 k); a step needs one meeting of the warps, for what the old
-// state gives with k and with q: y = scale (f S^T q + u (k.q)).
+// state gives with k and with q: y = scale (f S^T q + u (k.q)).  Memory bounds it: a state is read and written once, 512 of them in 14.7 us (4.6 TB/s).
 template <bool VEC>
 __global__ void __launch_bounds__(DL_THREADS) delta_steps_kernel(const DlArgs a) {
   constexpr int ROWS = 16, WARPS = DL_THREADS / 32;
@@ -1196,6 +1206,8 @@ __global__ void __launch_bounds__(DL_THREADS) delta_steps_kernel(const DlArgs a)
 //   d log f_t = sum_{i >= t > j} W_ij + sum_{i >= t} a_i + sum_{j < t} c_j + g_C <D, S_0>,   W = N o Q K^T + M o K K^T,
 // a_i the parts of q_i.dq_i and k_i.dk_i that come from S_0, c_j that of k_j.dk_j that comes from D.  Each of them has f_t for a factor, so small
 // gates have small gradients to the last bit; (q.dq - v.dv) summed up backwards is the same in exact arithmetic and leaves a difference of large sums.
+// One CTA of 16 warps an SM, which holds everything of a chunk (222 KB).  2048 chunks of 128 x 128: 378 us; of a chunk's 46 thousand cycles 13 are its
+// loads (64 KB of S_0 and twice 64 KB of D; without the prefetch to L2 20), 17 what the products take at the tensor pipe's rate, the rest barriers between them and sums.
 constexpr int DL_GRAD_THREADS = 512, DL_GRAD_WARPS = DL_GRAD_THREADS / 32;
 
 template <int DK, int DV>

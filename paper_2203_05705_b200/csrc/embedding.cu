@@ -2,13 +2,17 @@
 //   Y[r][j] = alpha * table[ids[r]][col(j)],   dtable[v][col(j)] (+)= alpha * sum over r with ids[r] = v of dY[r][j],
 // col(j) = j, or the j-th kept unit of a row pattern.
 //
-// Memory bounds both.  The gradient needs each token's rows side by side; sorting all of them through global memory would take
-// several launches that hand one another the order.  Instead a CTA owns the tokens v = group (mod groups) and some columns: it
-// looks through all ids (they come from the L2: 4 bytes a position where a row of dY has thousands), keeps those that are
-// its own in shared memory, sorts them by token and position there, and adds their rows up in that order.  One launch, no scratch,
-// and the same bits every time: each sum is cut at the same places.  Equal shares of the sorted list go to the warps, so a token that
-// comes up in every other position costs no more than any other; tokens are dealt out in turn, so frequent ones, which
-// lie side by side in a dictionary sorted by frequency, fall to different CTAs.
+// Memory bounds both.  The gradient needs each token's rows side by side; sorting all of them through global memory would take several launches that
+// hand one another the order.  Instead a CTA owns the tokens v = group (mod groups) and at most 128 columns: it looks through all ids (they come from the L2: 4
+// bytes a position where a row of dY has thousands), keeps those that are its own in shared memory, sorts them there (by counting where they are few, else
+// digit by digit, either way with a token's rows in their order), and adds their rows up.  One launch, no scratch, and the same bits every time: each
+// sum is cut at the same places.  Equal shares of the sorted list go to the warps, so a token that comes up in every other position costs no more than any
+// other; tokens are dealt out in turn, so frequent ones, which lie side by side in a dictionary sorted by frequency, fall to different CTAs.  Zeros for
+// tokens that no position holds are written beside the sums, by warps that have nothing to add.
+//
+// 16384 positions, 32000 tokens, 2048 columns, bf16: lookup 20.7 us (134 MB), gradient 81 (329 MB: 4.1 TB/s; the list of a CTA, its sort and then its
+// rows follow one another).  700 positions, 8800 tokens, 750 of 1500 columns kept: 4.2 and 18.5, of which 7.4 the 53 MB of the gradient and 4 the start (a CTA has
+// looked at its ids 8000 cycles after it began).
 #include <cooperative_groups.h>
 
 #include "ard_internal.h"
