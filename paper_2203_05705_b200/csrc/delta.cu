@@ -482,6 +482,13 @@ __global__ void __launch_bounds__(DL_THREADS, 4) delta_prep_kernel(const DlArgs 
 // which the tensor pipe is busy for 45 %; with 16 the helper's copies and products are the longer chain, 5.8 thousand.  (A warp to 16 columns, with all of the state:
 // 217 / 260 us for the two scans in place of 190 / 216, since its chain is twice as long and a scheduler has one of them; the state's parts in shared memory, eight
 // warps to a product: the forward call 599 us.)
+// With one or two times 16 columns, where registers are left, a warp beside each helper does nothing but fetch.
+template <int NP>
+struct DlTeams {
+  static constexpr int HELP = 32 * NP, FETCH = NP <= 2 ? HELP : 0, FIRST = 3 * HELP, ALL = FIRST + FETCH;  // threads; FIRST: mains, and who brings the keys
+  // barriers: 0 the keys are there; three for each pair of mains; among helpers, or between helpers and who fetches for them
+  static constexpr int LATE = 1 + 3 * NP, EARLY = LATE + 1, PAST = LATE + 2, READ = LATE + 3;
+};
 // Some of a CTA's warps, in branches of their own (0: all of them).
 __device__ __forceinline__ void dl_meet(int id, int threads) {
   __syncwarp();
@@ -618,14 +625,17 @@ struct DlScanShared {
 };
 
 template <int DK, int NP>
-__global__ void __launch_bounds__(96 * NP, 1) delta_scan_kernel(const DlArgs a) {
-  constexpr int LDK = DK + 8, LDV = NP * 16 + 8, PT = DL_CHUNK * DL_LD64, HELP = 32 * NP, ALL = 96 * NP, HALF = DK / 2;
+__global__ void __launch_bounds__(DlTeams<NP>::ALL, 1) delta_scan_kernel(const DlArgs a) {
+  constexpr int LDK = DK + 8, LDV = NP * 16 + 8, PT = DL_CHUNK * DL_LD64, HALF = DK / 2;
+  using Teams = DlTeams<NP>;
+  constexpr int HELP = Teams::HELP, FIRST = Teams::FIRST, ALL = Teams::ALL;
+  constexpr bool FETCH = Teams::FETCH != 0;
   extern __shared__ __align__(16) uint8_t dl_smem[];
   auto& sh = *reinterpret_cast<DlScanShared<DK, NP>*>(dl_smem);
   pdl_launch_dependents();
   pdl_wait_prior_grids();
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, pair = warp % NP, half = warp / NP;  // half 2: the helper
-  const int states = 1 + pair, updates = 1 + NP + pair, early = 1 + 2 * NP + pair, helpers = 1 + 3 * NP;  // barriers
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, pair = warp % NP, half = warp / NP;  // half 2: the helper; 3: who fetches
+  const int states = 1 + pair, updates = 1 + NP + pair, early = 1 + 2 * NP + pair;  // barriers
   const int blocks = (a.Dv + NP * 16 - 1) / (NP * 16);
   const uint32_t n = blockIdx.x / (uint32_t)blocks;
   const long long size = (long long)a.Dk * a.Dv;
@@ -635,8 +645,8 @@ __global__ void __launch_bounds__(96 * NP, 1) delta_scan_kernel(const DlArgs a) 
   const int chunks = (u.len + DL_CHUNK - 1) / DL_CHUNK;
   const bf *Q = a.Q + (long long)u.head * a.Dk, *K = a.K + (long long)u.head * a.Dk, *V = a.V + (long long)u.head * a.Dv + c0;
   bf* Y = a.Y + (long long)u.head * a.Dv + c0;
-  if (half == 2) {
-    const int t = threadIdx.x - 2 * HELP;
+  if (half >= 2) {
+    const int t = threadIdx.x - (FETCH ? 3 : 2) * HELP;
     auto fetch_k = [&](int chunk) {
       if (chunk >= chunks) return;
       dl_move(a, u, chunk);
@@ -650,20 +660,49 @@ __global__ void __launch_bounds__(96 * NP, 1) delta_scan_kernel(const DlArgs a) 
       dl_load<NP * 16, HELP>(&sh.v[0][0], LDV, V + u.row0 * a.ldv, a.B * a.ldv, u.live, cols, a.vec_v, t);
       dl_load64<3, HELP>(&sh.tri[0][0][0], a.tri + u.unit * 3 * DL_SQ, t);
     };
-    fetch_k(0);
-    dl_commit();
-    fetch_others(0);
-    dl_commit();
-    dl_wait<1>();
-    if (chunks > 0) dl_tell(0, ALL);  // K is there: nobody else waits for this warp, whose outputs may lag behind
-    for (int chunk = 0; chunk < chunks; ++chunk) {
-      const int at = chunk & 1;
-      dl_wait<0>();
-      dl_meet(helpers, HELP);  // Q, V and T are there, and nobody reads P any more
-      dl_meet(states, 96);     // nor, since all have gone on to this chunk, the keys before it
-      fetch_k(chunk + 1);
-      dl_load64<2, HELP>(&sh.p[0][0][0], a.p + ((long long)chunk * (a.B * a.heads) + n) * 3 * DL_SQ, t);
+    auto fetch_p = [&](int chunk) { dl_load64<2, HELP>(&sh.p[0][0][0], a.p + ((long long)chunk * (a.B * a.heads) + n) * 3 * DL_SQ, t); };
+    if (half == (FETCH ? 3 : 2)) {
+      fetch_k(0);
       dl_commit();
+      fetch_others(0);
+      dl_commit();
+      dl_wait<1>();
+      if (chunks > 0) dl_tell(0, FIRST);  // K is there: nobody else waits for a helper, whose outputs may lag behind
+    }
+    if (half == 3) {
+      dl_wait<0>();
+      if (chunks > 0) dl_tell(Teams::LATE, 2 * HELP);  // Q, V and T are there
+      for (int chunk = 0; chunk < chunks; ++chunk) {
+        const bool more = chunk + 1 < chunks;
+        dl_meet(Teams::PAST, 2 * HELP);  // all have gone on to this chunk: nobody reads P any more, nor the keys before it
+        fetch_k(chunk + 1);
+        fetch_p(chunk);
+        dl_commit();
+        dl_wait<0>();
+        if (more) dl_tell(0, FIRST);
+        dl_tell(Teams::EARLY, 2 * HELP);
+        if (!more) break;
+        dl_meet(Teams::READ, 2 * HELP);  // nobody reads Q, V and T any more
+        fetch_others(chunk + 1);
+        dl_commit();
+        dl_wait<0>();
+        dl_tell(Teams::LATE, 2 * HELP);
+      }
+    }
+    for (int chunk = 0; half == 2 && chunk < chunks; ++chunk) {
+      const int at = chunk & 1;
+      if constexpr (FETCH) {
+        dl_meet(Teams::LATE, 2 * HELP);
+        dl_meet(states, 96);
+        dl_tell(Teams::PAST, 2 * HELP);
+      } else {
+        dl_wait<0>();
+        dl_meet(Teams::LATE, HELP);  // Q, V and T are there, and nobody reads P any more
+        dl_meet(states, 96);         // nor, since all have gone on to this chunk, the keys before it
+        fetch_k(chunk + 1);
+        fetch_p(chunk);
+        dl_commit();
+      }
       float o[8][4] = {};
 #pragma unroll
       for (int kd = 0; kd < DK / 16; ++kd) {
@@ -678,11 +717,16 @@ __global__ void __launch_bounds__(96 * NP, 1) delta_scan_kernel(const DlArgs a) 
         o[i][0] *= g.x, o[i][1] *= g.y, o[i][2] *= g.x, o[i][3] *= g.y;
       }
       dl_meet(updates, 96);
-      dl_wait<0>();
-      dl_meet(helpers, HELP);  // P and the next keys are there, and nobody reads Q, V and T any more
-      if (chunk + 1 < chunks) dl_tell(0, ALL);
-      fetch_others(chunk + 1);
-      dl_commit();
+      if constexpr (FETCH) {
+        if (chunk + 1 < chunks) dl_tell(Teams::READ, 2 * HELP);
+        dl_meet(Teams::EARLY, 2 * HELP);  // P is there
+      } else {
+        dl_wait<0>();
+        dl_meet(Teams::LATE, HELP);  // P and the next keys are there, and nobody reads Q, V and T any more
+        if (chunk + 1 < chunks) dl_tell(0, FIRST);
+        fetch_others(chunk + 1);
+        dl_commit();
+      }
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
         uint32_t x[2][4];
@@ -719,7 +763,7 @@ __global__ void __launch_bounds__(96 * NP, 1) delta_scan_kernel(const DlArgs a) 
       const DlSteps& row = sh.row[chunk & 1];
       const bf* k0 = &sh.k[chunk & 1][0][0];
       const bf* tri = &sh.tri[0][0][0] + half * 32 * DL_LD64;  // this warp's steps
-      dl_meet(0, ALL);
+      dl_meet(0, FIRST);
       float r[4][4];
       {
         float e[8][4] = {};
@@ -837,14 +881,17 @@ struct DlBackShared {
 };
 
 template <int DK, int NP>
-__global__ void __launch_bounds__(96 * NP, 1) delta_back_kernel(const DlArgs a) {
-  constexpr int LDK = DK + 8, LDV = NP * 16 + 8, PT = DL_CHUNK * DL_LD64, HELP = 32 * NP, ALL = 96 * NP, HALF = DK / 2;
+__global__ void __launch_bounds__(DlTeams<NP>::ALL, 1) delta_back_kernel(const DlArgs a) {
+  constexpr int LDK = DK + 8, LDV = NP * 16 + 8, PT = DL_CHUNK * DL_LD64, HALF = DK / 2;
+  using Teams = DlTeams<NP>;
+  constexpr int HELP = Teams::HELP, FIRST = Teams::FIRST, ALL = Teams::ALL;
+  constexpr bool FETCH = Teams::FETCH != 0;
   extern __shared__ __align__(16) uint8_t dl_smem[];
   auto& sh = *reinterpret_cast<DlBackShared<DK, NP>*>(dl_smem);
   pdl_launch_dependents();
   pdl_wait_prior_grids();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, pair = warp % NP, half = warp / NP;
-  const int states = 1 + pair, updates = 1 + NP + pair, late = 1 + 2 * NP + pair, helpers = 1 + 3 * NP;
+  const int states = 1 + pair, updates = 1 + NP + pair, late = 1 + 2 * NP + pair;
   const int blocks = (a.Dv + NP * 16 - 1) / (NP * 16);
   const uint32_t n = blockIdx.x / (uint32_t)blocks;
   const long long size = (long long)a.Dk * a.Dv;
@@ -854,8 +901,8 @@ __global__ void __launch_bounds__(96 * NP, 1) delta_back_kernel(const DlArgs a) 
   const int chunks = (u.len + DL_CHUNK - 1) / DL_CHUNK;
   const bf *Q = a.Q + (long long)u.head * a.Dk, *K = a.K + (long long)u.head * a.Dk, *dY = a.dY + (long long)u.head * a.Dv + c0;
   bf* dV = a.dV + (long long)u.head * a.Dv + c0;
-  if (half == 2) {
-    const int t = threadIdx.x - 2 * HELP;
+  if (half >= 2) {
+    const int t = threadIdx.x - (FETCH ? 3 : 2) * HELP;
     auto fetch_k = [&](int chunk) {
       if (chunk < 0) return;
       dl_move(a, u, chunk);
@@ -907,32 +954,68 @@ __global__ void __launch_bounds__(96 * NP, 1) delta_back_kernel(const DlArgs a) 
         if constexpr (DK > 64) dl_step<4, 8, 3, 1, 2, true>(y, x, &sh.q[0][0], LDK, 0, 16 * k, lane);
       }
     };
-    if (chunks > 0) {
+    if (half == (FETCH ? 3 : 2) && chunks > 0) {
       fetch_k(chunks - 1);
       fetch_mine(chunks - 1);
+      dl_commit();
       fetch_tri(chunks - 1);
       dl_commit();
+      dl_wait<1>();
+      if (!FETCH) dl_meet(Teams::LATE, HELP);
+      dl_tell(0, FIRST);  // K is there
+    }
+    if (half == 3 && chunks > 0) {
+      dl_tell(Teams::EARLY, 2 * HELP);  // P, Q and dY are there
       dl_wait<0>();
-      dl_meet(helpers, HELP);
-      dl_tell(0, ALL);  // K is there
+      dl_tell(Teams::LATE, 2 * HELP);   // T is there
+      for (int chunk = chunks - 1; chunk > 0; --chunk) {
+        dl_meet(Teams::PAST, 2 * HELP);  // all have gone on to this chunk: nobody reads P, Q and dY any more, nor the keys behind it
+        fetch_k(chunk - 1);
+        fetch_mine(chunk - 1);
+        dl_commit();
+        dl_wait<0>();
+        dl_tell(0, FIRST);
+        dl_tell(Teams::EARLY, 2 * HELP);
+        dl_meet(Teams::READ, 2 * HELP);  // nobody reads T any more
+        fetch_tri(chunk - 1);
+        dl_commit();
+        dl_wait<0>();
+        dl_tell(Teams::LATE, 2 * HELP);
+      }
+    }
+    if (half == 2 && chunks > 0) {
+      if (FETCH) dl_meet(Teams::EARLY, 2 * HELP);
       ahead(chunks - 1);
     }
-    for (int chunk = chunks - 1; chunk >= 0; --chunk) {
-      dl_wait<0>();
-      dl_meet(helpers, HELP);  // T is there, and nobody reads P, Q and dY any more
-      dl_meet(states, 96);     // nor, since all have gone on to this chunk, the keys behind it and the last Y
+    for (int chunk = chunks - 1; half == 2 && chunk >= 0; --chunk) {
+      if constexpr (FETCH) {
+        dl_meet(Teams::LATE, 2 * HELP);
+      } else {
+        dl_wait<0>();
+        dl_meet(Teams::LATE, HELP);  // T is there, and nobody reads P, Q and dY any more
+      }
+      dl_meet(states, 96);  // nor, since all have gone on to this chunk, the keys behind it and the last Y
+      if (FETCH && chunk > 0) dl_tell(Teams::PAST, 2 * HELP);
 #pragma unroll
       for (int i = 0; i < DK / 8; ++i) sh.y[pair][i][lane] = make_float4(y[i][0], y[i][1], y[i][2], y[i][3]);
-      fetch_k(chunk - 1);
-      fetch_mine(chunk - 1);
-      dl_commit();
+      if constexpr (!FETCH) {
+        fetch_k(chunk - 1);
+        fetch_mine(chunk - 1);
+        dl_commit();
+      }
       dl_meet(updates, 96);
-      dl_wait<0>();
-      dl_meet(helpers, HELP);  // the next keys, P, Q and dY are there, and nobody reads T any more
-      if (chunk == 0) break;
-      dl_tell(0, ALL);
-      fetch_tri(chunk - 1);
-      dl_commit();
+      if constexpr (FETCH) {
+        if (chunk == 0) break;
+        dl_tell(Teams::READ, 2 * HELP);
+        dl_meet(Teams::EARLY, 2 * HELP);
+      } else {
+        dl_wait<0>();
+        dl_meet(Teams::LATE, HELP);  // the next keys, P, Q and dY are there, and nobody reads T any more
+        if (chunk == 0) break;
+        dl_tell(0, FIRST);
+        fetch_tri(chunk - 1);
+        dl_commit();
+      }
       ahead(chunk - 1);
     }
   } else {
@@ -946,7 +1029,7 @@ __global__ void __launch_bounds__(96 * NP, 1) delta_back_kernel(const DlArgs a) 
       const bf* k0 = &sh.k[chunk & 1][0][0];
       const bf* tri = &sh.tri[0][0][0] + half * 32;  // this warp's steps
       dl_move(a, u, chunk);
-      dl_meet(0, ALL);
+      dl_meet(0, FIRST);
       float r[4][4];
       {
         float f[8][4] = {};
@@ -1652,7 +1735,9 @@ __global__ void __launch_bounds__(DL_GRAD_THREADS) delta_grad_kernel(const DlArg
   }
 }
 
-constexpr int DL_STEPS = 16;  // up to so many steps go one by one
+// Up to so many steps go one by one, which needs no workspace: 17 steps of 64 x 8 states of 128 x 128 take 83 us so and 86 as a chunk, of 4 x 8 states 33 and 21 (there 9
+// steps would be the edge).
+constexpr int DL_STEPS = 16;
 
 inline bool dl_on16(const void* p, long long ld, int head) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld % 8 == 0 && head % 8 == 0; }
 inline long long dl_units(int T, int B, int heads) { return (long long)((T + DL_CHUNK - 1) / DL_CHUNK) * B * heads; }
@@ -1700,8 +1785,8 @@ ard_status dl_run(ard_ctx* ctx, K kern, long long grid, int threads, size_t smem
 template <int DK, int NP>
 ard_status dl_scan(ard_ctx* ctx, const DlArgs& a, bool backward, cudaStream_t s) {
   const long long grid = (long long)a.B * a.heads * ((a.Dv + NP * 16 - 1) / (NP * 16));
-  return backward ? dl_run(ctx, delta_back_kernel<DK, NP>, grid, 96 * NP, sizeof(DlBackShared<DK, NP>), a, s)
-                  : dl_run(ctx, delta_scan_kernel<DK, NP>, grid, 96 * NP, sizeof(DlScanShared<DK, NP>), a, s);
+  return backward ? dl_run(ctx, delta_back_kernel<DK, NP>, grid, DlTeams<NP>::ALL, sizeof(DlBackShared<DK, NP>), a, s)
+                  : dl_run(ctx, delta_scan_kernel<DK, NP>, grid, DlTeams<NP>::ALL, sizeof(DlScanShared<DK, NP>), a, s);
 }
 template <int DK>
 ard_status dl_chunks(ard_ctx* ctx, const DlArgs& a, bool backward, cudaStream_t s) {
