@@ -23,8 +23,8 @@
 // tcgen05 product would bring each result from tensor memory to registers and its parts back, and its 128 rows of an accumulator would leave half of
 // the SMs without work at 64 sequences and heads.
 //
-// Time of 2048 steps, 8 sequences of 8 heads, 128 x 128: forward 250 us (systems 69, scan 190), backward 655 (systems 69, scan 216, gradients 378); of 16384 steps of
-// one sequence 850, a chunk in 3.0 us; of one step of 64 x 8 heads 14.7, for 67 MB.
+// Time of 2048 steps, 8 sequences of 8 heads, 128 x 128: forward 250 us (systems 69, scan 185), backward 655 (systems 69, scan 214, gradients 378); of 16384 steps of
+// one sequence 773, a chunk in 2.7 us; of one step of 64 x 8 heads 14.7, for 67 MB.
 #include "ard_internal.h"
 #include "sm100_ptx.h"
 
@@ -474,15 +474,16 @@ __global__ void __launch_bounds__(DL_THREADS, 4) delta_prep_kernel(const DlArgs 
 }
 
 // ---- from chunk to chunk ----------------------------------------------------------------------------
-// Two warps hold 16 columns of the state, transposed, as accumulators [16 columns][DK / 2]: one the first half of its rows, one the second.  As rows of a left operand they lie
-// in registers the way a product wants them, and so do the results that follow from them: E' = S' K', R' = b (V' - g E'), U' = R' T', S' += U' K.  Of a chunk's 64 steps each of the two
-// finishes 32; they meet three times a chunk, for the sums E, for what the earlier steps' R says to the later ones, and for U.  What all columns share (K, Q, T, P) lies in shared memory.
+// Two warps hold 16 columns of the state, transposed, as accumulators [16 columns][DK / 2]: one the first half of its rows, one the second.  As rows of a left
+// operand they lie in registers the way a product wants them, and so do the results that follow from them: E' = S' K', R' = b (V' - g E'), U' = R' T', S' += U' K.
+// Of a chunk's 64 steps each of the two finishes 32; they meet three times a chunk, for the sums E, for what the earlier steps' R says to the later ones, and for U.
+// What all columns share (K, Q, T, P) lies in shared memory.
 // Beside each two stands a warp that fetches the next chunk and does what nobody waits for: forward the outputs, which take the state's and U's parts over shared
 // memory, backward what comes from dY alone.  With 64 columns a CTA (2048 x 8 x 8: 128 CTAs) main warps and helpers have alike to do, 11 thousand cycles a chunk, of
-// which the tensor pipe is busy for 45 %; with 16 the helper's copies and products are the longer chain, 5.8 thousand.  (A warp to 16 columns, with all of the state:
-// 217 / 260 us for the two scans in place of 190 / 216, since its chain is twice as long and a scheduler has one of them; the state's parts in shared memory, eight
-// warps to a product: the forward call 599 us.)
-// With one or two times 16 columns, where registers are left, a warp beside each helper does nothing but fetch.
+// which the tensor pipe is busy for 45 %.  With one or two times 16 columns the helper's copies and products were the longer chain, and registers are left: there a warp
+// beside each helper does nothing but fetch (16384 x 1 x 8 forward 842 -> 773 us, 2.7 a chunk).  (A warp to 16 columns, with all of the state: 217 / 260 us for the two
+// scans of 2048 x 8 x 8 in place of 185 / 214, since its chain is twice as long and a scheduler has one of them; the state's parts in shared memory, eight warps to a
+// product: the forward call 599 us.)
 template <int NP>
 struct DlTeams {
   static constexpr int HELP = 32 * NP, FETCH = NP <= 2 ? HELP : 0, FIRST = 3 * HELP, ALL = FIRST + FETCH;  // threads; FIRST: mains, and who brings the keys
