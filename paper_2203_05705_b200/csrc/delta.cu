@@ -190,6 +190,16 @@ __device__ __forceinline__ void dl_wait() {
   asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory");
 }
 
+// A word, or else its first element, or else nothing; without a branch that the load would wait in.
+__device__ __forceinline__ uint32_t dl_word(const bf* p, bool whole, bool one) {
+  uint32_t r;
+  asm volatile("{ .reg .pred a, b; setp.ne.b32 a, %2, 0; setp.ne.b32 b, %3, 0; mov.b32 %0, 0; @a ld.global.b32 %0, [%1]; @b ld.global.u16 %0, [%1]; }"
+               : "=&r"(r)
+               : "l"(p), "r"((int)whole), "r"((int)(one && !whole))
+               : "memory");
+  return r;
+}
+
 // [64][cols] of a matrix whose rows are `step` elements apart, on its way to shared memory with pitch ld; rows from `live` on and columns up to PAD are
 // zeros.  Rows off the grid of 16 bytes go through registers, at once.  By threads t of OF.
 template <int PAD, int OF>
@@ -209,31 +219,25 @@ __device__ __forceinline__ void dl_load(bf* s, int ld, const bf* g, long long st
     }
     return;
   }
-  // Words of 4 bytes, shifted by an element where the piece begins inside one; a word is asked for if one of its elements is, else one that is there.
+  // Words of 4 bytes, shifted by an element where the piece begins inside one; of words that reach over its ends the one element that is in it.
   constexpr int MOST = OF <= 128 ? 8 : 2, AHEAD = ROUNDS < MOST ? ROUNDS : MOST;
-  auto word_of = [](const bf* x) { return reinterpret_cast<const uint32_t*>(reinterpret_cast<uintptr_t>(x) & ~(uintptr_t)3); };
 #pragma unroll 1
   for (int i0 = 0; i0 < ROUNDS; i0 += AHEAD) {
     uint32_t w[AHEAD][5];
 #pragma unroll
     for (int i = 0; i < AHEAD; ++i) {
       const bf* x = p + i * (ROWS * step);
-      const int n = r0 + (i0 + i) * ROWS < live ? min(cols - c, 8) : 0, words = n > 0 ? (n + 1 + (int)((reinterpret_cast<uintptr_t>(x) >> 1) & 1u)) >> 1 : 0;
-      const uint32_t *from = word_of(x), *other = word_of(g);
+      const int n = r0 + (i0 + i) * ROWS < live ? min(cols - c, 8) : 0, odd = (int)((reinterpret_cast<uintptr_t>(x) >> 1) & 1u);
+      w[i][0] = dl_word(x, !odd && n > 1, n > 0);
 #pragma unroll
-      for (int k = 0; k < 5; ++k) w[i][k] = *(k < words ? from + k : other);
+      for (int k = 1; k < 5; ++k) w[i][k] = dl_word(x + 2 * k - odd, 2 * k - odd + 1 < n, 2 * k - odd < n);
     }
 #pragma unroll
     for (int i = 0; i < AHEAD; ++i) {
-      const int n = r0 + (i0 + i) * ROWS < live ? min(cols - c, 8) : 0, shift = (int)((reinterpret_cast<uintptr_t>(p + i * (ROWS * step)) >> 1) & 1u) * 16;
-      uint32_t q[4];
-#pragma unroll
-      for (int k = 0; k < 4; ++k) q[k] = __funnelshift_r(w[i][k], w[i][k + 1], shift);
-      if (n < 8) {
-#pragma unroll
-        for (int k = 0; k < 4; ++k) q[k] = 2 * k + 1 < n ? q[k] : 2 * k < n ? q[k] & 0xFFFFu : 0u;
-      }
-      *reinterpret_cast<uint4*>(d + (i0 + i) * ROWS * ld) = make_uint4(q[0], q[1], q[2], q[3]);
+      const int shift = (int)((reinterpret_cast<uintptr_t>(p + i * (ROWS * step)) >> 1) & 1u) * 16;
+      w[i][0] <<= shift;
+      *reinterpret_cast<uint4*>(d + (i0 + i) * ROWS * ld) = make_uint4(__funnelshift_r(w[i][0], w[i][1], shift), __funnelshift_r(w[i][1], w[i][2], shift),
+                                                                       __funnelshift_r(w[i][2], w[i][3], shift), __funnelshift_r(w[i][3], w[i][4], shift));
     }
     p += AHEAD * (ROWS * step);
   }
