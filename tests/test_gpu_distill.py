@@ -252,3 +252,14 @@ def test_on_a_stream_and_from_a_graph(V):
         graph.replay()
         case.check(host(case.z))
     ctx.close()
+
+
+@pytest.mark.parametrize("dtype,rows,V,k", [(BF16, 40, 80, 80), (F32, 9, 100, 128), (BF16, 20, 700, 65), (F32, 7, 900, 128), (BF16, 6, 2000, 100), (BF16, 5, 4096, 128),
+                                            (F32, 3, 2040, 90), (BF16, 5, 300, 129)])
+@pytest.mark.parametrize("tau", [1.0, 2.7])
+def test_many_entries_over_short_rows(dtype, rows, V, k, tau):
+    ctx = Ctx()
+    case = Case(dtype, rows, V, k, tau=tau, hard=0.4, soft=0.6, pad=1, off=1)
+    case.call(ctx)
+    case.check(host(case.z[:, :V]))
+    ctx.close()
