@@ -864,7 +864,8 @@ ard_status ard_embedding_bwd(ard_ctx* ctx, const ard_pattern* pat, ard_dtype dty
  * without probability; a row of nothing else gives NaN.  Z, dZ of element type `dtype`, from any whole element on; sums are fp32.
  * Uses the context's scratch.  Errors: ARD_ERR_INVALID_ARG (NULL, negative size, dtype, tau not positive or not finite, also its inverse, hard or soft not
  * finite), ARD_ERR_SHAPE (leading dimension below V or k), ARD_ERR_ALIGNMENT (a pointer inside an element), ARD_ERR_UNSUPPORTED
- * (k above 1024, rows above 2^30, a row of more than 1.2 MB).  Asynchronous. */
+ * (k above 1024, rows above 2^30, a row that eight SMs cannot hold: above 1.82 MB without a teacher, 1.30 MB with k =
+ * 1024).  Asynchronous. */
 ard_status ard_distill_loss(ard_ctx* ctx, ard_dtype dtype, int rows, int V, const void* Z, int ldz, const int32_t* labels, int k,
                             const int32_t* teacher_ids, const float* teacher_logits, int ldk, float tau, float hard, float soft,
                             const float* row_weight, float* loss, float* total, void* dZ, int lddz, void* cuda_stream);

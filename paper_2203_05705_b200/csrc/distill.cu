@@ -418,6 +418,9 @@ struct DsTeam {
 };
 template <int TEAMS>
 struct DsShared {
+  // A slot serves any team's rows, a parity tells a wait one phase from the next alone: so a row's barrier `full` goes by the row's number and is one team's, which
+  // meets every phase of it.  By slots, a team could ask for a phase while the one before, another team's, was yet to complete, and take that for its own.
+  static_assert(DS_SLOTS % TEAMS == 0, "a barrier to a team");
   unsigned long long full[DS_SLOTS], empty[DS_SLOTS];
   DsInfo info[DS_SLOTS];
   float edge[DS_SLOTS][32];  // a row's loose logits
@@ -484,7 +487,7 @@ __global__ void __launch_bounds__(TEAMS * (WORKERS + 64) + 32, 1) distill_ring_k
       __syncwarp();
       if (lane == 0) {
         sh.info[slot] = {w, label, skip ? 1 : 0};
-        const uint32_t bytes = skip ? 0u : (uint32_t)max(0, min(row.vecs - v0, a.slice)) * 16u, bar = smem_u32(&sh.full[slot]);
+        const uint32_t bytes = skip ? 0u : (uint32_t)max(0, min(row.vecs - v0, a.slice)) * 16u, bar = smem_u32(&sh.full[n % DS_SLOTS]);
         if (bytes == 0u) {
           mbar_arrive(bar);
         } else {
@@ -632,7 +635,7 @@ __global__ void __launch_bounds__(TEAMS * (WORKERS + 64) + 32, 1) distill_ring_k
         T* dz = a.dZ ? (T*)a.dZ + r * a.lddz : nullptr;
         const DsRow<T> row(z, a.V);
         const int mine = max(0, min(row.vecs - v0, a.slice));
-        mbar_wait(smem_u32(&sh.full[slot]), (uint32_t)(all / a.slots) & 1u, &sh.abort, a.status);
+        mbar_wait(smem_u32(&sh.full[all % DS_SLOTS]), (uint32_t)(all / DS_SLOTS) & 1u, &sh.abort, a.status);
         const DsInfo info = sh.info[slot];
         const uint4* zs = reinterpret_cast<const uint4*>(ds_smem + (size_t)slot * a.slot_bytes);
         const bool edged = rank == 0 && tw < row.loose && !info.skip;
