@@ -81,6 +81,7 @@ struct DlSteps {                 // what the scans read
 struct DlRow : DlSteps {
   float rk[DL_CHUNK], rq[DL_CHUNK];        // 1 / |k|, 1 / |q|
   float f[DL_CHUNK], rest[DL_CHUNK];       // f, 1 - f
+  float closed[DL_CHUNK];                  // 1 - b, to some units of its own size: a gate near 1 has its gradient from it
   float last[DL_CHUNK];                    // G_Ci
   float from[DL_CHUNK], to[DL_CHUNK];      // a_i: from its block's first step to i; b_j: from behind j to its block's last step
   float block[4];                          // a whole block
@@ -174,7 +175,7 @@ __device__ __forceinline__ void dl_put(bf* s, int stride, float x, float y) {
   for (int i = 0; i < PARTS; ++i) *reinterpret_cast<uint32_t*>(s + i * stride) = w[i];
 }
 
-// s(z) and 1 - s(z), each to a few units of its own size.
+// s(z) and 1 - s(z), each to a few units of its own size, the smaller one to |z| of them more: the exponential's argument is rounded.
 __device__ __forceinline__ void dl_gate(float z, float& f, float& rest) {
   const float e = __expf(-fabsf(z)), big = __frcp_rn(1.f + e), small = e * big;
   f = z >= 0.f ? big : small;
@@ -347,12 +348,13 @@ __global__ void __launch_bounds__(DL_THREADS, 4) delta_prep_kernel(const DlArgs 
   dl_load<DK, DL_THREADS>(&sh.q[0][0], DK + 8, a.Q + u.row0 * a.ldq + (long long)u.head * a.Dk, a.B * a.ldq, u.live, a.Dk, a.vec_q, t);
   dl_commit();
   if (t < DL_CHUNK) {
-    float f = 1.f, rest = 0.f, beta = 0.f, no;
+    float f = 1.f, rest = 0.f, beta = 0.f, closed = 1.f;
     if (t < u.live) {
       const long long r = (u.row0 + (long long)t * a.B) * a.ldz + u.head;
       dl_gate(__bfloat162float(a.Zf[r]), f, rest);
-      dl_gate(__bfloat162float(a.Zb[r]), beta, no);
+      dl_gate(__bfloat162float(a.Zb[r]), beta, closed);
     }
+    sh.row.closed[t] = closed;
     sh.row.f[t] = f;
     sh.row.rest[t] = rest;
     sh.row.beta[t] = beta;
@@ -1735,7 +1737,7 @@ __global__ void __launch_bounds__(DL_GRAD_THREADS) delta_grad_kernel(const DlArg
       if (r >= u.live) continue;
       const long long z = (u.row0 + (long long)r * a.B) * a.lddz + u.head;
       a.dZf[z] = __float2bfloat16_rn((sh.seen[r] + (h ? x1 : x0) + c + ds) * sh.row.rest[r]);
-      a.dZb[z] = __float2bfloat16_rn(sh.xu[r] * (1.f - sh.row.beta[r]));
+      a.dZb[z] = __float2bfloat16_rn(sh.xu[r] * sh.row.closed[r]);
     }
   }
 }
