@@ -752,6 +752,7 @@ ard_status ard_glr_backward(ard_ctx* ctx, const ard_pattern* pat, ard_dtype dtyp
  *         starts from, or NULL when there is none.
  *   work  device memory of ard_delta_work_bytes(T, B, heads, Dk, Dv, 0 or, for the backward call, 1) bytes, from any byte on; holds nothing between
  *         calls, so one piece serves many layers whose calls are ordered.  NULL where that is 0 (decoding).
+ * Dk or Dv may be 0: sums over no keys, or for no values, are zero, and so are the gates' gradients.
  * Decoding is T = 1 with hT = h0.  A gate of -infinity (f = 0) starts anew.  Steps are computed ARD_DELTA_CHUNK at a time, so what a NaN or an
  * infinity in a sequence's inputs makes of its own step and later ones it may make of the same chunk's earlier ones too.  Q, K, V, Z, Y are ARD_BF16, from any whole element on (fastest
  * with 16-byte aligned pointers and rows, Dk and Dv multiples of 8); gates, states and their products are fp32.  Y must not overlap an input.

@@ -1742,6 +1742,20 @@ __global__ void __launch_bounds__(DL_GRAD_THREADS) delta_grad_kernel(const DlArg
   }
 }
 
+// Heads without keys' or without values' columns: sums over nothing, and gates that nothing depends on.
+struct DlZeros {
+  bf* p[5];
+  long long step[5];
+  int cols[5];
+};
+__global__ void __launch_bounds__(DL_THREADS) delta_zeros_kernel(const DlZeros z, long long rows) {
+  pdl_launch_dependents();
+  pdl_wait_prior_grids();
+  for (int m = 0; m < 5; ++m)
+    for (long long i = (long long)blockIdx.x * DL_THREADS + threadIdx.x; i < rows * z.cols[m]; i += (long long)gridDim.x * DL_THREADS)
+      z.p[m][i / z.cols[m] * z.step[m] + i % z.cols[m]] = __float2bfloat16_rn(0.f);
+}
+
 // Up to so many steps go one by one, which needs no workspace: 17 steps of 64 x 8 states of 128 x 128 take 83 us so and 86 as a chunk, of 4 x 8 states 33 and 21 (there 9
 // steps would be the edge).
 constexpr int DL_STEPS = 16;
@@ -1789,6 +1803,16 @@ ard_status dl_run(ard_ctx* ctx, K kern, long long grid, int threads, size_t smem
   ARD_CUDA_OK(cudaGetLastError());
   return ARD_OK;
 }
+ard_status dl_zeros(ard_ctx* ctx, const DlZeros& z, long long rows, cudaStream_t s) {
+  int most = 0;
+  for (int cols : z.cols) most = cols > most ? cols : most;
+  if (rows == 0 || most == 0) return ARD_OK;
+  const long long want = (rows * most + DL_THREADS - 1) / DL_THREADS, room = 8ll * ctx->sm_count;
+  ARD_CUDA_OK(ard_launch(ctx, delta_zeros_kernel, dim3((unsigned)(want < room ? want : room)), dim3(DL_THREADS), 0, s, z, rows));
+  ctx->launches++;
+  ARD_CUDA_OK(cudaGetLastError());
+  return ARD_OK;
+}
 template <int DK, int NP>
 ard_status dl_scan(ard_ctx* ctx, const DlArgs& a, bool backward, cudaStream_t s) {
   const long long grid = (long long)a.B * a.heads * ((a.Dv + NP * 16 - 1) / (NP * 16));
@@ -1825,7 +1849,8 @@ size_t delta_work_bytes(int T, int B, int heads, int Dk, int Dv, bool backward) 
 ard_status launch_delta_forward(ard_ctx* ctx, int T, int B, int heads, int Dk, int Dv, float scale, float eps, const void* Q, int ldq, const void* K, int ldk,
                                 const void* V, int ldv, const void* Zf, const void* Zb, int ldz, const int32_t* lens, const float* h0, void* Y, int ldy,
                                 float* hT, float* S, void* work, cudaStream_t s) {
-  if (B == 0 || heads == 0 || Dv == 0 || Dk == 0) return ARD_OK;
+  if (B == 0 || heads == 0 || Dv == 0) return ARD_OK;
+  if (Dk == 0) return dl_zeros(ctx, {{(bf*)Y}, {ldy}, {heads * Dv}}, (long long)T * B, s);
   DlArgs a = {};
   a.T = T, a.B = B, a.heads = heads, a.Dk = Dk, a.Dv = Dv, a.scale = scale, a.eps = eps;
   a.Q = (const bf*)Q, a.K = (const bf*)K, a.V = (const bf*)V, a.ldq = ldq, a.ldk = ldk, a.ldv = ldv;
@@ -1848,7 +1873,10 @@ ard_status launch_delta_backward(ard_ctx* ctx, int T, int B, int heads, int Dk, 
                                  const void* V, int ldv, const void* Zf, const void* Zb, int ldz, const int32_t* lens, const float* S, const void* dY,
                                  int lddy, const float* dhT, void* dQ, int lddq, void* dK, int lddk, void* dV, int lddv, void* dZf, void* dZb, int lddz,
                                  float* dh0, void* work, cudaStream_t s) {
-  if (B == 0 || heads == 0 || Dv == 0 || Dk == 0) return ARD_OK;
+  if (B == 0 || heads == 0) return ARD_OK;
+  if (Dk == 0 || Dv == 0)
+    return dl_zeros(ctx, {{(bf*)dQ, (bf*)dK, (bf*)dV, (bf*)dZf, (bf*)dZb}, {lddq, lddk, lddv, lddz, lddz}, {heads * Dk, heads * Dk, heads * Dv, heads, heads}},
+                    (long long)T * B, s);
   if (T == 0) {
     const size_t bytes = (size_t)B * heads * Dk * Dv * 4;
     if (dh0 && dhT && dh0 != dhT) ARD_CUDA_OK(cudaMemcpyAsync(dh0, dhT, bytes, cudaMemcpyDeviceToDevice, s));
