@@ -35,6 +35,7 @@ class TokenEnds:
         self.z = new(rows, self.ldz, dtype=BF)
         self.losses, self.total = new(rows), new(1)
         self.ids = self.y = None
+        self.lookups, self.under_loss, self.under_dy = 0, None, None      # which lookup the loss, and then dy, belong to
 
     def close(self):
         ard.ard_pattern_destroy(self.pat)
@@ -46,12 +47,12 @@ class TokenEnds:
 
     def embed(self, ids):
         """ids: int32 [rows], negative: padding.  Returns x bf16 [rows][N] (with in_pat compact).  Fewer rows than the batch's, as decoding has them, are taken too;
-        then x has as many."""
+        then x has as many.  x is one buffer, which the first layer reads again on its way back: not between a batch's embed() and its embed_backward()."""
         rows = ids.shape[0]
         if rows > self.rows:
             raise ValueError("ids has %d positions, the model %d" % (rows, self.rows))
         self._check("ids", ids, (rows,), torch.int32)
-        self.ids = ids
+        self.ids, self.lookups = ids, self.lookups + 1
         ard.ard_embedding_fwd(self.ctx, self.in_pat, ard.ARD_BF16, rows, self.V, self.N, self.alpha, ids, self.table, self.N, self.x, self.N)
         return self.x[:rows]
 
@@ -79,7 +80,7 @@ class TokenEnds:
         self.logits(y)
         ard.ard_distill_loss(self.ctx, ard.ARD_BF16, rows, self.V, self.z, self.ldz, labels, k, teacher_ids, teacher_logits, k, tau, hard, soft, row_weight,
                              self.losses, self.total, self.z, self.ldz)
-        self.y = y
+        self.y, self.under_loss = y, self.lookups
         return self.total
 
     def backward(self):
@@ -91,13 +92,17 @@ class TokenEnds:
                                  self.dtable, self.N, 1)
         ard.ard_layer_bwd_data(self.ctx, self.pat, None, ard.ARD_BF16, rows, self.N, self.V, 1.0, self.z, self.ldz, 1, self.table, self.N, None, 0,
                                self.dy, self.N)
+        self.under_dy = self.under_loss
         return self.dy[:rows]
 
     def embed_backward(self, dx):
-        """Behind backward(): dx bf16 [rows][N], the gradient of embed()'s x (with in_pat compact), whose share is added to dtable."""
+        """Behind backward(), once: dx bf16 [rows][N], the gradient of embed()'s x (with in_pat compact), whose share is added to dtable."""
         if self.ids is None:
             raise RuntimeError("embed_backward() before embed()")
         self._check("dx", dx, (self.ids.shape[0], self.N), BF)
+        if self.under_dy != self.lookups:
+            raise RuntimeError("embed_backward() without a backward() of the last embed()'s loss, or a second time")
+        self.under_dy = None
         ard.ard_embedding_bwd(self.ctx, self.in_pat, ard.ARD_BF16, self.ids.shape[0], self.V, self.N, self.alpha, self.ids, dx, self.N, self.dtable, self.N, True)
 
     def adamw_rows(self, weight_decay=0.0, state_bits=32):
