@@ -52,7 +52,9 @@ class DeltaLayer:
         self.Wk = new(N, I, dtype=BF) if in_pat is not None else self.W   # packed over the kept inputs
         self.dWk = new(N, I) if in_pat is not None else self.dW
         self.X = None
-        self.live = None
+        self.live = None                         # of padded batches
+        self.times = torch.arange(T, device="cuda")[:, None]     # (here: what a capture makes is not there before its replay)
+        self.signs = (1 - 2 * (torch.arange(I, device="cuda") % 2)).to(BF)
 
     def close(self):
         ard.ard_pattern_destroy(self.pat)
@@ -89,8 +91,7 @@ class DeltaLayer:
         self._check("lens", lens, (self.B,), torch.int32)
         if lens is not None:      # norm and product run over all rows, whose gradients are zero there: they may not be infinite, or all alike
             if self.live is None:
-                self.live, self.times = torch.empty_like(X), torch.arange(self.T, device=X.device)[:, None]
-                self.signs = (1 - 2 * (torch.arange(self.I, device=X.device) % 2)).to(BF)
+                self.live = torch.empty_like(X)
             torch.where((self.times < lens).view(-1, 1), X, self.signs, out=self.live)
             X = self.live
         self.X, self.lens = X, lens
