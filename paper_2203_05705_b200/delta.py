@@ -40,7 +40,6 @@ class DeltaLayer:
         self.W = self.p_W.to(BF)
         self.dW, self.db, self.dnw, self.dnb = new(N, I), new(N), new(I), new(I)
         self.Xn, self.dXn, self.dX = (new(T * B, I, dtype=BF) for _ in range(3))
-        self.dXs = new(T * B, I)
         self.mean, self.rstd = new(T * B), new(T * B)
         self.ld = -(-N // 8) * 8                 # rows on a grid of 16 bytes
         self.Z, self.dZ = new(T * B, self.ld, dtype=BF), new(T * B, self.ld, dtype=BF)
