@@ -1394,14 +1394,19 @@ __device__ __forceinline__ void dl_load_parts(bf* s, const bf* g, int from, int 
   }
 }
 
-// Lines of 128 bytes on their way to L2: `bytes` from p on, or rows of a chunk.
-__device__ __forceinline__ void dl_ahead(const void* p, long long bytes) {
-  for (long long i = threadIdx.x * 128ll; i < bytes; i += DL_GRAD_THREADS * 128)
-    asm volatile("prefetch.global.L2 [%0];" ::"l"(reinterpret_cast<const uint8_t*>(p) + i));
+// The k-th line of 128 bytes of those that hold `bytes` from p on, on its way to L2.
+__device__ __forceinline__ bool dl_ahead_line(const void* p, long long bytes, long long k) {
+  const uintptr_t from = reinterpret_cast<uintptr_t>(p), at = k == 0 ? from : (from & ~(uintptr_t)127) + 128 * k;
+  if (at >= from + bytes) return false;
+  asm volatile("prefetch.global.L2 [%0];" ::"l"(at));
+  return true;
 }
-__device__ __forceinline__ void dl_ahead_rows(const bf* p, long long step, int live, int cols) {
-  const int r = threadIdx.x >> 3, c = (threadIdx.x & 7) * 64;
-  if (r < live && c < cols) asm volatile("prefetch.global.L2 [%0];" ::"l"(p + r * step + c));
+__device__ __forceinline__ void dl_ahead(const void* p, long long bytes) {
+  for (long long k = threadIdx.x; dl_ahead_line(p, bytes, k); k += DL_GRAD_THREADS) {}
+}
+__device__ __forceinline__ void dl_ahead_rows(const bf* p, long long step, int live, int cols) {  // rows of a chunk, of up to 128 columns
+  const int r = threadIdx.x >> 3;
+  if (r < live) dl_ahead_line(p + r * step, 2ll * cols, threadIdx.x & 7);
 }
 // All that the unit of the CTA after this one on the SM reads, while this one computes: the loads of all SMs together are as fast as memory is, and nothing overlaps
 // them where one CTA fills an SM.
@@ -1415,7 +1420,8 @@ __device__ __forceinline__ void dl_ahead(const DlArgs& a, long long at) {
   dl_ahead_rows(a.V + u.row0 * a.ldv + (long long)u.head * a.Dv, a.B * a.ldv, u.live, a.Dv);
   dl_ahead_rows(a.dY + u.row0 * a.lddy + (long long)u.head * a.Dv, a.B * a.lddy, u.live, a.Dv);
   dl_ahead(a.x + u.unit * 2 * DL_CHUNK * a.ldx, 4ll * DL_CHUNK * a.ldx);
-  dl_ahead(a.d + u.unit * 2 * (a.Dk <= 64 ? 64 : 128) * a.ldx, 4ll * a.Dv * (a.Dk <= 64 ? 64 : 128));
+  const long long dk = a.Dk <= 64 ? 64 : 128;
+  for (int p = 0; p < 2; ++p) dl_ahead(a.d + (u.unit * 2 + p) * dk * a.ldx, 2ll * a.Dv * dk);  // of each part the rows that are read
   dl_ahead(a.tri + u.unit * 3 * DL_SQ, 4ll * DL_SQ);
   dl_ahead(a.row + u.unit * DL_ROW_FLOATS, 4ll * DL_ROW_FLOATS);
 }
