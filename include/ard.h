@@ -754,7 +754,8 @@ ard_status ard_glr_backward(ard_ctx* ctx, const ard_pattern* pat, ard_dtype dtyp
  *         calls, so one piece serves many layers whose calls are ordered.  NULL where that is 0 (decoding).
  * Dk or Dv may be 0: sums over no keys, or for no values, are zero, and so are the gates' gradients.
  * Decoding is T = 1 with hT = h0.  A gate of -infinity (f = 0) starts anew.  Steps are computed ARD_DELTA_CHUNK at a time, so what a NaN or an
- * infinity in a sequence's inputs makes of its own step and later ones it may make of the same chunk's earlier ones too.  Q, K, V, Z, Y are ARD_BF16, from any whole element on (fastest
+ * infinity in a sequence's inputs makes of its own step and later ones it may make of the same chunk's earlier ones too.  Lengths come from sums of squares in
+ * fp32: with eps >= 0, entries of Q and K of at most 2^60, and with eps = 0 of 2^-60 at least or zero.  Q, K, V, Z, Y are ARD_BF16, from any whole element on (fastest
  * with 16-byte aligned pointers and rows, Dk and Dv multiples of 8); gates, states and their products are fp32.  Y must not overlap an input.
  * Errors: ARD_ERR_INVALID_ARG (NULL, negative size, unknown dtype, scale or eps not finite), ARD_ERR_SHAPE (leading dimension too small),
  * ARD_ERR_ALIGNMENT (a pointer inside an element), ARD_ERR_NOMEM (work_bytes too small), ARD_ERR_UNSUPPORTED (ARD_F32, Dk or Dv above 128, T
@@ -841,7 +842,7 @@ ard_status ard_embedding_fwd(ard_ctx* ctx, const ard_pattern* pat, ard_dtype dty
                              const int32_t* ids, const void* table, int ldt, void* Y, int ldy, void* cuda_stream);
 /* Its adjoint:  dtable[v][j] (+)= alpha * sum over r with ids[r] = v of dY[r][j],  dtable fp32 [V][N], full width.  accumulate
  * = 0: all of it is written, tokens that no row holds and dropped units as zero; accumulate != 0: added to what stands there (the output
- * layer's gradient where both share the table), the rest is left.  Sums are fp32 in an order that the sizes fix: the same inputs give the same
+ * layer's gradient where both share the table), the rest is left.  Sums are fp32 in an order that sizes and ids fix: the same inputs give the same
  * bits.  Asynchronous. */
 ard_status ard_embedding_bwd(ard_ctx* ctx, const ard_pattern* pat, ard_dtype dtype, int rows, int V, int N, float alpha,
                              const int32_t* ids, const void* dY, int lddy, float* dtable, int lddt, int accumulate,
@@ -861,7 +862,7 @@ ard_status ard_embedding_bwd(ard_ctx* ctx, const ard_pattern* pat, ard_dtype dty
  *                  take them away), is not read: its loss is 0 and its gradient zeros.
  *   loss           fp32 [rows]; total: fp32 on the device, summed in fp64 in a fixed order, or NULL.
  *   dZ             like Z (lddz), or NULL: not wanted.  May be Z itself, else must not overlap it.
- * Labels and teacher's tokens of V or more count as absent, and the device status becomes ARD_ERR_INVALID_ARG.  Logits of -infinity are classes
+ * Labels and teacher's tokens of V or more count as absent, and the device status becomes ARD_ERR_INVALID_ARG, whatever the row's weight.  Logits of -infinity are classes
  * without probability; a row of nothing else gives NaN.  Z, dZ of element type `dtype`, from any whole element on; sums are fp32.
  * Uses the context's scratch.  Errors: ARD_ERR_INVALID_ARG (NULL, negative size, dtype, tau not positive or not finite, also its inverse, hard or soft not
  * finite), ARD_ERR_SHAPE (leading dimension below V or k), ARD_ERR_ALIGNMENT (a pointer inside an element), ARD_ERR_UNSUPPORTED

@@ -4,7 +4,7 @@
 //
 // Memory bounds it: a row is read once and its gradient written once, 4 bytes an element in bf16; its exponentials, two an element (four where both temperatures
 // are wanted), take seven tenths of that time on the special function units.  So rows stream through a ring in shared memory, filled by bulk copies that one warp
-// asks for, while the others work on what is there, and a row too long for a ring of two is cut over a cluster of CTAs, which exchange a maximum and
+// asks for, while the others work on what is there, and a row too long for a ring of three is cut over a cluster of CTAs, which exchange a maximum and
 // sums once a row.  A third kind of warp does what depends on a few scattered logits: the teacher's softmax for the next row, and for this one the loss and the
 // gradient's entries at the label and the teacher's tokens, which are written once more behind the others.  Each thread keeps the maximum of what it looks at and
 // sums of exponentials relative to it; these pairs meet once a row.  Rows of up to 4096 logits (fp32: 2048) are held by a warp or 8 lanes, in registers.

@@ -6,12 +6,14 @@
 // hand one another the order.  Instead a CTA owns the tokens v = group (mod groups) and at most 128 columns: it looks through all ids (they come from the L2: 4
 // bytes a position where a row of dY has thousands), keeps those that are its own in shared memory, sorts them there (by counting where they are few, else
 // digit by digit, either way with a token's rows in their order), and adds their rows up.  One launch, no scratch, and the same bits every time: each
-// sum is cut at the same places.  Equal shares of the sorted list go to the warps, so a token that comes up in every other position costs no more than any
-// other; tokens are dealt out in turn, so frequent ones, which lie side by side in a dictionary sorted by frequency, fall to different CTAs.  Zeros for
-// tokens that no position holds are written beside the sums, by warps that have nothing to add.
+// sum is cut at the same places.  Equal shares of the sorted list go to the warps, so a frequent token has all warps of its CTA at work, but no other CTA's: with one
+// token in half of 65536 positions, 128 columns take 342 us where tokens that are all alike often take 35.  Tokens are dealt out in turn, so frequent ones, which lie
+// side by side in a dictionary sorted by frequency, fall to different CTAs.  Zeros for tokens that no position holds are written beside the sums, by warps that
+// have nothing to add.
 //
-// 16384 positions, 32000 tokens (all alike often), 2048 columns, bf16: lookup 20.7 us (134 MB), gradient 81 (329 MB: 4.1 TB/s; the list of a CTA, its
-// sort and then its rows follow one another).  700 positions, 8800 tokens, 750 of 1500 columns kept: 4.2 and 18.5, of which 7.4 the 53 MB of the gradient and 4 the start (a CTA has
+// 16384 positions, 32000 tokens, 2048 columns, bf16: lookup 20.6 us with tokens all alike often, 16.5 by falling frequency (5400 of them come up), gradient 81 (329 MB: 4.1
+// TB/s) and 89: the list of a CTA, its sort and then its rows follow one another, and 64 registers a thread with 16 rows in flight spill 340 bytes; fp32 31 to 43, and 96
+// and 109.  700 positions, 8800 tokens, 750 of 1500 columns kept: 4.2 and 18.5, of which 7.4 the 53 MB of the gradient and 4 the start (a CTA has
 // looked at its ids 8000 cycles after it began).
 #include <cooperative_groups.h>
 

@@ -69,7 +69,7 @@ class TokenEnds:
 
     def loss(self, y, labels=None, teacher_ids=None, teacher_logits=None, tau=1.0, hard=1.0, soft=0.0, row_weight=None):
         """The loss of y (kept until backward()) against labels (int32 [rows]) and a teacher's top logits (int32 and fp32 [rows][k]).  Returns total, fp32 [1] on the device; each row's is in
-        losses, and the gradient of the logits takes the logits' place until backward()."""
+        losses[:rows], and the gradient of the logits takes the logits' place until backward()."""
         rows, k = y.shape[0], 0 if teacher_ids is None else teacher_ids.shape[1]
         self._check("labels", labels, (rows,), torch.int32)
         self._check("teacher_ids", teacher_ids, (rows, k), torch.int32)
